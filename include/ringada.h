@@ -291,6 +291,97 @@ ringada_status ringada_head_ce(void* stream, int32_t dtype, const void* y,
 ringada_status ringada_sgd_f32(void* stream, float* w, float* g, int64_t n,
                                float lr);
 
+/* ---------------------------------------------------------------- block operators
+ * Attention and dropout as calls of their own, for blocks that are put together
+ * outside a stage; ringada_stage_set_attention and ringada_stage_set_dropout use
+ * the same kernels inside one. */
+
+/* A [batch, row, head, d_head] tensor: strides in elements, d_head contiguous.
+ * bf16: strides multiples of 8 and data 16-byte aligned; f32: any alignment of a
+ * float. */
+typedef struct {
+  void* data;
+  int64_t batch, row, head;
+} ringada_view;
+
+typedef struct {
+  int32_t dtype;          /* RINGADA_F32 or RINGADA_BF16 */
+  int32_t batch;
+  int32_t n_heads;        /* query heads, a multiple of n_kv_heads: head h reads */
+  int32_t n_kv_heads;     /* key-value head h / (n_heads / n_kv_heads) */
+  int32_t d_head;         /* bf16: 64 or 128; f32: 1 .. 128 */
+  int32_t seq_q, seq_k;   /* rows per sequence in q / o and in k / v */
+  int32_t causal;         /* 1: a query sees no key after its own position */
+  int32_t window;         /* 0: none, else a query sees the keys less than this far away */
+  int32_t sinks;          /* and, with a window, the first so many keys however far */
+  float scale;            /* of q.k, > 0 */
+  int32_t n_buckets;      /* relative position bias: 0 = none, else 1 .. 65535 */
+  int32_t max_distance;   /* R, 0 .. 1024: distances beyond count as R */
+} ringada_attn_desc;
+
+/* Query row i of a sequence with len_q queries and len_k keys stands at position
+ * p = len_k - len_q + i, key row j at j (a new token's query: at the end of its
+ * cache).  With table, bucket[clamp(j - p, -R, R) + R] names the table row whose
+ * entry for the head is added to the score.  A row that sees nothing, and one at or past
+ * its length, gives zeros (and lse -inf).  Rows of k, v and gradients at or past the
+ * lengths are not read into any result, whatever they hold. */
+typedef struct {
+  ringada_view q, k, v;   /* [batch, seq_q, n_heads, d_head]; [batch, seq_k, n_kv_heads, d_head] */
+  ringada_view o;         /* as q: written by the forward, read by the backward */
+  float* lse;             /* [batch, n_heads, seq_q]: base-2 log-sum-exp of the scores, written by the
+                             forward (may be NULL there), read by the backward */
+  const int32_t* len_q;   /* device [batch], NULL: seq_q; values are taken into [0, seq_q] */
+  const int32_t* len_k;   /* device [batch], NULL: seq_k; values are taken into [0, seq_k] */
+  const float* table;     /* device [n_buckets, n_heads]; an entry of -1e30 or less hides its bucket */
+  const int32_t* bucket;  /* device [2 R + 1], values taken into [0, n_buckets) */
+} ringada_attn_tensors;
+
+typedef struct {
+  ringada_view dout;        /* as o */
+  ringada_view dq, dk, dv;  /* as q, k, v; written, zeros at and past the lengths */
+  float* dtable;            /* [n_buckets, n_heads], ADDED into; NULL: the table is frozen */
+} ringada_attn_grads;
+
+/* Host only.  Bytes of the workspaces of one forward and one backward (0: none needed);
+ * with_dtable: whether the backward forms the table's gradient.  Either pointer may be
+ * NULL.  Calls that may run at the same time (other streams, other graphs) take
+ * workspaces of their own. */
+ringada_status ringada_attn_plan(const ringada_attn_desc* desc, int32_t with_dtable,
+                                 size_t* forward_bytes, size_t* backward_bytes);
+
+/* o = softmax(scale q k^T + bias, visible keys) v.  Outputs must not overlap inputs.
+ * Workspaces are 256-byte aligned. */
+ringada_status ringada_attn_forward(void* stream, const ringada_attn_desc* desc,
+                                    const ringada_attn_tensors* t, void* workspace,
+                                    size_t workspace_bytes);
+
+/* Gradients of ringada_attn_forward with the same desc and tensors.  Every sum has
+ * a fixed order: the same inputs give the same bits. */
+ringada_status ringada_attn_backward(void* stream, const ringada_attn_desc* desc,
+                                     const ringada_attn_tensors* t, const ringada_attn_grads* g,
+                                     void* workspace, size_t workspace_bytes);
+
+/* Host only.  Fills map[2 max_distance + 1], indexed by key - query + max_distance, with
+ * the usual buckets of learned relative positions: of the n buckets of a direction
+ * (half of n_buckets each when bidirectional, the keys after the query in the second
+ * half; else all for the keys before it, the keys after it in bucket 0), the first
+ * n / 2 hold one distance each, the others distances spaced evenly in their
+ * logarithm up to max_distance, which is in the last with everything beyond. */
+ringada_status ringada_relpos_buckets(int32_t n_buckets, int32_t max_distance,
+                                      int32_t bidirectional, int32_t* map);
+
+/* y = [res +] dropout(x) over n <= 2^35 contiguous elements of `dtype`: an element is zeroed
+ * with probability p (0 <= p < 1, in steps of 2^-16), else multiplied by 1 / (1 - p).
+ * The mask is a function of (seed, offset, site, element) alone and is stored nowhere:
+ * the backward is the same call on dy, without res.  rng: {seed, offset}, two
+ * uint64 in device memory, read when the kernel runs, so a captured graph takes
+ * a new mask from a new offset; site tells apart the calls that share them.  Element e
+ * takes 16-bit half e % 2 (low first) of word e % 8 / 2 of Philox4x32-10 with key seed
+ * and counter (e / 8, site, offset), and is dropped when that is below 65536 p.  res may be
+ * NULL; y may be x or res; any other overlap returns RINGADA_E_INVALID. */
+ringada_status ringada_dropout(void* stream, int32_t dtype, const void* x, const void* res,
+                               void* y, int64_t n, float p, const uint64_t* rng, uint32_t site);
+
 /* ---------------------------------------------------------------- diagnostics */
 
 /* Thread-local message of the last failing call ("" if none). */

@@ -5,7 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, byref, c_char, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_void_p
+from ctypes import POINTER, byref, c_char, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libringada.so")
@@ -48,6 +48,26 @@ class ProfEntry(ctypes.Structure):
                 ("flops", c_double), ("bytes", c_double)]
 
 
+class View(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("batch", c_int64), ("row", c_int64), ("head", c_int64)]
+
+
+class AttnDesc(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("batch", c_int32), ("n_heads", c_int32), ("n_kv_heads", c_int32),
+                ("d_head", c_int32), ("seq_q", c_int32), ("seq_k", c_int32), ("causal", c_int32),
+                ("window", c_int32), ("sinks", c_int32), ("scale", c_float), ("n_buckets", c_int32),
+                ("max_distance", c_int32)]
+
+
+class AttnTensors(ctypes.Structure):
+    _fields_ = [("q", View), ("k", View), ("v", View), ("o", View), ("lse", c_void_p), ("len_q", c_void_p),
+                ("len_k", c_void_p), ("table", c_void_p), ("bucket", c_void_p)]
+
+
+class AttnGrads(ctypes.Structure):
+    _fields_ = [("dout", View), ("dq", View), ("dk", View), ("dv", View), ("dtable", c_void_p)]
+
+
 # (name, restype, argtypes): every symbol declared in include/ringada.h
 SIGNATURES = [
     ("ringada_stage_plan", c_int32, [POINTER(StageDesc), c_int32, c_int32, c_int32,
@@ -67,6 +87,13 @@ SIGNATURES = [
     ("ringada_head_ce", c_int32, [c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p,
                                   c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     ("ringada_sgd_f32", c_int32, [c_void_p, c_void_p, c_void_p, c_int64, c_float]),
+    ("ringada_attn_plan", c_int32, [POINTER(AttnDesc), c_int32, POINTER(c_size_t), POINTER(c_size_t)]),
+    ("ringada_attn_forward", c_int32, [c_void_p, POINTER(AttnDesc), POINTER(AttnTensors), c_void_p, c_size_t]),
+    ("ringada_attn_backward", c_int32, [c_void_p, POINTER(AttnDesc), POINTER(AttnTensors), POINTER(AttnGrads),
+                                        c_void_p, c_size_t]),
+    ("ringada_relpos_buckets", c_int32, [c_int32, c_int32, c_int32, POINTER(c_int32)]),
+    ("ringada_dropout", c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_float, c_void_p,
+                                  c_uint32]),
     ("ringada_last_error", c_char_p, []),
     ("ringada_prof_begin", c_int32, [c_void_p]),
     ("ringada_prof_end", c_int32, [c_void_p, POINTER(ProfEntry), c_int32, POINTER(c_int32)]),
@@ -169,6 +196,32 @@ def ringada_head_ce(stream, dtype, y, batch, seq, d, w_h, b_h, n_classes, labels
 
 def ringada_sgd_f32(stream, w, g, n, lr):
     _check(lib().ringada_sgd_f32(stream, _p(w), _p(g), n, lr))
+
+
+def ringada_attn_plan(desc, with_dtable):
+    f, b = c_size_t(0), c_size_t(0)
+    _check(lib().ringada_attn_plan(byref(desc), int(with_dtable), byref(f), byref(b)))
+    return f.value, b.value
+
+
+def ringada_attn_forward(stream, desc, tensors, workspace, workspace_bytes):
+    _check(lib().ringada_attn_forward(stream, byref(desc), byref(tensors), _p(workspace), workspace_bytes))
+
+
+def ringada_attn_backward(stream, desc, tensors, grads, workspace, workspace_bytes):
+    _check(lib().ringada_attn_backward(stream, byref(desc), byref(tensors), byref(grads), _p(workspace),
+                                       workspace_bytes))
+
+
+def ringada_relpos_buckets(n_buckets, max_distance, bidirectional):
+    """The map as a list of 2 max_distance + 1 ints, indexed by key - query + max_distance."""
+    m = (c_int32 * max(1, 2 * max_distance + 1))()
+    _check(lib().ringada_relpos_buckets(n_buckets, max_distance, int(bidirectional), m))
+    return list(m)
+
+
+def ringada_dropout(stream, dtype, x, res, y, n, p, rng, site):
+    _check(lib().ringada_dropout(stream, dtype, _p(x), _p(res), _p(y), n, p, _p(rng), site))
 
 
 def ringada_last_error():

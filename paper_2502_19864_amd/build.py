@@ -17,7 +17,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libringada.so")
-SOURCES = ["k_gemm.hip", "k_attention.hip", "k_adapter.hip", "k_misc.hip", "stage.hip"]
+SOURCES = ["k_gemm.hip", "k_attention.hip", "k_attn_masked.hip", "k_adapter.hip", "k_dropout.hip", "k_misc.hip",
+           "operators.hip", "stage.hip"]
 ARCH = "gfx950"
 
 

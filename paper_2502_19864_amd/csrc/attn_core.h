@@ -139,4 +139,81 @@ __device__ __forceinline__ void attn_seq128_wave(bf16* sQ, const bf16* sK, const
   if (half == 0) lse_row[q] = m2 + log2f(rs);
 }
 
+// Fragments (B operand, k = head dim) of one row held by this lane: dims
+// 16s + 8*(lane/32) + v, zero when !valid (src is a valid row even then: the loads are
+// unconditional and issued together, the values masked afterwards).
+template <int DH>
+__device__ __forceinline__ void load_row_frags(const bf16* src, bool valid, int half, bf16x8 f[DH / 16]) {
+#pragma unroll
+  for (int s = 0; s < DH / 16; ++s) f[s] = ld_frag(src + 16 * s + 8 * half);
+#pragma unroll
+  for (int s = 0; s < DH / 16; ++s)
+    if (!valid) f[s] = zero_frag();
+}
+
+// ---------------------------------------------------------------- tiles by DMA
+// A [R x DH] tile goes global -> LDS by DMA, rows unpadded (the DMA writes 1 KB runs):
+// 16-B chunk c of row r sits at c ^ swz(r).  The swizzle has to serve two reads:
+// ld_frag of one chunk of 16 consecutive rows (all sixteen must land on
+// different 16-B slots of the 256 B that one pass of the LDS covers), and the
+// transpose read of four chunks of four consecutive rows (each row on a 64-B
+// group of its own; rows padded by 16 B, as before, put all four on two groups).
+template <int DH>
+__device__ __forceinline__ int swz(int r) {
+  return DH == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+}
+// this wave's DMAs have landed and its LDS reads are done, then everybody's
+__device__ __forceinline__ void tiles_ready() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// Element offsets of this lane's reads in such a tile: row for dims 8*half of row
+// lane%32, tr for perm_frag's transpose read of block 0.  The swizzle is an XOR
+// below the row bits, so other dims are reached by an XOR of their own (16s, 32
+// db) and the rows 8 further down, whose swizzle differs in bit 1 of the chunk, by 16;
+// rows + 16 i are constant offsets.
+template <int DH>
+struct TileRead {
+  int row, tr;
+  __device__ __forceinline__ explicit TileRead(int lane) {
+    const int l32 = lane & 31, half = lane >> 5, g = lane >> 4, r = lane & 15;
+    row = l32 * DH + ((half ^ swz<DH>(l32)) * 8);
+    const int rr = 4 * (g >> 1) + (r >> 2), c = 2 * (g & 1) + ((r & 3) >> 1);
+    tr = rr * DH + ((c ^ swz<DH>(rr)) * 8) + 4 * (r & 1);
+  }
+  // fragment of rows kb*32 + lane%32, dims 16s + 8*half + 0..7
+  __device__ __forceinline__ bf16x8 frag(const bf16* tile, int kb, int s) const {
+    return ld_frag(tile + (row ^ (16 * s)) + kb * 32 * DH);
+  }
+  // the same operand as perm_frag
+  __device__ __forceinline__ bf16x8 perm(const bf16* tile, int db, int kb, int j) const {
+    const bf16* lo = tile + (tr ^ (32 * db)) + (kb * 32 + 16 * j) * DH;
+    const bf16* hi = tile + (tr ^ (32 * db) ^ 16) + (kb * 32 + 16 * j + 8) * DH;
+    const uint2 l = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)lo));
+    const uint2 h = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4i16_ptr)hi));
+    return __builtin_bit_cast(bf16x8, make_uint4(l.x, l.y, h.x, h.y));
+  }
+};
+
+// Causal tiles do unequal work: query tile t of nq takes t + 1 key tiles (the dK/dV
+// pass: key block j takes nq - j query tiles).  At d_h = 128 a workgroup fills its CU,
+// so the CUs take the workgroups in dispatch order as they free up; dispatching the
+// heaviest tiles first (each XCD gets its workgroups in linear-id order, one in eight)
+// keeps the light ones for the end, where the plain order could leave one CU a heavy
+// tile last.  Returns rank 0 for the heaviest tile and the batch-head index; shapes
+// whose workgroups do not split evenly over the XCDs keep xcd_block's order.
+__device__ __forceinline__ void heavy_first(int lin, int nq, int nbh, int& rank, int& bh) {
+  const int n = nq * nbh, P = n / 8;
+  if (n % 8 || P % nq) {
+    const int blk = xcd_block(lin, n);
+    rank = nq - 1 - blk % nq;
+    bh = blk / nq;
+    return;
+  }
+  const int x = lin % 8, o = lin / 8, per = P / nq;  // XCD x, its o-th workgroup
+  rank = o / per;
+  bh = x * per + o % per;
+}
+
 }  // namespace rg

@@ -137,6 +137,12 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+// D[32x32] += A[32x2] * B[2x32] in fp32; lane l supplies A[l%32][l/32] and B[l/32][l%32];
+// D as for mfma32.
+__device__ __forceinline__ f32x16 mfma32_f32(float a, float b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+}
+
 __device__ __forceinline__ bf16x8 ld_frag(const bf16* p) {  // 16 B
   return *reinterpret_cast<const bf16x8*>(p);
 }
@@ -252,6 +258,19 @@ typedef __attribute__((address_space(3))) void* lds_ptr_t;
 // else.
 __device__ __forceinline__ void dma16_m0(const void* gbase, uint32_t voff, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(gbase)
+               : "memory");
+}
+// The base has to be in scalar registers; the compiler may have formed a wave-uniform
+// pointer in vector ones (integer division runs there).
+template <typename T>
+__device__ __forceinline__ const T* uniform_ptr(const T* p) {
+  const uint64_t u = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)u), hi = __builtin_amdgcn_readfirstlane((int)(u >> 32));
+  return reinterpret_cast<const T*>(((uint64_t)hi << 32) | lo);
+}
+// the same with 4 B per lane (lane i lands at the LDS address + 4 i)
+__device__ __forceinline__ void dma4_m0(const void* gbase, uint32_t voff, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(voff), "s"(gbase)
                : "memory");
 }
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {

@@ -1,0 +1,715 @@
+// Attention with a sliding window, first tokens that stay visible (sinks) and a
+// learned relative position bias by buckets; shared key-value heads, padded
+// sequences; forward and backward.
+//
+//   p_i = len_k - len_q + i                       position of query row i
+//   visible(i, j): j < len_k, [j <= p_i,] and [|p_i - j| < window or j < sinks]
+//   x_ij = scale q_i.k_j + table[bucket[clamp(j - p_i, -R, R) + R]][head]
+//   P = softmax of x over the visible keys (a row without any: all zero), O = P V
+//   dP = dO V^T, D_i = sum_j P_ij dP_ij, dS = P (dP - D)
+//   dQ = scale dS K, dK = scale dS^T Q, dV = P^T dO, dtable[t][h] += sum of dS over
+//   the pairs of bucket t
+//
+// One pass over the visible key tiles with the running maximum and sum of the
+// softmax; tiles outside every row's window are never touched, whole tiles inside
+// it take no mask.  The score block is held transposed (one query, or key, per
+// lane) as in k_attention.hip.  The storage types differ in an Ops struct: how a
+// tile gets to LDS, how a score block and a product with the tile's transpose are
+// formed.  bf16 products run on MFMA 32x32x16, P and dS rounded to bf16 on their
+// way into the second product (they are never stored; every sum stays in fp32);
+// fp32 ones on MFMA 32x32x2 in fp32 throughout.
+#include "attn_core.h"
+#include "common.h"
+#include "kernels.h"
+
+namespace rg {
+
+// A table entry at or below this hides its bucket (the type's lowest value and
+// -infinity alike): its pairs are not visible.
+constexpr float kHidden = -1e30f;
+
+// ================================================================ who sees whom
+struct Seq {
+  int lq, lk, off;  // queries, keys, position of query 0
+};
+__device__ __forceinline__ Seq seq_of(const MaskedAttnArgs& a, int b) {
+  Seq s;
+  s.lq = a.len_q ? min(max(a.len_q[b], 0), a.Sq) : a.Sq;
+  s.lk = a.len_k ? min(max(a.len_k[b], 0), a.Sk) : a.Sk;
+  s.off = s.lk - s.lq;
+  return s;
+}
+
+struct Mask {
+  int lk, causal, window, sinks;  // window 0: none
+  __device__ __forceinline__ Mask(const MaskedAttnArgs& a, int lk_)
+      : lk(lk_), causal(a.causal), window(a.window), sinks(a.sinks) {}
+  __device__ __forceinline__ bool pair(int p, int j) const {
+    return j < lk && (!causal || j <= p) && (!window || abs(p - j) < window || j < sinks);
+  }
+  // keys k0 .. k0 + n - 1 against positions plo .. phi: 0 nothing visible, 2 everything, 1 else
+  __device__ __forceinline__ int block(int k0, int n, int plo, int phi) const {
+    const int k1 = k0 + n - 1;
+    if (k0 >= lk || (causal && k0 > phi)) return 0;
+    if (window && k0 >= sinks && (k0 - phi >= window || plo - k1 >= window)) return 0;
+    return k1 < lk && (!causal || k1 <= plo) &&
+                   (!window || k1 < sinks || (phi - k0 < window && k1 - plo < window))
+               ? 2
+               : 1;
+  }
+};
+
+// the tiles of KR keys that positions plo .. phi can see: the sinks' tiles, then
+// the window's
+struct KeyTiles {
+  int nsink, t0, n;
+  __device__ __forceinline__ int at(int i) const { return i < nsink ? i : t0 + i - nsink; }
+};
+template <int KR>
+__device__ __forceinline__ KeyTiles key_tiles(const Mask& m, int plo, int phi) {
+  int hi = m.lk - 1, lo = 0, ns = 0;
+  if (m.causal) hi = min(hi, phi);
+  if (m.window) {
+    if (!m.causal) hi = min(hi, phi + m.window - 1);
+    lo = max(0, plo - m.window + 1);
+    int s = min(m.sinks, m.lk);
+    if (m.causal) s = min(s, phi + 1);
+    ns = s > 0 ? (s + KR - 1) / KR : 0;
+  }
+  KeyTiles t{ns, 0, ns};
+  if (hi >= lo) {
+    t.t0 = lo / KR;
+    t.nsink = min(ns, t.t0);
+    t.n = t.nsink + max(hi / KR, ns - 1) - t.t0 + 1;  // sinks may reach past the window
+  }
+  return t;
+}
+
+// ================================================================ storage types
+// A tile is KR rows of one head in LDS.  dma() brings rows 0 .. KR - 1 from src (rows past
+// `last` read row `last`: what they score is masked); scores() forms the block
+// [32 tile rows][32 own rows] (lane = own row, register r = tile row perm_pos(r)); accum() adds
+// tile^T p to acc (lane = own row, registers = head dims).
+template <int DH_>
+struct OpsBf16 {
+  static constexpr int DH = DH_, KR = 64, TILE = KR * DH, STAGE = 32 * (DH + 8), WAVES = 2;
+  typedef bf16 E;
+  struct Rows {
+    bf16x8 f[DH / 16];
+  };
+  TileRead<DH> rd;
+  __device__ __forceinline__ OpsBf16(int lane, int) : rd(lane) {}
+  static __device__ __forceinline__ void load_rows(Rows& o, const E* row, bool valid, int half, int) {
+    load_row_frags<DH>(row, valid, half, o.f);
+  }
+  static __device__ __forceinline__ float dot(const Rows& x, const Rows& y) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) {
+      float u[8], w[8];
+      unpack_frag(x.f[i], u);
+      unpack_frag(y.f[i], w);
+#pragma unroll
+      for (int v = 0; v < 8; ++v) s += u[v] * w[v];
+    }
+    return s + __shfl_xor(s, 32, 64);
+  }
+  template <int NW>
+  static __device__ __forceinline__ void dma(const E* src, long ld, int last, E* dst, int) {
+    constexpr int CPR = DH / 8, RPI = 64 / CPR;
+    static_assert(KR % (RPI * NW) == 0, "whole DMA instructions per wave");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    src = uniform_ptr(src);
+#pragma unroll
+    for (int i = 0; i < KR / (RPI * NW); ++i) {
+      const int r = (i * NW + wave) * RPI + lane / CPR, c = (lane % CPR) ^ swz<DH>(r);
+      dma16_m0(src, ((uint32_t)min(r, last) * (uint32_t)ld + c * 8) * 2, lds_addr(dst) + (i * NW + wave) * 1024);
+    }
+  }
+  __device__ __forceinline__ void scores(f32x16& st, const E* tile, int kb, const Rows& own) const {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st[r] = 0.f;
+#pragma unroll
+    for (int s = 0; s < DH / 16; ++s) st = mfma32(rd.frag(tile, kb, s), own.f[s], st);
+  }
+  __device__ __forceinline__ void accum(f32x16 (&acc)[DH / 32], const E* tile, int kb, const f32x16& p) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const bf16x8 pf = pack8(p, j);
+#pragma unroll
+      for (int db = 0; db < DH / 32; ++db) acc[db] = mfma32(rd.perm(tile, db, kb, j), pf, acc[db]);
+    }
+  }
+  static __device__ __forceinline__ void store(const f32x16 (&acc)[DH / 32], float scale, int lane, E* stage, E* dst,
+                                               long ld, bool nt, int n, int) {
+    store_rows_staged<DH>(acc, scale, lane >> 5, lane, stage, dst, ld, nt, n);
+  }
+};
+
+// Head dims dh <= DHM; columns dh .. DHM - 1 of a tile repeat column dh - 1 and meet
+// zeros in the own rows.
+template <int DHM>
+struct OpsF32 {
+  static constexpr int DH = DHM, KR = 32, P = DHM + 4, TILE = KR * P, STAGE = 32 * P, WAVES = 1;
+  typedef float E;
+  struct Rows {
+    float f[DHM / 2];  // dims half * DHM / 2 + i
+  };
+  int row, col, half;
+  __device__ __forceinline__ OpsF32(int lane, int) {
+    half = lane >> 5;
+    row = (lane & 31) * P + half * (DHM / 2);
+    col = lane & 31;
+  }
+  static __device__ __forceinline__ void load_rows(Rows& o, const E* src, bool valid, int half, int dh) {
+#pragma unroll
+    for (int i = 0; i < DHM / 2; ++i) o.f[i] = src[min(half * (DHM / 2) + i, dh - 1)];
+#pragma unroll
+    for (int i = 0; i < DHM / 2; ++i)
+      if (!valid || half * (DHM / 2) + i >= dh) o.f[i] = 0.f;
+  }
+  static __device__ __forceinline__ float dot(const Rows& x, const Rows& y) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < DHM / 2; ++i) s = fmaf(x.f[i], y.f[i], s);
+    return s + __shfl_xor(s, 32, 64);
+  }
+  // 4 B per lane: any alignment of the rows will do
+  template <int NW>
+  static __device__ __forceinline__ void dma(const E* src, long ld, int last, E* dst, int dh) {
+    constexpr int CPR = DHM / 64;
+    static_assert(KR * CPR % NW == 0, "whole DMA instructions per wave");
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    src = uniform_ptr(src);
+#pragma unroll
+    for (int i = 0; i < KR * CPR / NW; ++i) {
+      const int n = i * NW + wave, r = n / CPR, c = n % CPR;
+      dma4_m0(src, ((uint32_t)min(r, last) * (uint32_t)ld + min(c * 64 + lane, dh - 1)) * 4,
+              lds_addr(dst) + (r * P + c * 64) * 4);
+    }
+  }
+  __device__ __forceinline__ void scores(f32x16& st, const E* tile, int kb, const Rows& own) const {
+    (void)kb;  // a tile is one block
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st[r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < DHM / 8; ++i) {
+      const float4 t = *reinterpret_cast<const float4*>(tile + row + 4 * i);
+      st = mfma32_f32(t.x, own.f[4 * i], st);
+      st = mfma32_f32(t.y, own.f[4 * i + 1], st);
+      st = mfma32_f32(t.z, own.f[4 * i + 2], st);
+      st = mfma32_f32(t.w, own.f[4 * i + 3], st);
+    }
+  }
+  __device__ __forceinline__ void accum(f32x16 (&acc)[DHM / 32], const E* tile, int kb, const f32x16& p) const {
+    (void)kb;
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int db = 0; db < DHM / 32; ++db)
+        acc[db] = mfma32_f32(tile[perm_pos(r, half) * P + db * 32 + col], p[r], acc[db]);
+  }
+  static __device__ __forceinline__ void store(const f32x16 (&acc)[DHM / 32], float scale, int lane, E* stage, E* dst,
+                                               long ld, bool, int n, int dh) {
+    const int l32 = lane & 31, half = lane >> 5;
+#pragma unroll
+    for (int db = 0; db < DHM / 32; ++db)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = acc[db][4 * g + q] * scale;
+        St<float>::st4(stage + l32 * P, db * 32 + 8 * g + 4 * half, v);
+      }
+    for (int r = 0; r < min(n, 32); ++r)
+#pragma unroll
+      for (int c = 0; c < DHM; c += 64)
+        if (c + lane < dh) dst[r * ld + c + lane] = stage[r * P + c + lane];
+  }
+};
+
+// ================================================================ the bias
+// The bias of one head by relative position, times log2 e, from -R to R.  Beyond R it
+// is constant, so a block past it reads one value.
+__device__ __forceinline__ void load_bias(const MaskedAttnArgs& a, int h, float* dst) {
+  for (int i = threadIdx.x; i < 2 * a.R + 1; i += blockDim.x) {
+    const int t = min(max(a.bucket[i], 0), a.nb - 1);
+    const float v = a.table[(long)t * a.H + h];
+    dst[i] = v <= kHidden ? -INFINITY : v * kLog2e;
+  }
+}
+// x = st * sl2 + bias for a block whose register r has relative position rel0 + sgn * perm_pos(r)
+// in this lane; relmin .. relmax over the wave's block
+template <int SGN>
+__device__ __forceinline__ void add_bias(f32x16& st, float sl2, const float* bias, int R, int rel0, int relmin,
+                                         int relmax, int half) {
+  if (relmin >= R || relmax <= -R) {
+    const float b = bias[relmin >= R ? 2 * R : 0];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st[r] = fmaf(st[r], sl2, b);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int rel = rel0 + SGN * perm_pos(r, half);
+      st[r] = fmaf(st[r], sl2, bias[min(max(rel, -R), R) + R]);
+    }
+  }
+}
+
+// Sums of a 32 x 32 block of dS along its diagonals, added to the wave's own array
+// diag[rel + R]; what is at or beyond +-R goes to this lane's hi / lo.  Lane c gathers, by
+// one lane permutation per register, the value of the query that puts register r's
+// key on diagonal c (key >= query) or c - 32: no two lanes add to one address, and
+// every sum has a fixed order.
+__device__ __forceinline__ void add_diag(const f32x16& ds, int base, int R, float* diag, float& lo, float& hi,
+                                         int lane) {
+  const int half = lane >> 5, c = lane & 31;
+  if (base - 31 >= R || base + 31 <= -R) {
+    float s = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s += ds[r];
+    if (base > 0) hi += s;
+    else lo += s;
+    return;
+  }
+  float pos = 0.f, neg = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int k = perm_pos(r, half);
+    const float w = __shfl(ds[r], 32 * half + ((k - c) & 31), 64);
+    if (c <= k) pos += w;
+    else neg += w;
+  }
+  pos += __shfl_xor(pos, 32, 64);
+  neg += __shfl_xor(neg, 32, 64);
+  const float val = half ? neg : pos;
+  const int rel = base + c - 32 * half;
+  if (rel >= R) hi += val;
+  else if (rel <= -R) lo += val;
+  else diag[rel + R] += val;
+}
+
+// ================================================================ forward
+template <class O, bool BIAS, int NW>
+__global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnArgs a) {
+  typedef typename O::E E;
+  constexpr int DH = O::DH, KR = O::KR, TILE = O::TILE;
+  __shared__ __attribute__((aligned(1024))) E sm[4 * TILE];  // [buffer][K, V]
+  extern __shared__ float sbias[];
+  static_assert(4 * TILE >= NW * O::STAGE, "the O rows fit the tiles' space");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
+  const int nq = (a.Sq + 32 * NW - 1) / (32 * NW);
+  int qb, bh;
+  heavy_first(blockIdx.x, nq, a.B * a.H, qb, bh);
+  qb = nq - 1 - qb;
+  const int b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hkv);
+  const Seq sq = seq_of(a, b);
+  const Mask mask(a, sq.lk);
+  const int qw0 = qb * 32 * NW, q0 = qw0 + wave * 32, q = q0 + l32, p = sq.off + q;
+  const bool qv = q < sq.lq;
+  const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
+  KeyTiles kt{0, 0, 0};
+  if (qw0 < sq.lq) kt = key_tiles<KR>(mask, sq.off + qw0, sq.off + min(qw0 + 32 * NW, sq.lq) - 1);
+  const float sl2 = kLog2e * a.scale;
+  const E* K = static_cast<const E*>(a.k.p) + b * a.k.b + hk * a.k.h;
+  const E* V = static_cast<const E*>(a.v.p) + b * a.v.b + hk * a.v.h;
+  const O ops(lane, a.dh);
+  auto issue = [&](int i) {
+    const int k0 = kt.at(i) * KR, last = sq.lk - 1 - k0;
+    E* dst = sm + (i & 1) * 2 * TILE;
+    O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh);
+    O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh);
+  };
+  if (kt.n > 0) issue(0);
+  typename O::Rows qf;
+  O::load_rows(qf, static_cast<const E*>(a.q.p) + b * a.q.b + (long)(qv ? q : 0) * a.q.t + h * a.q.h, qv, half, a.dh);
+  if (BIAS) load_bias(a, h, sbias);
+
+  f32x16 oacc[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
+  float mrun = -INFINITY, lrun = 0.f;
+
+  for (int i = 0; i < kt.n; ++i) {
+    tiles_ready();
+    if (i + 1 < kt.n) issue(i + 1);
+    const int k0 = kt.at(i) * KR;
+    const int kind = q0 < sq.lq ? mask.block(k0, KR, plo, phi) : 0;
+    if (kind == 0) continue;  // wave-uniform
+    const E* sK = sm + (i & 1) * 2 * TILE;
+    const E* sV = sK + TILE;
+    f32x16 sc[KR / 32];
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < KR / 32; ++kb) {
+      ops.scores(sc[kb], sK, kb, qf);
+      if (BIAS)
+        add_bias<1>(sc[kb], sl2, sbias, a.R, k0 + kb * 32 - p, k0 + kb * 32 - phi, k0 + kb * 32 + 31 - plo, half);
+    }
+    if (kind == 1) {
+#pragma unroll
+      for (int kb = 0; kb < KR / 32; ++kb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!mask.pair(p, k0 + kb * 32 + perm_pos(r, half))) sc[kb][r] = -INFINITY;
+    }
+#pragma unroll
+    for (int kb = 0; kb < KR / 32; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[kb][r]);
+    // without a bias the scale (positive) is folded into the exponent's FMA
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * (BIAS ? 1.f : sl2);
+    const float mnew = fmaxf(mrun, mx);
+    const float mfin = mnew == -INFINITY ? 0.f : mnew;  // nothing visible yet: exp2(-inf - 0) = 0
+    const float alpha = __builtin_amdgcn_exp2f(mrun - mfin);
+    float rs = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KR / 32; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        sc[kb][r] = __builtin_amdgcn_exp2f(BIAS ? sc[kb][r] - mfin : fmaf(sc[kb][r], sl2, -mfin));
+        rs += sc[kb][r];
+      }
+    rs += __shfl_xor(rs, 32, 64);
+    lrun = lrun * alpha + rs;
+    mrun = mnew;
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[d][r] *= alpha;
+#pragma unroll
+    for (int kb = 0; kb < KR / 32; ++kb) ops.accum(oacc, sV, kb, sc[kb]);
+  }
+  tiles_ready();  // the tiles' space now takes the O rows
+  if (q0 >= a.Sq) return;
+  const float inv = qv && lrun > 0.f ? 1.f / lrun : 0.f;
+  O::store(oacc, inv, lane, sm + wave * O::STAGE,
+           static_cast<E*>(a.o.p) + b * a.o.b + (long)q0 * a.o.t + h * a.o.h, a.o.t,
+           stream_out((long)a.B * a.Sq * a.H * DH * (long)sizeof(E)), a.Sq - q0, a.dh);
+  if (a.lse && q < a.Sq && half == 0)
+    a.lse[(long)bh * a.Sq + q] = qv && lrun > 0.f ? mrun + log2f(lrun) : -INFINITY;
+}
+
+// ================================================================ backward
+// exponent offset of a row that sees nothing: exp2(x - inf) = 0
+__device__ __forceinline__ float lse_or_inf(float l) { return l == -INFINITY ? INFINITY : l; }
+
+// One score block of the backward: st = P, dp = dP - D times P (dS), both zero where masked.
+// Registers run over the tile rows (SGN 1: keys, own row = query; SGN -1: queries, own row = key).
+
+// dQ pass (lane = query); writes D.  DTAB: dtable is wanted, and D is formed from
+// P and dP themselves in a first sweep over the tiles: the sums over dS cancel, and a D
+// from the stored (rounded) O would leave an error of that rounding in them.  That sweep
+// is two of the pass's five products.
+template <class O, bool BIAS, bool DTAB, int NW>
+__global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAttnArgs a) {
+  typedef typename O::E E;
+  constexpr int DH = O::DH, KR = O::KR, TILE = O::TILE;
+  __shared__ __attribute__((aligned(1024))) E sm[4 * TILE];  // [buffer][K, V]
+  extern __shared__ float sbias[];                           // bias, then (DTAB) one diagonal array per wave
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
+  const int nq = (a.Sq + 32 * NW - 1) / (32 * NW);
+  int qb, bh;
+  heavy_first(blockIdx.x, nq, a.B * a.H, qb, bh);
+  qb = nq - 1 - qb;
+  const int b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hkv);
+  const Seq sq = seq_of(a, b);
+  const Mask mask(a, sq.lk);
+  const int qw0 = qb * 32 * NW, q0 = qw0 + wave * 32, q = q0 + l32, p = sq.off + q;
+  const bool qv = q < sq.lq;
+  const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
+  KeyTiles kt{0, 0, 0};
+  if (qw0 < sq.lq) kt = key_tiles<KR>(mask, sq.off + qw0, sq.off + min(qw0 + 32 * NW, sq.lq) - 1);
+  const float sl2 = kLog2e * a.scale;
+  const E* K = static_cast<const E*>(a.k.p) + b * a.k.b + hk * a.k.h;
+  const E* V = static_cast<const E*>(a.v.p) + b * a.v.b + hk * a.v.h;
+  const O ops(lane, a.dh);
+  const int nit = DTAB ? 2 * kt.n : kt.n;  // DTAB: the tiles twice
+  auto issue = [&](int i) {
+    const int k0 = kt.at(DTAB && i >= kt.n ? i - kt.n : i) * KR, last = sq.lk - 1 - k0;
+    E* dst = sm + (i & 1) * 2 * TILE;
+    O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh);
+    O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh);
+  };
+  if (nit > 0) issue(0);
+  const long row = qv ? q : 0;
+  typename O::Rows qf, df;
+  O::load_rows(qf, static_cast<const E*>(a.q.p) + b * a.q.b + row * a.q.t + h * a.q.h, qv, half, a.dh);
+  O::load_rows(df, static_cast<const E*>(a.dout.p) + b * a.dout.b + row * a.dout.t + h * a.dout.h, qv, half, a.dh);
+  float dsum = 0.f;
+  if (!DTAB) {
+    typename O::Rows of;
+    O::load_rows(of, static_cast<const E*>(a.o.p) + b * a.o.b + row * a.o.t + h * a.o.h, qv, half, a.dh);
+    dsum = O::dot(of, df);
+  }
+  const float lse = qv ? lse_or_inf(a.lse[(long)bh * a.Sq + row]) : INFINITY;
+  const int W = 2 * a.R + 1;
+  float* diag = sbias + (1 + wave) * W;
+  if (BIAS) load_bias(a, h, sbias);
+  if (DTAB)
+    for (int i = lane; i < W; i += 64) diag[i] = 0.f;
+  float dlo = 0.f, dhi = 0.f;
+
+  f32x16 dq[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dq[i][r] = 0.f;
+
+  for (int i = 0; i < nit; ++i) {
+    tiles_ready();
+    if (i + 1 < nit) issue(i + 1);
+    if (q0 >= sq.lq) continue;
+    const bool first = DTAB && i < kt.n;
+    if (DTAB && i == kt.n) dsum += __shfl_xor(dsum, 32, 64);
+    const E* sK = sm + (i & 1) * 2 * TILE;
+    const E* sV = sK + TILE;
+    // one key block at a time (not unrolled): keeps the kernel within its registers
+#pragma unroll 1
+    for (int kb = 0; kb < KR / 32; ++kb) {
+      const int k0 = kt.at(DTAB && i >= kt.n ? i - kt.n : i) * KR + kb * 32;
+      const int kind = mask.block(k0, 32, plo, phi);
+      if (kind == 0) continue;  // wave-uniform
+      const bool full = kind == 2 && q0 + 32 <= sq.lq;
+      f32x16 st, dp;
+      ops.scores(st, sK, kb, qf);
+      ops.scores(dp, sV, kb, df);
+      if (BIAS) add_bias<1>(st, sl2, sbias, a.R, k0 - p, k0 - phi, k0 + 31 - plo, half);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const bool ok = full || (qv && mask.pair(p, k0 + perm_pos(r, half)));
+        const float e = __builtin_amdgcn_exp2f(BIAS ? st[r] - lse : fmaf(st[r], sl2, -lse));
+        st[r] = ok ? e : 0.f;
+      }
+      if (first) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dsum = fmaf(st[r], dp[r], dsum);
+        continue;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[r] *= dp[r] - dsum;  // dS
+      if (DTAB) add_diag(st, k0 - sq.off - q0, a.R, diag, dlo, dhi, lane);
+      ops.accum(dq, sK, kb, st);
+    }
+  }
+  if (qv && half == 0) a.dsum[(long)bh * a.Sq + q] = dsum;
+  if (DTAB) {
+    dlo = wave_sum(dlo);
+    dhi = wave_sum(dhi);
+    if (lane == 0) {
+      diag[0] += dlo;
+      diag[W - 1] += dhi;
+    }
+  }
+  tiles_ready();  // the tiles' space now takes the dQ rows
+  if (DTAB) {
+    float* out = a.diag + ((long)(b * nq + qb) * a.H + h) * W;
+    for (int i = threadIdx.x; i < W; i += 64 * NW) {
+      float s = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) s += sbias[(1 + w) * W + i];
+      out[i] = s;
+    }
+  }
+  if (q0 >= a.Sq) return;
+  O::store(dq, a.scale, lane, sm + wave * O::STAGE,
+           static_cast<E*>(a.dq.p) + b * a.dq.b + (long)q0 * a.dq.t + h * a.dq.h, a.dq.t,
+           stream_out((long)a.B * a.Sq * a.H * DH * (long)sizeof(E)), a.Sq - q0, a.dh);
+}
+
+// dK/dV pass (lane = key): the query heads of the key's group one after another
+template <class O, bool BIAS, int NW>
+__global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(MaskedAttnArgs a) {
+  typedef typename O::E E;
+  constexpr int DH = O::DH, KR = O::KR, TILE = O::TILE;
+  __shared__ __attribute__((aligned(1024))) E sm[4 * TILE];  // [buffer][Q, dO]
+  __shared__ __attribute__((aligned(16))) float sL[2][KR], sD[2][KR];
+  extern __shared__ float sbias[];  // two heads' bias
+  static_assert(KR <= 64 * NW, "one row statistic per thread");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
+  const int nk = (a.Sk + 32 * NW - 1) / (32 * NW), grp = a.H / a.Hkv;
+  int kb0, bh;
+  heavy_first(blockIdx.x, nk, a.B * a.Hkv, kb0, bh);  // causal: the first block has the most queries
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  const Seq sq = seq_of(a, b);
+  const Mask mask(a, sq.lk);
+  const int kw0 = kb0 * 32 * NW, k0 = kw0 + wave * 32, key = k0 + l32;
+  const bool kv = key < sq.lk;
+  // the queries that see any of this workgroup's keys
+  int qlo = 0, qhi = -1;
+  if (kw0 < sq.lk) {
+    const int kw1 = min(kw0 + 32 * NW, sq.lk) - 1;
+    qhi = sq.lq - 1;
+    if (a.causal) qlo = max(0, kw0 - sq.off);
+    if (a.window && kw0 >= a.sinks) {
+      qhi = min(qhi, kw1 + a.window - 1 - sq.off);
+      if (!a.causal) qlo = max(0, kw0 - a.window + 1 - sq.off);
+    }
+  }
+  const int qt0 = qlo / KR, nt = qhi >= qlo ? qhi / KR - qt0 + 1 : 0, nit = nt * grp;
+  const float sl2 = kLog2e * a.scale;
+  const int W = 2 * a.R + 1;
+  const O ops(lane, a.dh);
+  auto issue = [&](int i) {
+    const int h = hk * grp + i / nt, r0 = (qt0 + i % nt) * KR, last = sq.lq - 1 - r0;
+    E* dst = sm + (i & 1) * 2 * TILE;
+    O::template dma<NW>(static_cast<const E*>(a.q.p) + b * a.q.b + h * a.q.h + (long)r0 * a.q.t, a.q.t, last, dst, a.dh);
+    O::template dma<NW>(static_cast<const E*>(a.dout.p) + b * a.dout.b + h * a.dout.h + (long)r0 * a.dout.t, a.dout.t,
+                        last, dst + TILE, a.dh);
+  };
+  // the row statistics of iteration i, one query per thread of the first KR
+  auto load_stats = [&](int i, float& lv, float& dv) {
+    lv = dv = 0.f;
+    if (threadIdx.x < KR) {
+      const long at = ((long)b * a.H + hk * grp + i / nt) * a.Sq + min((qt0 + i % nt) * KR + (int)threadIdx.x, sq.lq - 1);
+      lv = lse_or_inf(a.lse[at]);
+      dv = a.dsum[at];
+    }
+  };
+  auto put_stats = [&](int i, float lv, float dv) {
+    if (threadIdx.x < KR) {
+      sL[i & 1][threadIdx.x] = lv;
+      sD[i & 1][threadIdx.x] = dv;
+    }
+  };
+  float lnext = 0.f, dnext = 0.f;
+  if (nit > 0) {
+    issue(0);
+    load_stats(0, lnext, dnext);
+    if (BIAS) load_bias(a, hk * grp, sbias);
+  }
+  typename O::Rows kf, vf;
+  const long row = kv ? key : 0;
+  O::load_rows(kf, static_cast<const E*>(a.k.p) + b * a.k.b + row * a.k.t + hk * a.k.h, kv, half, a.dh);
+  O::load_rows(vf, static_cast<const E*>(a.v.p) + b * a.v.b + row * a.v.t + hk * a.v.h, kv, half, a.dh);
+  f32x16 dk[DH / 32], dv[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dk[i][r] = dv[i][r] = 0.f;
+  if (nit > 0) put_stats(0, lnext, dnext);
+
+  for (int i = 0; i < nit; ++i) {
+    tiles_ready();
+    if (i + 1 < nit) {
+      load_stats(i + 1, lnext, dnext);
+      issue(i + 1);
+      // the next head's bias goes where the last head's was: read for the last time before this barrier
+      if (BIAS && (i + 1) % nt == 0) load_bias(a, hk * grp + (i + 1) / nt, sbias + ((i + 1) / nt & 1) * W);
+    }
+    const E* sQ = sm + (i & 1) * 2 * TILE;
+    const E* sO = sQ + TILE;
+    const float* pL = sL[i & 1];
+    const float* pD = sD[i & 1];
+    const float* bias = sbias + (i / nt & 1) * W;
+#pragma unroll 1
+    for (int qb = 0; qb < KR / 32; ++qb) {
+      const int q0 = (qt0 + i % nt) * KR + qb * 32;
+      if (q0 >= sq.lq || k0 >= sq.lk) break;  // wave-uniform
+      const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
+      const int kind = mask.block(k0, 32, plo, phi);
+      if (kind == 0) continue;
+      const bool full = kind == 2 && q0 + 32 <= sq.lq;
+      f32x16 st, dp;
+      ops.scores(st, sQ, qb, kf);
+      ops.scores(dp, sO, qb, vf);
+      if (BIAS) add_bias<-1>(st, sl2, bias, a.R, key - plo, k0 - phi, k0 + 31 - plo, half);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {  // queries q0 + 8g + 4*half + 0..3
+        const float4 L = *reinterpret_cast<const float4*>(pL + qb * 32 + 8 * g + 4 * half);
+        const float4 D = *reinterpret_cast<const float4*>(pD + qb * 32 + 8 * g + 4 * half);
+        const float lv[4] = {L.x, L.y, L.z, L.w}, sv[4] = {D.x, D.y, D.z, D.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = 4 * g + e, qq = q0 + 8 * g + 4 * half + e;
+          const bool ok = full || (qq < sq.lq && mask.pair(sq.off + qq, key));
+          const float x = __builtin_amdgcn_exp2f(BIAS ? st[r] - lv[e] : fmaf(st[r], sl2, -lv[e]));
+          st[r] = ok ? x : 0.f;
+          dp[r] = st[r] * (dp[r] - sv[e]);  // dS
+        }
+      }
+      ops.accum(dv, sO, qb, st);
+      ops.accum(dk, sQ, qb, dp);
+    }
+    if (i + 1 < nit) put_stats(i + 1, lnext, dnext);  // the other buffer: last read before this tile's barrier
+  }
+  tiles_ready();  // the tiles' space now takes the dK, then the dV rows
+  if (k0 >= a.Sk) return;
+  E* stage = sm + wave * O::STAGE;
+  const bool nt_out = stream_out((long)a.B * a.Sk * a.Hkv * DH * (long)sizeof(E));
+  O::store(dk, a.scale, lane, stage, static_cast<E*>(a.dk.p) + b * a.dk.b + (long)k0 * a.dk.t + hk * a.dk.h, a.dk.t,
+           nt_out, a.Sk - k0, a.dh);
+  O::store(dv, 1.f, lane, stage, static_cast<E*>(a.dv.p) + b * a.dv.b + (long)k0 * a.dv.t + hk * a.dv.h, a.dv.t,
+           nt_out, a.Sk - k0, a.dh);
+}
+
+// dtable[t][h] += the diagonals' sums of bucket t, over every workgroup's row of partial
+// sums.  One workgroup per (bucket, head); the order is fixed.
+__global__ __launch_bounds__(256) void attn_bias_grad(MaskedAttnArgs a, int rows) {
+  __shared__ double part[4];
+  const int t = blockIdx.x, h = blockIdx.y, W = 2 * a.R + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double s = 0.0;
+  for (int i = 0; i < W; ++i) {
+    if (min(max(a.bucket[i], 0), a.nb - 1) != t) continue;
+    for (int r = threadIdx.x; r < rows; r += 256) s += (double)a.diag[((long)r * a.H + h) * W + i];
+  }
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (lane == 0) part[wave] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) a.dtable[(long)t * a.H + h] += (float)(part[0] + part[1] + part[2] + part[3]);
+}
+
+// ================================================================ launchers
+constexpr int MA_NW = 4;
+
+static long blocks_of(int n) { return (n + 32 * MA_NW - 1) / (32 * MA_NW); }
+
+static size_t dsum_bytes(const MaskedAttnArgs& a) { return ((size_t)a.B * a.H * a.Sq * 4 + 255) & ~(size_t)255; }
+
+void masked_attn_bytes(int dtype, const MaskedAttnArgs& a, bool dtable, size_t* fwd, size_t* bwd) {
+  *fwd = 0;
+  *bwd = dsum_bytes(a);
+  if (dtable) *bwd += (size_t)a.B * blocks_of(a.Sq) * a.H * (2 * a.R + 1) * 4;
+}
+
+void masked_attn_workspace(MaskedAttnArgs& a, void* ws) {
+  a.dsum = static_cast<float*>(ws);
+  a.diag = reinterpret_cast<float*>(static_cast<char*>(ws) + dsum_bytes(a));
+}
+
+template <class O>
+static hipError_t fwd_ops(const MaskedAttnArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(blocks_of(a.Sq) * a.B * a.H)), block(64 * MA_NW);
+  if (a.table) RG_LAUNCH((attn_masked_fwd<O, true, MA_NW>), grid, block, (2 * a.R + 1) * 4, s, a);
+  else RG_LAUNCH((attn_masked_fwd<O, false, MA_NW>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+template <class O>
+static hipError_t bwd_ops(const MaskedAttnArgs& a, hipStream_t s) {
+  const dim3 gq((unsigned)(blocks_of(a.Sq) * a.B * a.H)), gk((unsigned)(blocks_of(a.Sk) * a.B * a.Hkv)), block(64 * MA_NW);
+  const unsigned W = (2 * a.R + 1) * 4;
+  if (a.table) {
+    if (a.dtable) RG_LAUNCH((attn_masked_bwd_dq<O, true, true, MA_NW>), gq, block, (1 + MA_NW) * W, s, a);
+    else RG_LAUNCH((attn_masked_bwd_dq<O, true, false, MA_NW>), gq, block, W, s, a);
+    RG_LAUNCH((attn_masked_bwd_dkdv<O, true, MA_NW>), gk, block, 2 * W, s, a);
+    if (a.dtable)
+      RG_LAUNCH(attn_bias_grad, dim3(a.nb, a.H), dim3(256), 0, s, a, (int)(a.B * blocks_of(a.Sq)));
+  } else {
+    RG_LAUNCH((attn_masked_bwd_dq<O, false, false, MA_NW>), gq, block, 0, s, a);
+    RG_LAUNCH((attn_masked_bwd_dkdv<O, false, MA_NW>), gk, block, 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_masked_attn_fwd(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
+  if (dtype == DT_BF16) return a.dh == 64 ? fwd_ops<OpsBf16<64>>(a, s) : fwd_ops<OpsBf16<128>>(a, s);
+  return a.dh <= 64 ? fwd_ops<OpsF32<64>>(a, s) : fwd_ops<OpsF32<128>>(a, s);
+}
+hipError_t launch_masked_attn_bwd(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
+  if (dtype == DT_BF16) return a.dh == 64 ? bwd_ops<OpsBf16<64>>(a, s) : bwd_ops<OpsBf16<128>>(a, s);
+  return a.dh <= 64 ? bwd_ops<OpsF32<64>>(a, s) : bwd_ops<OpsF32<128>>(a, s);
+}
+
+}  // namespace rg

@@ -81,6 +81,36 @@ struct AttnArgs {
 hipError_t launch_attn_fwd(int dtype, const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_bwd(int dtype, const AttnArgs& a, hipStream_t s);
 
+// Attention with a sliding window, sinks and a relative position bias (k_attn_masked.hip has
+// the formulas).  Element (b, row, head, i) of a view is p[b * b + row * t + head * h + i].
+struct View {
+  void* p;
+  long b, t, h;
+};
+struct MaskedAttnArgs {
+  int B, H, Hkv, dh, Sq, Sk;
+  int causal, window, sinks;  // window 0: none
+  float scale;                // > 0
+  View q, k, v, o;
+  float* lse;                 // [B, H, Sq], base 2 (-inf: the row sees nothing); the forward may go without
+  const int* len_q;           // [B] or null: valid rows per sequence, taken into [0, Sq]
+  const int* len_k;
+  const float* table;         // [nb, H] or null: no bias
+  const int* bucket;          // [2R + 1], taken into [0, nb)
+  int R, nb;
+  // backward
+  View dout, dq, dk, dv;
+  float* dtable;              // [nb, H] or null, added into
+  float* dsum;                // workspace: D [B, H, Sq]
+  float* diag;                // workspace (dtable): sums of dS by relative position, per workgroup of the dQ pass
+  float* part;                // workspace of the forward
+};
+// bytes of the workspaces, and the backward's pointers into its own
+void masked_attn_bytes(int dtype, const MaskedAttnArgs& a, bool dtable, size_t* fwd, size_t* bwd);
+void masked_attn_workspace(MaskedAttnArgs& a, void* ws);
+hipError_t launch_masked_attn_fwd(int dtype, const MaskedAttnArgs& a, hipStream_t s);
+hipError_t launch_masked_attn_bwd(int dtype, const MaskedAttnArgs& a, hipStream_t s);
+
 // ---------------------------------------------------------------- adapters (Eq. (1)) fused with the residual add and the norm
 enum class Norm { LN, RMS, None };
 struct AdapterFwdArgs {
@@ -201,6 +231,14 @@ hipError_t launch_adapter_sgd(int dtype, const AdapterSlot* slots, int n_slots, 
 // refresh working copies only
 hipError_t launch_adapter_sync(int dtype, const AdapterSlot* slots, int n_slots, int d, int m,
                                hipStream_t s);
+
+// ---------------------------------------------------------------- dropout
+// y = [res +] x, elements whose 16 random bits are below thr dropped, the others times
+// 65536 / (65536 - thr); rng: {seed, offset} in device memory; y may be x or res
+// 65536 p, rounded
+inline uint32_t dropout_threshold(float p) { return (uint32_t)(65536.0 * (double)p + 0.5); }
+hipError_t launch_dropout(int dtype, const void* x, const void* res, void* y, long n, uint32_t thr,
+                          const uint64_t* rng, uint32_t site, hipStream_t s);
 
 // ---------------------------------------------------------------- losses
 // whether dY overlaps the inputs in no other way than the losses can take

@@ -1,0 +1,205 @@
+// The block operators behind the C ABI: attention with a window, sinks and a relative
+// position bias, and dropout.  Argument checks and the kernels' argument
+// structs; nothing here allocates or keeps anything.
+#include <math.h>
+
+#include <utility>
+
+#include "kernels.h"
+#include "ringada.h"
+#include "status.h"
+
+using namespace rg;
+
+static constexpr int MAX_R = 1024;
+
+static ringada_status check_attn(const ringada_attn_desc* D) {
+  if (!D) return fail(RINGADA_E_INVALID, "desc is NULL");
+  if (D->dtype != RINGADA_F32 && D->dtype != RINGADA_BF16) return fail(RINGADA_E_INVALID, "unknown dtype %d", D->dtype);
+  if (D->batch < 1 || D->n_heads < 1 || D->n_kv_heads < 1 || D->d_head < 1 || D->seq_q < 1 || D->seq_k < 1)
+    return fail(RINGADA_E_INVALID, "sizes must be positive");
+  if (D->n_heads % D->n_kv_heads) return fail(RINGADA_E_INVALID, "n_heads %% n_kv_heads != 0");
+  if (D->window < 0 || D->sinks < 0) return fail(RINGADA_E_INVALID, "window and sinks must be >= 0");
+  if (!(D->scale > 0.f) || !isfinite(D->scale)) return fail(RINGADA_E_INVALID, "scale must be positive and finite");
+  if (D->n_buckets < 0 || D->n_buckets > 65535 || D->max_distance < 0)
+    return fail(RINGADA_E_INVALID, "n_buckets must be in [0, 65535] and max_distance >= 0");
+  if (D->max_distance > MAX_R) return fail(RINGADA_E_UNSUPPORTED, "max_distance above %d", MAX_R);
+  if (D->dtype == RINGADA_BF16 && D->d_head != 64 && D->d_head != 128)
+    return fail(RINGADA_E_UNSUPPORTED, "bf16 path: d_head must be 64 or 128 (got %d)", D->d_head);
+  if (D->d_head > 128) return fail(RINGADA_E_UNSUPPORTED, "f32 path: d_head must be at most 128 (got %d)", D->d_head);
+  if (D->seq_q > (1 << 24) || D->seq_k > (1 << 24)) return fail(RINGADA_E_UNSUPPORTED, "sequences above 2^24 rows");
+  const int64_t rows = D->seq_q > D->seq_k ? D->seq_q : D->seq_k;
+  if ((int64_t)D->batch * D->n_heads * ((rows + 31) / 32) >= (1ll << 31) || D->n_heads > 65535)
+    return fail(RINGADA_E_UNSUPPORTED, "too many rows for one launch");
+  return RINGADA_OK;
+}
+
+static MaskedAttnArgs attn_sizes(const ringada_attn_desc& D) {
+  MaskedAttnArgs a{};
+  a.B = D.batch; a.H = D.n_heads; a.Hkv = D.n_kv_heads; a.dh = D.d_head; a.Sq = D.seq_q; a.Sk = D.seq_k;
+  a.causal = D.causal != 0;
+  // no two rows are seq_q + seq_k apart: such a window hides nothing
+  a.window = D.window >= D.seq_q + D.seq_k ? 0 : D.window;
+  a.sinks = D.sinks < D.seq_k ? D.sinks : D.seq_k;
+  a.scale = D.scale;
+  a.R = D.n_buckets ? D.max_distance : 0;
+  a.nb = D.n_buckets;
+  return a;
+}
+
+// writes: no two elements of the view may share an address
+static ringada_status check_view(const ringada_attn_desc& D, const char* name, const ringada_view& v, int64_t rows,
+                                 int64_t heads, bool writes, View& out) {
+  if (!v.data) return fail(RINGADA_E_INVALID, "%s is NULL", name);
+  const uintptr_t p = reinterpret_cast<uintptr_t>(v.data);
+  int64_t stride[3] = {v.batch, v.row, v.head}, n[3] = {D.batch, rows, heads};
+  for (int i = 0; i < 3; ++i)
+    if (stride[i] < 0 || stride[i] >= (1ll << 40)) return fail(RINGADA_E_INVALID, "%s: stride out of range", name);
+  if (D.dtype == RINGADA_BF16 ? ((p & 15u) || ((v.batch | v.row | v.head) & 7)) : (p & 3u))
+    return fail(RINGADA_E_INVALID, "%s: bf16 views need 16-byte aligned data and strides that are multiples of 8, "
+                                   "f32 views 4-byte aligned data", name);
+  if (v.row >= (1 << 24)) return fail(RINGADA_E_UNSUPPORTED, "%s: row stride above 2^24 elements", name);
+  if (writes) {
+    for (int i = 0; i < 2; ++i)  // by stride, smallest first
+      for (int j = 0; j < 2 - i; ++j)
+        if (stride[j] > stride[j + 1]) {
+          std::swap(stride[j], stride[j + 1]);
+          std::swap(n[j], n[j + 1]);
+        }
+    int64_t extent = D.d_head;
+    for (int i = 0; i < 3; ++i) {
+      if (n[i] == 1) continue;
+      if (stride[i] < extent) return fail(RINGADA_E_INVALID, "%s: rows of an output overlap", name);
+      extent = stride[i] * (n[i] - 1) + extent;
+    }
+  }
+  out = View{v.data, (long)v.batch, (long)v.row, (long)v.head};
+  return RINGADA_OK;
+}
+
+static ringada_status fill_tensors(const ringada_attn_desc& D, const ringada_attn_tensors* t, MaskedAttnArgs& a) {
+  if (!t) return fail(RINGADA_E_INVALID, "tensors is NULL");
+  RG_TRY(check_view(D, "q", t->q, D.seq_q, D.n_heads, false, a.q));
+  RG_TRY(check_view(D, "k", t->k, D.seq_k, D.n_kv_heads, false, a.k));
+  RG_TRY(check_view(D, "v", t->v, D.seq_k, D.n_kv_heads, false, a.v));
+  RG_TRY(check_view(D, "o", t->o, D.seq_q, D.n_heads, true, a.o));
+  if (t->o.data == t->q.data || t->o.data == t->k.data || t->o.data == t->v.data)
+    return fail(RINGADA_E_INVALID, "o is one of the inputs");
+  if ((t->table != nullptr) != (D.n_buckets > 0) || (t->table && !t->bucket))
+    return fail(RINGADA_E_INVALID, "table and bucket must be given exactly when n_buckets > 0");
+  a.lse = t->lse;
+  a.len_q = t->len_q;
+  a.len_k = t->len_k;
+  a.table = t->table;
+  a.bucket = t->bucket;
+  return RINGADA_OK;
+}
+
+static ringada_status check_workspace(const void* ws, size_t have, size_t need) {
+  if (have < need || (need && !ws))
+    return fail(RINGADA_E_WORKSPACE, "workspace of %zu bytes, the call needs %zu", ws ? have : (size_t)0, need);
+  if (need && (reinterpret_cast<uintptr_t>(ws) & 255u)) return fail(RINGADA_E_INVALID, "workspace must be 256-byte aligned");
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_attn_plan(const ringada_attn_desc* desc, int32_t with_dtable, size_t* forward_bytes,
+                                            size_t* backward_bytes) {
+  RG_TRY(check_attn(desc));
+  size_t f, b;
+  masked_attn_bytes(desc->dtype, attn_sizes(*desc), with_dtable && desc->n_buckets, &f, &b);
+  if (forward_bytes) *forward_bytes = f;
+  if (backward_bytes) *backward_bytes = b;
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_attn_forward(void* stream, const ringada_attn_desc* desc,
+                                               const ringada_attn_tensors* t, void* workspace,
+                                               size_t workspace_bytes) {
+  RG_TRY(check_attn(desc));
+  MaskedAttnArgs a = attn_sizes(*desc);
+  RG_TRY(fill_tensors(*desc, t, a));
+  size_t need, unused;
+  masked_attn_bytes(desc->dtype, a, false, &need, &unused);
+  RG_TRY(check_workspace(workspace, workspace_bytes, need));
+  a.part = static_cast<float*>(workspace);
+  RG_HIP(launch_masked_attn_fwd(desc->dtype, a, static_cast<hipStream_t>(stream)));
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_attn_backward(void* stream, const ringada_attn_desc* desc,
+                                                const ringada_attn_tensors* t, const ringada_attn_grads* g,
+                                                void* workspace, size_t workspace_bytes) {
+  RG_TRY(check_attn(desc));
+  MaskedAttnArgs a = attn_sizes(*desc);
+  RG_TRY(fill_tensors(*desc, t, a));
+  if (!g) return fail(RINGADA_E_INVALID, "grads is NULL");
+  if (!t->lse) return fail(RINGADA_E_INVALID, "the backward needs the forward's lse");
+  RG_TRY(check_view(*desc, "dout", g->dout, desc->seq_q, desc->n_heads, false, a.dout));
+  RG_TRY(check_view(*desc, "dq", g->dq, desc->seq_q, desc->n_heads, true, a.dq));
+  RG_TRY(check_view(*desc, "dk", g->dk, desc->seq_k, desc->n_kv_heads, true, a.dk));
+  RG_TRY(check_view(*desc, "dv", g->dv, desc->seq_k, desc->n_kv_heads, true, a.dv));
+  const void* outs[3] = {g->dq.data, g->dk.data, g->dv.data};
+  const void* ins[5] = {t->q.data, t->k.data, t->v.data, t->o.data, g->dout.data};
+  for (int i = 0; i < 3; ++i) {
+    for (const void* in : ins)
+      if (outs[i] == in) return fail(RINGADA_E_INVALID, "a gradient is one of the inputs");
+    if (outs[i] == outs[(i + 1) % 3]) return fail(RINGADA_E_INVALID, "two gradients are one tensor");
+  }
+  if (g->dtable && !desc->n_buckets) return fail(RINGADA_E_INVALID, "dtable without a table");
+  a.dtable = g->dtable;
+  size_t need, unused;
+  masked_attn_bytes(desc->dtype, a, g->dtable != nullptr, &unused, &need);
+  RG_TRY(check_workspace(workspace, workspace_bytes, need));
+  masked_attn_workspace(a, workspace);
+  RG_HIP(launch_masked_attn_bwd(desc->dtype, a, static_cast<hipStream_t>(stream)));
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_relpos_buckets(int32_t n_buckets, int32_t max_distance, int32_t bidirectional,
+                                                 int32_t* map) {
+  if (!map) return fail(RINGADA_E_INVALID, "map is NULL");
+  const int n = bidirectional ? n_buckets / 2 : n_buckets, one = n / 2;
+  if (n_buckets < 2 || (bidirectional && n_buckets % 2) || one < 1)
+    return fail(RINGADA_E_INVALID, "n_buckets must be at least 2, or a multiple of 2 from 4 when bidirectional");
+  if (max_distance <= one || max_distance > MAX_R)
+    return fail(RINGADA_E_INVALID, "max_distance must be in (%d, %d]", one, MAX_R);
+  for (int r = -max_distance; r <= max_distance; ++r) {
+    const int d = bidirectional ? (r < 0 ? -r : r) : (r < 0 ? -r : 0);
+    int t = d;
+    if (d >= one) {
+      // one + k for the largest k with d >= one (max_distance / one)^(k / (n - one)); where that
+      // power is a whole number the long double power is off by far less than 1e-9 of it, and
+      // where it is not, no whole number up to 1024 is that near
+      int k = 0;
+      while (k < n - one &&
+             (long double)d * (1 + 1e-9L) >= one * powl((long double)max_distance / one, (k + 1) / (long double)(n - one)))
+        ++k;
+      t = one + k < n ? one + k : n - 1;
+    }
+    map[r + max_distance] = t + (bidirectional && r > 0 ? n : 0);
+  }
+  return RINGADA_OK;
+}
+
+// ================================================================ dropout
+static bool same_or_apart(const void* a, const void* b, size_t n) {
+  const char* x = static_cast<const char*>(a);
+  const char* y = static_cast<const char*>(b);
+  return x == y || x + n <= y || y + n <= x;
+}
+
+extern "C" ringada_status ringada_dropout(void* stream, int32_t dtype, const void* x, const void* res, void* y,
+                                          int64_t n, float p, const uint64_t* rng, uint32_t site) {
+  if (dtype != RINGADA_F32 && dtype != RINGADA_BF16) return fail(RINGADA_E_INVALID, "unknown dtype");
+  if (!x || !y || !rng || n <= 0 || n > (1ll << 35)) return fail(RINGADA_E_INVALID, "bad argument");
+  if (!(p >= 0.f && p < 1.f)) return fail(RINGADA_E_INVALID, "p must be in [0, 1)");
+  const uint32_t thr = dropout_threshold(p);
+  if (thr > 65535) return fail(RINGADA_E_INVALID, "p rounds to 1 in steps of 2^-16");
+  const size_t es = dtype == RINGADA_BF16 ? 2 : 4, bytes = (size_t)n * es;
+  const uintptr_t all = reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(res) | reinterpret_cast<uintptr_t>(y);
+  if ((all & (es - 1)) || (reinterpret_cast<uintptr_t>(rng) & 7u)) return fail(RINGADA_E_INVALID, "misaligned tensor");
+  if (!same_or_apart(x, y, bytes) || (res && !same_or_apart(res, y, bytes)))
+    return fail(RINGADA_E_INVALID, "y overlaps x or res without being the same tensor");
+  RG_HIP(launch_dropout(dtype, x, res, y, n, thr, rng, site, static_cast<hipStream_t>(stream)));
+  return RINGADA_OK;
+}

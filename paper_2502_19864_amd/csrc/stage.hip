@@ -13,13 +13,14 @@
 
 #include "kernels.h"
 #include "ringada.h"
+#include "status.h"
 
 using namespace rg;
 
 // ================================================================ errors
 static thread_local std::string g_err;
 
-static ringada_status fail(ringada_status s, const char* fmt, ...) {
+ringada_status rg::fail(ringada_status s, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -28,19 +29,6 @@ static ringada_status fail(ringada_status s, const char* fmt, ...) {
   g_err = buf;
   return s;
 }
-
-#define RG_HIP(x)                                                                              \
-  do {                                                                                         \
-    hipError_t e_ = (x);                                                                       \
-    if (e_ != hipSuccess)                                                                      \
-      return fail(RINGADA_E_HIP, "%s failed: %s", #x, hipGetErrorString(e_));                  \
-  } while (0)
-
-#define RG_TRY(x)                                                                              \
-  do {                                                                                         \
-    ringada_status s_ = (x);                                                                   \
-    if (s_ != RINGADA_OK) return s_;                                                           \
-  } while (0)
 
 extern "C" const char* ringada_last_error(void) { return g_err.c_str(); }
 

@@ -1,0 +1,172 @@
+"""Host-only checks of the block operators' entry points: what they refuse, the plans,
+the bucket map.  No call here reaches a device."""
+import ctypes
+from fractions import Fraction
+
+import pytest
+
+from paper_2502_19864_amd import binding as B
+
+
+def desc(**kw):
+    d = dict(dtype=B.BF16, batch=2, n_heads=4, n_kv_heads=2, d_head=64, seq_q=10, seq_k=20, causal=1, window=0,
+             sinks=0, scale=0.125, n_buckets=0, max_distance=0)
+    d.update(kw)
+    return B.AttnDesc(**d)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=7), B.RINGADA_E_INVALID),
+    (dict(batch=0), B.RINGADA_E_INVALID),
+    (dict(n_kv_heads=3), B.RINGADA_E_INVALID),
+    (dict(seq_q=0), B.RINGADA_E_INVALID),
+    (dict(window=-1), B.RINGADA_E_INVALID),
+    (dict(sinks=-1), B.RINGADA_E_INVALID),
+    (dict(scale=0.0), B.RINGADA_E_INVALID),
+    (dict(scale=float("nan")), B.RINGADA_E_INVALID),
+    (dict(scale=float("inf")), B.RINGADA_E_INVALID),
+    (dict(n_buckets=-1), B.RINGADA_E_INVALID),
+    (dict(n_buckets=4, max_distance=1025), B.RINGADA_E_UNSUPPORTED),
+    (dict(d_head=96), B.RINGADA_E_UNSUPPORTED),
+    (dict(dtype=B.F32, d_head=129), B.RINGADA_E_UNSUPPORTED),
+    (dict(seq_k=1 << 25), B.RINGADA_E_UNSUPPORTED),
+    (dict(batch=1 << 20, seq_k=1 << 20), B.RINGADA_E_UNSUPPORTED),
+])
+def test_attention_descriptor_is_checked(kw, status):
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_plan(desc(**kw), False)
+    assert e.value.status == status and B.ringada_last_error()
+
+
+def test_attention_plan():
+    f, b = B.ringada_attn_plan(desc(), False)
+    assert b >= 2 * 4 * 10 * 4
+    _, b2 = B.ringada_attn_plan(desc(n_buckets=8, max_distance=16), True)
+    _, b3 = B.ringada_attn_plan(desc(n_buckets=8, max_distance=16), False)
+    assert b3 == b and b2 >= b + 2 * 4 * 33 * 4
+
+
+BASE = 1 << 20  # addresses that no call gets to
+
+
+def view(at, rows, heads, dh=64):
+    return B.View(BASE * at, rows * heads * dh, heads * dh, dh)
+
+
+def tensors(**kw):
+    t = dict(q=view(1, 10, 4), k=view(2, 20, 2), v=view(3, 20, 2), o=view(4, 10, 4), lse=BASE * 5)
+    t.update(kw)
+    return B.AttnTensors(**t)
+
+
+def grads(**kw):
+    g = dict(dout=view(6, 10, 4), dq=view(7, 10, 4), dk=view(8, 20, 2), dv=view(9, 20, 2))
+    g.update(kw)
+    return B.AttnGrads(**g)
+
+
+@pytest.mark.parametrize("kw,dk", [
+    (dict(q=B.View(0, 1, 1, 1)), {}),                                # no data
+    (dict(k=B.View(BASE * 2 + 8, 2560, 128, 64)), {}),               # misaligned
+    (dict(k=B.View(BASE * 2, 2560, 100, 64)), {}),                   # a stride that is no multiple of 8
+    (dict(v=B.View(BASE * 3, 2560, -128, 64)), {}),                  # backwards
+    (dict(o=B.View(BASE * 4, 2560, 128, 64)), {}),                   # rows of the output overlap
+    (dict(o=B.View(BASE * 4, 64, 256, 64)), {}),                     # and its sequences
+    (dict(o=view(1, 10, 4)), {}),                                    # the output is an input
+    (dict(table=BASE * 10, bucket=BASE * 11), {}),                   # a table without buckets
+    ({}, dict(n_buckets=4, max_distance=3)),                         # and the other way round
+    (dict(table=BASE * 10), dict(n_buckets=4, max_distance=3)),      # no map
+])
+def test_attention_tensors_are_checked(kw, dk):
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_forward(None, desc(**dk), tensors(**kw), BASE * 12, 0)
+    assert e.value.status == B.RINGADA_E_INVALID
+
+
+def test_row_strides_are_bounded():
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_forward(None, desc(), tensors(k=B.View(BASE * 2, 64, 1 << 24, 64)), BASE * 12, 0)
+    assert e.value.status == B.RINGADA_E_UNSUPPORTED
+
+
+@pytest.mark.parametrize("kw,gkw", [
+    (dict(lse=None), {}),
+    ({}, dict(dq=view(1, 10, 4))),
+    ({}, dict(dq=view(6, 10, 4))),
+    ({}, dict(dv=view(8, 20, 2))),
+    ({}, dict(dtable=BASE * 10)),
+    ({}, dict(dk=B.View(BASE * 8, 2560, 64, 64))),
+])
+def test_gradients_are_checked(kw, gkw):
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_backward(None, desc(), tensors(**kw), grads(**gkw), BASE * 12, 1 << 20)
+    assert e.value.status == B.RINGADA_E_INVALID
+
+
+def test_workspaces_are_checked():
+    _, n = B.ringada_attn_plan(desc(), False)
+    for ws, have, status in ((None, n, B.RINGADA_E_WORKSPACE), (BASE * 12, n - 1, B.RINGADA_E_WORKSPACE),
+                             (BASE * 12 + 16, n, B.RINGADA_E_INVALID)):
+        with pytest.raises(B.RingadaError) as e:
+            B.ringada_attn_backward(None, desc(), tensors(), grads(), ws, have)
+        assert e.value.status == status
+    L = B.lib()
+    assert L.ringada_attn_plan(None, 0, None, None) == B.RINGADA_E_INVALID
+    assert L.ringada_attn_forward(None, ctypes.byref(desc()), None, None, 0) == B.RINGADA_E_INVALID
+    assert L.ringada_attn_backward(None, ctypes.byref(desc()), ctypes.byref(tensors()), None, None, 0) == \
+        B.RINGADA_E_INVALID
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dtype=3), dict(x=None), dict(y=None), dict(rng=None), dict(n=0), dict(n=(1 << 35) + 1), dict(p=-0.1),
+    dict(p=1.0), dict(p=float("nan")), dict(p=0.999999), dict(y=BASE + 16), dict(res=BASE * 3 + 4), dict(x=BASE + 1),
+    dict(rng=BASE * 9 + 4)])
+def test_dropout_arguments_are_checked(kw):
+    a = dict(dtype=B.BF16, x=BASE, res=None, y=BASE * 3, n=1000, p=0.1, rng=BASE * 9)
+    a.update(kw)
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_dropout(None, a["dtype"], a["x"], a["res"], a["y"], a["n"], a["p"], a["rng"], 0)
+    assert e.value.status == B.RINGADA_E_INVALID
+
+
+@pytest.mark.parametrize("n,dist,bidi", [(32, 128, True), (32, 128, False), (16, 20, True), (64, 512, False),
+                                         (4, 2, True), (2, 2, False), (2, 1024, False), (64, 1024, True),
+                                         (8, 16, True), (320, 500, True), (1000, 1024, False)])
+def test_bucket_map(n, dist, bidi):
+    """Against the rule in whole numbers: d >= one (dist / one)^(k / m) as powers of m."""
+    got = B.ringada_relpos_buckets(n, dist, bidi)
+    per = n // 2 if bidi else n
+    one = per // 2
+    m = per - one
+    for rel in range(-dist, dist + 1):
+        d = abs(rel) if bidi else max(-rel, 0)
+        t = d
+        if d >= one:
+            k = 0
+            while k < m and Fraction(d, one) ** m >= Fraction(dist, one) ** (k + 1):
+                k += 1
+            t = min(per - 1, one + k)
+        assert got[rel + dist] == t + (per if bidi and rel > 0 else 0), rel
+
+
+@pytest.mark.parametrize("n,dist,bidi", [(1, 8, False), (0, 8, False), (3, 8, True), (2, 8, True), (32, 8, True),
+                                         (32, 16, False), (32, 1025, True), (8, -1, False)])
+def test_bucket_map_refuses(n, dist, bidi):
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_relpos_buckets(n, dist, bidi)
+    assert e.value.status == B.RINGADA_E_INVALID
+
+
+def test_python_front_end_refuses():
+    import torch
+
+    from paper_2502_19864_amd import operators as ops
+    q = torch.zeros(1, 2, 3, 64)
+    with pytest.raises(ValueError):  # not on a GPU
+        ops.attention_forward(q, q, q)
+    with pytest.raises(ValueError):
+        ops.attention_forward(q[0], q, q)
+    with pytest.raises(ValueError):
+        ops.dropout(q, 0.1, torch.zeros(2, dtype=torch.int64))
+    with pytest.raises(ValueError):
+        ops.attention_backward(q, q, q, q, q, None)
