@@ -18,6 +18,8 @@
 // formed.  bf16 products run on MFMA 32x32x16, P and dS rounded to bf16 on their
 // way into the second product (they are never stored; every sum stays in fp32);
 // fp32 ones on MFMA 32x32x2 in fp32 throughout.
+#include <algorithm>
+
 #include "attn_core.h"
 #include "common.h"
 #include "kernels.h"
@@ -44,8 +46,10 @@ struct Mask {
   int lk, causal, window, sinks;  // window 0: none
   __device__ __forceinline__ Mask(const MaskedAttnArgs& a, int lk_)
       : lk(lk_), causal(a.causal), window(a.window), sinks(a.sinks) {}
+  // without branches: what follows in a wave has matrix instructions and transpose reads, which take
+  // all 64 lanes, so no lane may leave on its own
   __device__ __forceinline__ bool pair(int p, int j) const {
-    return j < lk && (!causal || j <= p) && (!window || abs(p - j) < window || j < sinks);
+    return (j < lk) & ((causal == 0) | (j <= p)) & ((window == 0) | (abs(p - j) < window) | (j < sinks));
   }
   // keys k0 .. k0 + n - 1 against positions plo .. phi: 0 nothing visible, 2 everything, 1 else
   __device__ __forceinline__ int block(int k0, int n, int plo, int phi) const {
@@ -99,6 +103,10 @@ struct OpsBf16 {
   };
   TileRead<DH> rd;
   __device__ __forceinline__ OpsBf16(int lane, int) : rd(lane) {}
+  // the LDS read offsets are formed anew from here on: kept across a loop they spill at d_head 128
+  __device__ __forceinline__ void fresh() {
+    if constexpr (DH == 128) asm volatile("" : "+v"(rd.row), "+v"(rd.tr));
+  }
   static __device__ __forceinline__ void load_rows(Rows& o, const E* row, bool valid, int half, int) {
     load_row_frags<DH>(row, valid, half, o.f);
   }
@@ -161,6 +169,7 @@ struct OpsF32 {
     row = (lane & 31) * P + half * (DHM / 2);
     col = lane & 31;
   }
+  __device__ __forceinline__ void fresh() {}
   static __device__ __forceinline__ void load_rows(Rows& o, const E* src, bool valid, int half, int dh) {
 #pragma unroll
     for (int i = 0; i < DHM / 2; ++i) o.f[i] = src[min(half * (DHM / 2) + i, dh - 1)];
@@ -297,7 +306,8 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
   __shared__ __attribute__((aligned(1024))) E sm[4 * TILE];  // [buffer][K, V]
   extern __shared__ float sbias[];
   static_assert(4 * TILE >= NW * O::STAGE, "the O rows fit the tiles' space");
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
+  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // what a wave skips, it skips whole
   const int nq = (a.Sq + 32 * NW - 1) / (32 * NW);
   int qb, bh;
   heavy_first(blockIdx.x, nq, a.B * a.H, qb, bh);
@@ -353,7 +363,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
       for (int kb = 0; kb < KR / 32; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (!mask.pair(p, k0 + kb * 32 + perm_pos(r, half))) sc[kb][r] = -INFINITY;
+          sc[kb][r] = mask.pair(p, k0 + kb * 32 + perm_pos(r, half)) ? sc[kb][r] : -INFINITY;
     }
 #pragma unroll
     for (int kb = 0; kb < KR / 32; ++kb)
@@ -396,9 +406,6 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
 // exponent offset of a row that sees nothing: exp2(x - inf) = 0
 __device__ __forceinline__ float lse_or_inf(float l) { return l == -INFINITY ? INFINITY : l; }
 
-// One score block of the backward: st = P, dp = dP - D times P (dS), both zero where masked.
-// Registers run over the tile rows (SGN 1: keys, own row = query; SGN -1: queries, own row = key).
-
 // dQ pass (lane = query); writes D.  DTAB: dtable is wanted, and D is formed from
 // P and dP themselves in a first sweep over the tiles: the sums over dS cancel, and a D
 // from the stored (rounded) O would leave an error of that rounding in them.  That sweep
@@ -409,7 +416,8 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   constexpr int DH = O::DH, KR = O::KR, TILE = O::TILE;
   __shared__ __attribute__((aligned(1024))) E sm[4 * TILE];  // [buffer][K, V]
   extern __shared__ float sbias[];                           // bias, then (DTAB) one diagonal array per wave
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
+  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // what a wave skips, it skips whole
   const int nq = (a.Sq + 32 * NW - 1) / (32 * NW);
   int qb, bh;
   heavy_first(blockIdx.x, nq, a.B * a.H, qb, bh);
@@ -425,7 +433,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   const float sl2 = kLog2e * a.scale;
   const E* K = static_cast<const E*>(a.k.p) + b * a.k.b + hk * a.k.h;
   const E* V = static_cast<const E*>(a.v.p) + b * a.v.b + hk * a.v.h;
-  const O ops(lane, a.dh);
+  O ops(lane, a.dh);
   const int nit = DTAB ? 2 * kt.n : kt.n;  // DTAB: the tiles twice
   auto issue = [&](int i) {
     const int k0 = kt.at(DTAB && i >= kt.n ? i - kt.n : i) * KR, last = sq.lk - 1 - k0;
@@ -472,17 +480,18 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
       const int k0 = kt.at(DTAB && i >= kt.n ? i - kt.n : i) * KR + kb * 32;
       const int kind = mask.block(k0, 32, plo, phi);
       if (kind == 0) continue;  // wave-uniform
-      const bool full = kind == 2 && q0 + 32 <= sq.lq;
+      ops.fresh();
       f32x16 st, dp;
       ops.scores(st, sK, kb, qf);
       ops.scores(dp, sV, kb, df);
       if (BIAS) add_bias<1>(st, sl2, sbias, a.R, k0 - p, k0 - phi, k0 + 31 - plo, half);
+      if (kind == 1) {  // a row past len_q has lse = +inf
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const bool ok = full || (qv && mask.pair(p, k0 + perm_pos(r, half)));
-        const float e = __builtin_amdgcn_exp2f(BIAS ? st[r] - lse : fmaf(st[r], sl2, -lse));
-        st[r] = ok ? e : 0.f;
+        for (int r = 0; r < 16; ++r)
+          st[r] = mask.pair(p, k0 + perm_pos(r, half)) ? st[r] : -INFINITY;
       }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[r] = __builtin_amdgcn_exp2f(BIAS ? st[r] - lse : fmaf(st[r], sl2, -lse));
       if (first) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) dsum = fmaf(st[r], dp[r], dsum);
@@ -519,66 +528,122 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
            stream_out((long)a.B * a.Sq * a.H * DH * (long)sizeof(E)), a.Sq - q0, a.dh);
 }
 
+// Work of the dK/dV pass.  A block of 32 NW keys meets the query tiles that see it, for every
+// query head of its group: `iters` iterations at most.  Blocks that hold sinks (all of them
+// without a window) are seen by every later query, so they are dealt to several
+// workgroups each, and so are the others when there are too few of them to fill the GPU;
+// such workgroups leave fp32 partial sums, which attn_masked_dkdv_join adds in order.
+// Before (one workgroup per block): 8192 causal tokens, 32 heads on 8, window 1024, 4 sinks
+// 3704 us.
+struct KeyWork {
+  int nk, nfar;       // key blocks, and how many of them (the first) are the sinks'
+  int s_far, s_near;  // workgroups per block
+  int c_far, c_near;  // iterations of each
+  __host__ __device__ long items() const { return (long)nfar * s_far + (long)(nk - nfar) * s_near; }
+  // items that leave partial sums (far blocks are split at least as finely)
+  __host__ __device__ long slots() const { return s_near > 1 ? items() : s_far > 1 ? (long)nfar * s_far : 0; }
+};
+struct KeyItem {
+  int kb, split, n, c;  // block, which of its n workgroups, iterations of each
+  __device__ __forceinline__ KeyItem(const KeyWork& w, int item) {
+    const int far = w.nfar * w.s_far, t = item - far;
+    const bool f = item < far;
+    kb = f ? item / w.s_far : w.nfar + t / w.s_near;
+    split = f ? item % w.s_far : t % w.s_near;
+    n = f ? w.s_far : w.s_near;
+    c = f ? w.c_far : w.c_near;
+  }
+};
+// the query tiles of KR rows that see keys kw0 .. kw0 + nkeys - 1: the first, and how many
+template <int KR>
+__device__ __forceinline__ void query_tiles(const MaskedAttnArgs& a, const Seq& sq, int kw0, int nkeys, int& qt0,
+                                            int& nt) {
+  qt0 = nt = 0;
+  if (kw0 >= sq.lk) return;
+  const int kw1 = min(kw0 + nkeys, sq.lk) - 1;
+  int qlo = 0, qhi = sq.lq - 1;
+  if (a.causal) qlo = max(0, kw0 - sq.off);
+  if (a.window && kw0 >= a.sinks) {
+    qhi = min(qhi, kw1 + a.window - 1 - sq.off);
+    if (!a.causal) qlo = max(0, kw0 - a.window + 1 - sq.off);
+  }
+  if (qhi < qlo) return;
+  qt0 = qlo / KR;
+  nt = qhi / KR - qt0 + 1;
+}
+// item and batch-head of a workgroup: items in order of weight over all heads of an XCD
+__device__ __forceinline__ void key_item(int lin, int items, int nbh, int& item, int& bh) {
+  const int n = items * nbh, P = n / 8;
+  if (n % 8 || P % items) {
+    const int blk = xcd_block(lin, n);
+    item = blk % items;
+    bh = blk / items;
+    return;
+  }
+  const int x = lin % 8, o = lin / 8, per = P / items;
+  item = o / per;
+  bh = x * per + o % per;
+}
+
 // dK/dV pass (lane = key): the query heads of the key's group one after another
 template <class O, bool BIAS, int NW>
-__global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(MaskedAttnArgs a) {
+__global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(MaskedAttnArgs a, KeyWork w) {
   typedef typename O::E E;
   constexpr int DH = O::DH, KR = O::KR, TILE = O::TILE;
   __shared__ __attribute__((aligned(1024))) E sm[4 * TILE];  // [buffer][Q, dO]
   __shared__ __attribute__((aligned(16))) float sL[2][KR], sD[2][KR];
   extern __shared__ float sbias[];  // two heads' bias
   static_assert(KR <= 64 * NW, "one row statistic per thread");
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, l32 = lane & 31;
-  const int nk = (a.Sk + 32 * NW - 1) / (32 * NW), grp = a.H / a.Hkv;
-  int kb0, bh;
-  heavy_first(blockIdx.x, nk, a.B * a.Hkv, kb0, bh);  // causal: the first block has the most queries
+  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // what a wave skips, it skips whole
+  const int grp = a.H / a.Hkv;
+  int item, bh;
+  key_item(blockIdx.x, (int)w.items(), a.B * a.Hkv, item, bh);
+  const KeyItem ki(w, item);
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   const Seq sq = seq_of(a, b);
   const Mask mask(a, sq.lk);
-  const int kw0 = kb0 * 32 * NW, k0 = kw0 + wave * 32, key = k0 + l32;
+  const int kw0 = ki.kb * 32 * NW, k0 = kw0 + wave * 32, key = k0 + l32;
   const bool kv = key < sq.lk;
-  // the queries that see any of this workgroup's keys
-  int qlo = 0, qhi = -1;
-  if (kw0 < sq.lk) {
-    const int kw1 = min(kw0 + 32 * NW, sq.lk) - 1;
-    qhi = sq.lq - 1;
-    if (a.causal) qlo = max(0, kw0 - sq.off);
-    if (a.window && kw0 >= a.sinks) {
-      qhi = min(qhi, kw1 + a.window - 1 - sq.off);
-      if (!a.causal) qlo = max(0, kw0 - a.window + 1 - sq.off);
-    }
-  }
-  const int qt0 = qlo / KR, nt = qhi >= qlo ? qhi / KR - qt0 + 1 : 0, nit = nt * grp;
+  int qt0, nt;
+  query_tiles<KR>(a, sq, kw0, 32 * NW, qt0, nt);
+  const int i0 = ki.n > 1 ? ki.split * ki.c : 0, i1 = ki.n > 1 ? min(nt * grp, i0 + ki.c) : nt * grp;
+  if (ki.n > 1 && i0 >= i1) return;  // the join counts the same way
   const float sl2 = kLog2e * a.scale;
   const int W = 2 * a.R + 1;
-  const O ops(lane, a.dh);
-  auto issue = [&](int i) {
-    const int h = hk * grp + i / nt, r0 = (qt0 + i % nt) * KR, last = sq.lq - 1 - r0;
-    E* dst = sm + (i & 1) * 2 * TILE;
+  O ops(lane, a.dh);
+  int h = hk * grp, t = 0;  // head and query tile (of nt) of the iteration that is issued
+  if (nt > 0) {
+    h += i0 / nt;
+    t = i0 % nt;
+  }
+  auto issue = [&](int buf) {
+    const int r0 = (qt0 + t) * KR, last = sq.lq - 1 - r0;
+    E* dst = sm + buf * 2 * TILE;
     O::template dma<NW>(static_cast<const E*>(a.q.p) + b * a.q.b + h * a.q.h + (long)r0 * a.q.t, a.q.t, last, dst, a.dh);
     O::template dma<NW>(static_cast<const E*>(a.dout.p) + b * a.dout.b + h * a.dout.h + (long)r0 * a.dout.t, a.dout.t,
                         last, dst + TILE, a.dh);
   };
-  // the row statistics of iteration i, one query per thread of the first KR
-  auto load_stats = [&](int i, float& lv, float& dv) {
+  // that iteration's row statistics, one query per thread of the first KR
+  auto load_stats = [&](float& lv, float& dv) {
     lv = dv = 0.f;
     if (threadIdx.x < KR) {
-      const long at = ((long)b * a.H + hk * grp + i / nt) * a.Sq + min((qt0 + i % nt) * KR + (int)threadIdx.x, sq.lq - 1);
+      const long at = ((long)b * a.H + h) * a.Sq + min((qt0 + t) * KR + (int)threadIdx.x, sq.lq - 1);
       lv = lse_or_inf(a.lse[at]);
       dv = a.dsum[at];
     }
   };
-  auto put_stats = [&](int i, float lv, float dv) {
+  auto put_stats = [&](int buf, float lv, float dv) {
     if (threadIdx.x < KR) {
-      sL[i & 1][threadIdx.x] = lv;
-      sD[i & 1][threadIdx.x] = dv;
+      sL[buf][threadIdx.x] = lv;
+      sD[buf][threadIdx.x] = dv;
     }
   };
   float lnext = 0.f, dnext = 0.f;
-  if (nit > 0) {
+  if (i0 < i1) {
     issue(0);
-    load_stats(0, lnext, dnext);
-    if (BIAS) load_bias(a, hk * grp, sbias);
+    load_stats(lnext, dnext);
+    if (BIAS) load_bias(a, h, sbias);
   }
   typename O::Rows kf, vf;
   const long row = kv ? key : 0;
@@ -589,33 +654,48 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
   for (int i = 0; i < DH / 32; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) dk[i][r] = dv[i][r] = 0.f;
-  if (nit > 0) put_stats(0, lnext, dnext);
+  if (i0 < i1) put_stats(0, lnext, dnext);
 
-  for (int i = 0; i < nit; ++i) {
+  int hb = 0;  // the buffer of the current head's bias
+  for (int i = i0; i < i1; ++i) {
+    const int buf = (i - i0) & 1, qt = qt0 + t, hb_now = hb;
     tiles_ready();
-    if (i + 1 < nit) {
-      load_stats(i + 1, lnext, dnext);
-      issue(i + 1);
-      // the next head's bias goes where the last head's was: read for the last time before this barrier
-      if (BIAS && (i + 1) % nt == 0) load_bias(a, hk * grp + (i + 1) / nt, sbias + ((i + 1) / nt & 1) * W);
+    if (i + 1 < i1) {
+      if (++t == nt) {
+        t = 0;
+        ++h;
+        hb ^= 1;
+        // goes where the last head's was: read for the last time before this barrier
+        if (BIAS) load_bias(a, h, sbias + hb * W);
+      }
+      load_stats(lnext, dnext);
+      issue(buf ^ 1);
     }
-    const E* sQ = sm + (i & 1) * 2 * TILE;
+    const E* sQ = sm + buf * 2 * TILE;
     const E* sO = sQ + TILE;
-    const float* pL = sL[i & 1];
-    const float* pD = sD[i & 1];
-    const float* bias = sbias + (i / nt & 1) * W;
+    const float* pL = sL[buf];
+    const float* pD = sD[buf];
+    const float* bias = sbias + hb_now * W;
 #pragma unroll 1
     for (int qb = 0; qb < KR / 32; ++qb) {
-      const int q0 = (qt0 + i % nt) * KR + qb * 32;
+      const int q0 = qt * KR + qb * 32;
       if (q0 >= sq.lq || k0 >= sq.lk) break;  // wave-uniform
       const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
       const int kind = mask.block(k0, 32, plo, phi);
       if (kind == 0) continue;
+      ops.fresh();
       const bool full = kind == 2 && q0 + 32 <= sq.lq;
       f32x16 st, dp;
       ops.scores(st, sQ, qb, kf);
       ops.scores(dp, sO, qb, vf);
       if (BIAS) add_bias<-1>(st, sl2, bias, a.R, key - plo, k0 - phi, k0 + 31 - plo, half);
+      if (!full) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int qq = q0 + perm_pos(r, half);
+          st[r] = ((qq < sq.lq) & mask.pair(sq.off + qq, key)) ? st[r] : -INFINITY;
+        }
+      }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {  // queries q0 + 8g + 4*half + 0..3
         const float4 L = *reinterpret_cast<const float4*>(pL + qb * 32 + 8 * g + 4 * half);
@@ -623,17 +703,26 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
         const float lv[4] = {L.x, L.y, L.z, L.w}, sv[4] = {D.x, D.y, D.z, D.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int r = 4 * g + e, qq = q0 + 8 * g + 4 * half + e;
-          const bool ok = full || (qq < sq.lq && mask.pair(sq.off + qq, key));
-          const float x = __builtin_amdgcn_exp2f(BIAS ? st[r] - lv[e] : fmaf(st[r], sl2, -lv[e]));
-          st[r] = ok ? x : 0.f;
+          const int r = 4 * g + e;
+          st[r] = __builtin_amdgcn_exp2f(BIAS ? st[r] - lv[e] : fmaf(st[r], sl2, -lv[e]));
           dp[r] = st[r] * (dp[r] - sv[e]);  // dS
         }
       }
       ops.accum(dv, sO, qb, st);
       ops.accum(dk, sQ, qb, dp);
     }
-    if (i + 1 < nit) put_stats(i + 1, lnext, dnext);  // the other buffer: last read before this tile's barrier
+    if (i + 1 < i1) put_stats(buf ^ 1, lnext, dnext);  // the other buffer: last read before this tile's barrier
+  }
+  if (ki.n > 1) {  // in the accumulators' own order, 1 KB per store
+    float4* dst = reinterpret_cast<float4*>(a.part + (((long)bh * w.slots() + item) * NW + wave) * (2 * 32 * DH)) + lane;
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        dst[(i * 4 + g) * 64] = make_float4(dk[i][4 * g], dk[i][4 * g + 1], dk[i][4 * g + 2], dk[i][4 * g + 3]);
+        dst[(DH / 8 + i * 4 + g) * 64] = make_float4(dv[i][4 * g], dv[i][4 * g + 1], dv[i][4 * g + 2], dv[i][4 * g + 3]);
+      }
+    return;
   }
   tiles_ready();  // the tiles' space now takes the dK, then the dV rows
   if (k0 >= a.Sk) return;
@@ -645,20 +734,73 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
            nt_out, a.Sk - k0, a.dh);
 }
 
-// dtable[t][h] += the diagonals' sums of bucket t, over every workgroup's row of partial
-// sums.  One workgroup per (bucket, head); the order is fixed.
-__global__ __launch_bounds__(256) void attn_bias_grad(MaskedAttnArgs a, int rows) {
-  __shared__ double part[4];
-  const int t = blockIdx.x, h = blockIdx.y, W = 2 * a.R + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  double s = 0.0;
-  for (int i = 0; i < W; ++i) {
-    if (min(max(a.bucket[i], 0), a.nb - 1) != t) continue;
-    for (int r = threadIdx.x; r < rows; r += 256) s += (double)a.diag[((long)r * a.H + h) * W + i];
+// adds a split block's partial sums, in order, and writes its rows; one wave per 32 keys
+// and output
+template <class O, int NW>
+__global__ __launch_bounds__(64) void attn_masked_dkdv_join(MaskedAttnArgs a, KeyWork w, int blocks) {
+  typedef typename O::E E;
+  constexpr int DH = O::DH;
+  __shared__ __attribute__((aligned(16))) E stage[O::STAGE];
+  const int lane = threadIdx.x, wave = blockIdx.x % NW, kb = blockIdx.x / NW % blocks, bh = blockIdx.x / NW / blocks;
+  const bool is_v = blockIdx.y;
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  const Seq sq = seq_of(a, b);
+  int qt0, nt;
+  query_tiles<O::KR>(a, sq, kb * 32 * NW, 32 * NW, qt0, nt);
+  const int item = kb < w.nfar ? kb * w.s_far : w.nfar * w.s_far + (kb - w.nfar) * w.s_near;
+  const int c = kb < w.nfar ? w.c_far : w.c_near, n = (nt * (a.H / a.Hkv) + c - 1) / c;
+  const int k0 = kb * 32 * NW + wave * 32;
+  if (k0 >= a.Sk) return;
+  f32x16 acc[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+  for (int s = 0; s < n; ++s) {
+    const float4* src = reinterpret_cast<const float4*>(a.part + (((long)bh * w.slots() + item + s) * NW + wave) * (2 * 32 * DH)) +
+                        (is_v ? DH / 8 * 64 : 0) + lane;
+#pragma unroll
+    for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 v = src[(i * 4 + g) * 64];
+        acc[i][4 * g] += v.x;
+        acc[i][4 * g + 1] += v.y;
+        acc[i][4 * g + 2] += v.z;
+        acc[i][4 * g + 3] += v.w;
+      }
   }
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if (lane == 0) part[wave] = s;
+  const View& o = is_v ? a.dv : a.dk;
+  O::store(acc, is_v ? 1.f : a.scale, lane, stage, static_cast<E*>(o.p) + b * o.b + (long)k0 * o.t + hk * o.h, o.t,
+           stream_out((long)a.B * a.Sk * a.Hkv * DH * (long)sizeof(E)), a.Sk - k0, a.dh);
+}
+
+// The table's gradient from the dQ pass's partial sums diag[row][head][W]: first the sum
+// over the rows for each relative position (64 of them per workgroup, a row per wave and
+// step), then dtable[t][h] += the positions of bucket t (a wave each).  Both in a fixed order;
+// in 64 bits, which costs nothing here.
+__global__ __launch_bounds__(1024) void attn_bias_rows(MaskedAttnArgs a, int rows) {
+  __shared__ double part[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = 2 * a.R + 1, h = blockIdx.y;
+  const int i = blockIdx.x * 64 + lane;
+  double s = 0.0;
+  if (i < W)
+#pragma unroll 4
+    for (int r = wave; r < rows; r += 16) s += (double)a.diag[((long)r * a.H + h) * W + i];
+  part[wave][lane] = s;
   __syncthreads();
-  if (threadIdx.x == 0) a.dtable[(long)t * a.H + h] += (float)(part[0] + part[1] + part[2] + part[3]);
+  if (wave == 0 && i < W) {
+    for (int k = 1; k < 16; ++k) s += part[k][lane];
+    a.diag_sum[(long)h * W + i] = s;
+  }
+}
+__global__ __launch_bounds__(64) void attn_bias_grad(MaskedAttnArgs a) {
+  const int t = blockIdx.x, h = blockIdx.y, W = 2 * a.R + 1;
+  double s = 0.0;
+  for (int i = threadIdx.x; i < W; i += 64)
+    if (min(max(a.bucket[i], 0), a.nb - 1) == t) s += a.diag_sum[(long)h * W + i];
+  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+  if (threadIdx.x == 0) a.dtable[(long)t * a.H + h] += (float)s;
 }
 
 // ================================================================ launchers
@@ -666,17 +808,56 @@ constexpr int MA_NW = 4;
 
 static long blocks_of(int n) { return (n + 32 * MA_NW - 1) / (32 * MA_NW); }
 
-static size_t dsum_bytes(const MaskedAttnArgs& a) { return ((size_t)a.B * a.H * a.Sq * 4 + 255) & ~(size_t)255; }
+static size_t al256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// Workgroups of the dK/dV pass: two per CU hide each other's barriers, so blocks are split
+// until there are 512, but no finer than four iterations.
+static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
+  const int KR = dtype == DT_BF16 ? 64 : 32, grp = a.H / a.Hkv, rows = 32 * MA_NW;
+  KeyWork w;
+  w.nk = (int)blocks_of(a.Sk);
+  w.nfar = a.window ? (int)std::min<long>(w.nk, (a.sinks + rows - 1) / rows) : w.nk;
+  const long far = (long)grp * ((a.Sq + KR - 1) / KR);
+  const long span = (long)rows + (a.causal ? 1l : 2l) * a.window;
+  const long near = a.window ? std::min(far, grp * (span / KR + 2)) : far;
+  const long wgs = (long)w.nk * a.B * a.Hkv, want = std::max(1l, std::min((512 + wgs - 1) / wgs, near / 4));
+  // a far block as finely as its workgroups take no longer than a near one's, within 64
+  w.c_near = (int)((near + want - 1) / want);
+  w.s_near = (int)((near + w.c_near - 1) / w.c_near);
+  w.c_far = (int)std::max<long>(w.c_near, (far + 63) / 64);
+  w.s_far = (int)((far + w.c_far - 1) / w.c_far);
+  if (w.s_far < w.s_near || (long)w.items() * a.B * a.Hkv >= (1l << 31)) {
+    w.s_far = w.s_near = 1;
+    w.c_far = w.c_near = (int)far;
+  }
+  return w;
+}
+
+struct BwdSpace {
+  size_t diag, sum, part, total;
+};
+static BwdSpace bwd_space(int dtype, const MaskedAttnArgs& a, bool dtable) {
+  BwdSpace s;
+  s.diag = al256((size_t)a.B * a.H * a.Sq * 4);
+  s.sum = s.diag + (dtable ? al256((size_t)a.B * blocks_of(a.Sq) * a.H * (2 * a.R + 1) * 4) : 0);
+  s.part = s.sum + (dtable ? al256((size_t)a.H * (2 * a.R + 1) * 8) : 0);
+  const int dh = a.dh <= 64 ? 64 : 128;
+  s.total = s.part + al256((size_t)a.B * a.Hkv * key_work(dtype, a).slots() * MA_NW * 2 * 32 * dh * 4);
+  return s;
+}
 
 void masked_attn_bytes(int dtype, const MaskedAttnArgs& a, bool dtable, size_t* fwd, size_t* bwd) {
   *fwd = 0;
-  *bwd = dsum_bytes(a);
-  if (dtable) *bwd += (size_t)a.B * blocks_of(a.Sq) * a.H * (2 * a.R + 1) * 4;
+  *bwd = bwd_space(dtype, a, dtable).total;
 }
 
-void masked_attn_workspace(MaskedAttnArgs& a, void* ws) {
-  a.dsum = static_cast<float*>(ws);
-  a.diag = reinterpret_cast<float*>(static_cast<char*>(ws) + dsum_bytes(a));
+void masked_attn_workspace(int dtype, MaskedAttnArgs& a, void* ws) {
+  const BwdSpace s = bwd_space(dtype, a, a.dtable != nullptr);
+  char* p = static_cast<char*>(ws);
+  a.dsum = reinterpret_cast<float*>(p);
+  a.diag = reinterpret_cast<float*>(p + s.diag);
+  a.diag_sum = reinterpret_cast<double*>(p + s.sum);
+  a.part = reinterpret_cast<float*>(p + s.part);
 }
 
 template <class O>
@@ -687,19 +868,25 @@ static hipError_t fwd_ops(const MaskedAttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 template <class O>
-static hipError_t bwd_ops(const MaskedAttnArgs& a, hipStream_t s) {
-  const dim3 gq((unsigned)(blocks_of(a.Sq) * a.B * a.H)), gk((unsigned)(blocks_of(a.Sk) * a.B * a.Hkv)), block(64 * MA_NW);
-  const unsigned W = (2 * a.R + 1) * 4;
+static hipError_t bwd_ops(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
+  const KeyWork w = key_work(dtype, a);
+  const dim3 gq((unsigned)(blocks_of(a.Sq) * a.B * a.H)), gk((unsigned)(w.items() * a.B * a.Hkv)), block(64 * MA_NW);
+  const int W = 2 * a.R + 1;
   if (a.table) {
-    if (a.dtable) RG_LAUNCH((attn_masked_bwd_dq<O, true, true, MA_NW>), gq, block, (1 + MA_NW) * W, s, a);
-    else RG_LAUNCH((attn_masked_bwd_dq<O, true, false, MA_NW>), gq, block, W, s, a);
-    RG_LAUNCH((attn_masked_bwd_dkdv<O, true, MA_NW>), gk, block, 2 * W, s, a);
-    if (a.dtable)
-      RG_LAUNCH(attn_bias_grad, dim3(a.nb, a.H), dim3(256), 0, s, a, (int)(a.B * blocks_of(a.Sq)));
+    if (a.dtable) RG_LAUNCH((attn_masked_bwd_dq<O, true, true, MA_NW>), gq, block, (1 + MA_NW) * W * 4, s, a);
+    else RG_LAUNCH((attn_masked_bwd_dq<O, true, false, MA_NW>), gq, block, W * 4, s, a);
+    RG_LAUNCH((attn_masked_bwd_dkdv<O, true, MA_NW>), gk, block, 2 * W * 4, s, a, w);
+    if (a.dtable) {
+      RG_LAUNCH(attn_bias_rows, dim3((W + 63) / 64, a.H), dim3(1024), 0, s, a, (int)(a.B * blocks_of(a.Sq)));
+      RG_LAUNCH(attn_bias_grad, dim3(a.nb, a.H), dim3(64), 0, s, a);
+    }
   } else {
     RG_LAUNCH((attn_masked_bwd_dq<O, false, false, MA_NW>), gq, block, 0, s, a);
-    RG_LAUNCH((attn_masked_bwd_dkdv<O, false, MA_NW>), gk, block, 0, s, a);
+    RG_LAUNCH((attn_masked_bwd_dkdv<O, false, MA_NW>), gk, block, 0, s, a, w);
   }
+  const int split = w.s_near > 1 ? w.nk : w.s_far > 1 ? w.nfar : 0;
+  if (split)
+    RG_LAUNCH((attn_masked_dkdv_join<O, MA_NW>), dim3((unsigned)(a.B * a.Hkv * split * MA_NW), 2), dim3(64), 0, s, a, w, split);
   return hipGetLastError();
 }
 
@@ -708,8 +895,8 @@ hipError_t launch_masked_attn_fwd(int dtype, const MaskedAttnArgs& a, hipStream_
   return a.dh <= 64 ? fwd_ops<OpsF32<64>>(a, s) : fwd_ops<OpsF32<128>>(a, s);
 }
 hipError_t launch_masked_attn_bwd(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
-  if (dtype == DT_BF16) return a.dh == 64 ? bwd_ops<OpsBf16<64>>(a, s) : bwd_ops<OpsBf16<128>>(a, s);
-  return a.dh <= 64 ? bwd_ops<OpsF32<64>>(a, s) : bwd_ops<OpsF32<128>>(a, s);
+  if (dtype == DT_BF16) return a.dh == 64 ? bwd_ops<OpsBf16<64>>(dtype, a, s) : bwd_ops<OpsBf16<128>>(dtype, a, s);
+  return a.dh <= 64 ? bwd_ops<OpsF32<64>>(dtype, a, s) : bwd_ops<OpsF32<128>>(dtype, a, s);
 }
 
 }  // namespace rg

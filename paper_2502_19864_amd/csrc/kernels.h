@@ -103,11 +103,12 @@ struct MaskedAttnArgs {
   float* dtable;              // [nb, H] or null, added into
   float* dsum;                // workspace: D [B, H, Sq]
   float* diag;                // workspace (dtable): sums of dS by relative position, per workgroup of the dQ pass
-  float* part;                // workspace of the forward
+  double* diag_sum;           // and those sums over the workgroups, [H, 2R + 1]
+  float* part;                // workspace: partial sums of workgroups that share their output rows
 };
 // bytes of the workspaces, and the backward's pointers into its own
 void masked_attn_bytes(int dtype, const MaskedAttnArgs& a, bool dtable, size_t* fwd, size_t* bwd);
-void masked_attn_workspace(MaskedAttnArgs& a, void* ws);
+void masked_attn_workspace(int dtype, MaskedAttnArgs& a, void* ws);
 hipError_t launch_masked_attn_fwd(int dtype, const MaskedAttnArgs& a, hipStream_t s);
 hipError_t launch_masked_attn_bwd(int dtype, const MaskedAttnArgs& a, hipStream_t s);
 

@@ -150,7 +150,7 @@ extern "C" ringada_status ringada_attn_backward(void* stream, const ringada_attn
   size_t need, unused;
   masked_attn_bytes(desc->dtype, a, g->dtable != nullptr, &unused, &need);
   RG_TRY(check_workspace(workspace, workspace_bytes, need));
-  masked_attn_workspace(a, workspace);
+  masked_attn_workspace(desc->dtype, a, workspace);
   RG_HIP(launch_masked_attn_bwd(desc->dtype, a, static_cast<hipStream_t>(stream)));
   return RINGADA_OK;
 }
