@@ -90,13 +90,14 @@ __device__ __forceinline__ KeyTiles key_tiles(const Mask& m, int plo, int phi) {
 }
 
 // ================================================================ storage types
-// A tile is KR rows of one head in LDS.  dma() brings rows 0 .. KR - 1 from src (rows past
-// `last` read row `last`: what they score is masked); scores() forms the block
+// A tile is KR rows of one head in LDS.  dma() brings this wave's share (of NW) of rows 0 .. ROWS - 1
+// from src (rows past `last` read row `last`: what they score is masked); scores() forms the block
 // [32 tile rows][32 own rows] (lane = own row, register r = tile row perm_pos(r)); accum() adds
 // tile^T p to acc (lane = own row, registers = head dims).
 template <int DH_>
 struct OpsBf16 {
   static constexpr int DH = DH_, KR = 64, TILE = KR * DH, STAGE = 32 * (DH + 8), WAVES = 2;
+  static constexpr int BLOCK = 32 * DH, DMAS = 32 * DH / 512;  // elements of 32 rows, and one wave's DMAs for them
   typedef bf16 E;
   struct Rows {
     bf16x8 f[DH / 16];
@@ -122,14 +123,13 @@ struct OpsBf16 {
     }
     return s + __shfl_xor(s, 32, 64);
   }
-  template <int NW>
-  static __device__ __forceinline__ void dma(const E* src, long ld, int last, E* dst, int) {
+  template <int NW, int ROWS = KR>
+  static __device__ __forceinline__ void dma(const E* src, long ld, int last, E* dst, int, int lane, int wave) {
     constexpr int CPR = DH / 8, RPI = 64 / CPR;
-    static_assert(KR % (RPI * NW) == 0, "whole DMA instructions per wave");
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    static_assert(ROWS % (RPI * NW) == 0, "whole DMA instructions per wave");
     src = uniform_ptr(src);
 #pragma unroll
-    for (int i = 0; i < KR / (RPI * NW); ++i) {
+    for (int i = 0; i < ROWS / (RPI * NW); ++i) {
       const int r = (i * NW + wave) * RPI + lane / CPR, c = (lane % CPR) ^ swz<DH>(r);
       dma16_m0(src, ((uint32_t)min(r, last) * (uint32_t)ld + c * 8) * 2, lds_addr(dst) + (i * NW + wave) * 1024);
     }
@@ -159,6 +159,7 @@ struct OpsBf16 {
 template <int DHM>
 struct OpsF32 {
   static constexpr int DH = DHM, KR = 32, P = DHM + 4, TILE = KR * P, STAGE = 32 * P, WAVES = 1;
+  static constexpr int BLOCK = TILE, DMAS = KR * DHM / 64;
   typedef float E;
   struct Rows {
     float f[DHM / 2];  // dims half * DHM / 2 + i
@@ -184,11 +185,10 @@ struct OpsF32 {
     return s + __shfl_xor(s, 32, 64);
   }
   // 4 B per lane: any alignment of the rows will do
-  template <int NW>
-  static __device__ __forceinline__ void dma(const E* src, long ld, int last, E* dst, int dh) {
+  template <int NW, int ROWS = KR>
+  static __device__ __forceinline__ void dma(const E* src, long ld, int last, E* dst, int dh, int lane, int wave) {
     constexpr int CPR = DHM / 64;
-    static_assert(KR * CPR % NW == 0, "whole DMA instructions per wave");
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    static_assert(ROWS == KR && KR * CPR % NW == 0, "whole DMA instructions per wave");
     src = uniform_ptr(src);
 #pragma unroll
     for (int i = 0; i < KR * CPR / NW; ++i) {
@@ -327,8 +327,8 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
   auto issue = [&](int i) {
     const int k0 = kt.at(i) * KR, last = sq.lk - 1 - k0;
     E* dst = sm + (i & 1) * 2 * TILE;
-    O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh);
-    O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh);
+    O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, wave);
+    O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh, lane, wave);
   };
   if (kt.n > 0) issue(0);
   typename O::Rows qf;
@@ -402,6 +402,210 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
     a.lse[(long)bh * a.Sq + q] = qv && lrun > 0.f ? mrun + log2f(lrun) : -INFINITY;
 }
 
+// ================================================================ a few queries, many keys
+// Bound by the bytes of the visible keys and values.  The queries of a key-value head (every token
+// of every query head of its group) are the 32 rows of one score block, so its keys
+// are read once for all of them; the keys are dealt to workgroups, and inside one, tile by
+// tile, to waves that run on their own: tiles of 32 keys that only their wave reads, two deep
+// by DMA, no barrier.  The waves' (maximum, sum, O) are joined in LDS, the workgroups' by
+// attn_few_join.
+// Before (attn_masked_fwd, no split): 4 x 32 heads on 8, window 32768: 876 us; 32 heads, window 1024: 29 us.
+struct FewWork {
+  int split, rb;  // workgroups over the keys, blocks of 32 rows
+};
+// the rest of a table's bias for one lane: constant beyond +-R
+struct LaneBias {
+  float lo, hi;
+  static __device__ __forceinline__ float at(const MaskedAttnArgs& a, int i, int h) {
+    const float v = a.table[(long)min(max(a.bucket[i], 0), a.nb - 1) * a.H + h];
+    return v <= kHidden ? -INFINITY : v * kLog2e;
+  }
+};
+
+template <class O, bool BIAS, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, FewWork w) {
+  typedef typename O::E E;
+  constexpr int DH = O::DH, BLOCK = O::BLOCK;
+  __shared__ __attribute__((aligned(1024))) E sm[NW][4 * BLOCK];  // per wave: [buffer][K, V]; later its O
+  __shared__ float sM[NW][32], sS[NW][32];
+  static_assert(4 * BLOCK * sizeof(E) >= 32 * DH * 4, "a wave's O fits its tiles' space");
+  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int blk = xcd_block(blockIdx.x, gridDim.x), rb = blk % w.rb, split = blk / w.rb % w.split, bh = blk / w.rb / w.split;
+  const int grp = a.H / a.Hkv, b = bh / a.Hkv, hk = bh % a.Hkv;
+  const Seq sq = seq_of(a, b);
+  const Mask mask(a, sq.lk);
+  const int row = rb * 32 + l32, tok = row / grp, h = hk * grp + row % grp, p = sq.off + tok;
+  const bool qv = tok < sq.lq;
+  const int tok0 = rb * 32 / grp, plo = sq.off + tok0, phi = sq.off + min((rb * 32 + 31) / grp, sq.lq - 1);
+  KeyTiles kt{0, 0, 0};
+  if (tok0 < sq.lq) kt = key_tiles<32>(mask, plo, phi);
+  const int per = (kt.n + w.split - 1) / w.split, i1 = min(kt.n, (split + 1) * per);
+  const float sl2 = kLog2e * a.scale;
+  const E* K = static_cast<const E*>(a.k.p) + b * a.k.b + hk * a.k.h;
+  const E* V = static_cast<const E*>(a.v.p) + b * a.v.b + hk * a.v.h;
+  O ops(lane, a.dh);
+  E* tiles = sm[wave];
+  auto issue = [&](int i, int buf) {
+    const int k0 = kt.at(i) * 32, last = sq.lk - 1 - k0;
+    E* dst = tiles + buf * 2 * BLOCK;
+    O::template dma<1, 32>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, 0);
+    O::template dma<1, 32>(V + (long)k0 * a.v.t, a.v.t, last, dst + BLOCK, a.dh, lane, 0);
+  };
+  int i = split * per + wave;
+  if (i < i1) issue(i, 0);
+  typename O::Rows qf;
+  O::load_rows(qf, static_cast<const E*>(a.q.p) + b * a.q.b + (long)(qv ? tok : 0) * a.q.t + h * a.q.h, qv, half, a.dh);
+  LaneBias lb{0.f, 0.f};
+  if (BIAS) lb = LaneBias{LaneBias::at(a, 0, h), LaneBias::at(a, 2 * a.R, h)};
+
+  f32x16 oacc[DH / 32];
+#pragma unroll
+  for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[d][r] = 0.f;
+  float mrun = -INFINITY, lrun = 0.f;
+  for (int buf = 0; i < i1; i += NW, buf ^= 1) {
+    // the other buffer's reads have ended; its next tile is under way while this one is waited for,
+    // where the counter of loads in flight (63 at most) can tell the two apart
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if constexpr (2 * O::DMAS <= 32) {
+      if (i + NW < i1) {
+        issue(i + NW, buf ^ 1);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * O::DMAS) : "memory");
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      }
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (i + NW < i1) issue(i + NW, buf ^ 1);
+    }
+    const int k0 = kt.at(i) * 32, kind = mask.block(k0, 32, plo, phi);
+    if (kind == 0) continue;
+    const E* sK = tiles + buf * 2 * BLOCK;
+    f32x16 sc;
+    ops.scores(sc, sK, 0, qf);
+    if (BIAS) {
+      if (k0 - phi >= a.R || k0 + 31 - plo <= -a.R) {
+        const float c = k0 - phi >= a.R ? lb.hi : lb.lo;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = fmaf(sc[r], sl2, c);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int rel = k0 + perm_pos(r, half) - p;
+          sc[r] = fmaf(sc[r], sl2, LaneBias::at(a, min(max(rel, -a.R), a.R) + a.R, h));
+        }
+      }
+    }
+    if (kind == 1) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sc[r] = mask.pair(p, k0 + perm_pos(r, half)) ? sc[r] : -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * (BIAS ? 1.f : sl2);
+    const float mnew = fmaxf(mrun, mx), mfin = mnew == -INFINITY ? 0.f : mnew;
+    const float alpha = __builtin_amdgcn_exp2f(mrun - mfin);
+    float rs = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      sc[r] = __builtin_amdgcn_exp2f(BIAS ? sc[r] - mfin : fmaf(sc[r], sl2, -mfin));
+      rs += sc[r];
+    }
+    lrun = lrun * alpha + rs + __shfl_xor(rs, 32, 64);
+    mrun = mnew;
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[d][r] *= alpha;
+    ops.accum(oacc, sK + BLOCK, 0, sc);
+  }
+
+  // join the waves: O in the accumulators' own order
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  float4* so = reinterpret_cast<float4*>(tiles) + lane;
+#pragma unroll
+  for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      so[(d * 4 + g) * 64] = make_float4(oacc[d][4 * g], oacc[d][4 * g + 1], oacc[d][4 * g + 2], oacc[d][4 * g + 3]);
+  if (half == 0) {
+    sM[wave][l32] = mrun;
+    sS[wave][l32] = lrun;
+  }
+  __syncthreads();
+  float M = -INFINITY, L = 0.f, f[NW];
+#pragma unroll
+  for (int k = 0; k < NW; ++k) M = qv ? fmaxf(M, sM[k][l32]) : -INFINITY;
+#pragma unroll
+  for (int k = 0; k < NW; ++k) {
+    f[k] = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sM[k][l32] - M);
+    L = fmaf(sS[k][l32], f[k], L);
+  }
+  if (tok >= a.Sq) return;
+  const float inv = L > 0.f ? 1.f / L : 0.f;
+  float* po = a.part + ((long)blk * 32 + l32) * DH;
+  E* o = static_cast<E*>(a.o.p) + b * a.o.b + (long)tok * a.o.t + h * a.o.h;
+  for (int d = wave; d < DH / 32; d += NW)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < NW; ++k) {
+        const float4 x = reinterpret_cast<const float4*>(sm[k])[(d * 4 + g) * 64 + lane];
+        v[0] = fmaf(x.x, f[k], v[0]);
+        v[1] = fmaf(x.y, f[k], v[1]);
+        v[2] = fmaf(x.z, f[k], v[2]);
+        v[3] = fmaf(x.w, f[k], v[3]);
+      }
+      const int c = d * 32 + 8 * g + 4 * half;
+      if (w.split > 1) {
+        St<float>::st4(po, c, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < a.dh) St<E>::st(o, c + e, v[e] * inv);
+      }
+    }
+  if (wave == 0 && half == 0) {
+    if (w.split > 1) reinterpret_cast<float2*>(a.part + (long)gridDim.x * 32 * DH)[(long)blk * 32 + l32] = make_float2(M, L);
+    else if (a.lse) a.lse[((long)b * a.H + h) * a.Sq + tok] = L > 0.f ? M + log2f(L) : -INFINITY;
+  }
+}
+
+// joins a row's partial results (at most 64) in order; one wave per row
+template <class O>
+__global__ __launch_bounds__(256) void attn_few_join(MaskedAttnArgs a, FewWork w) {
+  typedef typename O::E E;
+  constexpr int DH = O::DH;
+  const int lane = threadIdx.x & 63, grp = a.H / a.Hkv, rows = a.Sq * grp;
+  const long id = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (id >= (long)a.B * a.Hkv * rows) return;
+  const int bh = (int)(id / rows), row = (int)(id % rows), b = bh / a.Hkv, hk = bh % a.Hkv;
+  const long blk0 = ((long)bh * w.split) * w.rb + row / 32, n = (long)a.B * a.Hkv * w.split * w.rb;
+  const float2 ml = lane < w.split ? reinterpret_cast<const float2*>(a.part + n * 32 * DH)[(blk0 + (long)lane * w.rb) * 32 + row % 32]
+                                   : make_float2(-INFINITY, 0.f);
+  const float M = wave_max(ml.x), f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M), L = wave_sum(ml.y * f);
+  float acc[DH / 64];
+#pragma unroll
+  for (int d = 0; d < DH / 64; ++d) acc[d] = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < w.split; ++s) {
+    const float fs = __shfl(f, s, 64);
+    const float* src = a.part + ((blk0 + (long)s * w.rb) * 32 + row % 32) * DH + lane;
+#pragma unroll
+    for (int d = 0; d < DH / 64; ++d) acc[d] = fmaf(src[64 * d], fs, acc[d]);
+  }
+  const int tok = row / grp, h = hk * grp + row % grp;
+  E* o = static_cast<E*>(a.o.p) + b * a.o.b + (long)tok * a.o.t + h * a.o.h;
+#pragma unroll
+  for (int d = 0; d < DH / 64; ++d)
+    if (lane + 64 * d < a.dh) St<E>::st(o, lane + 64 * d, L > 0.f ? acc[d] / L : 0.f);
+  if (a.lse && lane == 0) a.lse[((long)b * a.H + h) * a.Sq + tok] = L > 0.f ? M + log2f(L) : -INFINITY;
+}
+
 // ================================================================ backward
 // exponent offset of a row that sees nothing: exp2(x - inf) = 0
 __device__ __forceinline__ float lse_or_inf(float l) { return l == -INFINITY ? INFINITY : l; }
@@ -438,8 +642,8 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   auto issue = [&](int i) {
     const int k0 = kt.at(DTAB && i >= kt.n ? i - kt.n : i) * KR, last = sq.lk - 1 - k0;
     E* dst = sm + (i & 1) * 2 * TILE;
-    O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh);
-    O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh);
+    O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, wave);
+    O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh, lane, wave);
   };
   if (nit > 0) issue(0);
   const long row = qv ? q : 0;
@@ -620,9 +824,9 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
   auto issue = [&](int buf) {
     const int r0 = (qt0 + t) * KR, last = sq.lq - 1 - r0;
     E* dst = sm + buf * 2 * TILE;
-    O::template dma<NW>(static_cast<const E*>(a.q.p) + b * a.q.b + h * a.q.h + (long)r0 * a.q.t, a.q.t, last, dst, a.dh);
+    O::template dma<NW>(static_cast<const E*>(a.q.p) + b * a.q.b + h * a.q.h + (long)r0 * a.q.t, a.q.t, last, dst, a.dh, lane, wave);
     O::template dma<NW>(static_cast<const E*>(a.dout.p) + b * a.dout.b + h * a.dout.h + (long)r0 * a.dout.t, a.dout.t,
-                        last, dst + TILE, a.dh);
+                        last, dst + TILE, a.dh, lane, wave);
   };
   // that iteration's row statistics, one query per thread of the first KR
   auto load_stats = [&](float& lv, float& dv) {
@@ -846,8 +1050,25 @@ static BwdSpace bwd_space(int dtype, const MaskedAttnArgs& a, bool dtable) {
   return s;
 }
 
+// A few queries against many keys: all rows of a key-value head in at most four blocks.
+static bool few(const MaskedAttnArgs& a) { return (long)a.Sq * (a.H / a.Hkv) <= 128; }
+// One workgroup per CU and as many as there are tiles for its waves, with two tiles each.
+static FewWork few_work(const MaskedAttnArgs& a) {
+  FewWork w;
+  w.rb = (a.Sq * (a.H / a.Hkv) + 31) / 32;
+  const long span = a.window ? std::min<long>(a.Sk, (long)a.Sq + (a.causal ? 1 : 2) * (long)a.window + a.sinks) : a.Sk;
+  const long wgs = (long)a.B * a.Hkv * w.rb;
+  w.split = (int)std::max(1l, std::min({64l, (256 + wgs - 1) / wgs, span / 256}));
+  return w;
+}
+
 void masked_attn_bytes(int dtype, const MaskedAttnArgs& a, bool dtable, size_t* fwd, size_t* bwd) {
   *fwd = 0;
+  if (few(a)) {
+    const FewWork w = few_work(a);
+    const int dh = a.dh <= 64 ? 64 : 128;
+    if (w.split > 1) *fwd = (size_t)a.B * a.Hkv * w.split * w.rb * 32 * (dh + 2) * 4;
+  }
   *bwd = bwd_space(dtype, a, dtable).total;
 }
 
@@ -860,6 +1081,17 @@ void masked_attn_workspace(int dtype, MaskedAttnArgs& a, void* ws) {
   a.part = reinterpret_cast<float*>(p + s.part);
 }
 
+// NW: waves whose private tiles fit the LDS of a CU
+template <class O, int NW>
+static hipError_t few_ops(const MaskedAttnArgs& a, hipStream_t s) {
+  const FewWork w = few_work(a);
+  const dim3 grid((unsigned)((long)a.B * a.Hkv * w.split * w.rb)), block(64 * NW);
+  if (a.table) RG_LAUNCH((attn_few_fwd<O, true, NW>), grid, block, 0, s, a, w);
+  else RG_LAUNCH((attn_few_fwd<O, false, NW>), grid, block, 0, s, a, w);
+  if (w.split > 1)
+    RG_LAUNCH((attn_few_join<O>), dim3((unsigned)(((long)a.B * a.H * a.Sq + 3) / 4)), dim3(256), 0, s, a, w);
+  return hipGetLastError();
+}
 template <class O>
 static hipError_t fwd_ops(const MaskedAttnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(blocks_of(a.Sq) * a.B * a.H)), block(64 * MA_NW);
@@ -891,6 +1123,10 @@ static hipError_t bwd_ops(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_masked_attn_fwd(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
+  if (few(a)) {
+    if (dtype == DT_BF16) return a.dh == 64 ? few_ops<OpsBf16<64>, 4>(a, s) : few_ops<OpsBf16<128>, 4>(a, s);
+    return a.dh <= 64 ? few_ops<OpsF32<64>, 4>(a, s) : few_ops<OpsF32<128>, 2>(a, s);
+  }
   if (dtype == DT_BF16) return a.dh == 64 ? fwd_ops<OpsBf16<64>>(a, s) : fwd_ops<OpsBf16<128>>(a, s);
   return a.dh <= 64 ? fwd_ops<OpsF32<64>>(a, s) : fwd_ops<OpsF32<128>>(a, s);
 }

@@ -42,6 +42,15 @@ CASES = [
     A("bf16", 2, 4, 1, 128, 260, causal=True, window=70, sinks=5, nb=64, dist=512, len_q=[260, 100], len_k=[260, 100]),
     A("bf16", 2, 2, 2, 64, 50, 130, causal=True, nb=8, dist=9, len_q=[50, 20], len_k=[130, 77]),
     A("bf16", 1, 2, 2, 64, 90, causal=False, nb=2, dist=0),
+    # a few queries against a long cache: split over its keys, shared heads packed into one block
+    A("bf16", 2, 8, 2, 128, 1, 3000, causal=True),
+    A("bf16", 1, 4, 4, 64, 1, 2100, causal=True, window=1000, sinks=5),
+    A("bf16", 3, 16, 2, 128, 5, 1500, causal=True, window=700, sinks=40, len_q=[5, 3, 0], len_k=[1500, 1, 900]),
+    A("bf16", 2, 8, 1, 64, 9, 777, causal=True, nb=32, dist=128, len_q=[9, 4], len_k=[700, 777]),
+    A("bf16", 1, 2, 1, 128, 3, 600, causal=False, window=50, sinks=300, nb=16, dist=40),
+    A("bf16", 2, 2, 2, 64, 128, 129, causal=True, len_q=[128, 77], len_k=[60, 129]),
+    A("f32", 2, 4, 2, 128, 1, 1111, causal=True, window=600, sinks=2),
+    A("f32", 2, 6, 2, 40, 4, 700, causal=True, nb=8, dist=20, len_q=[4, 2], len_k=[700, 99]),
     # fp32, head dims that are not a tile's
     A("f32", 1, 1, 1, 1, 5),
     A("f32", 4, 2, 2, 64, 32, causal=False, window=9, sinks=1, nb=16, dist=12),
@@ -112,7 +121,7 @@ def test_attention_matches_float64(c):
         print(n, R.check(n, got[n], *want[n]), flush=True)
 
 
-@pytest.mark.parametrize("i", [6, 11, 18, 24])
+@pytest.mark.parametrize("i", [6, 11, 18, 22, 24, 31])
 def test_attention_repeats_bit_for_bit_and_with_a_frozen_table(i):
     import torch
 
