@@ -213,6 +213,44 @@ ringada_status ringada_stage_sync_adapters(ringada_stage* st, void* stream);
  * caller's). */
 void ringada_stage_destroy(ringada_stage* st);
 
+/* ---------------------------------------------------------------- options of a stage
+ * Both are set on a handle after ringada_stage_create, hold for every later forward
+ * and backward until they are set again, and return RINGADA_E_STATE while a forward
+ * is pending its backward. */
+
+/* Attention of every block with a sliding window, sinks and a relative position
+ * bias; the fields are those of ringada_attn_desc and ringada_attn_tensors.  One table
+ * serves all blocks; g_table (NULL: a frozen table) is ADDED into by the backward,
+ * over the blocks whose attention it passes.  The memory is borrowed until the
+ * options are set again or the stage is destroyed. */
+typedef struct {
+  int32_t window, sinks;
+  int32_t n_buckets, max_distance;
+  const float* table;     /* [n_buckets, n_heads], NULL when n_buckets is 0 */
+  const int32_t* bucket;  /* [2 max_distance + 1] */
+  float* g_table;
+  void* workspace;        /* at least the bytes of ringada_stage_plan_attention, 256-byte aligned */
+  size_t workspace_bytes;
+} ringada_stage_attention;
+
+/* Host only.  Bytes of opt->workspace that a forward and backward of (batch, seq)
+ * need; only the integers of opt and whether g_table is NULL are looked at. */
+ringada_status ringada_stage_plan_attention(const ringada_stage_desc* desc,
+                                            const ringada_stage_attention* opt, int32_t batch,
+                                            int32_t seq, size_t* workspace_bytes);
+
+/* opt NULL, or without a window and buckets: the plain attention.  A forward whose
+ * (batch, seq) needs a larger workspace returns RINGADA_E_WORKSPACE. */
+ringada_status ringada_stage_set_attention(ringada_stage* st, const ringada_stage_attention* opt);
+
+/* Dropout with probability p (0: none) on each sublayer's output, before its
+ * adapter and the residual add (ringada_dropout's masks, with site first_site + 2 l for
+ * block l's attention sublayer and first_site + 2 l + 1 for its FFN).  The backward
+ * reads rng again: {seed, offset} must stay as its forward found them until it has
+ * run.  Forwards of a frozen stage drop too. */
+ringada_status ringada_stage_set_dropout(ringada_stage* st, float p, const uint64_t* rng,
+                                         uint32_t first_site);
+
 /* ---------------------------------------------------------------- hot path */
 
 /* Forward through all n_blocks blocks: y = blocks(x), x and y [batch, seq, d]

@@ -143,10 +143,13 @@ def merge_heads(x):
     return x.transpose(0, 2, 1, 3).reshape(B * S, H * dh)
 
 
-def attention_fwd(q, k, v, causal):
-    """softmax(q k^T / sqrt(dh) [+ causal mask]) v over [B, H, S, dh]."""
+def attention_fwd(q, k, v, causal, add=None):
+    """softmax(q k^T / sqrt(dh) [+ add] [+ causal mask]) v over [B, H, S, dh]; add: [H, S, S],
+    a bias on the scores, -inf where a window hides a pair."""
     dh = q.shape[-1]
     s = (q @ np.swapaxes(k, -1, -2)) / math.sqrt(dh)
+    if add is not None:
+        s = s + add
     if causal:
         S = s.shape[-1]
         s = np.where(np.triu(np.ones((S, S), dtype=bool), 1), -np.inf, s)
@@ -165,6 +168,12 @@ def attention_bwd(do, q, k, v, p):
     dq = (ds @ k) / math.sqrt(dh)
     dk = (np.swapaxes(ds, -1, -2) @ q) / math.sqrt(dh)
     return dq, dk, dv
+
+
+def attention_score_grad(do, v, p):
+    """Gradient of the scores of attention_fwd, so of a bias on them: [B, H, S, S]."""
+    dp = do @ np.swapaxes(v, -1, -2)
+    return p * (dp - (dp * p).sum(axis=-1, keepdims=True))
 
 
 def rope_tables(S, dh, theta, dtype):
@@ -195,7 +204,11 @@ def rope_bwd(dy, cos, sin):
 def make_desc(arch, n_blocks, d_model, n_heads, d_ffn, d_adapter,
               norm_eps=None, rope_theta=10000.0, placement="houlsby"):
     """arch is 'bert' (post-LN, GELU FFN, bidirectional) or 'llama'
-    (pre-RMSNorm, SwiGLU FFN, RoPE, causal).  placement is 'houlsby' (an
+    (pre-RMSNorm, SwiGLU FFN, RoPE, causal).  The description may be given
+    score_add, attention_fwd's add for every block (the backward then leaves the
+    scores' gradient in the block's cache as dscore), and a block's weights
+    keep_attn and keep_ffn [B*S, d], factors on its sublayers' outputs before the
+    adapters (dropout).  placement is 'houlsby' (an
     adapter on the attention and on the FFN sublayer of every block) or
     'ffn' (the single adapter after the feed-forward sublayer, Sec. II-A)."""
     if norm_eps is None:
@@ -221,16 +234,16 @@ def bert_block_fwd(desc, w, ad, x, B, S):
     q = split_heads(qkv[:, :d], B, S, H)
     k = split_heads(qkv[:, d:2 * d], B, S, H)
     v = split_heads(qkv[:, 2 * d:], B, S, H)
-    o_h, p = attention_fwd(q, k, v, causal=False)
+    o_h, p = attention_fwd(q, k, v, causal=False, add=desc.get("score_add"))
     o = merge_heads(o_h)
-    attn = o @ w["w_o"] + w["b_o"]
+    attn = (o @ w["w_o"] + w["b_o"]) * w.get("keep_attn", 1.0)
     if _single(desc):
         a, u1 = attn, None
     else:
         a, u1 = adapter_fwd(attn, ad[0]["w_down"], ad[0]["w_up"])
     h1, xhat1, rstd1 = layer_norm(x + a, w["ln1_g"], w["ln1_b"], eps)
     a1 = h1 @ w["w_i"] + w["b_i"]
-    f2 = gelu(a1) @ w["w_f"] + w["b_f"]
+    f2 = (gelu(a1) @ w["w_f"] + w["b_f"]) * w.get("keep_ffn", 1.0)
     fa, u2 = adapter_fwd(f2, ad[1]["w_down"], ad[1]["w_up"])
     y, xhat2, rstd2 = layer_norm(h1 + fa, w["ln2_g"], w["ln2_b"], eps)
     cache = dict(q=q, k=k, v=v, p=p, attn=attn, u1=u1, xhat1=xhat1,
@@ -252,6 +265,7 @@ def bert_block_bwd(desc, w, ad, c, dy, B, S, stop):
     g_ffn = {"w_down": gdn2, "w_up": gup2}
     if single and stop:
         return None, (None, g_ffn)
+    df2 = df2 * w.get("keep_ffn", 1.0)
     da1 = (df2 @ w["w_f"].T) * gelu_grad(c["a1"])
     dh1 = dz2 + da1 @ w["w_i"].T
     dz1 = layer_norm_bwd(dh1, w["ln1_g"], c["xhat1"], c["rstd1"])
@@ -264,7 +278,10 @@ def bert_block_bwd(desc, w, ad, c, dy, B, S, stop):
         grads = ({"w_down": gdn1, "w_up": gup1}, g_ffn)
     if stop:
         return None, grads
-    do = split_heads(dattn @ w["w_o"].T, B, S, desc["n_heads"])
+    do = split_heads((dattn * w.get("keep_attn", 1.0)) @ w["w_o"].T, B, S,
+                     desc["n_heads"])
+    if "score_add" in desc:
+        c["dscore"] = attention_score_grad(do, c["v"], c["p"])
     dq, dk, dv = attention_bwd(do, c["q"], c["k"], c["v"], c["p"])
     dqkv = np.concatenate([merge_heads(dq), merge_heads(dk), merge_heads(dv)],
                           axis=1)
@@ -285,8 +302,8 @@ def llama_block_fwd(desc, w, ad, x, B, S):
     q = rope_fwd(split_heads(qkv[:, :d], B, S, H), cos, sin)
     k = rope_fwd(split_heads(qkv[:, d:2 * d], B, S, H), cos, sin)
     v = split_heads(qkv[:, 2 * d:], B, S, H)
-    o_h, p = attention_fwd(q, k, v, causal=True)
-    attn = merge_heads(o_h) @ w["w_o"]
+    o_h, p = attention_fwd(q, k, v, causal=True, add=desc.get("score_add"))
+    attn = (merge_heads(o_h) @ w["w_o"]) * w.get("keep_attn", 1.0)
     if _single(desc):
         a, u1 = attn, None
     else:
@@ -295,7 +312,7 @@ def llama_block_fwd(desc, w, ad, x, B, S):
     n2, xhat2, rstd2 = rms_norm(h, w["rms2_g"], eps)
     gu = n2 @ w["w_gu"]
     gate, up = gu[:, :F], gu[:, F:]
-    f = (silu(gate) * up) @ w["w_d"]
+    f = ((silu(gate) * up) @ w["w_d"]) * w.get("keep_ffn", 1.0)
     fa, u2 = adapter_fwd(f, ad[1]["w_down"], ad[1]["w_up"])
     y = h + fa
     cache = dict(xhat1=xhat1, rstd1=rstd1, q=q, k=k, v=v, p=p, attn=attn,
@@ -314,7 +331,7 @@ def llama_block_bwd(desc, w, ad, c, dy, B, S, stop):
     g_ffn = {"w_down": gdn2, "w_up": gup2}
     if single and stop:
         return None, (None, g_ffn)
-    dact = df @ w["w_d"].T
+    dact = (df * w.get("keep_ffn", 1.0)) @ w["w_d"].T
     dgate = dact * c["up"] * silu_grad(c["gate"])
     dup = dact * silu(c["gate"])
     dn2 = np.concatenate([dgate, dup], axis=1) @ w["w_gu"].T
@@ -328,7 +345,9 @@ def llama_block_bwd(desc, w, ad, c, dy, B, S, stop):
         grads = ({"w_down": gdn1, "w_up": gup1}, g_ffn)
     if stop:
         return None, grads
-    do = split_heads(dattn @ w["w_o"].T, B, S, H)
+    do = split_heads((dattn * w.get("keep_attn", 1.0)) @ w["w_o"].T, B, S, H)
+    if "score_add" in desc:
+        c["dscore"] = attention_score_grad(do, c["v"], c["p"])
     dq, dk, dv = attention_bwd(do, c["q"], c["k"], c["v"], c["p"])
     dq = rope_bwd(dq, c["cos"], c["sin"])
     dk = rope_bwd(dk, c["cos"], c["sin"])

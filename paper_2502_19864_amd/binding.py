@@ -64,6 +64,12 @@ class AttnTensors(ctypes.Structure):
                 ("len_k", c_void_p), ("table", c_void_p), ("bucket", c_void_p)]
 
 
+class StageAttention(ctypes.Structure):
+    _fields_ = [("window", c_int32), ("sinks", c_int32), ("n_buckets", c_int32), ("max_distance", c_int32),
+                ("table", c_void_p), ("bucket", c_void_p), ("g_table", c_void_p), ("workspace", c_void_p),
+                ("workspace_bytes", c_size_t)]
+
+
 class AttnGrads(ctypes.Structure):
     _fields_ = [("dout", View), ("dq", View), ("dk", View), ("dv", View), ("dtable", c_void_p)]
 
@@ -79,6 +85,10 @@ SIGNATURES = [
                                            POINTER(Adapter), c_void_p, c_size_t, c_void_p]),
     ("ringada_stage_sync_adapters", c_int32, [c_void_p, c_void_p]),
     ("ringada_stage_destroy", None, [c_void_p]),
+    ("ringada_stage_plan_attention", c_int32, [POINTER(StageDesc), POINTER(StageAttention), c_int32, c_int32,
+                                               POINTER(c_size_t)]),
+    ("ringada_stage_set_attention", c_int32, [c_void_p, POINTER(StageAttention)]),
+    ("ringada_stage_set_dropout", c_int32, [c_void_p, c_float, c_void_p, c_uint32]),
     ("ringada_stage_forward", c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32,
                                         c_void_p, c_size_t, c_void_p, c_size_t]),
     ("ringada_stage_backward", c_int32, [c_void_p, c_void_p, c_void_p, c_int32, c_void_p]),
@@ -168,6 +178,21 @@ def ringada_stage_sync_adapters(stage, stream):
 
 def ringada_stage_destroy(stage):
     lib().ringada_stage_destroy(stage)
+
+
+def ringada_stage_plan_attention(desc, opt, batch, seq):
+    n = c_size_t(0)
+    _check(lib().ringada_stage_plan_attention(byref(desc), byref(opt), batch, seq, byref(n)))
+    return n.value
+
+
+def ringada_stage_set_attention(stage, opt):
+    """opt None: the plain attention."""
+    _check(lib().ringada_stage_set_attention(stage, None if opt is None else byref(opt)))
+
+
+def ringada_stage_set_dropout(stage, p, rng, first_site):
+    _check(lib().ringada_stage_set_dropout(stage, p, _p(rng), first_site))
 
 
 def ringada_stage_forward(stage, stream, x, y, batch, seq, lowest_unfrozen, stash, stash_bytes, scratch,

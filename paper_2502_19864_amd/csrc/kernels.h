@@ -83,6 +83,7 @@ hipError_t launch_attn_bwd(int dtype, const AttnArgs& a, hipStream_t s);
 
 // Attention with a sliding window, sinks and a relative position bias (k_attn_masked.hip has
 // the formulas).  Element (b, row, head, i) of a view is p[b * b + row * t + head * h + i].
+constexpr int ATTN_MAX_DISTANCE = 1024;  // R: a head's bias and four waves' diagonal sums share the LDS with the tiles
 struct View {
   void* p;
   long b, t, h;
@@ -99,6 +100,7 @@ struct MaskedAttnArgs {
   const int* bucket;          // [2R + 1], taken into [0, nb)
   int R, nb;
   // backward
+  const float2* rope_tab;     // bf16: q and k come rotated (positions = rows); dq and dk are rotated back; or null
   View dout, dq, dk, dv;
   float* dtable;              // [nb, H] or null, added into
   float* dsum;                // workspace: D [B, H, Sq]

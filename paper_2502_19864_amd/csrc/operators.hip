@@ -11,8 +11,6 @@
 
 using namespace rg;
 
-static constexpr int MAX_R = 1024;
-
 static ringada_status check_attn(const ringada_attn_desc* D) {
   if (!D) return fail(RINGADA_E_INVALID, "desc is NULL");
   if (D->dtype != RINGADA_F32 && D->dtype != RINGADA_BF16) return fail(RINGADA_E_INVALID, "unknown dtype %d", D->dtype);
@@ -23,7 +21,7 @@ static ringada_status check_attn(const ringada_attn_desc* D) {
   if (!(D->scale > 0.f) || !isfinite(D->scale)) return fail(RINGADA_E_INVALID, "scale must be positive and finite");
   if (D->n_buckets < 0 || D->n_buckets > 65535 || D->max_distance < 0)
     return fail(RINGADA_E_INVALID, "n_buckets must be in [0, 65535] and max_distance >= 0");
-  if (D->max_distance > MAX_R) return fail(RINGADA_E_UNSUPPORTED, "max_distance above %d", MAX_R);
+  if (D->max_distance > ATTN_MAX_DISTANCE) return fail(RINGADA_E_UNSUPPORTED, "max_distance above %d", ATTN_MAX_DISTANCE);
   if (D->dtype == RINGADA_BF16 && D->d_head != 64 && D->d_head != 128)
     return fail(RINGADA_E_UNSUPPORTED, "bf16 path: d_head must be 64 or 128 (got %d)", D->d_head);
   if (D->d_head > 128) return fail(RINGADA_E_UNSUPPORTED, "f32 path: d_head must be at most 128 (got %d)", D->d_head);
@@ -161,8 +159,8 @@ extern "C" ringada_status ringada_relpos_buckets(int32_t n_buckets, int32_t max_
   const int n = bidirectional ? n_buckets / 2 : n_buckets, one = n / 2;
   if (n_buckets < 2 || (bidirectional && n_buckets % 2) || one < 1)
     return fail(RINGADA_E_INVALID, "n_buckets must be at least 2, or a multiple of 2 from 4 when bidirectional");
-  if (max_distance <= one || max_distance > MAX_R)
-    return fail(RINGADA_E_INVALID, "max_distance must be in (%d, %d]", one, MAX_R);
+  if (max_distance <= one || max_distance > ATTN_MAX_DISTANCE)
+    return fail(RINGADA_E_INVALID, "max_distance must be in (%d, %d]", one, ATTN_MAX_DISTANCE);
   for (int r = -max_distance; r <= max_distance; ++r) {
     const int d = bidirectional ? (r < 0 ? -r : r) : (r < 0 ? -r : 0);
     int t = d;

@@ -315,6 +315,12 @@ struct ringada_stage {
   // 128x192 tile of the QKV projection is then one head of one sequence, and
   // 128-token sequences take the attention in that GEMM's epilogue
   bool qkv_per_head = false;
+  // options: the attention's mask and bias (masked: any of them is set), and dropout
+  bool masked = false;
+  ringada_stage_attention att{};
+  float drop_p = 0.f;
+  const uint64_t* drop_rng = nullptr;
+  uint32_t drop_site = 0;
   // weight-gradient work of the adapters back-propagated so far in this
   // backward, launched together when it ends
   std::vector<AdapterDwArgs> dw_pending;
@@ -551,6 +557,115 @@ static ringada_status gemm(const Ctx& c, Role role, Epi epi, int M, int N, int K
   return run(c.st, c.s, role_name(role), flops, bytes, [&] { return launch_gemm(c.dt, role, epi, g, c.s); });
 }
 
+// ================================================================ options
+static ringada_status check_attention(const ringada_stage_attention* o) {
+  if (o->window < 0 || o->sinks < 0) return fail(RINGADA_E_INVALID, "window and sinks must be >= 0");
+  if (o->n_buckets < 0 || o->n_buckets > 65535 || o->max_distance < 0)
+    return fail(RINGADA_E_INVALID, "n_buckets must be in [0, 65535] and max_distance >= 0");
+  if (o->max_distance > ATTN_MAX_DISTANCE) return fail(RINGADA_E_UNSUPPORTED, "max_distance above %d", ATTN_MAX_DISTANCE);
+  return RINGADA_OK;
+}
+
+// the sizes and mask of a block's attention under the options
+static MaskedAttnArgs masked_attn_sizes(const ringada_stage_desc& D, const ringada_stage_attention& o, int B, int S) {
+  MaskedAttnArgs a{};
+  a.B = B; a.H = a.Hkv = D.n_heads; a.dh = D.d_model / D.n_heads; a.Sq = a.Sk = S;
+  a.causal = D.arch == RINGADA_ARCH_PRERMS_SWIGLU;
+  a.window = o.window >= 2 * (int64_t)S ? 0 : o.window;
+  a.sinks = std::min(o.sinks, S);
+  a.scale = 1.f / std::sqrt((float)a.dh);
+  a.nb = o.n_buckets;
+  a.R = o.n_buckets ? o.max_distance : 0;
+  a.table = o.table;
+  a.bucket = o.bucket;
+  return a;
+}
+
+static size_t masked_attn_need(const ringada_stage_desc& D, const ringada_stage_attention& o, int B, int S) {
+  size_t f, b;
+  masked_attn_bytes(D.dtype, masked_attn_sizes(D, o, B, S), o.n_buckets && o.g_table, &f, &b);
+  return std::max(f, b);
+}
+
+extern "C" ringada_status ringada_stage_plan_attention(const ringada_stage_desc* desc,
+                                                       const ringada_stage_attention* opt, int32_t batch, int32_t seq,
+                                                       size_t* workspace_bytes) {
+  RG_TRY(check_desc(desc));
+  if (!opt || !workspace_bytes) return fail(RINGADA_E_INVALID, "NULL argument");
+  RG_TRY(check_attention(opt));
+  if (batch < 1 || seq < 1 || batch > desc->max_batch || seq > desc->max_seq)
+    return fail(RINGADA_E_INVALID, "batch %d / seq %d outside [1, max]", batch, seq);
+  *workspace_bytes = opt->window || opt->n_buckets ? masked_attn_need(*desc, *opt, batch, seq) : 0;
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_stage_set_attention(ringada_stage* st, const ringada_stage_attention* opt) {
+  if (!st) return fail(RINGADA_E_INVALID, "NULL stage");
+  if (st->pending) return fail(RINGADA_E_STATE, "a forward is pending its backward");
+  if (!opt) {
+    st->masked = false;
+    return RINGADA_OK;
+  }
+  RG_TRY(check_attention(opt));
+  if ((opt->table != nullptr) != (opt->n_buckets > 0) || (opt->table && !opt->bucket) || (opt->g_table && !opt->table))
+    return fail(RINGADA_E_INVALID, "table and bucket must be given exactly when n_buckets > 0");
+  if (reinterpret_cast<uintptr_t>(opt->workspace) & 255u)
+    return fail(RINGADA_E_INVALID, "workspace must be 256-byte aligned");
+  st->att = *opt;
+  st->masked = opt->window > 0 || opt->n_buckets > 0;
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_stage_set_dropout(ringada_stage* st, float p, const uint64_t* rng,
+                                                    uint32_t first_site) {
+  if (!st) return fail(RINGADA_E_INVALID, "NULL stage");
+  if (st->pending) return fail(RINGADA_E_STATE, "a forward is pending its backward");
+  if (!(p >= 0.f && p < 1.f) || dropout_threshold(p) > 65535) return fail(RINGADA_E_INVALID, "p must be in [0, 1)");
+  if (p > 0.f && (!rng || (reinterpret_cast<uintptr_t>(rng) & 7u)))
+    return fail(RINGADA_E_INVALID, "dropout needs rng, 8-byte aligned");
+  st->drop_p = p;
+  st->drop_rng = rng;
+  st->drop_site = first_site;
+  return RINGADA_OK;
+}
+
+// dropout of block l's sublayer (0 attention, 1 FFN) on a [T, d] tensor
+static ringada_status drop(const Ctx& c, int l, int sublayer, const void* x, void* y) {
+  ringada_stage* st = c.st;
+  return run(st, c.s, "dropout", 0, (double)c.es * 2.0 * c.T * c.d, [&] {
+    return launch_dropout(c.dt, x, nullptr, y, (long)c.T * c.d, dropout_threshold(st->drop_p), st->drop_rng,
+                          st->drop_site + 2 * (uint32_t)l + sublayer, c.s);
+  });
+}
+
+// a block's attention under the options: views of the [T, 3d] projection
+static MaskedAttnArgs masked_attn_args(const Ctx& c, const void* qkv, void* o, float* lse) {
+  const ringada_stage* st = c.st;
+  const Layout& L = st->L;
+  MaskedAttnArgs a = masked_attn_sizes(st->D, st->att, L.B, L.S);
+  const long hs = st->qkv_per_head ? 3 * c.dh : c.dh, ko = st->qkv_per_head ? c.dh : c.d;
+  char* base = static_cast<char*>(const_cast<void*>(qkv));
+  const long row = 3 * c.d;
+  a.q = View{base, L.S * row, row, hs};
+  a.k = View{base + ko * c.es, L.S * row, row, hs};
+  a.v = View{base + 2 * ko * c.es, L.S * row, row, hs};
+  a.o = View{o, (long)L.S * c.d, c.d, c.dh};
+  a.lse = lse;
+  a.part = static_cast<float*>(st->att.workspace);
+  return a;
+}
+
+// pairs that a head's queries see, summed over a batch
+static double masked_pairs(const MaskedAttnArgs& a) {
+  double n = 0;
+  for (int p = 0; p < a.Sq; ++p) {
+    const int hi = a.causal ? p + 1 : a.window ? std::min(a.Sk, p + a.window) : a.Sk;
+    const int lo = a.window ? std::max(0, p - a.window + 1) : 0;
+    n += hi - lo + (a.window ? std::min(lo, a.sinks) + (a.causal ? 0 : std::max(0, a.sinks - hi)) : 0);
+  }
+  return n * a.B;
+}
+
 // ================================================================ forward
 static ringada_status block_forward(const Ctx& c, int l, const void* X, void* Y) {
   ringada_stage* st = c.st;
@@ -582,7 +697,7 @@ static ringada_status block_forward(const Ctx& c, int l, const void* X, void* Y)
     xin = n1;
   }
   const double attn_flops = 4.0 * L.B * c.H * (double)L.S * L.S * c.dh * (c.llama ? 0.5 : 1.0);
-  if (st->qkv_per_head && L.S == 128) {
+  if (st->qkv_per_head && L.S == 128 && !st->masked) {
     // projection + attention in one kernel; the projections leave it only
     // when the backward needs them
     GemmArgs g{xin, d, b.wt_qkv, d, T, 3 * d, d, b.bqkv, nullptr, 0, SN(sb.qkv), 3 * d, o, d, 0};
@@ -603,15 +718,22 @@ static ringada_status block_forward(const Ctx& c, int l, const void* X, void* Y)
       RG_TRY(gemm(c, R_QKV_FWD, Epi::Store, T, 3 * d, d, xin, d, b.wt_qkv, d, qkv, 3 * d,
                   st->qkv_per_head ? b.bqkv : b.w.b_qkv));
     }
-    AttnArgs aa{};
-    aa.B = L.B; aa.S = L.S; aa.H = c.H; aa.dh = c.dh;
-    aa.causal = c.llama; aa.rope = c.llama;
-    aa.rope_tab = st->rope_tab; aa.rope_rows = st->D.max_seq;
-    aa.qkv = qkv; aa.ld_qkv = 3 * d; aa.o = o; aa.ld_o = d; aa.lse = lse;
-    if (st->qkv_per_head) { aa.qkv_hs = 3 * c.dh; aa.qkv_ko = c.dh; aa.qkv_vo = 2 * c.dh; }
-    RG_TRY(run(st, c.s, "attn_fwd", attn_flops, es * 4.0 * T * d, [&] { return launch_attn_fwd(c.dt, aa, c.s); }));
+    if (st->masked) {
+      const MaskedAttnArgs ma = masked_attn_args(c, qkv, o, lse);
+      RG_TRY(run(st, c.s, "attn_masked_fwd", st->prof ? 4.0 * c.H * c.dh * masked_pairs(ma) : 0, es * 4.0 * T * d,
+                 [&] { return launch_masked_attn_fwd(c.dt, ma, c.s); }));
+    } else {
+      AttnArgs aa{};
+      aa.B = L.B; aa.S = L.S; aa.H = c.H; aa.dh = c.dh;
+      aa.causal = c.llama; aa.rope = c.llama;
+      aa.rope_tab = st->rope_tab; aa.rope_rows = st->D.max_seq;
+      aa.qkv = qkv; aa.ld_qkv = 3 * d; aa.o = o; aa.ld_o = d; aa.lse = lse;
+      if (st->qkv_per_head) { aa.qkv_hs = 3 * c.dh; aa.qkv_ko = c.dh; aa.qkv_vo = 2 * c.dh; }
+      RG_TRY(run(st, c.s, "attn_fwd", attn_flops, es * 4.0 * T * d, [&] { return launch_attn_fwd(c.dt, aa, c.s); }));
+    }
   }
   RG_TRY(gemm(c, R_O_FWD, Epi::Store, T, d, d, o, d, b.wt_o, d, attn, d, b.w.b_o));
+  if (st->drop_p > 0.f) RG_TRY(drop(c, l, 0, attn, attn));
 
   AdapterFwdArgs fa{};
   fa.T = T; fa.d = d; fa.m = m; fa.eps = st->D.norm_eps;
@@ -640,6 +762,7 @@ static ringada_status block_forward(const Ctx& c, int l, const void* X, void* Y)
     RG_TRY(gemm(c, R_FFN_IN_FWD, Epi::Gelu, T, F, d, ffn_in, d, b.wt_in, d, g, F, b.w.b_in, nullptr, 0,
                 SN(sb.a1), F));
   RG_TRY(gemm(c, R_FFN_OUT_FWD, Epi::Store, T, d, F, g, F, b.wt_out, F, f2, d, b.w.b_out));
+  if (st->drop_p > 0.f) RG_TRY(drop(c, l, 1, f2, f2));
 
   AdapterFwdArgs fb{};
   fb.T = T; fb.d = d; fb.m = m; fb.eps = st->D.norm_eps;
@@ -694,6 +817,12 @@ extern "C" ringada_status ringada_stage_forward(ringada_stage* st, void* stream,
   plan_layout(D, batch, seq, c, L);
   if (stash_bytes < L.stash_bytes || (L.stash_bytes && !stash))
     return fail(RINGADA_E_WORKSPACE, "stash of %zu bytes, plan needs %zu", stash_bytes, L.stash_bytes);
+  if (st->masked) {
+    const size_t need = masked_attn_need(D, st->att, batch, seq);
+    if (st->att.workspace_bytes < need || (need && !st->att.workspace))
+      return fail(RINGADA_E_WORKSPACE, "attention workspace of %zu bytes, batch %d x %d needs %zu",
+                  st->att.workspace_bytes, batch, seq, need);
+  }
   if (scratch_bytes < L.scratch_bytes || !scratch)
     return fail(RINGADA_E_WORKSPACE, "scratch of %zu bytes, plan needs %zu", scratch_bytes, L.scratch_bytes);
   if ((reinterpret_cast<uintptr_t>(stash) | reinterpret_cast<uintptr_t>(scratch) |
@@ -750,6 +879,7 @@ static ringada_status block_backward(const Ctx& c, int l, const void* G, void* d
       AdapterDwArgs{T, d, m, c.S(sb.u2), dz2, c.S(sb.f2), ab.du, b.ad[1].g_up, b.ad[1].g_down, ab.gu});
   if (stop_ffn) return RINGADA_OK;
 
+  if (st->drop_p > 0.f) RG_TRY(drop(c, l, 1, c.W(L.df2), c.W(L.df2)));
   // FFN (dX only through frozen weights)
   void* da1 = c.W(L.da1);
   if (c.llama) {
@@ -789,19 +919,38 @@ static ringada_status block_backward(const Ctx& c, int l, const void* G, void* d
         AdapterDwArgs{T, d, m, c.S(sb.u1), dz1, c.S(sb.attn), aa.du, b.ad[0].g_up, b.ad[0].g_down, aa.gu});
   if (stop) return RINGADA_OK;
 
+  if (st->drop_p > 0.f) {  // the single placement's dz1 is the residual's gradient too
+    RG_TRY(drop(c, l, 0, dattn, c.W(L.dattn)));
+    dattn = c.W(L.dattn);
+  }
   // attention (dX only)
   RG_TRY(gemm(c, R_O_DX, Epi::Store, T, d, d, dattn, d, b.w.w_o, d, c.W(L.dout), d));
-  AttnArgs at{};
-  at.B = L.B; at.S = L.S; at.H = c.H; at.dh = c.dh;
-  at.causal = c.llama; at.rope = c.llama;
-  at.rope_tab = st->rope_tab; at.rope_rows = st->D.max_seq;
-  at.qkv = c.S(sb.qkv); at.ld_qkv = 3 * d; at.o = c.S(sb.o); at.ld_o = d;
-  if (st->qkv_per_head) { at.qkv_hs = 3 * c.dh; at.qkv_ko = c.dh; at.qkv_vo = 2 * c.dh; }
-  at.lse = static_cast<float*>(c.S(sb.lse));
-  at.dout = c.W(L.dout); at.ld_do = d; at.dsum = static_cast<float*>(c.W(L.dsum));
-  at.dqkv = c.W(L.dqkv); at.ld_dqkv = 3 * d;
-  const double attn_flops = 8.0 * L.B * c.H * (double)L.S * L.S * c.dh * (c.llama ? 0.5 : 1.0);
-  RG_TRY(run(st, c.s, "attn_bwd", attn_flops, es * 8.0 * T * d, [&] { return launch_attn_bwd(c.dt, at, c.s); }));
+  if (st->masked) {
+    MaskedAttnArgs ma = masked_attn_args(c, c.S(sb.qkv), c.S(sb.o), static_cast<float*>(c.S(sb.lse)));
+    char* dqkv = static_cast<char*>(c.W(L.dqkv));
+    const long row = 3 * d;
+    ma.rope_tab = st->rope_tab;
+    ma.dout = View{c.W(L.dout), (long)L.S * d, d, c.dh};
+    ma.dq = View{dqkv, L.S * row, row, c.dh};
+    ma.dk = View{dqkv + d * c.es, L.S * row, row, c.dh};
+    ma.dv = View{dqkv + 2 * d * c.es, L.S * row, row, c.dh};
+    ma.dtable = st->att.g_table;
+    masked_attn_workspace(c.dt, ma, st->att.workspace);
+    RG_TRY(run(st, c.s, "attn_masked_bwd", st->prof ? 10.0 * c.H * c.dh * masked_pairs(ma) : 0, es * 8.0 * T * d,
+               [&] { return launch_masked_attn_bwd(c.dt, ma, c.s); }));
+  } else {
+    AttnArgs at{};
+    at.B = L.B; at.S = L.S; at.H = c.H; at.dh = c.dh;
+    at.causal = c.llama; at.rope = c.llama;
+    at.rope_tab = st->rope_tab; at.rope_rows = st->D.max_seq;
+    at.qkv = c.S(sb.qkv); at.ld_qkv = 3 * d; at.o = c.S(sb.o); at.ld_o = d;
+    if (st->qkv_per_head) { at.qkv_hs = 3 * c.dh; at.qkv_ko = c.dh; at.qkv_vo = 2 * c.dh; }
+    at.lse = static_cast<float*>(c.S(sb.lse));
+    at.dout = c.W(L.dout); at.ld_do = d; at.dsum = static_cast<float*>(c.W(L.dsum));
+    at.dqkv = c.W(L.dqkv); at.ld_dqkv = 3 * d;
+    const double attn_flops = 8.0 * L.B * c.H * (double)L.S * L.S * c.dh * (c.llama ? 0.5 : 1.0);
+    RG_TRY(run(st, c.s, "attn_bwd", attn_flops, es * 8.0 * T * d, [&] { return launch_attn_bwd(c.dt, at, c.s); }));
+  }
   if (c.llama) {
     RG_TRY(gemm(c, R_QKV_DX, Epi::Store, T, d, 3 * d, c.W(L.dqkv), 3 * d, b.w.w_qkv, 3 * d, c.W(L.dn1), d));
     RG_TRY(run(st, c.s, "rms_bwd", 0, es * 4.0 * T * d, [&] {

@@ -40,10 +40,17 @@ class Alg1Driver:
     stage: a bound Stage; w_h [d, C], b_h [C]: the initiator's head (float32
     numpy); batches: list of (x [B, S, d] float numpy in the stage's storage
     values, labels [B] int); n_tm: Trm blocks of the whole model;
-    first_block: 0-indexed first block of this stage."""
+    first_block: 0-indexed first block of this stage; dropout, seed: dropout on the
+    sublayers' outputs, with a new mask every iteration (its sites follow the
+    blocks' numbers in the whole model, so a ring's stages differ)."""
 
-    def __init__(self, stage: Stage, w_h, b_h, batches, n_tm, first_block=0, lr=1e-3, lr_head=1e-3):
+    def __init__(self, stage: Stage, w_h, b_h, batches, n_tm, first_block=0, lr=1e-3, lr_head=1e-3, dropout=0.0,
+                 seed=0):
         self.st = stage
+        self.rng = None
+        if dropout:
+            self.rng = stage.torch.tensor([seed, 0], dtype=stage.torch.int64, device=stage.dev)
+            stage.set_dropout(dropout, self.rng, 2 * first_block)
         torch = stage.torch
         self.torch = torch
         self.n_tm, self.first = n_tm, first_block
@@ -68,6 +75,8 @@ class Alg1Driver:
         x, lab = self.x[i % len(self.x)], self.labels[i % len(self.labels)]
         Bt, S, d = x.shape
         loss = self.torch.zeros(1, dtype=self.torch.float32, device=st.dev)
+        if self.rng is not None:
+            self.rng[1:] += 1  # in stream order: after the last backward, before this forward
         st.forward(x, self.y, c)
         B.ringada_head_ce(st.sptr, st.desc.dtype, self.y, Bt, S, d, self.wh, self.bh, self.wh.shape[1], lab,
                           self.dy, self.gwh, self.gbh, loss)
@@ -131,6 +140,11 @@ def main(argv=None):
     ap.add_argument("--iters", type=int, default=3, help="initiator iterations per round")
     ap.add_argument("--batches", type=int, default=2)
     ap.add_argument("--lr", type=float, default=1e-3)
+    ap.add_argument("--dropout", type=float, default=0.0, help="on the sublayers' outputs")
+    ap.add_argument("--window", type=int, default=0, help="sliding attention window (0: none)")
+    ap.add_argument("--sinks", type=int, default=0, help="first tokens that stay visible outside the window")
+    ap.add_argument("--bias-buckets", type=int, default=0, help="learned relative position bias (0: none)")
+    ap.add_argument("--bias-distance", type=int, default=128, help="distance from which its last bucket holds")
     args = ap.parse_args(argv)
 
     import torch
@@ -153,7 +167,15 @@ def main(argv=None):
         batches.append((x, rng.integers(0, 2, w.batch).astype(np.int32)))
     st = Stage(w, inp)
     try:
-        drv = Alg1Driver(st, inp["w_h"], inp["b_h"], batches, n_tm=w.n_blocks, lr=args.lr, lr_head=args.lr)
+        if args.window or args.bias_buckets:
+            table = bucket = None
+            if args.bias_buckets:
+                from .operators import relpos_buckets
+                table = st.f32(rng.standard_normal((args.bias_buckets, w.n_heads)) * 0.02)
+                bucket = relpos_buckets(args.bias_buckets, args.bias_distance, w.arch == "bert", st.dev)
+            st.set_attention(args.window, args.sinks, table, bucket)
+        drv = Alg1Driver(st, inp["w_h"], inp["b_h"], batches, n_tm=w.n_blocks, lr=args.lr, lr_head=args.lr,
+                         dropout=args.dropout, seed=w.seed)
         rounds = args.rounds or args.k * (w.n_blocks - args.d0 + 1)
         drv.run(args.d0, args.k, 1, 1)  # warm-up: kernel loading, first workspace
         recs = drv.run(args.d0, args.k, rounds, args.iters)

@@ -69,6 +69,7 @@ class Stage:
             # stay allocated here, untouched, so grads() keeps one layout)
             B.ringada_stage_bind_block(self.handle, l, bw, None if w.placement == "ffn" else ca[0], ca[1],
                                        self.block_mem[l], self.block_bytes, self.sptr)
+        self.attention = None  # StageAttention and the tensors it borrows
         self.stash = self.scratch = None
         self.stash_bytes = self.scratch_bytes = 0
 
@@ -97,7 +98,47 @@ class Stage:
         if self.scratch is None or self.scratch_bytes < sc:
             self.scratch = self.torch.empty(max(sc, 256), dtype=self.torch.uint8, device=self.dev)
             self.scratch_bytes = self.scratch.numel()
+        if self.attention is not None:
+            opt = self.attention[0]
+            n = B.ringada_stage_plan_attention(self.desc, opt, batch, seq)
+            if opt.workspace_bytes < n:
+                ws = self.torch.empty(n, dtype=self.torch.uint8, device=self.dev)
+                new = B.StageAttention(opt.window, opt.sinks, opt.n_buckets, opt.max_distance, opt.table, opt.bucket,
+                                       opt.g_table, ws.data_ptr(), n)
+                B.ringada_stage_set_attention(self.handle, new)  # refused while a backward reads the old one
+                self.attention = (new,) + self.attention[1:4] + (ws,)
         return st, sc
+
+    # ------------------------------------------------------------ options
+    def set_attention(self, window=0, sinks=0, table=None, bucket=None, g_table=None):
+        """Attention of every block with a sliding window, sinks and a relative position bias: table and
+        g_table [n_buckets, heads] float32, bucket [2 max_distance + 1] int32, on the device (g_table None: a
+        frozen table).  Without arguments: the plain attention."""
+        torch, h = self.torch, self.w.n_heads
+        nb = r = 0
+        if table is not None:
+            if bucket is None or bucket.dim() != 1 or bucket.numel() % 2 == 0:
+                raise ValueError("a table takes a bucket map [2 max_distance + 1]")
+            nb, r = table.shape[0], bucket.numel() // 2
+            for name, t, dt, shape in (("table", table, torch.float32, (nb, h)),
+                                       ("bucket", bucket, torch.int32, (2 * r + 1,)),
+                                       ("g_table", g_table, torch.float32, (nb, h))):
+                if t is not None and (t.dtype != dt or tuple(t.shape) != shape or t.device != self.dev
+                                      or not t.is_contiguous()):
+                    raise ValueError(f"{name}: expected a contiguous {dt} tensor of shape {shape} on {self.dev}")
+        opt = B.StageAttention(window, sinks, nb, r, B._p(table), B._p(bucket), B._p(g_table), None, 0)
+        B.ringada_stage_set_attention(self.handle, opt)
+        self.attention = (opt, table, bucket, g_table, None) if window or nb else None
+
+    def set_dropout(self, p, rng=None, first_site=0):
+        """Dropout on each sublayer's output; rng: int64 [2] on the device, {seed, offset}, to be changed
+        only between a backward and the next forward."""
+        torch = self.torch
+        if rng is not None and (rng.dtype != torch.int64 or tuple(rng.shape) != (2,) or rng.device != self.dev
+                                or not rng.is_contiguous()):
+            raise ValueError(f"rng: expected a contiguous int64 tensor of two values on {self.dev}")
+        B.ringada_stage_set_dropout(self.handle, p, rng, first_site)
+        self.rng = rng
 
     # ------------------------------------------------------------ hot path
     def forward(self, x, y, c, batch=None, seq=None):

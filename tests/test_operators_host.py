@@ -170,3 +170,47 @@ def test_python_front_end_refuses():
         ops.dropout(q, 0.1, torch.zeros(2, dtype=torch.int64))
     with pytest.raises(ValueError):
         ops.attention_backward(q, q, q, q, q, None)
+
+
+def stage_desc(**kw):
+    from paper_2502_19864_amd.stage import make_desc
+    from paper_2502_19864_amd.workloads import WORKLOADS
+    return make_desc(WORKLOADS["bert_base"].replace(**kw))
+
+
+def test_stage_attention_plan():
+    d = stage_desc()
+    assert B.ringada_stage_plan_attention(d, B.StageAttention(), 32, 128) == 0
+    n = B.ringada_stage_plan_attention(d, B.StageAttention(window=40), 32, 128)
+    assert n >= 32 * 12 * 128 * 4
+    t = B.StageAttention(n_buckets=8, max_distance=20, g_table=BASE)
+    assert B.ringada_stage_plan_attention(d, t, 32, 128) >= 32 * 12 * 128 * 4 + 32 * 12 * 41 * 4
+    for bad, status in ((B.StageAttention(window=-1), B.RINGADA_E_INVALID),
+                        (B.StageAttention(sinks=-1), B.RINGADA_E_INVALID),
+                        (B.StageAttention(n_buckets=4, max_distance=2000), B.RINGADA_E_UNSUPPORTED)):
+        with pytest.raises(B.RingadaError) as e:
+            B.ringada_stage_plan_attention(d, bad, 32, 128)
+        assert e.value.status == status
+    with pytest.raises(B.RingadaError):
+        B.ringada_stage_plan_attention(d, B.StageAttention(window=4), 33, 128)
+
+
+def test_stage_options_are_checked():
+    h = B.ringada_stage_create(stage_desc(), None, 0)
+    try:
+        for bad in (B.StageAttention(window=-1), B.StageAttention(n_buckets=4, max_distance=3),
+                    B.StageAttention(table=BASE, bucket=BASE), B.StageAttention(window=1, g_table=BASE),
+                    B.StageAttention(n_buckets=4, max_distance=3, table=BASE),
+                    B.StageAttention(window=4, workspace=BASE + 16, workspace_bytes=1 << 20)):
+            with pytest.raises(B.RingadaError) as e:
+                B.ringada_stage_set_attention(h, bad)
+            assert e.value.status == B.RINGADA_E_INVALID
+        for p, rng in ((-0.1, BASE), (1.0, BASE), (0.1, None), (0.1, BASE + 4), (float("nan"), BASE)):
+            with pytest.raises(B.RingadaError) as e:
+                B.ringada_stage_set_dropout(h, p, rng, 0)
+            assert e.value.status == B.RINGADA_E_INVALID
+        B.ringada_stage_set_attention(h, B.StageAttention(window=4))
+        B.ringada_stage_set_attention(h, None)
+        B.ringada_stage_set_dropout(h, 0.0, None, 0)
+    finally:
+        B.ringada_stage_destroy(h)
