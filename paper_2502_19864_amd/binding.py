@@ -97,10 +97,10 @@ SIGNATURES = [
     ("ringada_head_ce", c_int32, [c_void_p, c_int32, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p,
                                   c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     ("ringada_sgd_f32", c_int32, [c_void_p, c_void_p, c_void_p, c_int64, c_float]),
-    ("ringada_attn_plan", c_int32, [POINTER(AttnDesc), c_int32, POINTER(c_size_t), POINTER(c_size_t)]),
-    ("ringada_attn_forward", c_int32, [c_void_p, POINTER(AttnDesc), POINTER(AttnTensors), c_void_p, c_size_t]),
-    ("ringada_attn_backward", c_int32, [c_void_p, POINTER(AttnDesc), POINTER(AttnTensors), POINTER(AttnGrads),
-                                        c_void_p, c_size_t]),
+    ("ringada_attn_plan", c_int32, [c_void_p, c_int32, POINTER(c_size_t), POINTER(c_size_t)]),
+    # the structs may come as the ctypes structures or packed into bytes
+    ("ringada_attn_forward", c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_size_t]),
+    ("ringada_attn_backward", c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_size_t]),
     ("ringada_relpos_buckets", c_int32, [c_int32, c_int32, c_int32, POINTER(c_int32)]),
     ("ringada_dropout", c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_float, c_void_p,
                                   c_uint32]),
@@ -141,6 +141,11 @@ def _p(x):
     if isinstance(x, int):
         return x
     return x.data_ptr()
+
+
+def _ref(x):
+    """A structure by reference, or its packed bytes as they are."""
+    return x if type(x) is bytes else byref(x)
 
 
 def ringada_stage_plan(desc, batch, seq, lowest_unfrozen):
@@ -225,17 +230,16 @@ def ringada_sgd_f32(stream, w, g, n, lr):
 
 def ringada_attn_plan(desc, with_dtable):
     f, b = c_size_t(0), c_size_t(0)
-    _check(lib().ringada_attn_plan(byref(desc), int(with_dtable), byref(f), byref(b)))
+    _check(lib().ringada_attn_plan(_ref(desc), int(with_dtable), byref(f), byref(b)))
     return f.value, b.value
 
 
 def ringada_attn_forward(stream, desc, tensors, workspace, workspace_bytes):
-    _check(lib().ringada_attn_forward(stream, byref(desc), byref(tensors), _p(workspace), workspace_bytes))
+    _check(lib().ringada_attn_forward(stream, _ref(desc), _ref(tensors), _p(workspace), workspace_bytes))
 
 
 def ringada_attn_backward(stream, desc, tensors, grads, workspace, workspace_bytes):
-    _check(lib().ringada_attn_backward(stream, byref(desc), byref(tensors), byref(grads), _p(workspace),
-                                       workspace_bytes))
+    _check(lib().ringada_attn_backward(stream, _ref(desc), _ref(tensors), _ref(grads), _p(workspace), workspace_bytes))
 
 
 def ringada_relpos_buckets(n_buckets, max_distance, bidirectional):
