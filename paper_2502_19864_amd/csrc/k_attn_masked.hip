@@ -51,18 +51,68 @@ struct Mask {
   __device__ __forceinline__ bool pair(int p, int j) const {
     return (j < lk) & ((causal == 0) | (j <= p)) & ((window == 0) | (abs(p - j) < window) | (j < sinks));
   }
-  // keys k0 .. k0 + n - 1 against positions plo .. phi: 0 nothing visible, 2 everything, 1 else
-  __device__ __forceinline__ int block(int k0, int n, int plo, int phi) const {
-    const int k1 = k0 + n - 1;
-    if (k0 >= lk || (causal && k0 > phi)) return 0;
-    if (window && k0 >= sinks && (k0 - phi >= window || plo - k1 >= window)) return 0;
-    return k1 < lk && (!causal || k1 <= plo) &&
-                   (!window || k1 < sinks || (phi - k0 < window && k1 - plo < window))
-               ? 2
-               : 1;
-  }
 };
 
+// What a loop meets, by blocks of 32: blocks v0 .. v1 and those below vs hold something
+// visible, f0 .. f1 and those below fs nothing else.  Worked out once per wave, so that a step
+// costs a few scalar comparisons (formed anew per block, these and the tests of
+// Mask were a quarter of the instructions).
+struct Span {
+  int v0, v1, vs, f0, f1, fs;
+  // 0 nothing visible, 2 everything, 1 else
+  __device__ __forceinline__ int kind(int blk) const {
+    const bool full = (blk >= f0 && blk <= f1) || blk < fs, some = (blk >= v0 && blk <= v1) || blk < vs;
+    return full ? 2 : some ? 1 : 0;
+  }
+};
+// key blocks for the query positions plo .. phi
+__device__ __forceinline__ Span key_span(const Mask& m, int plo, int phi) {
+  Span s{0, 0, 0, 0, 0, 0};
+  int hi = m.lk - 1, fhi = m.lk - 1;
+  if (m.causal) {
+    hi = min(hi, phi);
+    fhi = min(fhi, plo);
+  }
+  if (m.window) {
+    s.v0 = max(0, plo - m.window + 1) >> 5;
+    s.f0 = (max(0, phi - m.window + 1) + 31) >> 5;
+    s.vs = (min(m.sinks, hi + 1) + 31) >> 5;
+    s.fs = max(0, min(m.sinks, fhi + 1)) >> 5;
+    if (!m.causal) {
+      hi = min(hi, phi + m.window - 1);
+      fhi = min(fhi, plo + m.window - 1);
+    }
+  }
+  s.v1 = hi >> 5;
+  s.f1 = ((fhi + 1) >> 5) - 1;
+  return s;
+}
+// blocks of query rows (positions off + row, lq rows) for the keys k0 .. k0 + 31; the whole 32
+// rows and keys exist in a full one
+__device__ __forceinline__ Span query_span(const Mask& m, int k0, int off, int lq) {
+  const int k1 = k0 + 31;
+  Span s{0, 0, 0, 0, 0, 0};
+  int lo = 0, hi = lq - 1, flo = 0, fhi = lq - 1;
+  if (m.causal) {
+    lo = max(lo, k0 - off);
+    flo = max(flo, k1 - off);
+  }
+  if (m.window) {
+    if (k0 >= m.sinks) hi = min(hi, k1 + m.window - 1 - off);
+    if (k1 >= m.sinks) fhi = min(fhi, k0 + m.window - 1 - off);
+    if (!m.causal) {
+      if (k0 >= m.sinks) lo = max(lo, k0 - m.window + 1 - off);
+      if (k1 >= m.sinks) flo = max(flo, k1 - m.window + 1 - off);
+    }
+  }
+  if (k0 >= m.lk) hi = -1;
+  if (k1 >= m.lk) fhi = -1;
+  s.v0 = lo >> 5;
+  s.v1 = hi >> 5;
+  s.f0 = (flo + 31) >> 5;
+  s.f1 = ((fhi + 1) >> 5) - 1;
+  return s;
+}
 // the tiles of KR keys that positions plo .. phi can see: the sinks' tiles, then
 // the window's
 struct KeyTiles {
@@ -89,6 +139,34 @@ __device__ __forceinline__ KeyTiles key_tiles(const Mask& m, int plo, int phi) {
   return t;
 }
 
+// ================================================================ the pipeline
+// Pairs of tiles stream through ST stages in LDS, ST - 1 of them under way: a stage is
+// refilled once the barrier says that its readers are done, and waited for by the count of
+// DMAs issued since (PER per tile and wave; memory returns them in order).  One tile ahead, as in
+// k_attention.hip, the wait for memory was most of an iteration at short windows.
+template <int N>
+__device__ __forceinline__ void wait_dma() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+}
+// tile i of n has landed, for every wave; `ahead` tiles are in flight behind it at most
+template <int ST, int PER>
+__device__ __forceinline__ void tile_ready(int i, int n) {
+  static_assert(ST >= 2 && ST <= 4 && PER * (ST - 2) < 64, "vmcnt counts to 63");
+  const int ahead = min(ST - 2, n - 1 - i);
+  if (ST == 4 && ahead == 2) wait_dma<PER*(ST > 3 ? 2 : 0)>();
+  else if (ST >= 3 && ahead == 1) wait_dma<PER*(ST > 2 ? 1 : 0)>();
+  else wait_dma<0>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// Values loaded before the loop are waited for there: left to the first use, the wait sits inside
+// the loop, where every step then waits for the DMAs it has just issued.
+template <typename T>
+__device__ __forceinline__ void settle(T& x) {
+  asm volatile("" : "+v"(x));
+}
+
 // ================================================================ storage types
 // A tile is KR rows of one head in LDS.  dma() brings this wave's share (of NW) of rows 0 .. ROWS - 1
 // from src (rows past `last` read row `last`: what they score is masked); scores() forms the block
@@ -96,11 +174,16 @@ __device__ __forceinline__ KeyTiles key_tiles(const Mask& m, int plo, int phi) {
 // tile^T p to acc (lane = own row, registers = head dims).
 template <int DH_>
 struct OpsBf16 {
-  static constexpr int DH = DH_, KR = 64, TILE = KR * DH, STAGE = 32 * (DH + 8), WAVES = 2;
-  static constexpr int BLOCK = 32 * DH, DMAS = 32 * DH / 512;  // elements of 32 rows, and one wave's DMAs for them
+  static constexpr int BLOCK_DMAS(int rows) { return rows * DH_ / 512; }  // 1 KB each
+  static constexpr int DH = DH_, KR = 64, ST = DH == 64 ? 3 : 2, TILE = KR * DH, STAGE = 32 * (DH + 8), WAVES = 2;
+  static constexpr int BLOCK = 32 * DH, DMAS = BLOCK_DMAS(32);  // elements of 32 rows, and their DMAs
   typedef bf16 E;
   struct Rows {
     bf16x8 f[DH / 16];
+    __device__ __forceinline__ void settled() {
+#pragma unroll
+      for (int i = 0; i < DH / 16; ++i) settle(f[i]);
+    }
   };
   TileRead<DH> rd;
   __device__ __forceinline__ OpsBf16(int lane, int) : rd(lane) {}
@@ -161,11 +244,16 @@ struct OpsBf16 {
 // zeros in the own rows.
 template <int DHM>
 struct OpsF32 {
-  static constexpr int DH = DHM, KR = 32, P = DHM + 4, TILE = KR * P, STAGE = 32 * P, WAVES = 1;
-  static constexpr int BLOCK = TILE, DMAS = KR * DHM / 64;
+  static constexpr int BLOCK_DMAS(int rows) { return rows * DHM / 64; }  // 64 floats each
+  static constexpr int DH = DHM, KR = 32, ST = DHM == 64 ? 4 : 3, P = DHM + 4, TILE = KR * P, STAGE = 32 * P, WAVES = 1;
+  static constexpr int BLOCK = TILE, DMAS = BLOCK_DMAS(KR);
   typedef float E;
   struct Rows {
     float f[DHM / 2];  // dims half * DHM / 2 + i
+    __device__ __forceinline__ void settled() {
+#pragma unroll
+      for (int i = 0; i < DHM / 2; ++i) settle(f[i]);
+    }
   };
   int row, col, half;
   __device__ __forceinline__ OpsF32(int lane, int) {
@@ -303,13 +391,31 @@ __device__ __forceinline__ void add_diag(const f32x16& ds, int base, int R, floa
 }
 
 // ================================================================ forward
+// The running maximum (base 2) moves only when some row's new one is more than 8 above it:
+// until then P is at most 2^8, which costs fp32 sums and bf16 products nothing, and the
+// wave keeps its sums as they are.
+template <int N>
+__device__ __forceinline__ void move_max(float& mrun, float& lrun, f32x16 (&oacc)[N], float mx) {
+  if (__any(mx > mrun + 8.f)) {
+    const float mnew = fmaxf(mrun, mx);
+    const float alpha = mnew == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mrun - mnew);
+    mrun = mnew;
+    lrun *= alpha;
+#pragma unroll
+    for (int d = 0; d < N; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[d][r] *= alpha;
+  }
+}
+
 template <class O, bool BIAS, int NW>
 __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnArgs a) {
   typedef typename O::E E;
   constexpr int DH = O::DH, KR = O::KR, TILE = O::TILE;
-  __shared__ __attribute__((aligned(1024))) E sm[4 * TILE];  // [buffer][K, V]
+  constexpr int ST = O::ST, PER = 2 * O::BLOCK_DMAS(KR) / NW;
+  __shared__ __attribute__((aligned(1024))) E sm[ST * 2 * TILE];  // [stage][K, V]
   extern __shared__ float sbias[];
-  static_assert(4 * TILE >= NW * O::STAGE, "the O rows fit the tiles' space");
+  static_assert(ST * 2 * TILE >= NW * O::STAGE, "the O rows fit the tiles' space");
   const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // what a wave skips, it skips whole
   const int nq = (a.Sq + 32 * NW - 1) / (32 * NW);
@@ -322,6 +428,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
   const int qw0 = qb * 32 * NW, q0 = qw0 + wave * 32, q = q0 + l32, p = sq.off + q;
   const bool qv = q < sq.lq;
   const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
+  const Span span = key_span(mask, plo, phi);
   KeyTiles kt{0, 0, 0};
   if (qw0 < sq.lq) kt = key_tiles<KR>(mask, sq.off + qw0, sq.off + min(qw0 + 32 * NW, sq.lq) - 1);
   const float sl2 = kLog2e * a.scale;
@@ -330,11 +437,11 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
   const O ops(lane, a.dh);
   auto issue = [&](int i) {
     const int k0 = kt.at(i) * KR, last = sq.lk - 1 - k0;
-    E* dst = sm + (i & 1) * 2 * TILE;
+    E* dst = sm + (i % ST) * 2 * TILE;
     O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, wave);
     O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh, lane, wave);
   };
-  if (kt.n > 0) issue(0);
+  for (int i = 0; i < min(ST - 1, kt.n); ++i) issue(i);
   typename O::Rows qf;
   O::load_rows(qf, static_cast<const E*>(a.q.p) + b * a.q.b + (long)(qv ? q : 0) * a.q.t + h * a.q.h, qv, half, a.dh);
   if (BIAS) load_bias(a, h, sbias);
@@ -346,13 +453,21 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
     for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
   float mrun = -INFINITY, lrun = 0.f;
 
+  qf.settled();
   for (int i = 0; i < kt.n; ++i) {
-    tiles_ready();
-    if (i + 1 < kt.n) issue(i + 1);
+    tile_ready<ST, PER>(i, kt.n);
+    if (i + ST - 1 < kt.n) issue(i + ST - 1);
     const int k0 = kt.at(i) * KR;
-    const int kind = q0 < sq.lq ? mask.block(k0, KR, plo, phi) : 0;
-    if (kind == 0) continue;  // wave-uniform
-    const E* sK = sm + (i & 1) * 2 * TILE;
+    if (q0 >= sq.lq) continue;  // wave-uniform, as all of this
+    int most = 0, least = 2;
+#pragma unroll
+    for (int kb = 0; kb < KR / 32; ++kb) {
+      const int kind = span.kind(k0 / 32 + kb);
+      most = max(most, kind);
+      least = min(least, kind);
+    }
+    if (most == 0) continue;
+    const E* sK = sm + (i % ST) * 2 * TILE;
     const E* sV = sK + TILE;
     f32x16 sc[KR / 32];
     float mx = -INFINITY;
@@ -362,7 +477,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
       if (BIAS)
         add_bias<1>(sc[kb], sl2, sbias, a.R, k0 + kb * 32 - p, k0 + kb * 32 - phi, k0 + kb * 32 + 31 - plo, half);
     }
-    if (kind == 1) {
+    if (least < 2) {
 #pragma unroll
       for (int kb = 0; kb < KR / 32; ++kb)
 #pragma unroll
@@ -375,9 +490,8 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[kb][r]);
     // without a bias the scale (positive) is folded into the exponent's FMA
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * (BIAS ? 1.f : sl2);
-    const float mnew = fmaxf(mrun, mx);
-    const float mfin = mnew == -INFINITY ? 0.f : mnew;  // nothing visible yet: exp2(-inf - 0) = 0
-    const float alpha = __builtin_amdgcn_exp2f(mrun - mfin);
+    move_max(mrun, lrun, oacc, mx);
+    const float mfin = mrun == -INFINITY ? 0.f : mrun;  // nothing visible yet: exp2(-inf - 0) = 0
     float rs = 0.f;
 #pragma unroll
     for (int kb = 0; kb < KR / 32; ++kb)
@@ -386,13 +500,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
         sc[kb][r] = __builtin_amdgcn_exp2f(BIAS ? sc[kb][r] - mfin : fmaf(sc[kb][r], sl2, -mfin));
         rs += sc[kb][r];
       }
-    rs += __shfl_xor(rs, 32, 64);
-    lrun = lrun * alpha + rs;
-    mrun = mnew;
-#pragma unroll
-    for (int d = 0; d < DH / 32; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[d][r] *= alpha;
+    lrun += rs + __shfl_xor(rs, 32, 64);
 #pragma unroll
     for (int kb = 0; kb < KR / 32; ++kb) ops.accum(oacc, sV, kb, sc[kb]);
   }
@@ -442,6 +550,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
   const int row = rb * 32 + l32, tok = row / grp, h = hk * grp + row % grp, p = sq.off + tok;
   const bool qv = tok < sq.lq;
   const int tok0 = rb * 32 / grp, plo = sq.off + tok0, phi = sq.off + min((rb * 32 + 31) / grp, sq.lq - 1);
+  const Span span = key_span(mask, plo, phi);
   KeyTiles kt{0, 0, 0};
   if (tok0 < sq.lq) kt = key_tiles<32>(mask, plo, phi);
   const int per = (kt.n + w.split - 1) / w.split, i1 = min(kt.n, (split + 1) * per);
@@ -469,6 +578,11 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
 #pragma unroll
     for (int r = 0; r < 16; ++r) oacc[d][r] = 0.f;
   float mrun = -INFINITY, lrun = 0.f;
+  qf.settled();
+  if (BIAS) {
+    settle(lb.lo);
+    settle(lb.hi);
+  }
   for (int buf = 0; i < i1; i += NW, buf ^= 1) {
     // the other buffer's reads have ended; its next tile is under way while this one is waited for,
     // where the counter of loads in flight (63 at most) can tell the two apart
@@ -484,7 +598,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       if (i + NW < i1) issue(i + NW, buf ^ 1);
     }
-    const int k0 = kt.at(i) * 32, kind = mask.block(k0, 32, plo, phi);
+    const int k0 = kt.at(i) * 32, kind = span.kind(k0 / 32);
     if (kind == 0) continue;
     const E* sK = tiles + buf * 2 * BLOCK;
     f32x16 sc;
@@ -510,20 +624,15 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
 #pragma unroll
     for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * (BIAS ? 1.f : sl2);
-    const float mnew = fmaxf(mrun, mx), mfin = mnew == -INFINITY ? 0.f : mnew;
-    const float alpha = __builtin_amdgcn_exp2f(mrun - mfin);
+    move_max(mrun, lrun, oacc, mx);
+    const float mfin = mrun == -INFINITY ? 0.f : mrun;
     float rs = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       sc[r] = __builtin_amdgcn_exp2f(BIAS ? sc[r] - mfin : fmaf(sc[r], sl2, -mfin));
       rs += sc[r];
     }
-    lrun = lrun * alpha + rs + __shfl_xor(rs, 32, 64);
-    mrun = mnew;
-#pragma unroll
-    for (int d = 0; d < DH / 32; ++d)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) oacc[d][r] *= alpha;
+    lrun += rs + __shfl_xor(rs, 32, 64);
     ops.accum(oacc, sK + BLOCK, 0, sc);
   }
 
@@ -595,12 +704,20 @@ __global__ __launch_bounds__(256) void attn_few_join(MaskedAttnArgs a, FewWork w
   float acc[DH / 64];
 #pragma unroll
   for (int d = 0; d < DH / 64; ++d) acc[d] = 0.f;
-#pragma unroll 8
-  for (int s = 0; s < w.split; ++s) {
-    const float fs = __shfl(f, s, 64);
-    const float* src = a.part + ((blk0 + (long)s * w.rb) * 32 + row % 32) * DH + lane;
+  for (int s0 = 0; s0 < w.split; s0 += 8) {  // eight loads in flight; past the last one with weight 0
+    float v[8][DH / 64], fs[8];
 #pragma unroll
-    for (int d = 0; d < DH / 64; ++d) acc[d] = fmaf(src[64 * d], fs, acc[d]);
+    for (int k = 0; k < 8; ++k) {
+      const int s = min(s0 + k, w.split - 1);
+      const float* src = a.part + ((blk0 + (long)s * w.rb) * 32 + row % 32) * DH + lane;
+#pragma unroll
+      for (int d = 0; d < DH / 64; ++d) v[k][d] = src[64 * d];
+      fs[k] = s0 + k < w.split ? __shfl(f, s, 64) : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int d = 0; d < DH / 64; ++d) acc[d] = fmaf(v[k][d], fs[k], acc[d]);
   }
   const int tok = row / grp, h = hk * grp + row % grp;
   E* o = static_cast<E*>(a.o.p) + b * a.o.b + (long)tok * a.o.t + h * a.o.h;
@@ -614,7 +731,7 @@ __global__ __launch_bounds__(256) void attn_few_join(MaskedAttnArgs a, FewWork w
 // exponent offset of a row that sees nothing: exp2(x - inf) = 0
 __device__ __forceinline__ float lse_or_inf(float l) { return l == -INFINITY ? INFINITY : l; }
 
-// dQ pass (lane = query); writes D.  DTAB: dtable is wanted, and D is formed from
+// dQ pass (lane = query); writes (lse, D).  DTAB: dtable is wanted, and D is formed from
 // P and dP themselves in a first sweep over the tiles: the sums over dS cancel, and a D
 // from the stored (rounded) O would leave an error of that rounding in them.  That sweep
 // is two of the pass's five products.
@@ -622,8 +739,9 @@ template <class O, bool BIAS, bool DTAB, int NW>
 __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAttnArgs a) {
   typedef typename O::E E;
   constexpr int DH = O::DH, KR = O::KR, TILE = O::TILE;
-  __shared__ __attribute__((aligned(1024))) E sm[4 * TILE];  // [buffer][K, V]
-  extern __shared__ float sbias[];                           // bias, then (DTAB) one diagonal array per wave
+  constexpr int ST = O::ST, PER = 2 * O::BLOCK_DMAS(KR) / NW;
+  __shared__ __attribute__((aligned(1024))) E sm[ST * 2 * TILE];  // [stage][K, V]
+  extern __shared__ float sbias[];                                // bias, then (DTAB) one diagonal array per wave
   const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // what a wave skips, it skips whole
   const int nq = (a.Sq + 32 * NW - 1) / (32 * NW);
@@ -636,6 +754,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   const int qw0 = qb * 32 * NW, q0 = qw0 + wave * 32, q = q0 + l32, p = sq.off + q;
   const bool qv = q < sq.lq;
   const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
+  const Span span = key_span(mask, plo, phi);
   KeyTiles kt{0, 0, 0};
   if (qw0 < sq.lq) kt = key_tiles<KR>(mask, sq.off + qw0, sq.off + min(qw0 + 32 * NW, sq.lq) - 1);
   const float sl2 = kLog2e * a.scale;
@@ -645,11 +764,11 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   const int nit = DTAB ? 2 * kt.n : kt.n;  // DTAB: the tiles twice
   auto issue = [&](int i) {
     const int k0 = kt.at(DTAB && i >= kt.n ? i - kt.n : i) * KR, last = sq.lk - 1 - k0;
-    E* dst = sm + (i & 1) * 2 * TILE;
+    E* dst = sm + (i % ST) * 2 * TILE;
     O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, wave);
     O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh, lane, wave);
   };
-  if (nit > 0) issue(0);
+  for (int i = 0; i < min(ST - 1, nit); ++i) issue(i);
   const long row = qv ? q : 0;
   typename O::Rows qf, df;
   O::load_rows(qf, static_cast<const E*>(a.q.p) + b * a.q.b + row * a.q.t + h * a.q.h, qv, half, a.dh);
@@ -660,7 +779,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
     O::load_rows(of, static_cast<const E*>(a.o.p) + b * a.o.b + row * a.o.t + h * a.o.h, qv, half, a.dh);
     dsum = O::dot(of, df);
   }
-  const float lse = qv ? lse_or_inf(a.lse[(long)bh * a.Sq + row]) : INFINITY;
+  float lse = qv ? lse_or_inf(a.lse[(long)bh * a.Sq + row]) : INFINITY;
   const int W = 2 * a.R + 1;
   float* diag = sbias + (1 + wave) * W;
   if (BIAS) load_bias(a, h, sbias);
@@ -674,19 +793,23 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
 #pragma unroll
     for (int r = 0; r < 16; ++r) dq[i][r] = 0.f;
 
+  qf.settled();
+  df.settled();
+  settle(lse);
+  settle(dsum);
   for (int i = 0; i < nit; ++i) {
-    tiles_ready();
-    if (i + 1 < nit) issue(i + 1);
+    tile_ready<ST, PER>(i, nit);
+    if (i + ST - 1 < nit) issue(i + ST - 1);
     if (q0 >= sq.lq) continue;
     const bool first = DTAB && i < kt.n;
     if (DTAB && i == kt.n) dsum += __shfl_xor(dsum, 32, 64);
-    const E* sK = sm + (i & 1) * 2 * TILE;
+    const E* sK = sm + (i % ST) * 2 * TILE;
     const E* sV = sK + TILE;
     // one key block at a time (not unrolled): keeps the kernel within its registers
 #pragma unroll 1
     for (int kb = 0; kb < KR / 32; ++kb) {
       const int k0 = kt.at(DTAB && i >= kt.n ? i - kt.n : i) * KR + kb * 32;
-      const int kind = mask.block(k0, 32, plo, phi);
+      const int kind = span.kind(k0 / 32);
       if (kind == 0) continue;  // wave-uniform
       ops.fresh();
       f32x16 st, dp;
@@ -694,7 +817,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
       ops.scores(dp, sV, kb, df);
       if (BIAS) add_bias<1>(st, sl2, sbias, a.R, k0 - p, k0 - phi, k0 + 31 - plo, half);
       if (kind == 1) {  // a row past len_q has lse = +inf
-#pragma unroll
+  #pragma unroll
         for (int r = 0; r < 16; ++r)
           st[r] = mask.pair(p, k0 + perm_pos(r, half)) ? st[r] : -INFINITY;
       }
@@ -711,7 +834,8 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
       ops.accum(dq, sK, kb, st);
     }
   }
-  if (qv && half == 0) a.dsum[(long)bh * a.Sq + q] = dsum;
+  // the row statistics that the dK/dV pass reads
+  if (q < a.Sq && half == 0) a.stat[(long)bh * a.Sq + q] = make_float2(lse, dsum);
   if (DTAB) {
     dlo = wave_sum(dlo);
     dhi = wave_sum(dhi);
@@ -799,10 +923,11 @@ template <class O, bool BIAS, int NW>
 __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(MaskedAttnArgs a, KeyWork w) {
   typedef typename O::E E;
   constexpr int DH = O::DH, KR = O::KR, TILE = O::TILE;
-  __shared__ __attribute__((aligned(1024))) E sm[4 * TILE];  // [buffer][Q, dO]
-  __shared__ __attribute__((aligned(16))) float sL[2][KR], sD[2][KR];
+  constexpr int ST = O::ST, PER = 2 * O::BLOCK_DMAS(KR) / NW + 1;
+  __shared__ __attribute__((aligned(1024))) E sm[ST * 2 * TILE];  // [stage][Q, dO]
+  __shared__ __attribute__((aligned(1024))) float2 sS[ST][KR];   // (lse, D) of the tile's rows
   extern __shared__ float sbias[];  // two heads' bias
-  static_assert(KR <= 64 * NW, "one row statistic per thread");
+  static_assert(NW % (KR / 32) == 0, "32 rows' statistics per DMA");
   const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // what a wave skips, it skips whole
   const int grp = a.H / a.Hkv;
@@ -816,44 +941,40 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
   const bool kv = key < sq.lk;
   int qt0, nt;
   query_tiles<KR>(a, sq, kw0, 32 * NW, qt0, nt);
+  const Span span = query_span(mask, k0, sq.off, sq.lq);
   const int i0 = ki.n > 1 ? ki.split * ki.c : 0, i1 = ki.n > 1 ? min(nt * grp, i0 + ki.c) : nt * grp;
   if (ki.n > 1 && i0 >= i1) return;  // the join counts the same way
   const float sl2 = kLog2e * a.scale;
   const int W = 2 * a.R + 1;
   O ops(lane, a.dh);
-  int h = hk * grp, t = 0;  // head and query tile (of nt) of the iteration that is issued
+  int h = hk * grp, t = 0;  // head and query tile (of nt) that is issued next
   if (nt > 0) {
     h += i0 / nt;
     t = i0 % nt;
   }
-  auto issue = [&](int buf) {
-    const int r0 = (qt0 + t) * KR, last = sq.lq - 1 - r0;
-    E* dst = sm + buf * 2 * TILE;
-    O::template dma<NW>(static_cast<const E*>(a.q.p) + b * a.q.b + h * a.q.h + (long)r0 * a.q.t, a.q.t, last, dst, a.dh, lane, wave);
+  // brings the tile of (h, t) into a stage and moves on to the next one
+  int issued = i0;
+  auto issue = [&]() {
+    const int r0 = (qt0 + t) * KR, last = sq.lq - 1 - r0, stage = (issued - i0) % ST;
+    E* dst = sm + stage * 2 * TILE;
+    O::template dma<NW>(static_cast<const E*>(a.q.p) + b * a.q.b + h * a.q.h + (long)r0 * a.q.t, a.q.t, last, dst, a.dh,
+                        lane, wave);
     O::template dma<NW>(static_cast<const E*>(a.dout.p) + b * a.dout.b + h * a.dout.h + (long)r0 * a.dout.t, a.dout.t,
                         last, dst + TILE, a.dh, lane, wave);
-  };
-  // that iteration's row statistics, one query per thread of the first KR
-  auto load_stats = [&](float& lv, float& dv) {
-    lv = dv = 0.f;
-    if (threadIdx.x < KR) {
-      const long at = ((long)b * a.H + h) * a.Sq + min((qt0 + t) * KR + (int)threadIdx.x, sq.lq - 1);
-      lv = lse_or_inf(a.lse[at]);
-      dv = a.dsum[at];
+    // 32 rows per DMA; waves of the same remainder bring the same ones, so that every wave counts alike
+    const int s0 = wave % (KR / 32) * 32;
+    dma4_m0(uniform_ptr(a.stat + ((long)b * a.H + h) * a.Sq + r0), (uint32_t)(min(s0 + lane / 2, last) * 8 + lane % 2 * 4),
+            lds_addr(sS[stage]) + s0 * 8);
+    ++issued;
+    if (++t == nt) {
+      t = 0;
+      ++h;
     }
   };
-  auto put_stats = [&](int buf, float lv, float dv) {
-    if (threadIdx.x < KR) {
-      sL[buf][threadIdx.x] = lv;
-      sD[buf][threadIdx.x] = dv;
-    }
-  };
-  float lnext = 0.f, dnext = 0.f;
-  if (i0 < i1) {
-    issue(0);
-    load_stats(lnext, dnext);
-    if (BIAS) load_bias(a, h, sbias);
-  }
+  while (issued < min(i1, i0 + ST - 1)) issue();
+  // head and query tile of the iteration that is computed, and its bias
+  int hc = hk * grp + (nt > 0 ? i0 / nt : 0), tc = nt > 0 ? i0 % nt : 0, hb = 0;
+  if (BIAS && i0 < i1) load_bias(a, hc, sbias);
   typename O::Rows kf, vf;
   const long row = kv ? key : 0;
   O::load_rows(kf, static_cast<const E*>(a.k.p) + b * a.k.b + row * a.k.t + hk * a.k.h, kv, half, a.dh);
@@ -863,43 +984,38 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
   for (int i = 0; i < DH / 32; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) dk[i][r] = dv[i][r] = 0.f;
-  if (i0 < i1) put_stats(0, lnext, dnext);
 
-  int hb = 0;  // the buffer of the current head's bias
+  kf.settled();
+  vf.settled();
   for (int i = i0; i < i1; ++i) {
-    const int buf = (i - i0) & 1, qt = qt0 + t, hb_now = hb;
-    tiles_ready();
-    if (i + 1 < i1) {
-      if (++t == nt) {
-        t = 0;
-        ++h;
-        hb ^= 1;
-        // goes where the last head's was: read for the last time before this barrier
-        if (BIAS) load_bias(a, h, sbias + hb * W);
-      }
-      load_stats(lnext, dnext);
-      issue(buf ^ 1);
+    const int stage = (i - i0) % ST, qt = qt0 + tc, hb_now = hb;
+    tile_ready<ST, PER>(i - i0, i1 - i0);
+    if (issued < i1) issue();
+    if (++tc == nt) {
+      tc = 0;
+      ++hc;
+      hb ^= 1;
+      // goes where the last head's was: read for the last time before this barrier
+      if (BIAS && i + 1 < i1) load_bias(a, hc, sbias + hb * W);
     }
-    const E* sQ = sm + buf * 2 * TILE;
+    const E* sQ = sm + stage * 2 * TILE;
     const E* sO = sQ + TILE;
-    const float* pL = sL[buf];
-    const float* pD = sD[buf];
     const float* bias = sbias + hb_now * W;
 #pragma unroll 1
     for (int qb = 0; qb < KR / 32; ++qb) {
       const int q0 = qt * KR + qb * 32;
-      if (q0 >= sq.lq || k0 >= sq.lk) break;  // wave-uniform
-      const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
-      const int kind = mask.block(k0, 32, plo, phi);
-      if (kind == 0) continue;
+      const int kind = span.kind(q0 / 32);
+      if (kind == 0) continue;  // wave-uniform
       ops.fresh();
-      const bool full = kind == 2 && q0 + 32 <= sq.lq;
       f32x16 st, dp;
       ops.scores(st, sQ, qb, kf);
       ops.scores(dp, sO, qb, vf);
-      if (BIAS) add_bias<-1>(st, sl2, bias, a.R, key - plo, k0 - phi, k0 + 31 - plo, half);
-      if (!full) {
-#pragma unroll
+      if (BIAS) {
+        const int plo = sq.off + q0;
+        add_bias<-1>(st, sl2, bias, a.R, key - plo, k0 - plo - 31, k0 + 31 - plo, half);
+      }
+      if (kind == 1) {
+  #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int qq = q0 + perm_pos(r, half);
           st[r] = ((qq < sq.lq) & mask.pair(sq.off + qq, key)) ? st[r] : -INFINITY;
@@ -907,9 +1023,9 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {  // queries q0 + 8g + 4*half + 0..3
-        const float4 L = *reinterpret_cast<const float4*>(pL + qb * 32 + 8 * g + 4 * half);
-        const float4 D = *reinterpret_cast<const float4*>(pD + qb * 32 + 8 * g + 4 * half);
-        const float lv[4] = {L.x, L.y, L.z, L.w}, sv[4] = {D.x, D.y, D.z, D.w};
+        const float4* ld = reinterpret_cast<const float4*>(sS[stage] + qb * 32 + 8 * g + 4 * half);
+        const float4 x = ld[0], y = ld[1];
+        const float lv[4] = {x.x, x.z, y.x, y.z}, sv[4] = {x.y, x.w, y.y, y.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int r = 4 * g + e;
@@ -920,7 +1036,6 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
       ops.accum(dv, sO, qb, st);
       ops.accum(dk, sQ, qb, dp);
     }
-    if (i + 1 < i1) put_stats(buf ^ 1, lnext, dnext);  // the other buffer: last read before this tile's barrier
   }
   if (ki.n > 1) {  // in the accumulators' own order, 1 KB per store
     float4* dst = reinterpret_cast<float4*>(a.part + (((long)bh * w.slots() + item) * NW + wave) * (2 * 32 * DH)) + lane;
@@ -986,32 +1101,35 @@ __global__ __launch_bounds__(64) void attn_masked_dkdv_join(MaskedAttnArgs a, Ke
            stream_out((long)a.B * a.Sk * a.Hkv * DH * (long)sizeof(E)), a.Sk - k0, a.dh);
 }
 
-// The table's gradient from the dQ pass's partial sums diag[row][head][W]: first the sum
-// over the rows for each relative position (64 of them per workgroup, a row per wave and
-// step), then dtable[t][h] += the positions of bucket t (a wave each).  Both in a fixed order;
-// in 64 bits, which costs nothing here.
-__global__ __launch_bounds__(1024) void attn_bias_rows(MaskedAttnArgs a, int rows) {
-  __shared__ double part[16][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = 2 * a.R + 1, h = blockIdx.y;
-  const int i = blockIdx.x * 64 + lane;
-  double s = 0.0;
-  if (i < W)
-#pragma unroll 4
-    for (int r = wave; r < rows; r += 16) s += (double)a.diag[((long)r * a.H + h) * W + i];
-  part[wave][lane] = s;
-  __syncthreads();
-  if (wave == 0 && i < W) {
-    for (int k = 1; k < 16; ++k) s += part[k][lane];
-    a.diag_sum[(long)h * W + i] = s;
+// dtable[t][h] += the sums of dS over the relative positions of bucket t, from the dQ pass's
+// partial sums diag[row][head][W]: one workgroup per head; position by position over the rows (as
+// many rows at a time as 1024 threads hold positions), then a wave per bucket.  In a
+// fixed order; in 64 bits, which costs nothing here.
+__global__ __launch_bounds__(1024) void attn_bias_grad(MaskedAttnArgs a, int rows) {
+  __shared__ double part[1024], sum[2 * ATTN_MAX_DISTANCE + 1];
+  const int W = 2 * a.R + 1, h = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int span = min(1024, (W + 63) / 64 * 64), groups = 1024 / span, g = threadIdx.x / span, at = threadIdx.x % span;
+  for (int i0 = 0; i0 < W; i0 += span) {
+    const int i = i0 + at;
+    double s = 0.0;
+    if (g < groups && i < W)
+#pragma unroll 8
+      for (int r = g; r < rows; r += groups) s += (double)a.diag[((long)r * a.H + h) * W + i];
+    part[threadIdx.x] = s;
+    __syncthreads();
+    if (g == 0 && i < W) {
+      for (int k = 1; k < groups; ++k) s += part[k * span + at];
+      sum[i] = s;
+    }
+    __syncthreads();
   }
-}
-__global__ __launch_bounds__(64) void attn_bias_grad(MaskedAttnArgs a) {
-  const int t = blockIdx.x, h = blockIdx.y, W = 2 * a.R + 1;
-  double s = 0.0;
-  for (int i = threadIdx.x; i < W; i += 64)
-    if (min(max(a.bucket[i], 0), a.nb - 1) == t) s += a.diag_sum[(long)h * W + i];
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-  if (threadIdx.x == 0) a.dtable[(long)t * a.H + h] += (float)s;
+  for (int t = wave; t < a.nb; t += 16) {
+    double s = 0.0;
+    for (int i = lane; i < W; i += 64)
+      if (min(max(a.bucket[i], 0), a.nb - 1) == t) s += sum[i];
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    if (lane == 0) a.dtable[(long)t * a.H + h] += (float)s;
+  }
 }
 
 // ================================================================ launchers
@@ -1045,13 +1163,12 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
 }
 
 struct BwdSpace {
-  size_t diag, sum, part, total;
+  size_t diag, part, total;
 };
 static BwdSpace bwd_space(int dtype, const MaskedAttnArgs& a, bool dtable) {
   BwdSpace s;
-  s.diag = al256((size_t)a.B * a.H * a.Sq * 4);
-  s.sum = s.diag + (dtable ? al256((size_t)a.B * blocks_of(a.Sq) * a.H * (2 * a.R + 1) * 4) : 0);
-  s.part = s.sum + (dtable ? al256((size_t)a.H * (2 * a.R + 1) * 8) : 0);
+  s.diag = al256((size_t)a.B * a.H * a.Sq * 8);
+  s.part = s.diag + (dtable ? al256((size_t)a.B * blocks_of(a.Sq) * a.H * (2 * a.R + 1) * 4) : 0);
   const int dh = a.dh <= 64 ? 64 : 128;
   s.total = s.part + al256((size_t)a.B * a.Hkv * key_work(dtype, a).slots() * MA_NW * 2 * 32 * dh * 4);
   return s;
@@ -1087,9 +1204,8 @@ void masked_attn_bytes(int dtype, const MaskedAttnArgs& a, bool dtable, size_t* 
 void masked_attn_workspace(int dtype, MaskedAttnArgs& a, void* ws) {
   const BwdSpace s = bwd_space(dtype, a, a.dtable != nullptr);
   char* p = static_cast<char*>(ws);
-  a.dsum = reinterpret_cast<float*>(p);
+  a.stat = reinterpret_cast<float2*>(p);
   a.diag = reinterpret_cast<float*>(p + s.diag);
-  a.diag_sum = reinterpret_cast<double*>(p + s.sum);
   a.part = reinterpret_cast<float*>(p + s.part);
 }
 
@@ -1121,8 +1237,7 @@ static hipError_t bwd_ops(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
     else RG_LAUNCH((attn_masked_bwd_dq<O, true, false, MA_NW>), gq, block, W * 4, s, a);
     RG_LAUNCH((attn_masked_bwd_dkdv<O, true, MA_NW>), gk, block, 2 * W * 4, s, a, w);
     if (a.dtable) {
-      RG_LAUNCH(attn_bias_rows, dim3((W + 63) / 64, a.H), dim3(1024), 0, s, a, (int)(a.B * blocks_of(a.Sq)));
-      RG_LAUNCH(attn_bias_grad, dim3(a.nb, a.H), dim3(64), 0, s, a);
+      RG_LAUNCH(attn_bias_grad, dim3(a.H), dim3(1024), 0, s, a, (int)(a.B * blocks_of(a.Sq)));
     }
   } else {
     RG_LAUNCH((attn_masked_bwd_dq<O, false, false, MA_NW>), gq, block, 0, s, a);

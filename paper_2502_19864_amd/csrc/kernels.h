@@ -103,9 +103,8 @@ struct MaskedAttnArgs {
   const float2* rope_tab;     // bf16: q and k come rotated (positions = rows); dq and dk are rotated back; or null
   View dout, dq, dk, dv;
   float* dtable;              // [nb, H] or null, added into
-  float* dsum;                // workspace: D [B, H, Sq]
+  float2* stat;               // workspace: (lse, D) [B, H, Sq], lse +inf for a row that sees nothing
   float* diag;                // workspace (dtable): sums of dS by relative position, per workgroup of the dQ pass
-  double* diag_sum;           // and those sums over the workgroups, [H, 2R + 1]
   float* part;                // workspace: partial sums of workgroups that share their output rows
 };
 // bytes of the workspaces, and the backward's pointers into its own
