@@ -46,17 +46,48 @@ struct Mask {
   int lk, causal, window, sinks;  // window 0: none
   __device__ __forceinline__ Mask(const MaskedAttnArgs& a, int lk_)
       : lk(lk_), causal(a.causal), window(a.window), sinks(a.sinks) {}
-  // without branches: what follows in a wave has matrix instructions and transpose reads, which take
-  // all 64 lanes, so no lane may leave on its own
-  __device__ __forceinline__ bool pair(int p, int j) const {
-    return (j < lk) & ((causal == 0) | (j <= p)) & ((window == 0) | (abs(p - j) < window) | (j < sinks));
-  }
 };
+// The visible ones among consecutive rows: one interval (and, for a query, the first `sinks`
+// keys), so a test is a subtraction and a comparison or two.  No branches: what follows in a
+// wave has matrix instructions and transpose reads, which take all 64 lanes, so no lane
+// may leave on its own.
+struct Visible {
+  int lo;
+  unsigned n1;  // interval lo .. lo + n1
+  int sinks;
+  __device__ __forceinline__ Visible(int lo_, int hi, int sinks_) : lo(lo_), n1(hi - lo_), sinks(sinks_) {
+    if (hi < lo_) {
+      lo = 1 << 30;  // beyond every row
+      n1 = 0;
+    }
+  }
+  __device__ __forceinline__ bool has(int i) const { return ((unsigned)(i - lo) <= n1) | (i < sinks); }
+};
+// keys of the query at position p
+__device__ __forceinline__ Visible keys_of(const Mask& m, int p) {
+  int lo = 0, hi = m.lk - 1, sk = 0;
+  if (m.causal) hi = min(hi, p);
+  if (m.window) {
+    sk = min(m.sinks, hi + 1);
+    lo = max(lo, p - m.window + 1);
+    hi = min(hi, p + m.window - 1);
+  }
+  return Visible(lo, hi, sk);
+}
+// query rows (row i at position off + i, lq of them) of a key; no sinks: to one every row is near
+__device__ __forceinline__ Visible rows_of(const Mask& m, int key, int off, int lq) {
+  int lo = 0, hi = lq - 1;
+  if (m.causal) lo = max(lo, key - off);
+  if (m.window && key >= m.sinks) {
+    lo = max(lo, key - m.window + 1 - off);
+    hi = min(hi, key + m.window - 1 - off);
+  }
+  return Visible(lo, key < m.lk ? hi : -1, 0);
+}
 
 // What a loop meets, by blocks of 32: blocks v0 .. v1 and those below vs hold something
 // visible, f0 .. f1 and those below fs nothing else.  Worked out once per wave, so that a step
-// costs a few scalar comparisons (formed anew per block, these and the tests of
-// Mask were a quarter of the instructions).
+// costs a few scalar comparisons.
 struct Span {
   int v0, v1, vs, f0, f1, fs;
   // 0 nothing visible, 2 everything, 1 else
@@ -168,7 +199,7 @@ __device__ __forceinline__ void settle(T& x) {
 }
 
 // ================================================================ storage types
-// A tile is KR rows of one head in LDS.  dma() brings this wave's share (of NW) of rows 0 .. ROWS - 1
+// A tile is KR rows of one head in LDS.  dma() brings this wave's share (of NW) of rows 0 .. KR - 1
 // from src (rows past `last` read row `last`: what they score is masked); scores() forms the block
 // [32 tile rows][32 own rows] (lane = own row, register r = tile row perm_pos(r)); accum() adds
 // tile^T p to acc (lane = own row, registers = head dims).
@@ -206,16 +237,38 @@ struct OpsBf16 {
     }
     return s + __shfl_xor(s, 32, 64);
   }
-  template <int NW, int ROWS = KR>
-  static __device__ __forceinline__ void dma(const E* src, long ld, int last, E* dst, int, int lane, int wave) {
+  // byte offset of this lane in DMA i of a wave; rows past `last` give row `last`
+  template <int NW>
+  static __device__ __forceinline__ uint32_t dma_at(int i, long ld, int last, int, int lane, int wave) {
     constexpr int CPR = DH / 8, RPI = 64 / CPR;
-    static_assert(ROWS % (RPI * NW) == 0, "whole DMA instructions per wave");
+    const int r = (i * NW + wave) * RPI + lane / CPR, c = (lane % CPR) ^ swz<DH>(r);
+    return ((uint32_t)min(r, last) * (uint32_t)ld + c * 8) * 2;
+  }
+  // ... in DMA 0 of a whole tile: DMA i is i * NW * RPI rows on (the swizzle repeats after 16 rows)
+  template <int NW>
+  static __device__ __forceinline__ uint32_t dma_first(long ld, int dh, int lane, int wave) {
+    return dma_at<NW>(0, ld, KR, dh, lane, wave);
+  }
+  template <int NW>
+  static __device__ __forceinline__ void dma(const E* src, long ld, int last, E* dst, int dh, int lane, int wave,
+                                             uint32_t first) {
+    constexpr int RPI = 512 / DH, N = KR / (RPI * NW);
+    static_assert(KR % (RPI * NW) == 0 && NW * RPI % 16 == 0, "whole DMA instructions per wave");
+    src = uniform_ptr(src);
+    const uint32_t lds = lds_addr(dst) + wave * 1024;
+    if (last >= KR - 1) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) dma16_m0(src + i * (NW * RPI) * ld, first, lds + i * NW * 1024);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) dma16_m0(src, dma_at<NW>(i, ld, last, dh, lane, wave), lds + i * NW * 1024);
+    }
+  }
+  // 32 rows by one wave
+  static __device__ __forceinline__ void dma_block(const E* src, long ld, int last, E* dst, int dh, int lane) {
     src = uniform_ptr(src);
 #pragma unroll
-    for (int i = 0; i < ROWS / (RPI * NW); ++i) {
-      const int r = (i * NW + wave) * RPI + lane / CPR, c = (lane % CPR) ^ swz<DH>(r);
-      dma16_m0(src, ((uint32_t)min(r, last) * (uint32_t)ld + c * 8) * 2, lds_addr(dst) + (i * NW + wave) * 1024);
-    }
+    for (int i = 0; i < BLOCK_DMAS(32); ++i) dma16_m0(src, dma_at<1>(i, ld, last, dh, lane, 0), lds_addr(dst) + i * 1024);
   }
   __device__ __forceinline__ void scores(f32x16& st, const E* tile, int kb, const Rows& own) const {
 #pragma unroll
@@ -276,17 +329,37 @@ struct OpsF32 {
     return s + __shfl_xor(s, 32, 64);
   }
   // 4 B per lane: any alignment of the rows will do
-  template <int NW, int ROWS = KR>
-  static __device__ __forceinline__ void dma(const E* src, long ld, int last, E* dst, int dh, int lane, int wave) {
+  template <int NW>
+  static __device__ __forceinline__ uint32_t dma_at(int i, long ld, int last, int dh, int lane, int wave) {
     constexpr int CPR = DHM / 64;
-    static_assert(ROWS == KR && KR * CPR % NW == 0, "whole DMA instructions per wave");
+    const int n = i * NW + wave;
+    return ((uint32_t)min(n / CPR, last) * (uint32_t)ld + min(n % CPR * 64 + lane, dh - 1)) * 4;
+  }
+  template <int NW>
+  static __device__ __forceinline__ uint32_t dma_first(long ld, int dh, int lane, int wave) {
+    return dma_at<NW>(0, ld, KR, dh, lane, wave);
+  }
+  template <int NW>
+  static __device__ __forceinline__ void dma(const E* src, long ld, int last, E* dst, int dh, int lane, int wave,
+                                             uint32_t first) {
+    constexpr int CPR = DHM / 64, N = KR * CPR / NW;
+    static_assert(KR * CPR % NW == 0 && NW % CPR == 0, "whole DMA instructions per wave, each of one part of the rows");
+    src = uniform_ptr(src);
+    const uint32_t lds = lds_addr(dst) + (wave / CPR * P + wave % CPR * 64) * 4;
+    if (last >= KR - 1) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) dma4_m0(src + i * (NW / CPR) * ld, first, lds + i * (NW / CPR) * P * 4);
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) dma4_m0(src, dma_at<NW>(i, ld, last, dh, lane, wave), lds + i * (NW / CPR) * P * 4);
+    }
+  }
+  static __device__ __forceinline__ void dma_block(const E* src, long ld, int last, E* dst, int dh, int lane) {
+    constexpr int CPR = DHM / 64;
     src = uniform_ptr(src);
 #pragma unroll
-    for (int i = 0; i < KR * CPR / NW; ++i) {
-      const int n = i * NW + wave, r = n / CPR, c = n % CPR;
-      dma4_m0(src, ((uint32_t)min(r, last) * (uint32_t)ld + min(c * 64 + lane, dh - 1)) * 4,
-              lds_addr(dst) + (r * P + c * 64) * 4);
-    }
+    for (int i = 0; i < BLOCK_DMAS(KR); ++i)
+      dma4_m0(src, dma_at<1>(i, ld, last, dh, lane, 0), lds_addr(dst) + (i / CPR * P + i % CPR * 64) * 4);
   }
   __device__ __forceinline__ void scores(f32x16& st, const E* tile, int kb, const Rows& own) const {
     (void)kb;  // a tile is one block
@@ -357,14 +430,33 @@ __device__ __forceinline__ void add_bias(f32x16& st, float sl2, const float* bia
   }
 }
 
-// Sums of a 32 x 32 block of dS along its diagonals, added to the wave's own array
-// diag[rel + R]; what is at or beyond +-R goes to this lane's hi / lo.  Lane c gathers, by
-// one lane permutation per register, the value of the query that puts register r's
-// key on diagonal c (key >= query) or c - 32: no two lanes add to one address, and
-// every sum has a fixed order.
+// x shifted by N lanes within rows of 16, zeros coming in: lane i gets lane i + N (N > 0) or i - |N|
+template <int N>
+__device__ __forceinline__ float row_shift(float x) {
+  if constexpr (N == 0) return x;
+  constexpr int ctrl = N > 0 ? 0x100 + N : 0x110 - N;
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), ctrl, 0xf, 0xf, true));
+}
+// adds register R's part of a block to the diagonals v[j] (add_diag below)
+template <int R>
+__device__ __forceinline__ void diag_part(const f32x16& ds, float (&v)[3]) {
+  if constexpr (R < 16) {
+    constexpr int kap = 8 * ((R >> 2) & 1) + (R & 3), k16 = R >> 3;
+    v[k16] += row_shift<kap>(ds[R]);
+    if constexpr (kap > 0) v[k16 + 1] += row_shift<kap - 16>(ds[R]);
+    diag_part<R + 1>(ds, v);
+  }
+}
+// Sums of a 32 x 32 block of dS (lane = query, register = key) along its diagonals, added to
+// the wave's own array diag[rel + R]; what is at or beyond +-R goes to this lane's hi / lo.  Register
+// r holds key k = 16 k16 + kap + 4 half, so shifting it by kap lanes puts the values of
+// one q - k = c + 16 (lane / 16 % 2 - k16) - 4 half on one lane c of each row of 16, and
+// what a row's end cuts off, shifted the other way, those 16 further: 30 additions give each
+// lane three diagonals' sums, one exchange across 16 lanes two, which no other lane of
+// its half shares.  The halves then add one after the other; a wave's LDS operations run in
+// order, so the sums' order is fixed.
 __device__ __forceinline__ void add_diag(const f32x16& ds, int base, int R, float* diag, float& lo, float& hi,
                                          int lane) {
-  const int half = lane >> 5, c = lane & 31;
   if (base - 31 >= R || base + 31 <= -R) {
     float s = 0.f;
 #pragma unroll
@@ -373,21 +465,32 @@ __device__ __forceinline__ void add_diag(const f32x16& ds, int base, int R, floa
     else lo += s;
     return;
   }
-  float pos = 0.f, neg = 0.f;
+  float v[3] = {0.f, 0.f, 0.f};
+  diag_part<0>(ds, v);
+  // q - k + 4 half: v[0] lane, v[1] lane - 16, v[2] lane - 32
+  const int half = lane >> 5, l32 = lane & 31;
+  const float x = __shfl_xor(v[1], 16, 64);
+  const float sum[2] = {v[0] + (l32 < 16 ? x : 0.f), v[2] + (l32 < 16 ? 0.f : x)};
+  const int rel[2] = {base - l32 + 4 * half, base - l32 + 4 * half + 32};
 #pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int k = perm_pos(r, half);
-    const float w = __shfl(ds[r], 32 * half + ((k - c) & 31), 64);
-    if (c <= k) pos += w;
-    else neg += w;
+  for (int j = 0; j < 2; ++j) {
+    if (rel[j] >= R) hi += sum[j];
+    else if (rel[j] <= -R) lo += sum[j];
   }
-  pos += __shfl_xor(pos, 32, 64);
-  neg += __shfl_xor(neg, 32, 64);
-  const float val = half ? neg : pos;
-  const int rel = base + c - 32 * half;
-  if (rel >= R) hi += val;
-  else if (rel <= -R) lo += val;
-  else diag[rel + R] += val;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (half == h) {
+      float old[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) old[j] = abs(rel[j]) < R ? diag[rel[j] + R] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (abs(rel[j]) < R) diag[rel[j] + R] = old[j] + sum[j];
+    }
+    // to one lane the two steps are alternatives: nothing but this keeps them apart
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 // ================================================================ forward
@@ -429,17 +532,20 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
   const bool qv = q < sq.lq;
   const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
   const Span span = key_span(mask, plo, phi);
+  const Visible seen = keys_of(mask, p);
   KeyTiles kt{0, 0, 0};
   if (qw0 < sq.lq) kt = key_tiles<KR>(mask, sq.off + qw0, sq.off + min(qw0 + 32 * NW, sq.lq) - 1);
   const float sl2 = kLog2e * a.scale;
   const E* K = static_cast<const E*>(a.k.p) + b * a.k.b + hk * a.k.h;
   const E* V = static_cast<const E*>(a.v.p) + b * a.v.b + hk * a.v.h;
   const O ops(lane, a.dh);
+  const uint32_t kfirst = O::template dma_first<NW>(a.k.t, a.dh, lane, wave);
+  const uint32_t vfirst = O::template dma_first<NW>(a.v.t, a.dh, lane, wave);
   auto issue = [&](int i) {
     const int k0 = kt.at(i) * KR, last = sq.lk - 1 - k0;
     E* dst = sm + (i % ST) * 2 * TILE;
-    O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, wave);
-    O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh, lane, wave);
+    O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, wave, kfirst);
+    O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh, lane, wave, vfirst);
   };
   for (int i = 0; i < min(ST - 1, kt.n); ++i) issue(i);
   typename O::Rows qf;
@@ -482,7 +588,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
       for (int kb = 0; kb < KR / 32; ++kb)
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          sc[kb][r] = mask.pair(p, k0 + kb * 32 + perm_pos(r, half)) ? sc[kb][r] : -INFINITY;
+          sc[kb][r] = seen.has(k0 + kb * 32 + perm_pos(r, half)) ? sc[kb][r] : -INFINITY;
     }
 #pragma unroll
     for (int kb = 0; kb < KR / 32; ++kb)
@@ -551,6 +657,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
   const bool qv = tok < sq.lq;
   const int tok0 = rb * 32 / grp, plo = sq.off + tok0, phi = sq.off + min((rb * 32 + 31) / grp, sq.lq - 1);
   const Span span = key_span(mask, plo, phi);
+  const Visible seen = keys_of(mask, p);
   KeyTiles kt{0, 0, 0};
   if (tok0 < sq.lq) kt = key_tiles<32>(mask, plo, phi);
   const int per = (kt.n + w.split - 1) / w.split, i1 = min(kt.n, (split + 1) * per);
@@ -562,8 +669,8 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
   auto issue = [&](int i, int buf) {
     const int k0 = kt.at(i) * 32, last = sq.lk - 1 - k0;
     E* dst = tiles + buf * 2 * BLOCK;
-    O::template dma<1, 32>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, 0);
-    O::template dma<1, 32>(V + (long)k0 * a.v.t, a.v.t, last, dst + BLOCK, a.dh, lane, 0);
+    O::dma_block(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane);
+    O::dma_block(V + (long)k0 * a.v.t, a.v.t, last, dst + BLOCK, a.dh, lane);
   };
   int i = split * per + wave;
   if (i < i1) issue(i, 0);
@@ -618,7 +725,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
     }
     if (kind == 1) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = mask.pair(p, k0 + perm_pos(r, half)) ? sc[r] : -INFINITY;
+      for (int r = 0; r < 16; ++r) sc[r] = seen.has(k0 + perm_pos(r, half)) ? sc[r] : -INFINITY;
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -755,6 +862,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   const bool qv = q < sq.lq;
   const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
   const Span span = key_span(mask, plo, phi);
+  const Visible seen = keys_of(mask, p);
   KeyTiles kt{0, 0, 0};
   if (qw0 < sq.lq) kt = key_tiles<KR>(mask, sq.off + qw0, sq.off + min(qw0 + 32 * NW, sq.lq) - 1);
   const float sl2 = kLog2e * a.scale;
@@ -762,11 +870,13 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   const E* V = static_cast<const E*>(a.v.p) + b * a.v.b + hk * a.v.h;
   O ops(lane, a.dh);
   const int nit = DTAB ? 2 * kt.n : kt.n;  // DTAB: the tiles twice
+  const uint32_t kfirst = O::template dma_first<NW>(a.k.t, a.dh, lane, wave);
+  const uint32_t vfirst = O::template dma_first<NW>(a.v.t, a.dh, lane, wave);
   auto issue = [&](int i) {
     const int k0 = kt.at(DTAB && i >= kt.n ? i - kt.n : i) * KR, last = sq.lk - 1 - k0;
     E* dst = sm + (i % ST) * 2 * TILE;
-    O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, wave);
-    O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh, lane, wave);
+    O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, wave, kfirst);
+    O::template dma<NW>(V + (long)k0 * a.v.t, a.v.t, last, dst + TILE, a.dh, lane, wave, vfirst);
   };
   for (int i = 0; i < min(ST - 1, nit); ++i) issue(i);
   const long row = qv ? q : 0;
@@ -819,7 +929,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
       if (kind == 1) {  // a row past len_q has lse = +inf
   #pragma unroll
         for (int r = 0; r < 16; ++r)
-          st[r] = mask.pair(p, k0 + perm_pos(r, half)) ? st[r] : -INFINITY;
+          st[r] = seen.has(k0 + perm_pos(r, half)) ? st[r] : -INFINITY;
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) st[r] = __builtin_amdgcn_exp2f(BIAS ? st[r] - lse : fmaf(st[r], sl2, -lse));
@@ -904,6 +1014,15 @@ __device__ __forceinline__ void query_tiles(const MaskedAttnArgs& a, const Seq& 
   qt0 = qlo / KR;
   nt = qhi / KR - qt0 + 1;
 }
+// Whether the iterations i0 .. i1 - 1 (query tile i % nt, from qt0) touch any block of `span`: a wave
+// without any leaves no partial sums, and the join reads none.
+template <int KR>
+__device__ __forceinline__ bool touches(const Span& span, int qt0, int nt, int i0, int i1) {
+  const int t0 = span.v0 / (KR / 32) - qt0, t1 = (span.v1 >= 0 ? span.v1 / (KR / 32) : -1) - qt0;
+  if (span.v1 < span.v0 || i1 <= i0) return false;
+  const int a = i0 % nt, b = a + (i1 - i0) - 1;  // tiles a .. b, taken modulo nt
+  return i1 - i0 >= nt || (t0 <= b && t1 >= a) || (b >= nt && t0 <= b - nt);
+}
 // item and batch-head of a workgroup: items in order of weight over all heads of an XCD
 __device__ __forceinline__ void key_item(int lin, int items, int nbh, int& item, int& bh) {
   const int n = items * nbh, P = n / 8;
@@ -942,6 +1061,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
   int qt0, nt;
   query_tiles<KR>(a, sq, kw0, 32 * NW, qt0, nt);
   const Span span = query_span(mask, k0, sq.off, sq.lq);
+  const Visible seen = rows_of(mask, key, sq.off, sq.lq);
   const int i0 = ki.n > 1 ? ki.split * ki.c : 0, i1 = ki.n > 1 ? min(nt * grp, i0 + ki.c) : nt * grp;
   if (ki.n > 1 && i0 >= i1) return;  // the join counts the same way
   const float sl2 = kLog2e * a.scale;
@@ -952,15 +1072,17 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
     h += i0 / nt;
     t = i0 % nt;
   }
+  const uint32_t qfirst = O::template dma_first<NW>(a.q.t, a.dh, lane, wave);
+  const uint32_t ofirst = O::template dma_first<NW>(a.dout.t, a.dh, lane, wave);
   // brings the tile of (h, t) into a stage and moves on to the next one
   int issued = i0;
   auto issue = [&]() {
     const int r0 = (qt0 + t) * KR, last = sq.lq - 1 - r0, stage = (issued - i0) % ST;
     E* dst = sm + stage * 2 * TILE;
     O::template dma<NW>(static_cast<const E*>(a.q.p) + b * a.q.b + h * a.q.h + (long)r0 * a.q.t, a.q.t, last, dst, a.dh,
-                        lane, wave);
+                        lane, wave, qfirst);
     O::template dma<NW>(static_cast<const E*>(a.dout.p) + b * a.dout.b + h * a.dout.h + (long)r0 * a.dout.t, a.dout.t,
-                        last, dst + TILE, a.dh, lane, wave);
+                        last, dst + TILE, a.dh, lane, wave, ofirst);
     // 32 rows per DMA; waves of the same remainder bring the same ones, so that every wave counts alike
     const int s0 = wave % (KR / 32) * 32;
     dma4_m0(uniform_ptr(a.stat + ((long)b * a.H + h) * a.Sq + r0), (uint32_t)(min(s0 + lane / 2, last) * 8 + lane % 2 * 4),
@@ -1017,8 +1139,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
       if (kind == 1) {
   #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int qq = q0 + perm_pos(r, half);
-          st[r] = ((qq < sq.lq) & mask.pair(sq.off + qq, key)) ? st[r] : -INFINITY;
+          st[r] = (unsigned)(q0 + perm_pos(r, half) - seen.lo) <= seen.n1 ? st[r] : -INFINITY;
         }
       }
 #pragma unroll
@@ -1038,6 +1159,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
     }
   }
   if (ki.n > 1) {  // in the accumulators' own order, 1 KB per store
+    if (!touches<KR>(span, qt0, nt, i0, i1)) return;
     float4* dst = reinterpret_cast<float4*>(a.part + (((long)bh * w.slots() + item) * NW + wave) * (2 * 32 * DH)) + lane;
 #pragma unroll
     for (int i = 0; i < DH / 32; ++i)
@@ -1059,46 +1181,87 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
            nt_out, a.Sk - k0, a.dh);
 }
 
-// adds a split block's partial sums, in order, and writes its rows; one wave per 32 keys
-// and output
+// Adds a split block's partial sums and writes its rows: one workgroup per 32 keys, output and
+// pair of dim blocks (d, d + DH / 64: what a rotation mixes).  Its four waves take every fourth
+// split each, then wave 0 adds the four, always in this order.
 template <class O, int NW>
-__global__ __launch_bounds__(64) void attn_masked_dkdv_join(MaskedAttnArgs a, KeyWork w, int blocks) {
+__global__ __launch_bounds__(256) void attn_masked_dkdv_join(MaskedAttnArgs a, KeyWork w, int blocks) {
   typedef typename O::E E;
-  constexpr int DH = O::DH;
-  __shared__ __attribute__((aligned(16))) E stage[O::STAGE];
-  const int lane = threadIdx.x, wave = blockIdx.x % NW, kb = blockIdx.x / NW % blocks, bh = blockIdx.x / NW / blocks;
-  const bool is_v = blockIdx.y;
-  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  constexpr int DH = O::DH, ND = DH / 32;
+  __shared__ float4 part[3][8][64];
+  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int sub = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = blockIdx.x % NW, kb = blockIdx.x / NW % blocks, bh = blockIdx.x / NW / blocks;
+  const bool is_v = blockIdx.y & 1;
+  const int d0 = blockIdx.y >> 1, b = bh / a.Hkv, hk = bh % a.Hkv;
+  const int kw0 = kb * 32 * NW, k0 = kw0 + wave * 32, key = k0 + l32;
+  if (k0 >= a.Sk) return;  // the whole workgroup
   const Seq sq = seq_of(a, b);
+  const Mask mask(a, sq.lk);
+  const Span span = query_span(mask, k0, sq.off, sq.lq);
   int qt0, nt;
-  query_tiles<O::KR>(a, sq, kb * 32 * NW, 32 * NW, qt0, nt);
+  query_tiles<O::KR>(a, sq, kw0, 32 * NW, qt0, nt);
   const int item = kb < w.nfar ? kb * w.s_far : w.nfar * w.s_far + (kb - w.nfar) * w.s_near;
-  const int c = kb < w.nfar ? w.c_far : w.c_near, n = (nt * (a.H / a.Hkv) + c - 1) / c;
-  const int k0 = kb * 32 * NW + wave * 32;
-  if (k0 >= a.Sk) return;
-  f32x16 acc[DH / 32];
+  const int c = kb < w.nfar ? w.c_far : w.c_near, nit = nt * (a.H / a.Hkv), n = (nit + c - 1) / c;
+  float4 acc[8];
 #pragma unroll
-  for (int i = 0; i < DH / 32; ++i)
+  for (int i = 0; i < 8; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float4* src = reinterpret_cast<const float4*>(a.part + (((long)bh * w.slots() + item) * NW + wave) * (2 * 32 * DH)) +
+                      (is_v ? DH / 8 * 64 : 0) + lane;
+  const long step = (long)NW * 2 * 32 * DH / 4;
+  for (int s = sub; s < n; s += 4) {
+    if (!touches<O::KR>(span, qt0, nt, s * c, min(nit, s * c + c))) continue;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
-  for (int s = 0; s < n; ++s) {
-    const float4* src = reinterpret_cast<const float4*>(a.part + (((long)bh * w.slots() + item + s) * NW + wave) * (2 * 32 * DH)) +
-                        (is_v ? DH / 8 * 64 : 0) + lane;
-#pragma unroll
-    for (int i = 0; i < DH / 32; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 v = src[(i * 4 + g) * 64];
-        acc[i][4 * g] += v.x;
-        acc[i][4 * g + 1] += v.y;
-        acc[i][4 * g + 2] += v.z;
-        acc[i][4 * g + 3] += v.w;
-      }
+    for (int i = 0; i < 8; ++i) {
+      const float4 v = src[s * step + ((d0 + i / 4 * (ND / 2)) * 4 + i % 4) * 64];
+      acc[i].x += v.x;
+      acc[i].y += v.y;
+      acc[i].z += v.z;
+      acc[i].w += v.w;
+    }
   }
-  if (!is_v) O::rotate_back(acc, a.rope_tab, min(k0 + (lane & 31), a.Sk - 1), lane >> 5);
+  if (sub)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[sub - 1][i][lane] = acc[i];
+  __syncthreads();
+  if (sub || key >= a.Sk) return;
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float4 v = part[k][i][lane];
+      acc[i].x += v.x;
+      acc[i].y += v.y;
+      acc[i].z += v.z;
+      acc[i].w += v.w;
+    }
   const View& o = is_v ? a.dv : a.dk;
-  O::store(acc, is_v ? 1.f : a.scale, lane, stage, static_cast<E*>(o.p) + b * o.b + (long)k0 * o.t + hk * o.h, o.t,
-           stream_out((long)a.B * a.Sk * a.Hkv * DH * (long)sizeof(E)), a.Sk - k0, a.dh);
+  E* dst = static_cast<E*>(o.p) + b * o.b + (long)key * o.t + hk * o.h;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    float x[2][4] = {{acc[g].x, acc[g].y, acc[g].z, acc[g].w}, {acc[4 + g].x, acc[4 + g].y, acc[4 + g].z, acc[4 + g].w}};
+    const int at = d0 * 32 + 8 * g + 4 * half;
+    if (!is_v)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x0 = x[0][e] * a.scale, x1 = x[1][e] * a.scale;
+        float cs = 1.f, sn = 0.f;
+        if (a.rope_tab) rope_cs(a.rope_tab, key, at + e, DH, &cs, &sn);
+        x[0][e] = x0 * cs + x1 * sn;
+        x[1][e] = x1 * cs - x0 * sn;
+      }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int dim = i * (DH / 2) + at;
+      if constexpr (sizeof(E) == 2) {
+        St<E>::st4(dst, dim, x[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (dim + e < a.dh) St<E>::st(dst, dim + e, x[i][e]);
+      }
+    }
+  }
 }
 
 // dtable[t][h] += the sums of dS over the relative positions of bucket t, from the dQ pass's
@@ -1150,10 +1313,12 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
   const long span = (long)rows + (a.causal ? 1l : 2l) * a.window;
   const long near = a.window ? std::min(far, grp * (span / KR + 2)) : far;
   const long wgs = (long)w.nk * a.B * a.Hkv, want = std::max(1l, std::min((512 + wgs - 1) / wgs, near / 4));
-  // a far block as finely as its workgroups take no longer than a near one's, within 64
   w.c_near = (int)((near + want - 1) / want);
   w.s_near = (int)((near + w.c_near - 1) / w.c_near);
-  w.c_far = (int)std::max<long>(w.c_near, (far + 63) / 64);
+  // A far block is left whole up to twice a near one's length (the join costs as much), else
+  // dealt out in quarters of that, so that they fill the gaps: 512 near workgroups of 80
+  // iterations are one round of the GPU, and far ones as long would begin another.
+  w.c_far = (int)(w.s_near == 1 && far <= 2 * near ? far : std::max({(long)(w.c_near + 3) / 4, 4l, (far + 63) / 64}));
   w.s_far = (int)((far + w.c_far - 1) / w.c_far);
   if (w.s_far < w.s_near || (long)w.items() * a.B * a.Hkv >= (1l << 31)) {
     w.s_far = w.s_near = 1;
@@ -1245,7 +1410,8 @@ static hipError_t bwd_ops(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
   }
   const int split = w.s_near > 1 ? w.nk : w.s_far > 1 ? w.nfar : 0;
   if (split)
-    RG_LAUNCH((attn_masked_dkdv_join<O, MA_NW>), dim3((unsigned)(a.B * a.Hkv * split * MA_NW), 2), dim3(64), 0, s, a, w, split);
+    RG_LAUNCH((attn_masked_dkdv_join<O, MA_NW>), dim3((unsigned)(a.B * a.Hkv * split * MA_NW), 2 * O::DH / 64),
+              dim3(256), 0, s, a, w, split);
   return hipGetLastError();
 }
 
