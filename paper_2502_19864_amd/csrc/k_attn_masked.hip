@@ -225,6 +225,11 @@ struct OpsBf16 {
   static __device__ __forceinline__ void load_rows(Rows& o, const E* row, bool valid, int half, int) {
     load_row_frags<DH>(row, valid, half, o.f);
   }
+  // the same from a tile: rows kb * 32 + lane % 32
+  __device__ __forceinline__ void tile_rows(Rows& o, const E* tile, int kb, int) const {
+#pragma unroll
+    for (int i = 0; i < DH / 16; ++i) o.f[i] = rd.frag(tile, kb, i);
+  }
   static __device__ __forceinline__ float dot(const Rows& x, const Rows& y) {
     float s = 0.f;
 #pragma unroll
@@ -303,6 +308,12 @@ struct OpsF32 {
   typedef float E;
   struct Rows {
     float f[DHM / 2];  // dims half * DHM / 2 + i
+    // zero from dim n on; by integer masks, as comparisons would take a scalar pair per element
+    __device__ __forceinline__ void cut(int half, int n) {
+#pragma unroll
+      for (int i = 0; i < DHM / 2; ++i)
+        f[i] = __int_as_float(__float_as_int(f[i]) & ((half * (DHM / 2) + i - n) >> 31));
+    }
     __device__ __forceinline__ void settled() {
 #pragma unroll
       for (int i = 0; i < DHM / 2; ++i) settle(f[i]);
@@ -318,9 +329,19 @@ struct OpsF32 {
   static __device__ __forceinline__ void load_rows(Rows& o, const E* src, bool valid, int half, int dh) {
 #pragma unroll
     for (int i = 0; i < DHM / 2; ++i) o.f[i] = src[min(half * (DHM / 2) + i, dh - 1)];
+    o.cut(half, valid ? dh : 0);
+  }
+  // dims dh .. DHM - 1 hold what the tile holds there: zero them in one operand of a product
+  __device__ __forceinline__ void tile_rows(Rows& o, const E* tile, int, int dh) const {
 #pragma unroll
-    for (int i = 0; i < DHM / 2; ++i)
-      if (!valid || half * (DHM / 2) + i >= dh) o.f[i] = 0.f;
+    for (int i = 0; i < DHM / 8; ++i) {
+      const float4 t = *reinterpret_cast<const float4*>(tile + row + 4 * i);
+      o.f[4 * i] = t.x;
+      o.f[4 * i + 1] = t.y;
+      o.f[4 * i + 2] = t.z;
+      o.f[4 * i + 3] = t.w;
+    }
+    o.cut(half, dh);
   }
   static __device__ __forceinline__ float dot(const Rows& x, const Rows& y) {
     float s = 0.f;
@@ -405,8 +426,14 @@ struct OpsF32 {
 // ================================================================ the bias
 // The bias of one head by relative position, times log2 e, from -R to R.  Beyond R it
 // is constant, so a block past it reads one value.
+// All NT threads go through the loop together, the last ones on the last entry: after a loop that
+// lanes leave one by one, the compiler has been seen to save a register (to an accumulation
+// register, the scalar ones being spilled there too) before it restored the execution mask.
+template <int NT>
 __device__ __forceinline__ void load_bias(const MaskedAttnArgs& a, int h, float* dst) {
-  for (int i = threadIdx.x; i < 2 * a.R + 1; i += blockDim.x) {
+  const int W = 2 * a.R + 1;
+  for (int i0 = 0; i0 < W; i0 += NT) {
+    const int i = min(i0 + (int)threadIdx.x, W - 1);
     const int t = min(max(a.bucket[i], 0), a.nb - 1);
     const float v = a.table[(long)t * a.H + h];
     dst[i] = v <= kHidden ? -INFINITY : v * kLog2e;
@@ -550,7 +577,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
   for (int i = 0; i < min(ST - 1, kt.n); ++i) issue(i);
   typename O::Rows qf;
   O::load_rows(qf, static_cast<const E*>(a.q.p) + b * a.q.b + (long)(qv ? q : 0) * a.q.t + h * a.q.h, qv, half, a.dh);
-  if (BIAS) load_bias(a, h, sbias);
+  if (BIAS) load_bias<64 * NW>(a, h, sbias);
 
   f32x16 oacc[DH / 32];
 #pragma unroll
@@ -838,6 +865,74 @@ __global__ __launch_bounds__(256) void attn_few_join(MaskedAttnArgs a, FewWork w
 // exponent offset of a row that sees nothing: exp2(x - inf) = 0
 __device__ __forceinline__ float lse_or_inf(float l) { return l == -INFINITY ? INFINITY : l; }
 
+// st = P and dp = dP of a block (lane = query, registers = keys k0 ..) against tiles of K and V
+template <class O, bool BIAS>
+__device__ __forceinline__ void p_and_dp(const O& ops, f32x16& st, f32x16& dp, const typename O::E* sK,
+                                         const typename O::E* sV, int kb, const typename O::Rows& qf,
+                                         const typename O::Rows& df, float sl2, const float* bias, int R, int k0, int p,
+                                         int plo, int phi, bool whole, const Visible& seen, float lse, int half) {
+  ops.scores(st, sK, kb, qf);
+  ops.scores(dp, sV, kb, df);
+  if (BIAS) add_bias<1>(st, sl2, bias, R, k0 - p, k0 - phi, k0 + 31 - plo, half);
+  if (!whole) {  // a row past len_q has lse = +inf
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st[r] = seen.has(k0 + perm_pos(r, half)) ? st[r] : -INFINITY;
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) st[r] = __builtin_amdgcn_exp2f(BIAS ? st[r] - lse : fmaf(st[r], sl2, -lse));
+}
+// st = P and dp = dS of a block (lane = key, registers = query rows q0 ..) against tiles of Q and
+// dO; stat: (lse, D) of those rows
+template <class O, bool BIAS>
+__device__ __forceinline__ void p_and_ds(const O& ops, f32x16& st, f32x16& dp, const typename O::E* sQ,
+                                         const typename O::E* sO, int qb, const typename O::Rows& kf,
+                                         const typename O::Rows& vf, float sl2, const float* bias, int R, int q0, int off,
+                                         int key, int k0, bool whole, const Visible& seen, const float2* stat, int half) {
+  ops.scores(st, sQ, qb, kf);
+  ops.scores(dp, sO, qb, vf);
+  if (BIAS) {
+    const int plo = off + q0;
+    add_bias<-1>(st, sl2, bias, R, key - plo, k0 - plo - 31, k0 + 31 - plo, half);
+  }
+  if (!whole) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      st[r] = (unsigned)(q0 + perm_pos(r, half) - seen.lo) <= seen.n1 ? st[r] : -INFINITY;
+  }
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {  // queries q0 + 8g + 4*half + 0..3
+    const float4* ld = reinterpret_cast<const float4*>(stat + 8 * g + 4 * half);
+    const float4 x = ld[0], y = ld[1];
+    const float lv[4] = {x.x, x.z, y.x, y.z}, sv[4] = {x.y, x.w, y.y, y.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = 4 * g + e;
+      st[r] = __builtin_amdgcn_exp2f(BIAS ? st[r] - lv[e] : fmaf(st[r], sl2, -lv[e]));
+      dp[r] = st[r] * (dp[r] - sv[e]);
+    }
+  }
+}
+// a workgroup's sums along the diagonals leave as one row of the workspace: the waves' arrays
+// follow the bias in LDS, what lay beyond +-R is in the lanes' lo and hi
+__device__ __forceinline__ void close_diag(float* diag, int W, float lo, float hi, int lane) {
+  lo = wave_sum(lo);
+  hi = wave_sum(hi);
+  if (lane == 0) {
+    diag[0] += lo;
+    diag[W - 1] += hi;
+  }
+}
+template <int NW>
+__device__ __forceinline__ void put_diag(const float* sbias, int W, float* out) {
+  for (int i0 = 0; i0 < W; i0 += 64 * NW) {  // all threads, as in load_bias
+    const int i = min(i0 + (int)threadIdx.x, W - 1);
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) s += sbias[(1 + w) * W + i];
+    out[i] = s;
+  }
+}
+
 // dQ pass (lane = query); writes (lse, D).  DTAB: dtable is wanted, and D is formed from
 // P and dP themselves in a first sweep over the tiles: the sums over dS cancel, and a D
 // from the stored (rounded) O would leave an error of that rounding in them.  That sweep
@@ -892,9 +987,9 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   float lse = qv ? lse_or_inf(a.lse[(long)bh * a.Sq + row]) : INFINITY;
   const int W = 2 * a.R + 1;
   float* diag = sbias + (1 + wave) * W;
-  if (BIAS) load_bias(a, h, sbias);
+  if (BIAS) load_bias<64 * NW>(a, h, sbias);
   if (DTAB)
-    for (int i = lane; i < W; i += 64) diag[i] = 0.f;
+    for (int i = 0; i < W; i += 64) diag[min(i + lane, W - 1)] = 0.f;  // all lanes, as in load_bias
   float dlo = 0.f, dhi = 0.f;
 
   f32x16 dq[DH / 32];
@@ -923,16 +1018,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
       if (kind == 0) continue;  // wave-uniform
       ops.fresh();
       f32x16 st, dp;
-      ops.scores(st, sK, kb, qf);
-      ops.scores(dp, sV, kb, df);
-      if (BIAS) add_bias<1>(st, sl2, sbias, a.R, k0 - p, k0 - phi, k0 + 31 - plo, half);
-      if (kind == 1) {  // a row past len_q has lse = +inf
-  #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          st[r] = seen.has(k0 + perm_pos(r, half)) ? st[r] : -INFINITY;
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) st[r] = __builtin_amdgcn_exp2f(BIAS ? st[r] - lse : fmaf(st[r], sl2, -lse));
+      p_and_dp<O, BIAS>(ops, st, dp, sK, sV, kb, qf, df, sl2, sbias, a.R, k0, p, plo, phi, kind == 2, seen, lse, half);
       if (first) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) dsum = fmaf(st[r], dp[r], dsum);
@@ -946,24 +1032,9 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   }
   // the row statistics that the dK/dV pass reads
   if (q < a.Sq && half == 0) a.stat[(long)bh * a.Sq + q] = make_float2(lse, dsum);
-  if (DTAB) {
-    dlo = wave_sum(dlo);
-    dhi = wave_sum(dhi);
-    if (lane == 0) {
-      diag[0] += dlo;
-      diag[W - 1] += dhi;
-    }
-  }
+  if (DTAB) close_diag(diag, W, dlo, dhi, lane);
   tiles_ready();  // the tiles' space now takes the dQ rows
-  if (DTAB) {
-    float* out = a.diag + ((long)(b * nq + qb) * a.H + h) * W;
-    for (int i = threadIdx.x; i < W; i += 64 * NW) {
-      float s = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) s += sbias[(1 + w) * W + i];
-      out[i] = s;
-    }
-  }
+  if (DTAB) put_diag<NW>(sbias, W, a.diag + ((long)(b * nq + qb) * a.H + h) * W);
   if (q0 >= a.Sq) return;
   O::rotate_back(dq, a.rope_tab, min(q, a.Sq - 1), half);
   O::store(dq, a.scale, lane, sm + wave * O::STAGE,
@@ -1096,7 +1167,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
   while (issued < min(i1, i0 + ST - 1)) issue();
   // head and query tile of the iteration that is computed, and its bias
   int hc = hk * grp + (nt > 0 ? i0 / nt : 0), tc = nt > 0 ? i0 % nt : 0, hb = 0;
-  if (BIAS && i0 < i1) load_bias(a, hc, sbias);
+  if (BIAS && i0 < i1) load_bias<64 * NW>(a, hc, sbias);
   typename O::Rows kf, vf;
   const long row = kv ? key : 0;
   O::load_rows(kf, static_cast<const E*>(a.k.p) + b * a.k.b + row * a.k.t + hk * a.k.h, kv, half, a.dh);
@@ -1118,7 +1189,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
       ++hc;
       hb ^= 1;
       // goes where the last head's was: read for the last time before this barrier
-      if (BIAS && i + 1 < i1) load_bias(a, hc, sbias + hb * W);
+      if (BIAS && i + 1 < i1) load_bias<64 * NW>(a, hc, sbias + hb * W);
     }
     const E* sQ = sm + stage * 2 * TILE;
     const E* sO = sQ + TILE;
@@ -1130,30 +1201,8 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dkdv(Masked
       if (kind == 0) continue;  // wave-uniform
       ops.fresh();
       f32x16 st, dp;
-      ops.scores(st, sQ, qb, kf);
-      ops.scores(dp, sO, qb, vf);
-      if (BIAS) {
-        const int plo = sq.off + q0;
-        add_bias<-1>(st, sl2, bias, a.R, key - plo, k0 - plo - 31, k0 + 31 - plo, half);
-      }
-      if (kind == 1) {
-  #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          st[r] = (unsigned)(q0 + perm_pos(r, half) - seen.lo) <= seen.n1 ? st[r] : -INFINITY;
-        }
-      }
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {  // queries q0 + 8g + 4*half + 0..3
-        const float4* ld = reinterpret_cast<const float4*>(sS[stage] + qb * 32 + 8 * g + 4 * half);
-        const float4 x = ld[0], y = ld[1];
-        const float lv[4] = {x.x, x.z, y.x, y.z}, sv[4] = {x.y, x.w, y.y, y.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = 4 * g + e;
-          st[r] = __builtin_amdgcn_exp2f(BIAS ? st[r] - lv[e] : fmaf(st[r], sl2, -lv[e]));
-          dp[r] = st[r] * (dp[r] - sv[e]);  // dS
-        }
-      }
+      p_and_ds<O, BIAS>(ops, st, dp, sQ, sO, qb, kf, vf, sl2, bias, a.R, q0, sq.off, key, k0, kind == 2, seen,
+                        sS[stage] + qb * 32, half);
       ops.accum(dv, sO, qb, st);
       ops.accum(dk, sQ, qb, dp);
     }
@@ -1261,6 +1310,133 @@ __global__ __launch_bounds__(256) void attn_masked_dkdv_join(MaskedAttnArgs a, K
           if (dim + e < a.dh) St<E>::st(dst, dim + e, x[i][e]);
       }
     }
+  }
+}
+
+// Both passes of a (batch, head) whose queries and keys fit one workgroup's LDS, without shared
+// heads: bound by latency, so Q, dO, K and V are brought once, all at a time, and the dK/dV pass
+// finds them, the statistics and the bias where the dQ pass left them.  384 of 128 x 128, head
+// dim 64, with the table's gradient: 25.1 us, 36.4 as two kernels.
+template <class O, bool BIAS, bool DTAB, int ROWS>
+__global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 : 1) void attn_masked_bwd_small(MaskedAttnArgs a) {
+  typedef typename O::E E;
+  constexpr int DH = O::DH, KR = O::KR, TILE = O::TILE, NW = 4, NT = ROWS / KR;
+  __shared__ __attribute__((aligned(1024))) E sm[4 * NT * TILE];  // Q, dO, K, V
+  __shared__ __attribute__((aligned(16))) float2 sS[ROWS];        // (lse, D)
+  extern __shared__ float sbias[];                                // bias, then (DTAB) one diagonal array per wave
+  static_assert(4 * NT * TILE >= NW * O::STAGE, "the rows fit the tiles' space on their way out");
+  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int bh = xcd_block(blockIdx.x, gridDim.x), b = bh / a.H, h = bh % a.H;
+  const Seq sq = seq_of(a, b);
+  const Mask mask(a, sq.lk);
+  const float sl2 = kLog2e * a.scale;
+  const int W = 2 * a.R + 1;
+  O ops(lane, a.dh);
+  auto bring = [&](const View& v, int rows, E* dst) {
+    const E* src = static_cast<const E*>(v.p) + b * v.b + h * v.h;
+    const uint32_t first = O::template dma_first<NW>(v.t, a.dh, lane, wave);
+    for (int r0 = 0; r0 < rows; r0 += KR)
+      O::template dma<NW>(src + (long)r0 * v.t, v.t, rows - 1 - r0, dst + r0 / KR * TILE, a.dh, lane, wave, first);
+  };
+  E *sQ = sm, *sO = sm + NT * TILE, *sK = sm + 2 * NT * TILE, *sV = sm + 3 * NT * TILE;
+  bring(a.k, sq.lk, sK);
+  bring(a.q, sq.lq, sQ);
+  bring(a.v, sq.lk, sV);
+  bring(a.dout, sq.lq, sO);
+  const int q0 = wave * 32, q = q0 + l32, p = sq.off + q;
+  const bool qv = q < sq.lq;
+  const long row = qv ? q : 0;
+  typename O::Rows of;
+  if (!DTAB)
+    O::load_rows(of, static_cast<const E*>(a.o.p) + b * a.o.b + row * a.o.t + h * a.o.h, qv, half, a.dh);
+  float lse = qv ? lse_or_inf(a.lse[(long)bh * a.Sq + row]) : INFINITY;
+  float* diag = sbias + (1 + wave) * W;
+  if (BIAS) load_bias<64 * NW>(a, h, sbias);
+  if (DTAB)
+    for (int i = 0; i < W; i += 64) diag[min(i + lane, W - 1)] = 0.f;  // all lanes, as in load_bias
+  tiles_ready();
+
+  // queries q0 .. q0 + 31 against every key
+  f32x16 dq[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dq[i][r] = 0.f;
+  float dsum = 0.f, dlo = 0.f, dhi = 0.f;
+  if (q0 < sq.lq) {
+    const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
+    const Span span = key_span(mask, plo, phi);
+    const Visible seen = keys_of(mask, p);
+    typename O::Rows qf, df;
+    ops.tile_rows(qf, sQ + q0 / KR * TILE, q0 / 32 % (KR / 32), a.dh);
+    ops.tile_rows(df, sO + q0 / KR * TILE, q0 / 32 % (KR / 32), a.dh);
+    if (!DTAB) dsum = O::dot(of, df);
+#pragma unroll 1
+    for (int sweep = DTAB ? 0 : 1; sweep < 2; ++sweep) {
+#pragma unroll 1
+      for (int k0 = 0; k0 < sq.lk; k0 += 32) {
+        const int kind = span.kind(k0 / 32), kb = k0 / 32 % (KR / 32), t = k0 / KR * TILE;
+        if (kind == 0) continue;
+        f32x16 st, dp;
+        p_and_dp<O, BIAS>(ops, st, dp, sK + t, sV + t, kb, qf, df, sl2, sbias, a.R, k0, p, plo, phi, kind == 2, seen, lse,
+                          half);
+        if (sweep == 0) {  // D from P and dP, as in the dQ pass
+#pragma unroll
+          for (int r = 0; r < 16; ++r) dsum = fmaf(st[r], dp[r], dsum);
+          continue;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st[r] *= dp[r] - dsum;  // dS
+        if (DTAB) add_diag(st, k0 - sq.off - q0, a.R, diag, dlo, dhi, lane);
+        ops.accum(dq, sK + t, kb, st);
+      }
+      if (sweep == 0) dsum += __shfl_xor(dsum, 32, 64);
+    }
+  }
+  if (q < ROWS && half == 0) sS[q] = make_float2(lse, dsum);
+  if (DTAB) close_diag(diag, W, dlo, dhi, lane);
+  __syncthreads();
+  if (DTAB) put_diag<NW>(sbias, W, a.diag + (long)bh * W);
+
+  // keys k0 .. k0 + 31 against every query
+  const int k0 = wave * 32, key = k0 + l32;
+  f32x16 dk[DH / 32], dv[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dk[i][r] = dv[i][r] = 0.f;
+  if (k0 < sq.lk) {
+    const Span span = query_span(mask, k0, sq.off, sq.lq);
+    const Visible seen = rows_of(mask, key, sq.off, sq.lq);
+    typename O::Rows kf, vf;
+    ops.tile_rows(kf, sK + k0 / KR * TILE, k0 / 32 % (KR / 32), a.dh);
+    ops.tile_rows(vf, sV + k0 / KR * TILE, k0 / 32 % (KR / 32), a.dh);
+#pragma unroll 1
+    for (int r0 = 0; r0 < sq.lq; r0 += 32) {
+      const int kind = span.kind(r0 / 32), qb = r0 / 32 % (KR / 32), t = r0 / KR * TILE;
+      if (kind == 0) continue;
+      f32x16 st, dp;
+      p_and_ds<O, BIAS>(ops, st, dp, sQ + t, sO + t, qb, kf, vf, sl2, sbias, a.R, r0, sq.off, key, k0, kind == 2, seen,
+                        sS + r0, half);
+      ops.accum(dv, sO + t, qb, st);
+      ops.accum(dk, sQ + t, qb, dp);
+    }
+  }
+  __syncthreads();  // the tiles' space now takes the rows on their way out
+  E* stage = sm + wave * O::STAGE;
+  const bool nt = stream_out((long)a.B * max(a.Sq, a.Sk) * a.H * DH * (long)sizeof(E));
+  if (q0 < a.Sq) {
+    O::rotate_back(dq, a.rope_tab, min(q, a.Sq - 1), half);
+    O::store(dq, a.scale, lane, stage, static_cast<E*>(a.dq.p) + b * a.dq.b + (long)q0 * a.dq.t + h * a.dq.h, a.dq.t, nt,
+             a.Sq - q0, a.dh);
+  }
+  if (k0 < a.Sk) {
+    O::rotate_back(dk, a.rope_tab, min(key, a.Sk - 1), half);
+    O::store(dk, a.scale, lane, stage, static_cast<E*>(a.dk.p) + b * a.dk.b + (long)k0 * a.dk.t + h * a.dk.h, a.dk.t, nt,
+             a.Sk - k0, a.dh);
+    O::store(dv, 1.f, lane, stage, static_cast<E*>(a.dv.p) + b * a.dv.b + (long)k0 * a.dv.t + h * a.dv.h, a.dv.t, nt,
+             a.Sk - k0, a.dh);
   }
 }
 
@@ -1392,8 +1568,26 @@ static hipError_t fwd_ops(const MaskedAttnArgs& a, hipStream_t s) {
   else RG_LAUNCH((attn_masked_fwd<O, false, MA_NW>), grid, block, 0, s, a);
   return hipGetLastError();
 }
-template <class O>
+// ROWS: queries, and keys, that the LDS of attn_masked_bwd_small holds
+template <class O, int ROWS>
+static bool fits_small(const MaskedAttnArgs& a) {
+  const size_t lds = sizeof(typename O::E) * 4 * (ROWS / O::KR) * O::TILE + ROWS * 8 +
+                     (a.table ? (size_t)(2 * a.R + 1) * 4 * (a.dtable ? 5 : 1) : 0);
+  return a.H == a.Hkv && a.Sq <= ROWS && a.Sk <= ROWS && lds <= 160 * 1024;
+}
+template <class O, int ROWS>
 static hipError_t bwd_ops(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
+  if (fits_small<O, ROWS>(a)) {
+    const dim3 grid((unsigned)(a.B * a.H)), block(256);
+    const int W4 = (2 * a.R + 1) * 4;
+    if (!a.table) RG_LAUNCH((attn_masked_bwd_small<O, false, false, ROWS>), grid, block, 0, s, a);
+    else if (!a.dtable) RG_LAUNCH((attn_masked_bwd_small<O, true, false, ROWS>), grid, block, W4, s, a);
+    else {
+      RG_LAUNCH((attn_masked_bwd_small<O, true, true, ROWS>), grid, block, 5 * W4, s, a);
+      RG_LAUNCH(attn_bias_grad, dim3(a.H), dim3(1024), 0, s, a, a.B);
+    }
+    return hipGetLastError();
+  }
   const KeyWork w = key_work(dtype, a);
   const dim3 gq((unsigned)(blocks_of(a.Sq) * a.B * a.H)), gk((unsigned)(w.items() * a.B * a.Hkv)), block(64 * MA_NW);
   const int W = 2 * a.R + 1;
@@ -1424,8 +1618,8 @@ hipError_t launch_masked_attn_fwd(int dtype, const MaskedAttnArgs& a, hipStream_
   return a.dh <= 64 ? fwd_ops<OpsF32<64>>(a, s) : fwd_ops<OpsF32<128>>(a, s);
 }
 hipError_t launch_masked_attn_bwd(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
-  if (dtype == DT_BF16) return a.dh == 64 ? bwd_ops<OpsBf16<64>>(dtype, a, s) : bwd_ops<OpsBf16<128>>(dtype, a, s);
-  return a.dh <= 64 ? bwd_ops<OpsF32<64>>(dtype, a, s) : bwd_ops<OpsF32<128>>(dtype, a, s);
+  if (dtype == DT_BF16) return a.dh == 64 ? bwd_ops<OpsBf16<64>, 128>(dtype, a, s) : bwd_ops<OpsBf16<128>, 128>(dtype, a, s);
+  return a.dh <= 64 ? bwd_ops<OpsF32<64>, 128>(dtype, a, s) : bwd_ops<OpsF32<128>, 64>(dtype, a, s);
 }
 
 }  // namespace rg

@@ -58,6 +58,15 @@ CASES = [
     A("f32", 2, 3, 1, 128, 161, causal=True, nb=32, dist=64, len_q=[161, 30], len_k=[161, 30]),
     A("f32", 1, 2, 2, 96, 300, causal=False),
     A("f32", 2, 2, 1, 17, 40, 90, causal=True, window=30, sinks=2, len_q=[40, 0], len_k=[90, 8]),
+    # queries and keys that fit one workgroup, with and without the bias, and one whose bias does not
+    A("bf16", 2, 2, 2, 128, 100, causal=True, window=30, sinks=2, nb=16, dist=40, len_q=[100, 37], len_k=[100, 37]),
+    A("bf16", 2, 3, 3, 128, 128, 17, causal=False, len_q=[128, 0], len_k=[17, 17]),
+    A("bf16", 1, 2, 2, 64, 33, 128, causal=True, nb=32, dist=1000),
+    A("bf16", 1, 2, 2, 128, 60, nb=32, dist=1000),
+    A("f32", 2, 3, 3, 96, 64, causal=True, nb=8, dist=20, len_q=[64, 5], len_k=[64, 0]),
+    A("f32", 1, 2, 2, 128, 50, 33, causal=False, window=12, sinks=1),
+    A("f32", 1, 2, 2, 33, 128, 100, causal=True, window=50, nb=16, dist=64),
+    A("f32", 1, 2, 2, 128, 65, causal=True, nb=16, dist=30),
 ]
 IDS = ["-".join(f"{k}{v}".replace(" ", "") for k, v in c.items() if v not in (0, None, False)) for c in CASES]
 
