@@ -1316,7 +1316,7 @@ __global__ __launch_bounds__(256) void attn_masked_dkdv_join(MaskedAttnArgs a, K
 // Both passes of a (batch, head) whose queries and keys fit one workgroup's LDS, without shared
 // heads: bound by latency, so Q, dO, K and V are brought once, all at a time, and the dK/dV pass
 // finds them, the statistics and the bias where the dQ pass left them.  384 of 128 x 128, head
-// dim 64, with the table's gradient: 25.1 us, 36.4 as two kernels.
+// dim 64, with the table's gradient: 22.6 us, 36.4 as two kernels.
 template <class O, bool BIAS, bool DTAB, int ROWS>
 __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 : 1) void attn_masked_bwd_small(MaskedAttnArgs a) {
   typedef typename O::E E;
@@ -1372,26 +1372,38 @@ __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 
     ops.tile_rows(qf, sQ + q0 / KR * TILE, q0 / 32 % (KR / 32), a.dh);
     ops.tile_rows(df, sO + q0 / KR * TILE, q0 / 32 % (KR / 32), a.dh);
     if (!DTAB) dsum = O::dot(of, df);
-#pragma unroll 1
-    for (int sweep = DTAB ? 0 : 1; sweep < 2; ++sweep) {
+    auto block = [&](int k0, int kind, f32x16& st, f32x16& dp) {
+      p_and_dp<O, BIAS>(ops, st, dp, sK + k0 / KR * TILE, sV + k0 / KR * TILE, k0 / 32 % (KR / 32), qf, df, sl2, sbias, a.R,
+                        k0, p, plo, phi, kind == 2, seen, lse, half);
+    };
+    auto add = [&](int k0, f32x16& st, const f32x16& dp) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[r] *= dp[r] - dsum;  // dS
+      if (DTAB) add_diag(st, k0 - sq.off - q0, a.R, diag, dlo, dhi, lane);
+      ops.accum(dq, sK + k0 / KR * TILE, k0 / 32 % (KR / 32), st);
+    };
+    if constexpr (DTAB) {  // D from P and dP, as in the dQ pass, which stay in registers here
+      f32x16 st[ROWS / 32], dp[ROWS / 32];
+#pragma unroll
+      for (int i = 0; i < ROWS / 32; ++i) {
+        if (span.kind(i) == 0) continue;
+        block(i * 32, span.kind(i), st[i], dp[i]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dsum = fmaf(st[i][r], dp[i][r], dsum);
+      }
+      dsum += __shfl_xor(dsum, 32, 64);
+#pragma unroll
+      for (int i = 0; i < ROWS / 32; ++i)
+        if (span.kind(i) != 0) add(i * 32, st[i], dp[i]);
+    } else {
 #pragma unroll 1
       for (int k0 = 0; k0 < sq.lk; k0 += 32) {
-        const int kind = span.kind(k0 / 32), kb = k0 / 32 % (KR / 32), t = k0 / KR * TILE;
+        const int kind = span.kind(k0 / 32);
         if (kind == 0) continue;
         f32x16 st, dp;
-        p_and_dp<O, BIAS>(ops, st, dp, sK + t, sV + t, kb, qf, df, sl2, sbias, a.R, k0, p, plo, phi, kind == 2, seen, lse,
-                          half);
-        if (sweep == 0) {  // D from P and dP, as in the dQ pass
-#pragma unroll
-          for (int r = 0; r < 16; ++r) dsum = fmaf(st[r], dp[r], dsum);
-          continue;
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) st[r] *= dp[r] - dsum;  // dS
-        if (DTAB) add_diag(st, k0 - sq.off - q0, a.R, diag, dlo, dhi, lane);
-        ops.accum(dq, sK + t, kb, st);
+        block(k0, kind, st, dp);
+        add(k0, st, dp);
       }
-      if (sweep == 0) dsum += __shfl_xor(dsum, 32, 64);
     }
   }
   if (q < ROWS && half == 0) sS[q] = make_float2(lse, dsum);
@@ -1522,13 +1534,14 @@ static bool few(const MaskedAttnArgs& a) {
   const long rows = (long)a.Sq * (a.H / a.Hkv);
   return rows <= 32 || (rows <= 128 && (long)a.B * a.H * blocks_of(a.Sq) < 256 && a.Sk >= 512);
 }
-// One workgroup per CU and as many as there are tiles for its waves, with two tiles each.
+// One workgroup per CU, and no more than there are tiles for its four waves.  64 heads, window
+// 1024: 13.9 us with both kernels; with two tiles for each wave 14.8.
 static FewWork few_work(const MaskedAttnArgs& a) {
   FewWork w;
   w.rb = (a.Sq * (a.H / a.Hkv) + 31) / 32;
   const long span = a.window ? std::min<long>(a.Sk, (long)a.Sq + (a.causal ? 1 : 2) * (long)a.window + a.sinks) : a.Sk;
   const long wgs = (long)a.B * a.Hkv * w.rb;
-  w.split = (int)std::max(1l, std::min({64l, (256 + wgs - 1) / wgs, span / 256}));
+  w.split = (int)std::max(1l, std::min({64l, (256 + wgs - 1) / wgs, span / 128}));
   return w;
 }
 
