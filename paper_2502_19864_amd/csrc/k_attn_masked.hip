@@ -1523,7 +1523,11 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
   // dealt out in eighths of that, so that they fill the gaps: 512 near workgroups of 80
   // iterations are one round of the GPU, and far ones as long would begin another.  With the
   // join, 8192 tokens and window 1024: halves 430 us, quarters 383, eighths 365.
-  w.c_far = (int)(w.s_near == 1 && far <= 2 * near ? far : std::max({(long)(w.c_near + 7) / 8, 4l, (far + 63) / 64}));
+  // Not into more than 2048 workgroups, as their partial sums take 64 or 128 KB each.
+  const long nfar = (long)w.nfar * a.B * a.Hkv;
+  w.c_far = (int)(w.s_near == 1 && far <= 2 * near
+                      ? far
+                      : std::min(far, std::max({(long)(w.c_near + 7) / 8, 4l, (far + 63) / 64, (far * nfar + 2047) / 2048})));
   w.s_far = (int)((far + w.c_far - 1) / w.c_far);
   if (w.s_far < w.s_near || (long)w.items() * a.B * a.Hkv >= (1l << 31)) {
     w.s_far = w.s_near = 1;
@@ -1544,21 +1548,25 @@ static BwdSpace bwd_space(int dtype, const MaskedAttnArgs& a, bool dtable) {
   return s;
 }
 
-// A few queries against many keys: the rows of a key-value head fill one block, or at most
-// four where the other kernel's grid would leave CUs idle over a long loop.  32 x 12 heads of 128
-// x 128: 27.6 us here, 11.6 there.
+// keys that a query block may see, at most about
+static long key_reach(const MaskedAttnArgs& a) {
+  return a.window ? std::min<long>(a.Sk, (long)a.Sq + (a.causal ? 1 : 2) * (long)a.window + a.sinks) : a.Sk;
+}
+// A few queries against many keys: the rows of a key-value head fill one block, or the other
+// kernel would leave more than half of the SIMDs without a wave over a long loop.  32 heads on 8 of 128,
+// 256 queries (256 waves there) on 1024 and 8192 keys: 17.0 and 85 us here, 26.6 and 169 there; 512 queries
+// on 1024 keys: 29.2 and 27.0.
 static bool few(const MaskedAttnArgs& a) {
   const long rows = (long)a.Sq * (a.H / a.Hkv);
-  return rows <= 32 || (rows <= 128 && (long)a.B * a.H * blocks_of(a.Sq) < 256 && a.Sk >= 512);
+  return rows <= 32 || ((long)a.B * a.H * ((a.Sq + 31) / 32) < 512 && key_reach(a) >= 512);
 }
 // One workgroup per CU, and no more than there are tiles for its four waves.  64 heads, window
 // 1024: 13.9 us with both kernels; with two tiles for each wave 14.8.
 static FewWork few_work(const MaskedAttnArgs& a) {
   FewWork w;
   w.rb = (a.Sq * (a.H / a.Hkv) + 31) / 32;
-  const long span = a.window ? std::min<long>(a.Sk, (long)a.Sq + (a.causal ? 1 : 2) * (long)a.window + a.sinks) : a.Sk;
   const long wgs = (long)a.B * a.Hkv * w.rb;
-  w.split = (int)std::max(1l, std::min({64l, (256 + wgs - 1) / wgs, span / 128}));
+  w.split = (int)std::max(1l, std::min({64l, (256 + wgs - 1) / wgs, key_reach(a) / 128}));
   return w;
 }
 

@@ -67,6 +67,16 @@ CASES = [
     A("f32", 1, 2, 2, 128, 50, 33, causal=False, window=12, sinks=1),
     A("f32", 1, 2, 2, 33, 128, 100, causal=True, window=50, nb=16, dist=64),
     A("f32", 1, 2, 2, 128, 65, causal=True, nb=16, dist=30),
+    # fp32: a few queries with the bias at the larger head dim, key blocks split at the smaller one
+    A("f32", 1, 4, 1, 100, 2, 600, causal=True, nb=16, dist=40),
+    A("f32", 1, 2, 1, 64, 700, causal=True, window=300, sinks=2),
+    # a chunk of a prompt against its cache: split over the keys, and with enough rows not to be
+    A("bf16", 1, 4, 2, 128, 200, 1300, causal=True, window=600, sinks=5),
+    A("bf16", 1, 3, 3, 64, 150, 900, causal=True, nb=32, dist=128, len_q=[131], len_k=[888]),
+    A("bf16", 2, 32, 8, 128, 300, 700, causal=True, window=600, sinks=2),
+    A("bf16", 2, 32, 8, 64, 300, 700, causal=True, nb=16, dist=30, len_q=[300, 211], len_k=[700, 640]),
+    A("f32", 2, 32, 4, 64, 270, 530, causal=True),
+    A("f32", 1, 2, 2, 64, 130, 640, causal=True, nb=16, dist=64),
 ]
 IDS = ["-".join(f"{k}{v}".replace(" ", "") for k, v in c.items() if v not in (0, None, False)) for c in CASES]
 
@@ -144,6 +154,40 @@ def test_attention_repeats_bit_for_bit_and_with_a_frozen_table(i):
         want = R.attention(t["q"], t["k"], t["v"], t["do"], lowp=c["dtype"] == "bf16", **t["how"])
         for n in got:
             R.check(n, got[n], *want[n])
+
+
+@pytest.mark.parametrize("dtype,dh,Sq", [("bf16", 64, 90), ("bf16", 128, 90), ("f32", 40, 90), ("f32", 100, 60),
+                                         ("f32", 40, 200), ("f32", 100, 200)])
+def test_a_frozen_table_leaves_its_gradient_out(dtype, dh, Sq):
+    c = A(dtype, 1, 2, 2, dh, Sq, causal=True, window=70, sinks=2, nb=16, dist=40)
+    t = make(c)
+    got = run(t, frozen_table=True)
+    want = R.attention(t["q"], t["k"], t["v"], t["do"], lowp=dtype == "bf16", **t["how"])
+    assert "dtable" not in got
+    for n in got:
+        R.check(n, got[n], *want[n])
+
+
+@pytest.mark.parametrize("Sq,nb", [(1, 0), (200, 0), (200, 16)])
+def test_offsets_past_32_bits(Sq, nb):
+    """A cache whose rows lie 2 MiB apart, 5 GiB from the first to the last, and its gradients in such rows."""
+    import torch
+
+    c = A("bf16", 1, 4, 2, 64, Sq, 2500, causal=True, window=900, sinks=3, nb=nb, dist=40 if nb else 0)
+    t = make(c)
+    buf = torch.empty(2500 << 20, dtype=torch.bfloat16, device="cuda")
+    rows = buf.view(1, 2500, 1 << 20)
+    wide = [rows[:, :, i * 128:(i + 1) * 128].unflatten(2, (2, 64)) for i in range(4)]
+    k, v, dk, dv = wide
+    k.copy_(t["k"])
+    v.copy_(t["v"])
+    want = R.attention(t["q"], t["k"], t["v"], t["do"], lowp=True, d_exact=bool(nb), **t["how"])
+    from paper_2502_19864_amd import operators as ops
+    o, lse = ops.attention_forward(t["q"], k, v, **t["how"])
+    dtable = torch.zeros_like(t["table"]) if nb else None
+    dq, _, _ = ops.attention_backward(t["do"], t["q"], k, v, o, lse, dk=dk, dv=dv, dtable=dtable, **t["how"])
+    for n, x in dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv, **({"dtable": dtable} if nb else {})).items():
+        R.check(n, x, *want[n])
 
 
 def test_hidden_buckets_and_rows_that_see_nothing():

@@ -46,6 +46,16 @@ def test_attention_plan():
     assert b3 == b and b2 >= b + 2 * 4 * 33 * 4
 
 
+@pytest.mark.parametrize("kw", [dict(batch=1, n_heads=32, n_kv_heads=8, window=16, sinks=1 << 20),
+                                dict(batch=500, window=16, sinks=4), dict(batch=500, window=1000, sinks=4),
+                                dict(batch=64, n_heads=16, n_kv_heads=1, window=0), dict(batch=1, window=0)])
+def test_split_backward_stays_within_its_workspace(kw):
+    """At most some 4096 workgroups of 128 KB of partial sums, beside 8 bytes a row."""
+    d = desc(d_head=128, seq_q=8192, seq_k=8192, **kw)
+    _, b = B.ringada_attn_plan(d, False)
+    assert b <= 8 * d.batch * d.n_heads * 8192 + (4096 << 17) + 512
+
+
 BASE = 1 << 20  # addresses that no call gets to
 
 
