@@ -1042,6 +1042,146 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
            stream_out((long)a.B * a.Sq * a.H * DH * (long)sizeof(E)), a.Sq - q0, a.dh);
 }
 
+// The same for calls whose 32-row blocks would hold fewer than half of the SIMDs: a workgroup takes one of
+// them, and its waves every fourth (second) block of its keys each, from tiles of their own as
+// in attn_few_fwd; D and dQ are joined in LDS.  4 heads on 2 of 128, 1824 tokens, with the
+// table's gradient: 69 us, 208 with one wave per block.
+template <class O, bool BIAS, bool DTAB, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void attn_few_dq(MaskedAttnArgs a) {
+  typedef typename O::E E;
+  constexpr int DH = O::DH, BLOCK = O::BLOCK;
+  __shared__ __attribute__((aligned(1024))) E sm[NW][4 * BLOCK];  // per wave: [buffer][K, V]; later its dQ
+  __shared__ float sD[NW][32];
+  extern __shared__ float sbias[];  // bias, then (DTAB) one diagonal array per wave
+  static_assert(4 * BLOCK * sizeof(E) >= 32 * DH * 4 && 4 * BLOCK >= O::STAGE, "a wave's dQ fits its tiles' space");
+  const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int nq = (a.Sq + 31) / 32, blk = xcd_block(blockIdx.x, gridDim.x), qb = blk % nq, bh = blk / nq;
+  const int b = bh / a.H, h = bh % a.H, hk = h / (a.H / a.Hkv);
+  const Seq sq = seq_of(a, b);
+  const Mask mask(a, sq.lk);
+  const int q0 = qb * 32, q = q0 + l32, p = sq.off + q;
+  const bool qv = q < sq.lq;
+  const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
+  const Span span = key_span(mask, plo, phi);
+  const Visible seen = keys_of(mask, p);
+  KeyTiles kt{0, 0, 0};
+  if (q0 < sq.lq) kt = key_tiles<32>(mask, plo, phi);
+  const float sl2 = kLog2e * a.scale;
+  const int W = 2 * a.R + 1;
+  const E* K = static_cast<const E*>(a.k.p) + b * a.k.b + hk * a.k.h;
+  const E* V = static_cast<const E*>(a.v.p) + b * a.v.b + hk * a.v.h;
+  O ops(lane, a.dh);
+  E* tiles = sm[wave];
+  auto issue = [&](int i, int buf) {
+    const int k0 = kt.at(i) * 32, last = sq.lk - 1 - k0;
+    E* dst = tiles + buf * 2 * BLOCK;
+    O::dma_block(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane);
+    O::dma_block(V + (long)k0 * a.v.t, a.v.t, last, dst + BLOCK, a.dh, lane);
+  };
+  if (wave < kt.n) issue(wave, 0);
+  const long row = qv ? q : 0;
+  typename O::Rows qf, df;
+  O::load_rows(qf, static_cast<const E*>(a.q.p) + b * a.q.b + row * a.q.t + h * a.q.h, qv, half, a.dh);
+  O::load_rows(df, static_cast<const E*>(a.dout.p) + b * a.dout.b + row * a.dout.t + h * a.dout.h, qv, half, a.dh);
+  float dsum = 0.f, dlo = 0.f, dhi = 0.f;
+  if (!DTAB) {
+    typename O::Rows of;
+    O::load_rows(of, static_cast<const E*>(a.o.p) + b * a.o.b + row * a.o.t + h * a.o.h, qv, half, a.dh);
+    dsum = O::dot(of, df);
+  }
+  float lse = qv ? lse_or_inf(a.lse[(long)bh * a.Sq + row]) : INFINITY;
+  float* diag = sbias + (1 + wave) * W;
+  if (BIAS) load_bias<64 * NW>(a, h, sbias);
+  if (DTAB)
+    for (int i = 0; i < W; i += 64) diag[min(i + lane, W - 1)] = 0.f;  // all lanes, as in load_bias
+  f32x16 dq[DH / 32];
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dq[i][r] = 0.f;
+  qf.settled();
+  df.settled();
+  settle(lse);
+  settle(dsum);
+  __syncthreads();  // the bias
+
+#pragma unroll 1
+  for (int sweep = DTAB ? 0 : 1; sweep < 2; ++sweep) {
+#pragma unroll 1
+    for (int i = wave, buf = 0; i < kt.n; i += NW, buf ^= 1) {
+      // as in attn_few_fwd
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if constexpr (2 * O::DMAS <= 32) {
+        if (i + NW < kt.n) {
+          issue(i + NW, buf ^ 1);
+          asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * O::DMAS) : "memory");
+        } else {
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+      } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (i + NW < kt.n) issue(i + NW, buf ^ 1);
+      }
+      const int k0 = kt.at(i) * 32, kind = span.kind(k0 / 32);
+      if (kind == 0) continue;  // wave-uniform
+      const E* sK = tiles + buf * 2 * BLOCK;
+      f32x16 st, dp;
+      p_and_dp<O, BIAS>(ops, st, dp, sK, sK + BLOCK, 0, qf, df, sl2, sbias, a.R, k0, p, plo, phi, kind == 2, seen, lse,
+                        half);
+      if (DTAB && sweep == 0) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dsum = fmaf(st[r], dp[r], dsum);
+        continue;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[r] *= dp[r] - dsum;  // dS
+      if (DTAB) add_diag(st, k0 - plo, a.R, diag, dlo, dhi, lane);
+      ops.accum(dq, sK, 0, st);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (DTAB && sweep == 0) {
+      if (wave < kt.n) issue(wave, 0);
+      dsum += __shfl_xor(dsum, 32, 64);
+      if (half == 0) sD[wave][l32] = dsum;
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      dsum = 0.f;
+#pragma unroll
+      for (int k = 0; k < NW; ++k) dsum += sD[k][l32];
+    }
+  }
+  if (wave == 0 && half == 0 && q < a.Sq) a.stat[(long)bh * a.Sq + q] = make_float2(lse, dsum);
+  if (DTAB) close_diag(diag, W, dlo, dhi, lane);
+  float4* so = reinterpret_cast<float4*>(tiles) + lane;
+  if (wave > 0) {
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        so[(d * 4 + g) * 64] = make_float4(dq[d][4 * g], dq[d][4 * g + 1], dq[d][4 * g + 2], dq[d][4 * g + 3]);
+  }
+  __syncthreads();
+  if (DTAB) put_diag<NW>(sbias, W, a.diag + ((long)(b * nq + qb) * a.H + h) * W);
+  if (wave > 0) return;
+#pragma unroll
+  for (int k = 1; k < NW; ++k)
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 x = reinterpret_cast<const float4*>(sm[k])[(d * 4 + g) * 64 + lane];
+        dq[d][4 * g] += x.x;
+        dq[d][4 * g + 1] += x.y;
+        dq[d][4 * g + 2] += x.z;
+        dq[d][4 * g + 3] += x.w;
+      }
+  O::rotate_back(dq, a.rope_tab, min(q, a.Sq - 1), half);
+  O::store(dq, a.scale, lane, sm[0], static_cast<E*>(a.dq.p) + b * a.dq.b + (long)q0 * a.dq.t + h * a.dq.h, a.dq.t, false,
+           a.Sq - q0, a.dh);
+}
+
 // Work of the dK/dV pass.  A block of 32 NW keys meets the query tiles that see it, for every
 // query head of its group: `iters` iterations at most.  Blocks that hold sinks (all of them
 // without a window) are seen by every later query, so they are dealt to several
@@ -1462,7 +1602,7 @@ __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 
 }
 
 // dtable[t][h] += the sums of dS over the relative positions of bucket t, from the dQ pass's
-// partial sums diag[row][head][W]: one workgroup per head; position by position over the rows (as
+// partial sums diag[row][head][W]: one workgroup per head; 256 positions at a time over the rows (as
 // many rows at a time as 1024 threads hold positions), then a wave per bucket.  In a
 // fixed order; in 64 bits, which costs nothing here.  Bound by the latency of its loads: eight
 // are in flight at a time, past the last row too (with weight 0), and the buckets beside them.
@@ -1470,7 +1610,7 @@ __global__ __launch_bounds__(1024) void attn_bias_grad(MaskedAttnArgs a, int row
   __shared__ double part[1024], sum[2 * ATTN_MAX_DISTANCE + 1];
   __shared__ int bucket[2 * ATTN_MAX_DISTANCE + 1];
   const int W = 2 * a.R + 1, h = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int span = min(1024, (W + 63) / 64 * 64), groups = 1024 / span, g = threadIdx.x / span, at = threadIdx.x % span;
+  const int span = min(256, (W + 63) / 64 * 64), groups = 1024 / span, g = threadIdx.x / span, at = threadIdx.x % span;
   for (int i0 = 0; i0 < W; i0 += span) {
     const int i = i0 + at;
     double s = 0.0;
@@ -1506,10 +1646,21 @@ constexpr int MA_NW = 4;
 
 static long blocks_of(int n) { return (n + 32 * MA_NW - 1) / (32 * MA_NW); }
 
+// keys that a query block may see, at most about
+static long key_reach(const MaskedAttnArgs& a) {
+  return a.window ? std::min<long>(a.Sk, (long)a.Sq + (a.causal ? 1 : 2) * (long)a.window + a.sinks) : a.Sk;
+}
+// 32-row blocks would hold fewer than half of the SIMDs, over a loop of some length
+static bool few_blocks(const MaskedAttnArgs& a, long reach) {
+  return (long)a.B * a.H * ((a.Sq + 31) / 32) < 512 && key_reach(a) >= reach;
+}
+
 static size_t al256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Workgroups of the dK/dV pass: two per CU hide each other's barriers, so blocks are split
-// until there are 512, but no finer than four iterations.
+// until there are 512, but no finer than four iterations (fp32, whose products take 8 times as
+// long: one.  2 x 2 heads of 96, 557 tokens, window 183: 44 us with the join, 82 with four; bf16, 4 heads on 2 of 128,
+// 1824 tokens: 50 us, 69 with two).
 static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
   const int KR = dtype == DT_BF16 ? 64 : 32, grp = a.H / a.Hkv, rows = 32 * MA_NW;
   KeyWork w;
@@ -1518,7 +1669,8 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
   const long far = (long)grp * ((a.Sq + KR - 1) / KR);
   const long span = (long)rows + (a.causal ? 1l : 2l) * a.window;
   const long near = a.window ? std::min(far, grp * (span / KR + 2)) : far;
-  const long wgs = (long)w.nk * a.B * a.Hkv, want = std::max(1l, std::min((512 + wgs - 1) / wgs, near / 4));
+  const long least = dtype == DT_BF16 ? 4 : 1;
+  const long wgs = (long)w.nk * a.B * a.Hkv, want = std::max(1l, std::min((512 + wgs - 1) / wgs, near / least));
   w.c_near = (int)((near + want - 1) / want);
   w.s_near = (int)((near + w.c_near - 1) / w.c_near);
   // A far block is left whole up to twice a near one's length (the join costs as much), else
@@ -1529,7 +1681,7 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
   const long nfar = (long)w.nfar * a.B * a.Hkv;
   w.c_far = (int)(w.s_near == 1 && far <= 2 * near
                       ? far
-                      : std::min(far, std::max({(long)(w.c_near + 7) / 8, 4l, (far + 63) / 64, (far * nfar + 2047) / 2048})));
+                      : std::min(far, std::max({(long)(w.c_near + 7) / 8, least, (far + 63) / 64, (far * nfar + 2047) / 2048})));
   w.s_far = (int)((far + w.c_far - 1) / w.c_far);
   if (w.s_far < w.s_near || (long)w.items() * a.B * a.Hkv >= (1l << 31)) {
     w.s_far = w.s_near = 1;
@@ -1538,29 +1690,27 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
   return w;
 }
 
+constexpr long FEW_DQ = 64;  // keys from which attn_few_dq has work for two waves
 struct BwdSpace {
   size_t diag, part, total;
 };
 static BwdSpace bwd_space(int dtype, const MaskedAttnArgs& a, bool dtable) {
   BwdSpace s;
   s.diag = al256((size_t)a.B * a.H * a.Sq * 8);
-  s.part = s.diag + (dtable ? al256((size_t)a.B * blocks_of(a.Sq) * a.H * (2 * a.R + 1) * 4) : 0);
+  s.part = s.diag + (dtable ? al256((size_t)a.B * (few_blocks(a, FEW_DQ) ? (a.Sq + 31) / 32 : blocks_of(a.Sq)) * a.H *
+                                     (2 * a.R + 1) * 4) : 0);
   const int dh = a.dh <= 64 ? 64 : 128;
   s.total = s.part + al256((size_t)a.B * a.Hkv * key_work(dtype, a).slots() * MA_NW * 2 * 32 * dh * 4);
   return s;
 }
 
-// keys that a query block may see, at most about
-static long key_reach(const MaskedAttnArgs& a) {
-  return a.window ? std::min<long>(a.Sk, (long)a.Sq + (a.causal ? 1 : 2) * (long)a.window + a.sinks) : a.Sk;
-}
 // A few queries against many keys: the rows of a key-value head fill one block, or the other
 // kernel would leave more than half of the SIMDs without a wave over a long loop.  32 heads on 8 of 128,
 // 256 queries (256 waves there) on 1024 and 8192 keys: 17.0 and 85 us here, 26.6 and 169 there; 512 queries
 // on 1024 keys: 29.2 and 27.0.
 static bool few(const MaskedAttnArgs& a) {
   const long rows = (long)a.Sq * (a.H / a.Hkv);
-  return rows <= 32 || ((long)a.B * a.H * ((a.Sq + 31) / 32) < 512 && key_reach(a) >= 512);
+  return rows <= 32 || few_blocks(a, 512);
 }
 // One workgroup per CU, and no more than there are tiles for its four waves.  64 heads, window
 // 1024: 13.9 us with both kernels; with two tiles for each wave 14.8.
@@ -1615,7 +1765,22 @@ static bool fits_small(const MaskedAttnArgs& a) {
                      (a.table ? (size_t)(2 * a.R + 1) * 4 * (a.dtable ? 5 : 1) : 0);
   return a.H == a.Hkv && a.Sq <= ROWS && a.Sk <= ROWS && lds <= 160 * 1024;
 }
-template <class O, int ROWS>
+template <class O, int NW>
+static bool launch_few_dq(const MaskedAttnArgs& a, hipStream_t s) {
+  const int W4 = (2 * a.R + 1) * 4;
+  const size_t lds = sizeof(typename O::E) * NW * 4 * O::BLOCK + NW * 128 + (a.table ? (size_t)W4 * (a.dtable ? 1 + NW : 1) : 0);
+  const long wgs = (long)a.B * a.H * ((a.Sq + 31) / 32);
+  // one and a half rounds of the CUs at most: 348 workgroups of one per CU (fp32, 29 x 2 heads of 191, with the
+  // table's gradient) take 41 us, 54 in the other kernel; 448 (bf16, 4 x 8 heads of 430) 25.7 and 20.2
+  if (!few_blocks(a, FEW_DQ) || lds > 160 * 1024 || wgs > 384 * (long)(160 * 1024 / lds)) return false;
+  const dim3 grid((unsigned)wgs), block(64 * NW);
+  if (!a.table) RG_LAUNCH((attn_few_dq<O, false, false, NW>), grid, block, 0, s, a);
+  else if (!a.dtable) RG_LAUNCH((attn_few_dq<O, true, false, NW>), grid, block, W4, s, a);
+  else RG_LAUNCH((attn_few_dq<O, true, true, NW>), grid, block, (1 + NW) * W4, s, a);
+  return true;
+}
+// FNW: as few_ops' NW
+template <class O, int ROWS, int FNW>
 static hipError_t bwd_ops(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
   if (fits_small<O, ROWS>(a)) {
     const dim3 grid((unsigned)(a.B * a.H)), block(256);
@@ -1631,17 +1796,16 @@ static hipError_t bwd_ops(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
   const KeyWork w = key_work(dtype, a);
   const dim3 gq((unsigned)(blocks_of(a.Sq) * a.B * a.H)), gk((unsigned)(w.items() * a.B * a.Hkv)), block(64 * MA_NW);
   const int W = 2 * a.R + 1;
-  if (a.table) {
-    if (a.dtable) RG_LAUNCH((attn_masked_bwd_dq<O, true, true, MA_NW>), gq, block, (1 + MA_NW) * W * 4, s, a);
-    else RG_LAUNCH((attn_masked_bwd_dq<O, true, false, MA_NW>), gq, block, W * 4, s, a);
-    RG_LAUNCH((attn_masked_bwd_dkdv<O, true, MA_NW>), gk, block, 2 * W * 4, s, a, w);
-    if (a.dtable) {
-      RG_LAUNCH(attn_bias_grad, dim3(a.H), dim3(1024), 0, s, a, (int)(a.B * blocks_of(a.Sq)));
-    }
-  } else {
-    RG_LAUNCH((attn_masked_bwd_dq<O, false, false, MA_NW>), gq, block, 0, s, a);
-    RG_LAUNCH((attn_masked_bwd_dkdv<O, false, MA_NW>), gk, block, 0, s, a, w);
+  const bool few_dq = launch_few_dq<O, FNW>(a, s);
+  if (!few_dq) {
+    if (!a.table) RG_LAUNCH((attn_masked_bwd_dq<O, false, false, MA_NW>), gq, block, 0, s, a);
+    else if (!a.dtable) RG_LAUNCH((attn_masked_bwd_dq<O, true, false, MA_NW>), gq, block, W * 4, s, a);
+    else RG_LAUNCH((attn_masked_bwd_dq<O, true, true, MA_NW>), gq, block, (1 + MA_NW) * W * 4, s, a);
   }
+  if (a.table) RG_LAUNCH((attn_masked_bwd_dkdv<O, true, MA_NW>), gk, block, 2 * W * 4, s, a, w);
+  else RG_LAUNCH((attn_masked_bwd_dkdv<O, false, MA_NW>), gk, block, 0, s, a, w);
+  if (a.dtable)
+    RG_LAUNCH(attn_bias_grad, dim3(a.H), dim3(1024), 0, s, a, (int)(a.B * (few_dq ? (a.Sq + 31) / 32 : blocks_of(a.Sq))));
   const int split = w.s_near > 1 ? w.nk : w.s_far > 1 ? w.nfar : 0;
   if (split)
     RG_LAUNCH((attn_masked_dkdv_join<O, MA_NW>), dim3((unsigned)(a.B * a.Hkv * split * MA_NW), 2 * O::DH / 64),
@@ -1658,8 +1822,8 @@ hipError_t launch_masked_attn_fwd(int dtype, const MaskedAttnArgs& a, hipStream_
   return a.dh <= 64 ? fwd_ops<OpsF32<64>>(a, s) : fwd_ops<OpsF32<128>>(a, s);
 }
 hipError_t launch_masked_attn_bwd(int dtype, const MaskedAttnArgs& a, hipStream_t s) {
-  if (dtype == DT_BF16) return a.dh == 64 ? bwd_ops<OpsBf16<64>, 128>(dtype, a, s) : bwd_ops<OpsBf16<128>, 128>(dtype, a, s);
-  return a.dh <= 64 ? bwd_ops<OpsF32<64>, 128>(dtype, a, s) : bwd_ops<OpsF32<128>, 64>(dtype, a, s);
+  if (dtype == DT_BF16) return a.dh == 64 ? bwd_ops<OpsBf16<64>, 128, 4>(dtype, a, s) : bwd_ops<OpsBf16<128>, 128, 4>(dtype, a, s);
+  return a.dh <= 64 ? bwd_ops<OpsF32<64>, 128, 4>(dtype, a, s) : bwd_ops<OpsF32<128>, 64, 2>(dtype, a, s);
 }
 
 }  // namespace rg
