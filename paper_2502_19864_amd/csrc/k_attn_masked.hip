@@ -538,6 +538,11 @@ __device__ __forceinline__ void move_max(float& mrun, float& lrun, f32x16 (&oacc
   }
 }
 
+// One workgroup per 128 queries of a head, 32 per wave; the four share the key tiles.  Bound by
+// issue: at 32 heads on 8 of 128, 8192 causal tokens, window 1024, 200 us (0.43 of the matrix rate of
+// a large product): matrix unit 35 %, vector unit 40 % busy with two waves per SIMD, which meet in the
+// same phase about as often as not; exponentials take half as long as the products.  LDS is 20 % busy,
+// and more fragments read ahead change nothing.
 template <class O, bool BIAS, int NW>
 __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnArgs a) {
   typedef typename O::E E;
@@ -654,7 +659,8 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
 // tile, to waves that run on their own: tiles of 32 keys that only their wave reads, two deep
 // by DMA, no barrier.  The waves' (maximum, sum, O) are joined in LDS, the workgroups' by
 // attn_few_join.
-// Before (attn_masked_fwd, no split): 4 x 32 heads on 8, window 32768: 876 us; 32 heads, window 1024: 29 us.
+// Now: 4 x 32 heads on 8 of 128, window 32768: 86 us (5.3 TB/s) and 5 for the join; 32 heads, window
+// 1024: 10 and 4.  Before (attn_masked_fwd, no split): 876 and 29 us.
 struct FewWork {
   int split, rb;  // workgroups over the keys, blocks of 32 rows
 };
@@ -936,7 +942,9 @@ __device__ __forceinline__ void put_diag(const float* sbias, int W, float* out) 
 // dQ pass (lane = query); writes (lse, D).  DTAB: dtable is wanted, and D is formed from
 // P and dP themselves in a first sweep over the tiles: the sums over dS cancel, and a D
 // from the stored (rounded) O would leave an error of that rounding in them.  That sweep
-// is two of the pass's five products.
+// is two of the pass's five products.  Bound by issue, as the forward: 8192 tokens, window 1024
+// 255 us, matrix unit 39 %, vector unit 34 % busy; with the table's gradient (1777 tokens, 2 x 16 heads,
+// window 500) 109 us, 45 registers spilled at head dim 128.
 template <class O, bool BIAS, bool DTAB, int NW>
 __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAttnArgs a) {
   typedef typename O::E E;
@@ -1187,8 +1195,8 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_dq(MaskedAttnArgs a) {
 // without a window) are seen by every later query, so they are dealt to several
 // workgroups each, and so are the others when there are too few of them to fill the GPU;
 // such workgroups leave fp32 partial sums, which attn_masked_dkdv_join adds in order.
-// Before (one workgroup per block): 8192 causal tokens, 32 heads on 8, window 1024, 4 sinks
-// 3704 us.
+// 8192 causal tokens, 32 heads on 8, window 1024, 4 sinks: 353 us and 12 for the join; with one
+// workgroup per block 3704 us.
 struct KeyWork {
   int nk, nfar;       // key blocks, and how many of them (the first) are the sinks'
   int s_far, s_near;  // workgroups per block
@@ -1254,7 +1262,10 @@ __device__ __forceinline__ void key_item(int lin, int items, int nbh, int& item,
   bh = x * per + o % per;
 }
 
-// dK/dV pass (lane = key): the query heads of the key's group one after another.  bf16, head dim
+// dK/dV pass (lane = key): the query heads of the key's group one after another.  At head dim 128
+// dK, dV and the own rows of K and V take 192 of 256 registers, so a fragment from LDS is waited for
+// before the next is asked for: waves wait 57 % of the time, the matrix unit is 34 % busy.  With 512
+// registers and one wave per SIMD: 460 us where this takes 390.  bf16, head dim
 // 64, without a bias: held to 168 registers (169 otherwise), three waves fit a SIMD; 4 x 16 heads on 4
 // of 2048 tokens, both passes: 188 us, 209 with two.
 template <class O, bool BIAS, int NW>

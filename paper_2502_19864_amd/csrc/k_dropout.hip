@@ -7,6 +7,9 @@
 // counter and a 64-bit key into four words.  One evaluation serves the eight elements of a
 // chunk, 16 bits each (16 B of bf16), so p comes in steps of 2^-16 and the twenty
 // products are spread over eight elements; the factor is 1 / (1 - p) for that p.
+//
+// Bound by memory: one chunk per thread, 67 M bf16 elements with a residual 73 us (5.5 TB/s),
+// 3.1 M 5.5 us, which is the launch.
 #include "common.h"
 #include "kernels.h"
 

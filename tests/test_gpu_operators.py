@@ -77,6 +77,10 @@ CASES = [
     A("bf16", 2, 32, 8, 64, 300, 700, causal=True, nb=16, dist=30, len_q=[300, 211], len_k=[700, 640]),
     A("f32", 2, 32, 4, 64, 270, 530, causal=True),
     A("f32", 1, 2, 2, 64, 130, 640, causal=True, nb=16, dist=64),
+    # rows that fill the GPU: a wave per block of them
+    A("bf16", 2, 32, 8, 64, 300, causal=True, window=90, sinks=3),
+    A("f32", 2, 32, 16, 100, 270, causal=True),
+    A("f32", 2, 32, 16, 100, 270, causal=False, window=60, sinks=1, nb=16, dist=30),
 ]
 IDS = ["-".join(f"{k}{v}".replace(" ", "") for k, v in c.items() if v not in (0, None, False)) for c in CASES]
 
@@ -156,10 +160,12 @@ def test_attention_repeats_bit_for_bit_and_with_a_frozen_table(i):
             R.check(n, got[n], *want[n])
 
 
-@pytest.mark.parametrize("dtype,dh,Sq", [("bf16", 64, 90), ("bf16", 128, 90), ("f32", 40, 90), ("f32", 100, 60),
-                                         ("f32", 40, 200), ("f32", 100, 200)])
-def test_a_frozen_table_leaves_its_gradient_out(dtype, dh, Sq):
-    c = A(dtype, 1, 2, 2, dh, Sq, causal=True, window=70, sinks=2, nb=16, dist=40)
+@pytest.mark.parametrize("dtype,dh,H,Sq", [("bf16", 64, 2, 90), ("bf16", 128, 2, 90), ("f32", 40, 2, 90),
+                                           ("f32", 100, 2, 60), ("f32", 40, 2, 200), ("f32", 100, 2, 200),
+                                           ("bf16", 64, 64, 270), ("bf16", 128, 64, 270), ("f32", 40, 64, 270),
+                                           ("f32", 100, 64, 270)])
+def test_a_frozen_table_leaves_its_gradient_out(dtype, dh, H, Sq):
+    c = A(dtype, 1, H, H, dh, Sq, causal=True, window=70, sinks=2, nb=16, dist=40)
     t = make(c)
     got = run(t, frozen_table=True)
     want = R.attention(t["q"], t["k"], t["v"], t["do"], lowp=dtype == "bf16", **t["how"])
