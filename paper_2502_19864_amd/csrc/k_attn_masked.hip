@@ -198,6 +198,17 @@ __device__ __forceinline__ void settle(T& x) {
   asm volatile("" : "+v"(x));
 }
 
+// Products that a branch follows are waited for before it.  The compiler counts wait states from a matrix
+// instruction to the first use of its result along one of the ways only where both start at its block: behind the
+// two branches that choose a block's constant bias it left 7 of 11, and the scores read there changed from run
+// to run.  STATES: of the instruction's passes, and then some.
+template <int STATES>
+__device__ __forceinline__ void landed(f32x16& x) {
+  static_assert(STATES > 0 && STATES <= 32, "two s_nop");
+  if constexpr (STATES > 16) asm volatile("s_nop 15\n\ts_nop %1" : "+v"(x) : "n"(STATES - 17));
+  else asm volatile("s_nop %1" : "+v"(x) : "n"(STATES - 1));
+}
+
 // ================================================================ storage types
 // A tile is KR rows of one head in LDS.  dma() brings this wave's share (of NW) of rows 0 .. KR - 1
 // from src (rows past `last` read row `last`: what they score is masked); scores() forms the block
@@ -207,6 +218,7 @@ template <int DH_>
 struct OpsBf16 {
   static constexpr int BLOCK_DMAS(int rows) { return rows * DH_ / 512; }  // 1 KB each
   static constexpr int DH = DH_, KR = 64, ST = DH == 64 ? 3 : 2, TILE = KR * DH, STAGE = 32 * (DH + 8), WAVES = 2;
+  static constexpr int LANDS = 12;  // wait states of a product (8 passes)
   static constexpr int BLOCK = 32 * DH, DMAS = BLOCK_DMAS(32);  // elements of 32 rows, and their DMAs
   typedef bf16 E;
   struct Rows {
@@ -304,6 +316,7 @@ template <int DHM>
 struct OpsF32 {
   static constexpr int BLOCK_DMAS(int rows) { return rows * DHM / 64; }  // 64 floats each
   static constexpr int DH = DHM, KR = 32, ST = DHM == 64 ? 4 : 3, P = DHM + 4, TILE = KR * P, STAGE = 32 * P, WAVES = 1;
+  static constexpr int LANDS = 20;  // wait states of a product (16 passes)
   static constexpr int BLOCK = TILE, DMAS = BLOCK_DMAS(KR);
   typedef float E;
   struct Rows {
@@ -612,6 +625,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
 #pragma unroll
     for (int kb = 0; kb < KR / 32; ++kb) {
       ops.scores(sc[kb], sK, kb, qf);
+      if (BIAS || kb == KR / 32 - 1) landed<O::LANDS>(sc[kb]);
       if (BIAS)
         add_bias<1>(sc[kb], sl2, sbias, a.R, k0 + kb * 32 - p, k0 + kb * 32 - phi, k0 + kb * 32 + 31 - plo, half);
     }
@@ -743,6 +757,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
     const E* sK = tiles + buf * 2 * BLOCK;
     f32x16 sc;
     ops.scores(sc, sK, 0, qf);
+    landed<O::LANDS>(sc);
     if (BIAS) {
       if (k0 - phi >= a.R || k0 + 31 - plo <= -a.R) {
         const float c = k0 - phi >= a.R ? lb.hi : lb.lo;
@@ -879,6 +894,8 @@ __device__ __forceinline__ void p_and_dp(const O& ops, f32x16& st, f32x16& dp, c
                                          int plo, int phi, bool whole, const Visible& seen, float lse, int half) {
   ops.scores(st, sK, kb, qf);
   ops.scores(dp, sV, kb, df);
+  landed<O::LANDS>(st);
+  landed<O::LANDS>(dp);
   if (BIAS) add_bias<1>(st, sl2, bias, R, k0 - p, k0 - phi, k0 + 31 - plo, half);
   if (!whole) {  // a row past len_q has lse = +inf
 #pragma unroll
@@ -896,6 +913,8 @@ __device__ __forceinline__ void p_and_ds(const O& ops, f32x16& st, f32x16& dp, c
                                          int key, int k0, bool whole, const Visible& seen, const float2* stat, int half) {
   ops.scores(st, sQ, qb, kf);
   ops.scores(dp, sO, qb, vf);
+  landed<O::LANDS>(st);
+  landed<O::LANDS>(dp);
   if (BIAS) {
     const int plo = off + q0;
     add_bias<-1>(st, sl2, bias, R, key - plo, k0 - plo - 31, k0 + 31 - plo, half);
@@ -1661,9 +1680,9 @@ static long blocks_of(int n) { return (n + 32 * MA_NW - 1) / (32 * MA_NW); }
 static long key_reach(const MaskedAttnArgs& a) {
   return a.window ? std::min<long>(a.Sk, (long)a.Sq + (a.causal ? 1 : 2) * (long)a.window + a.sinks) : a.Sk;
 }
-// 32-row blocks would hold fewer than half of the SIMDs, over a loop of some length
-static bool few_blocks(const MaskedAttnArgs& a, long reach) {
-  return (long)a.B * a.H * ((a.Sq + 31) / 32) < 512 && key_reach(a) >= reach;
+// for attn_few_dq: 32-row blocks hold fewer than half of the SIMDs, and see keys for two waves
+static bool few_blocks(const MaskedAttnArgs& a) {
+  return (long)a.B * a.H * ((a.Sq + 31) / 32) < 512 && key_reach(a) >= 64;
 }
 
 static size_t al256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -1701,35 +1720,37 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
   return w;
 }
 
-constexpr long FEW_DQ = 64;  // keys from which attn_few_dq has work for two waves
 struct BwdSpace {
   size_t diag, part, total;
 };
 static BwdSpace bwd_space(int dtype, const MaskedAttnArgs& a, bool dtable) {
   BwdSpace s;
   s.diag = al256((size_t)a.B * a.H * a.Sq * 8);
-  s.part = s.diag + (dtable ? al256((size_t)a.B * (few_blocks(a, FEW_DQ) ? (a.Sq + 31) / 32 : blocks_of(a.Sq)) * a.H *
+  s.part = s.diag + (dtable ? al256((size_t)a.B * (few_blocks(a) ? (a.Sq + 31) / 32 : blocks_of(a.Sq)) * a.H *
                                      (2 * a.R + 1) * 4) : 0);
   const int dh = a.dh <= 64 ? 64 : 128;
   s.total = s.part + al256((size_t)a.B * a.Hkv * key_work(dtype, a).slots() * MA_NW * 2 * 32 * dh * 4);
   return s;
 }
 
-// A few queries against many keys: the rows of a key-value head fill one block, or the other
-// kernel would leave more than half of the SIMDs without a wave over a long loop.  32 heads on 8 of 128,
-// 256 queries (256 waves there) on 1024 and 8192 keys: 17.0 and 85 us here, 26.6 and 169 there; 512 queries
-// on 1024 keys: 29.2 and 27.0.
+// A few queries against many keys: the rows of a key-value head fill one block, or the blocks
+// are one round of workgroups (two per CU at head dims up to 64; fp32 ones gain there in two rounds
+// as well), over a loop that gives each wave some of it.  16 heads on 4 of 128, 256 queries on 1024 and 8192
+// keys: 16.4 and 51 us here, 26.5 and 170 in attn_masked_fwd; 8 heads of 64, 100 on 100 5.8 and 6.9, 64 on 64
+// 5.8 and 5.3; 2 x 16 heads on 4 of 128, 300 on 300 (304 blocks) 16.8 and 11.5.
 static bool few(const MaskedAttnArgs& a) {
-  const long rows = (long)a.Sq * (a.H / a.Hkv);
-  return rows <= 32 || few_blocks(a, 512);
+  const long rows = (long)a.Sq * (a.H / a.Hkv), blocks = a.B * a.Hkv * ((rows + 31) / 32);
+  return rows <= 32 || (blocks <= (a.dh <= 64 ? 512 : 256) && key_reach(a) >= 96);
 }
-// One workgroup per CU, and no more than there are tiles for its four waves.  64 heads, window
-// 1024: 13.9 us with both kernels; with two tiles for each wave 14.8.
+// One workgroup per CU, and no more than there are tiles for its four waves (64 heads, window
+// 1024: 13.9 us with both kernels; with two tiles for each wave 14.8); none split below 512 keys, as the join
+// takes 4 us.
 static FewWork few_work(const MaskedAttnArgs& a) {
   FewWork w;
   w.rb = (a.Sq * (a.H / a.Hkv) + 31) / 32;
   const long wgs = (long)a.B * a.Hkv * w.rb;
-  w.split = (int)std::max(1l, std::min({64l, (256 + wgs - 1) / wgs, key_reach(a) / 128}));
+  const long reach = key_reach(a);
+  w.split = reach < 512 ? 1 : (int)std::max(1l, std::min({64l, (256 + wgs - 1) / wgs, reach / 128}));
   return w;
 }
 
@@ -1783,7 +1804,7 @@ static bool launch_few_dq(const MaskedAttnArgs& a, hipStream_t s) {
   const long wgs = (long)a.B * a.H * ((a.Sq + 31) / 32);
   // one and a half rounds of the CUs at most: 348 workgroups of one per CU (fp32, 29 x 2 heads of 191, with the
   // table's gradient) take 41 us, 54 in the other kernel; 448 (bf16, 4 x 8 heads of 430) 25.7 and 20.2
-  if (!few_blocks(a, FEW_DQ) || lds > 160 * 1024 || wgs > 384 * (long)(160 * 1024 / lds)) return false;
+  if (!few_blocks(a) || lds > 160 * 1024 || wgs > 384 * (long)(160 * 1024 / lds)) return false;
   const dim3 grid((unsigned)wgs), block(64 * NW);
   if (!a.table) RG_LAUNCH((attn_few_dq<O, false, false, NW>), grid, block, 0, s, a);
   else if (!a.dtable) RG_LAUNCH((attn_few_dq<O, true, false, NW>), grid, block, W4, s, a);

@@ -77,6 +77,12 @@ CASES = [
     A("bf16", 2, 32, 8, 64, 300, 700, causal=True, nb=16, dist=30, len_q=[300, 211], len_k=[700, 640]),
     A("f32", 2, 32, 4, 64, 270, 530, causal=True),
     A("f32", 1, 2, 2, 64, 130, 640, causal=True, nb=16, dist=64),
+    # keys on both sides of the bias' reach, wholly visible blocks among them
+    A("bf16", 1, 2, 2, 64, 100, nb=16, dist=20),
+    A("bf16", 1, 2, 1, 128, 250, nb=16, dist=20),
+    A("bf16", 2, 2, 2, 64, 600, window=300, sinks=40, nb=32, dist=50, len_q=[600, 333], len_k=[600, 333]),
+    A("f32", 1, 2, 2, 64, 130, nb=16, dist=20),
+    A("f32", 1, 2, 2, 100, 230, nb=16, dist=20),
     # rows that fill the GPU: a wave per block of them
     A("bf16", 2, 32, 8, 64, 300, causal=True, window=90, sinks=3),
     A("f32", 2, 32, 16, 100, 270, causal=True),
