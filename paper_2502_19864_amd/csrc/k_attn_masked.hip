@@ -1737,10 +1737,11 @@ static BwdSpace bwd_space(int dtype, const MaskedAttnArgs& a, bool dtable) {
 // are one round of workgroups (two per CU at head dims up to 64; fp32 ones gain there in two rounds
 // as well), over a loop that gives each wave some of it.  16 heads on 4 of 128, 256 queries on 1024 and 8192
 // keys: 16.4 and 51 us here, 26.5 and 170 in attn_masked_fwd; 8 heads of 64, 100 on 100 5.8 and 6.9, 64 on 64
-// 5.8 and 5.3; 2 x 16 heads on 4 of 128, 300 on 300 (304 blocks) 16.8 and 11.5.
+// 5.8 and 5.3; 2 x 16 heads on 4 of 128, 300 on 300 (304 blocks) 16.8 and 11.5; over 8192 keys two rounds are
+// no worse (512 blocks: 163 and 172).
 static bool few(const MaskedAttnArgs& a) {
   const long rows = (long)a.Sq * (a.H / a.Hkv), blocks = a.B * a.Hkv * ((rows + 31) / 32);
-  return rows <= 32 || (blocks <= (a.dh <= 64 ? 512 : 256) && key_reach(a) >= 96);
+  return rows <= 32 || (blocks <= (a.dh <= 64 ? 512 : 256) && key_reach(a) >= 96) || (blocks <= 512 && key_reach(a) >= 4096);
 }
 // One workgroup per CU, and no more than there are tiles for its four waves (64 heads, window
 // 1024: 13.9 us with both kernels; with two tiles for each wave 14.8); none split below 512 keys, as the join
@@ -1802,9 +1803,10 @@ static bool launch_few_dq(const MaskedAttnArgs& a, hipStream_t s) {
   const int W4 = (2 * a.R + 1) * 4;
   const size_t lds = sizeof(typename O::E) * NW * 4 * O::BLOCK + NW * 128 + (a.table ? (size_t)W4 * (a.dtable ? 1 + NW : 1) : 0);
   const long wgs = (long)a.B * a.H * ((a.Sq + 31) / 32);
-  // one and a half rounds of the CUs at most: 348 workgroups of one per CU (fp32, 29 x 2 heads of 191, with the
-  // table's gradient) take 41 us, 54 in the other kernel; 448 (bf16, 4 x 8 heads of 430) 25.7 and 20.2
-  if (!few_blocks(a) || lds > 160 * 1024 || wgs > 384 * (long)(160 * 1024 / lds)) return false;
+  // one and a half rounds of the CUs at most, but over long loops: 348 workgroups of one per CU (fp32, 29 x 2 heads
+  // of 191, with the table's gradient) take 41 us, 54 in the other kernel; 448 (bf16, 4 x 8 heads of 430) 25.7 and
+  // 20.2; 408 (bf16, 3 heads of 4323, with the table's gradient) 248 and 460
+  if (!few_blocks(a) || lds > 160 * 1024 || (wgs > 384 * (long)(160 * 1024 / lds) && key_reach(a) < 1024)) return false;
   const dim3 grid((unsigned)wgs), block(64 * NW);
   if (!a.table) RG_LAUNCH((attn_few_dq<O, false, false, NW>), grid, block, 0, s, a);
   else if (!a.dtable) RG_LAUNCH((attn_few_dq<O, true, false, NW>), grid, block, W4, s, a);

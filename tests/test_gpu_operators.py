@@ -83,6 +83,9 @@ CASES = [
     A("bf16", 2, 2, 2, 64, 600, window=300, sinks=40, nb=32, dist=50, len_q=[600, 333], len_k=[600, 333]),
     A("f32", 1, 2, 2, 64, 130, nb=16, dist=20),
     A("f32", 1, 2, 2, 100, 230, nb=16, dist=20),
+    # groups of three heads, whose rows straddle the blocks
+    A("bf16", 1, 6, 2, 64, 120, 150, causal=True, window=40, sinks=2),
+    A("f32", 2, 9, 3, 24, 70, 333, causal=False, window=100, sinks=40, nb=8, dist=6, len_q=[70, 41], len_k=[333, 99]),
     # rows that fill the GPU: a wave per block of them
     A("bf16", 2, 32, 8, 64, 300, causal=True, window=90, sinks=3),
     A("f32", 2, 32, 16, 100, 270, causal=True),
