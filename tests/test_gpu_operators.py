@@ -83,6 +83,14 @@ CASES = [
     A("bf16", 2, 2, 2, 64, 600, window=300, sinks=40, nb=32, dist=50, len_q=[600, 333], len_k=[600, 333]),
     A("f32", 1, 2, 2, 64, 130, nb=16, dist=20),
     A("f32", 1, 2, 2, 100, 230, nb=16, dist=20),
+    # the longest reach of the bias, which fills the LDS; one bucket; each query its own key alone
+    A("f32", 1, 2, 2, 100, 200, causal=True, nb=32, dist=1024),
+    A("f32", 1, 1, 1, 64, 700, nb=32, dist=1024),
+    A("bf16", 1, 2, 1, 128, 260, nb=32, dist=1024),
+    A("bf16", 2, 2, 2, 64, 70, nb=1, dist=0),
+    A("bf16", 1, 2, 2, 64, 1, 1, nb=2, dist=3),
+    A("bf16", 1, 4, 2, 64, 150, causal=False, window=1),
+    A("f32", 2, 3, 1, 7, 33, 2, causal=True, len_q=[33, 1], len_k=[0, 2]),
     # groups of three heads, whose rows straddle the blocks
     A("bf16", 1, 6, 2, 64, 120, 150, causal=True, window=40, sinks=2),
     A("f32", 2, 9, 3, 24, 70, 333, causal=False, window=100, sinks=40, nb=8, dist=6, len_q=[70, 41], len_k=[333, 99]),
@@ -242,6 +250,59 @@ def test_strides_and_outputs_in_place():
     for n, x in (("o", ov), ("dq", dq), ("dk", dk), ("dv", dv)):
         R.check(n, x, *want[n])
     assert bool((o[:, :, 75:] == 7).all()) and bool((f[:, 75:] == 5).all())
+
+
+def test_broadcast_inputs():
+    """One sequence of keys for every batch row, one key-value head under another name."""
+    import torch
+
+    from paper_2502_19864_amd import operators as ops
+    t = make(A("bf16", 3, 4, 2, 64, 90, 140, causal=True, window=60, sinks=2))
+    k, v = t["k"][:1].expand(3, 140, 2, 64), t["v"][:, :, :1].expand(3, 140, 2, 64)
+    o, lse = ops.attention_forward(t["q"], k, v, **t["how"])
+    dq, dk, dv = ops.attention_backward(t["do"], t["q"], k, v, o, lse, **t["how"])
+    want = R.attention(t["q"], k, v, t["do"], lowp=True, **t["how"])
+    for n, x in dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv).items():
+        R.check(n, x, *want[n])
+
+
+def test_many_short_sequences():
+    """More sequences than a grid's other dimensions hold, of two tokens each."""
+    import torch
+
+    from paper_2502_19864_amd import operators as ops
+    B = 70000
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v, do = (torch.randn(B, 2, 1, 64, generator=g, device="cuda").bfloat16() for _ in range(4))
+    o, lse = ops.attention_forward(q, k, v, causal=True)
+    dq, dk, dv = ops.attention_backward(do, q, k, v, o, lse, causal=True)
+    at = [0, 1, 65535, 65536, B - 1]
+    want = R.attention(*(x[at] for x in (q, k, v, do)), lowp=True, causal=True, scale=0.125)
+    for n, x in dict(o=o, lse=lse, dq=dq, dk=dk, dv=dv).items():
+        R.check(n, x[at], *want[n])
+
+
+def test_two_streams_at_once():
+    """Calls under way together, each with a workspace of its own, give what one alone gives."""
+    import torch
+
+    ts = [make(CASES[i], seed=i) for i in (12, 18, 23)]
+    alone = [run(t) for t in ts]
+    streams = [torch.cuda.Stream() for _ in ts]
+    got = [None] * len(ts)
+    from paper_2502_19864_amd import operators as ops
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i, (t, s) in enumerate(zip(ts, streams)):
+            with torch.cuda.stream(s):
+                o, lse = ops.attention_forward(t["q"], t["k"], t["v"], **t["how"])
+                dtable = None if t["table"] is None else torch.zeros_like(t["table"])
+                grads = ops.attention_backward(t["do"], t["q"], t["k"], t["v"], o, lse, dtable=dtable, **t["how"])
+                got[i] = dict(zip(("o", "lse", "dq", "dk", "dv", "dtable"), (o, lse) + tuple(grads) + (dtable,)))
+    torch.cuda.synchronize()
+    for a, b in zip(alone, got):
+        for n in a:
+            assert torch.equal(a[n], b[n]), n
 
 
 def test_gradients_against_differences():
