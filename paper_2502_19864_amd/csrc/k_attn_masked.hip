@@ -19,6 +19,7 @@
 // way into the second product (they are never stored; every sum stays in fp32);
 // fp32 ones on MFMA 32x32x2 in fp32 throughout.
 #include <algorithm>
+#include <type_traits>
 
 #include "attn_core.h"
 #include "common.h"
@@ -963,7 +964,8 @@ __device__ __forceinline__ void put_diag(const float* sbias, int W, float* out) 
 // from the stored (rounded) O would leave an error of that rounding in them.  That sweep
 // is two of the pass's five products.  Bound by issue, as the forward: 8192 tokens, window 1024
 // 255 us, matrix unit 39 %, vector unit 34 % busy; with the table's gradient (1777 tokens, 2 x 16 heads,
-// window 500) 109 us, 45 registers spilled at head dim 128.
+// window 500) 81 us.  The two sweeps are two loops, so that dQ holds no registers in the first: as one loop
+// with a flag 45 registers spilled and the same took 109.
 template <class O, bool BIAS, bool DTAB, int NW>
 __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAttnArgs a) {
   typedef typename O::E E;
@@ -994,7 +996,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   const int nit = DTAB ? 2 * kt.n : kt.n;  // DTAB: the tiles twice
   const uint32_t kfirst = O::template dma_first<NW>(a.k.t, a.dh, lane, wave);
   const uint32_t vfirst = O::template dma_first<NW>(a.v.t, a.dh, lane, wave);
-  auto issue = [&](int i) {
+  auto issue = [&](int i) __attribute__((always_inline)) {
     const int k0 = kt.at(DTAB && i >= kt.n ? i - kt.n : i) * KR, last = sq.lk - 1 - k0;
     E* dst = sm + (i % ST) * 2 * TILE;
     O::template dma<NW>(K + (long)k0 * a.k.t, a.k.t, last, dst, a.dh, lane, wave, kfirst);
@@ -1019,44 +1021,50 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
     for (int i = 0; i < W; i += 64) diag[min(i + lane, W - 1)] = 0.f;  // all lanes, as in load_bias
   float dlo = 0.f, dhi = 0.f;
 
-  f32x16 dq[DH / 32];
-#pragma unroll
-  for (int i = 0; i < DH / 32; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) dq[i][r] = 0.f;
-
   qf.settled();
   df.settled();
   settle(lse);
   settle(dsum);
-  for (int i = 0; i < nit; ++i) {
-    tile_ready<ST, PER>(i, nit);
-    if (i + ST - 1 < nit) issue(i + ST - 1);
-    if (q0 >= sq.lq) continue;
-    const bool first = DTAB && i < kt.n;
-    if (DTAB && i == kt.n) dsum += __shfl_xor(dsum, 32, 64);
-    const E* sK = sm + (i % ST) * 2 * TILE;
-    const E* sV = sK + TILE;
-    // one key block at a time (not unrolled): keeps the kernel within its registers
+  f32x16 dq[DH / 32];
+  // the key tiles once, as iterations from .. of the pipeline; first: for D alone
+  auto sweep = [&](auto first, int from) __attribute__((always_inline)) {
+    for (int t = 0; t < kt.n; ++t) {
+      const int i = from + t;
+      tile_ready<ST, PER>(i, nit);
+      if (i + ST - 1 < nit) issue(i + ST - 1);
+      if (q0 >= sq.lq) continue;
+      const E* sK = sm + (i % ST) * 2 * TILE;
+      const E* sV = sK + TILE;
+      // one key block at a time (not unrolled): keeps the kernel within its registers
 #pragma unroll 1
-    for (int kb = 0; kb < KR / 32; ++kb) {
-      const int k0 = kt.at(DTAB && i >= kt.n ? i - kt.n : i) * KR + kb * 32;
-      const int kind = span.kind(k0 / 32);
-      if (kind == 0) continue;  // wave-uniform
-      ops.fresh();
-      f32x16 st, dp;
-      p_and_dp<O, BIAS>(ops, st, dp, sK, sV, kb, qf, df, sl2, sbias, a.R, k0, p, plo, phi, kind == 2, seen, lse, half);
-      if (first) {
+      for (int kb = 0; kb < KR / 32; ++kb) {
+        const int k0 = kt.at(t) * KR + kb * 32;
+        const int kind = span.kind(k0 / 32);
+        if (kind == 0) continue;  // wave-uniform
+        ops.fresh();
+        f32x16 st, dp;
+        p_and_dp<O, BIAS>(ops, st, dp, sK, sV, kb, qf, df, sl2, sbias, a.R, k0, p, plo, phi, kind == 2, seen, lse, half);
+        if constexpr (first) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dsum = fmaf(st[r], dp[r], dsum);
-        continue;
+          for (int r = 0; r < 16; ++r) dsum = fmaf(st[r], dp[r], dsum);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) st[r] *= dp[r] - dsum;  // dS
+          if (DTAB) add_diag(st, k0 - sq.off - q0, a.R, diag, dlo, dhi, lane);
+          ops.accum(dq, sK, kb, st);
+        }
       }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) st[r] *= dp[r] - dsum;  // dS
-      if (DTAB) add_diag(st, k0 - sq.off - q0, a.R, diag, dlo, dhi, lane);
-      ops.accum(dq, sK, kb, st);
     }
+  };
+  if constexpr (DTAB) {
+    sweep(std::true_type{}, 0);
+    dsum += __shfl_xor(dsum, 32, 64);
   }
+#pragma unroll
+  for (int i = 0; i < DH / 32; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dq[i][r] = 0.f;
+  sweep(std::false_type{}, DTAB ? __builtin_amdgcn_readfirstlane(kt.n) : 0);
   // the row statistics that the dK/dV pass reads
   if (q < a.Sq && half == 0) a.stat[(long)bh * a.Sq + q] = make_float2(lse, dsum);
   if (DTAB) close_diag(diag, W, dlo, dhi, lane);
@@ -1072,7 +1080,7 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
 // The same for calls whose 32-row blocks would hold fewer than half of the SIMDs: a workgroup takes one of
 // them, and its waves every fourth (second) block of its keys each, from tiles of their own as
 // in attn_few_fwd; D and dQ are joined in LDS.  4 heads on 2 of 128, 1824 tokens, with the
-// table's gradient: 69 us, 208 with one wave per block.
+// table's gradient: 69 us, 147 with one wave per block.
 template <class O, bool BIAS, bool DTAB, int NW>
 __global__ __launch_bounds__(64 * NW, 1) void attn_few_dq(MaskedAttnArgs a) {
   typedef typename O::E E;
@@ -1804,8 +1812,8 @@ static bool launch_few_dq(const MaskedAttnArgs& a, hipStream_t s) {
   const size_t lds = sizeof(typename O::E) * NW * 4 * O::BLOCK + NW * 128 + (a.table ? (size_t)W4 * (a.dtable ? 1 + NW : 1) : 0);
   const long wgs = (long)a.B * a.H * ((a.Sq + 31) / 32);
   // one and a half rounds of the CUs at most, but over long loops: 348 workgroups of one per CU (fp32, 29 x 2 heads
-  // of 191, with the table's gradient) take 41 us, 54 in the other kernel; 448 (bf16, 4 x 8 heads of 430) 25.7 and
-  // 20.2; 408 (bf16, 3 heads of 4323, with the table's gradient) 248 and 460
+  // of 191, with the table's gradient) take 41 us, 51 in the other kernel; 448 (bf16, 4 x 8 heads of 430) 25.7 and
+  // 20.2; 408 (bf16, 3 heads of 4323, with the table's gradient) 248 and 293
   if (!few_blocks(a) || lds > 160 * 1024 || (wgs > 384 * (long)(160 * 1024 / lds) && key_reach(a) < 1024)) return false;
   const dim3 grid((unsigned)wgs), block(64 * NW);
   if (!a.table) RG_LAUNCH((attn_few_dq<O, false, false, NW>), grid, block, 0, s, a);
