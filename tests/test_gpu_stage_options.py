@@ -26,6 +26,9 @@ CASES = {
     "bert_dh128": (Workload("opt_bd", "bert", "bf16", 2, 512, 4, 512, 64, 150, 2, 0, "dy", 3106), 50, 3, 0, 0, 0.1),
     "llama": (Workload("opt_l", "llama", "bf16", 2, 256, 2, 512, 64, 300, 2, 0, "dy", 3107), 65, 4, 32, 128, 0.1),
     "llama_64": (Workload("opt_l64", "llama", "bf16", 2, 256, 4, 512, 64, 140, 2, 0, "dy", 3108), 30, 0, 0, 0, 0.1),
+    # rotated heads of short sequences, and of rows that fill the GPU
+    "llama_short": (Workload("opt_ls", "llama", "bf16", 2, 256, 2, 512, 64, 100, 2, 0, "dy", 3109), 45, 2, 16, 30, 0.1),
+    "llama_rows": (Workload("opt_lr", "llama", "bf16", 2, 256, 4, 512, 64, 260, 16, 0, "dy", 3110), 65, 3, 16, 40, 0.0),
 }
 SEED, OFFSET, SITE = 77, 123456789012, 6
 
