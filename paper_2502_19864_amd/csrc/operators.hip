@@ -153,6 +153,41 @@ extern "C" ringada_status ringada_attn_backward(void* stream, const ringada_attn
   return RINGADA_OK;
 }
 
+// A whole number of up to 328 32-bit words: 1024^1024 and 16 words to spare.
+struct Whole {
+  int n = 1;
+  uint32_t w[328] = {1};
+  void times(uint32_t f, int power) {
+    for (; power > 0; --power) {
+      uint64_t carry = 0;
+      for (int i = 0; i < n; ++i) {
+        carry += (uint64_t)w[i] * f;
+        w[i] = (uint32_t)carry;
+        carry >>= 32;
+      }
+      if (carry) w[n++] = (uint32_t)carry;
+    }
+  }
+  bool operator>=(const Whole& o) const {
+    if (n != o.n) return n > o.n;
+    for (int i = n - 1; i >= 0; --i)
+      if (w[i] != o.w[i]) return w[i] > o.w[i];
+    return true;
+  }
+};
+// d >= one (dist / one)^(k / m), 1 <= k <= m <= 1024, all of them at most 1024.  The power is off by some 1e-16 of
+// it; a distance nearer than that allows is compared in whole numbers, d^m with dist^k one^(m - k): some
+// reach the power exactly, others lie within 1e-10 of it without reaching it.
+static bool reaches(int d, int one, int dist, int k, int m) {
+  const long double power = one * powl((long double)dist / one, k / (long double)m);
+  if (fabsl(d - power) > 1e-12L * power) return d > power;
+  Whole a, b;
+  a.times(d, m);
+  b.times(dist, k);
+  b.times(one, m - k);
+  return a >= b;
+}
+
 extern "C" ringada_status ringada_relpos_buckets(int32_t n_buckets, int32_t max_distance, int32_t bidirectional,
                                                  int32_t* map) {
   if (!map) return fail(RINGADA_E_INVALID, "map is NULL");
@@ -165,13 +200,9 @@ extern "C" ringada_status ringada_relpos_buckets(int32_t n_buckets, int32_t max_
     const int d = bidirectional ? (r < 0 ? -r : r) : (r < 0 ? -r : 0);
     int t = d;
     if (d >= one) {
-      // one + k for the largest k with d >= one (max_distance / one)^(k / (n - one)); where that
-      // power is a whole number the long double power is off by far less than 1e-9 of it, and
-      // where it is not, no whole number up to 1024 is that near
+      // one + k for the largest k with d >= one (max_distance / one)^(k / (n - one))
       int k = 0;
-      while (k < n - one &&
-             (long double)d * (1 + 1e-9L) >= one * powl((long double)max_distance / one, (k + 1) / (long double)(n - one)))
-        ++k;
+      while (k < n - one && reaches(d, one, max_distance, k + 1, n - one)) ++k;
       t = one + k < n ? one + k : n - 1;
     }
     map[r + max_distance] = t + (bidirectional && r > 0 ? n : 0);

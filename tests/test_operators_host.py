@@ -159,6 +159,17 @@ def test_bucket_map(n, dist, bidi):
         assert got[rel + dist] == t + (per if bidi and rel > 0 else 0), rel
 
 
+@pytest.mark.parametrize("n,dist,rel,bucket", [(73, 905, 347, 61), (222, 316, 245, 194), (226, 188, 157, 185),
+                                               (281, 527, 297, 219)])
+def test_bucket_map_next_to_a_border(n, dist, rel, bucket):
+    """Distances 3e-11 to 6e-10 of themselves below a border that is no whole number."""
+    one = n // 2
+    m, k = n - one, bucket + 1 - one
+    assert rel ** m < dist ** k * one ** (m - k) and (rel + 1) ** m > dist ** k * one ** (m - k)
+    assert B.ringada_relpos_buckets(n, dist, False)[dist - rel] == bucket
+    assert B.ringada_relpos_buckets(2 * n, dist, True)[dist - rel] == bucket
+
+
 @pytest.mark.parametrize("n,dist,bidi", [(1, 8, False), (0, 8, False), (3, 8, True), (2, 8, True), (32, 8, True),
                                          (32, 16, False), (32, 1025, True), (8, -1, False)])
 def test_bucket_map_refuses(n, dist, bidi):
