@@ -1693,6 +1693,10 @@ static bool few_blocks(const MaskedAttnArgs& a) {
   return (long)a.B * a.H * ((a.Sq + 31) / 32) < 512 && key_reach(a) >= 64;
 }
 
+// HIP takes fewer than 2^32 threads in a launch's x dimension, and workgroups here have 256 (attn_bias_grad, one
+// workgroup of 1024 per head, stays below that)
+constexpr long MAX_WGS = (1l << 24) - 1;
+
 static size_t al256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Workgroups of the dK/dV pass: two per CU hide each other's barriers, so blocks are split
@@ -1721,7 +1725,7 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
                       ? far
                       : std::min(far, std::max({(long)(w.c_near + 7) / 8, least, (far + 63) / 64, (far * nfar + 2047) / 2048})));
   w.s_far = (int)((far + w.c_far - 1) / w.c_far);
-  if (w.s_far < w.s_near || (long)w.items() * a.B * a.Hkv >= (1l << 31)) {
+  if (w.s_far < w.s_near || w.items() * a.B * a.Hkv > MAX_WGS) {
     w.s_far = w.s_near = 1;
     w.c_far = w.c_near = (int)far;
   }
@@ -1761,6 +1765,18 @@ static FewWork few_work(const MaskedAttnArgs& a) {
   const long reach = key_reach(a);
   w.split = reach < 512 ? 1 : (int)std::max(1l, std::min({64l, (256 + wgs - 1) / wgs, reach / 128}));
   return w;
+}
+
+bool masked_attn_fits(int dtype, const MaskedAttnArgs& a) {
+  long most = std::max(blocks_of(a.Sq) * a.H, blocks_of(a.Sk) * a.Hkv) * a.B;
+  if (few(a)) {
+    const FewWork w = few_work(a);
+    most = std::max(most, (long)a.B * a.Hkv * w.split * w.rb);
+    if (w.split > 1) most = std::max(most, ((long)a.B * a.H * a.Sq + 3) / 4);
+  }
+  const KeyWork w = key_work(dtype, a);
+  if (w.slots()) most = std::max(most, (long)a.B * a.Hkv * (w.s_near > 1 ? w.nk : w.nfar) * MA_NW);
+  return most <= MAX_WGS;
 }
 
 void masked_attn_bytes(int dtype, const MaskedAttnArgs& a, bool dtable, size_t* fwd, size_t* bwd) {

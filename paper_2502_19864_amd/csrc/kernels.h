@@ -107,6 +107,8 @@ struct MaskedAttnArgs {
   float* diag;                // workspace (dtable): sums of dS by relative position, per workgroup of the dQ pass
   float* part;                // workspace: partial sums of workgroups that share their output rows
 };
+// whether every launch of a forward and backward stays within what HIP takes
+bool masked_attn_fits(int dtype, const MaskedAttnArgs& a);
 // bytes of the workspaces, and the backward's pointers into its own
 void masked_attn_bytes(int dtype, const MaskedAttnArgs& a, bool dtable, size_t* fwd, size_t* bwd);
 void masked_attn_workspace(int dtype, MaskedAttnArgs& a, void* ws);

@@ -11,6 +11,19 @@
 
 using namespace rg;
 
+static MaskedAttnArgs attn_sizes(const ringada_attn_desc& D) {
+  MaskedAttnArgs a{};
+  a.B = D.batch; a.H = D.n_heads; a.Hkv = D.n_kv_heads; a.dh = D.d_head; a.Sq = D.seq_q; a.Sk = D.seq_k;
+  a.causal = D.causal != 0;
+  // no two rows are seq_q + seq_k apart: such a window hides nothing
+  a.window = D.window >= D.seq_q + D.seq_k ? 0 : D.window;
+  a.sinks = D.sinks < D.seq_k ? D.sinks : D.seq_k;
+  a.scale = D.scale;
+  a.R = D.n_buckets ? D.max_distance : 0;
+  a.nb = D.n_buckets;
+  return a;
+}
+
 static ringada_status check_attn(const ringada_attn_desc* D) {
   if (!D) return fail(RINGADA_E_INVALID, "desc is NULL");
   if (D->dtype != RINGADA_F32 && D->dtype != RINGADA_BF16) return fail(RINGADA_E_INVALID, "unknown dtype %d", D->dtype);
@@ -27,22 +40,10 @@ static ringada_status check_attn(const ringada_attn_desc* D) {
   if (D->d_head > 128) return fail(RINGADA_E_UNSUPPORTED, "f32 path: d_head must be at most 128 (got %d)", D->d_head);
   if (D->seq_q > (1 << 24) || D->seq_k > (1 << 24)) return fail(RINGADA_E_UNSUPPORTED, "sequences above 2^24 rows");
   const int64_t rows = D->seq_q > D->seq_k ? D->seq_q : D->seq_k;
-  if ((int64_t)D->batch * D->n_heads * ((rows + 31) / 32) >= (1ll << 31) || D->n_heads > 65535)
+  if ((int64_t)D->batch * D->n_heads * ((rows + 31) / 32) >= (1ll << 31) || D->n_heads > 65535 ||
+      !masked_attn_fits(D->dtype, attn_sizes(*D)))
     return fail(RINGADA_E_UNSUPPORTED, "too many rows for one launch");
   return RINGADA_OK;
-}
-
-static MaskedAttnArgs attn_sizes(const ringada_attn_desc& D) {
-  MaskedAttnArgs a{};
-  a.B = D.batch; a.H = D.n_heads; a.Hkv = D.n_kv_heads; a.dh = D.d_head; a.Sq = D.seq_q; a.Sk = D.seq_k;
-  a.causal = D.causal != 0;
-  // no two rows are seq_q + seq_k apart: such a window hides nothing
-  a.window = D.window >= D.seq_q + D.seq_k ? 0 : D.window;
-  a.sinks = D.sinks < D.seq_k ? D.sinks : D.seq_k;
-  a.scale = D.scale;
-  a.R = D.n_buckets ? D.max_distance : 0;
-  a.nb = D.n_buckets;
-  return a;
 }
 
 // writes: no two elements of the view may share an address

@@ -581,10 +581,14 @@ static MaskedAttnArgs masked_attn_sizes(const ringada_stage_desc& D, const ringa
   return a;
 }
 
-static size_t masked_attn_need(const ringada_stage_desc& D, const ringada_stage_attention& o, int B, int S) {
+static ringada_status masked_attn_need(const ringada_stage_desc& D, const ringada_stage_attention& o, int B, int S,
+                                       size_t* need) {
+  const MaskedAttnArgs a = masked_attn_sizes(D, o, B, S);
+  if (!masked_attn_fits(D.dtype, a)) return fail(RINGADA_E_UNSUPPORTED, "too many rows for one launch");
   size_t f, b;
-  masked_attn_bytes(D.dtype, masked_attn_sizes(D, o, B, S), o.n_buckets && o.g_table, &f, &b);
-  return std::max(f, b);
+  masked_attn_bytes(D.dtype, a, o.n_buckets && o.g_table, &f, &b);
+  *need = std::max(f, b);
+  return RINGADA_OK;
 }
 
 extern "C" ringada_status ringada_stage_plan_attention(const ringada_stage_desc* desc,
@@ -595,8 +599,8 @@ extern "C" ringada_status ringada_stage_plan_attention(const ringada_stage_desc*
   RG_TRY(check_attention(opt));
   if (batch < 1 || seq < 1 || batch > desc->max_batch || seq > desc->max_seq)
     return fail(RINGADA_E_INVALID, "batch %d / seq %d outside [1, max]", batch, seq);
-  *workspace_bytes = opt->window || opt->n_buckets ? masked_attn_need(*desc, *opt, batch, seq) : 0;
-  return RINGADA_OK;
+  *workspace_bytes = 0;
+  return opt->window || opt->n_buckets ? masked_attn_need(*desc, *opt, batch, seq, workspace_bytes) : RINGADA_OK;
 }
 
 extern "C" ringada_status ringada_stage_set_attention(ringada_stage* st, const ringada_stage_attention* opt) {
@@ -818,7 +822,8 @@ extern "C" ringada_status ringada_stage_forward(ringada_stage* st, void* stream,
   if (stash_bytes < L.stash_bytes || (L.stash_bytes && !stash))
     return fail(RINGADA_E_WORKSPACE, "stash of %zu bytes, plan needs %zu", stash_bytes, L.stash_bytes);
   if (st->masked) {
-    const size_t need = masked_attn_need(D, st->att, batch, seq);
+    size_t need;
+    RG_TRY(masked_attn_need(D, st->att, batch, seq, &need));
     if (st->att.workspace_bytes < need || (need && !st->att.workspace))
       return fail(RINGADA_E_WORKSPACE, "attention workspace of %zu bytes, batch %d x %d needs %zu",
                   st->att.workspace_bytes, batch, seq, need);

@@ -38,6 +38,28 @@ def test_attention_descriptor_is_checked(kw, status):
     assert e.value.status == status and B.ringada_last_error()
 
 
+@pytest.mark.parametrize("kw", [dict(), dict(dtype=B.F32, d_head=16), dict(seq_q=128, seq_k=128),
+                                dict(n_kv_heads=1, seq_q=200, seq_k=200)])
+def test_launches_are_bounded_by_their_threads(kw):
+    """A launch holds fewer than 2^32 threads, 256 to a workgroup: refused before anything is enqueued."""
+    d = dict(dict(n_heads=16, n_kv_heads=16, seq_q=1, seq_k=1), **kw)
+    blocks = 16 * ((d["seq_q"] + 127) // 128)  # workgroups of a batch row, one per 128 queries of a head
+    most = ((1 << 24) - 1) // blocks
+    assert B.ringada_attn_plan(desc(batch=most, **d), False)[1] > 0
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_plan(desc(batch=most + 1, **d), False)
+    assert e.value.status == B.RINGADA_E_UNSUPPORTED
+
+
+def test_a_stage_refuses_what_no_launch_holds():
+    d = stage_desc(dtype="f32", d_model=64, n_heads=32, d_ffn=64, d_adapter=16, batch=1 << 19, seq=1)
+    opt = B.StageAttention(window=4)
+    assert B.ringada_stage_plan_attention(d, opt, (1 << 19) - 1, 1) > 0
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_stage_plan_attention(d, opt, 1 << 19, 1)
+    assert e.value.status == B.RINGADA_E_UNSUPPORTED
+
+
 def test_attention_plan():
     f, b = B.ringada_attn_plan(desc(), False)
     assert b >= 2 * 4 * 10 * 4
