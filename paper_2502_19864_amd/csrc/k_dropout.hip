@@ -37,7 +37,7 @@ __device__ __forceinline__ Philox philox4x32_10(uint32_t c0, uint32_t c1, uint32
 template <typename T, bool RES>
 __global__ __launch_bounds__(256) void dropout_k(const T* x, const T* res, T* y, long n, uint32_t thr, float f,
                                                  const uint64_t* rng, uint32_t site, bool wide) {
-  const long c = (long)blockIdx.x * 256 + threadIdx.x;
+  const long c = ((long)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
   if (c * 8 >= n) return;
   const uint64_t seed = rng[0], off = rng[1];
   const Philox u = philox4x32_10((uint32_t)c, site, (uint32_t)off, (uint32_t)(off >> 32), (uint32_t)seed,
@@ -80,7 +80,9 @@ static hipError_t dropout_t(const void* x, const void* res, void* y, long n, uin
                             uint32_t site, hipStream_t s) {
   const float f = 65536.f / (65536.f - (float)thr);
   const bool wide = ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y) | reinterpret_cast<uintptr_t>(res)) & 15u) == 0;
-  const dim3 grid((unsigned)((n + 2047) / 2048)), block(256);
+  // HIP takes fewer than 2^32 threads in a dimension of a launch: from 2^34 elements on, more than one row of them
+  const long wgs = (n + 2047) / 2048, rows = (wgs + (1l << 23) - 1) >> 23;
+  const dim3 grid((unsigned)((wgs + rows - 1) / rows), (unsigned)rows), block(256);
   if (res)
     RG_LAUNCH((dropout_k<T, true>), grid, block, 0, s, static_cast<const T*>(x), static_cast<const T*>(res),
               static_cast<T*>(y), n, thr, f, rng, site, wide);

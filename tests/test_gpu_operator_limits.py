@@ -1,0 +1,42 @@
+"""The block operators at the ends of their documented ranges."""
+import pytest
+
+import philox_vectors as P
+
+pytestmark = pytest.mark.gpu
+
+
+def signed(x):
+    return x - 2 ** 64 if x >= 2 ** 63 else x
+
+
+def keeps(x, at, want, rng, site):
+    """Elements at .. at + 7 of x stay exactly while the threshold is at most their 16 bits `want`."""
+    from paper_2502_19864_amd import operators as ops
+    for h in want:
+        for thr in (h, h + 1):
+            if thr > 65535:
+                continue
+            x[at:at + 8] = 1
+            ops.dropout(x, thr / 65536, rng, site, out=x)
+            assert (x[at:at + 8] != 0).tolist() == [w >= thr for w in want], (at, thr)
+
+
+@pytest.mark.parametrize("i,n", [(0, 8), (2, 8 * 0x243f6a88 + 8), (1, 1 << 35)])
+def test_dropout_gives_the_published_vectors(i, n):
+    """The generator's vectors read back from the mask of the elements that have their counter; the last one is
+    the last element of the largest tensor (64 GiB)."""
+    import torch
+
+    if torch.cuda.mem_get_info()[0] < 2 * n + (8 << 30):
+        pytest.skip("not enough free memory")
+    counter, key, out = P.VECTORS[i]
+    x = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    rng = torch.tensor([signed(key[0] | key[1] << 32), signed(counter[2] | counter[3] << 32)], device="cuda")
+    keeps(x, 8 * counter[0], [h for w in out for h in (w & 0xFFFF, w >> 16)], rng, counter[1])
+    if n > 1 << 34:  # both sides of where the launch takes a second row of workgroups
+        for at in ((1 << 34) - 8, 1 << 34):
+            want = P.halves(at // 8, key[0] | key[1] << 32, counter[2] | counter[3] << 32, counter[1])
+            keeps(x, at, want, rng, counter[1])
+    del x
+    torch.cuda.empty_cache()

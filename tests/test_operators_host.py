@@ -161,6 +161,16 @@ def test_dropout_arguments_are_checked(kw):
     assert e.value.status == B.RINGADA_E_INVALID
 
 
+def test_the_tests_generator_gives_the_published_vectors():
+    import operator_reference as R
+    import philox_vectors as P
+
+    for counter, key, out in P.VECTORS:
+        assert P.words(counter, key) == out
+    seed, offset, site = 0x0123456789abcdef, 0xfedcba9876543210, 0x13579bdf
+    assert R.philox(40, seed, offset, site) == [h for c in range(5) for h in P.halves(c, seed, offset, site)]
+
+
 @pytest.mark.parametrize("n,dist,bidi", [(32, 128, True), (32, 128, False), (16, 20, True), (64, 512, False),
                                          (4, 2, True), (2, 2, False), (2, 1024, False), (64, 1024, True),
                                          (8, 16, True), (320, 500, True), (1000, 1024, False)])
