@@ -1712,20 +1712,30 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
   const long span = (long)rows + (a.causal ? 1l : 2l) * a.window;
   const long near = a.window ? std::min(far, grp * (span / KR + 2)) : far;
   const long least = dtype == DT_BF16 ? 4 : 1;
-  const long wgs = (long)w.nk * a.B * a.Hkv, want = std::max(1l, std::min((512 + wgs - 1) / wgs, near / least));
-  w.c_near = (int)((near + want - 1) / want);
-  w.s_near = (int)((near + w.c_near - 1) / w.c_near);
+  const bool has_near = w.nfar < w.nk;
+  const long wgs = (long)w.nk * a.B * a.Hkv, nfar = (long)w.nfar * a.B * a.Hkv, longest = has_near ? near : far;
+  // Not into more than 64 pieces, which the join adds one after the other (fp32, 8 heads of 64 on 1, 512 tokens:
+  // 71 us, 89 with up to 128, 649 whole), nor the far ones into more than 2048 workgroups, as
+  // their partial sums take 64 or 128 KB each.
+  const long want = std::max(1l, std::min({(512 + wgs - 1) / wgs, longest / least, 64l}));
+  const long c_least = std::max({least, (far + 63) / 64, (far * nfar + 2047) / 2048});
+  w.c_near = (int)((longest + want - 1) / want);
+  w.s_near = has_near ? (int)((near + w.c_near - 1) / w.c_near) : 1;
+  long c = far;
+  // All of them far: nothing else fills gaps, so they are dealt as the others are (16 heads of 128, 2048 tokens:
+  // 154 us, 232 in eighths of that).  Causal ones in two pieces alone cannot even out their unequal
+  // lengths: quarters of that (32 heads on 8 of 128, 4096 tokens: 585 us, 640 in two pieces; 16 heads of 64, 2048
+  // tokens: 99.6 and 97.5).
+  if (!has_near) c = std::max(a.causal && want == 2 ? (far + 7) / 8 : (long)w.c_near, c_least);
   // A far block is left whole up to twice a near one's length (the join costs as much), else
   // dealt out in eighths of that, so that they fill the gaps: 512 near workgroups of 80
   // iterations are one round of the GPU, and far ones as long would begin another.  With the
   // join, 8192 tokens and window 1024: halves 430 us, quarters 383, eighths 365.
-  // Not into more than 2048 workgroups, as their partial sums take 64 or 128 KB each.
-  const long nfar = (long)w.nfar * a.B * a.Hkv;
-  w.c_far = (int)(w.s_near == 1 && far <= 2 * near
-                      ? far
-                      : std::min(far, std::max({(long)(w.c_near + 7) / 8, least, (far + 63) / 64, (far * nfar + 2047) / 2048})));
-  w.s_far = (int)((far + w.c_far - 1) / w.c_far);
-  if (w.s_far < w.s_near || w.items() * a.B * a.Hkv > MAX_WGS) {
+  // At least as many pieces as of a near one: KeyWork::slots.
+  else if (w.s_near > 1 || far > 2 * near) c = std::min(std::max((long)(w.c_near + 7) / 8, c_least), far / w.s_near);
+  w.c_far = (int)std::min(far, c);
+  w.s_far = w.nfar ? (int)((far + w.c_far - 1) / w.c_far) : 1;
+  if (w.items() * a.B * a.Hkv > MAX_WGS) {
     w.s_far = w.s_near = 1;
     w.c_far = w.c_near = (int)far;
   }

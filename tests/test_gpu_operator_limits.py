@@ -40,3 +40,27 @@ def test_dropout_gives_the_published_vectors(i, n):
             keeps(x, at, want, rng, counter[1])
     del x
     torch.cuda.empty_cache()
+
+
+def T(dtype, H, Hkv, dh, Sq, Sk, **kw):
+    from test_gpu_operators import A
+    return A(dtype, 1, H, Hkv, dh, Sq, Sk, **kw)
+
+
+@pytest.mark.parametrize("c", [
+    T("f32", 8, 1, 64, 512, 512, causal=True),
+    T("f32", 16, 2, 16, 305, 305, window=100),
+    T("f32", 16, 1, 40, 400, 400, causal=True, window=80, sinks=3, nb=16, dist=20),
+    T("bf16", 32, 1, 128, 600, 600, causal=True),
+    T("bf16", 8, 1, 64, 2048, 128),
+    T("bf16", 4, 4, 64, 700, 700, causal=True),
+], ids=str)
+def test_few_key_blocks_met_by_many_query_tiles(c):
+    """The dK/dV pass of few key blocks, or of blocks that every query sees, dealt to many workgroups."""
+    import operator_reference as R
+    from test_gpu_operators import make, run
+    t = make(c)
+    got = run(t)
+    want = R.attention(t["q"], t["k"], t["v"], t["do"], lowp=c["dtype"] == "bf16", d_exact=bool(c["nb"]), **t["how"])
+    for n in got:
+        R.check(n, got[n], *want[n])

@@ -78,6 +78,21 @@ def test_split_backward_stays_within_its_workspace(kw):
     assert b <= 8 * d.batch * d.n_heads * 8192 + (4096 << 17) + 512
 
 
+@pytest.mark.parametrize("kw", [
+    dict(dtype=B.F32, n_heads=8, n_kv_heads=1, seq_q=512, seq_k=512),
+    dict(dtype=B.F32, n_heads=4, n_kv_heads=1, seq_q=600, seq_k=600),
+    dict(dtype=B.F32, d_head=16, n_heads=16, n_kv_heads=2, seq_q=305, seq_k=305),
+    dict(dtype=B.F32, d_head=16, n_heads=16, n_kv_heads=2, seq_q=305, seq_k=305, window=100),
+    dict(dtype=B.F32, n_heads=16, n_kv_heads=1, seq_q=600, seq_k=600, window=80, sinks=3),
+    dict(d_head=128, n_heads=32, n_kv_heads=1, seq_q=768, seq_k=768),
+    dict(n_heads=8, n_kv_heads=1, seq_q=4096, seq_k=128, causal=0)])
+def test_few_key_blocks_are_split(kw):
+    """A backward of a few key blocks, each met by many query tiles, has partial sums of 16 workgroups at least."""
+    d = desc(batch=1, **kw)
+    rows = 8 * d.n_heads * d.seq_q
+    assert B.ringada_attn_plan(d, False)[1] - rows >= 16 * 4 * 2 * 32 * 64 * 4
+
+
 BASE = 1 << 20  # addresses that no call gets to
 
 
