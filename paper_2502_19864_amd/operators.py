@@ -5,7 +5,10 @@ torch supplies device memory and the stream; all compute is the library's
 (ringada_attn_forward, ringada_attn_backward, ringada_dropout of include/ringada.h).
 Every call is enqueued on the current stream of the tensors' device and can be
 captured into a HIP graph.  Tensors of another type, device or shape than documented raise
-ValueError; what the library refuses raises RingadaError."""
+ValueError; what the library refuses raises RingadaError.
+
+Nothing is recorded for autograd: the backward is a call of its own, and a tensor that
+requires a gradient is refused where autograd records (ValueError)."""
 from __future__ import annotations
 
 import ctypes
@@ -48,6 +51,15 @@ def _on(dev, call, *args):
             call(_raw_stream(i), *args)
 
 
+def _no_graph(*tensors):
+    """These calls record nothing for autograd: a tensor whose gradient it would miss is refused."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError("a tensor requires a gradient: call under torch.no_grad() (as in an autograd "
+                                 "Function) or on detached tensors, and take gradients from the backward calls")
+
+
 def _view(name, t, shape, dtype, dev):
     if t.dtype is not dtype or t.device != dev:
         raise ValueError(f"{name}: {t.dtype} on {t.device}, q is {dtype} on {dev}")
@@ -76,6 +88,7 @@ def _pack(how, *values):
 
 def _attn(q, k, v, o, lse, causal, window, sinks, scale, len_q, len_k, table, bucket):
     """The call's desc and tensors, packed; o, lse None: allocated here (lse False: none)."""
+    _no_graph(q, k, v, table)
     qs, ks, dtype, dev = q.shape, k.shape, q.dtype, q.device
     if len(qs) != 4 or len(ks) != 4:
         raise ValueError("q, k and v are [batch, rows, heads, d_head]")
@@ -134,6 +147,7 @@ def attention_backward(do, q, k, v, o, lse, *, causal=False, window=0, sinks=0, 
     if lse is None or o is None:
         raise ValueError("the backward needs the forward's o and lse")
     desc, t, _, _, dev = _attn(q, k, v, o, lse, causal, window, sinks, scale, len_q, len_k, table, bucket)
+    _no_graph(do)
     qs, ks, dtype = q.shape, k.shape, q.dtype
     if dtable is not None and table is None:
         raise ValueError("dtable without a table")
@@ -155,6 +169,7 @@ def attention_backward(do, q, k, v, o, lse, *, causal=False, window=0, sinks=0, 
 def dropout(x, p, rng, site=0, res=None, out=None):
     """res + dropout(x) (or dropout(x) alone): the backward is the same call on the gradient.  rng: int64 [2]
     on the device, {seed, offset}; x, res and out contiguous and of one shape (out may be x or res)."""
+    _no_graph(x, res)
     dtype, dev, shape = x.dtype, x.device, x.shape
     if dtype not in _DTYPES or dev.type != "cuda":
         raise ValueError(f"x: {dtype} on {dev}, expected float32 or bfloat16 on a GPU")

@@ -240,6 +240,24 @@ def test_python_front_end_refuses():
         ops.attention_backward(q, q, q, q, q, None)
 
 
+def test_python_front_end_refuses_what_autograd_would_miss():
+    import torch
+
+    from paper_2502_19864_amd import operators as ops
+    q = torch.zeros(1, 2, 3, 64)
+    leaf, rng = q.clone().requires_grad_(), torch.zeros(2, dtype=torch.int64)
+    table = torch.zeros(4, 3, requires_grad=True)
+    calls = [lambda: ops.attention_forward(leaf, q, q), lambda: ops.attention_forward(q, q, leaf),
+             lambda: ops.attention_forward(q, q, q, table=table, bucket=torch.zeros(3, dtype=torch.int32)),
+             lambda: ops.attention_backward(q, q, leaf, q, q, q), lambda: ops.dropout(leaf, 0.1, rng),
+             lambda: ops.dropout(q, 0.1, rng, res=leaf)]
+    for call in calls:
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="on cpu"):  # the next check
+            call()
+
+
 def stage_desc(**kw):
     from paper_2502_19864_amd.stage import make_desc
     from paper_2502_19864_amd.workloads import WORKLOADS
