@@ -388,13 +388,14 @@ ringada_status ringada_attn_plan(const ringada_attn_desc* desc, int32_t with_dta
                                  size_t* forward_bytes, size_t* backward_bytes);
 
 /* o = softmax(scale q k^T + bias, visible keys) v.  Outputs must not overlap inputs.
- * Workspaces are 256-byte aligned. */
+ * Workspaces are 256-byte aligned and overlap nothing else. */
 ringada_status ringada_attn_forward(void* stream, const ringada_attn_desc* desc,
                                     const ringada_attn_tensors* t, void* workspace,
                                     size_t workspace_bytes);
 
 /* Gradients of ringada_attn_forward with the same desc and tensors.  Every sum has
- * a fixed order: the same inputs give the same bits. */
+ * a fixed order: the same inputs give the same bits.  No gradient may overlap what is
+ * read or another gradient. */
 ringada_status ringada_attn_backward(void* stream, const ringada_attn_desc* desc,
                                      const ringada_attn_tensors* t, const ringada_attn_grads* g,
                                      void* workspace, size_t workspace_bytes);

@@ -53,7 +53,8 @@ static ringada_status check_view(const ringada_attn_desc& D, const char* name, c
   const uintptr_t p = reinterpret_cast<uintptr_t>(v.data);
   int64_t stride[3] = {v.batch, v.row, v.head}, n[3] = {D.batch, rows, heads};
   for (int i = 0; i < 3; ++i)
-    if (stride[i] < 0 || stride[i] >= (1ll << 40)) return fail(RINGADA_E_INVALID, "%s: stride out of range", name);
+    if (stride[i] < 0 || stride[i] >= (1ll << 40) || (n[i] > 1 && stride[i] > (1ll << 46) / (n[i] - 1)))
+      return fail(RINGADA_E_INVALID, "%s: stride out of range", name);  // 2^46 elements: no address space holds more
   if (D.dtype == RINGADA_BF16 ? ((p & 15u) || ((v.batch | v.row | v.head) & 7)) : (p & 3u))
     return fail(RINGADA_E_INVALID, "%s: bf16 views need 16-byte aligned data and strides that are multiples of 8, "
                                    "f32 views 4-byte aligned data", name);
@@ -76,14 +77,86 @@ static ringada_status check_view(const ringada_attn_desc& D, const char* name, c
   return RINGADA_OK;
 }
 
+// What a tensor takes in memory: runs of len bytes, n[i] of them every stride[i] bytes.
+struct Region {
+  const char* name;
+  uintptr_t p;
+  int64_t len, stride[3], n[3];
+};
+static Region flat(const char* name, const void* p, size_t bytes) {
+  return {name, reinterpret_cast<uintptr_t>(p), (int64_t)bytes, {0, 0, 0}, {1, 1, 1}};
+}
+static Region region(const char* name, const ringada_attn_desc& D, const ringada_view& v, int64_t rows, int64_t heads) {
+  const int64_t es = D.dtype == RINGADA_BF16 ? 2 : 4;
+  return {name, reinterpret_cast<uintptr_t>(v.data), D.d_head * es, {v.batch * es, v.row * es, v.head * es},
+          {D.batch, rows, heads}};
+}
+// Whether d + sum of c_k s_k, lo_k <= c_k <= hi_k, falls between -below and above: strides in falling order, each
+// coefficient tried where the smaller ones can still reach.  In tensors of one buffer, whose strides are
+// the same, that is two or three values a stride.
+struct Search {
+  int64_t s[6], lo[6], hi[6], rest_lo[7], rest_hi[7], below, above;
+  int n = 0, left = 1 << 16;
+  bool hit(int k, int64_t d) {
+    if (k == n) return -below < d && d < above;
+    auto floor_div = [](int64_t a, int64_t b) { return a >= 0 ? a / b : -((-a + b - 1) / b); };
+    const int64_t c0 = -floor_div(d + rest_hi[k + 1] + below - 1, s[k]);
+    const int64_t c1 = floor_div(above - 1 - d - rest_lo[k + 1], s[k]);
+    for (int64_t c = c0 > lo[k] ? c0 : lo[k]; c <= c1 && c <= hi[k] && left-- > 0; ++c)
+      if (hit(k + 1, d + c * s[k])) return true;
+    return false;
+  }
+};
+// Exact, but for tensors of different strides woven into each other beyond the search's limit
+static bool overlap(const Region& a, const Region& b) {
+  if (!a.p || !b.p || !a.len || !b.len) return false;
+  int64_t ea = a.len, eb = b.len;
+  for (int i = 0; i < 3; ++i) {
+    ea += a.stride[i] * (a.n[i] - 1);
+    eb += b.stride[i] * (b.n[i] - 1);
+  }
+  if (a.p + ea <= b.p || b.p + eb <= a.p) return false;
+  Search f;
+  f.below = b.len;
+  f.above = a.len;
+  for (int i = 0; i < 6; ++i) {  // from a's run to b's: b's strides forwards, a's back
+    const Region& r = i < 3 ? a : b;
+    const int64_t s = r.stride[i % 3], m = r.n[i % 3] - 1;
+    if (!s || !m) continue;
+    int at = 0;
+    while (at < f.n && f.s[at] > s) ++at;
+    if (at == f.n || f.s[at] != s) {
+      for (int k = f.n++; k > at; --k) {
+        f.s[k] = f.s[k - 1];
+        f.lo[k] = f.lo[k - 1];
+        f.hi[k] = f.hi[k - 1];
+      }
+      f.s[at] = s;
+      f.lo[at] = f.hi[at] = 0;
+    }
+    (i < 3 ? f.lo[at] : f.hi[at]) += i < 3 ? -m : m;
+  }
+  f.rest_lo[f.n] = f.rest_hi[f.n] = 0;
+  for (int k = f.n - 1; k >= 0; --k) {
+    f.rest_lo[k] = f.rest_lo[k + 1] + f.lo[k] * f.s[k];
+    f.rest_hi[k] = f.rest_hi[k + 1] + f.hi[k] * f.s[k];
+  }
+  return f.hit(0, (int64_t)(b.p - a.p));
+}
+// none of all[n_in .. n - 1], the outputs, may overlap an input (those before) or another output
+static ringada_status check_apart(const Region* all, int n_in, int n) {
+  for (int i = n_in; i < n; ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlap(all[i], all[j])) return fail(RINGADA_E_INVALID, "%s overlaps %s", all[i].name, all[j].name);
+  return RINGADA_OK;
+}
+
 static ringada_status fill_tensors(const ringada_attn_desc& D, const ringada_attn_tensors* t, MaskedAttnArgs& a) {
   if (!t) return fail(RINGADA_E_INVALID, "tensors is NULL");
   RG_TRY(check_view(D, "q", t->q, D.seq_q, D.n_heads, false, a.q));
   RG_TRY(check_view(D, "k", t->k, D.seq_k, D.n_kv_heads, false, a.k));
   RG_TRY(check_view(D, "v", t->v, D.seq_k, D.n_kv_heads, false, a.v));
   RG_TRY(check_view(D, "o", t->o, D.seq_q, D.n_heads, true, a.o));
-  if (t->o.data == t->q.data || t->o.data == t->k.data || t->o.data == t->v.data)
-    return fail(RINGADA_E_INVALID, "o is one of the inputs");
   if ((t->table != nullptr) != (D.n_buckets > 0) || (t->table && !t->bucket))
     return fail(RINGADA_E_INVALID, "table and bucket must be given exactly when n_buckets > 0");
   a.lse = t->lse;
@@ -93,11 +166,25 @@ static ringada_status fill_tensors(const ringada_attn_desc& D, const ringada_att
   a.bucket = t->bucket;
   return RINGADA_OK;
 }
+// what both passes read; returns how many
+static int read_regions(const ringada_attn_desc& D, const ringada_attn_tensors& t, Region* in) {
+  in[0] = region("q", D, t.q, D.seq_q, D.n_heads);
+  in[1] = region("k", D, t.k, D.seq_k, D.n_kv_heads);
+  in[2] = region("v", D, t.v, D.seq_k, D.n_kv_heads);
+  in[3] = flat("len_q", t.len_q, (size_t)D.batch * 4);
+  in[4] = flat("len_k", t.len_k, (size_t)D.batch * 4);
+  in[5] = flat("table", t.table, (size_t)D.n_buckets * D.n_heads * 4);
+  in[6] = flat("bucket", t.table ? t.bucket : nullptr, ((size_t)D.max_distance * 2 + 1) * 4);
+  return 7;
+}
 
-static ringada_status check_workspace(const void* ws, size_t have, size_t need) {
+static ringada_status check_workspace(const void* ws, size_t have, size_t need, const Region* all, int n) {
   if (have < need || (need && !ws))
     return fail(RINGADA_E_WORKSPACE, "workspace of %zu bytes, the call needs %zu", ws ? have : (size_t)0, need);
   if (need && (reinterpret_cast<uintptr_t>(ws) & 255u)) return fail(RINGADA_E_INVALID, "workspace must be 256-byte aligned");
+  const Region w = flat("workspace", ws, need);
+  for (int i = 0; i < n; ++i)
+    if (overlap(w, all[i])) return fail(RINGADA_E_INVALID, "the workspace overlaps %s", all[i].name);
   return RINGADA_OK;
 }
 
@@ -117,9 +204,14 @@ extern "C" ringada_status ringada_attn_forward(void* stream, const ringada_attn_
   RG_TRY(check_attn(desc));
   MaskedAttnArgs a = attn_sizes(*desc);
   RG_TRY(fill_tensors(*desc, t, a));
+  Region all[9];
+  const int n_in = read_regions(*desc, *t, all);
+  all[n_in] = region("o", *desc, t->o, desc->seq_q, desc->n_heads);
+  all[n_in + 1] = flat("lse", t->lse, (size_t)desc->batch * desc->n_heads * desc->seq_q * 4);
+  RG_TRY(check_apart(all, n_in, n_in + 2));
   size_t need, unused;
   masked_attn_bytes(desc->dtype, a, false, &need, &unused);
-  RG_TRY(check_workspace(workspace, workspace_bytes, need));
+  RG_TRY(check_workspace(workspace, workspace_bytes, need, all, n_in + 2));
   a.part = static_cast<float*>(workspace);
   RG_HIP(launch_masked_attn_fwd(desc->dtype, a, static_cast<hipStream_t>(stream)));
   return RINGADA_OK;
@@ -137,18 +229,22 @@ extern "C" ringada_status ringada_attn_backward(void* stream, const ringada_attn
   RG_TRY(check_view(*desc, "dq", g->dq, desc->seq_q, desc->n_heads, true, a.dq));
   RG_TRY(check_view(*desc, "dk", g->dk, desc->seq_k, desc->n_kv_heads, true, a.dk));
   RG_TRY(check_view(*desc, "dv", g->dv, desc->seq_k, desc->n_kv_heads, true, a.dv));
-  const void* outs[3] = {g->dq.data, g->dk.data, g->dv.data};
-  const void* ins[5] = {t->q.data, t->k.data, t->v.data, t->o.data, g->dout.data};
-  for (int i = 0; i < 3; ++i) {
-    for (const void* in : ins)
-      if (outs[i] == in) return fail(RINGADA_E_INVALID, "a gradient is one of the inputs");
-    if (outs[i] == outs[(i + 1) % 3]) return fail(RINGADA_E_INVALID, "two gradients are one tensor");
-  }
   if (g->dtable && !desc->n_buckets) return fail(RINGADA_E_INVALID, "dtable without a table");
   a.dtable = g->dtable;
+  const int64_t H = desc->n_heads, Hkv = desc->n_kv_heads;
+  Region all[14];
+  int n_in = read_regions(*desc, *t, all);
+  all[n_in++] = region("o", *desc, t->o, desc->seq_q, H);
+  all[n_in++] = region("dout", *desc, g->dout, desc->seq_q, H);
+  all[n_in++] = flat("lse", t->lse, (size_t)desc->batch * H * desc->seq_q * 4);
+  all[n_in] = region("dq", *desc, g->dq, desc->seq_q, H);
+  all[n_in + 1] = region("dk", *desc, g->dk, desc->seq_k, Hkv);
+  all[n_in + 2] = region("dv", *desc, g->dv, desc->seq_k, Hkv);
+  all[n_in + 3] = flat("dtable", g->dtable, (size_t)desc->n_buckets * H * 4);
+  RG_TRY(check_apart(all, n_in, n_in + 4));
   size_t need, unused;
   masked_attn_bytes(desc->dtype, a, g->dtable != nullptr, &unused, &need);
-  RG_TRY(check_workspace(workspace, workspace_bytes, need));
+  RG_TRY(check_workspace(workspace, workspace_bytes, need, all, n_in + 4));
   masked_attn_workspace(desc->dtype, a, workspace);
   RG_HIP(launch_masked_attn_bwd(desc->dtype, a, static_cast<hipStream_t>(stream)));
   return RINGADA_OK;

@@ -164,6 +164,124 @@ def test_workspaces_are_checked():
         B.RINGADA_E_INVALID
 
 
+def dec(**kw):
+    """A call whose forward needs a workspace: without one it gets past the checks of its tensors, and no further."""
+    return desc(batch=1, seq_q=1, seq_k=4096, **kw)
+
+
+def packed(at, heads, first=0, width=8, rows=4096, off=0):
+    """Heads first .. of a [1, rows, width, 64] buffer."""
+    return B.View(BASE * at + 2 * (64 * first + off), rows * width * 64, width * 64, 64)
+
+
+def decode(**kw):
+    t = dict(q=packed(1, 4, rows=1), k=packed(8, 2, 4), v=packed(8, 2, 6), o=packed(2, 4, rows=1), lse=BASE * 5)
+    t.update(kw)
+    return B.AttnTensors(**t)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(),
+    dict(o=packed(8, 4)),                                    # the first four heads of the keys' and values' buffer
+    dict(o=packed(8, 4, off=8 * 64 * 4095)),                 # of its last row
+    dict(q=packed(1, 4, 0, 8), o=packed(1, 4, 4, 8)),        # side by side in one row
+    dict(lse=BASE * 8 + 2 * 64 * 8 * 4096),                  # right behind the keys' buffer
+    dict(lse=BASE * 8),                                      # in a hole of it
+])
+def test_tensors_woven_into_each_other_are_taken(kw):
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_forward(None, dec(), decode(**kw), BASE * 100, 0)
+    assert e.value.status == B.RINGADA_E_WORKSPACE, str(e.value)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(o=packed(8, 4, 1)),                                 # its last head is k's first, in the first row
+    dict(o=packed(8, 4, 2, off=8 * 64 * 4095)),              # and in the last
+    dict(o=packed(1, 4, 3, rows=1)),                         # the last head of q
+    dict(o=B.View(BASE * 1 + 16, 256, 256, 64)),             # q, 16 bytes on
+    dict(lse=BASE * 2 + 4 * 64 * 2 - 8),                     # the end of o
+    dict(lse=BASE * 8 + 2 * 64 * 6),                         # v's first row
+    dict(len_k=BASE * 5 + 12),                               # lse's last entry
+])
+def test_partly_overlapping_tensors_are_refused(kw):
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_forward(None, dec(), decode(**kw), BASE * 100, 0)
+    assert e.value.status == B.RINGADA_E_INVALID and "overlaps" in str(e.value)
+
+
+@pytest.mark.parametrize("kw,gkw,ok", [
+    ({}, {}, True),
+    ({}, dict(dq=packed(7, 4, 0, rows=10), dk=packed(8, 2, 4, rows=20), dv=packed(8, 2, 6, rows=20)), True),
+    ({}, dict(dk=packed(8, 2, 4, rows=20), dv=packed(8, 2, 5, rows=20)), False),    # one head of two gradients
+    ({}, dict(dk=B.View(BASE * 8, 2560, 128, 64), dv=B.View(BASE * 8 + 2560, 2560, 128, 64)), False),
+    ({}, dict(dk=B.View(BASE * 8, 5120, 128, 64), dv=B.View(BASE * 8 + 5120, 5120, 128, 64)), True),  # batch by batch
+    ({}, dict(dq=B.View(BASE * 6 + 2 * 64, 2560, 256, 64)), False),                 # dout, a head on
+    ({}, dict(dv=B.View(BASE * 5 - 2 * 64, 2560, 128, 64)), False),                 # into lse
+    (dict(len_q=BASE * 8 + 16), {}, False),
+])
+def test_gradients_overlap_nothing(kw, gkw, ok):
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_backward(None, desc(), tensors(**kw), grads(**gkw), BASE * 12, 0)
+    assert e.value.status == (B.RINGADA_E_WORKSPACE if ok else B.RINGADA_E_INVALID), str(e.value)
+
+
+def test_overlaps_against_the_addresses_themselves():
+    """Small random views of one stretch of memory: dq refused exactly where it shares an element with q."""
+    import itertools
+    import random
+
+    rng = random.Random(5)
+    met = 0
+    for _ in range(600):
+        b, h, sq, dh = (rng.randint(1, 3) for _ in range(4))
+        d = desc(dtype=B.F32, batch=b, n_heads=h, n_kv_heads=h, d_head=dh, seq_q=sq, seq_k=sq)
+
+        def some():
+            out, extent = {}, dh
+            for name, n in rng.sample([("batch", b), ("row", sq), ("head", h)], 3):  # nested, with gaps
+                out[name] = extent + rng.randint(0, 4)
+                extent += out[name] * (n - 1)
+            return out, extent
+
+        (sq_, eq), (sd, ed) = some(), some()
+        if rng.random() < 0.5:  # slices of one tensor
+            sd, ed = sq_, eq
+        at = rng.randint(-ed, eq)
+        el = lambda s, o: {o + i * s["batch"] + j * s["row"] + k * s["head"] + x for i, j, k, x in
+                           itertools.product(range(b), range(sq), range(h), range(dh))}
+        far = lambda i: B.View(BASE * i, 1000, 100, 10)
+        q, dq = B.View(BASE * 30, sq_["batch"], sq_["row"], sq_["head"]), \
+            B.View(BASE * 30 + 4 * at, sd["batch"], sd["row"], sd["head"])
+        with pytest.raises(B.RingadaError) as e:
+            B.ringada_attn_backward(None, d, B.AttnTensors(q=q, k=far(2), v=far(3), o=far(4), lse=BASE * 5),
+                                    B.AttnGrads(dout=far(6), dq=dq, dk=far(8), dv=far(9)), BASE * 12, 0)
+        meet = bool(el(sq_, 0) & el(sd, at))
+        assert e.value.status == (B.RINGADA_E_INVALID if meet else B.RINGADA_E_WORKSPACE), str(e.value)
+        met += meet
+    assert 100 < met < 500
+
+
+def test_the_table_and_the_workspace_overlap_nothing():
+    d = desc(n_buckets=4, max_distance=3)
+    _, n = B.ringada_attn_plan(d, True)
+    t = dict(table=BASE * 10, bucket=BASE * 11)
+    for kw, gkw, ws, have in ((t, dict(dtable=BASE * 10 + 60), BASE * 12, 0), (t, dict(dtable=BASE * 11 + 24), BASE * 12, 0),
+                              (t, dict(dtable=BASE * 13), BASE * 10 - n + 256, n),
+                              (t, dict(dtable=BASE * 13), BASE * 9 + 256, n)):
+        with pytest.raises(B.RingadaError) as e:
+            B.ringada_attn_backward(None, d, tensors(**kw), grads(**gkw), ws, have)
+        assert e.value.status == B.RINGADA_E_INVALID and "overlaps" in str(e.value)
+
+
+def test_strides_beyond_any_memory_are_refused():
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_forward(None, dec(), decode(k=B.View(BASE * 8, 0, 512, 1 << 39), v=packed(9, 2)), BASE * 100, 0)
+    assert e.value.status == B.RINGADA_E_WORKSPACE  # 2^39 elements on, but within 2^46
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_backward(None, desc(batch=200), tensors(q=B.View(BASE * 1, 1 << 39, 256, 64)), grads(), BASE * 12, 0)
+    assert e.value.status == B.RINGADA_E_INVALID
+
+
 @pytest.mark.parametrize("kw", [
     dict(dtype=3), dict(x=None), dict(y=None), dict(rng=None), dict(n=0), dict(n=(1 << 35) + 1), dict(p=-0.1),
     dict(p=1.0), dict(p=float("nan")), dict(p=0.999999), dict(y=BASE + 16), dict(res=BASE * 3 + 4), dict(x=BASE + 1),
