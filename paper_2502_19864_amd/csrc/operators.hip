@@ -52,13 +52,16 @@ static ringada_status check_view(const ringada_attn_desc& D, const char* name, c
   if (!v.data) return fail(RINGADA_E_INVALID, "%s is NULL", name);
   const uintptr_t p = reinterpret_cast<uintptr_t>(v.data);
   int64_t stride[3] = {v.batch, v.row, v.head}, n[3] = {D.batch, rows, heads};
-  for (int i = 0; i < 3; ++i)
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] == 1) stride[i] = 0;  // whatever it is, it leads nowhere
     if (stride[i] < 0 || stride[i] >= (1ll << 40) || (n[i] > 1 && stride[i] > (1ll << 46) / (n[i] - 1)))
       return fail(RINGADA_E_INVALID, "%s: stride out of range", name);  // 2^46 elements: no address space holds more
-  if (D.dtype == RINGADA_BF16 ? ((p & 15u) || ((v.batch | v.row | v.head) & 7)) : (p & 3u))
+  }
+  out = View{v.data, (long)stride[0], (long)stride[1], (long)stride[2]};
+  if (D.dtype == RINGADA_BF16 ? ((p & 15u) || ((stride[0] | stride[1] | stride[2]) & 7)) : (p & 3u))
     return fail(RINGADA_E_INVALID, "%s: bf16 views need 16-byte aligned data and strides that are multiples of 8, "
                                    "f32 views 4-byte aligned data", name);
-  if (v.row >= (1 << 24)) return fail(RINGADA_E_UNSUPPORTED, "%s: row stride above 2^24 elements", name);
+  if (stride[1] >= (1 << 24)) return fail(RINGADA_E_UNSUPPORTED, "%s: row stride above 2^24 elements", name);
   if (writes) {
     for (int i = 0; i < 2; ++i)  // by stride, smallest first
       for (int j = 0; j < 2 - i; ++j)
@@ -73,7 +76,6 @@ static ringada_status check_view(const ringada_attn_desc& D, const char* name, c
       extent = stride[i] * (n[i] - 1) + extent;
     }
   }
-  out = View{v.data, (long)v.batch, (long)v.row, (long)v.head};
   return RINGADA_OK;
 }
 
@@ -86,10 +88,9 @@ struct Region {
 static Region flat(const char* name, const void* p, size_t bytes) {
   return {name, reinterpret_cast<uintptr_t>(p), (int64_t)bytes, {0, 0, 0}, {1, 1, 1}};
 }
-static Region region(const char* name, const ringada_attn_desc& D, const ringada_view& v, int64_t rows, int64_t heads) {
+static Region region(const char* name, const ringada_attn_desc& D, const View& v, int64_t rows, int64_t heads) {
   const int64_t es = D.dtype == RINGADA_BF16 ? 2 : 4;
-  return {name, reinterpret_cast<uintptr_t>(v.data), D.d_head * es, {v.batch * es, v.row * es, v.head * es},
-          {D.batch, rows, heads}};
+  return {name, reinterpret_cast<uintptr_t>(v.p), D.d_head * es, {v.b * es, v.t * es, v.h * es}, {D.batch, rows, heads}};
 }
 // Whether d + sum of c_k s_k, lo_k <= c_k <= hi_k, falls between -below and above: strides in falling order, each
 // coefficient tried where the smaller ones can still reach.  In tensors of one buffer, whose strides are
@@ -167,14 +168,14 @@ static ringada_status fill_tensors(const ringada_attn_desc& D, const ringada_att
   return RINGADA_OK;
 }
 // what both passes read; returns how many
-static int read_regions(const ringada_attn_desc& D, const ringada_attn_tensors& t, Region* in) {
-  in[0] = region("q", D, t.q, D.seq_q, D.n_heads);
-  in[1] = region("k", D, t.k, D.seq_k, D.n_kv_heads);
-  in[2] = region("v", D, t.v, D.seq_k, D.n_kv_heads);
-  in[3] = flat("len_q", t.len_q, (size_t)D.batch * 4);
-  in[4] = flat("len_k", t.len_k, (size_t)D.batch * 4);
-  in[5] = flat("table", t.table, (size_t)D.n_buckets * D.n_heads * 4);
-  in[6] = flat("bucket", t.table ? t.bucket : nullptr, ((size_t)D.max_distance * 2 + 1) * 4);
+static int read_regions(const ringada_attn_desc& D, const MaskedAttnArgs& a, Region* in) {
+  in[0] = region("q", D, a.q, D.seq_q, D.n_heads);
+  in[1] = region("k", D, a.k, D.seq_k, D.n_kv_heads);
+  in[2] = region("v", D, a.v, D.seq_k, D.n_kv_heads);
+  in[3] = flat("len_q", a.len_q, (size_t)D.batch * 4);
+  in[4] = flat("len_k", a.len_k, (size_t)D.batch * 4);
+  in[5] = flat("table", a.table, (size_t)D.n_buckets * D.n_heads * 4);
+  in[6] = flat("bucket", a.table ? a.bucket : nullptr, ((size_t)D.max_distance * 2 + 1) * 4);
   return 7;
 }
 
@@ -205,8 +206,8 @@ extern "C" ringada_status ringada_attn_forward(void* stream, const ringada_attn_
   MaskedAttnArgs a = attn_sizes(*desc);
   RG_TRY(fill_tensors(*desc, t, a));
   Region all[9];
-  const int n_in = read_regions(*desc, *t, all);
-  all[n_in] = region("o", *desc, t->o, desc->seq_q, desc->n_heads);
+  const int n_in = read_regions(*desc, a, all);
+  all[n_in] = region("o", *desc, a.o, desc->seq_q, desc->n_heads);
   all[n_in + 1] = flat("lse", t->lse, (size_t)desc->batch * desc->n_heads * desc->seq_q * 4);
   RG_TRY(check_apart(all, n_in, n_in + 2));
   size_t need, unused;
@@ -233,13 +234,13 @@ extern "C" ringada_status ringada_attn_backward(void* stream, const ringada_attn
   a.dtable = g->dtable;
   const int64_t H = desc->n_heads, Hkv = desc->n_kv_heads;
   Region all[14];
-  int n_in = read_regions(*desc, *t, all);
-  all[n_in++] = region("o", *desc, t->o, desc->seq_q, H);
-  all[n_in++] = region("dout", *desc, g->dout, desc->seq_q, H);
+  int n_in = read_regions(*desc, a, all);
+  all[n_in++] = region("o", *desc, a.o, desc->seq_q, H);
+  all[n_in++] = region("dout", *desc, a.dout, desc->seq_q, H);
   all[n_in++] = flat("lse", t->lse, (size_t)desc->batch * H * desc->seq_q * 4);
-  all[n_in] = region("dq", *desc, g->dq, desc->seq_q, H);
-  all[n_in + 1] = region("dk", *desc, g->dk, desc->seq_k, Hkv);
-  all[n_in + 2] = region("dv", *desc, g->dv, desc->seq_k, Hkv);
+  all[n_in] = region("dq", *desc, a.dq, desc->seq_q, H);
+  all[n_in + 1] = region("dk", *desc, a.dk, desc->seq_k, Hkv);
+  all[n_in + 2] = region("dv", *desc, a.dv, desc->seq_k, Hkv);
   all[n_in + 3] = flat("dtable", g->dtable, (size_t)desc->n_buckets * H * 4);
   RG_TRY(check_apart(all, n_in, n_in + 4));
   size_t need, unused;

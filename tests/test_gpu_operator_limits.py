@@ -64,3 +64,24 @@ def test_few_key_blocks_met_by_many_query_tiles(c):
     want = R.attention(t["q"], t["k"], t["v"], t["do"], lowp=c["dtype"] == "bf16", d_exact=bool(c["nb"]), **t["how"])
     for n in got:
         R.check(n, got[n], *want[n])
+
+
+@pytest.mark.parametrize("B,Sq,Sk,H", [(1, 1, 700, 4), (1, 90, 90, 1), (3, 1, 1, 2), (1, 1, 1, 1)])
+def test_any_stride_of_a_single_entry(B, Sq, Sk, H):
+    """Dimensions of one entry have the strides that torch happens to give them."""
+    import torch
+
+    from paper_2502_19864_amd import operators as ops
+
+    def odd(x):
+        return x.as_strided(x.shape, [s if n > 1 else 13 + (1 << 30) for n, s in zip(x.shape[:3], x.stride())] + [1])
+
+    g = torch.Generator().manual_seed(2)
+    q, do, k, v = (torch.randn(B, S, H, 64, generator=g).bfloat16().cuda() for S in (Sq, Sq, Sk, Sk))
+    o, lse = ops.attention_forward(q, k, v, causal=True)
+    grads = ops.attention_backward(do, q, k, v, o, lse, causal=True)
+    outs = [odd(torch.empty_like(x)) for x in (q, q, k, v)]
+    o2, lse2 = ops.attention_forward(odd(q), odd(k), odd(v), causal=True, out=outs[0])
+    ops.attention_backward(odd(do), odd(q), odd(k), odd(v), o2, lse2, causal=True, dq=outs[1], dk=outs[2], dv=outs[3])
+    for a, b in zip((o, lse) + grads, (o2, lse2) + tuple(outs[1:])):
+        assert torch.equal(a, b)

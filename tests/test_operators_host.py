@@ -273,6 +273,14 @@ def test_the_table_and_the_workspace_overlap_nothing():
         assert e.value.status == B.RINGADA_E_INVALID and "overlaps" in str(e.value)
 
 
+def test_strides_of_single_entries_do_not_count():
+    """A dimension of one entry may have any stride, as torch gives it."""
+    one = dict(q=B.View(BASE, -5, 3, 64), k=B.View(BASE * 8, 1 << 50, 512, 64), o=B.View(BASE * 2, 0, 1 << 30, 64))
+    with pytest.raises(B.RingadaError) as e:
+        B.ringada_attn_forward(None, dec(), decode(**one), BASE * 100, 0)
+    assert e.value.status == B.RINGADA_E_WORKSPACE, str(e.value)
+
+
 def test_strides_beyond_any_memory_are_refused():
     with pytest.raises(B.RingadaError) as e:
         B.ringada_attn_forward(None, dec(), decode(k=B.View(BASE * 8, 0, 512, 1 << 39), v=packed(9, 2)), BASE * 100, 0)
