@@ -148,6 +148,13 @@ def _ref(x):
     return x if type(x) is bytes else byref(x)
 
 
+def _in(name, x, low, bits):
+    """x, an integer from low to 2^bits - 1: ctypes would cut others to their low bits."""
+    if not low <= x < 1 << bits:
+        raise ValueError(f"{name}: {x} is out of range")
+    return x
+
+
 def ringada_stage_plan(desc, batch, seq, lowest_unfrozen):
     st, sc = c_size_t(0), c_size_t(0)
     _check(lib().ringada_stage_plan(byref(desc), batch, seq, lowest_unfrozen, byref(st), byref(sc)))
@@ -197,7 +204,7 @@ def ringada_stage_set_attention(stage, opt):
 
 
 def ringada_stage_set_dropout(stage, p, rng, first_site):
-    _check(lib().ringada_stage_set_dropout(stage, p, _p(rng), first_site))
+    _check(lib().ringada_stage_set_dropout(stage, p, _p(rng), _in("first_site", first_site, 0, 32)))
 
 
 def ringada_stage_forward(stage, stream, x, y, batch, seq, lowest_unfrozen, stash, stash_bytes, scratch,
@@ -244,13 +251,16 @@ def ringada_attn_backward(stream, desc, tensors, grads, workspace, workspace_byt
 
 def ringada_relpos_buckets(n_buckets, max_distance, bidirectional):
     """The map as a list of 2 max_distance + 1 ints, indexed by key - query + max_distance."""
+    _in("n_buckets", n_buckets, -1 << 31, 31)
+    _in("max_distance", max_distance, -1 << 31, 16)  # the library takes 1024
     m = (c_int32 * max(1, 2 * max_distance + 1))()
     _check(lib().ringada_relpos_buckets(n_buckets, max_distance, int(bidirectional), m))
     return list(m)
 
 
 def ringada_dropout(stream, dtype, x, res, y, n, p, rng, site):
-    _check(lib().ringada_dropout(stream, dtype, _p(x), _p(res), _p(y), n, p, _p(rng), site))
+    _check(lib().ringada_dropout(stream, dtype, _p(x), _p(res), _p(y), _in("n", n, -1 << 63, 63), p, _p(rng),
+                                 _in("site", site, 0, 32)))
 
 
 def ringada_last_error():

@@ -126,7 +126,7 @@ class Stage:
                 if t is not None and (t.dtype != dt or tuple(t.shape) != shape or t.device != self.dev
                                       or not t.is_contiguous()):
                     raise ValueError(f"{name}: expected a contiguous {dt} tensor of shape {shape} on {self.dev}")
-        opt = B.StageAttention(window, sinks, nb, r, B._p(table), B._p(bucket), B._p(g_table), None, 0)
+        opt = B.StageAttention(B._in("window", window, -1 << 31, 31), B._in("sinks", sinks, -1 << 31, 31), nb, r, B._p(table), B._p(bucket), B._p(g_table), None, 0)
         B.ringada_stage_set_attention(self.handle, opt)
         self.attention = (opt, table, bucket, g_table, None) if window or nb else None
 

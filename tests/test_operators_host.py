@@ -281,6 +281,25 @@ def test_strides_of_single_entries_do_not_count():
     assert e.value.status == B.RINGADA_E_WORKSPACE, str(e.value)
 
 
+def test_numbers_out_of_range_are_refused():
+    """ctypes alone would cut them to their low bits."""
+    import torch
+
+    from paper_2502_19864_amd import operators as ops
+    from paper_2502_19864_amd.stage import Stage
+    st = object.__new__(Stage)  # the numbers are looked at before the handle is
+    st.torch, st.handle, st.dev = torch, None, torch.device("cpu")
+    st.w = type("W", (), dict(n_heads=2))
+    for call in (lambda: st.set_attention(window=1 << 32), lambda: st.set_attention(window=4, sinks=(1 << 32) + 1),
+                 lambda: st.set_dropout(0.1, None, 1 << 32), lambda: st.set_dropout(0.1, None, -1),
+                 lambda: ops.relpos_buckets((1 << 32) + 32, 128, True),
+                 lambda: ops.relpos_buckets(32, (1 << 32) + 128, True),
+                 lambda: B.ringada_dropout(None, B.BF16, BASE, None, BASE * 3, 1000, 0.0, BASE * 9 + 1, 1 << 32),
+                 lambda: B.ringada_dropout(None, B.BF16, BASE, None, BASE * 3, (1 << 64) + 8, 0.0, BASE * 9 + 1, 0)):
+        with pytest.raises(ValueError):
+            call()
+
+
 def test_strides_beyond_any_memory_are_refused():
     with pytest.raises(B.RingadaError) as e:
         B.ringada_attn_forward(None, dec(), decode(k=B.View(BASE * 8, 0, 512, 1 << 39), v=packed(9, 2)), BASE * 100, 0)
