@@ -659,12 +659,13 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
   }
   tiles_ready();  // the tiles' space now takes the O rows
   if (q0 >= a.Sq) return;
-  const float inv = qv && lrun > 0.f ? 1.f / lrun : 0.f;
+  const bool sees = qv && lrun != 0.f;  // a sum that is NaN stays one
+  const float inv = sees ? 1.f / lrun : 0.f;
   O::store(oacc, inv, lane, sm + wave * O::STAGE,
            static_cast<E*>(a.o.p) + b * a.o.b + (long)q0 * a.o.t + h * a.o.h, a.o.t,
            stream_out((long)a.B * a.Sq * a.H * DH * (long)sizeof(E)), a.Sq - q0, a.dh);
   if (a.lse && q < a.Sq && half == 0)
-    a.lse[(long)bh * a.Sq + q] = qv && lrun > 0.f ? mrun + log2f(lrun) : -INFINITY;
+    a.lse[(long)bh * a.Sq + q] = sees ? mrun + log2f(lrun) : -INFINITY;
 }
 
 // ================================================================ a few queries, many keys
@@ -814,7 +815,8 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
     L = fmaf(sS[k][l32], f[k], L);
   }
   if (tok >= a.Sq) return;
-  const float inv = L > 0.f ? 1.f / L : 0.f;
+  if (!qv) L = 0.f;
+  const float inv = L != 0.f ? 1.f / L : 0.f;
   float* po = a.part + ((long)blk * 32 + l32) * DH;
   E* o = static_cast<E*>(a.o.p) + b * a.o.b + (long)tok * a.o.t + h * a.o.h;
   for (int d = wave; d < DH / 32; d += NW)
@@ -840,7 +842,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
     }
   if (wave == 0 && half == 0) {
     if (w.split > 1) reinterpret_cast<float2*>(a.part + (long)gridDim.x * 32 * DH)[(long)blk * 32 + l32] = make_float2(M, L);
-    else if (a.lse) a.lse[((long)b * a.H + h) * a.Sq + tok] = L > 0.f ? M + log2f(L) : -INFINITY;
+    else if (a.lse) a.lse[((long)b * a.H + h) * a.Sq + tok] = L != 0.f ? M + log2f(L) : -INFINITY;
   }
 }
 
@@ -879,8 +881,8 @@ __global__ __launch_bounds__(256) void attn_few_join(MaskedAttnArgs a, FewWork w
   E* o = static_cast<E*>(a.o.p) + b * a.o.b + (long)tok * a.o.t + h * a.o.h;
 #pragma unroll
   for (int d = 0; d < DH / 64; ++d)
-    if (lane + 64 * d < a.dh) St<E>::st(o, lane + 64 * d, L > 0.f ? acc[d] / L : 0.f);
-  if (a.lse && lane == 0) a.lse[((long)b * a.H + h) * a.Sq + tok] = L > 0.f ? M + log2f(L) : -INFINITY;
+    if (lane + 64 * d < a.dh) St<E>::st(o, lane + 64 * d, L != 0.f ? acc[d] / L : 0.f);
+  if (a.lse && lane == 0) a.lse[((long)b * a.H + h) * a.Sq + tok] = L != 0.f ? M + log2f(L) : -INFINITY;
 }
 
 // ================================================================ backward

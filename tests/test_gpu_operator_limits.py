@@ -85,3 +85,25 @@ def test_any_stride_of_a_single_entry(B, Sq, Sk, H):
     ops.attention_backward(odd(do), odd(q), odd(k), odd(v), o2, lse2, causal=True, dq=outs[1], dk=outs[2], dv=outs[3])
     for a, b in zip((o, lse) + grads, (o2, lse2) + tuple(outs[1:])):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("c", [T("bf16", 8, 2, 128, 1, 3000, causal=True), T("f32", 4, 2, 40, 3, 2000, causal=True, nb=8, dist=20),
+                               T("bf16", 4, 2, 64, 100, 100), T("f32", 2, 2, 100, 60, 60, causal=True),
+                               T("bf16", 64, 32, 64, 300, 300, causal=True, window=90, sinks=3),
+                               T("bf16", 32, 32, 128, 270, 270, causal=True, nb=16, dist=30)], ids=str)
+def test_a_nan_among_the_visible_keys_is_not_lost(c):
+    """Rows that see a key of NaN are NaN, in lse too, whichever kernels they take; the others are as they were."""
+    import torch
+    from paper_2502_19864_amd import operators as ops
+    from test_gpu_operators import make
+
+    t = make(c)
+    o, lse = ops.attention_forward(t["q"], t["k"], t["v"], **t["how"])
+    k = t["k"].clone()
+    k[:, c["Sk"] - 1] = float("nan")
+    o2, lse2 = ops.attention_forward(t["q"], k, t["v"], **t["how"])
+    hit = torch.ones(c["Sq"], dtype=torch.bool, device="cuda")
+    if c["causal"]:  # the last key is its own query's alone
+        hit[:-1] = False
+    assert torch.isnan(o2[:, hit]).all() and torch.isnan(lse2[:, :, hit]).all()
+    assert torch.equal(o2[:, ~hit], o[:, ~hit]) and torch.equal(lse2[:, :, ~hit], lse[:, :, ~hit])
