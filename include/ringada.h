@@ -362,7 +362,8 @@ typedef struct {
  * cache).  With table, bucket[clamp(j - p, -R, R) + R] names the table row whose
  * entry for the head is added to the score.  A row that sees nothing, and one at or past
  * its length, gives zeros (and lse -inf).  Rows of k, v and gradients at or past the
- * lengths are not read into any result, whatever they hold. */
+ * lengths are not read into any result, whatever they hold.  An infinity or NaN within the
+ * lengths of v or dout may reach rows of its sequence that do not see it (0 times it). */
 typedef struct {
   ringada_view q, k, v;   /* [batch, seq_q, n_heads, d_head]; [batch, seq_k, n_kv_heads, d_head] */
   ringada_view o;         /* as q: written by the forward, read by the backward */

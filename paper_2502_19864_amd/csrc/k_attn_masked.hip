@@ -534,6 +534,16 @@ __device__ __forceinline__ void add_diag(const f32x16& ds, int base, int R, floa
   }
 }
 
+// Rows that see nothing, or lie past the lengths, are zeros whatever the others hold: their products with
+// weights of zero are NaN where a tile has infinities.
+template <int N>
+__device__ __forceinline__ void clear_if(bool dead, f32x16 (&acc)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[i][r] = dead ? 0.f : acc[i][r];
+}
+
 // ================================================================ forward
 // The running maximum (base 2) moves only when some row's new one is more than 8 above it:
 // until then P is at most 2^8, which costs fp32 sums and bf16 products nothing, and the
@@ -660,7 +670,8 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_fwd(MaskedAttnA
   tiles_ready();  // the tiles' space now takes the O rows
   if (q0 >= a.Sq) return;
   const bool sees = qv && lrun != 0.f;  // a sum that is NaN stays one
-  const float inv = sees ? 1.f / lrun : 0.f;
+  const float inv = 1.f / (sees ? lrun : 1.f);
+  clear_if(!sees, oacc);
   O::store(oacc, inv, lane, sm + wave * O::STAGE,
            static_cast<E*>(a.o.p) + b * a.o.b + (long)q0 * a.o.t + h * a.o.h, a.o.t,
            stream_out((long)a.B * a.Sq * a.H * DH * (long)sizeof(E)), a.Sq - q0, a.dh);
@@ -816,7 +827,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
   }
   if (tok >= a.Sq) return;
   if (!qv) L = 0.f;
-  const float inv = L != 0.f ? 1.f / L : 0.f;
+  const float inv = 1.f / L;
   float* po = a.part + ((long)blk * 32 + l32) * DH;
   E* o = static_cast<E*>(a.o.p) + b * a.o.b + (long)tok * a.o.t + h * a.o.h;
   for (int d = wave; d < DH / 32; d += NW)
@@ -837,7 +848,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_fwd(MaskedAttnArgs a, Few
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (c + e < a.dh) St<E>::st(o, c + e, v[e] * inv);
+          if (c + e < a.dh) St<E>::st(o, c + e, L != 0.f ? v[e] * inv : 0.f);
       }
     }
   if (wave == 0 && half == 0) {
@@ -1067,6 +1078,9 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
 #pragma unroll
     for (int r = 0; r < 16; ++r) dq[i][r] = 0.f;
   sweep(std::false_type{}, DTAB ? __builtin_amdgcn_readfirstlane(kt.n) : 0);
+  const bool dead = lse == INFINITY;  // nothing visible, or past the length
+  if (dead) dsum = 0.f;
+  clear_if(dead, dq);
   // the row statistics that the dK/dV pass reads
   if (q < a.Sq && half == 0) a.stat[(long)bh * a.Sq + q] = make_float2(lse, dsum);
   if (DTAB) close_diag(diag, W, dlo, dhi, lane);
@@ -1189,6 +1203,8 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_dq(MaskedAttnArgs a) {
       for (int k = 0; k < NW; ++k) dsum += sD[k][l32];
     }
   }
+  const bool dead = lse == INFINITY;
+  if (dead) dsum = 0.f;
   if (wave == 0 && half == 0 && q < a.Sq) a.stat[(long)bh * a.Sq + q] = make_float2(lse, dsum);
   if (DTAB) close_diag(diag, W, dlo, dhi, lane);
   float4* so = reinterpret_cast<float4*>(tiles) + lane;
@@ -1214,6 +1230,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_dq(MaskedAttnArgs a) {
         dq[d][4 * g + 2] += x.z;
         dq[d][4 * g + 3] += x.w;
       }
+  clear_if(dead, dq);
   O::rotate_back(dq, a.rope_tab, min(q, a.Sq - 1), half);
   O::store(dq, a.scale, lane, sm[0], static_cast<E*>(a.dq.p) + b * a.dq.b + (long)q0 * a.dq.t + h * a.dq.h, a.dq.t, false,
            a.Sq - q0, a.dh);
@@ -1410,6 +1427,8 @@ __global__ __launch_bounds__(64 * NW, O::DH == 64 && O::KR == 64 && !BIAS ? 3 : 
   }
   tiles_ready();  // the tiles' space now takes the dK, then the dV rows
   if (k0 >= a.Sk) return;
+  clear_if(!kv, dk);
+  clear_if(!kv, dv);
   E* stage = sm + wave * O::STAGE;
   const bool nt_out = stream_out((long)a.B * a.Sk * a.Hkv * DH * (long)sizeof(E));
   O::rotate_back(dk, a.rope_tab, min(key, a.Sk - 1), half);
@@ -1473,6 +1492,9 @@ __global__ __launch_bounds__(256) void attn_masked_dkdv_join(MaskedAttnArgs a, K
       acc[i].z += v.z;
       acc[i].w += v.w;
     }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (key >= sq.lk) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);  // as clear_if
   const View& o = is_v ? a.dv : a.dk;
   E* dst = static_cast<E*>(o.p) + b * o.b + (long)key * o.t + hk * o.h;
 #pragma unroll
@@ -1595,6 +1617,8 @@ __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 
       }
     }
   }
+  if (lse == INFINITY) dsum = 0.f;
+  clear_if(lse == INFINITY, dq);
   if (q < ROWS && half == 0) sS[q] = make_float2(lse, dsum);
   if (DTAB) close_diag(diag, W, dlo, dhi, lane);
   __syncthreads();
@@ -1624,6 +1648,8 @@ __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 
       ops.accum(dk, sQ + t, qb, dp);
     }
   }
+  clear_if(key >= sq.lk, dk);
+  clear_if(key >= sq.lk, dv);
   __syncthreads();  // the tiles' space now takes the rows on their way out
   E* stage = sm + wave * O::STAGE;
   const bool nt = stream_out((long)a.B * max(a.Sq, a.Sk) * a.H * DH * (long)sizeof(E));

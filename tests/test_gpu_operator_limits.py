@@ -107,3 +107,35 @@ def test_a_nan_among_the_visible_keys_is_not_lost(c):
         hit[:-1] = False
     assert torch.isnan(o2[:, hit]).all() and torch.isnan(lse2[:, :, hit]).all()
     assert torch.equal(o2[:, ~hit], o[:, ~hit]) and torch.equal(lse2[:, :, ~hit], lse[:, :, ~hit])
+
+
+@pytest.mark.parametrize("dtype,dh,H,Hkv,S,nb,window", [
+    ("bf16", 64, 2, 2, 100, 0, 0), ("bf16", 128, 2, 2, 100, 16, 0), ("f32", 40, 2, 2, 100, 16, 0), ("f32", 100, 2, 2, 60, 0, 0),
+    ("bf16", 64, 4, 2, 200, 0, 70), ("bf16", 128, 4, 2, 200, 16, 70), ("f32", 40, 4, 2, 200, 16, 0), ("f32", 100, 4, 1, 100, 0, 0),
+    ("bf16", 64, 32, 8, 900, 16, 70), ("bf16", 128, 32, 8, 900, 0, 70), ("bf16", 128, 32, 8, 900, 16, 0), ("f32", 40, 32, 8, 900, 0, 70)])
+def test_zeros_stay_zeros_beside_infinities(dtype, dh, H, Hkv, S, nb, window):
+    """Infinities and NaN within one sequence: its rows past the lengths and those that see nothing are zeros as
+    ever, and the other sequence is as it was."""
+    import torch
+    from test_gpu_operators import A, make, run
+
+    lq, lk = S - 9, S - 21  # the first twelve rows stand before the first key
+    c = A(dtype, 2, H, Hkv, dh, S, causal=True, window=window, sinks=2 if window else 0, nb=nb, dist=20 if nb else 0,
+          len_q=[lq, S], len_k=[lk, S])
+    t = make(c, layout="cache")
+    clean = run(t)
+    inf = float("inf")
+    t["v"][0, 3] = inf
+    t["v"][0, lk - 1, :, 1:] = float("nan")
+    t["k"][0, 7, :, 0] = -inf
+    t["do"][0, 20] = inf
+    t["do"][0, lq - 1, :, :1] = float("nan")
+    got = run(t)
+    for n in ("o", "dq"):
+        assert torch.equal(got[n][1], clean[n][1]), n
+        assert (got[n][0, :12] == 0).all() and (got[n][0, lq:] == 0).all(), n
+    for n in ("dk", "dv"):
+        assert torch.equal(got[n][1], clean[n][1]), n
+        assert (got[n][0, lk:] == 0).all(), n
+    assert (got["lse"][0, :, :12] == -inf).all() and (got["lse"][0, :, lq:] == -inf).all()
+    assert torch.equal(got["lse"][1], clean["lse"][1])
