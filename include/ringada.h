@@ -371,7 +371,8 @@ typedef struct {
                              forward (may be NULL there), read by the backward */
   const int32_t* len_q;   /* device [batch], NULL: seq_q; values are taken into [0, seq_q] */
   const int32_t* len_k;   /* device [batch], NULL: seq_k; values are taken into [0, seq_k] */
-  const float* table;     /* device [n_buckets, n_heads]; an entry of -1e30 or less hides its bucket */
+  const float* table;     /* device [n_buckets, n_heads]; an entry of -1e30 or less hides its bucket.  Scores
+                             are held in fp32: beside an entry of 1e6 they are good to 1/16 */
   const int32_t* bucket;  /* device [2 R + 1], values taken into [0, n_buckets) */
 } ringada_attn_tensors;
 

@@ -900,6 +900,26 @@ __global__ __launch_bounds__(256) void attn_few_join(MaskedAttnArgs a, FewWork w
 // exponent offset of a row that sees nothing: exp2(x - inf) = 0
 __device__ __forceinline__ float lse_or_inf(float l) { return l == -INFINITY ? INFINITY : l; }
 
+// An lse is off by half its last digit, and P = exp2(x - lse) by that factor: 2^-18 at 128, but with entries of
+// -1e9 in all that a row sees its whole logarithm of the sum is lost, and P no longer sums to one.  Where a block
+// of 32 rows has one beyond 128 the passes divide by the sum of P; elsewhere that is a test and a branch (dK/dV
+// with the bias, bf16 64: 2 %).  Without a bias x is q.k, whose own products' rounding is as much.
+__device__ __forceinline__ bool is_far(float lse) { return fabsf(lse) > 128.f && fabsf(lse) < INFINITY; }
+__device__ __forceinline__ float inv_sum(float sum) { return sum > 0.f ? 1.f / sum : 1.f; }
+__device__ __forceinline__ float sum16(const f32x16& p) {
+  float s = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s += p[r];
+  return s;
+}
+template <int N>
+__device__ __forceinline__ void scale_by(float f, f32x16 (&acc)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[i][r] *= f;
+}
+
 // st = P and dp = dP of a block (lane = query, registers = keys k0 ..) against tiles of K and V
 template <class O, bool BIAS>
 __device__ __forceinline__ void p_and_dp(const O& ops, f32x16& st, f32x16& dp, const typename O::E* sK,
@@ -919,12 +939,13 @@ __device__ __forceinline__ void p_and_dp(const O& ops, f32x16& st, f32x16& dp, c
   for (int r = 0; r < 16; ++r) st[r] = __builtin_amdgcn_exp2f(BIAS ? st[r] - lse : fmaf(st[r], sl2, -lse));
 }
 // st = P and dp = dS of a block (lane = key, registers = query rows q0 ..) against tiles of Q and
-// dO; stat: (lse, D) of those rows
-template <class O, bool BIAS>
+// dO; stat: (lse, D) of those rows; inv(i): one over row q0 + i's sum of P, where one of the 32 is_far
+template <class O, bool BIAS, class Inv>
 __device__ __forceinline__ void p_and_ds(const O& ops, f32x16& st, f32x16& dp, const typename O::E* sQ,
                                          const typename O::E* sO, int qb, const typename O::Rows& kf,
                                          const typename O::Rows& vf, float sl2, const float* bias, int R, int q0, int off,
-                                         int key, int k0, bool whole, const Visible& seen, const float2* stat, int half) {
+                                         int key, int k0, bool whole, const Visible& seen, const float2* stat, int half,
+                                         const Inv& inv) {
   ops.scores(st, sQ, qb, kf);
   ops.scores(dp, sO, qb, vf);
   landed<O::LANDS>(st);
@@ -948,6 +969,16 @@ __device__ __forceinline__ void p_and_ds(const O& ops, f32x16& st, f32x16& dp, c
       const int r = 4 * g + e;
       st[r] = __builtin_amdgcn_exp2f(BIAS ? st[r] - lv[e] : fmaf(st[r], sl2, -lv[e]));
       dp[r] = st[r] * (dp[r] - sv[e]);
+    }
+  }
+  if (BIAS && __any(is_far(stat[threadIdx.x & 31].x))) {
+    const int own = __float_as_int(inv(threadIdx.x & 31));  // handed round by lane: registers are scarce here
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int f0 = __builtin_amdgcn_readlane(own, perm_pos(r, 0)), f1 = __builtin_amdgcn_readlane(own, perm_pos(r, 1));
+      const float f = __int_as_float(half ? f1 : f0);
+      st[r] *= f;
+      dp[r] *= f;
     }
   }
 }
@@ -1038,6 +1069,8 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   df.settled();
   settle(lse);
   settle(dsum);
+  const bool far = BIAS && __any(is_far(lse));
+  float psum = 0.f, inv = 1.f;
   f32x16 dq[DH / 32];
   // the key tiles once, as iterations from .. of the pipeline; first: for D alone
   auto sweep = [&](auto first, int from) __attribute__((always_inline)) {
@@ -1060,7 +1093,14 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
         if constexpr (first) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) dsum = fmaf(st[r], dp[r], dsum);
+          if (far) psum += sum16(st);
         } else {
+          if (far) {
+            if (DTAB)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) st[r] *= inv;
+            else psum += sum16(st);
+          }
 #pragma unroll
           for (int r = 0; r < 16; ++r) st[r] *= dp[r] - dsum;  // dS
           if (DTAB) add_diag(st, k0 - sq.off - q0, a.R, diag, dlo, dhi, lane);
@@ -1072,6 +1112,10 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   if constexpr (DTAB) {
     sweep(std::true_type{}, 0);
     dsum += __shfl_xor(dsum, 32, 64);
+    if (far) {
+      inv = inv_sum(psum + __shfl_xor(psum, 32, 64));
+      dsum *= inv;
+    }
   }
 #pragma unroll
   for (int i = 0; i < DH / 32; ++i)
@@ -1081,6 +1125,13 @@ __global__ __launch_bounds__(64 * NW, O::WAVES) void attn_masked_bwd_dq(MaskedAt
   const bool dead = lse == INFINITY;  // nothing visible, or past the length
   if (dead) dsum = 0.f;
   clear_if(dead, dq);
+  if (far) {
+    if (!DTAB) {
+      inv = inv_sum(psum + __shfl_xor(psum, 32, 64));
+      scale_by(inv, dq);
+    }
+    if (q < a.Sq && half == 0) a.inv[(long)bh * a.Sq + q] = inv;
+  }
   // the row statistics that the dK/dV pass reads
   if (q < a.Sq && half == 0) a.stat[(long)bh * a.Sq + q] = make_float2(lse, dsum);
   if (DTAB) close_diag(diag, W, dlo, dhi, lane);
@@ -1102,7 +1153,7 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_dq(MaskedAttnArgs a) {
   typedef typename O::E E;
   constexpr int DH = O::DH, BLOCK = O::BLOCK;
   __shared__ __attribute__((aligned(1024))) E sm[NW][4 * BLOCK];  // per wave: [buffer][K, V]; later its dQ
-  __shared__ float sD[NW][32];
+  __shared__ float sD[NW][32], sP[NW][32];
   extern __shared__ float sbias[];  // bias, then (DTAB) one diagonal array per wave
   static_assert(4 * BLOCK * sizeof(E) >= 32 * DH * 4 && 4 * BLOCK >= O::STAGE, "a wave's dQ fits its tiles' space");
   const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
@@ -1155,6 +1206,14 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_dq(MaskedAttnArgs a) {
   df.settled();
   settle(lse);
   settle(dsum);
+  const bool far = BIAS && __any(is_far(lse));  // of the workgroup: its waves have the same rows
+  float psum = 0.f, inv = 1.f;
+  auto join_psum = [&] {
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) sum += sP[k][l32];
+    inv = inv_sum(sum);
+  };
   __syncthreads();  // the bias
 
 #pragma unroll 1
@@ -1183,7 +1242,14 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_dq(MaskedAttnArgs a) {
       if (DTAB && sweep == 0) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) dsum = fmaf(st[r], dp[r], dsum);
+        if (far) psum += sum16(st);
         continue;
+      }
+      if (far) {
+        if (DTAB)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) st[r] *= inv;
+        else psum += sum16(st);
       }
 #pragma unroll
       for (int r = 0; r < 16; ++r) st[r] *= dp[r] - dsum;  // dS
@@ -1194,19 +1260,31 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_dq(MaskedAttnArgs a) {
     if (DTAB && sweep == 0) {
       if (wave < kt.n) issue(wave, 0);
       dsum += __shfl_xor(dsum, 32, 64);
-      if (half == 0) sD[wave][l32] = dsum;
+      psum += __shfl_xor(psum, 32, 64);
+      if (half == 0) {
+        sD[wave][l32] = dsum;
+        sP[wave][l32] = psum;
+      }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       dsum = 0.f;
 #pragma unroll
       for (int k = 0; k < NW; ++k) dsum += sD[k][l32];
+      if (far) {
+        join_psum();
+        dsum *= inv;
+      }
     }
   }
   const bool dead = lse == INFINITY;
   if (dead) dsum = 0.f;
   if (wave == 0 && half == 0 && q < a.Sq) a.stat[(long)bh * a.Sq + q] = make_float2(lse, dsum);
   if (DTAB) close_diag(diag, W, dlo, dhi, lane);
+  if (!DTAB && far) {
+    psum += __shfl_xor(psum, 32, 64);
+    if (half == 0) sP[wave][l32] = psum;
+  }
   float4* so = reinterpret_cast<float4*>(tiles) + lane;
   if (wave > 0) {
 #pragma unroll
@@ -1231,6 +1309,13 @@ __global__ __launch_bounds__(64 * NW, 1) void attn_few_dq(MaskedAttnArgs a) {
         dq[d][4 * g + 3] += x.w;
       }
   clear_if(dead, dq);
+  if (far) {
+    if (!DTAB) {
+      join_psum();
+      scale_by(inv, dq);
+    }
+    if (q < a.Sq && half == 0) a.inv[(long)bh * a.Sq + q] = inv;
+  }
   O::rotate_back(dq, a.rope_tab, min(q, a.Sq - 1), half);
   O::store(dq, a.scale, lane, sm[0], static_cast<E*>(a.dq.p) + b * a.dq.b + (long)q0 * a.dq.t + h * a.dq.h, a.dq.t, false,
            a.Sq - q0, a.dh);
@@ -1387,7 +1472,7 @@ __global__ __launch_bounds__(64 * NW, O::DH == 64 && O::KR == 64 && !BIAS ? 3 : 
   kf.settled();
   vf.settled();
   for (int i = i0; i < i1; ++i) {
-    const int stage = (i - i0) % ST, qt = qt0 + tc, hb_now = hb;
+    const int stage = (i - i0) % ST, qt = qt0 + tc, hb_now = hb, h_now = hc;
     tile_ready<ST, PER>(i - i0, i1 - i0);
     if (issued < i1) issue();
     if (++tc == nt) {
@@ -1408,7 +1493,8 @@ __global__ __launch_bounds__(64 * NW, O::DH == 64 && O::KR == 64 && !BIAS ? 3 : 
       ops.fresh();
       f32x16 st, dp;
       p_and_ds<O, BIAS>(ops, st, dp, sQ, sO, qb, kf, vf, sl2, bias, a.R, q0, sq.off, key, k0, kind == 2, seen,
-                        sS[stage] + qb * 32, half);
+                        sS[stage] + qb * 32, half,
+                        [&](int r) { return a.inv[((long)b * a.H + h_now) * a.Sq + min(q0 + r, a.Sq - 1)]; });
       ops.accum(dv, sO, qb, st);
       ops.accum(dk, sQ, qb, dp);
     }
@@ -1534,6 +1620,7 @@ __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 
   constexpr int DH = O::DH, KR = O::KR, TILE = O::TILE, NW = 4, NT = ROWS / KR;
   __shared__ __attribute__((aligned(1024))) E sm[4 * NT * TILE];  // Q, dO, K, V
   __shared__ __attribute__((aligned(16))) float2 sS[ROWS];        // (lse, D)
+  __shared__ float sInv[ROWS];
   extern __shared__ float sbias[];                                // bias, then (DTAB) one diagonal array per wave
   static_assert(4 * NT * TILE >= NW * O::STAGE, "the rows fit the tiles' space on their way out");
   const int lane = threadIdx.x & 63, half = lane >> 5, l32 = lane & 31;
@@ -1574,7 +1661,8 @@ __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 
   for (int i = 0; i < DH / 32; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) dq[i][r] = 0.f;
-  float dsum = 0.f, dlo = 0.f, dhi = 0.f;
+  float dsum = 0.f, dlo = 0.f, dhi = 0.f, psum = 0.f, inv = 1.f;
+  const bool far = BIAS && __any(is_far(lse));
   if (q0 < sq.lq) {
     const int plo = sq.off + q0, phi = sq.off + min(q0 + 31, sq.lq - 1);
     const Span span = key_span(mask, plo, phi);
@@ -1588,6 +1676,12 @@ __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 
                         k0, p, plo, phi, kind == 2, seen, lse, half);
     };
     auto add = [&](int k0, f32x16& st, const f32x16& dp) {
+      if (far) {
+        if (DTAB)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) st[r] *= inv;
+        else psum += sum16(st);
+      }
 #pragma unroll
       for (int r = 0; r < 16; ++r) st[r] *= dp[r] - dsum;  // dS
       if (DTAB) add_diag(st, k0 - sq.off - q0, a.R, diag, dlo, dhi, lane);
@@ -1601,8 +1695,13 @@ __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 
         block(i * 32, span.kind(i), st[i], dp[i]);
 #pragma unroll
         for (int r = 0; r < 16; ++r) dsum = fmaf(st[i][r], dp[i][r], dsum);
+        if (far) psum += sum16(st[i]);
       }
       dsum += __shfl_xor(dsum, 32, 64);
+      if (far) {
+        inv = inv_sum(psum + __shfl_xor(psum, 32, 64));
+        dsum *= inv;
+      }
 #pragma unroll
       for (int i = 0; i < ROWS / 32; ++i)
         if (span.kind(i) != 0) add(i * 32, st[i], dp[i]);
@@ -1619,7 +1718,14 @@ __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 
   }
   if (lse == INFINITY) dsum = 0.f;
   clear_if(lse == INFINITY, dq);
-  if (q < ROWS && half == 0) sS[q] = make_float2(lse, dsum);
+  if (!DTAB && far) {
+    inv = inv_sum(psum + __shfl_xor(psum, 32, 64));
+    scale_by(inv, dq);
+  }
+  if (q < ROWS && half == 0) {
+    sS[q] = make_float2(lse, dsum);
+    sInv[q] = inv;
+  }
   if (DTAB) close_diag(diag, W, dlo, dhi, lane);
   __syncthreads();
   if (DTAB) put_diag<NW>(sbias, W, a.diag + (long)bh * W);
@@ -1643,7 +1749,7 @@ __global__ __launch_bounds__(256, O::DH == 64 && sizeof(typename O::E) == 2 ? 2 
       if (kind == 0) continue;
       f32x16 st, dp;
       p_and_ds<O, BIAS>(ops, st, dp, sQ + t, sO + t, qb, kf, vf, sl2, sbias, a.R, r0, sq.off, key, k0, kind == 2, seen,
-                        sS + r0, half);
+                        sS + r0, half, [&](int r) { return sInv[r0 + r]; });
       ops.accum(dv, sO + t, qb, st);
       ops.accum(dk, sQ + t, qb, dp);
     }
@@ -1771,11 +1877,12 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
 }
 
 struct BwdSpace {
-  size_t diag, part, total;
+  size_t inv, diag, part, total;
 };
 static BwdSpace bwd_space(int dtype, const MaskedAttnArgs& a, bool dtable) {
   BwdSpace s;
-  s.diag = al256((size_t)a.B * a.H * a.Sq * 8);
+  s.inv = al256((size_t)a.B * a.H * a.Sq * 8);
+  s.diag = s.inv + al256((size_t)a.B * a.H * a.Sq * 4);
   s.part = s.diag + (dtable ? al256((size_t)a.B * (few_blocks(a) ? (a.Sq + 31) / 32 : blocks_of(a.Sq)) * a.H *
                                      (2 * a.R + 1) * 4) : 0);
   const int dh = a.dh <= 64 ? 64 : 128;
@@ -1831,6 +1938,7 @@ void masked_attn_workspace(int dtype, MaskedAttnArgs& a, void* ws) {
   const BwdSpace s = bwd_space(dtype, a, a.dtable != nullptr);
   char* p = static_cast<char*>(ws);
   a.stat = reinterpret_cast<float2*>(p);
+  a.inv = reinterpret_cast<float*>(p + s.inv);
   a.diag = reinterpret_cast<float*>(p + s.diag);
   a.part = reinterpret_cast<float*>(p + s.part);
 }
@@ -1856,14 +1964,14 @@ static hipError_t fwd_ops(const MaskedAttnArgs& a, hipStream_t s) {
 // ROWS: queries, and keys, that the LDS of attn_masked_bwd_small holds
 template <class O, int ROWS>
 static bool fits_small(const MaskedAttnArgs& a) {
-  const size_t lds = sizeof(typename O::E) * 4 * (ROWS / O::KR) * O::TILE + ROWS * 8 +
+  const size_t lds = sizeof(typename O::E) * 4 * (ROWS / O::KR) * O::TILE + ROWS * 12 +
                      (a.table ? (size_t)(2 * a.R + 1) * 4 * (a.dtable ? 5 : 1) : 0);
   return a.H == a.Hkv && a.Sq <= ROWS && a.Sk <= ROWS && lds <= 160 * 1024;
 }
 template <class O, int NW>
 static bool launch_few_dq(const MaskedAttnArgs& a, hipStream_t s) {
   const int W4 = (2 * a.R + 1) * 4;
-  const size_t lds = sizeof(typename O::E) * NW * 4 * O::BLOCK + NW * 128 + (a.table ? (size_t)W4 * (a.dtable ? 1 + NW : 1) : 0);
+  const size_t lds = sizeof(typename O::E) * NW * 4 * O::BLOCK + NW * 256 + (a.table ? (size_t)W4 * (a.dtable ? 1 + NW : 1) : 0);
   const long wgs = (long)a.B * a.H * ((a.Sq + 31) / 32);
   // one and a half rounds of the CUs at most, but over long loops: 348 workgroups of one per CU (fp32, 29 x 2 heads
   // of 191, with the table's gradient) take 41 us, 51 in the other kernel; 448 (bf16, 4 x 8 heads of 430) 25.7 and

@@ -104,6 +104,7 @@ struct MaskedAttnArgs {
   View dout, dq, dk, dv;
   float* dtable;              // [nb, H] or null, added into
   float2* stat;               // workspace: (lse, D) [B, H, Sq], lse +inf for a row that sees nothing
+  float* inv;                 // workspace: 1 / sum of P [B, H, Sq], where a block of 32 rows has a large lse
   float* diag;                // workspace (dtable): sums of dS by relative position, per workgroup of the dQ pass
   float* part;                // workspace: partial sums of workgroups that share their output rows
 };

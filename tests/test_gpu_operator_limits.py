@@ -1,4 +1,6 @@
 """The block operators at the ends of their documented ranges."""
+import math
+
 import pytest
 
 import philox_vectors as P
@@ -139,3 +141,39 @@ def test_zeros_stay_zeros_beside_infinities(dtype, dh, H, Hkv, S, nb, window):
         assert (got[n][0, lk:] == 0).all(), n
     assert (got["lse"][0, :, :12] == -inf).all() and (got["lse"][0, :, lq:] == -inf).all()
     assert torch.equal(got["lse"][1], clean["lse"][1])
+
+
+FAR = [("bf16", 64, 2, 2, 100, 100), ("bf16", 128, 2, 2, 90, 90), ("f32", 40, 2, 2, 100, 100), ("f32", 100, 2, 2, 60, 60),
+       ("bf16", 64, 4, 2, 150, 200), ("bf16", 128, 4, 2, 200, 200), ("f32", 40, 4, 2, 200, 200), ("f32", 100, 4, 1, 100, 130),
+       ("bf16", 64, 64, 16, 300, 300), ("bf16", 128, 64, 64, 270, 270), ("f32", 40, 64, 16, 270, 270), ("f32", 100, 64, 32, 270, 270),
+       ("bf16", 128, 8, 2, 3, 1500)]
+
+
+@pytest.mark.parametrize("big", [-1e9, -1e6, 1000.0])
+@pytest.mark.parametrize("frozen", [False, True])
+@pytest.mark.parametrize("dtype,dh,H,Hkv,Sq,Sk", FAR)
+def test_entries_of_large_magnitude_in_all_that_a_row_sees(dtype, dh, H, Hkv, Sq, Sk, frozen, big):
+    """A table of one value throughout is no bias: where the scores are all the same (q or k is zero), so that fp32
+    holds their sums with it exactly, outputs and gradients are those of a table of zeros, as head 0's is."""
+    import operator_reference as R
+    import torch
+    from test_gpu_operators import A, make, run
+
+    c = A(dtype, 2, H, Hkv, dh, Sq, Sk, causal=True, nb=8, dist=20, len_q=[Sq, Sq - Sq // 3], len_k=[Sk, Sk - Sk // 4])
+    t = make(c, layout="cache")
+    plain = torch.zeros_like(t["table"])
+    t["table"].fill_(big)
+    t["table"][:, 0] = 0
+    for zero in ("q", "k"):
+        z = dict(t)
+        z[zero] = torch.zeros_like(t[zero])
+        got = run(z, frozen)
+        want = R.attention(z["q"], z["k"], z["v"], z["do"], lowp=dtype == "bf16", d_exact=not frozen, **dict(t["how"], table=plain))
+        shift = t["table"][0].double().cpu() / math.log(2)
+        for n in got:
+            if n == "lse":
+                at = ~torch.isinf(want[n][0])
+                w = torch.where(at, want[n][0] + shift[None, :, None], want[n][0])
+                R.check(n, got[n], w, want[n][1] + 2.0 ** -22 * w.abs().nan_to_num(posinf=0))
+            else:
+                R.check(n + " " + zero, got[n], *want[n])
