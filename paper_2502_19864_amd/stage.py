@@ -70,6 +70,8 @@ class Stage:
             B.ringada_stage_bind_block(self.handle, l, bw, None if w.placement == "ffn" else ca[0], ca[1],
                                        self.block_mem[l], self.block_bytes, self.sptr)
         self.attention = None  # StageAttention and the tensors it borrows
+        self.rng = None
+        self.captured = []  # memory that captured graphs go on using, kept whatever replaces it here
         self.stash = self.scratch = None
         self.stash_bytes = self.scratch_bytes = 0
 
@@ -145,6 +147,8 @@ class Stage:
         batch = batch or x.shape[0]
         seq = seq or x.shape[1]
         self.ensure_workspace(batch, seq, c)
+        if self.torch.cuda.is_current_stream_capturing():
+            self.captured.append((self.stash, self.scratch, self.attention, self.rng))
         B.ringada_stage_forward(self.handle, self.sptr, x, y, batch, seq, c, self.stash, self.stash_bytes,
                                 self.scratch, self.scratch_bytes)
 

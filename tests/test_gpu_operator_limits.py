@@ -177,3 +177,60 @@ def test_entries_of_large_magnitude_in_all_that_a_row_sees(dtype, dh, H, Hkv, Sq
                 R.check(n, got[n], w, want[n][1] + 2.0 ** -22 * w.abs().nan_to_num(posinf=0))
             else:
                 R.check(n + " " + zero, got[n], *want[n])
+
+
+def test_a_captured_stage_keeps_its_memory():
+    """A graph of a stage with options goes on working after a larger batch, other options and another
+    generator have replaced what it uses, and writes into nobody else's memory."""
+    import torch
+    from paper_2502_19864_amd import operators as ops
+    from paper_2502_19864_amd.stage import Stage
+    from paper_2502_19864_amd.workloads import Workload, make_inputs
+
+    w = Workload("captured", "bert", "bf16", 2, 256, 4, 512, 64, 150, 2, 0, "dy", 3120)
+    inp = make_inputs(w)
+    st = Stage(w, inp, max_batch=8)
+    try:
+        def table(seed):
+            g = torch.Generator().manual_seed(seed)
+            return torch.randn(16, 4, generator=g).to(st.dev)
+
+        bucket = ops.relpos_buckets(16, 30, True, st.dev)
+        gt = torch.zeros(16, 4, device=st.dev)
+        st.set_attention(60, 1, table(1), bucket, gt)
+        st.set_dropout(0.1, torch.tensor([5, 6], dtype=torch.int64, device=st.dev), 4)
+        x, dy = st.upload(inp["x"]), st.upload(inp["dy"])
+        y, dx = st.empty(*x.shape), st.empty(*x.shape)
+
+        def step():
+            gt.zero_()
+            st.zero_grads()
+            st.forward(x, y, -1)
+            st.backward(dy, -1, dx)
+
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            step()
+        torch.cuda.current_stream().wait_stream(s)
+        torch.cuda.synchronize()
+        want = [t.clone() for t in (y, dx, gt)]
+        sizes = [t.numel() for t in (st.stash, st.scratch, st.attention[4])]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step()
+        big, out = st.empty(8, w.seq, w.d_model).normal_(), st.empty(8, w.seq, w.d_model)
+        st.set_attention(30, 2, table(2), bucket.clone(), torch.zeros_like(gt))
+        st.set_dropout(0.2, torch.tensor([7, 8], dtype=torch.int64, device=st.dev), 0)
+        st.forward(big, out, -1)
+        st.backward(big, -1, torch.empty_like(big))
+        torch.cuda.synchronize()
+        junk = [torch.full((n,), 91, dtype=torch.uint8, device=st.dev) for n in sizes + [16, 128, 256] * 8]
+        for _ in range(3):
+            g.replay()
+            torch.cuda.synchronize()
+            for a, b in zip((y, dx, gt), want):
+                assert torch.equal(a, b)
+            assert all(bool((j == 91).all()) for j in junk)
+    finally:
+        st.close()
