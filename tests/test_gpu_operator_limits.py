@@ -234,3 +234,22 @@ def test_a_captured_stage_keeps_its_memory():
             assert all(bool((j == 91).all()) for j in junk)
     finally:
         st.close()
+
+
+@pytest.mark.parametrize("table", ["none", "frozen", "trained"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,dh", [("bf16", 64), ("bf16", 128), ("f32", 40), ("f32", 100)])
+def test_rows_that_fill_the_gpu_over_several_tiles(dtype, dh, causal, table):
+    """Every form of the passes whose waves take a block of rows each: masks, window, sinks, lengths, shared heads
+    and a bias whose reach ends inside the sequence; 1.6 times the blocks from which these forms are taken."""
+    import operator_reference as R
+    from test_gpu_operators import A, make, run
+
+    c = A(dtype, 2, 24, 6, dh, 520, causal=causal, window=150, sinks=5, nb=0 if table == "none" else 16, dist=0 if
+          table == "none" else 40, len_q=[520, 333], len_k=[520, 333])
+    t = make(c)
+    got = run(t, frozen_table=table == "frozen")
+    want = R.attention(t["q"], t["k"], t["v"], t["do"], lowp=dtype == "bf16", d_exact=table == "trained", **t["how"])
+    assert ("dtable" in got) == (table == "trained")
+    for n in got:
+        print(n, R.check(n, got[n], *want[n]), flush=True)
