@@ -219,7 +219,8 @@ void ringada_stage_destroy(ringada_stage* st);
  * is pending its backward. */
 
 /* Attention of every block with a sliding window, sinks and a relative position
- * bias; the fields are those of ringada_attn_desc and ringada_attn_tensors.  One table
+ * bias; the fields are those of ringada_attn_desc and ringada_attn_tensors (no lengths: every
+ * row of a batch counts, as in the plain attention).  One table
  * serves all blocks; g_table (NULL: a frozen table) is ADDED into by the backward,
  * over the blocks whose attention it passes.  The memory is borrowed until the
  * options are set again or the stage is destroyed. */
@@ -363,7 +364,7 @@ typedef struct {
  * entry for the head is added to the score.  A row that sees nothing, and one at or past
  * its length, gives zeros (and lse -inf).  Rows of k, v and gradients at or past the
  * lengths are not read into any result, whatever they hold.  An infinity or NaN within the
- * lengths of v or dout may reach rows of its sequence that do not see it (0 times it). */
+ * lengths of k, v, q or dout may reach rows of its sequence that do not see it (0 times it). */
 typedef struct {
   ringada_view q, k, v;   /* [batch, seq_q, n_heads, d_head]; [batch, seq_k, n_kv_heads, d_head] */
   ringada_view o;         /* as q: written by the forward, read by the backward */
@@ -389,7 +390,10 @@ typedef struct {
 ringada_status ringada_attn_plan(const ringada_attn_desc* desc, int32_t with_dtable,
                                  size_t* forward_bytes, size_t* backward_bytes);
 
-/* o = softmax(scale q k^T + bias, visible keys) v.  Outputs must not overlap inputs.
+/* o = softmax(scale q k^T + bias, visible keys) v.  Sums and the softmax are held in fp32.  With
+ * bf16 tensors P (here and in the backward) and dS are rounded to bf16 on their way into a
+ * product, and the backward takes D = sum of dout o from the stored o unless it forms the
+ * table's gradient; with fp32 ones nothing is rounded to fewer bits.  Outputs must not overlap inputs.
  * Workspaces are 256-byte aligned and overlap nothing else. */
 ringada_status ringada_attn_forward(void* stream, const ringada_attn_desc* desc,
                                     const ringada_attn_tensors* t, void* workspace,

@@ -1900,9 +1900,10 @@ static bool few(const MaskedAttnArgs& a) {
   const long rows = (long)a.Sq * (a.H / a.Hkv), blocks = a.B * a.Hkv * ((rows + 31) / 32);
   return rows <= 32 || (blocks <= (a.dh <= 64 ? 512 : 256) && key_reach(a) >= 96) || (blocks <= 512 && key_reach(a) >= 4096);
 }
-// One workgroup per CU, and no more than there are tiles for its four waves (64 heads, window
+// At least 256 workgroups where there are tiles for their four waves (64 heads, window
 // 1024: 13.9 us with both kernels; with two tiles for each wave 14.8); none split below 512 keys, as the join
-// takes 4 us.
+// takes 4 us.  Rounded up: where the blocks of rows do not divide 256, head dim 128 (one workgroup per CU) runs a second,
+// nearly empty round (32 heads on 8, 16384 keys: 3.9 TB/s of them at batch 3, 5.4 at batch 4).
 static FewWork few_work(const MaskedAttnArgs& a) {
   FewWork w;
   w.rb = (a.Sq * (a.H / a.Hkv) + 31) / 32;
