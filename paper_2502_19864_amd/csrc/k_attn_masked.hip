@@ -18,6 +18,10 @@
 // formed.  bf16 products run on MFMA 32x32x16, P and dS rounded to bf16 on their
 // way into the second product (they are never stored; every sum stays in fp32);
 // fp32 ones on MFMA 32x32x2 in fp32 throughout.
+//
+// Times beside the kernels are traced launches in the first ten passes after a pause, where nothing else is said.
+// Under load for some hundred launches the card is up to a fifth faster: the case of 8192 tokens and window 1024
+// then takes 172 us forward, 227 for dQ, 296 for dK/dV and 11 for its join.
 #include <algorithm>
 #include <type_traits>
 
@@ -1834,9 +1838,9 @@ constexpr long MAX_WGS = (1l << 24) - 1;
 static size_t al256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Workgroups of the dK/dV pass: two per CU hide each other's barriers, so blocks are split
-// until there are 512, but no finer than four iterations (fp32, whose products take 8 times as
-// long: one.  2 x 2 heads of 96, 557 tokens, window 183: 44 us with the join, 82 with four; bf16, 4 heads on 2 of 128,
-// 1824 tokens: 50 us, 69 with two).
+// until there are 512, but no finer than four iterations (bf16 with the bias, 8 heads of 64, 1000 tokens: 20 us and 5 for the
+// join, 19 and 7 with two; 4 heads on 2 of 128, 1824 tokens: 40 and 8, 34 and 9 with two), fp32, whose products
+// take 8 times as long, one (2 x 2 heads of 96, 557 tokens, window 183: 35 and 7, 75 and 6 with four).
 static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
   const int KR = dtype == DT_BF16 ? 64 : 32, grp = a.H / a.Hkv, rows = 32 * MA_NW;
   KeyWork w;
@@ -1848,8 +1852,8 @@ static KeyWork key_work(int dtype, const MaskedAttnArgs& a) {
   const long least = dtype == DT_BF16 ? 4 : 1;
   const bool has_near = w.nfar < w.nk;
   const long wgs = (long)w.nk * a.B * a.Hkv, nfar = (long)w.nfar * a.B * a.Hkv, longest = has_near ? near : far;
-  // Not into more than 64 pieces, which the join adds one after the other (fp32, 8 heads of 64 on 1, 512 tokens:
-  // 71 us, 89 with up to 128, 649 whole), nor the far ones into more than 2048 workgroups, as
+  // Not into more than 64 pieces, which the join adds one after the other (whole backward, here and below, under
+  // load: fp32, 8 heads of 64 on 1, 512 tokens: 71 us, 89 with up to 128, 649 unsplit), nor the far ones into more than 2048 workgroups, as
   // their partial sums take 64 or 128 KB each.
   const long want = std::max(1l, std::min({(512 + wgs - 1) / wgs, longest / least, 64l}));
   const long c_least = std::max({least, (far + 63) / 64, (far * nfar + 2047) / 2048});
