@@ -331,9 +331,9 @@ ringada_status ringada_sgd_f32(void* stream, float* w, float* g, int64_t n,
                                float lr);
 
 /* ---------------------------------------------------------------- block operators
- * Attention and dropout as calls of their own, for blocks that are put together
- * outside a stage; ringada_stage_set_attention and ringada_stage_set_dropout use
- * the same kernels inside one. */
+ * Attention, dropout, norms, the rotary embedding and the vocabulary head as calls of
+ * their own, for blocks and heads that are put together outside a stage;
+ * ringada_stage_set_attention and ringada_stage_set_dropout use the same kernels inside one. */
 
 /* A [batch, row, head, d_head] tensor: strides in elements, d_head contiguous.
  * bf16: strides multiples of 8 and data 16-byte aligned; f32: any alignment of a
@@ -426,6 +426,110 @@ ringada_status ringada_relpos_buckets(int32_t n_buckets, int32_t max_distance,
  * NULL; y may be x or res; any other overlap returns RINGADA_E_INVALID. */
 ringada_status ringada_dropout(void* stream, int32_t dtype, const void* x, const void* res,
                                void* y, int64_t n, float p, const uint64_t* rng, uint32_t site);
+
+/* Rows of d elements, d contiguous; the stride in elements (of no account with one row). */
+typedef struct {
+  void* data;
+  int64_t row;
+} ringada_rows;
+
+enum { RINGADA_NORM_LAYER = 0, RINGADA_NORM_RMS = 1 };
+typedef struct {
+  int32_t dtype; /* RINGADA_F32 or RINGADA_BF16 */
+  int32_t kind;  /* RINGADA_NORM_* */
+  int64_t rows;
+  int32_t d;     /* 1 .. 16384 */
+  float eps;     /* added to the variance (the mean square), >= 0 */
+} ringada_norm_desc;
+
+/* y = (s - mean(s)) rstd gain + shift with rstd = 1 / sqrt(var(s) + eps), or for RINGADA_NORM_RMS
+ * y = s / sqrt(mean(s^2) + eps) gain + shift; s = x, or with res s = x + res rounded to `dtype` and written to
+ * sum (res and sum are given together or both NULL).  gain [d] and shift [d] (NULL: none) in `dtype`; stats [rows, 2]
+ * floats (NULL: not wanted), 8-byte aligned: mean (0 for RMS) and rstd, which the backward reads.  Any alignment of an
+ * element and any stride; 16-byte aligned rows whose d and strides are multiples of 16 bytes are read
+ * faster.  y and sum may each be x or res, not both the same tensor; any other overlap of an output is refused
+ * (RINGADA_E_INVALID).  Arithmetic and sums in fp32, one rounding each of s and y.  A row with an infinity or NaN
+ * gives NaN in that row alone. */
+ringada_status ringada_norm_forward(void* stream, const ringada_norm_desc* desc, const ringada_rows* x,
+                                    const ringada_rows* res, const ringada_rows* sum, const void* gain,
+                                    const void* shift, const ringada_rows* y, float* stats);
+
+/* Host only.  Bytes of the workspace of a backward that forms dgain or dshift (without them: none needed). */
+ringada_status ringada_norm_plan(const ringada_norm_desc* desc, size_t* backward_bytes);
+
+/* Gradients of ringada_norm_forward with the same desc, gain and stats; sum is what it normalised (x where there
+ * was no res).  dx is the gradient of s, so of x and of res: the norm's, plus dskip (NULL: none), what reaches
+ * s past the norm.  dgain and dshift [d] floats are ADDED into; NULL: frozen.  dx may be dy, dskip or sum; any other
+ * overlap of an output is refused.  Every sum has a fixed order: the same inputs give the same bits. */
+ringada_status ringada_norm_backward(void* stream, const ringada_norm_desc* desc, const ringada_rows* dy,
+                                     const ringada_rows* dskip, const ringada_rows* sum, const void* gain,
+                                     const float* stats, const ringada_rows* dx, float* dgain, float* dshift,
+                                     void* workspace, size_t workspace_bytes);
+
+typedef struct {
+  int32_t dtype;       /* RINGADA_F32 or RINGADA_BF16 */
+  int32_t batch, rows;
+  int32_t n_heads;     /* of q, 1 .. 2048 */
+  int32_t n_kv_heads;  /* of k; 0: there is no k */
+  int32_t d_head;      /* 2 .. 1024 */
+  int32_t n_axes;      /* 1 .. 4 */
+  int32_t section[4];  /* pairs that each axis turns, P in all, 2 P <= d_head */
+  int32_t inverse;     /* 1: by the opposite angles (the backward: the same call on the gradients) */
+} ringada_rotary_desc;
+
+/* Rotary embedding of q [batch, rows, n_heads, d_head] and k [batch, rows, n_kv_heads, d_head]: pair (i, i + P) of a head
+ * turns by positions[axis of pair i][batch][row] * freq[i] radians (the pairs of the stages' RoPE);
+ * dimensions from 2 P on are copied.  Axis 0 has the first section[0] pairs, axis 1 the next, and so on.
+ * positions: int32 [n_axes, batch, rows], any values; freq: double [P]; both device.  Angles are formed in 64 bits, the
+ * rotation in fp32 with one rounding.  q_out may be q and k_out may be k (the same data and
+ * strides); any other overlap of an output is refused.  k and k_out are NULL when n_kv_heads is 0. */
+ringada_status ringada_rotary(void* stream, const ringada_rotary_desc* desc, const ringada_view* q,
+                              const ringada_view* k, const int32_t* positions, const double* freq,
+                              const ringada_view* q_out, const ringada_view* k_out);
+
+/* Host only.  The usual frequencies: theta^(-j / section) for the j-th pair of each axis, or with shared
+ * theta^(-i / P) for pair i of all.  freq: double [P] host, P <= 512. */
+ringada_status ringada_rotary_frequencies(int32_t n_axes, const int32_t* section, double theta, int32_t shared,
+                                          double* freq);
+
+typedef struct {
+  int32_t dtype; /* RINGADA_F32 or RINGADA_BF16 */
+  int32_t rows;  /* 1 .. 2^23 */
+  int32_t d;     /* 1 .. 16384; bf16: a multiple of 8 */
+  int32_t vocab; /* 1 .. 2^22 */
+} ringada_vocab_desc;
+
+/* h, dh [rows, d]; w, dw [vocab, d] in the stage dtype: a row per class, as in an embedding table, so that a tied one can be
+ * passed (unlike the stages' [in, out] weights).  bf16: 16-byte aligned, strides multiples of 8. */
+typedef struct {
+  ringada_rows h, w;
+  const int32_t* labels; /* [rows]; a row with a label outside [0, vocab) does not count */
+  float* loss;           /* [rows] */
+  float* lse;            /* [rows] */
+  const float* dloss;    /* [rows]: the gradient that arrives at each row's loss; NULL: no gradients */
+  ringada_rows dh, dw;   /* written; data NULL: not wanted (a frozen head takes dh alone) */
+} ringada_vocab_tensors;
+
+/* Host only.  Bytes of the workspaces of ringada_vocab_ce without and with gradients, and of ringada_vocab_next.
+ * The logits are held for a piece of the rows at a time, at most 2^29 of them (or 256 rows), so the second is at most
+ * some 3 GiB, beside a copy of h and, for rows of more than one piece in bf16, 4 vocab d bytes.  Any pointer may be NULL. */
+ringada_status ringada_vocab_plan(const ringada_vocab_desc* desc, size_t* forward_bytes, size_t* train_bytes,
+                                  size_t* next_bytes);
+
+/* Softmax cross entropy of the logits s = h w^T, and its gradients in the same call:
+ *   lse = log sum exp s,  loss = lse - s[label],  P = dloss (softmax(s) - onehot(label)),  dh = P w,  dw = P^T h.
+ * A row that does not count has loss 0, lse 0 and a zero row in dh; its h and dloss are read into nothing, whatever they
+ * hold.  Logits, softmax and sums are fp32; with bf16 tensors P is rounded to bf16 on its way into the
+ * products.  An infinity or NaN in a row that counts gives NaN in it, and in dw.  No output may overlap
+ * anything else.  Every sum has a fixed order: the same inputs give the same bits. */
+ringada_status ringada_vocab_ce(void* stream, const ringada_vocab_desc* desc, const ringada_vocab_tensors* t,
+                                void* workspace, size_t workspace_bytes);
+
+/* The class of the largest logit of every row of h (of equal ones the lowest; NaN logits are passed over, and a row of
+ * nothing else gives some class in range) and its log-probability, s[token] - lse. */
+ringada_status ringada_vocab_next(void* stream, const ringada_vocab_desc* desc, const ringada_rows* h,
+                                  const ringada_rows* w, int32_t* token, float* logprob, void* workspace,
+                                  size_t workspace_bytes);
 
 /* ---------------------------------------------------------------- diagnostics */
 

@@ -14,6 +14,7 @@ RINGADA_OK, RINGADA_E_INVALID, RINGADA_E_STATE, RINGADA_E_WORKSPACE, RINGADA_E_U
 ARCH_POSTLN_GELU, ARCH_PRERMS_SWIGLU = 0, 1
 F32, BF16 = 0, 1
 PLACEMENT_HOULSBY, PLACEMENT_FFN = 0, 1
+NORM_LAYER, NORM_RMS = 0, 1
 STATUS_NAMES = {0: "OK", 1: "E_INVALID", 2: "E_STATE", 3: "E_WORKSPACE", 4: "E_UNSUPPORTED", 5: "E_HIP"}
 
 
@@ -74,6 +75,29 @@ class AttnGrads(ctypes.Structure):
     _fields_ = [("dout", View), ("dq", View), ("dk", View), ("dv", View), ("dtable", c_void_p)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("row", c_int64)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("kind", c_int32), ("rows", c_int64), ("d", c_int32), ("eps", c_float)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("batch", c_int32), ("rows", c_int32), ("n_heads", c_int32),
+                ("n_kv_heads", c_int32), ("d_head", c_int32), ("n_axes", c_int32), ("section", c_int32 * 4),
+                ("inverse", c_int32)]
+
+
+class VocabDesc(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("rows", c_int32), ("d", c_int32), ("vocab", c_int32)]
+
+
+class VocabTensors(ctypes.Structure):
+    _fields_ = [("h", Rows), ("w", Rows), ("labels", c_void_p), ("loss", c_void_p), ("lse", c_void_p),
+                ("dloss", c_void_p), ("dh", Rows), ("dw", Rows)]
+
+
 # (name, restype, argtypes): every symbol declared in include/ringada.h
 SIGNATURES = [
     ("ringada_stage_plan", c_int32, [POINTER(StageDesc), c_int32, c_int32, c_int32,
@@ -104,6 +128,14 @@ SIGNATURES = [
     ("ringada_relpos_buckets", c_int32, [c_int32, c_int32, c_int32, POINTER(c_int32)]),
     ("ringada_dropout", c_int32, [c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_float, c_void_p,
                                   c_uint32]),
+    ("ringada_norm_forward", c_int32, [c_void_p] * 9),
+    ("ringada_norm_plan", c_int32, [c_void_p, POINTER(c_size_t)]),
+    ("ringada_norm_backward", c_int32, [c_void_p] * 11 + [c_size_t]),
+    ("ringada_rotary", c_int32, [c_void_p] * 8),
+    ("ringada_rotary_frequencies", c_int32, [c_int32, POINTER(c_int32), c_double, c_int32, POINTER(c_double)]),
+    ("ringada_vocab_plan", c_int32, [c_void_p, POINTER(c_size_t), POINTER(c_size_t), POINTER(c_size_t)]),
+    ("ringada_vocab_ce", c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_size_t]),
+    ("ringada_vocab_next", c_int32, [c_void_p] * 7 + [c_size_t]),
     ("ringada_last_error", c_char_p, []),
     ("ringada_prof_begin", c_int32, [c_void_p]),
     ("ringada_prof_end", c_int32, [c_void_p, POINTER(ProfEntry), c_int32, POINTER(c_int32)]),
@@ -144,8 +176,8 @@ def _p(x):
 
 
 def _ref(x):
-    """A structure by reference, or its packed bytes as they are."""
-    return x if type(x) is bytes else byref(x)
+    """A structure by reference, or its packed bytes (or None) as they are."""
+    return x if type(x) is bytes or x is None else byref(x)
 
 
 def _in(name, x, low, bits):
@@ -261,6 +293,55 @@ def ringada_relpos_buckets(n_buckets, max_distance, bidirectional):
 def ringada_dropout(stream, dtype, x, res, y, n, p, rng, site):
     _check(lib().ringada_dropout(stream, dtype, _p(x), _p(res), _p(y), _in("n", n, -1 << 63, 63), p, _p(rng),
                                  _in("site", site, 0, 32)))
+
+
+def ringada_norm_forward(stream, desc, x, res, sum_, gain, shift, y, stats):
+    _check(lib().ringada_norm_forward(stream, _ref(desc), _ref(x), _ref(res), _ref(sum_), _p(gain), _p(shift), _ref(y),
+                                      _p(stats)))
+
+
+def ringada_norm_plan(desc):
+    n = c_size_t(0)
+    _check(lib().ringada_norm_plan(_ref(desc), byref(n)))
+    return n.value
+
+
+def ringada_norm_backward(stream, desc, dy, dskip, sum_, gain, stats, dx, dgain, dshift, workspace, workspace_bytes):
+    _check(lib().ringada_norm_backward(stream, _ref(desc), _ref(dy), _ref(dskip), _ref(sum_), _p(gain), _p(stats),
+                                       _ref(dx), _p(dgain), _p(dshift), _p(workspace), workspace_bytes))
+
+
+def ringada_rotary(stream, desc, q, k, positions, freq, q_out, k_out):
+    _check(lib().ringada_rotary(stream, _ref(desc), _ref(q), _ref(k), _p(positions), _p(freq), _ref(q_out),
+                                _ref(k_out)))
+
+
+def ringada_rotary_frequencies(sections, theta, shared):
+    """The frequencies as a list of sum(sections) floats."""
+    if not 1 <= len(sections) <= 4:
+        raise ValueError("sections: one to four axes")
+    for m in sections:
+        _in("section", m, 1, 10)
+    s = (c_int32 * len(sections))(*sections)
+    f = (c_double * sum(sections))()
+    _check(lib().ringada_rotary_frequencies(len(sections), s, theta, int(shared), f))
+    return list(f)
+
+
+def ringada_vocab_plan(desc):
+    """Workspace bytes of a call without gradients, of one with, and of ringada_vocab_next."""
+    f, t, n = c_size_t(0), c_size_t(0), c_size_t(0)
+    _check(lib().ringada_vocab_plan(_ref(desc), byref(f), byref(t), byref(n)))
+    return f.value, t.value, n.value
+
+
+def ringada_vocab_ce(stream, desc, tensors, workspace, workspace_bytes):
+    _check(lib().ringada_vocab_ce(stream, _ref(desc), _ref(tensors), _p(workspace), workspace_bytes))
+
+
+def ringada_vocab_next(stream, desc, h, w, token, logprob, workspace, workspace_bytes):
+    _check(lib().ringada_vocab_next(stream, _ref(desc), _ref(h), _ref(w), _p(token), _p(logprob), _p(workspace),
+                                    workspace_bytes))
 
 
 def ringada_last_error():

@@ -1,0 +1,291 @@
+// LayerNorm and RMSNorm of rows, a residual added before, with the gradients of x, gain and shift.
+//
+//   s = x + res (as stored)      u = (s - mean) rstd      y = u gain + shift
+//   rstd = 1 / sqrt(mean((s - mean)^2) + eps); RMSNorm: mean = 0
+//   a = dy gain;  ds = rstd (a - mean(a) - u mean(a u)) + dskip (RMSNorm: without mean(a))
+//   dgain += sum over rows of dy u;  dshift += sum over rows of dy
+//
+// Bound by memory.  A row stays in the registers of the threads that read it, so the mean, the
+// squares around it (not the difference of two sums) and the result take one read of it.  The backward's
+// workgroups run over many rows each and keep their columns' sums in registers; a second kernel adds
+// the workgroups' sums in a fixed order.
+#include "common.h"
+#include "kernels.h"
+
+namespace rg {
+
+// 16-byte pieces of a row: VE elements
+template <typename T> constexpr int VE = 16 / sizeof(T);
+
+template <typename T>
+__device__ __forceinline__ void ld_piece(const T* p, int left, bool wide, float v[VE<T>]) {
+  if (wide) {
+    if constexpr (sizeof(T) == 2) unpack_frag(*reinterpret_cast<const bf16x8*>(p), v);
+    else St<T>::ld4(p, 0, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VE<T>; ++i) v[i] = i < left ? St<T>::ld(p, i) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void st_piece(T* p, int left, bool wide, const float v[VE<T>]) {
+  if (wide) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x8*>(p) = pack_frag(v);
+    else St<T>::st4(p, 0, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VE<T>; ++i)
+      if (i < left) St<T>::st(p, i, v[i]);
+  }
+}
+// what storing and loading again makes of v
+template <typename T>
+__device__ __forceinline__ float stored(float v) {
+  if constexpr (sizeof(T) == 2) return bf2f(f2bf(v));
+  return v;
+}
+
+// sum over the TPR threads of a row, in every one of them; red: one float per wave, free again after the next barrier
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float* red) {
+  v = wave_sum(v);
+  if constexpr (TPR > 64) {
+    const int wave = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[wave] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; ++w) v += red[w];
+  }
+  return v;
+}
+
+// TPR threads per row, CH pieces per thread
+template <typename T, int TPR, int CH>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_k(NormArgs a, bool wide) {
+  constexpr int E = VE<T>, NT = TPR > 256 ? TPR : 256, RPW = NT / TPR;
+  __shared__ float red[16];
+  const int t = threadIdx.x % TPR;
+  const long row = ((long)blockIdx.y * gridDim.x + blockIdx.x) * RPW + threadIdx.x / TPR;
+  if (row >= a.rows) return;  // whole waves, or the workgroup
+  const T* x = static_cast<const T*>(a.x.p) + row * a.x.t;
+  const T* res = a.res.p ? static_cast<const T*>(a.res.p) + row * a.res.t : nullptr;
+  float v[CH][E];
+  float sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int at = (c * TPR + t) * E, left = a.d - at;
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[c][i] = 0.f;
+    if (left <= 0) continue;
+    ld_piece(x + at, left, wide, v[c]);
+    if (res) {
+      float r[E];
+      ld_piece(res + at, left, wide, r);
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[c][i] = stored<T>(v[c][i] + r[i]);
+      st_piece(static_cast<T*>(a.s.p) + row * a.s.t + at, left, wide, v[c]);
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) sum += v[c][i];
+  }
+  const float mean = a.rms ? 0.f : row_sum<TPR>(sum, red) / a.d;
+  float sq = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float w = (c * TPR + t) * E + i < a.d ? v[c][i] - mean : 0.f;
+      sq += w * w;
+    }
+  const float rstd = 1.f / sqrtf(row_sum<TPR>(sq, red) / a.d + a.eps);
+  if (a.stats && t == 0) a.stats[row] = make_float2(mean, rstd);
+  const T* gain = static_cast<const T*>(a.gain);
+  const T* shift = static_cast<const T*>(a.shift);
+  T* y = static_cast<T*>(a.y.p) + row * a.y.t;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int at = (c * TPR + t) * E, left = a.d - at;
+    if (left <= 0) continue;
+    float g[E], b[E];
+    ld_piece(gain + at, left, wide, g);
+    if (shift) ld_piece(shift + at, left, wide, b);
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float u = (v[c][i] - mean) * rstd * g[i];
+      v[c][i] = shift ? u + b[i] : u;
+    }
+    st_piece(y + at, left, wide, v[c]);
+  }
+}
+
+template <typename T, int TPR, int CH>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_k(NormArgs a, bool wide) {
+  constexpr int E = VE<T>, NT = TPR > 256 ? TPR : 256, RPW = NT / TPR;
+  __shared__ float red[16];
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  const T* gain = static_cast<const T*>(a.gain);
+  float g[CH][E], dg[CH][E], db[CH][E];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int at = (c * TPR + t) * E, left = a.d - at;
+#pragma unroll
+    for (int i = 0; i < E; ++i) g[c][i] = dg[c][i] = db[c][i] = 0.f;
+    if (left > 0) ld_piece(gain + at, left, wide, g[c]);
+  }
+  const float inv_d = 1.f / a.d;
+  // rows group, group + groups, ..; every row of a workgroup's loop has all its threads
+  for (long row = (long)blockIdx.x * RPW + sub; row < a.rows; row += (long)gridDim.x * RPW) {
+    const T* x = static_cast<const T*>(a.s.p) + row * a.s.t;
+    const T* dy = static_cast<const T*>(a.dy.p) + row * a.dy.t;
+    const float2 st = a.stats[row];
+    float u[CH][E], w[CH][E];
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int at = (c * TPR + t) * E, left = a.d - at;
+#pragma unroll
+      for (int i = 0; i < E; ++i) u[c][i] = w[c][i] = 0.f;
+      if (left <= 0) continue;
+      ld_piece(x + at, left, wide, u[c]);
+      ld_piece(dy + at, left, wide, w[c]);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        u[c][i] = i < left ? (u[c][i] - st.x) * st.y : 0.f;
+        dg[c][i] += w[c][i] * u[c][i];
+        db[c][i] += w[c][i];
+        w[c][i] *= g[c][i];
+        s1 += w[c][i];
+        s2 += w[c][i] * u[c][i];
+      }
+    }
+    s1 = a.rms ? 0.f : row_sum<TPR>(s1, red) * inv_d;
+    s2 = row_sum<TPR>(s2, red) * inv_d;
+    T* dx = static_cast<T*>(a.dx.p) + row * a.dx.t;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int at = (c * TPR + t) * E, left = a.d - at;
+      if (left <= 0) continue;
+      float k[E];
+      if (a.dskip.p) ld_piece(static_cast<const T*>(a.dskip.p) + row * a.dskip.t + at, left, wide, k);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float v = st.y * (w[c][i] - s1 - u[c][i] * s2);
+        w[c][i] = a.dskip.p ? v + k[i] : v;
+      }
+      st_piece(dx + at, left, wide, w[c]);
+    }
+  }
+  if (!a.part) return;
+  // the row groups of a workgroup, then its sums: part[group][0: dgain, 1: dshift][d]
+  __shared__ float acc[RPW > 1 ? (RPW - 1) * TPR * E * CH : 1];
+  for (int which = 0; which < 2; ++which) {
+    float* dst = which ? a.dshift : a.dgain;
+    if (!dst) continue;
+    float* out = a.part + ((long)blockIdx.x * 2 + which) * a.d;
+    if constexpr (RPW > 1) {
+      __syncthreads();
+      if (sub)
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+          for (int i = 0; i < E; ++i) acc[(((sub - 1) * CH + c) * E + i) * TPR + t] = which ? db[c][i] : dg[c][i];
+      __syncthreads();
+      if (sub) continue;
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const int at = (c * TPR + t) * E + i;
+        float v = which ? db[c][i] : dg[c][i];
+        if constexpr (RPW > 1)
+#pragma unroll
+          for (int r = 1; r < RPW; ++r) v += acc[(((r - 1) * CH + c) * E + i) * TPR + t];
+        if (at < a.d) out[at] = v;
+      }
+  }
+}
+
+// dgain += the workgroups' sums, dshift likewise (blockIdx.y 1): 32 columns and 8 shares of the groups per workgroup
+__global__ __launch_bounds__(256) void norm_sums_k(NormArgs a) {
+  __shared__ float red[8][33];
+  float* dst = blockIdx.y ? a.dshift : a.dgain;
+  if (!dst) return;
+  const int col = threadIdx.x & 31, share = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
+  float v = 0.f;
+  if (c < a.d)
+    for (int g = share; g < a.groups; g += 8) v += a.part[((long)g * 2 + blockIdx.y) * a.d + c];
+  red[share][col] = v;
+  __syncthreads();
+  if (share || c >= a.d) return;
+#pragma unroll
+  for (int s = 1; s < 8; ++s) v += red[s][col];
+  dst[c] += v;
+}
+
+// threads per row and pieces per thread: a wave takes up to four pieces per lane
+struct NormShape {
+  int tpr, ch;
+};
+static NormShape norm_shape(int dtype, int d) {
+  const int pieces = (d + (dtype == DT_BF16 ? 7 : 3)) / (dtype == DT_BF16 ? 8 : 4);
+  for (int tpr : {64, 256, 1024})
+    for (int ch : {1, 2, 4})
+      if (tpr * ch >= pieces) return {tpr, ch};
+  return {0, 0};
+}
+
+int norm_groups(int dtype, long rows, int d) {
+  const NormShape f = norm_shape(dtype, d);
+  const int rpw = f.tpr >= 256 ? 1 : 256 / f.tpr;
+  const long wgs = (rows + rpw - 1) / rpw;
+  return (int)(wgs < 512 ? wgs : 512);
+}
+
+static bool rows_wide(const NormRows& r, int es) {
+  return r.p == nullptr || ((reinterpret_cast<uintptr_t>(r.p) & 15u) == 0 && (r.t * es & 15) == 0);
+}
+
+template <typename T, int TPR, int CH>
+static hipError_t norm_go(const NormArgs& a, bool back, bool wide, hipStream_t s) {
+  constexpr int NT = TPR > 256 ? TPR : 256, RPW = NT / TPR;
+  if (back) RG_LAUNCH((norm_bwd_k<T, TPR, CH>), dim3(a.groups), dim3(NT), 0, s, a, wide);
+  else {
+    // HIP takes fewer than 2^32 threads in a dimension of a launch
+    const long wgs = (a.rows + RPW - 1) / RPW, y = (wgs + (1l << 21) - 1) >> 21;
+    RG_LAUNCH((norm_fwd_k<T, TPR, CH>), dim3((unsigned)((wgs + y - 1) / y), (unsigned)y), dim3(NT), 0, s, a, wide);
+  }
+  if (back && a.part) RG_LAUNCH(norm_sums_k, dim3((a.d + 31) / 32, 2), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t norm_t(int dtype, const NormArgs& a, bool back, hipStream_t s) {
+  const int es = sizeof(T);
+  const auto al = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
+  const bool wide = a.d % VE<T> == 0 && rows_wide(a.x, es) && rows_wide(a.res, es) && rows_wide(a.s, es) &&
+                    rows_wide(a.y, es) && rows_wide(a.dy, es) && rows_wide(a.dskip, es) && rows_wide(a.dx, es) &&
+                    al(a.gain) && al(a.shift);
+  const NormShape f = norm_shape(dtype, a.d);
+  switch (f.tpr * 8 + f.ch) {
+    case 64 * 8 + 1: return norm_go<T, 64, 1>(a, back, wide, s);
+    case 64 * 8 + 2: return norm_go<T, 64, 2>(a, back, wide, s);
+    case 64 * 8 + 4: return norm_go<T, 64, 4>(a, back, wide, s);
+    case 256 * 8 + 2: return norm_go<T, 256, 2>(a, back, wide, s);
+    case 256 * 8 + 4: return norm_go<T, 256, 4>(a, back, wide, s);
+    case 1024 * 8 + 2: return norm_go<T, 1024, 2>(a, back, wide, s);
+    case 1024 * 8 + 4: return norm_go<T, 1024, 4>(a, back, wide, s);
+  }
+  return hipErrorInvalidValue;
+}
+
+hipError_t launch_norm_fwd(int dtype, const NormArgs& a, hipStream_t s) {
+  return dtype == DT_BF16 ? norm_t<bf16>(dtype, a, false, s) : norm_t<float>(dtype, a, false, s);
+}
+hipError_t launch_norm_bwd(int dtype, const NormArgs& a, hipStream_t s) {
+  return dtype == DT_BF16 ? norm_t<bf16>(dtype, a, true, s) : norm_t<float>(dtype, a, true, s);
+}
+
+}  // namespace rg

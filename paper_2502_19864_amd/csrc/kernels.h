@@ -245,6 +245,70 @@ inline uint32_t dropout_threshold(float p) { return (uint32_t)(65536.0 * (double
 hipError_t launch_dropout(int dtype, const void* x, const void* res, void* y, long n, uint32_t thr,
                           const uint64_t* rng, uint32_t site, hipStream_t s);
 
+// ---------------------------------------------------------------- vocabulary head (k_vocab.hip has the formulas)
+struct VocabArgs {
+  int n, d, V;
+  const void* h; long ldh;      // [n][d]
+  const void* w; long ldw;      // [V][d]
+  const int* labels;            // [n], or null: the token of every row
+  const float* dloss;           // [n]: gradients wanted
+  float* loss; float* lse;      // [n]
+  void* dh; long lddh;          // [n][d] or null
+  void* dw; long lddw;          // [V][d] or null
+  int* token; float* logprob;   // [n]: without labels
+  // workspace
+  int dp, Vp, tiles, R;         // d and V up to a multiple of 64, column tiles of the logits, rows at a time
+  void* hc;                     // [n up][dp]: the rows that count, zeros past d and behind the last
+  float2* part; int* part_at;   // [R][tiles]
+  int* n_counted;
+  int* idx; int* lab_c; float* g_c; float* target;  // [n], by counted row: its place, label, gradient, label's logit
+  float2* stat;                 // [R]: lse, loss
+  float* logits;                // [R][Vp]
+  void* P;                      // [R][Vp] in the storage type (fp32: the logits' place)
+  float* dw_acc; long ld_acc;   // dw between the pieces
+  // a piece
+  const int* count;             // n_counted, or null: all rows
+  int row0, rows, first, last;
+};
+// bytes of the workspace, and with ws the pointers into it
+size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws);
+hipError_t launch_vocab(int dtype, const VocabArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- norms with their gradients (k_norm.hip)
+struct NormRows {
+  void* p;
+  long t;  // row stride in elements
+};
+struct NormArgs {
+  long rows;
+  int d, rms;
+  float eps;
+  NormRows x, res, s, y;        // res.p, s.p null: no residual (s = x)
+  const void* gain; const void* shift;  // shift may be null
+  float2* stats;                // [rows]: mean (0 for rms), 1 / deviation; the forward may go without
+  // backward
+  NormRows dy, dskip, dx;       // dskip.p may be null
+  float* dgain; float* dshift;  // [d], added into, or null
+  float* part;                  // workspace: [groups][2 or 1][d]
+  int groups;
+};
+// workgroups of the backward that leave partial sums of dgain and dshift
+int norm_groups(int dtype, long rows, int d);
+hipError_t launch_norm_fwd(int dtype, const NormArgs& a, hipStream_t s);
+hipError_t launch_norm_bwd(int dtype, const NormArgs& a, hipStream_t s);
+
+// ---------------------------------------------------------------- rotary embedding (k_rotary.hip)
+constexpr int ROTARY_MAX_PAIRS = 512;
+struct RotaryArgs {
+  int B, S, H, Hkv, dh;         // Hkv 0: no k
+  int pairs, axes, end[4];      // end[a]: first pair behind axis a's
+  int inverse;
+  View q, k, oq, ok;
+  const int* pos;               // [axes][B][S]
+  const double* freq;           // [pairs], radians per position
+};
+hipError_t launch_rotary(int dtype, const RotaryArgs& a, hipStream_t s);
+
 // ---------------------------------------------------------------- losses
 // whether dY overlaps the inputs in no other way than the losses can take
 bool mse_dy_ok(const void* y, const void* t, const void* dy, size_t bytes);

@@ -1,6 +1,6 @@
 // The block operators behind the C ABI: attention with a window, sinks and a relative
-// position bias, and dropout.  Argument checks and the kernels' argument
-// structs; nothing here allocates or keeps anything.
+// position bias, dropout, norms, the rotary embedding, and the vocabulary head.  Argument
+// checks and the kernels' argument structs; nothing here allocates or keeps anything.
 #include <math.h>
 
 #include <utility>
@@ -328,5 +328,313 @@ extern "C" ringada_status ringada_dropout(void* stream, int32_t dtype, const voi
   if (!same_or_apart(x, y, bytes) || (res && !same_or_apart(res, y, bytes)))
     return fail(RINGADA_E_INVALID, "y overlaps x or res without being the same tensor");
   RG_HIP(launch_dropout(dtype, x, res, y, n, thr, rng, site, static_cast<hipStream_t>(stream)));
+  return RINGADA_OK;
+}
+
+// ================================================================ norms
+static size_t elem_bytes(int dtype) { return dtype == RINGADA_BF16 ? 2 : 4; }
+
+// rows of d elements; writes: they may not overlap each other
+static ringada_status check_rows(int dtype, const char* name, const ringada_rows& v, int64_t rows, int64_t d, bool writes,
+                                 void*& data, long& row) {
+  if (!v.data) return fail(RINGADA_E_INVALID, "%s is NULL", name);
+  const int64_t t = rows == 1 ? 0 : v.row;
+  if (t < 0 || t >= (1ll << 40) || (rows > 1 && t > (1ll << 46) / (rows - 1)))
+    return fail(RINGADA_E_INVALID, "%s: row stride out of range", name);
+  if (reinterpret_cast<uintptr_t>(v.data) & (elem_bytes(dtype) - 1)) return fail(RINGADA_E_INVALID, "%s is misaligned", name);
+  if (writes && rows > 1 && t < d) return fail(RINGADA_E_INVALID, "%s: rows of an output overlap", name);
+  data = v.data;
+  row = (long)t;
+  return RINGADA_OK;
+}
+static Region rows_region(const char* name, int dtype, const void* data, long row, int64_t rows, int64_t d) {
+  const int64_t es = (int64_t)elem_bytes(dtype);
+  return {name, reinterpret_cast<uintptr_t>(data), d * es, {row * es, 0, 0}, {rows, 1, 1}};
+}
+static bool same_tensor(const Region& a, const Region& b) {
+  return a.p == b.p && a.len == b.len && a.stride[0] == b.stride[0] && a.stride[1] == b.stride[1] && a.stride[2] == b.stride[2];
+}
+// as check_apart, but an output may be one of the inputs before it that same marks
+static ringada_status check_apart_or_same(const Region* all, const bool* same, int n_in, int n) {
+  for (int i = n_in; i < n; ++i)
+    for (int j = 0; j < i; ++j) {
+      if (j < n_in && same[j] && same_tensor(all[i], all[j])) continue;
+      if (overlap(all[i], all[j])) return fail(RINGADA_E_INVALID, "%s overlaps %s", all[i].name, all[j].name);
+    }
+  return RINGADA_OK;
+}
+
+static ringada_status check_norm(const ringada_norm_desc* D) {
+  if (!D) return fail(RINGADA_E_INVALID, "desc is NULL");
+  if (D->dtype != RINGADA_F32 && D->dtype != RINGADA_BF16) return fail(RINGADA_E_INVALID, "unknown dtype %d", D->dtype);
+  if (D->kind != RINGADA_NORM_LAYER && D->kind != RINGADA_NORM_RMS) return fail(RINGADA_E_INVALID, "unknown kind %d", D->kind);
+  if (D->rows < 1 || D->d < 1) return fail(RINGADA_E_INVALID, "sizes must be positive");
+  if (!(D->eps >= 0.f) || !isfinite(D->eps)) return fail(RINGADA_E_INVALID, "eps must be finite and not negative");
+  if (D->d > 16384) return fail(RINGADA_E_UNSUPPORTED, "rows of more than 16384 elements (got %d)", D->d);
+  if (D->rows >= (1ll << 31)) return fail(RINGADA_E_UNSUPPORTED, "2^31 rows or more");
+  return RINGADA_OK;
+}
+static ringada_status check_param(int dtype, const char* name, const void* p) {
+  if (reinterpret_cast<uintptr_t>(p) & (elem_bytes(dtype) - 1)) return fail(RINGADA_E_INVALID, "%s is misaligned", name);
+  return RINGADA_OK;
+}
+static NormArgs norm_sizes(const ringada_norm_desc& D) {
+  NormArgs a{};
+  a.rows = D.rows;
+  a.d = D.d;
+  a.rms = D.kind == RINGADA_NORM_RMS;
+  a.eps = D.eps;
+  return a;
+}
+
+extern "C" ringada_status ringada_norm_forward(void* stream, const ringada_norm_desc* desc, const ringada_rows* x,
+                                               const ringada_rows* res, const ringada_rows* sum, const void* gain,
+                                               const void* shift, const ringada_rows* y, float* stats) {
+  RG_TRY(check_norm(desc));
+  if (!x || !y || !gain) return fail(RINGADA_E_INVALID, "x, y or gain is NULL");
+  if (!res != !sum) return fail(RINGADA_E_INVALID, "res and sum must be given together");
+  const int dt = desc->dtype;
+  const int64_t n = desc->rows, d = desc->d;
+  NormArgs a = norm_sizes(*desc);
+  RG_TRY(check_rows(dt, "x", *x, n, d, false, a.x.p, a.x.t));
+  if (res) {
+    RG_TRY(check_rows(dt, "res", *res, n, d, false, a.res.p, a.res.t));
+    RG_TRY(check_rows(dt, "sum", *sum, n, d, true, a.s.p, a.s.t));
+  }
+  RG_TRY(check_rows(dt, "y", *y, n, d, true, a.y.p, a.y.t));
+  RG_TRY(check_param(dt, "gain", gain));
+  RG_TRY(check_param(dt, "shift", shift));
+  if (reinterpret_cast<uintptr_t>(stats) & 7u) return fail(RINGADA_E_INVALID, "stats is misaligned");
+  const Region all[7] = {rows_region("x", dt, a.x.p, a.x.t, n, d), rows_region("res", dt, a.res.p, a.res.t, n, d),
+                         flat("gain", gain, (size_t)d * elem_bytes(dt)), flat("shift", shift, (size_t)d * elem_bytes(dt)),
+                         rows_region("sum", dt, a.s.p, a.s.t, n, d), rows_region("y", dt, a.y.p, a.y.t, n, d),
+                         flat("stats", stats, (size_t)n * 8)};
+  const bool same[4] = {true, true, false, false};
+  RG_TRY(check_apart_or_same(all, same, 4, 7));
+  a.gain = gain;
+  a.shift = shift;
+  a.stats = reinterpret_cast<float2*>(stats);
+  RG_HIP(launch_norm_fwd(dt, a, static_cast<hipStream_t>(stream)));
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_norm_plan(const ringada_norm_desc* desc, size_t* backward_bytes) {
+  RG_TRY(check_norm(desc));
+  if (backward_bytes) *backward_bytes = (size_t)norm_groups(desc->dtype, desc->rows, desc->d) * 2 * desc->d * 4;
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_norm_backward(void* stream, const ringada_norm_desc* desc, const ringada_rows* dy,
+                                                const ringada_rows* dskip, const ringada_rows* sum, const void* gain,
+                                                const float* stats, const ringada_rows* dx, float* dgain, float* dshift,
+                                                void* workspace, size_t workspace_bytes) {
+  RG_TRY(check_norm(desc));
+  if (!dy || !sum || !dx || !gain || !stats) return fail(RINGADA_E_INVALID, "dy, sum, gain, stats or dx is NULL");
+  const int dt = desc->dtype;
+  const int64_t n = desc->rows, d = desc->d;
+  NormArgs a = norm_sizes(*desc);
+  RG_TRY(check_rows(dt, "dy", *dy, n, d, false, a.dy.p, a.dy.t));
+  if (dskip) RG_TRY(check_rows(dt, "dskip", *dskip, n, d, false, a.dskip.p, a.dskip.t));
+  RG_TRY(check_rows(dt, "sum", *sum, n, d, false, a.s.p, a.s.t));
+  RG_TRY(check_rows(dt, "dx", *dx, n, d, true, a.dx.p, a.dx.t));
+  RG_TRY(check_param(dt, "gain", gain));
+  if ((reinterpret_cast<uintptr_t>(stats) & 7u) || ((reinterpret_cast<uintptr_t>(dgain) | reinterpret_cast<uintptr_t>(dshift)) & 3u))
+    return fail(RINGADA_E_INVALID, "stats, dgain or dshift is misaligned");
+  const Region all[8] = {rows_region("dy", dt, a.dy.p, a.dy.t, n, d), rows_region("dskip", dt, a.dskip.p, a.dskip.t, n, d),
+                         rows_region("sum", dt, a.s.p, a.s.t, n, d), flat("gain", gain, (size_t)d * elem_bytes(dt)),
+                         flat("stats", stats, (size_t)n * 8), rows_region("dx", dt, a.dx.p, a.dx.t, n, d),
+                         flat("dgain", dgain, (size_t)d * 4), flat("dshift", dshift, (size_t)d * 4)};
+  const bool same[5] = {true, true, true, false, false};
+  RG_TRY(check_apart_or_same(all, same, 5, 8));
+  a.groups = norm_groups(dt, n, desc->d);
+  const size_t need = dgain || dshift ? (size_t)a.groups * 2 * d * 4 : 0;
+  RG_TRY(check_workspace(workspace, workspace_bytes, need, all, 8));
+  a.gain = gain;
+  a.stats = reinterpret_cast<float2*>(const_cast<float*>(stats));
+  a.dgain = dgain;
+  a.dshift = dshift;
+  a.part = need ? static_cast<float*>(workspace) : nullptr;
+  RG_HIP(launch_norm_bwd(dt, a, static_cast<hipStream_t>(stream)));
+  return RINGADA_OK;
+}
+
+// ================================================================ rotary embedding
+static ringada_status check_rotary(const ringada_rotary_desc* D, int& pairs) {
+  if (!D) return fail(RINGADA_E_INVALID, "desc is NULL");
+  if (D->dtype != RINGADA_F32 && D->dtype != RINGADA_BF16) return fail(RINGADA_E_INVALID, "unknown dtype %d", D->dtype);
+  if (D->batch < 1 || D->rows < 1 || D->n_heads < 1 || D->n_kv_heads < 0 || D->d_head < 2)
+    return fail(RINGADA_E_INVALID, "sizes must be positive (n_kv_heads: or 0, d_head: at least 2)");
+  if (D->n_axes < 1 || D->n_axes > 4) return fail(RINGADA_E_INVALID, "n_axes must be in [1, 4]");
+  int64_t sum = 0;
+  for (int i = 0; i < D->n_axes; ++i) {
+    if (D->section[i] < 1) return fail(RINGADA_E_INVALID, "every axis turns at least one pair");
+    sum += D->section[i];
+  }
+  if (2 * sum > D->d_head) return fail(RINGADA_E_INVALID, "the sections hold %lld pairs, a head of %d has %d", (long long)sum,
+                                       D->d_head, D->d_head / 2);
+  if (D->d_head > 2 * ROTARY_MAX_PAIRS) return fail(RINGADA_E_UNSUPPORTED, "d_head above %d", 2 * ROTARY_MAX_PAIRS);
+  if (D->n_heads > 2048 || D->n_kv_heads > 2048) return fail(RINGADA_E_UNSUPPORTED, "more than 2048 heads");
+  if ((int64_t)D->batch * D->rows >= (1 << 24)) return fail(RINGADA_E_UNSUPPORTED, "2^24 rows or more");
+  pairs = (int)sum;
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_rotary(void* stream, const ringada_rotary_desc* desc, const ringada_view* q,
+                                         const ringada_view* k, const int32_t* positions, const double* freq,
+                                         const ringada_view* q_out, const ringada_view* k_out) {
+  int pairs = 0;
+  RG_TRY(check_rotary(desc, pairs));
+  if (!q || !q_out || !positions || !freq) return fail(RINGADA_E_INVALID, "q, q_out, positions or freq is NULL");
+  const bool has_k = desc->n_kv_heads > 0;
+  if ((k != nullptr) != has_k || (k_out != nullptr) != has_k)
+    return fail(RINGADA_E_INVALID, "k and k_out must be given exactly when n_kv_heads > 0");
+  if ((reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(freq) & 7u))
+    return fail(RINGADA_E_INVALID, "positions or freq is misaligned");
+  ringada_attn_desc D{};  // what check_view and region look at
+  D.dtype = desc->dtype;
+  D.batch = desc->batch;
+  D.d_head = desc->d_head;
+  RotaryArgs a{};
+  a.B = desc->batch; a.S = desc->rows; a.H = desc->n_heads; a.Hkv = desc->n_kv_heads; a.dh = desc->d_head;
+  a.pairs = pairs;
+  a.axes = desc->n_axes;
+  for (int i = 0; i < desc->n_axes; ++i) a.end[i] = (i ? a.end[i - 1] : 0) + desc->section[i];
+  a.inverse = desc->inverse != 0;
+  RG_TRY(check_view(D, "q", *q, a.S, a.H, false, a.q));
+  RG_TRY(check_view(D, "q_out", *q_out, a.S, a.H, true, a.oq));
+  Region all[6] = {flat("positions", positions, (size_t)a.axes * a.B * a.S * 4), flat("freq", freq, (size_t)pairs * 8),
+                   region("q", D, a.q, a.S, a.H), flat("k", nullptr, 0), region("q_out", D, a.oq, a.S, a.H),
+                   flat("k_out", nullptr, 0)};
+  if (has_k) {
+    RG_TRY(check_view(D, "k", *k, a.S, a.Hkv, false, a.k));
+    RG_TRY(check_view(D, "k_out", *k_out, a.S, a.Hkv, true, a.ok));
+    all[3] = region("k", D, a.k, a.S, a.Hkv);
+    all[5] = region("k_out", D, a.ok, a.S, a.Hkv);
+  }
+  // q_out may be q and k_out may be k
+  for (int i = 4; i < 6; ++i)
+    for (int j = 0; j < i; ++j) {
+      if (j == i - 2 && same_tensor(all[i], all[j])) continue;
+      if (overlap(all[i], all[j])) return fail(RINGADA_E_INVALID, "%s overlaps %s", all[i].name, all[j].name);
+    }
+  a.pos = positions;
+  a.freq = freq;
+  RG_HIP(launch_rotary(desc->dtype, a, static_cast<hipStream_t>(stream)));
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_rotary_frequencies(int32_t n_axes, const int32_t* section, double theta, int32_t shared,
+                                                     double* freq) {
+  if (!section || !freq) return fail(RINGADA_E_INVALID, "section or freq is NULL");
+  if (n_axes < 1 || n_axes > 4) return fail(RINGADA_E_INVALID, "n_axes must be in [1, 4]");
+  if (!(theta > 0.) || !isfinite(theta)) return fail(RINGADA_E_INVALID, "theta must be positive and finite");
+  int64_t pairs = 0;
+  for (int i = 0; i < n_axes; ++i) {
+    if (section[i] < 1 || section[i] > ROTARY_MAX_PAIRS) return fail(RINGADA_E_INVALID, "a section out of range");
+    pairs += section[i];
+  }
+  if (pairs > ROTARY_MAX_PAIRS) return fail(RINGADA_E_INVALID, "more than %d pairs", ROTARY_MAX_PAIRS);
+  for (int i = 0, at = 0; i < n_axes; ++i)
+    for (int j = 0; j < section[i]; ++j, ++at)
+      freq[at] = pow(theta, shared ? -(double)at / (double)pairs : -(double)j / section[i]);
+  return RINGADA_OK;
+}
+
+// ================================================================ vocabulary head
+static ringada_status check_vocab(const ringada_vocab_desc* D) {
+  if (!D) return fail(RINGADA_E_INVALID, "desc is NULL");
+  if (D->dtype != RINGADA_F32 && D->dtype != RINGADA_BF16) return fail(RINGADA_E_INVALID, "unknown dtype %d", D->dtype);
+  if (D->rows < 1 || D->d < 1 || D->vocab < 1) return fail(RINGADA_E_INVALID, "sizes must be positive");
+  if (D->dtype == RINGADA_BF16 && D->d % 8) return fail(RINGADA_E_UNSUPPORTED, "bf16 path: d must be a multiple of 8 (got %d)", D->d);
+  if (D->d > 16384) return fail(RINGADA_E_UNSUPPORTED, "d above 16384");
+  if (D->vocab > (1 << 22)) return fail(RINGADA_E_UNSUPPORTED, "more than 2^22 classes");
+  if (D->rows > (1 << 23)) return fail(RINGADA_E_UNSUPPORTED, "more than 2^23 rows");
+  return RINGADA_OK;
+}
+static ringada_status check_matrix(int dtype, const char* name, const ringada_rows& v, int64_t rows, int64_t d, bool writes,
+                                   void*& data, long& row) {
+  RG_TRY(check_rows(dtype, name, v, rows, d, writes, data, row));
+  if (rows > 1 && row < d) return fail(RINGADA_E_INVALID, "%s: row stride below d", name);
+  if (row >= (1 << 24)) return fail(RINGADA_E_UNSUPPORTED, "%s: row stride above 2^24 elements", name);
+  if (dtype == RINGADA_BF16 && ((reinterpret_cast<uintptr_t>(data) & 15u) || (row & 7)))
+    return fail(RINGADA_E_INVALID, "%s: bf16 rows need 16-byte aligned data and a stride that is a multiple of 8", name);
+  return RINGADA_OK;
+}
+static VocabArgs vocab_sizes(const ringada_vocab_desc& D) {
+  VocabArgs a{};
+  a.n = D.rows;
+  a.d = D.d;
+  a.V = D.vocab;
+  return a;
+}
+
+extern "C" ringada_status ringada_vocab_plan(const ringada_vocab_desc* desc, size_t* forward_bytes, size_t* train_bytes,
+                                             size_t* next_bytes) {
+  RG_TRY(check_vocab(desc));
+  VocabArgs a = vocab_sizes(*desc);
+  if (forward_bytes) *forward_bytes = vocab_layout(desc->dtype, a, false, false, nullptr);
+  if (train_bytes) *train_bytes = vocab_layout(desc->dtype, a, true, false, nullptr);
+  if (next_bytes) *next_bytes = vocab_layout(desc->dtype, a, false, true, nullptr);
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_vocab_ce(void* stream, const ringada_vocab_desc* desc, const ringada_vocab_tensors* t,
+                                           void* workspace, size_t workspace_bytes) {
+  RG_TRY(check_vocab(desc));
+  if (!t) return fail(RINGADA_E_INVALID, "tensors is NULL");
+  if (!t->labels || !t->loss || !t->lse) return fail(RINGADA_E_INVALID, "labels, loss or lse is NULL");
+  const bool grads = t->dh.data || t->dw.data;
+  if (grads != (t->dloss != nullptr)) return fail(RINGADA_E_INVALID, "dloss must be given exactly when a gradient is wanted");
+  const uintptr_t words = reinterpret_cast<uintptr_t>(t->labels) | reinterpret_cast<uintptr_t>(t->loss) |
+                          reinterpret_cast<uintptr_t>(t->lse) | reinterpret_cast<uintptr_t>(t->dloss);
+  if (words & 3u) return fail(RINGADA_E_INVALID, "labels, loss, lse or dloss is misaligned");
+  const int dt = desc->dtype;
+  const int64_t n = desc->rows, d = desc->d, V = desc->vocab;
+  VocabArgs a = vocab_sizes(*desc);
+  void* p;
+  RG_TRY(check_matrix(dt, "h", t->h, n, d, false, p, a.ldh));
+  a.h = p;
+  RG_TRY(check_matrix(dt, "w", t->w, V, d, false, p, a.ldw));
+  a.w = p;
+  if (t->dh.data) RG_TRY(check_matrix(dt, "dh", t->dh, n, d, true, a.dh, a.lddh));
+  if (t->dw.data) RG_TRY(check_matrix(dt, "dw", t->dw, V, d, true, a.dw, a.lddw));
+  const Region all[8] = {rows_region("h", dt, a.h, a.ldh, n, d), rows_region("w", dt, a.w, a.ldw, V, d),
+                         flat("labels", t->labels, (size_t)n * 4), flat("dloss", t->dloss, (size_t)n * 4),
+                         flat("loss", t->loss, (size_t)n * 4), flat("lse", t->lse, (size_t)n * 4),
+                         rows_region("dh", dt, a.dh, a.lddh, n, d), rows_region("dw", dt, a.dw, a.lddw, V, d)};
+  RG_TRY(check_apart(all, 4, 8));
+  RG_TRY(check_workspace(workspace, workspace_bytes, vocab_layout(dt, a, grads, false, nullptr), all, 8));
+  vocab_layout(dt, a, grads, false, workspace);
+  a.labels = t->labels;
+  a.dloss = t->dloss;
+  a.loss = t->loss;
+  a.lse = t->lse;
+  RG_HIP(launch_vocab(dt, a, static_cast<hipStream_t>(stream)));
+  return RINGADA_OK;
+}
+
+extern "C" ringada_status ringada_vocab_next(void* stream, const ringada_vocab_desc* desc, const ringada_rows* h,
+                                             const ringada_rows* w, int32_t* token, float* logprob, void* workspace,
+                                             size_t workspace_bytes) {
+  RG_TRY(check_vocab(desc));
+  if (!h || !w || !token || !logprob) return fail(RINGADA_E_INVALID, "h, w, token or logprob is NULL");
+  if ((reinterpret_cast<uintptr_t>(token) | reinterpret_cast<uintptr_t>(logprob)) & 3u)
+    return fail(RINGADA_E_INVALID, "token or logprob is misaligned");
+  const int dt = desc->dtype;
+  const int64_t n = desc->rows, d = desc->d, V = desc->vocab;
+  VocabArgs a = vocab_sizes(*desc);
+  void* p;
+  RG_TRY(check_matrix(dt, "h", *h, n, d, false, p, a.ldh));
+  a.h = p;
+  RG_TRY(check_matrix(dt, "w", *w, V, d, false, p, a.ldw));
+  a.w = p;
+  const Region all[4] = {rows_region("h", dt, a.h, a.ldh, n, d), rows_region("w", dt, a.w, a.ldw, V, d),
+                         flat("token", token, (size_t)n * 4), flat("logprob", logprob, (size_t)n * 4)};
+  RG_TRY(check_apart(all, 2, 4));
+  RG_TRY(check_workspace(workspace, workspace_bytes, vocab_layout(dt, a, false, true, nullptr), all, 4));
+  vocab_layout(dt, a, false, true, workspace);
+  a.token = token;
+  a.logprob = logprob;
+  RG_HIP(launch_vocab(dt, a, static_cast<hipStream_t>(stream)));
   return RINGADA_OK;
 }
