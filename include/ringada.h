@@ -500,7 +500,7 @@ typedef struct {
 } ringada_vocab_desc;
 
 /* h, dh [rows, d]; w, dw [vocab, d] in the stage dtype: a row per class, as in an embedding table, so that a tied one can be
- * passed (unlike the stages' [in, out] weights).  bf16: 16-byte aligned, strides multiples of 8. */
+ * passed (unlike the stages' [in, out] weights).  bf16: 16-byte aligned, strides multiples of 8; strides at most 2^22. */
 typedef struct {
   ringada_rows h, w;
   const int32_t* labels; /* [rows]; a row with a label outside [0, vocab) does not count */

@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libringada.so")
 SOURCES = ["k_gemm.hip", "k_attention.hip", "k_attn_masked.hip", "k_adapter.hip", "k_dropout.hip", "k_misc.hip",
-           "k_norm.hip", "k_rotary.hip", "k_vocab.hip", "operators.hip", "stage.hip"]
+           "k_norm.hip", "k_rotary.hip", "k_vocab.hip",
+           "k_vocab_mm.hip", "operators.hip", "stage.hip"]
 ARCH = "gfx950"
 
 

@@ -15,32 +15,9 @@
 // operations instead of 6.
 #include "common.h"
 #include "kernels.h"
+#include "vocab_peak.h"
 
 namespace rg {
-
-constexpr float LOG2E = 1.4426950408889634f;
-
-// exp(x) of a difference to a maximum, x <= 0
-__device__ __forceinline__ float exp_below(float x) { return __builtin_amdgcn_exp2f(x * LOG2E); }
-
-// (maximum, sum of exp(s - maximum)) of a run of columns, and the lowest column that has the maximum
-struct Peak {
-  float m, l;
-  int at;
-};
-__device__ __forceinline__ Peak join(Peak a, Peak b) {
-  const float m = fmaxf(a.m, b.m), z = m == -INFINITY ? 0.f : m;
-  Peak r;
-  r.m = m;
-  r.l = a.l * exp_below(a.m - z) + b.l * exp_below(b.m - z);
-  r.at = a.m > b.m ? a.at : b.m > a.m ? b.at : min(a.at, b.at);
-  return r;
-}
-
-// rows of a piece that count
-__device__ __forceinline__ int piece_rows(const VocabArgs& a) {
-  return a.count ? max(0, min(*a.count - a.row0, a.R)) : a.rows;
-}
 
 // ---------------------------------------------------------------- rows that count
 // One workgroup: a stable compaction of the labels, 1024 at a time.
@@ -98,17 +75,14 @@ __global__ __launch_bounds__(256) void vocab_gather_k(VocabArgs a) {
 // ---------------------------------------------------------------- products in fp32
 // C[m][n] = sum_k A(m, k) B(n, k) on 128 x 128 tiles: registers -> LDS [k][m], MFMA 32x32x2 f32, four waves of 64 x 64.
 // KA: A is [M][K], else [K][M]; KB likewise.
-enum class Prod { Stats, Logits, Dh, Dw };
-
-template <typename T>
-__device__ __forceinline__ void ld8_any(const T* p, int valid, float v[8]) {
+__device__ __forceinline__ void ld8_any(const float* p, int valid, float v[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < valid ? St<T>::ld(p, i) : 0.f;
+  for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.f;
 }
 
-template <typename TA, typename TB, typename TO, bool KA, bool KB, Prod E>
-__global__ __launch_bounds__(256) void vocab_gemm_any_k(VocabArgs a, const TA* A, long lda, const TB* B, long ldb, int M0,
-                                                        int N, int K0) {
+template <bool KA, bool KB, Prod E>
+__global__ __launch_bounds__(256) void vocab_f32_k(VocabArgs a, const float* A, long lda, const float* B, long ldb, int M0,
+                                                   int N, int K0) {
   constexpr int BT = 128, BK = 16, PITCH = 160, CP = BT + 4;
   __shared__ __attribute__((aligned(16))) float smem[BT * CP];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
@@ -228,11 +202,10 @@ __global__ __launch_bounds__(256) void vocab_gemm_any_k(VocabArgs a, const TA* A
       if (m >= M || n >= N) continue;
       const float v = smem[r * CP + c];
       if constexpr (E == Prod::Dh) {
-        St<TO>::st(static_cast<TO*>(a.dh), (long)a.idx[a.row0 + m] * a.lddh + n, v);
+        static_cast<float*>(a.dh)[(long)a.idx[a.row0 + m] * a.lddh + n] = v;
       } else {
-        const float t = a.first ? v : a.dw_acc[(long)m * a.ld_acc + n] + v;
-        if (a.last) St<TO>::st(static_cast<TO*>(a.dw), (long)m * a.lddw + n, t);
-        else a.dw_acc[(long)m * a.ld_acc + n] = t;
+        float* o = static_cast<float*>(a.dw) + (long)m * a.lddw + n;
+        *o = a.first ? v : *o + v;
       }
     }
   }
@@ -285,7 +258,7 @@ __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
 }
 
 // ---------------------------------------------------------------- launches
-constexpr int VT = 128;  // columns of a logits tile
+constexpr int F32_TILE = 128;
 
 static long up(long x, long m) { return (x + m - 1) / m * m; }
 
@@ -294,7 +267,8 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   const long es = dtype == DT_BF16 ? 2 : 4, np = up(a.n, 64);
   a.Vp = (int)up(a.V, 64);
   a.dp = (int)up(a.d, 64);
-  a.tiles = (a.V + VT - 1) / VT;
+  a.bn = dtype == DT_BF16 ? vocab_mm_bn(a.n, a.V) : F32_TILE;
+  a.tiles = (a.V + a.bn - 1) / a.bn;
   // rows at a time: 2^29 logits (2 GiB), 2^24 partial sums; whole tiles of rows
   const long most = grads ? (1l << 29) / a.Vp : (1l << 24) / a.tiles;
   a.R = (int)(np <= most ? np : most / 256 * 256 > 256 ? most / 256 * 256 : 256);
@@ -318,47 +292,52 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   if (grads) {
     a.g_c = static_cast<float*>(take((size_t)a.n * 4));
     a.logits = static_cast<float*>(take((size_t)a.R * a.Vp * 4));
-    a.P = dtype == DT_BF16 ? take((size_t)a.R * a.Vp * 2) : a.logits;
-    if (dtype == DT_BF16 && a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
+    if (dtype == DT_BF16) {
+      a.P = take((size_t)a.R * a.Vp * 2);
+      a.dh_splits = vocab_dh_splits(a.R, a.d, a.V);
+      a.dh_part = a.dh_splits > 1 ? static_cast<float*>(take((size_t)a.dh_splits * a.R * a.d * 4)) : nullptr;
+      if (a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
+      a.ld_acc = a.d;
+    } else {
+      a.P = a.logits;
+    }
   }
   return at;
 }
 
+template <bool KA, bool KB, Prod E>
+static void go_f32(const VocabArgs& a, const void* A, long lda, const void* B, long ldb, int M, int N, int K, hipStream_t s) {
+  const unsigned wgs = ((M + F32_TILE - 1) / F32_TILE) * ((N + F32_TILE - 1) / F32_TILE);
+  RG_LAUNCH((vocab_f32_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, static_cast<const float*>(A), lda,
+            static_cast<const float*>(B), ldb, M, N, K);
+}
+
 template <typename T>
 static hipError_t vocab_t(VocabArgs a, hipStream_t s) {
+  constexpr bool low = sizeof(T) == 2;
   const bool grads = a.dh || a.dw;
   if (a.labels) RG_LAUNCH(vocab_scan_k, dim3(1), dim3(1024), 0, s, a);
   RG_LAUNCH(vocab_gather_k<T>, dim3((unsigned)up(a.n, 64)), dim3(256), 0, s, a);
   a.count = a.labels ? a.n_counted : nullptr;
-  const T* W = static_cast<const T*>(a.w);
-  if (sizeof(T) == 4) {
-    a.dw_acc = static_cast<float*>(a.dw);
-    a.ld_acc = a.lddw;
-  } else {
-    a.ld_acc = a.d;
-  }
   for (a.row0 = 0; a.row0 < a.n; a.row0 += a.R) {
     a.rows = a.n - a.row0 < a.R ? a.n - a.row0 : a.R;
     a.first = a.row0 == 0;
-    a.last = a.row0 + a.R >= a.n || sizeof(T) == 4;
-    const unsigned mt = (a.rows + VT - 1) / VT, nt = (a.d + VT - 1) / VT;
+    a.last = a.row0 + a.R >= a.n;
     const T* H = static_cast<const T*>(a.hc) + (long)a.row0 * a.dp;
-    if (grads)
-      RG_LAUNCH((vocab_gemm_any_k<T, T, T, true, true, Prod::Logits>), dim3(a.tiles * mt), dim3(256), 0, s, a, H, (long)a.dp,
-                W, a.ldw, 0, a.V, a.d);
-    else
-      RG_LAUNCH((vocab_gemm_any_k<T, T, T, true, true, Prod::Stats>), dim3(a.tiles * mt), dim3(256), 0, s, a, H, (long)a.dp, W,
-                a.ldw, 0, a.V, a.d);
+    if constexpr (low) launch_vocab_logits_bf16(a, grads, s);
+    else if (grads) go_f32<true, true, Prod::Logits>(a, H, a.dp, a.w, a.ldw, a.rows, a.V, a.d, s);
+    else go_f32<true, true, Prod::Stats>(a, H, a.dp, a.w, a.ldw, a.rows, a.V, a.d, s);
     RG_LAUNCH(vocab_rows_k, dim3((a.rows + 3) / 4), dim3(256), 0, s, a);
     if (!grads) continue;
-    const T* P = static_cast<const T*>(a.P);
     RG_LAUNCH(vocab_p_k<T>, dim3((unsigned)up(a.rows, 64), (a.Vp + 1023) / 1024), dim3(256), 0, s, a);
-    if (a.dh)
-      RG_LAUNCH((vocab_gemm_any_k<T, T, T, true, false, Prod::Dh>), dim3(nt * mt), dim3(256), 0, s, a, P, (long)a.Vp, W, a.ldw,
-                0, a.d, a.V);
-    if (a.dw)
-      RG_LAUNCH((vocab_gemm_any_k<T, T, T, false, false, Prod::Dw>), dim3(nt * a.tiles), dim3(256), 0, s, a, P,
-                (long)a.Vp, H, (long)a.dp, a.V, a.d, 0);
+    if (a.dh) {
+      if constexpr (low) launch_vocab_dh_bf16(a, s);
+      else go_f32<true, false, Prod::Dh>(a, a.P, a.Vp, a.w, a.ldw, a.rows, a.d, a.V, s);
+    }
+    if (a.dw) {
+      if constexpr (low) launch_vocab_dw_bf16(a, s);
+      else go_f32<false, false, Prod::Dw>(a, a.P, a.Vp, H, a.dp, a.V, a.d, 0, s);
+    }
   }
   return hipGetLastError();
 }

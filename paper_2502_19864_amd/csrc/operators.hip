@@ -555,7 +555,7 @@ static ringada_status check_matrix(int dtype, const char* name, const ringada_ro
                                    void*& data, long& row) {
   RG_TRY(check_rows(dtype, name, v, rows, d, writes, data, row));
   if (rows > 1 && row < d) return fail(RINGADA_E_INVALID, "%s: row stride below d", name);
-  if (row >= (1 << 24)) return fail(RINGADA_E_UNSUPPORTED, "%s: row stride above 2^24 elements", name);
+  if (row > (1 << 22)) return fail(RINGADA_E_UNSUPPORTED, "%s: row stride above 2^22 elements", name);
   if (dtype == RINGADA_BF16 && ((reinterpret_cast<uintptr_t>(data) & 15u) || (row & 7)))
     return fail(RINGADA_E_INVALID, "%s: bf16 rows need 16-byte aligned data and a stride that is a multiple of 8", name);
   return RINGADA_OK;
