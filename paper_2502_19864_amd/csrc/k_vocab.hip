@@ -13,6 +13,8 @@
 // The logits of a piece of the rows are held in fp32 while they are needed.  Pieces of the vocabulary would need
 // no more memory, but lse needs all columns before P has any: the product h w^T would run twice, 8 n V d
 // operations instead of 6.
+#include <type_traits>
+
 #include "common.h"
 #include "kernels.h"
 #include "vocab_peak.h"
@@ -20,81 +22,185 @@
 namespace rg {
 
 // ---------------------------------------------------------------- rows that count
-// One workgroup: a stable compaction of the labels, 1024 at a time.
-__global__ __launch_bounds__(1024) void vocab_scan_k(VocabArgs a) {
-  __shared__ int wsum[16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int base = 0;
-  for (int n0 = 0; n0 < a.n; n0 += 1024) {
-    const int n = n0 + tid;
-    const int lab = n < a.n ? a.labels[n] : -1;
-    const bool in = lab >= 0 && lab < a.V;
-    const uint64_t vote = __ballot(in);
-    if (lane == 0) wsum[wave] = __popcll(vote);
-    __syncthreads();
-    int before = base, all = 0;
+constexpr int PICK_ROWS = 8;       // of h per workgroup
+constexpr int PICK_DIRECT = 16384; // labels that a workgroup counts by itself; beyond, blocks of 1024 are counted first
+
+__device__ __forceinline__ bool counts(const VocabArgs& a, int lab) { return lab >= 0 && lab < a.V; }
+
+// sum over the 256 threads of a workgroup; red: 4 ints
+__device__ __forceinline__ int wg_sum(int v, int* red) {
 #pragma unroll
-    for (int w = 0; w < 16; ++w) {
-      before += w < wave ? wsum[w] : 0;
-      all += wsum[w];
-    }
-    if (in) {
-      const int at = before + __popcll(vote & ((1ull << lane) - 1));
-      a.idx[at] = n;
-      a.lab_c[at] = lab;
-      if (a.dloss) a.g_c[at] = a.dloss[n];
-    } else if (n < a.n) {
-      a.loss[n] = 0.f;
-      a.lse[n] = 0.f;
-    }
-    base += all;
-    __syncthreads();
-  }
-  if (tid == 0) *a.n_counted = base;
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0] + red[1] + red[2] + red[3];
+  __syncthreads();
+  return v;
 }
 
-// hc[i] = h[idx[i]], zeros past d and past the rows that count up to a multiple of 64; the gradient's rows that do
-// not count are zeros.  One workgroup per row.
-template <typename T>
-__global__ __launch_bounds__(256) void vocab_gather_k(VocabArgs a) {
-  const int i = blockIdx.x, cnt = a.labels ? *a.n_counted : a.n;
-  if (i < ((cnt + 63) & ~63)) {
-    const T* src = static_cast<const T*>(a.h) + (i < cnt ? (long)(a.labels ? a.idx[i] : i) : 0) * a.ldh;
-    T* dst = static_cast<T*>(a.hc) + (long)i * a.dp;
-    for (int k = threadIdx.x; k < a.dp; k += 256) dst[k] = i < cnt && k < a.d ? src[k] : T(0);
+__global__ __launch_bounds__(256) void vocab_count_k(VocabArgs a) {
+  __shared__ int red[4];
+  int v = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int n = blockIdx.x * 1024 + i * 256 + threadIdx.x;
+    v += n < a.n && counts(a, a.labels[n]) ? 1 : 0;
   }
-  if (a.dh && i < a.n) {
-    const int lab = a.labels[i];
-    if (lab < 0 || lab >= a.V) {
-      T* dst = static_cast<T*>(a.dh) + (long)i * a.lddh;
-      for (int k = threadIdx.x; k < a.d; k += 256) dst[k] = T(0);
+  v = wg_sum(v, red);
+  if (threadIdx.x == 0) a.block_count[blockIdx.x] = v;
+}
+
+// A stable compaction: hc[i] is the i-th row that counts, zeros past d; without labels, every row.  A workgroup
+// takes PICK_ROWS rows of h and counts the labels before them.  The results of rows that do not count are written here.
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_pick_k(VocabArgs a, bool wide) {
+  __shared__ int red[4];
+  const int r0 = blockIdx.x * PICK_ROWS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = r0;
+  if (a.labels) {
+    int v = 0, n = threadIdx.x;
+    if (a.block_count) {
+      for (int b = threadIdx.x; b < r0 / 1024; b += 256) v += a.block_count[b];
+      n += r0 / 1024 * 1024;
+    }
+    for (; n < r0; n += 256) v += counts(a, a.labels[n]) ? 1 : 0;
+    before = wg_sum(v, red);
+  }
+  for (int i = wave; i < PICK_ROWS && r0 + i < a.n; i += 4) {
+    const int n = r0 + i;
+    int at = n;
+    if (a.labels) {
+      const int lab = lane <= i ? a.labels[r0 + lane] : -1;  // the rows up to this one
+      const uint64_t vote = __ballot(lane <= i && counts(a, lab));
+      const int mine = __shfl(lab, i);
+      at = before + __popcll(vote) - 1;
+      if (n == a.n - 1 && lane == 0) *a.n_counted = at + 1;
+      if (!counts(a, mine)) {
+        if (lane == 0) a.loss[n] = a.lse[n] = 0.f;
+        if (a.dh) {
+          T* dst = static_cast<T*>(a.dh) + (long)n * a.lddh;
+          for (int k = lane; k < a.d; k += 64) dst[k] = T(0);
+        }
+        continue;
+      }
+      if (lane == 0) {
+        a.idx[at] = n;
+        a.lab_c[at] = mine;
+        if (a.dloss) a.g_c[at] = a.dloss[n];
+      }
+    }
+    const T* src = static_cast<const T*>(a.h) + (long)n * a.ldh;
+    T* dst = static_cast<T*>(a.hc) + (long)at * a.dp;
+    constexpr int E = 16 / sizeof(T);
+    if (wide) {
+      for (int k = lane * E; k < a.dp; k += 64 * E)
+        *reinterpret_cast<uint4*>(dst + k) = k < a.d ? *reinterpret_cast<const uint4*>(src + k) : make_uint4(0, 0, 0, 0);
+    } else {
+      for (int k = lane; k < a.dp; k += 64) dst[k] = k < a.d ? src[k] : T(0);
     }
   }
 }
 
 // ---------------------------------------------------------------- products in fp32
-// C[m][n] = sum_k A(m, k) B(n, k) on 128 x 128 tiles: registers -> LDS [k][m], MFMA 32x32x2 f32, four waves of 64 x 64.
-// KA: A is [M][K], else [K][M]; KB likewise.
-__device__ __forceinline__ void ld8_any(const float* p, int valid, float v[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.f;
+// C[m][n] = sum_k A(m, k) B(n, k) by MFMA 32x32x2 f32.  KA: A is [M][K], else [K][M]; KB likewise.  The logits' tiles leave
+// (maximum, sum); dh's k (the vocabulary) is dealt to several workgroups where its tiles are few.
+//
+// Sums over a vocabulary are long: 300,000 terms in one chain of the matrix unit were off by 9 sqrt(n) roundings. So
+// a chain ends after LONG terms, and the chains are added up.
+struct F32Product {
+  const float* A; long lda;
+  const float* B; long ldb;
+  int M, N, K;     // M of dw, k of the logits and of dh; the others are the rows that count
+  bool vb;         // B's rows are 16-byte aligned (A's always are)
+  int slots;       // dh: workgroups of one round
+};
+// shares of dh's k per tile, each of 256 columns at least
+__device__ __forceinline__ int f32_splits(const F32Product& p, int tiles) {
+  return max(1, min(min(p.slots / tiles, p.K / 256), 64));
 }
 
+__device__ __forceinline__ void ld8_f32(const float* p, int valid, bool wide, float v[8]) {
+  if (wide && valid >= 8) {
+    *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
+    *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(p + 4);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.f;
+  }
+}
+
+// the tile's sums, cf[row * CP + column], into what the product is for
+template <int BT, int CP, Prod E>
+__device__ __forceinline__ void f32_epilogue(const VocabArgs& a, const F32Product& p, const float* cf, int M, int N, int m0, int n0,
+                                             int tile, int split, int splits, int tiles) {
+  const int tid = threadIdx.x;
+  if constexpr (E == Prod::Stats || E == Prod::Logits) {
+    constexpr int TPR = 256 / BT, CPT = BT / TPR;  // threads per row, columns of each: t, t + TPR, ..
+    const int row = tid / TPR, t = tid % TPR, m = m0 + row;
+    const int lab = a.lab_c && m < M ? a.lab_c[a.row0 + m] : -1;
+    Peak q{-INFINITY, 0.f, INT32_MAX};
+#pragma unroll 8
+    for (int i = 0; i < CPT; ++i) {
+      const int c = i * TPR + t;
+      const float s = n0 + c < N ? cf[row * CP + c] : -INFINITY;
+      if (s > q.m) {
+        q.m = s;
+        q.at = n0 + c;
+      }
+      if (n0 + c == lab) a.target[a.row0 + m] = s;
+    }
+    const float z = q.m == -INFINITY ? 0.f : q.m;
+#pragma unroll 8
+    for (int i = 0; i < CPT; ++i) {
+      const int c = i * TPR + t;
+      if (n0 + c < N) q.l += exp_below(cf[row * CP + c] - z);
+    }
+#pragma unroll
+    for (int o = 1; o < TPR; o <<= 1) q = join(q, Peak{__shfl_xor(q.m, o), __shfl_xor(q.l, o), __shfl_xor(q.at, o)});
+    if (m < M && t == 0) {
+      a.part[(long)m * a.tiles + n0 / BT] = make_float2(q.m, q.l);
+      if (a.part_at) a.part_at[(long)m * a.tiles + n0 / BT] = min(q.at, N - 1);
+    }
+    if constexpr (E == Prod::Logits)
+      for (int i = tid; i < BT * BT / 4; i += 256) {
+        const int r = i / (BT / 4), c = i % (BT / 4) * 4;
+        if (m0 + r < M && n0 + c < a.Vp)
+          *reinterpret_cast<float4*>(a.logits + (long)(m0 + r) * a.Vp + n0 + c) = *reinterpret_cast<const float4*>(cf + r * CP + c);
+      }
+  } else {
+    float* part = a.dh_part + ((long)split * tiles + tile) * (BT * BT);
+    for (int i = tid; i < BT * BT; i += 256) {
+      const int r = i / BT, c = i % BT, m = m0 + r, n = n0 + c;
+      if (m >= M || n >= N) continue;
+      const float v = cf[r * CP + c];
+      if constexpr (E == Prod::Dh) {
+        if (splits > 1) part[i] = v;
+        else static_cast<float*>(a.dh)[(long)a.idx[a.row0 + m] * a.lddh + n] = v;
+      } else {
+        float* o = static_cast<float*>(a.dw) + (long)m * a.lddw + n;
+        *o = a.first ? v : *o + v;
+      }
+    }
+  }
+}
+
+// 128 x 128 tiles: registers -> LDS, four waves of 64 x 64.  LDS keeps [k][row] with a pitch that puts the two k of an MFMA in
+// different banks.
 template <bool KA, bool KB, Prod E>
-__global__ __launch_bounds__(256) void vocab_f32_k(VocabArgs a, const float* A, long lda, const float* B, long ldb, int M0,
-                                                   int N, int K0) {
-  constexpr int BT = 128, BK = 16, PITCH = 160, CP = BT + 4;
+__global__ __launch_bounds__(256) void vocab_f32_k(VocabArgs a, F32Product p) {
+  constexpr int BT = 128, BK = 16, PITCH = 160, CP = BT + 4, LONG = 1024;
   __shared__ __attribute__((aligned(16))) float smem[BT * CP];
+  static_assert(4 * BK * PITCH <= BT * CP, "two buffers");
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
   const int cnt = piece_rows(a);
-  const int M = E == Prod::Dw ? M0 : cnt, K = E == Prod::Dw ? cnt : K0;
-  const int tn = (N + BT - 1) / BT, m0 = (int)(blockIdx.x / tn) * BT, n0 = (int)(blockIdx.x % tn) * BT;
-  if (m0 >= M) return;
-  float* sa = smem;
-  float* sb = smem + BK * PITCH;
-  // Sums over a vocabulary are long, and the matrix unit's additions lean to one side: 300,000 terms in one chain were off by
-  // 1e-3 of a gradient beside a label's large term.  So a chain ends after LONG, and the chains are added up.
-  constexpr int LONG = 1024;
+  const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
+  const int tn = (N + BT - 1) / BT, tiles = (M + BT - 1) / BT * tn;
+  const int splits = E == Prod::Dh && tiles ? f32_splits(p, tiles) : 1;
+  if ((int)blockIdx.x >= tiles * splits) return;
+  const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
+  const int m0 = tile / tn * BT, n0 = tile % tn * BT;
+  const int Kall = E == Prod::Dw ? cnt : p.K, nkt = (Kall + BK - 1) / BK;
+  const int kb = (int)((long)nkt * split / splits) * BK, K = min(Kall, (int)((long)nkt * (split + 1) / splits) * BK);
   f32x16 acc[2][2], sum[2][2];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -114,115 +220,177 @@ __global__ __launch_bounds__(256) void vocab_f32_k(VocabArgs a, const float* A, 
         }
   };
   float ra[8], rb[8];
-  auto fetch = [&](int k0) {
-    if constexpr (KA) {
-      const int m = m0 + (tid >> 1), k = k0 + (tid & 1) * 8;
-      ld8_any(A + (long)min(m, M - 1) * lda + k, m < M ? K - k : 0, ra);
+  // one operand's 8 elements of this thread: along k for [rows][k], along the rows else
+  auto fetch1 = [&](auto KM, const float* X, long ld, int r0, int rows, bool wide, int k0, float (&v)[8]) {
+    if constexpr (decltype(KM)::value) {
+      const int r = r0 + (tid >> 1), k = k0 + (tid & 1) * 8;
+      ld8_f32(X + (long)min(r, rows - 1) * ld + k, r < rows ? K - k : 0, wide, v);
     } else {
-      const int k = k0 + (tid >> 4), m = m0 + (tid & 15) * 8;
-      ld8_any(A + (long)min(k, K - 1) * lda + m, k < K ? M - m : 0, ra);
-    }
-    if constexpr (KB) {
-      const int n = n0 + (tid >> 1), k = k0 + (tid & 1) * 8;
-      ld8_any(B + (long)min(n, N - 1) * ldb + k, n < N ? K - k : 0, rb);
-    } else {
-      const int k = k0 + (tid >> 4), n = n0 + (tid & 15) * 8;
-      ld8_any(B + (long)min(k, K - 1) * ldb + n, k < K ? N - n : 0, rb);
+      const int k = k0 + (tid >> 4), r = r0 + (tid & 15) * 8;
+      ld8_f32(X + (long)min(k, K - 1) * ld + r, k < K ? rows - r : 0, wide, v);
     }
   };
-  if (K > 0) fetch(0);
-  for (int k0 = 0; k0 < K; k0 += BK) {
-    __syncthreads();
+  auto fetch = [&](int k0) {
+    fetch1(std::integral_constant<bool, KA>{}, p.A, p.lda, m0, M, true, k0, ra);
+    fetch1(std::integral_constant<bool, KB>{}, p.B, p.ldb, n0, N, p.vb, k0, rb);
+  };
+  auto put1 = [&](auto KM, float* s, const float (&v)[8]) {
+    if constexpr (decltype(KM)::value) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if constexpr (KA) sa[((tid & 1) * 8 + i) * PITCH + (tid >> 1)] = ra[i];
-      else sa[(tid >> 4) * PITCH + (tid & 15) * 8 + i] = ra[i];
-      if constexpr (KB) sb[((tid & 1) * 8 + i) * PITCH + (tid >> 1)] = rb[i];
-      else sb[(tid >> 4) * PITCH + (tid & 15) * 8 + i] = rb[i];
+      for (int i = 0; i < 8; ++i) s[((tid & 1) * 8 + i) * PITCH + (tid >> 1)] = v[i];
+    } else {
+      float* d = s + (tid >> 4) * PITCH + (tid & 15) * 8;
+      *reinterpret_cast<float4*>(d) = *reinterpret_cast<const float4*>(v);
+      *reinterpret_cast<float4*>(d + 4) = *reinterpret_cast<const float4*>(v + 4);
     }
+  };
+  auto put = [&](int buf) {
+    put1(std::integral_constant<bool, KA>{}, smem + buf * 2 * BK * PITCH, ra);
+    put1(std::integral_constant<bool, KB>{}, smem + (buf * 2 + 1) * BK * PITCH, rb);
+  };
+  if (kb < K) {
+    fetch(kb);
+    put(0);
+    if (kb + BK < K) fetch(kb + BK);
     __syncthreads();
-    if (k0 + BK < K) fetch(k0 + BK);
+    int buf = 0;
+    for (int k0 = kb; k0 < K; k0 += BK, buf ^= 1) {
+      const float* sa = smem + buf * 2 * BK * PITCH + (lane >> 5) * PITCH + wm * 64 + (lane & 31);
+      const float* sb = smem + (buf * 2 + 1) * BK * PITCH + (lane >> 5) * PITCH + wn * 64 + (lane & 31);
 #pragma unroll
-    for (int k = 0; k < BK; k += 2) {
-      float fa[2], fb[2];
+      for (int k = 0; k < BK; k += 2) {
+        float fa[2], fb[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fa[i] = sa[(k + (lane >> 5)) * PITCH + wm * 64 + i * 32 + (lane & 31)];
-        fb[i] = sb[(k + (lane >> 5)) * PITCH + wn * 64 + i * 32 + (lane & 31)];
+        for (int i = 0; i < 2; ++i) {
+          fa[i] = sa[k * PITCH + i * 32];
+          fb[i] = sb[k * PITCH + i * 32];
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) acc[i][j] = mfma32_f32(fb[j], fa[i], acc[i][j]);
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = mfma32_f32(fb[j], fa[i], acc[i][j]);
+      if (k0 + BK < K) put(buf ^ 1);
+      if (k0 + 2 * BK < K) fetch(k0 + 2 * BK);
+      if ((k0 - kb + BK) % LONG == 0) settle();
+      __syncthreads();
     }
-    if ((k0 + BK) % LONG == 0) settle();
+    settle();
   }
-  settle();
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        smem[(wm * 64 + i * 32 + (lane & 31)) * CP + wn * 64 + j * 32 + 8 * (r / 4) + 4 * (lane >> 5) + r % 4] = sum[i][j][r];
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4*>(smem + (wm * 64 + i * 32 + (lane & 31)) * CP + wn * 64 + j * 32 + 8 * g + 4 * (lane >> 5)) =
+            make_float4(sum[i][j][4 * g], sum[i][j][4 * g + 1], sum[i][j][4 * g + 2], sum[i][j][4 * g + 3]);
   __syncthreads();
-  if constexpr (E == Prod::Stats || E == Prod::Logits) {
-    // two threads per row, 64 columns each
-    const int row = tid >> 1, m = m0 + row, c0 = (tid & 1) * 64;
-    const int lab = a.lab_c && m < M ? a.lab_c[a.row0 + m] : -1;
-    Peak p{-INFINITY, 0.f, n0 + c0 < N ? n0 + c0 : n0};
-    for (int c = c0; c < c0 + 64 && n0 + c < N; ++c) {
-      const float s = smem[row * CP + c];
-      if (s > p.m) {
-        p.m = s;
-        p.at = n0 + c;
-      }
-    }
-    const float z = p.m == -INFINITY ? 0.f : p.m;
-    for (int c = c0; c < c0 + 64 && n0 + c < N; ++c) {
-      const float s = smem[row * CP + c];
-      p.l += exp_below(s - z);
-      if (n0 + c == lab) a.target[a.row0 + m] = s;
-    }
-    const Peak q{__shfl_xor(p.m, 1), __shfl_xor(p.l, 1), __shfl_xor(p.at, 1)};
-    p = join(p, q);
-    if (m < M && (tid & 1) == 0) {
-      a.part[(long)m * a.tiles + n0 / BT] = make_float2(p.m, p.l);
-      if (a.part_at) a.part_at[(long)m * a.tiles + n0 / BT] = p.at;
-    }
-    if constexpr (E == Prod::Logits)
-      for (int i = tid; i < BT * BT; i += 256) {
-        const int r = i / BT, c = i % BT;
-        if (m0 + r < M && n0 + c < N) a.logits[(long)(m0 + r) * a.Vp + n0 + c] = smem[r * CP + c];
-      }
-  } else {
-    for (int i = tid; i < BT * BT; i += 256) {
-      const int r = i / BT, c = i % BT, m = m0 + r, n = n0 + c;
-      if (m >= M || n >= N) continue;
-      const float v = smem[r * CP + c];
-      if constexpr (E == Prod::Dh) {
-        static_cast<float*>(a.dh)[(long)a.idx[a.row0 + m] * a.lddh + n] = v;
+  f32_epilogue<BT, CP, E>(a, p, smem, M, N, m0, n0, tile, split, splits, tiles);
+}
+
+// 32 x 32 tiles for small products, where what counts is the latency of one chain on many CUs: fragments go from memory straight
+// to registers, the four waves take every fourth eight of k and are added up in LDS in their order.  Lane l
+// holds row l % 32; half l / 32 feeds k0 + 4 (l / 32) + j to the j-th MFMA, the same in both operands.
+template <bool KA, bool KB, Prod E>
+__global__ __launch_bounds__(256) void vocab_f32_small_k(VocabArgs a, F32Product p) {
+  constexpr int BT = 32, CP = BT + 4, PF = 4, LONG = 1024;
+  __shared__ __attribute__((aligned(16))) float red[4][BT * CP];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
+  const int cnt = piece_rows(a);
+  const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
+  const int tn = (N + BT - 1) / BT, tiles = (M + BT - 1) / BT * tn;
+  const int splits = E == Prod::Dh && tiles ? f32_splits(p, tiles) : 1;
+  if ((int)blockIdx.x >= tiles * splits) return;
+  const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
+  const int m0 = tile / tn * BT, n0 = tile % tn * BT;
+  const int Kall = E == Prod::Dw ? cnt : p.K, n8 = (Kall + 7) / 8;
+  const int kb = (int)((long)n8 * split / splits) * 8, K = min(Kall, (int)((long)n8 * (split + 1) / splits) * 8);
+  f32x16 acc, sum;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = sum[r] = 0.f;
+  auto load = [&](auto KM, const float* X, long ld, int r0, int rows, bool wide, int k, float (&v)[4]) {
+    const int r = r0 + l32;
+    if constexpr (decltype(KM)::value) {
+      const float* q = X + (long)min(r, rows - 1) * ld + k;
+      if (wide && k + 4 <= K) {
+        *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(q);
       } else {
-        float* o = static_cast<float*>(a.dw) + (long)m * a.lddw + n;
-        *o = a.first ? v : *o + v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = k + i < K ? q[i] : 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = k + i < K ? X[(long)(k + i) * ld + min(r, rows - 1)] : 0.f;
+    }
+  };
+  int done = 0;
+  for (int k0 = kb + wave * 8; k0 < K; k0 += 32 * PF) {
+    float fa[PF][4], fb[PF][4];
+#pragma unroll
+    for (int q = 0; q < PF; ++q) {  // past K: zeros
+      load(std::integral_constant<bool, KA>{}, p.A, p.lda, m0, M, true, k0 + q * 32 + half * 4, fa[q]);
+      load(std::integral_constant<bool, KB>{}, p.B, p.ldb, n0, N, p.vb, k0 + q * 32 + half * 4, fb[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < PF; ++q)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc = mfma32_f32(fb[q][j], fa[q][j], acc);
+    if ((done += 8 * PF) >= LONG) {
+      done = 0;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        sum[r] += acc[r];
+        acc[r] = 0.f;
       }
     }
   }
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+    *reinterpret_cast<float4*>(red[wave] + l32 * CP + 8 * g + 4 * half) =
+        make_float4(sum[4 * g] + acc[4 * g], sum[4 * g + 1] + acc[4 * g + 1], sum[4 * g + 2] + acc[4 * g + 2], sum[4 * g + 3] + acc[4 * g + 3]);
+  __syncthreads();
+  for (int i = tid; i < BT * BT; i += 256) {
+    const int at = i / BT * CP + i % BT;
+    red[0][at] = ((red[0][at] + red[1][at]) + red[2][at]) + red[3][at];
+  }
+  __syncthreads();
+  f32_epilogue<BT, CP, E>(a, p, red[0], M, N, m0, n0, tile, split, splits, tiles);
+}
+
+// dh of a piece from its splits' sums, in their order
+__global__ __launch_bounds__(256) void vocab_f32_dh_sum_k(VocabArgs a, F32Product p, int bt) {
+  const int cnt = piece_rows(a), m = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
+  if (m >= cnt || n >= p.N) return;
+  const int tn = (p.N + bt - 1) / bt, tiles = (cnt + bt - 1) / bt * tn, splits = f32_splits(p, tiles);
+  if (splits == 1) return;
+  const float* q = a.dh_part + (long)(m / bt * tn + n / bt) * bt * bt + (m % bt) * bt + n % bt;
+  float v = 0.f;
+#pragma unroll 8
+  for (int s = 0; s < splits; ++s) v += q[(long)s * tiles * bt * bt];
+  static_cast<float*>(a.dh)[(long)a.idx[a.row0 + m] * a.lddh + n] = v;
 }
 
 // ---------------------------------------------------------------- rows
-// One wave per row: its tiles' (maximum, sum) joined; loss and lse, or the token and its log-probability.
+// a row's tiles joined by the lanes of a wave
+__device__ __forceinline__ Peak join_wave(Peak p) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) p = join(p, Peak{__shfl_xor(p.m, o), __shfl_xor(p.l, o), __shfl_xor(p.at, o)});
+  return p;
+}
+
+// One wave per row: loss and lse, or the token and its log-probability.
 __global__ __launch_bounds__(256) void vocab_rows_k(VocabArgs a) {
   const int m = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (m >= piece_rows(a)) return;
   Peak p{-INFINITY, 0.f, INT32_MAX};
+#pragma unroll 4
   for (int t = lane; t < a.tiles; t += 64) {
     const float2 q = a.part[(long)m * a.tiles + t];
     p = join(p, Peak{q.x, q.y, a.part_at ? a.part_at[(long)m * a.tiles + t] : 0});
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) p = join(p, Peak{__shfl_xor(p.m, o), __shfl_xor(p.l, o), __shfl_xor(p.at, o)});
+  p = join_wave(p);
   if (lane) return;
   const float log_l = logf(p.l);
   if (a.token) {
@@ -231,43 +399,79 @@ __global__ __launch_bounds__(256) void vocab_rows_k(VocabArgs a) {
     return;
   }
   const int row = a.idx[a.row0 + m];
-  const float t = a.target[a.row0 + m], lse = p.m + log_l;
-  a.loss[row] = (p.m - t) + log_l;  // not lse - t: of a row that is sure of its label little is left
-  a.lse[row] = lse;
-  a.stat[m] = make_float2(lse, (p.m - t) + log_l);
+  a.loss[row] = (p.m - a.target[a.row0 + m]) + log_l;  // not lse - s: of a row that is sure of its label little is left
+  a.lse[row] = p.m + log_l;
 }
 
-// P of a piece from its logits, rounded once to the storage type; zeros past V and in the rows up to a multiple of 64
+// Loss and lse of a row, and its P from the logits, rounded once to the storage type; zeros past V and in the rows up to a
+// multiple of 64.  A workgroup takes 8192 columns of one row and joins the row's tiles by itself.
+constexpr int P_COLS = 8192;
 template <typename T>
 __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
-  const int m = blockIdx.x, cnt = piece_rows(a);
+  __shared__ Peak red[4];
+  const int m = blockIdx.x, cnt = piece_rows(a), tid = threadIdx.x;
   if (m >= ((cnt + 63) & ~63)) return;
   const bool in = m < cnt;
-  const float2 st = in ? a.stat[m] : make_float2(0.f, 0.f);
-  const float g = in ? a.g_c[a.row0 + m] : 0.f;
-  const int lab = in ? a.lab_c[a.row0 + m] : -1;
+  float lse = 0.f, loss = 0.f, g = 0.f;
+  int lab = -1;
+  if (in) {
+    Peak p{-INFINITY, 0.f, 0};
+    for (int t = tid; t < a.tiles; t += 256) {
+      const float2 q = a.part[(long)m * a.tiles + t];
+      p = join(p, Peak{q.x, q.y, 0});
+    }
+    p = join_wave(p);
+    if ((tid & 63) == 0) red[tid >> 6] = p;
+    __syncthreads();
+    p = join(join(red[0], red[1]), join(red[2], red[3]));
+    const float log_l = logf(p.l);
+    lse = p.m + log_l;
+    loss = (p.m - a.target[a.row0 + m]) + log_l;  // not lse - s: of a row that is sure of its label little is left
+    g = a.g_c[a.row0 + m];
+    lab = a.lab_c[a.row0 + m];
+    if (blockIdx.y == 0 && tid == 0) {
+      const int row = a.idx[a.row0 + m];
+      a.loss[row] = loss;
+      a.lse[row] = lse;
+    }
+  }
   const float* s = a.logits + (long)m * a.Vp;
   T* p = static_cast<T*>(a.P) + (long)m * a.Vp;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int v = blockIdx.y * 1024 + i * 256 + threadIdx.x;
-    if (v >= a.Vp) break;
-    const float x = in && v < a.V ? g * (v == lab ? expm1f(-st.y) : exp_below(s[v] - st.x)) : 0.f;
-    St<T>::st(p, v, x);
+  for (int i = 0; i < P_COLS / 2048; ++i) {
+    const int v0 = blockIdx.y * P_COLS + i * 2048 + tid * 8;
+    if (v0 >= a.Vp) break;
+    float x[8];
+    if (in) {
+      *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(s + v0);
+      *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(s + v0 + 4);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = in && v0 + e < a.V ? g * exp_below(x[e] - lse) : 0.f;
+    if (lab >= v0 && lab < v0 + 8) {
+      const float y = g * expm1f(-loss);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = v0 + e == lab ? y : x[e];
+    }
+    St<T>::st4(p, v0, x);
+    St<T>::st4(p, v0 + 4, x + 4);
   }
 }
 
 // ---------------------------------------------------------------- launches
-constexpr int F32_TILE = 128;
-
 static long up(long x, long m) { return (x + m - 1) / m * m; }
+
+// Whether the fp32 products take 32-wide tiles: where 128-wide ones leave most CUs idle
+static bool f32_small(long rows, long cols) { return up(rows, 128) / 128 * (up(cols, 128) / 128) < 128; }
+constexpr int F32_SLOTS = 512;
 
 // The workspace: sizes, and the pointers into it where there is one
 size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
-  const long es = dtype == DT_BF16 ? 2 : 4, np = up(a.n, 64);
+  const bool low = dtype == DT_BF16;
+  const long es = low ? 2 : 4, np = up(a.n, 64);
   a.Vp = (int)up(a.V, 64);
   a.dp = (int)up(a.d, 64);
-  a.bn = dtype == DT_BF16 ? vocab_mm_bn(a.n, a.V) : F32_TILE;
+  a.bn = low ? vocab_mm_bn(a.n, a.d, a.V) : f32_small(a.n, a.V) ? 32 : 128;
   a.tiles = (a.V + a.bn - 1) / a.bn;
   // rows at a time: 2^29 logits (2 GiB), 2^24 partial sums; whole tiles of rows
   const long most = grads ? (1l << 29) / a.Vp : (1l << 24) / a.tiles;
@@ -284,59 +488,79 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   a.part_at = next ? static_cast<int*>(take((size_t)a.R * a.tiles * 4)) : nullptr;
   if (!next) {
     a.n_counted = static_cast<int*>(take(4));
+    a.block_count = a.n > PICK_DIRECT ? static_cast<int*>(take((size_t)(np / 1024 + 1) * 4)) : nullptr;
     a.idx = static_cast<int*>(take((size_t)a.n * 4));
     a.lab_c = static_cast<int*>(take((size_t)a.n * 4));
     a.target = static_cast<float*>(take((size_t)a.n * 4));
-    a.stat = static_cast<float2*>(take((size_t)a.R * 8));
   }
   if (grads) {
     a.g_c = static_cast<float*>(take((size_t)a.n * 4));
     a.logits = static_cast<float*>(take((size_t)a.R * a.Vp * 4));
-    if (dtype == DT_BF16) {
-      a.P = take((size_t)a.R * a.Vp * 2);
-      a.dh_splits = vocab_dh_splits(a.R, a.d, a.V);
-      a.dh_part = a.dh_splits > 1 ? static_cast<float*>(take((size_t)a.dh_splits * a.R * a.d * 4)) : nullptr;
-      if (a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
-      a.ld_acc = a.d;
-    } else {
-      a.P = a.logits;
-    }
+    a.P = low ? take((size_t)a.R * a.Vp * 2) : a.logits;
+    a.dh_part = static_cast<float*>(take(low ? vocab_dh_part_bytes(a.n, a.d, a.V) : (size_t)F32_SLOTS * 4 * (f32_small(a.n, a.d) ? 1024 : 16384)));
+    if (low && a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
+    a.ld_acc = a.d;
   }
   return at;
 }
 
 template <bool KA, bool KB, Prod E>
-static void go_f32(const VocabArgs& a, const void* A, long lda, const void* B, long ldb, int M, int N, int K, hipStream_t s) {
-  const unsigned wgs = ((M + F32_TILE - 1) / F32_TILE) * ((N + F32_TILE - 1) / F32_TILE);
-  RG_LAUNCH((vocab_f32_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, static_cast<const float*>(A), lda,
-            static_cast<const float*>(B), ldb, M, N, K);
+static void go_f32(const VocabArgs& a, F32Product p, bool small, hipStream_t s) {
+  const int bt = small ? 32 : 128;
+  const long rows = E == Prod::Dw ? p.M : a.rows;
+  long wgs = (up(rows, bt) / bt) * (up(p.N, bt) / bt);
+  p.slots = F32_SLOTS;
+  if (E == Prod::Dh && wgs < F32_SLOTS) wgs = F32_SLOTS;
+  if (small) RG_LAUNCH((vocab_f32_small_k<KA, KB, E>), dim3((unsigned)wgs), dim3(256), 0, s, a, p);
+  else RG_LAUNCH((vocab_f32_k<KA, KB, E>), dim3((unsigned)wgs), dim3(256), 0, s, a, p);
+  if (E == Prod::Dh && a.V >= 512) RG_LAUNCH(vocab_f32_dh_sum_k, dim3(a.rows, (p.N + 255) / 256), dim3(256), 0, s, a, p, bt);
+}
+
+static void vocab_products_f32(const VocabArgs& a, int which, hipStream_t s) {
+  const float* H = static_cast<const float*>(a.hc) + (long)a.row0 * a.dp;
+  const float* W = static_cast<const float*>(a.w);
+  const float* P = static_cast<const float*>(a.P);
+  const bool vw = (reinterpret_cast<uintptr_t>(W) & 15u) == 0 && a.ldw % 4 == 0;
+  F32Product p{};
+  if (which < 2) {
+    p = F32Product{H, a.dp, W, a.ldw, 0, a.V, a.d, vw, 0};
+    if (which) go_f32<true, true, Prod::Logits>(a, p, a.bn == 32, s);
+    else go_f32<true, true, Prod::Stats>(a, p, a.bn == 32, s);
+  } else if (which == 2) {
+    p = F32Product{P, a.Vp, W, a.ldw, 0, a.d, a.V, vw, 0};
+    go_f32<true, false, Prod::Dh>(a, p, f32_small(a.n, a.d), s);
+  } else {
+    p = F32Product{P, a.Vp, H, a.dp, a.V, a.d, 0, true, 0};
+    go_f32<false, false, Prod::Dw>(a, p, f32_small(a.V, a.d), s);
+  }
 }
 
 template <typename T>
 static hipError_t vocab_t(VocabArgs a, hipStream_t s) {
   constexpr bool low = sizeof(T) == 2;
   const bool grads = a.dh || a.dw;
-  if (a.labels) RG_LAUNCH(vocab_scan_k, dim3(1), dim3(1024), 0, s, a);
-  RG_LAUNCH(vocab_gather_k<T>, dim3((unsigned)up(a.n, 64)), dim3(256), 0, s, a);
+  if (a.labels && a.block_count) RG_LAUNCH(vocab_count_k, dim3((a.n + 1023) / 1024), dim3(256), 0, s, a);
+  const bool wide = (reinterpret_cast<uintptr_t>(a.h) & 15u) == 0 && a.ldh * sizeof(T) % 16 == 0 && a.d * sizeof(T) % 16 == 0;
+  RG_LAUNCH(vocab_pick_k<T>, dim3((a.n + PICK_ROWS - 1) / PICK_ROWS), dim3(256), 0, s, a, wide);
   a.count = a.labels ? a.n_counted : nullptr;
   for (a.row0 = 0; a.row0 < a.n; a.row0 += a.R) {
     a.rows = a.n - a.row0 < a.R ? a.n - a.row0 : a.R;
     a.first = a.row0 == 0;
     a.last = a.row0 + a.R >= a.n;
-    const T* H = static_cast<const T*>(a.hc) + (long)a.row0 * a.dp;
     if constexpr (low) launch_vocab_logits_bf16(a, grads, s);
-    else if (grads) go_f32<true, true, Prod::Logits>(a, H, a.dp, a.w, a.ldw, a.rows, a.V, a.d, s);
-    else go_f32<true, true, Prod::Stats>(a, H, a.dp, a.w, a.ldw, a.rows, a.V, a.d, s);
-    RG_LAUNCH(vocab_rows_k, dim3((a.rows + 3) / 4), dim3(256), 0, s, a);
-    if (!grads) continue;
-    RG_LAUNCH(vocab_p_k<T>, dim3((unsigned)up(a.rows, 64), (a.Vp + 1023) / 1024), dim3(256), 0, s, a);
+    else vocab_products_f32(a, grads, s);
+    if (!grads) {
+      RG_LAUNCH(vocab_rows_k, dim3((a.rows + 3) / 4), dim3(256), 0, s, a);
+      continue;
+    }
+    RG_LAUNCH(vocab_p_k<T>, dim3((unsigned)up(a.rows, 64), (a.Vp + P_COLS - 1) / P_COLS), dim3(256), 0, s, a);
     if (a.dh) {
       if constexpr (low) launch_vocab_dh_bf16(a, s);
-      else go_f32<true, false, Prod::Dh>(a, a.P, a.Vp, a.w, a.ldw, a.rows, a.d, a.V, s);
+      else vocab_products_f32(a, 2, s);
     }
     if (a.dw) {
       if constexpr (low) launch_vocab_dw_bf16(a, s);
-      else go_f32<false, false, Prod::Dw>(a, a.P, a.Vp, H, a.dp, a.V, a.d, 0, s);
+      else vocab_products_f32(a, 3, s);
     }
   }
   return hipGetLastError();

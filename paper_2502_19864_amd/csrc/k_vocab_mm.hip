@@ -130,10 +130,14 @@ struct VocabProduct {
   const bf16* B; long ldb;
   int M, N;        // M: of dw (the logits and dh have the rows that count)
   int K;           // k of the logits (d) and of dh (V)
-  int splits;      // dh: k dealt to so many workgroups per tile, sums in part
-  float* part;     // [splits][R][d]
-  int ntm;         // rows of tiles that the grid is for
+  int slots;       // dh: workgroups of one round
 };
+// dh's k (the vocabulary) is dealt to several workgroups per tile where the tiles of the rows that count leave CUs
+// idle, eight k-tiles at least to each
+__host__ __device__ inline int dh_splits(int slots, int tiles, int V) {
+  const int by_slots = slots / tiles, by_k = V / 512, s = by_slots < by_k ? by_slots : by_k;
+  return s < 1 ? 1 : s;
+}
 
 // The tile of C[m][n] = sum_k A(m, k) B(n, k) that a workgroup makes, by XCD: workgroups are dealt round-robin to the eight
 // XCDs; each takes a contiguous run of a raster in bands of GROUP tile rows, so what its L2 holds is shared.
@@ -167,27 +171,33 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int cnt = __builtin_amdgcn_readfirstlane(piece_rows(a));
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
-  const int K = E == Prod::Dw ? (cnt + 63) & ~63 : p.K;
+  const int K = E == Prod::Dw ? cnt : p.K;
   const int ntm = (M + BM - 1) / BM, ntn = (N + BN - 1) / BN;
-  const int split = E == Prod::Dh ? (int)(blockIdx.x / (p.ntm * ntn)) : 0;
+  int splits = 1, split = 0;
+  if constexpr (E == Prod::Dh) {
+    if (ntm == 0) return;
+    splits = __builtin_amdgcn_readfirstlane(dh_splits(p.slots, ntm * ntn, p.K));
+    split = __builtin_amdgcn_readfirstlane(blockIdx.x / (ntm * ntn));
+    if (split >= splits) return;
+  }
   int tm, tn;
-  if (!vocab_tile<4>((int)blockIdx.x - split * p.ntm * ntn, ntm, ntn, tm, tn)) return;
+  if (!vocab_tile<4>((int)blockIdx.x - split * ntm * ntn, ntm, ntn, tm, tn)) return;
   tm = __builtin_amdgcn_readfirstlane(tm);
   tn = __builtin_amdgcn_readfirstlane(tn);
   const int m0 = tm * BM, n0 = tn * BN;
   const int nk_all = (K + 63) / 64;
-  const int kt0 = E == Prod::Dh ? (int)((long)nk_all * split / p.splits) : 0;
-  const int kt1 = E == Prod::Dh ? (int)((long)nk_all * (split + 1) / p.splits) : nk_all;
+  const int kt0 = E == Prod::Dh ? (int)((long)nk_all * split / splits) : 0;
+  const int kt1 = E == Prod::Dh ? (int)((long)nk_all * (split + 1) / splits) : nk_all;
   const int nk = kt1 - kt0;
 
   OA oa;
   OB ob;
   oa.init(p.A, p.lda, m0, M, wave, lane);
   ob.init(p.B, p.ldb, n0, N, wave, lane);
-  // part q of `of` of k-tile kt's DMA instructions.  w lacks the k that hc and P are padded with.
+  // part q of `of` of k-tile kt's DMA instructions.  A (hc in the logits, P) has zeros up to whole k-tiles; B has not.
   auto issue = [&](int kt, int slot, int q, int of) {
     const uint32_t l0 = lds_addr(smem) + slot * STAGE;
-    const int left = E == Prod::Dw ? 64 : min(64, K - (kt0 + kt) * 64);
+    const int left = min(64, K - (kt0 + kt) * 64);
 #pragma unroll
     for (int i = LPT * q / of; i < LPT * (q + 1) / of; ++i) {
       if (i < OA::L) oa.dma(i, kt0 + kt, 64, l0, wave_u);
@@ -354,8 +364,8 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
         *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(cf + row * CP + c);
         *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(cf + row * CP + c + 4);
         if constexpr (E == Prod::Dh) {
-          if (p.splits > 1) {
-            float* o = p.part + ((long)split * a.R + m) * a.d + n;
+          if (splits > 1) {
+            float* o = a.dh_part + (((long)split * ntm + tm) * ntn + tn) * (BM * BN) + (pass * RPP + row) * BN + c;
             *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
             *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
           } else {
@@ -380,17 +390,21 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
   }
 }
 
-// dh of a piece from its splits' sums, in their order
-__global__ __launch_bounds__(256) void vocab_dh_sum_k(VocabArgs a, VocabProduct p) {
-  const int m = blockIdx.x;
-  if (m >= piece_rows(a)) return;
-  const int n = (blockIdx.y * 256 + threadIdx.x) * 8;
-  if (n >= a.d) return;
+// dh of a piece from its splits' sums, in their order; tiles are bt x bt
+__global__ __launch_bounds__(256) void vocab_dh_sum_k(VocabArgs a, VocabProduct p, int bt) {
+  const int cnt = piece_rows(a), cols = p.N / 8, i = blockIdx.x * 256 + threadIdx.x, m = i / cols, n = i % cols * 8;
+  if (m >= cnt) return;
+  const int ntn = (p.N + bt - 1) / bt, tiles = (cnt + bt - 1) / bt * ntn, splits = dh_splits(p.slots, tiles, p.K);
+  if (splits == 1) return;
+  const float* q = a.dh_part + (long)(m / bt * ntn + n / bt) * bt * bt + (m % bt) * bt + n % bt;
   float v[8] = {};
-  for (int s = 0; s < p.splits; ++s) {
-    const float* o = p.part + ((long)s * a.R + m) * a.d + n;
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    float x[8];
+    *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(q + (long)s * tiles * bt * bt);
+    *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(q + (long)s * tiles * bt * bt + 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += o[e];
+    for (int e = 0; e < 8; ++e) v[e] += x[e];
   }
   *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dh) + (long)a.idx[a.row0 + m] * a.lddh + n) = pack_frag(v);
 }
@@ -399,19 +413,21 @@ static int tiles_of(int x, int t) { return (x + t - 1) / t; }
 
 template <int BM, int BN, int WM, int WN, int NS, bool KA, bool KB, Prod E>
 static void go(const VocabArgs& a, VocabProduct p, hipStream_t s) {
-  p.ntm = tiles_of(E == Prod::Dw ? p.M : a.rows, BM);
-  const int wgs = p.ntm * tiles_of(p.N, BN) * (E == Prod::Dh ? p.splits : 1);
+  int wgs = tiles_of(E == Prod::Dw ? p.M : a.rows, BM) * tiles_of(p.N, BN);
+  if (E == Prod::Dh && wgs < p.slots) wgs = p.slots;
   RG_LAUNCH((vocab_mm_k<BM, BN, WM, WN, NS, KA, KB, E>), dim3(wgs), dim3(64 * WM * WN), 0, s, a, p);
 }
 
-int vocab_mm_bn(int rows, int V) { return rows > 128 && V > 128 ? 256 : 128; }
+int vocab_mm_bn(int rows, int d, int V) { return rows > 128 && V > 128 && d >= 2048 ? 256 : 128; }
+static int dh_tile(int rows) { return rows > 128 ? 256 : 128; }
+static int dh_slots(int rows) { return rows > 128 ? 256 : 512; }
 
-// workgroups that share a tile of dh: enough to fill the GPU
-int vocab_dh_splits(int rows, int d, int V) {
-  const int t = rows > 128 ? 256 : 128, tiles = tiles_of(rows, t) * tiles_of(d, t), k = tiles_of(V, 64);
-  int s = (t == 256 ? 256 : 512) / tiles;
-  if (s > k / 8) s = k / 8;
-  return s < 1 ? 1 : s > 64 ? 64 : s;
+size_t vocab_dh_part_bytes(int rows, int d, int V) {
+  const int t = dh_tile(rows), slots = dh_slots(rows);
+  const long tiles = (long)tiles_of(rows, t) * tiles_of(d, t);
+  // one tile to all of them: whichever rows count, splits times tiles are at most slots
+  const long most = tiles * dh_splits(slots, 1, V);
+  return (size_t)(most < slots ? most : slots) * t * t * 4;
 }
 
 void launch_vocab_logits_bf16(const VocabArgs& a, bool keep, hipStream_t s) {
@@ -438,11 +454,12 @@ void launch_vocab_dh_bf16(const VocabArgs& a, hipStream_t s) {
   p.ldb = a.ldw;
   p.N = a.d;
   p.K = a.V;
-  p.splits = a.dh_splits;
-  p.part = a.dh_part;
-  if (a.n > 128) go<256, 256, 4, 2, 2, true, false, Prod::Dh>(a, p, s);
+  p.slots = dh_slots(a.n);
+  const int t = dh_tile(a.n);
+  if (t == 256) go<256, 256, 4, 2, 2, true, false, Prod::Dh>(a, p, s);
   else go<128, 128, 2, 2, 2, true, false, Prod::Dh>(a, p, s);
-  if (p.splits > 1) RG_LAUNCH(vocab_dh_sum_k, dim3(a.rows, (a.d + 2047) / 2048), dim3(256), 0, s, a, p);
+  if (dh_splits(p.slots, 1, a.V) > 1)
+    RG_LAUNCH(vocab_dh_sum_k, dim3((unsigned)(((long)a.rows * (a.d / 8) + 255) / 256)), dim3(256), 0, s, a, p, t);
 }
 void launch_vocab_dw_bf16(const VocabArgs& a, hipStream_t s) {
   VocabProduct p{};

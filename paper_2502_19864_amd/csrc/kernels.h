@@ -258,14 +258,13 @@ struct VocabArgs {
   int* token; float* logprob;   // [n]: without labels
   // workspace
   int dp, Vp, bn, tiles, R;     // d and V up to a multiple of 64, column tiles of the logits, rows at a time
-  void* hc;                     // [n up][dp]: the rows that count, zeros past d and behind the last
+  void* hc;                     // [n up][dp]: the rows that count, zeros past d
   float2* part; int* part_at;   // [R][tiles]
-  int* n_counted;
+  int* n_counted; int* block_count;  // block_count: of every 1024 rows, or null where rows are few
   int* idx; int* lab_c; float* g_c; float* target;  // [n], by counted row: its place, label, gradient, label's logit
-  float2* stat;                 // [R]: lse, loss
   float* logits;                // [R][Vp]
   void* P;                      // [R][Vp] in the storage type (fp32: the logits' place)
-  int dh_splits; float* dh_part;  // bf16: [splits][R][d], sums of dh over shares of the columns
+  float* dh_part;               // tiles of dh over shares of the columns
   float* dw_acc; long ld_acc;   // bf16: dw between the pieces, [V][d]
   // a piece
   const int* count;             // n_counted, or null: all rows
@@ -273,9 +272,9 @@ struct VocabArgs {
 };
 // bytes of the workspace, and with ws the pointers into it
 size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws);
-// the bf16 products (k_vocab_mm.hip): columns of a tile of logits, the splits of dh, the launches of one piece
-int vocab_mm_bn(int rows, int V);
-int vocab_dh_splits(int rows, int d, int V);
+// the bf16 products (k_vocab_mm.hip): columns of a tile of logits, bytes of dh_part, the launches of one piece
+int vocab_mm_bn(int rows, int d, int V);
+size_t vocab_dh_part_bytes(int rows, int d, int V);
 void launch_vocab_logits_bf16(const VocabArgs& a, bool keep, hipStream_t s);
 void launch_vocab_dh_bf16(const VocabArgs& a, hipStream_t s);
 void launch_vocab_dw_bf16(const VocabArgs& a, hipStream_t s);
