@@ -51,38 +51,26 @@ struct Operand {
   const char* base;   // the tile's first element
   long step;          // bytes per k-tile
   uint32_t off[L];    // per-lane byte offsets within a k-tile
-  int row[L], chunk[L];
   uint32_t ld2;
-  // rows0: first row; rows: how many there are (KMAJOR: clamped one by one, else in chunks of 8)
-  __device__ __forceinline__ void init(const bf16* p, long ld, int rows0, int rows, int wave, int lane) {
+  // first of `rows` rows: those past the end are clamped (KMAJOR: one by one, else in chunks of 8)
+  __device__ __forceinline__ void init(const bf16* p, long ld, int first, int rows, int wave, int lane) {
     ld2 = (uint32_t)ld * 2;
-    if constexpr (KMAJOR) {
-      base = reinterpret_cast<const char*>(p + (long)rows0 * ld);
-      step = 128;
-    } else {
-      base = reinterpret_cast<const char*>(p + rows0);
-      step = ld * 128;
-    }
-    base = uniform_ptr(base);
+    base = uniform_ptr(reinterpret_cast<const char*>(KMAJOR ? p + (long)first * ld : p + first));
+    step = KMAJOR ? 128 : ld * 128;
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       const int r = (i * NW + wave) * RPI + lane / CPR, pos = lane % CPR;
-      if constexpr (KMAJOR) {
-        chunk[i] = pos ^ ((r >> 1) & 7);
-        row[i] = min(rows0 + r, rows - 1) - rows0;
-      } else {
-        chunk[i] = min(pos ^ ((r & 3) << 2), (rows - rows0 + 7) / 8 - 1);
-        row[i] = r;
-      }
-      off[i] = (uint32_t)row[i] * ld2 + chunk[i] * 16;
+      if constexpr (KMAJOR) off[i] = (uint32_t)min(r, rows - 1 - first) * ld2 + (pos ^ ((r >> 1) & 7)) * 16;
+      else off[i] = (uint32_t)r * ld2 + min(pos ^ ((r & 3) << 2), (rows - first + 7) / 8 - 1) * 16;
     }
   }
-  // instruction i of k-tile kt; left: k of this tile that the operand has (a whole tile: 64)
-  __device__ __forceinline__ void dma(int i, int kt, int left, uint32_t lds, int wave_u) const {
+  // instruction i of k-tile kt; left: k of this tile that the operand has (64: all).  Past them the last ones are read again.
+  __device__ __forceinline__ void dma(int i, int kt, int left, uint32_t lds, int wave, int wave_u, int lane) const {
     uint32_t o = off[i];
     if (left < 64) {
-      if constexpr (KMAJOR) o -= max(0, chunk[i] - (left / 8 - 1)) * 16;
-      else o -= max(0, row[i] - (left - 1)) * ld2;
+      const int r = (i * NW + wave) * RPI + lane / CPR;
+      if constexpr (KMAJOR) o -= max(0, (lane % CPR ^ ((r >> 1) & 7)) - (left / 8 - 1)) * 16;
+      else o -= max(0, r - (left - 1)) * ld2;
     }
     dma16_m0(base + (long)kt * step, o, lds + (i * NW + wave_u) * 1024);
   }
@@ -119,12 +107,6 @@ struct Frags {
   }
 };
 
-constexpr int stage_rows(int bm, int row_bytes, int lds_bytes) {
-  int r = bm;
-  while (r > 32 && r * row_bytes > lds_bytes) r /= 2;
-  return r;
-}
-
 struct VocabProduct {
   const bf16* A; long lda;
   const bf16* B; long ldb;
@@ -153,64 +135,63 @@ __device__ __forceinline__ bool vocab_tile(int g, int ntm, int ntn, int& tm, int
   return true;
 }
 
+// Workgroups stay: one round of the GPU, each over its tiles.  While a tile is stored the first k-tiles of the next are
+// on their way, and its stores drain under the next one's products (2048 x 32000 logits, d 4096: 1.08 times less than a workgroup per tile).
+// So the epilogue has no LDS but 4 KB per wave beside the stages, and no barrier: each wave sends its 32 x 32 blocks
+// through its own, in 16-byte pieces at c ^ row % 8, and stores whole 128-byte (bf16: 64-byte) runs of rows; the logits'
+// statistics are per wave too, one (maximum, sum) for BN / WN columns.
 template <int BM, int BN, int WM, int WN, int NS, bool KA, bool KB, Prod E>
 __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabProduct p) {
-  constexpr int NW = WM * WN, NT = 64 * NW, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32, KS = 4;
+  constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32, KS = 4;
   using OA = Operand<BM, NW, KA>;
   using OB = Operand<BN, NW, KB>;
-  constexpr int LPT = OA::L + OB::L, STAGE = (BM + BN) * 128, CP = BN + 4;
+  constexpr int LPT = OA::L + OB::L, STAGE = (BM + BN) * 128;
   constexpr int ND = FM * (KA ? 1 : 2) + FN * (KB ? 1 : 2);
   static_assert(FM * 32 * WM == BM && FN * 32 * WN == BN && NS >= 2 && NS <= 4 && LPT * (NS - 1) < 64, "tile");
-  constexpr int EPI_MIN = (BM == 256 && BN == 256 ? 128 : 64) * CP * 4;
-  constexpr int LDS = EPI_MIN > NS * STAGE ? EPI_MIN : NS * STAGE;
-  constexpr int RPP = stage_rows(BM, CP * 4, LDS);
-  static_assert(BM % RPP == 0 && RPP * CP * 4 <= LDS && LDS <= 160 * 1024, "epilogue passes");
-  __shared__ __attribute__((aligned(1024))) char smem[LDS];
+  static_assert(NS * STAGE + NW * 4096 <= 160 * 1024, "LDS");
+  __shared__ __attribute__((aligned(1024))) char smem[NS * STAGE + NW * 4096];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave / WN, wn = wave % WN;
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int cnt = __builtin_amdgcn_readfirstlane(piece_rows(a));
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
   const int K = E == Prod::Dw ? cnt : p.K;
-  const int ntm = (M + BM - 1) / BM, ntn = (N + BN - 1) / BN;
-  int splits = 1, split = 0;
-  if constexpr (E == Prod::Dh) {
-    if (ntm == 0) return;
-    splits = __builtin_amdgcn_readfirstlane(dh_splits(p.slots, ntm * ntn, p.K));
-    split = __builtin_amdgcn_readfirstlane(blockIdx.x / (ntm * ntn));
-    if (split >= splits) return;
-  }
-  int tm, tn;
-  if (!vocab_tile<4>((int)blockIdx.x - split * ntm * ntn, ntm, ntn, tm, tn)) return;
-  tm = __builtin_amdgcn_readfirstlane(tm);
-  tn = __builtin_amdgcn_readfirstlane(tn);
-  const int m0 = tm * BM, n0 = tn * BN;
+  const int ntm = (M + BM - 1) / BM, ntn = (N + BN - 1) / BN, tiles = ntm * ntn;
+  const int splits = E == Prod::Dh && tiles ? __builtin_amdgcn_readfirstlane(dh_splits(p.slots, tiles, p.K)) : 1;
   const int nk_all = (K + 63) / 64;
-  const int kt0 = E == Prod::Dh ? (int)((long)nk_all * split / splits) : 0;
-  const int kt1 = E == Prod::Dh ? (int)((long)nk_all * (split + 1) / splits) : nk_all;
-  const int nk = kt1 - kt0;
-
+  int m0 = 0, n0 = 0, split = 0, kt0 = 0, nk = 0, tile = 0;
+  // the g-th piece of work, or none
+  auto locate = [&](int g) {
+    if (g >= tiles * splits) return false;
+    if constexpr (E == Prod::Dh) split = __builtin_amdgcn_readfirstlane(g / tiles);
+    int tm, tn;
+    vocab_tile<4>(g - split * tiles, ntm, ntn, tm, tn);
+    tile = __builtin_amdgcn_readfirstlane(tm * ntn + tn);
+    m0 = __builtin_amdgcn_readfirstlane(tm * BM);
+    n0 = __builtin_amdgcn_readfirstlane(tn * BN);
+    kt0 = (int)((long)nk_all * split / splits);
+    nk = (int)((long)nk_all * (split + 1) / splits) - kt0;
+    return true;
+  };
   OA oa;
   OB ob;
-  oa.init(p.A, p.lda, m0, M, wave, lane);
-  ob.init(p.B, p.ldb, n0, N, wave, lane);
   // part q of `of` of k-tile kt's DMA instructions.  A (hc in the logits, P) has zeros up to whole k-tiles; B has not.
   auto issue = [&](int kt, int slot, int q, int of) {
     const uint32_t l0 = lds_addr(smem) + slot * STAGE;
     const int left = min(64, K - (kt0 + kt) * 64);
 #pragma unroll
     for (int i = LPT * q / of; i < LPT * (q + 1) / of; ++i) {
-      if (i < OA::L) oa.dma(i, kt0 + kt, 64, l0, wave_u);
-      else ob.dma(i - OA::L, kt0 + kt, left, l0 + BM * 128, wave_u);
+      if (i < OA::L) oa.dma(i, kt0 + kt, 64, l0, wave, wave_u, lane);
+      else ob.dma(i - OA::L, kt0 + kt, left, l0 + BM * 128, wave, wave_u, lane);
     }
   };
-  f32x16 acc[FM][FN];
+  auto begin = [&] {
+    oa.init(p.A, p.lda, m0, M, wave, lane);
+    ob.init(p.B, p.ldb, n0, N, wave, lane);
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
-#pragma unroll
-    for (int j = 0; j < FN; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    for (int t = 0; t < NS; ++t)
+      if (t < nk) issue(t, t, 0, 1);
+  };
   Frags<BM, FM, KA> ra;
   Frags<BN, FN, KB> rb;
   ra.init(wm * TM, lane);
@@ -221,12 +202,13 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
     rb.read(smem + slot * STAGE + BM * 128, ks, lane, fb[buf]);
   };
   auto wait_tiles = [&](int n) {  // at most n k-tiles still in flight
-    if constexpr (NS >= 4) { if (n >= 3) { wait_dma<3 * LPT>(); return; } }
-    if constexpr (NS >= 3) { if (n >= 2) { wait_dma<2 * LPT>(); return; } }
-    if (n >= 1) { wait_dma<LPT>(); return; }
+    if constexpr (NS >= 4) { if (n >= 2) { wait_dma<2 * LPT>(); return; } }
+    if constexpr (NS >= 3) { if (n >= 1) { wait_dma<LPT>(); return; } }
     wait_dma<0>();
   };
-  // A finished stage is refilled in pieces, the first right after the barrier that frees it
+  f32x16 acc[FM][FN];
+  // A finished stage is refilled in pieces, the first right after the barrier that frees it.  The first NS k-tiles of a tile
+  // had landed before the stores of the last one were issued: they are not waited for, so neither are the stores.
   constexpr int PARTS = NS >= 3 ? KS : 2;
   auto step = [&](auto S, int kt) {
     constexpr int s = decltype(S)::value, sn = (s + 1) % NS, sp = (s + NS - 1) % NS;
@@ -236,7 +218,8 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
         if (ks + 1 < PARTS && kt > 0 && kt - 1 + NS < nk) issue(kt - 1 + NS, sp, ks + 1, PARTS);
         read_frags(s, ks + 1, (ks + 1) & 1);
       } else if (kt + 1 < nk) {
-        wait_tiles(min(NS - 2, nk - 2 - kt));
+        if (kt + 1 >= NS) wait_tiles(min(NS - 2, nk - 2 - kt));
+        else __builtin_amdgcn_s_waitcnt(0xF | (0x7 << 4) | (0x3 << 14));  // lgkmcnt == 0
         wg_barrier();
         if (kt + NS < nk) issue(kt + NS, s, 0, PARTS);
         read_frags(sn, 0, 0);
@@ -248,145 +231,148 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
       spread_reads<ND, FM * FN>(std::make_integer_sequence<int, FM * FN>{});
     }
   };
-  if (nk > 0) {
-#pragma unroll
-    for (int t = 0; t < NS; ++t)
-      if (t < nk) issue(t, t, 0, 1);
-    wait_tiles(min(NS, nk) - 1);
-    wg_barrier();
-    read_frags(0, 0, 0);
-    for (int kt = 0; kt < nk; kt += NS) {
-      step(std::integral_constant<int, 0>{}, kt);
-      if (kt + 1 < nk) step(std::integral_constant<int, 1>{}, kt + 1);
-      if constexpr (NS > 2) if (kt + 2 < nk) step(std::integral_constant<int, 2>{}, kt + 2);
-      if constexpr (NS > 3) if (kt + 3 < nk) step(std::integral_constant<int, 3>{}, kt + 3);
-    }
-  }
-  wait_dma<0>();
-  wg_barrier();  // every wave is done with the operands
 
-  // Lane l holds of each 32x32 block row l % 32, columns 8 g + 4 (l / 32) + 0..3, g = 0..3.
-  const int l32 = lane & 31, half = lane >> 5;
-  float* cf = reinterpret_cast<float*>(smem);
-  if constexpr (E == Prod::Stats || E == Prod::Logits) {
-    float* sm = cf;                                  // [BM][WN] maxima, sums, places
-    float* sl = cf + BM * WN;
-    int* sa = reinterpret_cast<int*>(cf + 2 * BM * WN);
-    const int c0 = n0 + wn * TN + 4 * half;
-    const bool edge = n0 + BN > N;
-    auto col = [&](int j, int r) { return c0 + j * 32 + 8 * (r / 4) + r % 4; };
+  if (!locate(blockIdx.x)) return;
+  begin();
+  wait_dma<0>();
+  for (int g = blockIdx.x;;) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int row = wm * TM + i * 32 + l32;
-      const int lab = a.lab_c && m0 + row < M ? a.lab_c[a.row0 + m0 + row] : -1;
-      if (lab >= n0 && lab < n0 + BN) {  // few lanes
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+      for (int j = 0; j < FN; ++j)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (col(j, r) == lab) a.target[a.row0 + m0 + row] = acc[i][j][r];
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+    wg_barrier();
+    if (nk > 0) {
+      read_frags(0, 0, 0);
+      for (int kt = 0; kt < nk; kt += NS) {
+        step(std::integral_constant<int, 0>{}, kt);
+        if (kt + 1 < nk) step(std::integral_constant<int, 1>{}, kt + 1);
+        if constexpr (NS > 2) if (kt + 2 < nk) step(std::integral_constant<int, 2>{}, kt + 2);
+        if constexpr (NS > 3) if (kt + 3 < nk) step(std::integral_constant<int, 3>{}, kt + 3);
       }
-      float m = -INFINITY;
-      if (edge) {
+    }
+    const int em0 = m0 + wm * TM, en0 = n0 + wn * TN, etile = tile, esplit = split;
+    g += gridDim.x;
+    const bool more = locate(g);
+    __builtin_amdgcn_s_waitcnt(0xF | (0x7 << 4) | (0x3 << 14));  // lgkmcnt == 0
+    wg_barrier();  // every wave is done with the stages
+    if (more) begin();
+
+    // Lane l holds of each 32x32 block row l % 32, columns 8 g + 4 (l / 32) + 0..3, g = 0..3.
+    int at = lane;
+    asm volatile("" : "+v"(at));  // what follows is worked out here, not kept over the products
+    const int l32 = at & 31, half = at >> 5;
+    if constexpr (E == Prod::Stats || E == Prod::Logits) {
+      const int c0 = en0 + 4 * half;
+      auto col = [&](int j, int r) { return c0 + j * 32 + 8 * (r / 4) + r % 4; };
+      if (en0 + TN > N) {  // columns past the vocabulary
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) m = fmaxf(m, col(j, r) < N ? acc[i][j][r] : -INFINITY);
-      } else {
+          for (int r = 0; r < 16; ++r) {
+            const bool past = col(j, r) >= N;
+#pragma unroll
+            for (int i = 0; i < FM; ++i) acc[i][j][r] = past ? -INFINITY : acc[i][j][r];
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const int row = em0 + i * 32 + l32;
+        const int lab = a.lab_c && row < M ? a.lab_c[a.row0 + row] : -1;
+        const int mine = lab - c0;  // 32 j + 8 (r / 4) + r % 4 where the label is among this lane's columns
+        if (mine >= 0 && lab < en0 + TN && !(mine & 4)) {
+          float t = 0.f;
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) t = mine == j * 32 + 8 * (r / 4) + r % 4 ? acc[i][j][r] : t;
+          a.target[a.row0 + row] = t;
+        }
+        float m = -INFINITY;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
           for (int r = 0; r < 16; ++r) m = fmaxf(m, acc[i][j][r]);
-      }
-      m = fmaxf(m, __shfl_xor(m, 32));
-      const float z = m == -INFINITY ? 0.f : m;
-      float l = 0.f;
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float e = exp_below(acc[i][j][r] - z);
-          l += !edge || col(j, r) < N ? e : 0.f;
-        }
-      l += __shfl_xor(l, 32);
-      int at = INT32_MAX;
-      if (a.part_at) {
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const float z = m == -INFINITY ? 0.f : m;
+        float l = 0.f;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (acc[i][j][r] == m && (!edge || col(j, r) < N)) at = min(at, col(j, r));
-        at = min(at, __shfl_xor(at, 32));
-      }
-      if (half == 0) {
-        sm[row * WN + wn] = m;
-        sl[row * WN + wn] = l;
-        sa[row * WN + wn] = at;
+          for (int r = 0; r < 16; ++r) l += exp_below(acc[i][j][r] - z);
+        l += __shfl_xor(l, 32);
+        if (half == 0 && row < M && en0 < N) a.part[(long)row * a.tiles + en0 / TN] = make_float2(m, l);
+        if (a.part_at) {
+          int lowest = INT32_MAX;
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              lowest = acc[i][j][r] == m ? min(lowest, col(j, r)) : lowest;
+          lowest = min(lowest, __shfl_xor(lowest, 32));
+          if (half == 0 && row < M && en0 < N) a.part_at[(long)row * a.tiles + en0 / TN] = min(lowest, N - 1);
+        }
       }
     }
-    __syncthreads();
-    for (int row = tid; row < BM; row += NT) {
-      if (m0 + row >= M) break;
-      Peak q{sm[row * WN], sl[row * WN], sa[row * WN]};
+    wait_dma<0>();  // the next tile's first k-tiles; then come the stores
+    if constexpr (E != Prod::Stats) {
+      char* mine = smem + NS * STAGE + wave * 4096;
 #pragma unroll
-      for (int w = 1; w < WN; ++w) q = join(q, Peak{sm[row * WN + w], sl[row * WN + w], sa[row * WN + w]});
-      a.part[(long)(m0 + row) * a.tiles + tn] = make_float2(q.m, q.l);
-      if (a.part_at) a.part_at[(long)(m0 + row) * a.tiles + tn] = min(q.at, N - 1);
-    }
-    if constexpr (E == Prod::Stats) return;
-    __syncthreads();
-  }
-  // the tile through LDS, RPP rows at a time, so that stores are whole rows' pieces of 16 bytes
-  constexpr int CPR = BN / 8;
+      for (int i = 0; i < FM; ++i) {
+        const int mb = em0 + i * 32;
+        if (mb >= M) continue;  // wave-uniform
 #pragma unroll
-  for (int pass = 0; pass < BM / RPP; ++pass) {
+        for (int j = 0; j < FN; ++j) {
+          const int nb = en0 + j * 32;
+          if (nb >= (E == Prod::Logits ? a.Vp : N)) continue;
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      if ((wm * TM + i * 32) / RPP != pass) continue;  // wave-uniform
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<float4*>(mine + l32 * 128 + (((2 * q + half) ^ (l32 & 7)) << 4)) =
+                make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+          auto ld = [&](int row, int c) { return *reinterpret_cast<const float4*>(mine + row * 128 + ((c ^ (row & 7)) << 4)); };
+          if constexpr (E == Prod::Logits) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          *reinterpret_cast<float4*>(cf + (wm * TM + i * 32 + l32 - pass * RPP) * CP + wn * TN + j * 32 + 8 * g + 4 * half) =
-              make_float4(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
-    }
-    __syncthreads();
-    if constexpr (E == Prod::Logits) {
-      for (int idx = tid; idx < RPP * CPR * 2; idx += NT) {
-        const int row = idx / (CPR * 2), c = idx % (CPR * 2) * 4, m = m0 + pass * RPP + row, n = n0 + c;
-        if (m < M && n < a.Vp) *reinterpret_cast<float4*>(a.logits + (long)m * a.Vp + n) = *reinterpret_cast<const float4*>(cf + row * CP + c);
-      }
-    } else {
-      for (int idx = tid; idx < RPP * CPR; idx += NT) {
-        const int row = idx / CPR, c = idx % CPR * 8, m = m0 + pass * RPP + row, n = n0 + c;
-        if (m >= M || n >= N) continue;
-        float v[8];
-        *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(cf + row * CP + c);
-        *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(cf + row * CP + c + 4);
-        if constexpr (E == Prod::Dh) {
-          if (splits > 1) {
-            float* o = a.dh_part + (((long)split * ntm + tm) * ntn + tn) * (BM * BN) + (pass * RPP + row) * BN + c;
-            *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
-            *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
+            for (int q = 0; q < 4; ++q) {
+              const int row = 8 * q + (at >> 3), c = at & 7;
+              const float4 v = ld(row, c);
+              if (mb + row < M) *reinterpret_cast<float4*>(a.logits + (long)(mb + row) * a.Vp + nb + 4 * c) = v;
+            }
           } else {
-            *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dh) + (long)a.idx[a.row0 + m] * a.lddh + n) = pack_frag(v);
-          }
-        } else {
-          float* o = a.dw_acc + (long)m * a.ld_acc + n;
-          if (!a.first) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += o[e];
-          }
-          if (a.last) {
-            *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dw) + (long)m * a.lddw + n) = pack_frag(v);
-          } else {
-            *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
-            *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
+            for (int q = 0; q < 2; ++q) {
+              const int row = 16 * q + (at >> 2), c = at & 3, m = mb + row, n = nb + 8 * c;
+              float v[8];
+              *reinterpret_cast<float4*>(v) = ld(row, 2 * c);
+              *reinterpret_cast<float4*>(v + 4) = ld(row, 2 * c + 1);
+              if (m >= M || n >= N) continue;
+              if constexpr (E == Prod::Dh) {
+                if (splits > 1) {
+                  float* o = a.dh_part + ((long)esplit * tiles + etile) * (BM * BN) + (wm * TM + i * 32 + row) * BN + wn * TN + j * 32 + 8 * c;
+                  *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
+                  *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
+                } else {
+                  *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dh) + (long)a.idx[a.row0 + m] * a.lddh + n) = pack_frag(v);
+                }
+              } else {
+                float* o = a.dw_acc + (long)m * a.ld_acc + n;
+                if (!a.first) {
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) v[e] += o[e];
+                }
+                if (a.last) {
+                  *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dw) + (long)m * a.lddw + n) = pack_frag(v);
+                } else {
+                  *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
+                  *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
+                }
+              }
+            }
           }
         }
       }
     }
-    if (pass + 1 < BM / RPP) __syncthreads();
+    if (!more) return;
   }
 }
 
@@ -413,12 +399,15 @@ static int tiles_of(int x, int t) { return (x + t - 1) / t; }
 
 template <int BM, int BN, int WM, int WN, int NS, bool KA, bool KB, Prod E>
 static void go(const VocabArgs& a, VocabProduct p, hipStream_t s) {
-  int wgs = tiles_of(E == Prod::Dw ? p.M : a.rows, BM) * tiles_of(p.N, BN);
-  if (E == Prod::Dh && wgs < p.slots) wgs = p.slots;
+  // workgroups of one round
+  constexpr int round = BM == 256 ? 256 : 512;
+  const int tiles = tiles_of(E == Prod::Dw ? p.M : a.rows, BM) * tiles_of(p.N, BN);
+  const int wgs = E == Prod::Dh || tiles > round ? round : tiles;
   RG_LAUNCH((vocab_mm_k<BM, BN, WM, WN, NS, KA, KB, E>), dim3(wgs), dim3(64 * WM * WN), 0, s, a, p);
 }
 
-int vocab_mm_bn(int rows, int d, int V) { return rows > 128 && V > 128 && d >= 2048 ? 256 : 128; }
+static bool wide_logits(int rows, int d, int V) { return rows > 128 && V > 128 && d >= 2048; }
+int vocab_mm_bn(int rows, int d, int V) { return wide_logits(rows, d, V) ? 128 : 64; }  // a wave's columns
 static int dh_tile(int rows) { return rows > 128 ? 256 : 128; }
 static int dh_slots(int rows) { return rows > 128 ? 256 : 512; }
 
@@ -438,7 +427,7 @@ void launch_vocab_logits_bf16(const VocabArgs& a, bool keep, hipStream_t s) {
   p.ldb = a.ldw;
   p.N = a.V;
   p.K = a.d;
-  if (a.bn == 256) {
+  if (a.bn == 128) {
     if (keep) go<256, 256, 4, 2, 2, true, true, Prod::Logits>(a, p, s);
     else go<256, 256, 4, 2, 2, true, true, Prod::Stats>(a, p, s);
   } else {
