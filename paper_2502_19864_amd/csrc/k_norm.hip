@@ -120,62 +120,130 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_k(NormArgs a, 
   }
 }
 
-template <typename T, int TPR, int CH>
+// a piece as it lies in memory
+template <typename T>
+__device__ __forceinline__ uint4 ld_raw(const T* p, int left, bool wide) {
+  if (wide) return *reinterpret_cast<const uint4*>(p);
+  union {
+    uint4 q;
+    T e[VE<T>];
+  } u;
+  u.q = make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < VE<T>; ++i)
+    if (i < left) u.e[i] = p[i];
+  return u.q;
+}
+template <typename T>
+__device__ __forceinline__ void unpack_raw(const uint4& q, float v[VE<T>]) {
+  if constexpr (sizeof(T) == 2) {
+    unpack_frag(__builtin_bit_cast(bf16x8, q), v);
+  } else {
+    v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y);
+    v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
+  }
+}
+
+// The next row of a workgroup is on its way while one is worked on (AHEAD; not in the widest rows, whose registers are full).  Rows
+// stay as they lie in memory, and are unpacked for the sums and again for the result.
+template <typename T, int TPR, int CH, bool AHEAD>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_k(NormArgs a, bool wide) {
   constexpr int E = VE<T>, NT = TPR > 256 ? TPR : 256, RPW = NT / TPR;
-  __shared__ float red[16];
+  __shared__ float red[32];
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-  const T* gain = static_cast<const T*>(a.gain);
-  float g[CH][E], dg[CH][E], db[CH][E];
+  uint4 g[CH];
+  float dg[CH][E], db[CH][E];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int at = (c * TPR + t) * E, left = a.d - at;
 #pragma unroll
-    for (int i = 0; i < E; ++i) g[c][i] = dg[c][i] = db[c][i] = 0.f;
-    if (left > 0) ld_piece(gain + at, left, wide, g[c]);
+    for (int i = 0; i < E; ++i) dg[c][i] = db[c][i] = 0.f;
+    g[c] = left > 0 ? ld_raw(static_cast<const T*>(a.gain) + at, left, wide) : make_uint4(0, 0, 0, 0);
   }
   const float inv_d = 1.f / a.d;
-  // rows group, group + groups, ..; every row of a workgroup's loop has all its threads
-  for (long row = (long)blockIdx.x * RPW + sub; row < a.rows; row += (long)gridDim.x * RPW) {
+  const long stride = (long)gridDim.x * RPW;
+  struct Row {
+    uint4 x[CH], y[CH], k[CH];
+    float2 st;
+  };
+  auto load = [&](long row, Row& r) {
     const T* x = static_cast<const T*>(a.s.p) + row * a.s.t;
     const T* dy = static_cast<const T*>(a.dy.p) + row * a.dy.t;
-    const float2 st = a.stats[row];
-    float u[CH][E], w[CH][E];
-    float s1 = 0.f, s2 = 0.f;
+    const T* k = static_cast<const T*>(a.dskip.p) + row * a.dskip.t;
+    r.st = a.stats[row];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int at = (c * TPR + t) * E, left = a.d - at;
-#pragma unroll
-      for (int i = 0; i < E; ++i) u[c][i] = w[c][i] = 0.f;
+      r.x[c] = r.y[c] = r.k[c] = make_uint4(0, 0, 0, 0);
       if (left <= 0) continue;
-      ld_piece(x + at, left, wide, u[c]);
-      ld_piece(dy + at, left, wide, w[c]);
+      r.x[c] = ld_raw(x + at, left, wide);
+      r.y[c] = ld_raw(dy + at, left, wide);
+      if (a.dskip.p) r.k[c] = ld_raw(k + at, left, wide);
+    }
+  };
+  // rows group, group + groups, ..; every row of a workgroup's loop has all its threads
+  long row = (long)blockIdx.x * RPW + sub;
+  Row now, next;
+  if (row < a.rows) load(row, now);
+  for (; row < a.rows; row += stride) {
+    if constexpr (AHEAD)
+      if (row + stride < a.rows) load(row + stride, next);
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int left = a.d - (c * TPR + t) * E;
+      float u[E], w[E], gf[E];
+      unpack_raw<T>(now.x[c], u);
+      unpack_raw<T>(now.y[c], w);
+      unpack_raw<T>(g[c], gf);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        u[c][i] = i < left ? (u[c][i] - st.x) * st.y : 0.f;
-        dg[c][i] += w[c][i] * u[c][i];
-        db[c][i] += w[c][i];
-        w[c][i] *= g[c][i];
-        s1 += w[c][i];
-        s2 += w[c][i] * u[c][i];
+        u[i] = i < left ? (u[i] - now.st.x) * now.st.y : 0.f;
+        dg[c][i] += w[i] * u[i];
+        db[c][i] += w[i];
+        w[i] *= gf[i];
+        s1 += w[i];
+        s2 += w[i] * u[i];
       }
     }
-    s1 = a.rms ? 0.f : row_sum<TPR>(s1, red) * inv_d;
-    s2 = row_sum<TPR>(s2, red) * inv_d;
+    s1 = wave_sum(s1);
+    s2 = wave_sum(s2);
+    if constexpr (TPR > 64) {
+      const int wave = threadIdx.x >> 6;
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) {
+        red[wave] = s1;
+        red[16 + wave] = s2;
+      }
+      __syncthreads();
+      s1 = s2 = 0.f;
+#pragma unroll
+      for (int v = 0; v < TPR / 64; ++v) {
+        s1 += red[v];
+        s2 += red[16 + v];
+      }
+    }
+    s1 = a.rms ? 0.f : s1 * inv_d;
+    s2 *= inv_d;
     T* dx = static_cast<T*>(a.dx.p) + row * a.dx.t;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int at = (c * TPR + t) * E, left = a.d - at;
       if (left <= 0) continue;
-      float k[E];
-      if (a.dskip.p) ld_piece(static_cast<const T*>(a.dskip.p) + row * a.dskip.t + at, left, wide, k);
+      float u[E], w[E], gf[E], k[E];
+      unpack_raw<T>(now.x[c], u);
+      unpack_raw<T>(now.y[c], w);
+      unpack_raw<T>(g[c], gf);
+      unpack_raw<T>(now.k[c], k);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        const float v = st.y * (w[c][i] - s1 - u[c][i] * s2);
-        w[c][i] = a.dskip.p ? v + k[i] : v;
+        const float v = now.st.y * (w[i] * gf[i] - s1 - (u[i] - now.st.x) * now.st.y * s2);
+        w[i] = a.dskip.p ? v + k[i] : v;
       }
-      st_piece(dx + at, left, wide, w[c]);
+      st_piece(dx + at, left, wide, w);
     }
+    if constexpr (AHEAD) now = next;
+    else if (row + stride < a.rows) load(row + stride, now);
   }
   if (!a.part) return;
   // the row groups of a workgroup, then its sums: part[group][0: dgain, 1: dshift][d]
@@ -208,40 +276,45 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_k(NormArgs a, 
   }
 }
 
-// dgain += the workgroups' sums, dshift likewise (blockIdx.y 1): 32 columns and 8 shares of the groups per workgroup
-__global__ __launch_bounds__(256) void norm_sums_k(NormArgs a) {
-  __shared__ float red[8][33];
+// dgain += the workgroups' sums, dshift likewise (blockIdx.y 1): 32 columns and 32 shares of the groups per workgroup
+__global__ __launch_bounds__(1024) void norm_sums_k(NormArgs a) {
+  __shared__ float red[32][33];
   float* dst = blockIdx.y ? a.dshift : a.dgain;
   if (!dst) return;
   const int col = threadIdx.x & 31, share = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
   float v = 0.f;
-  if (c < a.d)
-    for (int g = share; g < a.groups; g += 8) v += a.part[((long)g * 2 + blockIdx.y) * a.d + c];
+  if (c < a.d) {
+    const float* p = a.part + (long)blockIdx.y * a.d + c;
+#pragma unroll 8
+    for (int g = share; g < a.groups; g += 32) v += p[(long)g * 2 * a.d];
+  }
   red[share][col] = v;
   __syncthreads();
   if (share || c >= a.d) return;
+  v = 0.f;
 #pragma unroll
-  for (int s = 1; s < 8; ++s) v += red[s][col];
+  for (int s = 0; s < 32; ++s) v += red[s][col];
   dst[c] += v;
 }
 
-// threads per row and pieces per thread: a wave takes up to four pieces per lane
+// threads per row and pieces per thread
 struct NormShape {
   int tpr, ch;
 };
-static NormShape norm_shape(int dtype, int d) {
+static NormShape norm_shape(int dtype, int d, bool back) {
   const int pieces = (d + (dtype == DT_BF16 ? 7 : 3)) / (dtype == DT_BF16 ? 8 : 4);
+  // four pieces to a lane in the forward, two in the backward, which holds three rows and the columns' sums
   for (int tpr : {64, 256, 1024})
     for (int ch : {1, 2, 4})
-      if (tpr * ch >= pieces) return {tpr, ch};
+      if (tpr * ch >= pieces && (!back || ch < 4 || tpr == 1024)) return {tpr, ch};
   return {0, 0};
 }
 
 int norm_groups(int dtype, long rows, int d) {
-  const NormShape f = norm_shape(dtype, d);
+  const NormShape f = norm_shape(dtype, d, true);
   const int rpw = f.tpr >= 256 ? 1 : 256 / f.tpr;
   const long wgs = (rows + rpw - 1) / rpw;
-  return (int)(wgs < 512 ? wgs : 512);
+  return (int)(wgs < 1024 ? wgs : 1024);
 }
 
 static bool rows_wide(const NormRows& r, int es) {
@@ -251,13 +324,15 @@ static bool rows_wide(const NormRows& r, int es) {
 template <typename T, int TPR, int CH>
 static hipError_t norm_go(const NormArgs& a, bool back, bool wide, hipStream_t s) {
   constexpr int NT = TPR > 256 ? TPR : 256, RPW = NT / TPR;
-  if (back) RG_LAUNCH((norm_bwd_k<T, TPR, CH>), dim3(a.groups), dim3(NT), 0, s, a, wide);
-  else {
+  if (back) {
+    if constexpr (CH < 4 || TPR == 1024) RG_LAUNCH((norm_bwd_k<T, TPR, CH, CH * VE<T> <= 16 && (TPR < 1024 || CH == 1)>), dim3(a.groups), dim3(NT), 0, s, a, wide);
+    else return hipErrorInvalidValue;
+    if (a.part) RG_LAUNCH(norm_sums_k, dim3((a.d + 31) / 32, 2), dim3(1024), 0, s, a);
+  } else {
     // HIP takes fewer than 2^32 threads in a dimension of a launch
     const long wgs = (a.rows + RPW - 1) / RPW, y = (wgs + (1l << 21) - 1) >> 21;
     RG_LAUNCH((norm_fwd_k<T, TPR, CH>), dim3((unsigned)((wgs + y - 1) / y), (unsigned)y), dim3(NT), 0, s, a, wide);
   }
-  if (back && a.part) RG_LAUNCH(norm_sums_k, dim3((a.d + 31) / 32, 2), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -268,13 +343,15 @@ static hipError_t norm_t(int dtype, const NormArgs& a, bool back, hipStream_t s)
   const bool wide = a.d % VE<T> == 0 && rows_wide(a.x, es) && rows_wide(a.res, es) && rows_wide(a.s, es) &&
                     rows_wide(a.y, es) && rows_wide(a.dy, es) && rows_wide(a.dskip, es) && rows_wide(a.dx, es) &&
                     al(a.gain) && al(a.shift);
-  const NormShape f = norm_shape(dtype, a.d);
+  const NormShape f = norm_shape(dtype, a.d, back);
   switch (f.tpr * 8 + f.ch) {
     case 64 * 8 + 1: return norm_go<T, 64, 1>(a, back, wide, s);
     case 64 * 8 + 2: return norm_go<T, 64, 2>(a, back, wide, s);
     case 64 * 8 + 4: return norm_go<T, 64, 4>(a, back, wide, s);
+    case 256 * 8 + 1: return norm_go<T, 256, 1>(a, back, wide, s);
     case 256 * 8 + 2: return norm_go<T, 256, 2>(a, back, wide, s);
     case 256 * 8 + 4: return norm_go<T, 256, 4>(a, back, wide, s);
+    case 1024 * 8 + 1: return norm_go<T, 1024, 1>(a, back, wide, s);
     case 1024 * 8 + 2: return norm_go<T, 1024, 2>(a, back, wide, s);
     case 1024 * 8 + 4: return norm_go<T, 1024, 4>(a, back, wide, s);
   }

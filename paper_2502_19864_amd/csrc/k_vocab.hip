@@ -392,13 +392,17 @@ __global__ __launch_bounds__(256) void vocab_rows_k(VocabArgs a) {
   }
   p = join_wave(p);
   if (lane) return;
+  if (a.few && a.labels && !counts(a, a.labels[m])) {
+    a.loss[m] = a.lse[m] = 0.f;
+    return;
+  }
   const float log_l = logf(p.l);
   if (a.token) {
     a.token[a.row0 + m] = p.at;
     a.logprob[a.row0 + m] = -log_l;
     return;
   }
-  const int row = a.idx[a.row0 + m];
+  const int row = a.few ? m : a.idx[a.row0 + m];
   a.loss[row] = (p.m - a.target[a.row0 + m]) + log_l;  // not lse - s: of a row that is sure of its label little is left
   a.lse[row] = p.m + log_l;
 }
@@ -472,7 +476,8 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   a.Vp = (int)up(a.V, 64);
   a.dp = (int)up(a.d, 64);
   a.bn = low ? vocab_mm_bn(a.n, a.d, a.V) : f32_small(a.n, a.V) ? 32 : 128;
-  a.tiles = (a.V + a.bn - 1) / a.bn;
+  a.few = low && !grads && vocab_few(a.n, a.d);
+  a.tiles = a.few ? vocab_few_wgs(a.n, a.d) : (a.V + a.bn - 1) / a.bn;
   // rows at a time: 2^29 logits (2 GiB), 2^24 partial sums; whole tiles of rows
   const long most = grads ? (1l << 29) / a.Vp : (1l << 24) / a.tiles;
   a.R = (int)(np <= most ? np : most / 256 * 256 > 256 ? most / 256 * 256 : 256);
@@ -483,10 +488,12 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
     at = (at + bytes + 255) & ~(size_t)255;
     return p;
   };
-  a.hc = take((size_t)np * a.dp * es);
+  a.hc = a.few ? nullptr : take((size_t)np * a.dp * es);
   a.part = static_cast<float2*>(take((size_t)a.R * a.tiles * 8));
   a.part_at = next ? static_cast<int*>(take((size_t)a.R * a.tiles * 4)) : nullptr;
-  if (!next) {
+  if (a.few) {
+    a.target = next ? nullptr : static_cast<float*>(take((size_t)a.n * 4));
+  } else if (!next) {
     a.n_counted = static_cast<int*>(take(4));
     a.block_count = a.n > PICK_DIRECT ? static_cast<int*>(take((size_t)(np / 1024 + 1) * 4)) : nullptr;
     a.idx = static_cast<int*>(take((size_t)a.n * 4));
@@ -539,6 +546,12 @@ template <typename T>
 static hipError_t vocab_t(VocabArgs a, hipStream_t s) {
   constexpr bool low = sizeof(T) == 2;
   const bool grads = a.dh || a.dw;
+  if (a.few) {
+    a.rows = a.n;
+    launch_vocab_few_bf16(a, s);
+    RG_LAUNCH(vocab_rows_k, dim3((a.n + 3) / 4), dim3(256), 0, s, a);
+    return hipGetLastError();
+  }
   if (a.labels && a.block_count) RG_LAUNCH(vocab_count_k, dim3((a.n + 1023) / 1024), dim3(256), 0, s, a);
   const bool wide = (reinterpret_cast<uintptr_t>(a.h) & 15u) == 0 && a.ldh * sizeof(T) % 16 == 0 && a.d * sizeof(T) % 16 == 0;
   RG_LAUNCH(vocab_pick_k<T>, dim3((a.n + PICK_ROWS - 1) / PICK_ROWS), dim3(256), 0, s, a, wide);

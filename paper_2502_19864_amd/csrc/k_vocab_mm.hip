@@ -395,6 +395,193 @@ __global__ __launch_bounds__(256) void vocab_dh_sum_k(VocabArgs a, VocabProduct 
   *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dh) + (long)a.idx[a.row0 + m] * a.lddh + n) = pack_frag(v);
 }
 
+// ---------------------------------------------------------------- few rows
+// Statistics of the logits of up to 32 rows: w is read once, by far the most of the work, and straight into registers. A
+// wave makes 16 classes at a time by MFMA 16x16x32, its A operand 16 rows of w, B the rows of h, kept in LDS for all
+// waves.  STEPS loads of 1 KB are in flight per wave while the last STEPS are multiplied, over the ends of the blocks of classes
+// too.  Where classes are few, KS waves share a block's k.  One (maximum, sum, place) per row and workgroup is left.
+template <int NB, int KS, int LDSB>
+__global__ __launch_bounds__(512, LDSB > 65536 ? 2 : 4) void vocab_few_k(VocabArgs a, int pitch) {
+  constexpr int STEPS = 8, KC = 32 * STEPS, NW = 8, GRP = NW / KS;  // GRP groups of KS waves
+  __shared__ __attribute__((aligned(16))) char smem[LDSB];
+  __shared__ float red[NW][NB][16 * 17];
+  const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), grp = wave / KS, ks = wave % KS;
+  const int chunks = (a.d + KC - 1) / KC, mine = (chunks - ks + KS - 1) / KS;  // of k: ks, ks + KS, ..
+  const bf16* h = static_cast<const bf16*>(a.h);
+  for (int i = tid; i < a.n * (pitch / 16); i += 512) {
+    const int r = i / (pitch / 16), k = i % (pitch / 16) * 8;
+    *reinterpret_cast<uint4*>(smem + r * pitch + k * 2) =
+        k < a.d ? *reinterpret_cast<const uint4*>(h + (long)r * a.ldh + k) : make_uint4(0, 0, 0, 0);
+  }
+  const int blocks = (a.V + 15) / 16, stride = gridDim.x * GRP;
+  const int first = grp * gridDim.x + blockIdx.x;  // few blocks go to as many workgroups
+  int blk = first, c = 0;                          // what is loaded next
+  // KS waves meet at barriers, so all groups of a workgroup go as many rounds
+  const int rounds = max(0, (blocks - (KS > 1 ? (int)blockIdx.x : first) + stride - 1) / stride);
+  const bf16* w = static_cast<const bf16*>(a.w);
+  bf16x8 x[2][STEPS];
+  auto load = [&](bf16x8 (&y)[STEPS]) {
+    const bf16* row = w + (long)min(blk * 16 + l16, a.V - 1) * a.ldw;
+    const int k0 = (ks + c * KS) * KC + g4 * 8;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {  // past d: the row's first elements, against zeros of h
+      const int k = k0 + s * 32;
+      y[s] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(row + (k < a.d ? k : 0)));
+    }
+    if (++c >= mine) {
+      c = 0;
+      blk += stride;
+    }
+  };
+  const char* hb[NB];
+  int lab[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int r = b * 16 + l16;
+    hb[b] = smem + min(r, a.n - 1) * pitch + g4 * 16;
+    lab[b] = a.labels && r < a.n ? a.labels[r] : -1;
+  }
+  f32x4 acc[NB];
+  Peak p[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    p[b] = Peak{-INFINITY, 0.f, INT32_MAX};
+  }
+  __syncthreads();
+  // the four logits of this lane, classes v .. v + 3, into its running statistics
+  auto take = [&](int b, int v, const f32x4& s) {
+    float m = p[b].m;
+    int at = p[b].at;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (v + e < a.V) {
+        if (s[e] > m) {
+          m = s[e];
+          at = v + e;
+        }
+        if (v + e == lab[b]) a.target[b * 16 + l16] = s[e];
+      }
+    const float z = m == -INFINITY ? 0.f : m;
+    float l = p[b].l * exp_below(p[b].m - z);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (v + e < a.V) l += exp_below(s[e] - z);
+    p[b] = Peak{m, l, at};
+  };
+  auto mul = [&](const bf16x8 (&y)[STEPS], int kc) {
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        acc[b] = mfma16(y[s], *reinterpret_cast<const bf16x8*>(hb[b] + kc * (KC * 2) + s * 64), acc[b]);
+  };
+  const int steps = rounds * mine;
+  int done = 0, at_blk = first;  // what is multiplied
+  auto finish = [&] {
+    if (++done < mine) return;
+    done = 0;
+    if constexpr (KS > 1) {  // the shares, in their order
+      __syncthreads();
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) red[wave][b][(4 * g4 + e) * 17 + l16] = acc[b][e];
+      __syncthreads();
+    }
+    if (ks == 0 && at_blk < blocks) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        f32x4 s = acc[b];
+        if constexpr (KS > 1)
+#pragma unroll
+          for (int q = 1; q < KS; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += red[wave + q][b][(4 * g4 + e) * 17 + l16];
+        take(b, at_blk * 16 + 4 * g4, s);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    at_blk += stride;
+  };
+  if constexpr (KS > 1) {
+    // every wave of the workgroup passes the same number of barriers: a round each
+    for (int r = 0; r < rounds; ++r) {
+      const int have = blk < blocks ? mine : 0;
+      if (have) load(x[0]);
+      for (int i = 0; i < have; i += 2) {
+        if (i + 1 < have) load(x[1]);
+        mul(x[0], ks + i * KS);
+        if (i + 1 < have) {
+          if (i + 2 < have) load(x[0]);
+          mul(x[1], ks + (i + 1) * KS);
+        }
+      }
+      done = mine;
+      finish();
+    }
+  } else {
+    if (steps) load(x[0]);
+    for (int i = 0; i < steps; i += 2) {
+      if (i + 1 < steps) load(x[1]);
+      mul(x[0], done);
+      finish();
+      if (i + 1 < steps) {
+        if (i + 2 < steps) load(x[0]);
+        mul(x[1], done);
+        finish();
+      }
+    }
+  }
+  // lanes of a row, then waves
+  __syncthreads();
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1) p[b] = join(p[b], Peak{__shfl_xor(p[b].m, o), __shfl_xor(p[b].l, o), __shfl_xor(p[b].at, o)});
+    if (lane < 16) {
+      red[wave][b][l16 * 3] = p[b].m;
+      red[wave][b][l16 * 3 + 1] = p[b].l;
+      red[wave][b][l16 * 3 + 2] = __int_as_float(p[b].at);
+    }
+  }
+  __syncthreads();
+  if (tid < a.n) {
+    Peak q{-INFINITY, 0.f, INT32_MAX};
+    for (int v = 0; v < NW; ++v) {
+      const float* r = red[v][tid / 16] + tid % 16 * 3;
+      q = join(q, Peak{r[0], r[1], __float_as_int(r[2])});
+    }
+    a.part[(long)tid * a.tiles + blockIdx.x] = make_float2(q.m, q.l);
+    if (a.part_at) a.part_at[(long)tid * a.tiles + blockIdx.x] = min(q.at, a.V - 1);
+  }
+}
+
+// rows of h in LDS, whose 16-byte pieces of one k lie in different banks
+static int few_pitch(int d) { return (d + 255) / 256 * 512 + 16; }
+// up to 32 rows that fit the LDS beside the partial sums: 0 if not, else the LDS that is taken
+static int few_lds(int rows, int d) {
+  const long bytes = (long)rows * few_pitch(d);
+  return rows > 32 || bytes > 131072 ? 0 : bytes > 49152 ? 131072 : 49152;
+}
+bool vocab_few(int rows, int d) { return few_lds(rows, d) > 0; }
+int vocab_few_wgs(int rows, int d) { return few_lds(rows, d) > 65536 ? 256 : 512; }
+
+template <int NB, int KS>
+static void go_few(const VocabArgs& a, hipStream_t s) {
+  const int pitch = few_pitch(a.d);
+  if (few_lds(a.n, a.d) > 65536) RG_LAUNCH((vocab_few_k<NB, KS, 131072>), dim3(a.tiles), dim3(512), 0, s, a, pitch);
+  else RG_LAUNCH((vocab_few_k<NB, KS, 49152>), dim3(a.tiles), dim3(512), 0, s, a, pitch);
+}
+void launch_vocab_few_bf16(const VocabArgs& a, hipStream_t s) {
+  // a block of 16 classes to every wave where there are as many, else their k dealt to four
+  const bool share = (a.V + 15) / 16 < a.tiles * 8 / 2;
+  if (a.n <= 16) share ? go_few<1, 4>(a, s) : go_few<1, 1>(a, s);
+  else share ? go_few<2, 4>(a, s) : go_few<2, 1>(a, s);
+}
+
 static int tiles_of(int x, int t) { return (x + t - 1) / t; }
 
 template <int BM, int BN, int WM, int WN, int NS, bool KA, bool KB, Prod E>

@@ -257,6 +257,7 @@ struct VocabArgs {
   void* dw; long lddw;          // [V][d] or null
   int* token; float* logprob;   // [n]: without labels
   // workspace
+  int few;                      // forward of a few rows in bf16: they are not picked, labels are read as they are
   int dp, Vp, bn, tiles, R;     // d and V up to a multiple of 64, column tiles of the logits, rows at a time
   void* hc;                     // [n up][dp]: the rows that count, zeros past d
   float2* part; int* part_at;   // [R][tiles]
@@ -275,6 +276,9 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws);
 // the bf16 products (k_vocab_mm.hip): columns of a tile of logits, bytes of dh_part, the launches of one piece
 int vocab_mm_bn(int rows, int d, int V);
 size_t vocab_dh_part_bytes(int rows, int d, int V);
+bool vocab_few(int rows, int d);         // whether rows are few enough to read w straight into registers
+int vocab_few_wgs(int rows, int d);
+void launch_vocab_few_bf16(const VocabArgs& a, hipStream_t s);
 void launch_vocab_logits_bf16(const VocabArgs& a, bool keep, hipStream_t s);
 void launch_vocab_dh_bf16(const VocabArgs& a, hipStream_t s);
 void launch_vocab_dw_bf16(const VocabArgs& a, hipStream_t s);

@@ -4,7 +4,7 @@ may be off.
 The bounds count roundings.  u is half a step of the storage type (bf16 2^-8, fp32
 2^-24), e = 2^-24 that of the fp32 arithmetic.  A sum of n fp32 terms held by many threads is off by at most (steps in a
 row) e of the terms' absolute values: 64 where a row is summed (32 in a thread, then a tree), rows / groups +
-groups / 8 + 16 for the sums over rows; a matrix product of n terms by about 8 sqrt(n) e of them.
+groups / 32 + 64 for the sums over rows; a matrix product of n terms by about 8 sqrt(n) e of them.
 """
 import math
 
@@ -17,7 +17,7 @@ def half_step(dtype):
     return torch.finfo(dtype).eps / 2
 
 
-def norm(s, gain, shift, rms, eps, dy=None, dskip=None, groups=512):
+def norm(s, gain, shift, rms, eps, dy=None, dskip=None, groups=1024):
     """{name: (value, bound)} of y and with dy of dx, dgain, dshift; s [rows, d] as stored."""
     u, k = half_step(s.dtype), 64 * E
     x, g = s.double(), gain.double()
@@ -47,7 +47,7 @@ def norm(s, gain, shift, rms, eps, dy=None, dskip=None, groups=512):
         e = e + 2 * E * dx.abs()
     out["dx"] = (dx, 1.01 * e + u * dx.abs() * 1.01)
     rows = s.shape[0]
-    kr = (rows / max(1, min(rows, groups)) + groups / 8 + 16) * E
+    kr = (rows / max(1, min(rows, groups)) + groups / 32 + 64) * E
     out["dgain"] = ((d * xh).sum(0), (kr * (d * xh).abs() + d.abs() * exh).sum(0) * 1.01)
     out["dshift"] = (d.sum(0), kr * d.abs().sum(0) * 1.01)
     return out
