@@ -79,7 +79,11 @@ __global__ __launch_bounds__(256) void vocab_pick_k(VocabArgs a, bool wide) {
         if (lane == 0) a.loss[n] = a.lse[n] = 0.f;
         if (a.dh) {
           T* dst = static_cast<T*>(a.dh) + (long)n * a.lddh;
-          for (int k = lane; k < a.d; k += 64) dst[k] = T(0);
+          if constexpr (sizeof(T) == 2) {
+            for (int k = lane * 8; k < a.d; k += 512) *reinterpret_cast<uint4*>(dst + k) = make_uint4(0, 0, 0, 0);
+          } else {
+            for (int k = lane; k < a.d; k += 64) dst[k] = T(0);
+          }
         }
         continue;
       }
@@ -112,12 +116,9 @@ struct F32Product {
   const float* B; long ldb;
   int M, N, K;     // M of dw, k of the logits and of dh; the others are the rows that count
   bool vb;         // B's rows are 16-byte aligned (A's always are)
-  int slots;       // dh: workgroups of one round
+  int slots;       // dh, dw: workgroups of one round
 };
-// shares of dh's k per tile, each of 256 columns at least
-__device__ __forceinline__ int f32_splits(const F32Product& p, int tiles) {
-  return max(1, min(min(p.slots / tiles, p.K / 256), 64));
-}
+constexpr int F32_LEAST = 256;  // of k to a share
 
 __device__ __forceinline__ void ld8_f32(const float* p, int valid, bool wide, float v[8]) {
   if (wide && valid >= 8) {
@@ -129,6 +130,15 @@ __device__ __forceinline__ void ld8_f32(const float* p, int valid, bool wide, fl
   }
 }
 
+template <Prod E>
+__device__ __forceinline__ void f32_gradient(const VocabArgs& a, int m, int n, float v) {
+  if constexpr (E == Prod::Dh) {
+    static_cast<float*>(a.dh)[(long)a.idx[a.row0 + m] * a.lddh + n] = v;
+  } else {
+    float* o = static_cast<float*>(a.dw) + (long)m * a.lddw + n;
+    *o = a.first ? v : *o + v;
+  }
+}
 // the tile's sums, cf[row * CP + column], into what the product is for
 template <int BT, int CP, Prod E>
 __device__ __forceinline__ void f32_epilogue(const VocabArgs& a, const F32Product& p, const float* cf, int M, int N, int m0, int n0,
@@ -168,18 +178,13 @@ __device__ __forceinline__ void f32_epilogue(const VocabArgs& a, const F32Produc
           *reinterpret_cast<float4*>(a.logits + (long)(m0 + r) * a.Vp + n0 + c) = *reinterpret_cast<const float4*>(cf + r * CP + c);
       }
   } else {
-    float* part = a.dh_part + ((long)split * tiles + tile) * (BT * BT);
+    float* part = a.shares + ((long)split * tiles + tile) * (BT * BT);
     for (int i = tid; i < BT * BT; i += 256) {
       const int r = i / BT, c = i % BT, m = m0 + r, n = n0 + c;
       if (m >= M || n >= N) continue;
       const float v = cf[r * CP + c];
-      if constexpr (E == Prod::Dh) {
-        if (splits > 1) part[i] = v;
-        else static_cast<float*>(a.dh)[(long)a.idx[a.row0 + m] * a.lddh + n] = v;
-      } else {
-        float* o = static_cast<float*>(a.dw) + (long)m * a.lddw + n;
-        *o = a.first ? v : *o + v;
-      }
+      if (splits > 1) part[i] = v;
+      else f32_gradient<E>(a, m, n, v);
     }
   }
 }
@@ -195,11 +200,12 @@ __global__ __launch_bounds__(256) void vocab_f32_k(VocabArgs a, F32Product p) {
   const int cnt = piece_rows(a);
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
   const int tn = (N + BT - 1) / BT, tiles = (M + BT - 1) / BT * tn;
-  const int splits = E == Prod::Dh && tiles ? f32_splits(p, tiles) : 1;
+  const int Kall = E == Prod::Dw ? cnt : p.K;
+  const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? k_shares(p.slots, tiles, Kall, F32_LEAST) : 1;
   if ((int)blockIdx.x >= tiles * splits) return;
   const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
   const int m0 = tile / tn * BT, n0 = tile % tn * BT;
-  const int Kall = E == Prod::Dw ? cnt : p.K, nkt = (Kall + BK - 1) / BK;
+  const int nkt = (Kall + BK - 1) / BK;
   const int kb = (int)((long)nkt * split / splits) * BK, K = min(Kall, (int)((long)nkt * (split + 1) / splits) * BK);
   f32x16 acc[2][2], sum[2][2];
 #pragma unroll
@@ -301,11 +307,12 @@ __global__ __launch_bounds__(256) void vocab_f32_small_k(VocabArgs a, F32Product
   const int cnt = piece_rows(a);
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
   const int tn = (N + BT - 1) / BT, tiles = (M + BT - 1) / BT * tn;
-  const int splits = E == Prod::Dh && tiles ? f32_splits(p, tiles) : 1;
+  const int Kall = E == Prod::Dw ? cnt : p.K;
+  const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? k_shares(p.slots, tiles, Kall, F32_LEAST) : 1;
   if ((int)blockIdx.x >= tiles * splits) return;
   const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
   const int m0 = tile / tn * BT, n0 = tile % tn * BT;
-  const int Kall = E == Prod::Dw ? cnt : p.K, n8 = (Kall + 7) / 8;
+  const int n8 = (Kall + 7) / 8;
   const int kb = (int)((long)n8 * split / splits) * 8, K = min(Kall, (int)((long)n8 * (split + 1) / splits) * 8);
   f32x16 acc, sum;
 #pragma unroll
@@ -359,17 +366,19 @@ __global__ __launch_bounds__(256) void vocab_f32_small_k(VocabArgs a, F32Product
   f32_epilogue<BT, CP, E>(a, p, red[0], M, N, m0, n0, tile, split, splits, tiles);
 }
 
-// dh of a piece from its splits' sums, in their order
-__global__ __launch_bounds__(256) void vocab_f32_dh_sum_k(VocabArgs a, F32Product p, int bt) {
-  const int cnt = piece_rows(a), m = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
-  if (m >= cnt || n >= p.N) return;
-  const int tn = (p.N + bt - 1) / bt, tiles = (cnt + bt - 1) / bt * tn, splits = f32_splits(p, tiles);
+// dh or dw of a piece from its shares, in their order
+template <Prod E>
+__global__ __launch_bounds__(256) void vocab_f32_shares_k(VocabArgs a, F32Product p, int bt) {
+  const int cnt = piece_rows(a), M = E == Prod::Dw ? p.M : cnt, K = E == Prod::Dw ? cnt : p.K;
+  const int m = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
+  if (m >= M || n >= p.N) return;
+  const int tn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * tn, splits = k_shares(p.slots, tiles, K, F32_LEAST);
   if (splits == 1) return;
-  const float* q = a.dh_part + (long)(m / bt * tn + n / bt) * bt * bt + (m % bt) * bt + n % bt;
+  const float* q = a.shares + (long)(m / bt * tn + n / bt) * bt * bt + (m % bt) * bt + n % bt;
   float v = 0.f;
 #pragma unroll 8
   for (int s = 0; s < splits; ++s) v += q[(long)s * tiles * bt * bt];
-  static_cast<float*>(a.dh)[(long)a.idx[a.row0 + m] * a.lddh + n] = v;
+  f32_gradient<E>(a, m, n, v);
 }
 
 // ---------------------------------------------------------------- rows
@@ -432,6 +441,7 @@ __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
     lse = p.m + log_l;
     loss = (p.m - a.target[a.row0 + m]) + log_l;  // not lse - s: of a row that is sure of its label little is left
     g = a.g_c[a.row0 + m];
+    if constexpr (sizeof(T) == 2) g /= dloss_unit(a);
     lab = a.lab_c[a.row0 + m];
     if (blockIdx.y == 0 && tid == 0) {
       const int row = a.idx[a.row0 + m];
@@ -504,7 +514,8 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
     a.g_c = static_cast<float*>(take((size_t)a.n * 4));
     a.logits = static_cast<float*>(take((size_t)a.R * a.Vp * 4));
     a.P = low ? take((size_t)a.R * a.Vp * 2) : a.logits;
-    a.dh_part = static_cast<float*>(take(low ? vocab_dh_part_bytes(a.n, a.d, a.V) : (size_t)F32_SLOTS * 4 * (f32_small(a.n, a.d) ? 1024 : 16384)));
+    a.shares = static_cast<float*>(take(low ? vocab_share_bytes(a.n, a.d, a.V)
+                                            : (size_t)F32_SLOTS * 4 * (f32_small(a.n, a.d) && f32_small(a.V, a.d) ? 1024 : 16384)));
     if (low && a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
     a.ld_acc = a.d;
   }
@@ -513,14 +524,17 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
 
 template <bool KA, bool KB, Prod E>
 static void go_f32(const VocabArgs& a, F32Product p, bool small, hipStream_t s) {
+  constexpr bool shared = E == Prod::Dh || E == Prod::Dw;
   const int bt = small ? 32 : 128;
-  const long rows = E == Prod::Dw ? p.M : a.rows;
-  long wgs = (up(rows, bt) / bt) * (up(p.N, bt) / bt);
+  const long rows = E == Prod::Dw ? p.M : a.rows, tiles = (up(rows, bt) / bt) * (up(p.N, bt) / bt);
+  const int K = E == Prod::Dw ? a.rows : p.K;
   p.slots = F32_SLOTS;
-  if (E == Prod::Dh && wgs < F32_SLOTS) wgs = F32_SLOTS;
-  if (small) RG_LAUNCH((vocab_f32_small_k<KA, KB, E>), dim3((unsigned)wgs), dim3(256), 0, s, a, p);
-  else RG_LAUNCH((vocab_f32_k<KA, KB, E>), dim3((unsigned)wgs), dim3(256), 0, s, a, p);
-  if (E == Prod::Dh && a.V >= 512) RG_LAUNCH(vocab_f32_dh_sum_k, dim3(a.rows, (p.N + 255) / 256), dim3(256), 0, s, a, p, bt);
+  const unsigned wgs = (unsigned)(shared && tiles < F32_SLOTS ? F32_SLOTS : tiles);
+  if (small) RG_LAUNCH((vocab_f32_small_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, p);
+  else RG_LAUNCH((vocab_f32_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, p);
+  // dw's tiles are known here, dh's may be fewer
+  if (shared && k_shares(F32_SLOTS, E == Prod::Dw ? (int)tiles : 1, K, F32_LEAST) > 1)
+    RG_LAUNCH((vocab_f32_shares_k<shared ? E : Prod::Dh>), dim3((unsigned)rows, (p.N + 255) / 256), dim3(256), 0, s, a, p, bt);
 }
 
 static void vocab_products_f32(const VocabArgs& a, int which, hipStream_t s) {

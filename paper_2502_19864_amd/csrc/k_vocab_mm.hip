@@ -41,13 +41,14 @@ __device__ __forceinline__ void spread_reads(std::integer_sequence<int, Q...>) {
   }(), ...);
 }
 
-// One operand of a product: R rows (of the tile) by 64 k, KMAJOR: [rows][k] in memory.
-template <int R, int NW, bool KMAJOR>
+// One operand of a product: R rows (of the tile) by BK k, KMAJOR: [rows][k] in memory.
+template <int R, int BK, int NW, bool KMAJOR>
 struct Operand {
-  static constexpr int L = R / (8 * NW);            // DMA instructions per wave and tile
-  static constexpr int CPR = KMAJOR ? 8 : R / 8;    // chunks per LDS row
+  static constexpr int L = R * BK / (512 * NW);     // DMA instructions per wave and tile
+  static constexpr int CPR = (KMAJOR ? BK : R) / 8; // chunks per LDS row
   static constexpr int RPI = 64 / CPR;              // LDS rows per instruction
-  static_assert(L * 8 * NW == R && (KMAJOR || R >= 128), "whole instructions; four groups of columns");
+  static constexpr int SWD = 16 / CPR;              // KMAJOR: rows of one swizzle
+  static_assert(L * 512 * NW == R * BK && (KMAJOR || R >= 128), "whole instructions; four groups of columns");
   const char* base;   // the tile's first element
   long step;          // bytes per k-tile
   uint32_t off[L];    // per-lane byte offsets within a k-tile
@@ -56,20 +57,20 @@ struct Operand {
   __device__ __forceinline__ void init(const bf16* p, long ld, int first, int rows, int wave, int lane) {
     ld2 = (uint32_t)ld * 2;
     base = uniform_ptr(reinterpret_cast<const char*>(KMAJOR ? p + (long)first * ld : p + first));
-    step = KMAJOR ? 128 : ld * 128;
+    step = KMAJOR ? BK * 2 : ld * (BK * 2);
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       const int r = (i * NW + wave) * RPI + lane / CPR, pos = lane % CPR;
-      if constexpr (KMAJOR) off[i] = (uint32_t)min(r, rows - 1 - first) * ld2 + (pos ^ ((r >> 1) & 7)) * 16;
+      if constexpr (KMAJOR) off[i] = (uint32_t)min(r, rows - 1 - first) * ld2 + (pos ^ (r / SWD % CPR)) * 16;
       else off[i] = (uint32_t)r * ld2 + min(pos ^ ((r & 3) << 2), (rows - first + 7) / 8 - 1) * 16;
     }
   }
-  // instruction i of k-tile kt; left: k of this tile that the operand has (64: all).  Past them the last ones are read again.
+  // instruction i of k-tile kt; left: k of this tile that the operand has (BK: all).  Past them the last ones are read again.
   __device__ __forceinline__ void dma(int i, int kt, int left, uint32_t lds, int wave, int wave_u, int lane) const {
     uint32_t o = off[i];
-    if (left < 64) {
+    if (left < BK) {
       const int r = (i * NW + wave) * RPI + lane / CPR;
-      if constexpr (KMAJOR) o -= max(0, (lane % CPR ^ ((r >> 1) & 7)) - (left / 8 - 1)) * 16;
+      if constexpr (KMAJOR) o -= max(0, (lane % CPR ^ (r / SWD % CPR)) - (left / 8 - 1)) * 16;
       else o -= max(0, r - (left - 1)) * ld2;
     }
     dma16_m0(base + (long)kt * step, o, lds + (i * NW + wave_u) * 1024);
@@ -77,12 +78,12 @@ struct Operand {
 };
 
 // Fragments of F blocks of 32 rows from first row r0 of the tile in LDS
-template <int R, int F, bool KMAJOR>
+template <int R, int BK, int F, bool KMAJOR>
 struct Frags {
   uint32_t at[KMAJOR ? 1 : F];
   __device__ __forceinline__ void init(int r0, int lane) {
     if constexpr (KMAJOR) {
-      at[0] = (r0 + (lane & 31)) * 128;
+      at[0] = (r0 + (lane & 31)) * (BK * 2);
     } else {
       const int g = lane >> 4, r = lane & 15;
 #pragma unroll
@@ -92,9 +93,10 @@ struct Frags {
   }
   __device__ __forceinline__ void read(const char* tile, int ks, int lane, bf16x8 (&f)[F]) const {
     if constexpr (KMAJOR) {
-      const char* p = tile + at[0] + 16 * ((2 * ks + (lane >> 5)) ^ ((lane >> 1) & 7));
+      constexpr int CPR = BK / 8;
+      const char* p = tile + at[0] + 16 * ((2 * ks + (lane >> 5)) ^ ((lane & 31) / (16 / CPR) % CPR));
 #pragma unroll
-      for (int i = 0; i < F; ++i) f[i] = *reinterpret_cast<const bf16x8*>(p + i * 32 * 128);
+      for (int i = 0; i < F; ++i) f[i] = *reinterpret_cast<const bf16x8*>(p + i * 32 * (BK * 2));
     } else {
 #pragma unroll
       for (int i = 0; i < F; ++i) {
@@ -112,14 +114,9 @@ struct VocabProduct {
   const bf16* B; long ldb;
   int M, N;        // M: of dw (the logits and dh have the rows that count)
   int K;           // k of the logits (d) and of dh (V)
-  int slots;       // dh: workgroups of one round
+  int slots;       // dh, dw: workgroups of one round
 };
-// dh's k (the vocabulary) is dealt to several workgroups per tile where the tiles of the rows that count leave CUs
-// idle, eight k-tiles at least to each
-__host__ __device__ inline int dh_splits(int slots, int tiles, int V) {
-  const int by_slots = slots / tiles, by_k = V / 512, s = by_slots < by_k ? by_slots : by_k;
-  return s < 1 ? 1 : s;
-}
+constexpr int MM_LEAST = 512;  // of k to a share
 
 // The tile of C[m][n] = sum_k A(m, k) B(n, k) that a workgroup makes, by XCD: workgroups are dealt round-robin to the eight
 // XCDs; each takes a contiguous run of a raster in bands of GROUP tile rows, so what its L2 holds is shared.
@@ -135,17 +132,41 @@ __device__ __forceinline__ bool vocab_tile(int g, int ntm, int ntn, int& tm, int
   return true;
 }
 
+// eight columns of a row of dh or dw
+template <Prod E>
+__device__ __forceinline__ void store_gradient(const VocabArgs& a, int m, int n, float unit, float (&v)[8]) {
+  if constexpr (E == Prod::Dh) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= unit;
+    *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dh) + (long)a.idx[a.row0 + m] * a.lddh + n) = pack_frag(v);
+  } else {
+    float* o = a.dw_acc + (long)m * a.ld_acc + n;  // between pieces, in the unit
+    if (!a.first) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += o[e];
+    }
+    if (a.last) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= unit;
+      *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dw) + (long)m * a.lddw + n) = pack_frag(v);
+    } else {
+      *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
+      *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
+    }
+  }
+}
+
 // Workgroups stay: one round of the GPU, each over its tiles.  While a tile is stored the first k-tiles of the next are
 // on their way, and its stores drain under the next one's products (2048 x 32000 logits, d 4096: 1.08 times less than a workgroup per tile).
 // So the epilogue has no LDS but 4 KB per wave beside the stages, and no barrier: each wave sends its 32 x 32 blocks
 // through its own, in 16-byte pieces at c ^ row % 8, and stores whole 128-byte (bf16: 64-byte) runs of rows; the logits'
 // statistics are per wave too, one (maximum, sum) for BN / WN columns.
-template <int BM, int BN, int WM, int WN, int NS, bool KA, bool KB, Prod E>
+template <int BM, int BN, int WM, int WN, int BK, int NS, bool KA, bool KB, Prod E>
 __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabProduct p) {
-  constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32, KS = 4;
-  using OA = Operand<BM, NW, KA>;
-  using OB = Operand<BN, NW, KB>;
-  constexpr int LPT = OA::L + OB::L, STAGE = (BM + BN) * 128;
+  constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32, KS = BK / 16;
+  using OA = Operand<BM, BK, NW, KA>;
+  using OB = Operand<BN, BK, NW, KB>;
+  constexpr int LPT = OA::L + OB::L, STAGE = (BM + BN) * BK * 2;
   constexpr int ND = FM * (KA ? 1 : 2) + FN * (KB ? 1 : 2);
   static_assert(FM * 32 * WM == BM && FN * 32 * WN == BN && NS >= 2 && NS <= 4 && LPT * (NS - 1) < 64, "tile");
   static_assert(NS * STAGE + NW * 4096 <= 160 * 1024, "LDS");
@@ -157,13 +178,14 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
   const int K = E == Prod::Dw ? cnt : p.K;
   const int ntm = (M + BM - 1) / BM, ntn = (N + BN - 1) / BN, tiles = ntm * ntn;
-  const int splits = E == Prod::Dh && tiles ? __builtin_amdgcn_readfirstlane(dh_splits(p.slots, tiles, p.K)) : 1;
-  const int nk_all = (K + 63) / 64;
+  constexpr bool SHARED = E == Prod::Dh || E == Prod::Dw;
+  const int splits = SHARED && tiles ? __builtin_amdgcn_readfirstlane(k_shares(p.slots, tiles, K, MM_LEAST)) : 1;
+  const int nk_all = (K + BK - 1) / BK;
   int m0 = 0, n0 = 0, split = 0, kt0 = 0, nk = 0, tile = 0;
   // the g-th piece of work, or none
   auto locate = [&](int g) {
     if (g >= tiles * splits) return false;
-    if constexpr (E == Prod::Dh) split = __builtin_amdgcn_readfirstlane(g / tiles);
+    if constexpr (SHARED) split = __builtin_amdgcn_readfirstlane(g / tiles);
     int tm, tn;
     vocab_tile<4>(g - split * tiles, ntm, ntn, tm, tn);
     tile = __builtin_amdgcn_readfirstlane(tm * ntn + tn);
@@ -173,16 +195,17 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
     nk = (int)((long)nk_all * (split + 1) / splits) - kt0;
     return true;
   };
+  const float unit = SHARED ? dloss_unit(a) : 1.f;
   OA oa;
   OB ob;
   // part q of `of` of k-tile kt's DMA instructions.  A (hc in the logits, P) has zeros up to whole k-tiles; B has not.
   auto issue = [&](int kt, int slot, int q, int of) {
     const uint32_t l0 = lds_addr(smem) + slot * STAGE;
-    const int left = min(64, K - (kt0 + kt) * 64);
+    const int left = min(BK, K - (kt0 + kt) * BK);
 #pragma unroll
     for (int i = LPT * q / of; i < LPT * (q + 1) / of; ++i) {
-      if (i < OA::L) oa.dma(i, kt0 + kt, 64, l0, wave, wave_u, lane);
-      else ob.dma(i - OA::L, kt0 + kt, left, l0 + BM * 128, wave, wave_u, lane);
+      if (i < OA::L) oa.dma(i, kt0 + kt, BK, l0, wave, wave_u, lane);
+      else ob.dma(i - OA::L, kt0 + kt, left, l0 + BM * BK * 2, wave, wave_u, lane);
     }
   };
   auto begin = [&] {
@@ -192,14 +215,14 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
     for (int t = 0; t < NS; ++t)
       if (t < nk) issue(t, t, 0, 1);
   };
-  Frags<BM, FM, KA> ra;
-  Frags<BN, FN, KB> rb;
+  Frags<BM, BK, FM, KA> ra;
+  Frags<BN, BK, FN, KB> rb;
   ra.init(wm * TM, lane);
   rb.init(wn * TN, lane);
   bf16x8 fa[2][FM], fb[2][FN];
   auto read_frags = [&](int slot, int ks, int buf) {
     ra.read(smem + slot * STAGE, ks, lane, fa[buf]);
-    rb.read(smem + slot * STAGE + BM * 128, ks, lane, fb[buf]);
+    rb.read(smem + slot * STAGE + BM * BK * 2, ks, lane, fb[buf]);
   };
   auto wait_tiles = [&](int n) {  // at most n k-tiles still in flight
     if constexpr (NS >= 4) { if (n >= 2) { wait_dma<2 * LPT>(); return; } }
@@ -346,26 +369,12 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
               *reinterpret_cast<float4*>(v) = ld(row, 2 * c);
               *reinterpret_cast<float4*>(v + 4) = ld(row, 2 * c + 1);
               if (m >= M || n >= N) continue;
-              if constexpr (E == Prod::Dh) {
-                if (splits > 1) {
-                  float* o = a.dh_part + ((long)esplit * tiles + etile) * (BM * BN) + (wm * TM + i * 32 + row) * BN + wn * TN + j * 32 + 8 * c;
-                  *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
-                  *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
-                } else {
-                  *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dh) + (long)a.idx[a.row0 + m] * a.lddh + n) = pack_frag(v);
-                }
+              if (splits > 1) {
+                float* o = a.shares + ((long)esplit * tiles + etile) * (BM * BN) + (wm * TM + i * 32 + row) * BN + wn * TN + j * 32 + 8 * c;
+                *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
+                *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
               } else {
-                float* o = a.dw_acc + (long)m * a.ld_acc + n;
-                if (!a.first) {
-#pragma unroll
-                  for (int e = 0; e < 8; ++e) v[e] += o[e];
-                }
-                if (a.last) {
-                  *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dw) + (long)m * a.lddw + n) = pack_frag(v);
-                } else {
-                  *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
-                  *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
-                }
+                store_gradient<E>(a, m, n, unit, v);
               }
             }
           }
@@ -376,13 +385,15 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
   }
 }
 
-// dh of a piece from its splits' sums, in their order; tiles are bt x bt
-__global__ __launch_bounds__(256) void vocab_dh_sum_k(VocabArgs a, VocabProduct p, int bt) {
-  const int cnt = piece_rows(a), cols = p.N / 8, i = blockIdx.x * 256 + threadIdx.x, m = i / cols, n = i % cols * 8;
-  if (m >= cnt) return;
-  const int ntn = (p.N + bt - 1) / bt, tiles = (cnt + bt - 1) / bt * ntn, splits = dh_splits(p.slots, tiles, p.K);
+// dh or dw of a piece from its shares, in their order; tiles are bt x bt
+template <Prod E>
+__global__ __launch_bounds__(256) void vocab_shares_k(VocabArgs a, VocabProduct p, int bt) {
+  const int cnt = piece_rows(a), M = E == Prod::Dw ? p.M : cnt, K = E == Prod::Dw ? cnt : p.K;
+  const int cols = p.N / 8, i = blockIdx.x * 256 + threadIdx.x, m = i / cols, n = i % cols * 8;
+  if (m >= M) return;
+  const int ntn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * ntn, splits = k_shares(p.slots, tiles, K, MM_LEAST);
   if (splits == 1) return;
-  const float* q = a.dh_part + (long)(m / bt * ntn + n / bt) * bt * bt + (m % bt) * bt + n % bt;
+  const float* q = a.shares + (long)(m / bt * ntn + n / bt) * bt * bt + (m % bt) * bt + n % bt;
   float v[8] = {};
 #pragma unroll 4
   for (int s = 0; s < splits; ++s) {
@@ -392,7 +403,7 @@ __global__ __launch_bounds__(256) void vocab_dh_sum_k(VocabArgs a, VocabProduct 
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += x[e];
   }
-  *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dh) + (long)a.idx[a.row0 + m] * a.lddh + n) = pack_frag(v);
+  store_gradient<E>(a, m, n, dloss_unit(a), v);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -583,27 +594,38 @@ void launch_vocab_few_bf16(const VocabArgs& a, hipStream_t s) {
 }
 
 static int tiles_of(int x, int t) { return (x + t - 1) / t; }
+constexpr int mm_slots(int tile) { return tile == 256 ? 256 : 512; }  // one or two workgroups per CU
 
-template <int BM, int BN, int WM, int WN, int NS, bool KA, bool KB, Prod E>
+template <int BT, int WM, int WN, bool KA, bool KB, Prod E>
 static void go(const VocabArgs& a, VocabProduct p, hipStream_t s) {
-  // workgroups of one round
-  constexpr int round = BM == 256 ? 256 : 512;
-  const int tiles = tiles_of(E == Prod::Dw ? p.M : a.rows, BM) * tiles_of(p.N, BN);
-  const int wgs = E == Prod::Dh || tiles > round ? round : tiles;
-  RG_LAUNCH((vocab_mm_k<BM, BN, WM, WN, NS, KA, KB, E>), dim3(wgs), dim3(64 * WM * WN), 0, s, a, p);
+  constexpr bool shared = E == Prod::Dh || E == Prod::Dw;
+  const int M = E == Prod::Dw ? p.M : a.rows, K = E == Prod::Dw ? a.rows : p.K;
+  const int tiles = tiles_of(M, BT) * tiles_of(p.N, BT);
+  p.slots = mm_slots(BT);
+  const int most = k_shares(p.slots, 1, K, MM_LEAST);  // of a tile, however few the rows that count are
+  int wgs = shared && tiles < p.slots ? tiles * (E == Prod::Dw ? k_shares(p.slots, tiles, K, MM_LEAST) : most) : tiles;
+  if (wgs > p.slots) wgs = p.slots;
+  RG_LAUNCH((vocab_mm_k<BT, BT, WM, WN, 64, 2, KA, KB, E>), dim3(wgs), dim3(64 * WM * WN), 0, s, a, p);
+  // dw's tiles are known here, dh's are not
+  if (shared && (E == Prod::Dw ? k_shares(p.slots, tiles, K, MM_LEAST) : most) > 1)
+    RG_LAUNCH((vocab_shares_k<shared ? E : Prod::Dh>), dim3((unsigned)(((long)M * (p.N / 8) + 255) / 256)), dim3(256), 0, s, a, p, BT);
 }
 
+// a wave's columns: 256-wide tiles from K 2048 on, where their epilogue weighs little; two smaller ones per CU hide it
 static bool wide_logits(int rows, int d, int V) { return rows > 128 && V > 128 && d >= 2048; }
-int vocab_mm_bn(int rows, int d, int V) { return wide_logits(rows, d, V) ? 128 : 64; }  // a wave's columns
-static int dh_tile(int rows) { return rows > 128 ? 256 : 128; }
-static int dh_slots(int rows) { return rows > 128 ? 256 : 512; }
+int vocab_mm_bn(int rows, int d, int V) { return wide_logits(rows, d, V) ? 128 : 64; }
+static bool wide_dh(int rows, int d) { return rows > 128 && tiles_of(rows, 256) * tiles_of(d, 256) >= 128; }
+static bool wide_dw(int rows, int d, int V) { return rows > 128 && tiles_of(V, 256) * tiles_of(d, 256) >= 128; }
 
-size_t vocab_dh_part_bytes(int rows, int d, int V) {
-  const int t = dh_tile(rows), slots = dh_slots(rows);
-  const long tiles = (long)tiles_of(rows, t) * tiles_of(d, t);
-  // one tile to all of them: whichever rows count, splits times tiles are at most slots
-  const long most = tiles * dh_splits(slots, 1, V);
-  return (size_t)(most < slots ? most : slots) * t * t * 4;
+size_t vocab_share_bytes(int rows, int d, int V) {
+  auto bytes = [](int t, long tiles, int K) {
+    const long most = tiles * k_shares(mm_slots(t), 1, K, MM_LEAST);
+    return (size_t)(most < mm_slots(t) ? most : mm_slots(t)) * t * t * 4;
+  };
+  const int th = wide_dh(rows, d) ? 256 : 128, tw = wide_dw(rows, d, V) ? 256 : 128;
+  const size_t h = bytes(th, (long)tiles_of(rows, th) * tiles_of(d, th), V);
+  const size_t w = bytes(tw, (long)tiles_of(V, tw) * tiles_of(d, tw), rows);
+  return h > w ? h : w;
 }
 
 void launch_vocab_logits_bf16(const VocabArgs& a, bool keep, hipStream_t s) {
@@ -615,11 +637,11 @@ void launch_vocab_logits_bf16(const VocabArgs& a, bool keep, hipStream_t s) {
   p.N = a.V;
   p.K = a.d;
   if (a.bn == 128) {
-    if (keep) go<256, 256, 4, 2, 2, true, true, Prod::Logits>(a, p, s);
-    else go<256, 256, 4, 2, 2, true, true, Prod::Stats>(a, p, s);
+    if (keep) go<256, 4, 2, true, true, Prod::Logits>(a, p, s);
+    else go<256, 4, 2, true, true, Prod::Stats>(a, p, s);
   } else {
-    if (keep) go<128, 128, 2, 2, 2, true, true, Prod::Logits>(a, p, s);
-    else go<128, 128, 2, 2, 2, true, true, Prod::Stats>(a, p, s);
+    if (keep) go<128, 2, 2, true, true, Prod::Logits>(a, p, s);
+    else go<128, 2, 2, true, true, Prod::Stats>(a, p, s);
   }
 }
 void launch_vocab_dh_bf16(const VocabArgs& a, hipStream_t s) {
@@ -630,12 +652,8 @@ void launch_vocab_dh_bf16(const VocabArgs& a, hipStream_t s) {
   p.ldb = a.ldw;
   p.N = a.d;
   p.K = a.V;
-  p.slots = dh_slots(a.n);
-  const int t = dh_tile(a.n);
-  if (t == 256) go<256, 256, 4, 2, 2, true, false, Prod::Dh>(a, p, s);
-  else go<128, 128, 2, 2, 2, true, false, Prod::Dh>(a, p, s);
-  if (dh_splits(p.slots, 1, a.V) > 1)
-    RG_LAUNCH(vocab_dh_sum_k, dim3((unsigned)(((long)a.rows * (a.d / 8) + 255) / 256)), dim3(256), 0, s, a, p, t);
+  if (wide_dh(a.n, a.d)) go<256, 4, 2, true, false, Prod::Dh>(a, p, s);
+  else go<128, 2, 2, true, false, Prod::Dh>(a, p, s);
 }
 void launch_vocab_dw_bf16(const VocabArgs& a, hipStream_t s) {
   VocabProduct p{};
@@ -645,8 +663,8 @@ void launch_vocab_dw_bf16(const VocabArgs& a, hipStream_t s) {
   p.ldb = a.dp;
   p.M = a.V;
   p.N = a.d;
-  if (a.n > 128) go<256, 256, 4, 2, 2, false, false, Prod::Dw>(a, p, s);
-  else go<128, 128, 2, 2, 2, false, false, Prod::Dw>(a, p, s);
+  if (wide_dw(a.n, a.d, a.V)) go<256, 4, 2, false, false, Prod::Dw>(a, p, s);
+  else go<128, 2, 2, false, false, Prod::Dw>(a, p, s);
 }
 
 }  // namespace rg

@@ -265,7 +265,7 @@ struct VocabArgs {
   int* idx; int* lab_c; float* g_c; float* target;  // [n], by counted row: its place, label, gradient, label's logit
   float* logits;                // [R][Vp]
   void* P;                      // [R][Vp] in the storage type (fp32: the logits' place)
-  float* dh_part;               // tiles of dh over shares of the columns
+  float* shares;                // tiles of dh and of dw over shares of their k
   float* dw_acc; long ld_acc;   // bf16: dw between the pieces, [V][d]
   // a piece
   const int* count;             // n_counted, or null: all rows
@@ -273,9 +273,9 @@ struct VocabArgs {
 };
 // bytes of the workspace, and with ws the pointers into it
 size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws);
-// the bf16 products (k_vocab_mm.hip): columns of a tile of logits, bytes of dh_part, the launches of one piece
+// the bf16 products (k_vocab_mm.hip): columns of a tile of logits, bytes of shares, the launches of one piece
 int vocab_mm_bn(int rows, int d, int V);
-size_t vocab_dh_part_bytes(int rows, int d, int V);
+size_t vocab_share_bytes(int rows, int d, int V);
 bool vocab_few(int rows, int d);         // whether rows are few enough to read w straight into registers
 int vocab_few_wgs(int rows, int d);
 void launch_vocab_few_bf16(const VocabArgs& a, hipStream_t s);

@@ -29,6 +29,22 @@ __device__ __forceinline__ int piece_rows(const VocabArgs& a) {
   return a.count ? max(0, min(*a.count - a.row0, a.R)) : a.rows;
 }
 
+// The unit of dloss: with bf16 tensors P holds dloss / unit, and dh and dw are multiplied by the unit in fp32.  Most
+// often dloss is one number for all rows, so P's largest entries, -1 + p at the labels of unsure rows, are
+// rounded as such: with the number in them they are all off by its rounding, up to 2^-9 of dh to the same side (dh of 7373 rows of
+// which few are sure: 0.0026 off float64, now 0.0017, the rounding of dh itself).  A unit out of range is left out.
+__device__ __forceinline__ float dloss_unit(const VocabArgs& a) {
+  if (*a.n_counted == 0) return 1.f;
+  const float g = fabsf(a.g_c[0]);
+  return g >= 0x1p-40f && g <= 0x1p40f ? g : 1.f;
+}
+
+// Workgroups that share the k of a tile, where the tiles of the rows that count leave CUs idle: at least `least` of k to each
+__host__ __device__ inline int k_shares(int slots, int tiles, int K, int least) {
+  const int by_slots = slots / tiles, by_k = K / least, s = by_slots < by_k ? by_slots : by_k;
+  return s < 1 ? 1 : s;
+}
+
 // the logits' statistics alone, with the logits, dh = P w, dw = P^T h
 enum class Prod { Stats, Logits, Dh, Dw };
 
