@@ -22,7 +22,7 @@
 namespace rg {
 
 // ---------------------------------------------------------------- rows that count
-constexpr int PICK_ROWS = 8;       // of h per workgroup
+constexpr int PICK_ROWS = 4;       // of h per workgroup, one per wave
 constexpr int PICK_DIRECT = 16384; // labels that a workgroup counts by itself; beyond, blocks of 1024 are counted first
 
 __device__ __forceinline__ bool counts(const VocabArgs& a, int lab) { return lab >= 0 && lab < a.V; }
@@ -97,8 +97,19 @@ __global__ __launch_bounds__(256) void vocab_pick_k(VocabArgs a, bool wide) {
     T* dst = static_cast<T*>(a.hc) + (long)at * a.dp;
     constexpr int E = 16 / sizeof(T);
     if (wide) {
-      for (int k = lane * E; k < a.dp; k += 64 * E)
-        *reinterpret_cast<uint4*>(dst + k) = k < a.d ? *reinterpret_cast<const uint4*>(src + k) : make_uint4(0, 0, 0, 0);
+      for (int k0 = lane * E; k0 < a.dp; k0 += 512 * E) {  // eight pieces in flight
+        uint4 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int k = k0 + j * 64 * E;
+          x[j] = k < a.d ? *reinterpret_cast<const uint4*>(src + k) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int k = k0 + j * 64 * E;
+          if (k < a.dp) *reinterpret_cast<uint4*>(dst + k) = x[j];
+        }
+      }
     } else {
       for (int k = lane; k < a.dp; k += 64) dst[k] = k < a.d ? src[k] : T(0);
     }
@@ -119,16 +130,6 @@ struct F32Product {
   int slots;       // dh, dw: workgroups of one round
 };
 constexpr int F32_LEAST = 256;  // of k to a share
-
-__device__ __forceinline__ void ld8_f32(const float* p, int valid, bool wide, float v[8]) {
-  if (wide && valid >= 8) {
-    *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
-    *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(p + 4);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.f;
-  }
-}
 
 template <Prod E>
 __device__ __forceinline__ void f32_gradient(const VocabArgs& a, int m, int n, float v) {
@@ -189,24 +190,104 @@ __device__ __forceinline__ void f32_epilogue(const VocabArgs& a, const F32Produc
   }
 }
 
-// 128 x 128 tiles: registers -> LDS, four waves of 64 x 64.  LDS keeps [k][row] with a pitch that puts the two k of an MFMA in
-// different banks.
-template <bool KA, bool KB, Prod E>
-__global__ __launch_bounds__(256) void vocab_f32_k(VocabArgs a, F32Product p) {
-  constexpr int BT = 128, BK = 16, PITCH = 160, CP = BT + 4, LONG = 1024;
+// 128 x 128 tiles, 32 k at a time: registers -> LDS, four waves of 64 x 64, two workgroups per CU.  LDS keeps [k][row], rows of odd k
+// turned by 32 columns, so that the two k of an MFMA lie in different banks.  The loop has no branch: rows and k past the ends read
+// the last ones again.  Such rows are not stored, and such k meet zeros of A: hc and P are padded with them to whole tiles of
+// 64.  VB: B's rows are 16-byte aligned and a multiple of four long.
+// 4096 x 16000, d 2048: 132 TF (a tile of 16 k with guarded loads: 115; torch.mm 154).
+template <bool KM, bool V4>
+struct F32Operand {
+  const char* base;  // uniform: the tile's first element
+  long step;         // bytes per 32 k
+  uint32_t off[4];   // of this thread's four pieces of four
+  int more[4];       // elements behind each piece's first that are its own (not V4)
+  uint32_t ld4;
+  __device__ __forceinline__ void init(const float* X, long ld, int r0, int rows, int k0) {
+    const int tid = threadIdx.x;
+    ld4 = (uint32_t)ld * 4;
+    base = reinterpret_cast<const char*>(KM ? X + (long)r0 * ld + k0 : X + (long)k0 * ld + r0);
+    step = KM ? 128 : ld * 128;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (KM) {
+        off[i] = (uint32_t)min(tid & 127, rows - 1 - r0) * ld4 + ((tid >> 7) * 16 + 4 * i) * 4;
+        more[i] = 3;
+      } else {
+        const int c = min((tid & 31) * 4, rows - (V4 ? 4 : 1) - r0);
+        off[i] = (uint32_t)((tid >> 5) + 8 * i) * ld4 + c * 4;
+        more[i] = min(3, rows - 1 - r0 - c);
+      }
+    }
+  }
+  // tile t from k0 on; left: k of it that there are
+  __device__ __forceinline__ void fetch(int t, int left, f32x4 (&v)[4]) const {
+    const char* b = base + t * step;
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t o = off[i];
+      int m = more[i];
+      if (left < 32) {
+        if constexpr (KM) {
+          const int k = (tid >> 7) * 16 + 4 * i;
+          o -= max(0, k - (V4 ? left - 4 : left - 1)) * 4;
+          m = max(0, min(3, left - 1 - k));
+        } else {
+          o -= max(0, (tid >> 5) + 8 * i - (left - 1)) * ld4;
+        }
+      }
+      if constexpr (V4) {
+        v[i] = *reinterpret_cast<const f32x4*>(b + o);
+      } else {
+        v[i].x = *reinterpret_cast<const float*>(b + o);
+        v[i].y = *reinterpret_cast<const float*>(b + o + min(1, m) * 4);
+        v[i].z = *reinterpret_cast<const float*>(b + o + min(2, m) * 4);
+        v[i].w = *reinterpret_cast<const float*>(b + o + m * 4);
+      }
+    }
+  }
+};
+template <bool KM>
+__device__ __forceinline__ void f32_put(float* s, const f32x4 (&v)[4]) {
+  const int tid = threadIdx.x;
+  if constexpr (KM) {
+    float* even = s + (tid >> 7) * 16 * 128 + (tid & 127);
+    float* odd = s + (tid >> 7) * 16 * 128 + ((tid & 127) ^ 32);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      even[(4 * i) * 128] = v[i].x;
+      odd[(4 * i + 1) * 128] = v[i].y;
+      even[(4 * i + 2) * 128] = v[i].z;
+      odd[(4 * i + 3) * 128] = v[i].w;
+    }
+  } else {
+    // rows 8 i + tid / 32, of the parity of tid / 32
+    float* d = s + (tid >> 5) * 128 + (((tid & 31) * 4) ^ (32 * ((tid >> 5) & 1)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(d + i * 8 * 128) = v[i];
+  }
+}
+
+template <bool KA, bool KB, Prod E, bool VB>
+__global__ __launch_bounds__(256, 2) void vocab_f32_k(VocabArgs a, F32Product p) {
+  constexpr int BT = 128, BK = 32, CP = BT + 4, LONG = 1024, TILE = BK * BT;
   __shared__ __attribute__((aligned(16))) float smem[BT * CP];
-  static_assert(4 * BK * PITCH <= BT * CP, "two buffers");
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+  static_assert(4 * TILE <= BT * CP, "two buffers");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
   const int cnt = piece_rows(a);
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
   const int tn = (N + BT - 1) / BT, tiles = (M + BT - 1) / BT * tn;
   const int Kall = E == Prod::Dw ? cnt : p.K;
   const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? k_shares(p.slots, tiles, Kall, F32_LEAST) : 1;
   if ((int)blockIdx.x >= tiles * splits) return;
-  const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
-  const int m0 = tile / tn * BT, n0 = tile % tn * BT;
-  const int nkt = (Kall + BK - 1) / BK;
-  const int kb = (int)((long)nkt * split / splits) * BK, K = min(Kall, (int)((long)nkt * (split + 1) / splits) * BK);
+  const int split = blockIdx.x / tiles;
+  int tm, tc;
+  vocab_tile<4>(blockIdx.x - split * tiles, (M + BT - 1) / BT, tn, tm, tc);
+  const int tile = tm * tn + tc, m0 = tm * BT, n0 = tc * BT;
+  const int nkt = (Kall + BK - 1) / BK, t0 = (int)((long)nkt * split / splits), t1 = (int)((long)nkt * (split + 1) / splits);
+  // A is padded; what B has
+  const int Mp = KA ? M : a.Vp;
+  const int Nb = E == Prod::Dw ? a.dp : N;
   f32x16 acc[2][2], sum[2][2];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -225,60 +306,50 @@ __global__ __launch_bounds__(256) void vocab_f32_k(VocabArgs a, F32Product p) {
           acc[i][j][r] = 0.f;
         }
   };
-  float ra[8], rb[8];
-  // one operand's 8 elements of this thread: along k for [rows][k], along the rows else
-  auto fetch1 = [&](auto KM, const float* X, long ld, int r0, int rows, bool wide, int k0, float (&v)[8]) {
-    if constexpr (decltype(KM)::value) {
-      const int r = r0 + (tid >> 1), k = k0 + (tid & 1) * 8;
-      ld8_f32(X + (long)min(r, rows - 1) * ld + k, r < rows ? K - k : 0, wide, v);
-    } else {
-      const int k = k0 + (tid >> 4), r = r0 + (tid & 15) * 8;
-      ld8_f32(X + (long)min(k, K - 1) * ld + r, k < K ? rows - r : 0, wide, v);
-    }
-  };
-  auto fetch = [&](int k0) {
-    fetch1(std::integral_constant<bool, KA>{}, p.A, p.lda, m0, M, true, k0, ra);
-    fetch1(std::integral_constant<bool, KB>{}, p.B, p.ldb, n0, N, p.vb, k0, rb);
-  };
-  auto put1 = [&](auto KM, float* s, const float (&v)[8]) {
-    if constexpr (decltype(KM)::value) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s[((tid & 1) * 8 + i) * PITCH + (tid >> 1)] = v[i];
-    } else {
-      float* d = s + (tid >> 4) * PITCH + (tid & 15) * 8;
-      *reinterpret_cast<float4*>(d) = *reinterpret_cast<const float4*>(v);
-      *reinterpret_cast<float4*>(d + 4) = *reinterpret_cast<const float4*>(v + 4);
-    }
+  f32x4 ra[4], rb[4];
+  F32Operand<KA, true> oa;
+  F32Operand<KB, VB> ob;
+  auto fetch = [&](int t) {
+    t = min(t, t1 - 1);
+    oa.fetch(t - t0, 32, ra);
+    ob.fetch(t - t0, Kall - t * BK, rb);
   };
   auto put = [&](int buf) {
-    put1(std::integral_constant<bool, KA>{}, smem + buf * 2 * BK * PITCH, ra);
-    put1(std::integral_constant<bool, KB>{}, smem + (buf * 2 + 1) * BK * PITCH, rb);
+    f32_put<KA>(smem + buf * 2 * TILE, ra);
+    f32_put<KB>(smem + (buf * 2 + 1) * TILE, rb);
   };
-  if (kb < K) {
-    fetch(kb);
+  if (t0 < t1) {
+    oa.init(p.A, p.lda, m0, Mp, t0 * BK);
+    ob.init(p.B, p.ldb, n0, Nb, t0 * BK);
+    fetch(t0);
     put(0);
-    if (kb + BK < K) fetch(kb + BK);
+    fetch(t0 + 1);
     __syncthreads();
     int buf = 0;
-    for (int k0 = kb; k0 < K; k0 += BK, buf ^= 1) {
-      const float* sa = smem + buf * 2 * BK * PITCH + (lane >> 5) * PITCH + wm * 64 + (lane & 31);
-      const float* sb = smem + (buf * 2 + 1) * BK * PITCH + (lane >> 5) * PITCH + wn * 64 + (lane & 31);
-#pragma unroll
-      for (int k = 0; k < BK; k += 2) {
-        float fa[2], fb[2];
+    const int half = lane >> 5, ca = (wm * 64 + (lane & 31)) ^ (32 * half), cb = (wn * 64 + (lane & 31)) ^ (32 * half);
+    for (int t = t0; t < t1; ++t, buf ^= 1) {
+      const float* sa = smem + buf * 2 * TILE + half * BT;
+      const float* sb = sa + TILE;
+      float fa[2][2], fb[2][2];
+      auto read = [&](int kk, int at) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          fa[i] = sa[k * PITCH + i * 32];
-          fb[i] = sb[k * PITCH + i * 32];
+          fa[at][i] = sa[kk * 2 * BT + (ca ^ (32 * i))];
+          fb[at][i] = sb[kk * 2 * BT + (cb ^ (32 * i))];
         }
+      };
+      read(0, 0);
+#pragma unroll
+      for (int kk = 0; kk < BK / 2; ++kk) {
+        if (kk + 1 < BK / 2) read(kk + 1, (kk + 1) & 1);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = mfma32_f32(fb[j], fa[i], acc[i][j]);
+          for (int j = 0; j < 2; ++j) acc[i][j] = mfma32_f32(fb[kk & 1][j], fa[kk & 1][i], acc[i][j]);
+        if (kk == 7) put(buf ^ 1);
+        if (kk == 8) fetch(t + 2);
       }
-      if (k0 + BK < K) put(buf ^ 1);
-      if (k0 + 2 * BK < K) fetch(k0 + 2 * BK);
-      if ((k0 - kb + BK) % LONG == 0) settle();
+      if ((t - t0) % (LONG / BK) == LONG / BK - 1) settle();
       __syncthreads();
     }
     settle();
@@ -366,19 +437,29 @@ __global__ __launch_bounds__(256) void vocab_f32_small_k(VocabArgs a, F32Product
   f32_epilogue<BT, CP, E>(a, p, red[0], M, N, m0, n0, tile, split, splits, tiles);
 }
 
-// dh or dw of a piece from its shares, in their order
-template <Prod E>
+// dh or dw of a piece from its shares.  G threads take every G-th share of a column each, and are added up in their order.
+template <Prod E, int G>
 __global__ __launch_bounds__(256) void vocab_f32_shares_k(VocabArgs a, F32Product p, int bt) {
+  __shared__ float red[256];
   const int cnt = piece_rows(a), M = E == Prod::Dw ? p.M : cnt, K = E == Prod::Dw ? cnt : p.K;
-  const int m = blockIdx.x, n = blockIdx.y * 256 + threadIdx.x;
-  if (m >= M || n >= p.N) return;
+  const int m = blockIdx.x, lane = threadIdx.x % (256 / G), g = threadIdx.x / (256 / G), n = blockIdx.y * (256 / G) + lane;
+  if (m >= M) return;
   const int tn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * tn, splits = k_shares(p.slots, tiles, K, F32_LEAST);
   if (splits == 1) return;
-  const float* q = a.shares + (long)(m / bt * tn + n / bt) * bt * bt + (m % bt) * bt + n % bt;
   float v = 0.f;
+  if (n < p.N) {
+    const float* q = a.shares + (long)(m / bt * tn + n / bt) * bt * bt + (m % bt) * bt + n % bt;
 #pragma unroll 8
-  for (int s = 0; s < splits; ++s) v += q[(long)s * tiles * bt * bt];
-  f32_gradient<E>(a, m, n, v);
+    for (int s = g; s < splits; s += G) v += q[(long)s * tiles * bt * bt];
+  }
+  if constexpr (G > 1) {
+    red[threadIdx.x] = v;
+    __syncthreads();
+    if (g) return;
+#pragma unroll
+    for (int o = 1; o < G; ++o) v += red[o * (256 / G) + lane];
+  }
+  if (n < p.N) f32_gradient<E>(a, m, n, v);
 }
 
 // ---------------------------------------------------------------- rows
@@ -531,10 +612,15 @@ static void go_f32(const VocabArgs& a, F32Product p, bool small, hipStream_t s) 
   p.slots = F32_SLOTS;
   const unsigned wgs = (unsigned)(shared && tiles < F32_SLOTS ? F32_SLOTS : tiles);
   if (small) RG_LAUNCH((vocab_f32_small_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, p);
-  else RG_LAUNCH((vocab_f32_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, p);
+  else if (E == Prod::Dw || (p.vb && a.d % 4 == 0)) RG_LAUNCH((vocab_f32_k<KA, KB, E, true>), dim3(wgs), dim3(256), 0, s, a, p);
+  else RG_LAUNCH((vocab_f32_k<KA, KB, E, false>), dim3(wgs), dim3(256), 0, s, a, p);
   // dw's tiles are known here, dh's may be fewer
   if (shared && k_shares(F32_SLOTS, E == Prod::Dw ? (int)tiles : 1, K, F32_LEAST) > 1)
-    RG_LAUNCH((vocab_f32_shares_k<shared ? E : Prod::Dh>), dim3((unsigned)rows, (p.N + 255) / 256), dim3(256), 0, s, a, p, bt);
+  {
+    constexpr Prod S = shared ? E : Prod::Dh;
+    if (rows * p.N >= 262144) RG_LAUNCH((vocab_f32_shares_k<S, 1>), dim3((unsigned)rows, (p.N + 255) / 256), dim3(256), 0, s, a, p, bt);
+    else RG_LAUNCH((vocab_f32_shares_k<S, 8>), dim3((unsigned)rows, (p.N + 31) / 32), dim3(256), 0, s, a, p, bt);
+  }
 }
 
 static void vocab_products_f32(const VocabArgs& a, int which, hipStream_t s) {

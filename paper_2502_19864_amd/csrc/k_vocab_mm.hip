@@ -118,20 +118,6 @@ struct VocabProduct {
 };
 constexpr int MM_LEAST = 512;  // of k to a share
 
-// The tile of C[m][n] = sum_k A(m, k) B(n, k) that a workgroup makes, by XCD: workgroups are dealt round-robin to the eight
-// XCDs; each takes a contiguous run of a raster in bands of GROUP tile rows, so what its L2 holds is shared.
-template <int GROUP>
-__device__ __forceinline__ bool vocab_tile(int g, int ntm, int ntn, int& tm, int& tn) {
-  const int n = ntm * ntn;
-  if (g >= n) return false;
-  const int x = g & 7, q = n >> 3, r = n & 7;
-  g = x * q + min(x, r) + (g >> 3);
-  const int band = g / (GROUP * ntn), first = band * GROUP, size = min(ntm - first, GROUP), in = g - band * GROUP * ntn;
-  tm = first + in % size;
-  tn = in / size;
-  return true;
-}
-
 // eight columns of a row of dh or dw
 template <Prod E>
 __device__ __forceinline__ void store_gradient(const VocabArgs& a, int m, int n, float unit, float (&v)[8]) {
@@ -385,25 +371,39 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
   }
 }
 
-// dh or dw of a piece from its shares, in their order; tiles are bt x bt
-template <Prod E>
+// dh or dw of a piece from its shares; tiles are bt x bt.  G threads take every G-th share of eight columns each, and are
+// added up in their order.
+template <Prod E, int G>
 __global__ __launch_bounds__(256) void vocab_shares_k(VocabArgs a, VocabProduct p, int bt) {
+  __shared__ float red[G > 1 ? 256 : 1][9];
   const int cnt = piece_rows(a), M = E == Prod::Dw ? p.M : cnt, K = E == Prod::Dw ? cnt : p.K;
-  const int cols = p.N / 8, i = blockIdx.x * 256 + threadIdx.x, m = i / cols, n = i % cols * 8;
-  if (m >= M) return;
-  const int ntn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * ntn, splits = k_shares(p.slots, tiles, K, MM_LEAST);
+  const int cols = p.N / 8, g = threadIdx.x % G, i = blockIdx.x * (256 / G) + threadIdx.x / G, m = i / cols, n = i % cols * 8;
+  const int ntn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * ntn, splits = tiles ? k_shares(p.slots, tiles, K, MM_LEAST) : 1;
   if (splits == 1) return;
-  const float* q = a.shares + (long)(m / bt * ntn + n / bt) * bt * bt + (m % bt) * bt + n % bt;
+  const bool in = m < M;
   float v[8] = {};
+  if (in) {
+    const float* q = a.shares + (long)(m / bt * ntn + n / bt) * bt * bt + (m % bt) * bt + n % bt;
 #pragma unroll 4
-  for (int s = 0; s < splits; ++s) {
-    float x[8];
-    *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(q + (long)s * tiles * bt * bt);
-    *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(q + (long)s * tiles * bt * bt + 4);
+    for (int s = g; s < splits; s += G) {
+      float x[8];
+      *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(q + (long)s * tiles * bt * bt);
+      *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(q + (long)s * tiles * bt * bt + 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] += x[e];
+      for (int e = 0; e < 8; ++e) v[e] += x[e];
+    }
   }
-  store_gradient<E>(a, m, n, dloss_unit(a), v);
+  if constexpr (G > 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) red[threadIdx.x][e] = v[e];
+    __syncthreads();
+    if (g) return;
+#pragma unroll
+    for (int o = 1; o < G; ++o)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += red[threadIdx.x + o][e];
+  }
+  if (in) store_gradient<E>(a, m, n, dloss_unit(a), v);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -596,24 +596,40 @@ void launch_vocab_few_bf16(const VocabArgs& a, hipStream_t s) {
 static int tiles_of(int x, int t) { return (x + t - 1) / t; }
 constexpr int mm_slots(int tile) { return tile == 256 ? 256 : 512; }  // one or two workgroups per CU
 
-template <int BT, int WM, int WN, bool KA, bool KB, Prod E>
+template <int BT, int WM, int WN, bool KA, bool KB, Prod E, int BM = BT>
 static void go(const VocabArgs& a, VocabProduct p, hipStream_t s) {
   constexpr bool shared = E == Prod::Dh || E == Prod::Dw;
+  static_assert(BM == BT || !shared, "shares are of square tiles");
   const int M = E == Prod::Dw ? p.M : a.rows, K = E == Prod::Dw ? a.rows : p.K;
-  const int tiles = tiles_of(M, BT) * tiles_of(p.N, BT);
+  const int tiles = tiles_of(M, BM) * tiles_of(p.N, BT);
   p.slots = mm_slots(BT);
   const int most = k_shares(p.slots, 1, K, MM_LEAST);  // of a tile, however few the rows that count are
   int wgs = shared && tiles < p.slots ? tiles * (E == Prod::Dw ? k_shares(p.slots, tiles, K, MM_LEAST) : most) : tiles;
   if (wgs > p.slots) wgs = p.slots;
-  RG_LAUNCH((vocab_mm_k<BT, BT, WM, WN, 64, 2, KA, KB, E>), dim3(wgs), dim3(64 * WM * WN), 0, s, a, p);
+  RG_LAUNCH((vocab_mm_k<BM, BT, WM, WN, 64, 2, KA, KB, E>), dim3(wgs), dim3(64 * WM * WN), 0, s, a, p);
   // dw's tiles are known here, dh's are not
-  if (shared && (E == Prod::Dw ? k_shares(p.slots, tiles, K, MM_LEAST) : most) > 1)
-    RG_LAUNCH((vocab_shares_k<shared ? E : Prod::Dh>), dim3((unsigned)(((long)M * (p.N / 8) + 255) / 256)), dim3(256), 0, s, a, p, BT);
+  if (shared && (E == Prod::Dw ? k_shares(p.slots, tiles, K, MM_LEAST) : most) > 1) {
+    // one thread per eight columns where those are many, else eight
+    const long items = (long)M * (p.N / 8);
+    constexpr Prod S = shared ? E : Prod::Dh;
+    if (items >= 65536) RG_LAUNCH((vocab_shares_k<S, 1>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, a, p, BT);
+    else RG_LAUNCH((vocab_shares_k<S, 8>), dim3((unsigned)((items + 31) / 32)), dim3(256), 0, s, a, p, BT);
+  }
 }
 
-// a wave's columns: 256-wide tiles from K 2048 on, where their epilogue weighs little; two smaller ones per CU hide it
-static bool wide_logits(int rows, int d, int V) { return rows > 128 && V > 128 && d >= 2048; }
-int vocab_mm_bn(int rows, int d, int V) { return wide_logits(rows, d, V) ? 128 : 64; }
+// Rows and columns of the logits' tiles, by the rounds of the GPU that they take: f + r K / 64 us each, fitted to 333 to 4096
+// rows, 20000 to 50000 classes, d 768 to 4096.  256 x 256 has the best rate, 192 x 256 the rows that 256 leaves over (333 x 32000, d 4096: 84 us
+// against 109), 128 x 128, two to a CU, the shortest epilogue.
+enum class LogitsTile { T256, T192, T128 };
+static LogitsTile logits_tile(int rows, int d, int V) {
+  const int k = tiles_of(d, 64);
+  auto rounds = [](int tiles, int slots) { return (tiles + slots - 1) / slots; };
+  const float t256 = rounds(tiles_of(rows, 256) * tiles_of(V, 256), 256) * (8.f + 1.7f * k);
+  const float t192 = rounds(tiles_of(rows, 192) * tiles_of(V, 256), 256) * (8.f + 1.32f * k);
+  const float t128 = rounds(tiles_of(rows, 128) * tiles_of(V, 128), 512) * (7.f + 1.05f * k);
+  return t256 <= t192 && t256 <= t128 ? LogitsTile::T256 : t192 <= t128 ? LogitsTile::T192 : LogitsTile::T128;
+}
+int vocab_mm_bn(int rows, int d, int V) { return logits_tile(rows, d, V) == LogitsTile::T256 ? 128 : 64; }  // a wave's columns
 static bool wide_dh(int rows, int d) { return rows > 128 && tiles_of(rows, 256) * tiles_of(d, 256) >= 128; }
 static bool wide_dw(int rows, int d, int V) { return rows > 128 && tiles_of(V, 256) * tiles_of(d, 256) >= 128; }
 
@@ -636,12 +652,19 @@ void launch_vocab_logits_bf16(const VocabArgs& a, bool keep, hipStream_t s) {
   p.ldb = a.ldw;
   p.N = a.V;
   p.K = a.d;
-  if (a.bn == 128) {
-    if (keep) go<256, 4, 2, true, true, Prod::Logits>(a, p, s);
-    else go<256, 4, 2, true, true, Prod::Stats>(a, p, s);
-  } else {
-    if (keep) go<128, 2, 2, true, true, Prod::Logits>(a, p, s);
-    else go<128, 2, 2, true, true, Prod::Stats>(a, p, s);
+  switch (logits_tile(a.n, a.d, a.V)) {
+    case LogitsTile::T256:
+      if (keep) go<256, 4, 2, true, true, Prod::Logits>(a, p, s);
+      else go<256, 4, 2, true, true, Prod::Stats>(a, p, s);
+      break;
+    case LogitsTile::T192:
+      if (keep) go<256, 2, 4, true, true, Prod::Logits, 192>(a, p, s);
+      else go<256, 2, 4, true, true, Prod::Stats, 192>(a, p, s);
+      break;
+    case LogitsTile::T128:
+      if (keep) go<128, 2, 2, true, true, Prod::Logits>(a, p, s);
+      else go<128, 2, 2, true, true, Prod::Stats>(a, p, s);
+      break;
   }
 }
 void launch_vocab_dh_bf16(const VocabArgs& a, hipStream_t s) {

@@ -45,6 +45,20 @@ __host__ __device__ inline int k_shares(int slots, int tiles, int K, int least) 
   return s < 1 ? 1 : s;
 }
 
+// The tile of C[m][n] = sum_k A(m, k) B(n, k) that a workgroup makes, by XCD: workgroups are dealt round-robin to the eight
+// XCDs; each takes a contiguous run of a raster in bands of GROUP tile rows, so what its L2 holds is shared.
+template <int GROUP>
+__device__ __forceinline__ bool vocab_tile(int g, int ntm, int ntn, int& tm, int& tn) {
+  const int n = ntm * ntn;
+  if (g >= n) return false;
+  const int x = g & 7, q = n >> 3, r = n & 7;
+  g = x * q + min(x, r) + (g >> 3);
+  const int band = g / (GROUP * ntn), first = band * GROUP, size = min(ntm - first, GROUP), in = g - band * GROUP * ntn;
+  tm = first + in % size;
+  tn = in / size;
+  return true;
+}
+
 // the logits' statistics alone, with the logits, dh = P w, dw = P^T h
 enum class Prod { Stats, Logits, Dh, Dw };
 

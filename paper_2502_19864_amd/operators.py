@@ -187,6 +187,11 @@ def dropout(x, p, rng, site=0, res=None, out=None):
 
 
 # ---------------------------------------------------------------- rows of d elements: norms and the vocabulary head
+def _fresh(t):
+    """A new contiguous tensor as t (the quickest of torch's ways: a small call is bound by its time on the host)."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _storage(name, t):
     if t.dtype not in _DTYPES or t.device.type != "cuda":
         raise ValueError(f"{name}: {t.dtype} on {t.device}, expected float32 or bfloat16 on a GPU")
@@ -233,9 +238,9 @@ def norm_forward(x, gain, shift=None, *, rms=False, eps=1e-5, res=None, out=None
     s = x
     if res is not None:
         rr = _ROWS.pack(*_rows("res", res, shape, dtype, dev))
-        s = torch.empty(shape, dtype=dtype, device=dev) if out_sum is None else out_sum
+        s = _fresh(x) if out_sum is None else out_sum
         sr = _ROWS.pack(*_rows("out_sum", s, shape, dtype, dev))
-    y = torch.empty(shape, dtype=dtype, device=dev) if out is None else out
+    y = _fresh(x) if out is None else out
     yr = _ROWS.pack(*_rows("out", y, shape, dtype, dev))
     gp, bp = _plain("gain", gain, dtype, (d,), dev), _plain("shift", shift, dtype, (d,), dev)
     stats = torch.empty((x.numel() // d, 2), dtype=torch.float32, device=dev) if with_stats else None
@@ -254,7 +259,7 @@ def norm_backward(dy, s, gain, stats, *, rms=False, dskip=None, dgain=None, dshi
     rows = s.numel() // d
     if stats is None:
         raise ValueError("the backward needs the forward's stats")
-    dx = torch.empty(shape, dtype=dtype, device=dev) if out is None else out
+    dx = _fresh(s) if out is None else out
     dyr, sr = _ROWS.pack(*_rows("dy", dy, shape, dtype, dev)), _ROWS.pack(*_rows("s", s, shape, dtype, dev))
     kr = None if dskip is None else _ROWS.pack(*_rows("dskip", dskip, shape, dtype, dev))
     xr = _ROWS.pack(*_rows("out", dx, shape, dtype, dev))
@@ -298,9 +303,9 @@ def rotary(q, k=None, *, positions, freq, sections=None, inverse=False, out_q=No
         if kv == 0:
             raise ValueError("k: no heads")
         kr = _VIEW.pack(*_view("k", k, kshape, dtype, dev))
-        ok = torch.empty(kshape, dtype=dtype, device=dev) if out_k is None else out_k
+        ok = _fresh(k) if out_k is None else out_k
         okr = _VIEW.pack(*_view("out_k", ok, kshape, dtype, dev))
-    oq = torch.empty(q.shape, dtype=dtype, device=dev) if out_q is None else out_q
+    oq = _fresh(q) if out_q is None else out_q
     desc = _pack(_ROTARY, _DTYPES[dtype], b, rows, h, kv, dh, axes, *sections, *([0] * (4 - axes)), bool(inverse))
     _on(dev, B.ringada_rotary, desc, _VIEW.pack(*_view("q", q, q.shape, dtype, dev)), kr, pp, fp,
         _VIEW.pack(*_view("out_q", oq, q.shape, dtype, dev)), okr)
@@ -353,9 +358,9 @@ def vocab_ce_train(h, w, labels, dloss, *, frozen=False, dh=None, dw=None):
     if frozen and dw is not None:
         raise ValueError("dw of a frozen head")
     if dh is None:
-        dh = torch.empty(h.shape, dtype=h.dtype, device=h.device)
+        dh = _fresh(h)
     if dw is None and not frozen:
-        dw = torch.empty(w.shape, dtype=w.dtype, device=w.device)
+        dw = _fresh(w)
     loss, lse = _vocab_ce(h, w, labels, dloss, dh, dw)
     return loss, lse, dh, dw
 
