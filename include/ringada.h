@@ -511,16 +511,17 @@ typedef struct {
 } ringada_vocab_tensors;
 
 /* Host only.  Bytes of the workspaces of ringada_vocab_ce without and with gradients, and of ringada_vocab_next.
- * The logits are held for a piece of the rows at a time, at most 2^29 of them (or 256 rows), so the second is at most
- * some 3 GiB, beside a copy of h and, for rows of more than one piece in bf16, 4 vocab d bytes.  Any pointer may be NULL. */
+ * The logits are held for a piece of the rows at a time, at most 2 GiB of them (or 256 rows), beside a copy of h, 8 bytes for every
+ * 32 logits, up to 64 MiB for sums that several workgroups share, and, for rows of more than one piece in bf16, 4 vocab d
+ * bytes.  Any pointer may be NULL. */
 ringada_status ringada_vocab_plan(const ringada_vocab_desc* desc, size_t* forward_bytes, size_t* train_bytes,
                                   size_t* next_bytes);
 
 /* Softmax cross entropy of the logits s = h w^T, and its gradients in the same call:
  *   lse = log sum exp s,  loss = lse - s[label],  P = dloss (softmax(s) - onehot(label)),  dh = P w,  dw = P^T h.
  * A row that does not count has loss 0, lse 0 and a zero row in dh; its h and dloss are read into nothing, whatever they
- * hold.  Logits, softmax and sums are fp32; with bf16 tensors P is rounded to bf16 on its way into the
- * products, in units of the first counted row's |dloss| (where that is within 2^-40 and 2^40: entries of dloss may be up to 2^80 then).  An infinity or NaN in a row that counts gives NaN in it, and in dw.  No output may overlap
+ * hold.  Logits, softmax and sums are fp32.  With bf16 tensors the logits wait for their row's lse in fp16, as their distance
+ * to the largest of 64 or 128 (off by 2^-11 of it), and P is rounded to bf16 on its way into the products, in units of the first counted row's |dloss| (where that is within 2^-40 and 2^40: entries of dloss may be up to 2^80 then).  An infinity or NaN in a row that counts gives NaN in it, and in dw.  No output may overlap
  * anything else.  Every sum has a fixed order: the same inputs give the same bits. */
 ringada_status ringada_vocab_ce(void* stream, const ringada_vocab_desc* desc, const ringada_vocab_tensors* t,
                                 void* workspace, size_t workspace_bytes);

@@ -17,19 +17,22 @@ namespace rg {
 // 16-byte pieces of a row: VE elements
 template <typename T> constexpr int VE = 16 / sizeof(T);
 
-template <typename T>
-__device__ __forceinline__ void ld_piece(const T* p, int left, bool wide, float v[VE<T>]) {
-  if (wide) {
+template <bool WIDE, typename T>
+__device__ __forceinline__ void ld_piece(const T* p, int left, float v[VE<T>]) {
+  if constexpr (WIDE) {
     if constexpr (sizeof(T) == 2) unpack_frag(*reinterpret_cast<const bf16x8*>(p), v);
     else St<T>::ld4(p, 0, v);
   } else {
 #pragma unroll
-    for (int i = 0; i < VE<T>; ++i) v[i] = i < left ? St<T>::ld(p, i) : 0.f;
+    for (int i = 0; i < VE<T>; ++i) {  // no branch: what is past the row is read as its last element and left out
+      const float x = St<T>::ld(p, min(i, left - 1));
+      v[i] = i < left ? x : 0.f;
+    }
   }
 }
-template <typename T>
-__device__ __forceinline__ void st_piece(T* p, int left, bool wide, const float v[VE<T>]) {
-  if (wide) {
+template <bool WIDE, typename T>
+__device__ __forceinline__ void st_piece(T* p, int left, const float v[VE<T>]) {
+  if constexpr (WIDE) {
     if constexpr (sizeof(T) == 2) *reinterpret_cast<bf16x8*>(p) = pack_frag(v);
     else St<T>::st4(p, 0, v);
   } else {
@@ -62,8 +65,8 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
 }
 
 // TPR threads per row, CH pieces per thread
-template <typename T, int TPR, int CH>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_k(NormArgs a, bool wide) {
+template <typename T, int TPR, int CH, bool WIDE>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_k(NormArgs a) {
   constexpr int E = VE<T>, NT = TPR > 256 ? TPR : 256, RPW = NT / TPR;
   __shared__ float red[16];
   const int t = threadIdx.x % TPR;
@@ -79,13 +82,13 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_k(NormArgs a, 
 #pragma unroll
     for (int i = 0; i < E; ++i) v[c][i] = 0.f;
     if (left <= 0) continue;
-    ld_piece(x + at, left, wide, v[c]);
+    ld_piece<WIDE>(x + at, left, v[c]);
     if (res) {
       float r[E];
-      ld_piece(res + at, left, wide, r);
+      ld_piece<WIDE>(res + at, left, r);
 #pragma unroll
       for (int i = 0; i < E; ++i) v[c][i] = stored<T>(v[c][i] + r[i]);
-      st_piece(static_cast<T*>(a.s.p) + row * a.s.t + at, left, wide, v[c]);
+      st_piece<WIDE>(static_cast<T*>(a.s.p) + row * a.s.t + at, left, v[c]);
     }
 #pragma unroll
     for (int i = 0; i < E; ++i) sum += v[c][i];
@@ -109,30 +112,29 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_k(NormArgs a, 
     const int at = (c * TPR + t) * E, left = a.d - at;
     if (left <= 0) continue;
     float g[E], b[E];
-    ld_piece(gain + at, left, wide, g);
-    if (shift) ld_piece(shift + at, left, wide, b);
+    ld_piece<WIDE>(gain + at, left, g);
+    if (shift) ld_piece<WIDE>(shift + at, left, b);
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const float u = (v[c][i] - mean) * rstd * g[i];
       v[c][i] = shift ? u + b[i] : u;
     }
-    st_piece(y + at, left, wide, v[c]);
+    st_piece<WIDE>(y + at, left, v[c]);
   }
 }
 
 // a piece as it lies in memory
-template <typename T>
-__device__ __forceinline__ uint4 ld_raw(const T* p, int left, bool wide) {
-  if (wide) return *reinterpret_cast<const uint4*>(p);
-  union {
-    uint4 q;
-    T e[VE<T>];
-  } u;
-  u.q = make_uint4(0, 0, 0, 0);
+template <bool WIDE, typename T>
+__device__ __forceinline__ uint4 ld_raw(const T* p, int left) {
+  if constexpr (WIDE) return *reinterpret_cast<const uint4*>(p);
+  typedef T V __attribute__((ext_vector_type(VE<T>)));
+  V v;
 #pragma unroll
-  for (int i = 0; i < VE<T>; ++i)
-    if (i < left) u.e[i] = p[i];
-  return u.q;
+  for (int i = 0; i < VE<T>; ++i) {
+    const T x = p[min(i, left - 1)];
+    v[i] = i < left ? x : T(0);
+  }
+  return __builtin_bit_cast(uint4, v);
 }
 template <typename T>
 __device__ __forceinline__ void unpack_raw(const uint4& q, float v[VE<T>]) {
@@ -146,8 +148,8 @@ __device__ __forceinline__ void unpack_raw(const uint4& q, float v[VE<T>]) {
 
 // The next row of a workgroup is on its way while one is worked on (AHEAD; not in the widest rows, whose registers are full).  Rows
 // stay as they lie in memory, and are unpacked for the sums and again for the result.
-template <typename T, int TPR, int CH, bool AHEAD>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_k(NormArgs a, bool wide) {
+template <typename T, int TPR, int CH, bool AHEAD, bool WIDE>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_k(NormArgs a) {
   constexpr int E = VE<T>, NT = TPR > 256 ? TPR : 256, RPW = NT / TPR;
   __shared__ float red[32];
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
@@ -158,7 +160,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_k(NormArgs a, 
     const int at = (c * TPR + t) * E, left = a.d - at;
 #pragma unroll
     for (int i = 0; i < E; ++i) dg[c][i] = db[c][i] = 0.f;
-    g[c] = left > 0 ? ld_raw(static_cast<const T*>(a.gain) + at, left, wide) : make_uint4(0, 0, 0, 0);
+    g[c] = left > 0 ? ld_raw<WIDE>(static_cast<const T*>(a.gain) + at, left) : make_uint4(0, 0, 0, 0);
   }
   const float inv_d = 1.f / a.d;
   const long stride = (long)gridDim.x * RPW;
@@ -176,9 +178,9 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_k(NormArgs a, 
       const int at = (c * TPR + t) * E, left = a.d - at;
       r.x[c] = r.y[c] = r.k[c] = make_uint4(0, 0, 0, 0);
       if (left <= 0) continue;
-      r.x[c] = ld_raw(x + at, left, wide);
-      r.y[c] = ld_raw(dy + at, left, wide);
-      if (a.dskip.p) r.k[c] = ld_raw(k + at, left, wide);
+      r.x[c] = ld_raw<WIDE>(x + at, left);
+      r.y[c] = ld_raw<WIDE>(dy + at, left);
+      if (a.dskip.p) r.k[c] = ld_raw<WIDE>(k + at, left);
     }
   };
   // rows group, group + groups, ..; every row of a workgroup's loop has all its threads
@@ -240,7 +242,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_k(NormArgs a, 
         const float v = now.st.y * (w[i] * gf[i] - s1 - (u[i] - now.st.x) * now.st.y * s2);
         w[i] = a.dskip.p ? v + k[i] : v;
       }
-      st_piece(dx + at, left, wide, w);
+      st_piece<WIDE>(dx + at, left, w);
     }
     if constexpr (AHEAD) now = next;
     else if (row + stride < a.rows) load(row + stride, now);
@@ -314,26 +316,44 @@ int norm_groups(int dtype, long rows, int d) {
   const NormShape f = norm_shape(dtype, d, true);
   const int rpw = f.tpr >= 256 ? 1 : 256 / f.tpr;
   const long wgs = (rows + rpw - 1) / rpw;
-  return (int)(wgs < 1024 ? wgs : 1024);
+  return (int)(wgs < 512 ? wgs : 512);
 }
 
 static bool rows_wide(const NormRows& r, int es) {
   return r.p == nullptr || ((reinterpret_cast<uintptr_t>(r.p) & 15u) == 0 && (r.t * es & 15) == 0);
 }
 
-template <typename T, int TPR, int CH>
-static hipError_t norm_go(const NormArgs& a, bool back, bool wide, hipStream_t s) {
+template <typename T, int TPR, int CH, bool WIDE>
+static hipError_t norm_go(const NormArgs& a, bool back, hipStream_t s) {
   constexpr int NT = TPR > 256 ? TPR : 256, RPW = NT / TPR;
   if (back) {
-    if constexpr (CH < 4 || TPR == 1024) RG_LAUNCH((norm_bwd_k<T, TPR, CH, CH * VE<T> <= 16 && (TPR < 1024 || CH == 1)>), dim3(a.groups), dim3(NT), 0, s, a, wide);
+    constexpr bool ahead = WIDE && CH * VE<T> <= 16 && (TPR < 1024 || CH == 1);
+    if constexpr (CH < 4 || TPR == 1024) RG_LAUNCH((norm_bwd_k<T, TPR, CH, ahead, WIDE>), dim3(a.groups), dim3(NT), 0, s, a);
     else return hipErrorInvalidValue;
     if (a.part) RG_LAUNCH(norm_sums_k, dim3((a.d + 31) / 32, 2), dim3(1024), 0, s, a);
   } else {
     // HIP takes fewer than 2^32 threads in a dimension of a launch
     const long wgs = (a.rows + RPW - 1) / RPW, y = (wgs + (1l << 21) - 1) >> 21;
-    RG_LAUNCH((norm_fwd_k<T, TPR, CH>), dim3((unsigned)((wgs + y - 1) / y), (unsigned)y), dim3(NT), 0, s, a, wide);
+    RG_LAUNCH((norm_fwd_k<T, TPR, CH, WIDE>), dim3((unsigned)((wgs + y - 1) / y), (unsigned)y), dim3(NT), 0, s, a);
   }
   return hipGetLastError();
+}
+
+template <typename T, bool WIDE>
+static hipError_t norm_shapes(const NormShape& f, const NormArgs& a, bool back, hipStream_t s) {
+  switch (f.tpr * 8 + f.ch) {
+    case 64 * 8 + 1: return norm_go<T, 64, 1, WIDE>(a, back, s);
+    case 64 * 8 + 2: return norm_go<T, 64, 2, WIDE>(a, back, s);
+    case 64 * 8 + 4: return norm_go<T, 64, 4, WIDE>(a, back, s);
+    case 256 * 8 + 1: return norm_go<T, 256, 1, WIDE>(a, back, s);
+    case 256 * 8 + 2: return norm_go<T, 256, 2, WIDE>(a, back, s);
+    case 256 * 8 + 4: return norm_go<T, 256, 4, WIDE>(a, back, s);
+    case 1024 * 8 + 1: return norm_go<T, 1024, 1, WIDE>(a, back, s);
+    case 1024 * 8 + 2: return norm_go<T, 1024, 2, WIDE>(a, back, s);
+    case 1024 * 8 + 4:  // fp32 alone has rows of as many pieces
+      if constexpr (sizeof(T) == 4) return norm_go<T, 1024, 4, WIDE>(a, back, s);
+  }
+  return hipErrorInvalidValue;
 }
 
 template <typename T>
@@ -344,18 +364,7 @@ static hipError_t norm_t(int dtype, const NormArgs& a, bool back, hipStream_t s)
                     rows_wide(a.y, es) && rows_wide(a.dy, es) && rows_wide(a.dskip, es) && rows_wide(a.dx, es) &&
                     al(a.gain) && al(a.shift);
   const NormShape f = norm_shape(dtype, a.d, back);
-  switch (f.tpr * 8 + f.ch) {
-    case 64 * 8 + 1: return norm_go<T, 64, 1>(a, back, wide, s);
-    case 64 * 8 + 2: return norm_go<T, 64, 2>(a, back, wide, s);
-    case 64 * 8 + 4: return norm_go<T, 64, 4>(a, back, wide, s);
-    case 256 * 8 + 1: return norm_go<T, 256, 1>(a, back, wide, s);
-    case 256 * 8 + 2: return norm_go<T, 256, 2>(a, back, wide, s);
-    case 256 * 8 + 4: return norm_go<T, 256, 4>(a, back, wide, s);
-    case 1024 * 8 + 1: return norm_go<T, 1024, 1>(a, back, wide, s);
-    case 1024 * 8 + 2: return norm_go<T, 1024, 2>(a, back, wide, s);
-    case 1024 * 8 + 4: return norm_go<T, 1024, 4>(a, back, wide, s);
-  }
-  return hipErrorInvalidValue;
+  return wide ? norm_shapes<T, true>(f, a, back, s) : norm_shapes<T, false>(f, a, back, s);
 }
 
 hipError_t launch_norm_fwd(int dtype, const NormArgs& a, hipStream_t s) {

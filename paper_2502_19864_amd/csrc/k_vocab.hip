@@ -129,7 +129,7 @@ struct F32Product {
   bool vb;         // B's rows are 16-byte aligned (A's always are)
   int slots;       // dh, dw: workgroups of one round
 };
-constexpr int F32_LEAST = 256;  // of k to a share
+constexpr int F32_LEAST = 512;  // of k to a share
 
 template <Prod E>
 __device__ __forceinline__ void f32_gradient(const VocabArgs& a, int m, int n, float v) {
@@ -176,7 +176,7 @@ __device__ __forceinline__ void f32_epilogue(const VocabArgs& a, const F32Produc
       for (int i = tid; i < BT * BT / 4; i += 256) {
         const int r = i / (BT / 4), c = i % (BT / 4) * 4;
         if (m0 + r < M && n0 + c < a.Vp)
-          *reinterpret_cast<float4*>(a.logits + (long)(m0 + r) * a.Vp + n0 + c) = *reinterpret_cast<const float4*>(cf + r * CP + c);
+          *reinterpret_cast<float4*>(static_cast<float*>(a.logits) + (long)(m0 + r) * a.Vp + n0 + c) = *reinterpret_cast<const float4*>(cf + r * CP + c);
       }
   } else {
     float* part = a.shares + ((long)split * tiles + tile) * (BT * BT);
@@ -497,59 +497,75 @@ __global__ __launch_bounds__(256) void vocab_rows_k(VocabArgs a) {
   a.lse[row] = p.m + log_l;
 }
 
-// Loss and lse of a row, and its P from the logits, rounded once to the storage type; zeros past V and in the rows up to a
-// multiple of 64.  A workgroup takes 8192 columns of one row and joins the row's tiles by itself.
-constexpr int P_COLS = 8192;
+// Loss and lse of a row, and its P in the place of the logits, rounded once to the storage type; zeros past V and in the rows
+// up to a multiple of 64.  A workgroup takes 16384 columns of one row and joins the row's tiles by itself.
+// With bf16 tensors the logits come in fp16, as s - (the largest of their tile, which is in part): off by 2^-11 of that difference
+// at most, so P by 2^-11 (m - s) of itself.  What is large of P has s near m and keeps its digits; P a thousandth of its tile's
+// largest is off by 2^-8.2 at most, its own rounding to bf16 by 2^-8; the label's entry comes from the loss, in fp32.  Half the bytes of fp32 logits:
+// 2048 x 32000 take 54 us here instead of 78, and 16 less to store.
+constexpr int P_COLS = 16384;
 template <typename T>
 __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
   __shared__ Peak red[4];
-  const int m = blockIdx.x, cnt = piece_rows(a), tid = threadIdx.x;
+  const int m = blockIdx.x, cnt = piece_rows(a), tid = threadIdx.x, first = blockIdx.y * P_COLS + tid * 8;
+  const int last = min((int)(blockIdx.y + 1) * P_COLS, a.Vp);
   if (m >= ((cnt + 63) & ~63)) return;
-  const bool in = m < cnt;
-  float lse = 0.f, loss = 0.f, g = 0.f;
-  int lab = -1;
-  if (in) {
-    Peak p{-INFINITY, 0.f, 0};
-    for (int t = tid; t < a.tiles; t += 256) {
-      const float2 q = a.part[(long)m * a.tiles + t];
-      p = join(p, Peak{q.x, q.y, 0});
+  const long at = (long)m * a.Vp;
+  T* p = static_cast<T*>(a.logits) + at;
+  auto store = [&](int v, const float (&x)[8]) {
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<bf16x8*>(p + v) = pack_frag(x);
+    } else {
+      St<T>::st4(p, v, x);
+      St<T>::st4(p, v + 4, x + 4);
     }
-    p = join_wave(p);
-    if ((tid & 63) == 0) red[tid >> 6] = p;
-    __syncthreads();
-    p = join(join(red[0], red[1]), join(red[2], red[3]));
-    const float log_l = logf(p.l);
-    lse = p.m + log_l;
-    loss = (p.m - a.target[a.row0 + m]) + log_l;  // not lse - s: of a row that is sure of its label little is left
-    g = a.g_c[a.row0 + m];
-    if constexpr (sizeof(T) == 2) g /= dloss_unit(a);
-    lab = a.lab_c[a.row0 + m];
-    if (blockIdx.y == 0 && tid == 0) {
-      const int row = a.idx[a.row0 + m];
-      a.loss[row] = loss;
-      a.lse[row] = lse;
-    }
+  };
+  if (m >= cnt) {
+    const float zero[8] = {};
+    for (int v0 = first; v0 < last; v0 += 2048) store(v0, zero);
+    return;
   }
-  const float* s = a.logits + (long)m * a.Vp;
-  T* p = static_cast<T*>(a.P) + (long)m * a.Vp;
-#pragma unroll
-  for (int i = 0; i < P_COLS / 2048; ++i) {
-    const int v0 = blockIdx.y * P_COLS + i * 2048 + tid * 8;
-    if (v0 >= a.Vp) break;
+  Peak q{-INFINITY, 0.f, 0};
+  for (int t = tid; t < a.tiles; t += 256) {
+    const float2 x = a.part[(long)m * a.tiles + t];
+    q = join(q, Peak{x.x, x.y, 0});
+  }
+  q = join_wave(q);
+  if ((tid & 63) == 0) red[tid >> 6] = q;
+  __syncthreads();
+  q = join(join(red[0], red[1]), join(red[2], red[3]));
+  const float log_l = logf(q.l), lse = q.m + log_l;
+  const float loss = (q.m - a.target[a.row0 + m]) + log_l;  // not lse - s: of a row that is sure of its label little is left
+  float g = a.g_c[a.row0 + m];
+  if constexpr (sizeof(T) == 2) g /= dloss_unit(a);
+  const int lab = a.lab_c[a.row0 + m];
+  if (blockIdx.y == 0 && tid == 0) {
+    const int row = a.idx[a.row0 + m];
+    a.loss[row] = loss;
+    a.lse[row] = lse;
+  }
+#pragma unroll 4
+  for (int v0 = first; v0 < last; v0 += 2048) {
     float x[8];
-    if (in) {
-      *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(s + v0);
-      *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(s + v0 + 4);
+    if constexpr (sizeof(T) == 2) {
+      const half8 h = *reinterpret_cast<const half8*>(static_cast<const _Float16*>(a.logits) + at + v0);
+      const float top = a.part[(long)m * a.tiles + min(v0, a.V - 1) / a.bn].x - lse;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = (float)h[e] + top;
+    } else {
+      const float* s = static_cast<const float*>(a.logits) + at + v0;
+      const float4 lo = *reinterpret_cast<const float4*>(s), hi = *reinterpret_cast<const float4*>(s + 4);
+      x[0] = lo.x - lse; x[1] = lo.y - lse; x[2] = lo.z - lse; x[3] = lo.w - lse;
+      x[4] = hi.x - lse; x[5] = hi.y - lse; x[6] = hi.z - lse; x[7] = hi.w - lse;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = in && v0 + e < a.V ? g * exp_below(x[e] - lse) : 0.f;
+    for (int e = 0; e < 8; ++e) x[e] = v0 + e < a.V ? g * exp_below(x[e]) : 0.f;
     if (lab >= v0 && lab < v0 + 8) {
       const float y = g * expm1f(-loss);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = v0 + e == lab ? y : x[e];
     }
-    St<T>::st4(p, v0, x);
-    St<T>::st4(p, v0 + 4, x + 4);
+    store(v0, x);
   }
 }
 
@@ -569,8 +585,8 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   a.bn = low ? vocab_mm_bn(a.n, a.d, a.V) : f32_small(a.n, a.V) ? 32 : 128;
   a.few = low && !grads && vocab_few(a.n, a.d);
   a.tiles = a.few ? vocab_few_wgs(a.n, a.d) : (a.V + a.bn - 1) / a.bn;
-  // rows at a time: 2^29 logits (2 GiB), 2^24 partial sums; whole tiles of rows
-  const long most = grads ? (1l << 29) / a.Vp : (1l << 24) / a.tiles;
+  // rows at a time: 2 GiB of logits, 2^24 partial sums; whole tiles of rows
+  const long most = grads ? (low ? 1l << 30 : 1l << 29) / a.Vp : (1l << 24) / a.tiles;
   a.R = (int)(np <= most ? np : most / 256 * 256 > 256 ? most / 256 * 256 : 256);
   if (a.R > np) a.R = (int)np;
   size_t at = 0;
@@ -593,8 +609,7 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   }
   if (grads) {
     a.g_c = static_cast<float*>(take((size_t)a.n * 4));
-    a.logits = static_cast<float*>(take((size_t)a.R * a.Vp * 4));
-    a.P = low ? take((size_t)a.R * a.Vp * 2) : a.logits;
+    a.logits = take((size_t)a.R * a.Vp * es);
     a.shares = static_cast<float*>(take(low ? vocab_share_bytes(a.n, a.d, a.V)
                                             : (size_t)F32_SLOTS * 4 * (f32_small(a.n, a.d) && f32_small(a.V, a.d) ? 1024 : 16384)));
     if (low && a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
@@ -626,7 +641,7 @@ static void go_f32(const VocabArgs& a, F32Product p, bool small, hipStream_t s) 
 static void vocab_products_f32(const VocabArgs& a, int which, hipStream_t s) {
   const float* H = static_cast<const float*>(a.hc) + (long)a.row0 * a.dp;
   const float* W = static_cast<const float*>(a.w);
-  const float* P = static_cast<const float*>(a.P);
+  const float* P = static_cast<const float*>(a.logits);
   const bool vw = (reinterpret_cast<uintptr_t>(W) & 15u) == 0 && a.ldw % 4 == 0;
   F32Product p{};
   if (which < 2) {

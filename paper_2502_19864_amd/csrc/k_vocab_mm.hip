@@ -118,35 +118,23 @@ struct VocabProduct {
 };
 constexpr int MM_LEAST = 512;  // of k to a share
 
-// eight columns of a row of dh or dw
-template <Prod E>
-__device__ __forceinline__ void store_gradient(const VocabArgs& a, int m, int n, float unit, float (&v)[8]) {
-  if constexpr (E == Prod::Dh) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= unit;
-    *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dh) + (long)a.idx[a.row0 + m] * a.lddh + n) = pack_frag(v);
-  } else {
-    float* o = a.dw_acc + (long)m * a.ld_acc + n;  // between pieces, in the unit
-    if (!a.first) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += o[e];
-    }
-    if (a.last) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= unit;
-      *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.dw) + (long)m * a.lddw + n) = pack_frag(v);
-    } else {
-      *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
-      *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
-    }
+// four columns of a row of dw, summed over the pieces, which are in dloss' unit
+__device__ __forceinline__ void add_dw(const VocabArgs& a, int m, int n, float unit, f32x4 v) {
+  f32x4* o = reinterpret_cast<f32x4*>(a.dw_acc + (long)m * a.ld_acc + n);
+  if (!a.first) v += *o;
+  if (!a.last) {
+    *o = v;
+    return;
   }
+  *reinterpret_cast<uint2*>(static_cast<bf16*>(a.dw) + (long)m * a.lddw + n) =
+      make_uint2(f2bf2(v[0] * unit, v[1] * unit), f2bf2(v[2] * unit, v[3] * unit));
 }
 
 // Workgroups stay: one round of the GPU, each over its tiles.  While a tile is stored the first k-tiles of the next are
 // on their way, and its stores drain under the next one's products (2048 x 32000 logits, d 4096: 1.08 times less than a workgroup per tile).
 // So the epilogue has no LDS but 4 KB per wave beside the stages, and no barrier: each wave sends its 32 x 32 blocks
-// through its own, in 16-byte pieces at c ^ row % 8, and stores whole 128-byte (bf16: 64-byte) runs of rows; the logits'
-// statistics are per wave too, one (maximum, sum) for BN / WN columns.
+// through its own, in 16-byte pieces at c ^ row % 8, and stores whole 128-byte lines (64-byte runs: 2048 x 32000 logits 480 us instead of
+// 452); the logits' statistics are per wave too, one (maximum, sum) for BN / WN columns.
 template <int BM, int BN, int WM, int WN, int BK, int NS, bool KA, bool KB, Prod E>
 __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabProduct p) {
   constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32, KS = BK / 16;
@@ -309,7 +297,14 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
 #pragma unroll
         for (int j = 0; j < FN; ++j)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) l += exp_below(acc[i][j][r] - z);
+          for (int r = 0; r < 16; ++r) {
+            if constexpr (E == Prod::Logits) {  // stored so; differences beside the sums would not fit the registers
+              acc[i][j][r] -= z;
+              l += exp_below(acc[i][j][r]);
+            } else {
+              l += exp_below(acc[i][j][r] - z);
+            }
+          }
         l += __shfl_xor(l, 32);
         if (half == 0 && row < M && en0 < N) a.part[(long)row * a.tiles + en0 / TN] = make_float2(m, l);
         if (a.part_at) {
@@ -327,41 +322,62 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
     wait_dma<0>();  // the next tile's first k-tiles; then come the stores
     if constexpr (E != Prod::Stats) {
       char* mine = smem + NS * STAGE + wave * 4096;
+      const int limit = E == Prod::Logits ? a.Vp : N;
+      // 16-bit results, 64 columns of 32 rows at a time; else fp32 sums, 32 columns
+      const bool packed = E == Prod::Logits || (splits == 1 && (E == Prod::Dh || (a.first && a.last)));
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
         const int mb = em0 + i * 32;
         if (mb >= M) continue;  // wave-uniform
+        if (packed) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          const int nb = en0 + j * 32;
-          if (nb >= (E == Prod::Logits ? a.Vp : N)) continue;
+          for (int j = 0; j < FN; j += 2) {
+            const int nb = en0 + j * 32;
+            if (nb >= limit) continue;
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<float4*>(mine + l32 * 128 + (((2 * q + half) ^ (l32 & 7)) << 4)) =
-                make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-          auto ld = [&](int row, int c) { return *reinterpret_cast<const float4*>(mine + row * 128 + ((c ^ (row & 7)) << 4)); };
-          if constexpr (E == Prod::Logits) {
+            for (int q = 0; q < 8; ++q) {
+              float v[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[e] = acc[i][j + q / 4][q % 4 * 4 + e];
+              uint2 w;
+              if constexpr (E == Prod::Logits) {
+                const half4 h = {(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
+                w = __builtin_bit_cast(uint2, h);
+              } else {
+                w = make_uint2(f2bf2(v[0] * unit, v[1] * unit), f2bf2(v[2] * unit, v[3] * unit));
+              }
+              *reinterpret_cast<uint2*>(mine + l32 * 128 + ((q ^ (l32 & 7)) << 4) + half * 8) = w;
+            }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-              const int row = 8 * q + (at >> 3), c = at & 7;
-              const float4 v = ld(row, c);
-              if (mb + row < M) *reinterpret_cast<float4*>(a.logits + (long)(mb + row) * a.Vp + nb + 4 * c) = v;
+              const int row = 8 * q + (at >> 3), c = at & 7, m = mb + row, n = nb + 8 * c;
+              const bf16x8 v = *reinterpret_cast<const bf16x8*>(mine + row * 128 + ((c ^ (row & 7)) << 4));
+              if (m >= M || n >= limit) continue;
+              bf16* o;
+              if constexpr (E == Prod::Logits) o = static_cast<bf16*>(a.logits) + (long)m * a.Vp + n;
+              else if constexpr (E == Prod::Dh) o = static_cast<bf16*>(a.dh) + (long)a.idx[a.row0 + m] * a.lddh + n;
+              else o = static_cast<bf16*>(a.dw) + (long)m * a.lddw + n;
+              *reinterpret_cast<bf16x8*>(o) = v;
             }
-          } else {
+          }
+        } else if constexpr (SHARED) {
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-              const int row = 16 * q + (at >> 2), c = at & 3, m = mb + row, n = nb + 8 * c;
-              float v[8];
-              *reinterpret_cast<float4*>(v) = ld(row, 2 * c);
-              *reinterpret_cast<float4*>(v + 4) = ld(row, 2 * c + 1);
+          for (int j = 0; j < FN; ++j) {
+            const int nb = en0 + j * 32;
+            if (nb >= N) continue;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *reinterpret_cast<float4*>(mine + l32 * 128 + (((2 * q + half) ^ (l32 & 7)) << 4)) =
+                  make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const int row = 8 * q + (at >> 3), c = at & 7, m = mb + row, n = nb + 4 * c;
+              const f32x4 v = *reinterpret_cast<const f32x4*>(mine + row * 128 + ((c ^ (row & 7)) << 4));
               if (m >= M || n >= N) continue;
-              if (splits > 1) {
-                float* o = a.shares + ((long)esplit * tiles + etile) * (BM * BN) + (wm * TM + i * 32 + row) * BN + wn * TN + j * 32 + 8 * c;
-                *reinterpret_cast<float4*>(o) = *reinterpret_cast<float4*>(v);
-                *reinterpret_cast<float4*>(o + 4) = *reinterpret_cast<float4*>(v + 4);
-              } else {
-                store_gradient<E>(a, m, n, unit, v);
-              }
+              if (splits > 1)
+                *reinterpret_cast<f32x4*>(a.shares + ((long)esplit * tiles + etile) * (BM * BN) + (wm * TM + i * 32 + row) * BN + wn * TN + j * 32 + 4 * c) = v;
+              else
+                add_dw(a, m, n, unit, v);
             }
           }
         }
@@ -403,7 +419,17 @@ __global__ __launch_bounds__(256) void vocab_shares_k(VocabArgs a, VocabProduct 
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += red[threadIdx.x + o][e];
   }
-  if (in) store_gradient<E>(a, m, n, dloss_unit(a), v);
+  if (!in) return;
+  const float unit = dloss_unit(a);
+  if (E == Prod::Dw && !(a.first && a.last)) {
+    add_dw(a, m, n, unit, f32x4{v[0], v[1], v[2], v[3]});
+    add_dw(a, m, n + 4, unit, f32x4{v[4], v[5], v[6], v[7]});
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] *= unit;
+  bf16* o = E == Prod::Dh ? static_cast<bf16*>(a.dh) + (long)a.idx[a.row0 + m] * a.lddh : static_cast<bf16*>(a.dw) + (long)m * a.lddw;
+  *reinterpret_cast<bf16x8*>(o + n) = pack_frag(v);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -612,7 +638,7 @@ static void go(const VocabArgs& a, VocabProduct p, hipStream_t s) {
     // one thread per eight columns where those are many, else eight
     const long items = (long)M * (p.N / 8);
     constexpr Prod S = shared ? E : Prod::Dh;
-    if (items >= 65536) RG_LAUNCH((vocab_shares_k<S, 1>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, a, p, BT);
+    if (items >= 16384) RG_LAUNCH((vocab_shares_k<S, 1>), dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, a, p, BT);
     else RG_LAUNCH((vocab_shares_k<S, 8>), dim3((unsigned)((items + 31) / 32)), dim3(256), 0, s, a, p, BT);
   }
 }
@@ -669,7 +695,7 @@ void launch_vocab_logits_bf16(const VocabArgs& a, bool keep, hipStream_t s) {
 }
 void launch_vocab_dh_bf16(const VocabArgs& a, hipStream_t s) {
   VocabProduct p{};
-  p.A = static_cast<const bf16*>(a.P);
+  p.A = static_cast<const bf16*>(a.logits);
   p.lda = a.Vp;
   p.B = static_cast<const bf16*>(a.w);
   p.ldb = a.ldw;
@@ -680,7 +706,7 @@ void launch_vocab_dh_bf16(const VocabArgs& a, hipStream_t s) {
 }
 void launch_vocab_dw_bf16(const VocabArgs& a, hipStream_t s) {
   VocabProduct p{};
-  p.A = static_cast<const bf16*>(a.P);
+  p.A = static_cast<const bf16*>(a.logits);
   p.lda = a.Vp;
   p.B = static_cast<const bf16*>(a.hc) + (long)a.row0 * a.dp;
   p.ldb = a.dp;

@@ -24,6 +24,9 @@ __device__ __forceinline__ Peak join(Peak a, Peak b) {
   return r;
 }
 
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+
 // rows of a piece that count
 __device__ __forceinline__ int piece_rows(const VocabArgs& a) {
   return a.count ? max(0, min(*a.count - a.row0, a.R)) : a.rows;

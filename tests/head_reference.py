@@ -17,7 +17,7 @@ def half_step(dtype):
     return torch.finfo(dtype).eps / 2
 
 
-def norm(s, gain, shift, rms, eps, dy=None, dskip=None, groups=1024):
+def norm(s, gain, shift, rms, eps, dy=None, dskip=None, groups=512):
     """{name: (value, bound)} of y and with dy of dx, dgain, dshift; s [rows, d] as stored."""
     u, k = half_step(s.dtype), 64 * E
     x, g = s.double(), gain.double()
@@ -92,7 +92,10 @@ def vocab(h, w, labels, dloss=None):
         return out
     g = dloss[at].double()[:, None]
     P = p.scatter(1, lab, torch.expm1(-loss))
-    eP = (p * (elog + 4 * E * (1 + logp.abs()))).scatter(1, lab, p.gather(1, lab) * eloss + 4 * E * P.gather(1, lab).abs())
+    # with bf16 tensors a logit is held in fp16 as its distance to the largest near it, which is no more than that to lse: half a
+    # step of it, 2^-11 (2^-25 near zero)
+    e16 = 2.0 ** -11 * logp.abs() + 2.0 ** -24 if up else 0.0
+    eP = (p * (elog + e16 + 4 * E * (1 + logp.abs()))).scatter(1, lab, p.gather(1, lab) * eloss + 4 * E * P.gather(1, lab).abs())
     P, eP = g * P, g.abs() * eP
     eP = eP + up * (P.abs() + eP) * 1.01
     kv, kn = 8 * math.sqrt(V) * E, 8 * math.sqrt(max(1, at.numel())) * E

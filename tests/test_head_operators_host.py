@@ -192,7 +192,7 @@ def test_vocab_plan():
         for n, d, V in ((1, 64, 100), (4096, 768, 30011), (1 << 16, 4096, 131072), (1 << 23, 64, 50), (300, 16384, 1 << 22)):
             f, t, x = B.ringada_vocab_plan(vocab_desc(dtype=dtype, rows=n, d=d, vocab=V))
             copy = (n + 63) * (d + 63) * es + 32 * (n + 64) + 12 * 32 * 512
-            held = 6 * max(1 << 29, 256 * (V + 64)) if es == 2 else 4 * max(1 << 29, 256 * (V + 64))
+            held = es * max((1 << 31) // es, 256 * (V + 64)) * 5 // 4
             assert 0 < f <= copy + (1 << 28) and x <= copy + (1 << 28)
             assert f <= t + (1 << 20) and t <= copy + held + 4 * V * d + (1 << 28)
 
