@@ -447,7 +447,7 @@ typedef struct {
  * sum (res and sum are given together or both NULL).  gain [d] and shift [d] (NULL: none) in `dtype`; stats [rows, 2]
  * floats (NULL: not wanted), 8-byte aligned: mean (0 for RMS) and rstd, which the backward reads.  Any alignment of an
  * element and any stride; 16-byte aligned rows whose d and strides are multiples of 16 bytes are read
- * faster.  y and sum may each be x or res, not both the same tensor; any other overlap of an output is refused
+ * faster.  Squares of s are formed in fp32: s of 2^60 and more overflows them.  y and sum may each be x or res, not both the same tensor; any other overlap of an output is refused
  * (RINGADA_E_INVALID).  Arithmetic and sums in fp32, one rounding each of s and y.  A row with an infinity or NaN
  * gives NaN in that row alone. */
 ringada_status ringada_norm_forward(void* stream, const ringada_norm_desc* desc, const ringada_rows* x,

@@ -305,7 +305,7 @@ struct NormShape {
 };
 static NormShape norm_shape(int dtype, int d, bool back) {
   const int pieces = (d + (dtype == DT_BF16 ? 7 : 3)) / (dtype == DT_BF16 ? 8 : 4);
-  // four pieces to a lane in the forward, two in the backward, which holds three rows and the columns' sums
+  // up to four pieces to a lane in the forward, two in the backward, which holds three rows and the columns' sums
   for (int tpr : {64, 256, 1024})
     for (int ch : {1, 2, 4})
       if (tpr * ch >= pieces && (!back || ch < 4 || tpr == 1024)) return {tpr, ch};
@@ -331,10 +331,12 @@ static hipError_t norm_go(const NormArgs& a, bool back, hipStream_t s) {
     if constexpr (CH < 4 || TPR == 1024) RG_LAUNCH((norm_bwd_k<T, TPR, CH, ahead, WIDE>), dim3(a.groups), dim3(NT), 0, s, a);
     else return hipErrorInvalidValue;
     if (a.part) RG_LAUNCH(norm_sums_k, dim3((a.d + 31) / 32, 2), dim3(1024), 0, s, a);
-  } else {
+  } else if constexpr (CH > 1 || TPR == 64) {
     // HIP takes fewer than 2^32 threads in a dimension of a launch
     const long wgs = (a.rows + RPW - 1) / RPW, y = (wgs + (1l << 21) - 1) >> 21;
     RG_LAUNCH((norm_fwd_k<T, TPR, CH, WIDE>), dim3((unsigned)((wgs + y - 1) / y), (unsigned)y), dim3(NT), 0, s, a);
+  } else {
+    return hipErrorInvalidValue;
   }
   return hipGetLastError();
 }

@@ -628,7 +628,7 @@ static void go_f32(const VocabArgs& a, F32Product p, bool small, hipStream_t s) 
   const unsigned wgs = (unsigned)(shared && tiles < F32_SLOTS ? F32_SLOTS : tiles);
   if (small) RG_LAUNCH((vocab_f32_small_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, p);
   else if (E == Prod::Dw || (p.vb && a.d % 4 == 0)) RG_LAUNCH((vocab_f32_k<KA, KB, E, true>), dim3(wgs), dim3(256), 0, s, a, p);
-  else RG_LAUNCH((vocab_f32_k<KA, KB, E, false>), dim3(wgs), dim3(256), 0, s, a, p);
+  else if constexpr (E != Prod::Dw) RG_LAUNCH((vocab_f32_k<KA, KB, E, false>), dim3(wgs), dim3(256), 0, s, a, p);
   // dw's tiles are known here, dh's may be fewer
   if (shared && k_shares(F32_SLOTS, E == Prod::Dw ? (int)tiles : 1, K, F32_LEAST) > 1)
   {

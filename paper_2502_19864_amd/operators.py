@@ -281,7 +281,7 @@ def rotary(q, k=None, *, positions, freq, sections=None, inverse=False, out_q=No
     [axes, B, S], or [B, S] for one axis, contiguous.  freq: float64, the angle of each pair per position; sections:
     the pairs of each axis (default: one axis has them all).  inverse turns back, which is the backward.  Returns
     (q, k) turned (k None without k), in out_q and out_k if given, which may be q and k themselves."""
-    _no_graph(q, k)
+    _no_graph(q, k, freq)
     dtype, dev = _storage("q", q)
     if q.dim() != 4 or (k is not None and k.dim() != 4):
         raise ValueError("q and k are [batch, rows, heads, d_head]")
@@ -331,6 +331,7 @@ def _vocab(h, w):
 
 def _vocab_ce(h, w, labels, dloss, dh, dw):
     desc, hr, wr, n, dtype, dev = _vocab(h, w)
+    _no_graph(dloss)
     lead = h.shape[:-1]
     lp, gp = _plain("labels", labels, torch.int32, lead, dev), _plain("dloss", dloss, torch.float32, lead, dev)
     loss, lse = torch.empty((2,) + lead, dtype=torch.float32, device=dev)

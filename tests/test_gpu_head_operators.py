@@ -27,6 +27,8 @@ NORMS = [  # dtype, rows, d: pieces of a row, threads per row, and both sides of
     ("bf16", 4, 1024), ("bf16", 3000, 768), ("bf16", 33, 1029), ("bf16", 9, 2048), ("bf16", 700, 2056), ("bf16", 6, 8192),
     ("bf16", 3, 8200), ("bf16", 2, 16384), ("bf16", 5, 16383), ("f32", 1, 2), ("f32", 129, 128), ("f32", 77, 255),
     ("f32", 4, 1025), ("f32", 600, 1028), ("f32", 3, 4096), ("f32", 7, 4099), ("f32", 2, 16384), ("bf16", 5000, 64),
+    ("f32", 9, 400), ("f32", 5, 401), ("f32", 30, 800), ("f32", 6, 801), ("f32", 5, 3001), ("f32", 4, 8000), ("f32", 2, 16383),
+    ("bf16", 11, 1001), ("bf16", 3, 5001),
 ]
 
 
@@ -207,7 +209,12 @@ VOCAB = [  # dtype, rows, d, vocab, share of rows that count
     ("bf16", 1, 8, 1, 1.0), ("bf16", 1, 64, 65, 1.0), ("bf16", 2, 24, 127, 1.0), ("bf16", 16, 512, 4099, 1.0), ("bf16", 17, 264, 2000, 0.9),
     ("bf16", 64, 128, 3000, 1.0), ("bf16", 65, 768, 1283, 0.7), ("bf16", 127, 136, 1024, 1.0), ("bf16", 128, 64, 128, 1.0),
     ("bf16", 129, 320, 640, 1.0), ("bf16", 257, 768, 5001, 0.15), ("bf16", 500, 1024, 777, 0.9), ("bf16", 1000, 256, 9001, 1.0),
-    ("bf16", 700, 2056, 1030, 1.0), ("bf16", 2, 4096, 40000, 1.0), ("bf16", 1500, 520, 300, 0.8), ("bf16", 40, 16, 70000, 1.0),
+    ("bf16", 20000, 16, 130, 0.5), ("bf16", 16385, 24, 70, 0.2), ("f32", 17408, 5, 40, 0.3), ("bf16", 12000, 200, 86, 1.0), ("f32", 9000, 40, 50, 0.9),
+    ("bf16", 700, 2056, 1030, 1.0), ("bf16", 300, 2304, 3000, 1.0), ("bf16", 190, 640, 4000, 0.9), ("f32", 600, 260, 3001, 1.0), ("f32", 700, 257, 2001, 0.8),
+    ("f32", 1500, 1030, 1100, 1.0), ("f32", 400, 1500, 1200, 0.3), ("bf16", 33, 512, 3001, 1.0), ("bf16", 3, 16384, 300, 1.0), ("bf16", 4, 16376, 200, 1.0),
+    ("bf16", 32, 4096, 5000, 1.0), ("bf16", 32, 64, 20000, 0.7), ("bf16", 9, 1000, 100000, 1.0), ("bf16", 4500, 4096, 1000, 1.0),
+    ("f32", 2100, 1000, 300, 1.0), ("f32", 1500, 1032, 1400, 1.0), ("f32", 1200, 1100, 2000, 1.0), ("bf16", 16, 2048, 17000, 1.0),
+    ("bf16", 20, 2048, 17000, 0.9), ("bf16", 20, 512, 33000, 1.0), ("bf16", 20, 2048, 3000, 1.0), ("bf16", 1000, 72, 16000, 1.0), ("bf16", 2, 4096, 40000, 1.0), ("bf16", 1500, 520, 300, 0.8), ("bf16", 40, 16, 70000, 1.0),
 ]
 
 
@@ -272,8 +279,8 @@ def test_vocab_next_takes_the_lowest_of_equals(dtype, n):
     token, logprob = ops.vocab_next(h, w)
     for copies in ([1, 2], [700, 64], [2999, 1500]):
         w2 = torch.cat((w[:copies[0]], w, w[copies[1]:]))  # every row but some stands twice
-        first = torch.tensor([next(i for i in range(len(w2)) if torch.equal(w2[i], w[j])) for j in token.tolist()])
-        assert torch.equal(ops.vocab_next(h, w2)[0].cpu().long(), first)
+        first = [(w2 == w[j]).all(1).nonzero()[0, 0] for j in token.tolist()]
+        assert torch.equal(ops.vocab_next(h, w2)[0].long(), torch.stack(first))
     zero = ops.vocab_next(torch.zeros_like(h), w)
     assert (zero[0] == 0).all()
     R.check("logprob", zero[1], torch.full((n,), -math.log(3000), device="cuda", dtype=torch.float64), torch.full((n,), 64 * R.E * 8, device="cuda", dtype=torch.float64))
@@ -333,6 +340,55 @@ def test_vocab_strides(dtype):
         lead = ops.vocab_ce_train(h.view(2, n // 2, d), w, labels.view(2, -1), dloss.view(2, -1))
         assert lead[0].shape == (2, n // 2) and lead[2].shape == (2, n // 2, d)
         assert all(torch.equal(a.reshape(b.shape), b) for a, b in zip(lead, base))
+
+
+def test_vocab_gradients_one_at_a_time():
+    """dw without dh, through the C names; of rows with one dloss, several, and none in the first."""
+    import torch
+    from paper_2502_19864_amd import binding as B
+    from paper_2502_19864_amd import operators as ops
+    for dtype, code in (("bf16", B.BF16), ("f32", B.F32)):
+        n, d, V = 300, 72, 500
+        h, w, labels, dloss = head(dtype, n, d, V, 0.7)
+        first = int(((labels >= 0) & (labels < V)).nonzero()[0])
+        for k in range(4):
+            g = [dloss, torch.full_like(dloss, -3e-5), dloss * 1e4, dloss.clone()][k]
+            if k == 3:
+                g[first] = 0
+            want = R.vocab(h, w, labels, g)
+            loss, lse, dh, dw = ops.vocab_ce_train(h, w, labels, g)
+            R.check("dh", dh, *want["dh"])
+            R.check("dw", dw, *want["dw"])
+            alone = torch.full_like(w, 7)
+            size = B.ringada_vocab_plan(B.VocabDesc(code, n, d, V))[1]
+            ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+            t = B.VocabTensors(B.Rows(h.data_ptr(), d), B.Rows(w.data_ptr(), d), labels.data_ptr(), loss.data_ptr(), lse.data_ptr(),
+                               g.data_ptr(), B.Rows(0, 0), B.Rows(alone.data_ptr(), d))
+            B.ringada_vocab_ce(torch.cuda.current_stream().cuda_stream, B.VocabDesc(code, n, d, V), t, ws, size)
+            assert torch.equal(alone, dw)
+
+
+def test_vocab_infinities_and_nan_that_count():
+    """A row that counts and holds a NaN or an infinity is NaN, and so is dw; the other rows are as without it."""
+    import torch
+    from paper_2502_19864_amd import operators as ops
+    for dtype in ("bf16", "f32"):
+        for n in (6, 140):
+            h, w, labels, dloss = head(dtype, n, 64, 700, 1.0)
+            clean = ops.vocab_ce_train(h, w, labels, dloss)
+            bad = h.clone()
+            bad[3, 5], bad[n - 1, 0] = math.nan, math.inf
+            loss, lse, dh, dw = ops.vocab_ce_train(bad, w, labels, dloss)
+            sane = torch.ones(n, dtype=torch.bool, device="cuda")
+            sane[3] = sane[n - 1] = False
+            for got, want in ((loss, clean[0]), (lse, clean[1]), (dh, clean[2])):
+                assert torch.equal(got[sane], want[sane]) and torch.isnan(got[~sane]).all()
+            assert torch.isnan(dw).all()
+            f = ops.vocab_ce_forward(bad, w, labels)
+            assert all(torch.isnan(x[~sane]).all() and torch.isfinite(x[sane]).all() for x in f)
+            token, logprob = ops.vocab_next(bad, w)
+            assert ((token >= 0) & (token < 700)).all() and torch.isnan(logprob[~sane]).all()
+            assert torch.equal(token[sane], ops.vocab_next(h, w)[0][sane])
 
 
 def test_vocab_against_differences():
