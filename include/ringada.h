@@ -512,8 +512,8 @@ typedef struct {
 
 /* Host only.  Bytes of the workspaces of ringada_vocab_ce without and with gradients, and of ringada_vocab_next.
  * The logits are held for a piece of the rows at a time, at most 2 GiB of them (or 256 rows), beside a copy of h, 8 bytes for every
- * 32 logits, up to 64 MiB for sums that several workgroups share, and, for rows of more than one piece in bf16, 4 vocab d
- * bytes.  Any pointer may be NULL. */
+ * 32 logits, up to 64 MiB for sums that several workgroups share (over 2^18 classes or rows: one dh or dw in fp32 for each 2^18 of
+ * them), and, for rows of more than one piece in bf16, 4 vocab d bytes.  Any pointer may be NULL. */
 ringada_status ringada_vocab_plan(const ringada_vocab_desc* desc, size_t* forward_bytes, size_t* train_bytes,
                                   size_t* next_bytes);
 

@@ -129,7 +129,7 @@ struct F32Product {
   bool vb;         // B's rows are 16-byte aligned (A's always are)
   int slots;       // dh, dw: workgroups of one round
 };
-constexpr int F32_LEAST = 512;  // of k to a share
+constexpr int F32_LEAST = 512, F32_LONGEST = 1 << 30;  // of k to a share; chains are cut in the kernels
 
 template <Prod E>
 __device__ __forceinline__ void f32_gradient(const VocabArgs& a, int m, int n, float v) {
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(256, 2) void vocab_f32_k(VocabArgs a, F32Product p)
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
   const int tn = (N + BT - 1) / BT, tiles = (M + BT - 1) / BT * tn;
   const int Kall = E == Prod::Dw ? cnt : p.K;
-  const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? k_shares(p.slots, tiles, Kall, F32_LEAST) : 1;
+  const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? k_shares(p.slots, tiles, Kall, F32_LEAST, F32_LONGEST) : 1;
   if ((int)blockIdx.x >= tiles * splits) return;
   const int split = blockIdx.x / tiles;
   int tm, tc;
@@ -379,7 +379,7 @@ __global__ __launch_bounds__(256) void vocab_f32_small_k(VocabArgs a, F32Product
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
   const int tn = (N + BT - 1) / BT, tiles = (M + BT - 1) / BT * tn;
   const int Kall = E == Prod::Dw ? cnt : p.K;
-  const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? k_shares(p.slots, tiles, Kall, F32_LEAST) : 1;
+  const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? k_shares(p.slots, tiles, Kall, F32_LEAST, F32_LONGEST) : 1;
   if ((int)blockIdx.x >= tiles * splits) return;
   const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
   const int m0 = tile / tn * BT, n0 = tile % tn * BT;
@@ -444,7 +444,7 @@ __global__ __launch_bounds__(256) void vocab_f32_shares_k(VocabArgs a, F32Produc
   const int cnt = piece_rows(a), M = E == Prod::Dw ? p.M : cnt, K = E == Prod::Dw ? cnt : p.K;
   const int m = blockIdx.x, lane = threadIdx.x % (256 / G), g = threadIdx.x / (256 / G), n = blockIdx.y * (256 / G) + lane;
   if (m >= M) return;
-  const int tn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * tn, splits = k_shares(p.slots, tiles, K, F32_LEAST);
+  const int tn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * tn, splits = k_shares(p.slots, tiles, K, F32_LEAST, F32_LONGEST);
   if (splits == 1) return;
   float v = 0.f;
   if (n < p.N) {
@@ -470,18 +470,26 @@ __device__ __forceinline__ Peak join_wave(Peak p) {
   return p;
 }
 
-// One wave per row: loss and lse, or the token and its log-probability.
-__global__ __launch_bounds__(256) void vocab_rows_k(VocabArgs a) {
-  const int m = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (m >= piece_rows(a)) return;
+// ... and by those of a workgroup; red: one of each wave
+__device__ __forceinline__ Peak join_row(const VocabArgs& a, int m, Peak* red) {
   Peak p{-INFINITY, 0.f, INT32_MAX};
-#pragma unroll 4
-  for (int t = lane; t < a.tiles; t += 64) {
+  for (int t = threadIdx.x; t < a.tiles; t += 256) {
     const float2 q = a.part[(long)m * a.tiles + t];
     p = join(p, Peak{q.x, q.y, a.part_at ? a.part_at[(long)m * a.tiles + t] : 0});
   }
   p = join_wave(p);
-  if (lane) return;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = p;
+  __syncthreads();
+  return join(join(red[0], red[1]), join(red[2], red[3]));
+}
+
+// A workgroup per row: loss and lse, or the token and its log-probability.
+__global__ __launch_bounds__(256) void vocab_rows_k(VocabArgs a) {
+  __shared__ Peak red[4];
+  const int m = blockIdx.x;
+  if (m >= piece_rows(a)) return;
+  const Peak p = join_row(a, m, red);
+  if (threadIdx.x) return;
   if (a.few && a.labels && !counts(a, a.labels[m])) {
     a.loss[m] = a.lse[m] = 0.f;
     return;
@@ -525,15 +533,7 @@ __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
     for (int v0 = first; v0 < last; v0 += 2048) store(v0, zero);
     return;
   }
-  Peak q{-INFINITY, 0.f, 0};
-  for (int t = tid; t < a.tiles; t += 256) {
-    const float2 x = a.part[(long)m * a.tiles + t];
-    q = join(q, Peak{x.x, x.y, 0});
-  }
-  q = join_wave(q);
-  if ((tid & 63) == 0) red[tid >> 6] = q;
-  __syncthreads();
-  q = join(join(red[0], red[1]), join(red[2], red[3]));
+  const Peak q = join_row(a, m, red);
   const float log_l = logf(q.l), lse = q.m + log_l;
   const float loss = (q.m - a.target[a.row0 + m]) + log_l;  // not lse - s: of a row that is sure of its label little is left
   float g = a.g_c[a.row0 + m];
@@ -630,7 +630,7 @@ static void go_f32(const VocabArgs& a, F32Product p, bool small, hipStream_t s) 
   else if (E == Prod::Dw || (p.vb && a.d % 4 == 0)) RG_LAUNCH((vocab_f32_k<KA, KB, E, true>), dim3(wgs), dim3(256), 0, s, a, p);
   else if constexpr (E != Prod::Dw) RG_LAUNCH((vocab_f32_k<KA, KB, E, false>), dim3(wgs), dim3(256), 0, s, a, p);
   // dw's tiles are known here, dh's may be fewer
-  if (shared && k_shares(F32_SLOTS, E == Prod::Dw ? (int)tiles : 1, K, F32_LEAST) > 1)
+  if (shared && k_shares(F32_SLOTS, E == Prod::Dw ? (int)tiles : 1, K, F32_LEAST, F32_LONGEST) > 1)
   {
     constexpr Prod S = shared ? E : Prod::Dh;
     if (rows * p.N >= 262144) RG_LAUNCH((vocab_f32_shares_k<S, 1>), dim3((unsigned)rows, (p.N + 255) / 256), dim3(256), 0, s, a, p, bt);
@@ -664,7 +664,7 @@ static hipError_t vocab_t(VocabArgs a, hipStream_t s) {
   if (a.few) {
     a.rows = a.n;
     launch_vocab_few_bf16(a, s);
-    RG_LAUNCH(vocab_rows_k, dim3((a.n + 3) / 4), dim3(256), 0, s, a);
+    RG_LAUNCH(vocab_rows_k, dim3(a.n), dim3(256), 0, s, a);
     return hipGetLastError();
   }
   if (a.labels && a.block_count) RG_LAUNCH(vocab_count_k, dim3((a.n + 1023) / 1024), dim3(256), 0, s, a);
@@ -678,7 +678,7 @@ static hipError_t vocab_t(VocabArgs a, hipStream_t s) {
     if constexpr (low) launch_vocab_logits_bf16(a, grads, s);
     else vocab_products_f32(a, grads, s);
     if (!grads) {
-      RG_LAUNCH(vocab_rows_k, dim3((a.rows + 3) / 4), dim3(256), 0, s, a);
+      RG_LAUNCH(vocab_rows_k, dim3(a.rows), dim3(256), 0, s, a);
       continue;
     }
     RG_LAUNCH(vocab_p_k<T>, dim3((unsigned)up(a.rows, 64), (a.Vp + P_COLS - 1) / P_COLS), dim3(256), 0, s, a);

@@ -3,7 +3,7 @@
 //
 // One kernel on MFMA 32x32x16, whose operands may lie either way in memory: [rows][k], as h and w do for the
 // logits, or [k][rows], as w does for dh and both of P and h do for dw.  So nothing is transposed in memory, where
-// a copy of w or P would cost as much as reading it twice.  Tiles come by DMA, two to four stages deep, 64 k
+// a copy of w or P would cost as much as reading it twice.  Tiles come by DMA, two stages deep, 64 k
 // wide.  In LDS an operand keeps its order:
 //  * [rows][64]: chunk c (16 B) of row r at c ^ (r / 2) % 8, so the 16 rows that one pass of a fragment read
 //    touches hit all banks once;
@@ -116,7 +116,9 @@ struct VocabProduct {
   int K;           // k of the logits (d) and of dh (V)
   int slots;       // dh, dw: workgroups of one round
 };
-constexpr int MM_LEAST = 512;  // of k to a share
+// Of k to a share.  2^18 terms are 2^14 additions in a chain; if each leans by half a step of fp32, that is 2^-11 of the sum, below the
+// rounding to bf16.
+constexpr int MM_LEAST = 512, MM_LONGEST = 1 << 18;
 
 // four columns of a row of dw, summed over the pieces, which are in dloss' unit
 __device__ __forceinline__ void add_dw(const VocabArgs& a, int m, int n, float unit, f32x4 v) {
@@ -135,14 +137,14 @@ __device__ __forceinline__ void add_dw(const VocabArgs& a, int m, int n, float u
 // So the epilogue has no LDS but 4 KB per wave beside the stages, and no barrier: each wave sends its 32 x 32 blocks
 // through its own, in 16-byte pieces at c ^ row % 8, and stores whole 128-byte lines (64-byte runs: 2048 x 32000 logits 480 us instead of
 // 452); the logits' statistics are per wave too, one (maximum, sum) for BN / WN columns.
-template <int BM, int BN, int WM, int WN, int BK, int NS, bool KA, bool KB, Prod E>
+template <int BM, int BN, int WM, int WN, bool KA, bool KB, Prod E>
 __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabProduct p) {
-  constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32, KS = BK / 16;
+  constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32, BK = 64, NS = 2, KS = BK / 16;
   using OA = Operand<BM, BK, NW, KA>;
   using OB = Operand<BN, BK, NW, KB>;
   constexpr int LPT = OA::L + OB::L, STAGE = (BM + BN) * BK * 2;
   constexpr int ND = FM * (KA ? 1 : 2) + FN * (KB ? 1 : 2);
-  static_assert(FM * 32 * WM == BM && FN * 32 * WN == BN && NS >= 2 && NS <= 4 && LPT * (NS - 1) < 64, "tile");
+  static_assert(FM * 32 * WM == BM && FN * 32 * WN == BN, "tile");
   static_assert(NS * STAGE + NW * 4096 <= 160 * 1024, "LDS");
   __shared__ __attribute__((aligned(1024))) char smem[NS * STAGE + NW * 4096];
 
@@ -153,7 +155,7 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
   const int K = E == Prod::Dw ? cnt : p.K;
   const int ntm = (M + BM - 1) / BM, ntn = (N + BN - 1) / BN, tiles = ntm * ntn;
   constexpr bool SHARED = E == Prod::Dh || E == Prod::Dw;
-  const int splits = SHARED && tiles ? __builtin_amdgcn_readfirstlane(k_shares(p.slots, tiles, K, MM_LEAST)) : 1;
+  const int splits = SHARED && tiles ? __builtin_amdgcn_readfirstlane(k_shares(p.slots, tiles, K, MM_LEAST, MM_LONGEST)) : 1;
   const int nk_all = (K + BK - 1) / BK;
   int m0 = 0, n0 = 0, split = 0, kt0 = 0, nk = 0, tile = 0;
   // the g-th piece of work, or none
@@ -198,28 +200,23 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
     ra.read(smem + slot * STAGE, ks, lane, fa[buf]);
     rb.read(smem + slot * STAGE + BM * BK * 2, ks, lane, fb[buf]);
   };
-  auto wait_tiles = [&](int n) {  // at most n k-tiles still in flight
-    if constexpr (NS >= 4) { if (n >= 2) { wait_dma<2 * LPT>(); return; } }
-    if constexpr (NS >= 3) { if (n >= 1) { wait_dma<LPT>(); return; } }
-    wait_dma<0>();
-  };
   f32x16 acc[FM][FN];
   // A finished stage is refilled in pieces, the first right after the barrier that frees it.  The first NS k-tiles of a tile
   // had landed before the stores of the last one were issued: they are not waited for, so neither are the stores.
-  constexpr int PARTS = NS >= 3 ? KS : 2;
+  constexpr int PARTS = 2;
   auto step = [&](auto S, int kt) {
-    constexpr int s = decltype(S)::value, sn = (s + 1) % NS, sp = (s + NS - 1) % NS;
+    constexpr int s = decltype(S)::value, other = 1 - s;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       if (ks + 1 < KS) {
-        if (ks + 1 < PARTS && kt > 0 && kt - 1 + NS < nk) issue(kt - 1 + NS, sp, ks + 1, PARTS);
+        if (ks + 1 < PARTS && kt > 0 && kt + 1 < nk) issue(kt + 1, other, ks + 1, PARTS);
         read_frags(s, ks + 1, (ks + 1) & 1);
       } else if (kt + 1 < nk) {
-        if (kt + 1 >= NS) wait_tiles(min(NS - 2, nk - 2 - kt));
+        if (kt + 1 >= NS) wait_dma<0>();
         else __builtin_amdgcn_s_waitcnt(0xF | (0x7 << 4) | (0x3 << 14));  // lgkmcnt == 0
         wg_barrier();
         if (kt + NS < nk) issue(kt + NS, s, 0, PARTS);
-        read_frags(sn, 0, 0);
+        read_frags(other, 0, 0);
       }
 #pragma unroll
       for (int i = 0; i < FM; ++i)
@@ -245,8 +242,6 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
       for (int kt = 0; kt < nk; kt += NS) {
         step(std::integral_constant<int, 0>{}, kt);
         if (kt + 1 < nk) step(std::integral_constant<int, 1>{}, kt + 1);
-        if constexpr (NS > 2) if (kt + 2 < nk) step(std::integral_constant<int, 2>{}, kt + 2);
-        if constexpr (NS > 3) if (kt + 3 < nk) step(std::integral_constant<int, 3>{}, kt + 3);
       }
     }
     const int em0 = m0 + wm * TM, en0 = n0 + wn * TN, etile = tile, esplit = split;
@@ -394,7 +389,7 @@ __global__ __launch_bounds__(256) void vocab_shares_k(VocabArgs a, VocabProduct 
   __shared__ float red[G > 1 ? 256 : 1][9];
   const int cnt = piece_rows(a), M = E == Prod::Dw ? p.M : cnt, K = E == Prod::Dw ? cnt : p.K;
   const int cols = p.N / 8, g = threadIdx.x % G, i = blockIdx.x * (256 / G) + threadIdx.x / G, m = i / cols, n = i % cols * 8;
-  const int ntn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * ntn, splits = tiles ? k_shares(p.slots, tiles, K, MM_LEAST) : 1;
+  const int ntn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * ntn, splits = tiles ? k_shares(p.slots, tiles, K, MM_LEAST, MM_LONGEST) : 1;
   if (splits == 1) return;
   const bool in = m < M;
   float v[8] = {};
@@ -629,12 +624,12 @@ static void go(const VocabArgs& a, VocabProduct p, hipStream_t s) {
   const int M = E == Prod::Dw ? p.M : a.rows, K = E == Prod::Dw ? a.rows : p.K;
   const int tiles = tiles_of(M, BM) * tiles_of(p.N, BT);
   p.slots = mm_slots(BT);
-  const int most = k_shares(p.slots, 1, K, MM_LEAST);  // of a tile, however few the rows that count are
-  int wgs = shared && tiles < p.slots ? tiles * (E == Prod::Dw ? k_shares(p.slots, tiles, K, MM_LEAST) : most) : tiles;
+  const int most = k_shares(p.slots, 1, K, MM_LEAST, MM_LONGEST);  // of a tile, however few the rows that count are
+  long wgs = (long)tiles * (!shared ? 1 : E == Prod::Dw ? k_shares(p.slots, tiles, K, MM_LEAST, MM_LONGEST) : most);
   if (wgs > p.slots) wgs = p.slots;
-  RG_LAUNCH((vocab_mm_k<BM, BT, WM, WN, 64, 2, KA, KB, E>), dim3(wgs), dim3(64 * WM * WN), 0, s, a, p);
+  RG_LAUNCH((vocab_mm_k<BM, BT, WM, WN, KA, KB, E>), dim3((unsigned)wgs), dim3(64 * WM * WN), 0, s, a, p);
   // dw's tiles are known here, dh's are not
-  if (shared && (E == Prod::Dw ? k_shares(p.slots, tiles, K, MM_LEAST) : most) > 1) {
+  if (shared && (E == Prod::Dw ? k_shares(p.slots, tiles, K, MM_LEAST, MM_LONGEST) : most) > 1) {
     // one thread per eight columns where those are many, else eight
     const long items = (long)M * (p.N / 8);
     constexpr Prod S = shared ? E : Prod::Dh;
@@ -644,8 +639,8 @@ static void go(const VocabArgs& a, VocabProduct p, hipStream_t s) {
 }
 
 // Rows and columns of the logits' tiles, by the rounds of the GPU that they take: f + r K / 64 us each, fitted to 333 to 4096
-// rows, 20000 to 50000 classes, d 768 to 4096.  256 x 256 has the best rate, 192 x 256 the rows that 256 leaves over (333 x 32000, d 4096: 84 us
-// against 109), 128 x 128, two to a CU, the shortest epilogue.
+// rows, 20000 to 50000 classes, d 768 to 4096.  256 x 256 has the best rate, 192 x 256 the rows that 256 leaves over (333 x 32000, d 4096: 107 us
+// against 114), 128 x 128, two to a CU, the shortest epilogue.
 enum class LogitsTile { T256, T192, T128 };
 static LogitsTile logits_tile(int rows, int d, int V) {
   const int k = tiles_of(d, 64);
@@ -661,8 +656,10 @@ static bool wide_dw(int rows, int d, int V) { return rows > 128 && tiles_of(V, 2
 
 size_t vocab_share_bytes(int rows, int d, int V) {
   auto bytes = [](int t, long tiles, int K) {
-    const long most = tiles * k_shares(mm_slots(t), 1, K, MM_LEAST);
-    return (size_t)(most < mm_slots(t) ? most : mm_slots(t)) * t * t * 4;
+    // whichever rows count: shares times tiles are at most a round of workgroups, but for the chains
+    const long by_slots = tiles * k_shares(mm_slots(t), 1, K, MM_LEAST, MM_LONGEST), chains = tiles * ((K + (long)MM_LONGEST - 1) / MM_LONGEST);
+    const long most = by_slots < mm_slots(t) ? by_slots : mm_slots(t);
+    return (size_t)(most > chains ? most : chains) * t * t * 4;
   };
   const int th = wide_dh(rows, d) ? 256 : 128, tw = wide_dw(rows, d, V) ? 256 : 128;
   const size_t h = bytes(th, (long)tiles_of(rows, th) * tiles_of(d, th), V);

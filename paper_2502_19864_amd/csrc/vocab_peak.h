@@ -42,10 +42,11 @@ __device__ __forceinline__ float dloss_unit(const VocabArgs& a) {
   return g >= 0x1p-40f && g <= 0x1p40f ? g : 1.f;
 }
 
-// Workgroups that share the k of a tile, where the tiles of the rows that count leave CUs idle: at least `least` of k to each
-__host__ __device__ inline int k_shares(int slots, int tiles, int K, int least) {
-  const int by_slots = slots / tiles, by_k = K / least, s = by_slots < by_k ? by_slots : by_k;
-  return s < 1 ? 1 : s;
+// Workgroups that share the k of a tile: where the tiles of the rows that count leave CUs idle, at least `least` of k to each, and
+// never more than `longest`, the chain of additions in the matrix unit that a sum's precision allows
+__host__ __device__ inline int k_shares(int slots, int tiles, int K, int least, int longest) {
+  const int by_slots = slots / tiles, by_k = K / least, s = by_slots < by_k ? by_slots : by_k, chains = (int)(((long)K + longest - 1) / longest);
+  return s > chains ? s : chains > 1 ? chains : 1;
 }
 
 // The tile of C[m][n] = sum_k A(m, k) B(n, k) that a workgroup makes, by XCD: workgroups are dealt round-robin to the eight

@@ -189,7 +189,7 @@ def dropout(x, p, rng, site=0, res=None, out=None):
 # ---------------------------------------------------------------- rows of d elements: norms and the vocabulary head
 def _fresh(t):
     """A new contiguous tensor as t (the quickest of torch's ways: a small call is bound by its time on the host)."""
-    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _storage(name, t):
@@ -210,6 +210,14 @@ def _rows(name, t, shape, dtype, dev):
     if t.dim() != 2 or (t.stride(1) != 1 and d != 1):
         raise ValueError(f"{name}: rows must be contiguous, and evenly spaced in more than two dimensions")
     return t.data_ptr(), t.stride(0)
+
+
+def _out_rows(name, t, like, shape, dtype, dev):
+    """An output and its packed rows: t, or a new tensor."""
+    if t is None:
+        t = _fresh(like)
+        return t, _ROWS.pack(t.data_ptr(), shape[-1])
+    return t, _ROWS.pack(*_rows(name, t, shape, dtype, dev))
 
 
 @functools.lru_cache(maxsize=256)
@@ -238,10 +246,8 @@ def norm_forward(x, gain, shift=None, *, rms=False, eps=1e-5, res=None, out=None
     s = x
     if res is not None:
         rr = _ROWS.pack(*_rows("res", res, shape, dtype, dev))
-        s = _fresh(x) if out_sum is None else out_sum
-        sr = _ROWS.pack(*_rows("out_sum", s, shape, dtype, dev))
-    y = _fresh(x) if out is None else out
-    yr = _ROWS.pack(*_rows("out", y, shape, dtype, dev))
+        s, sr = _out_rows("out_sum", out_sum, x, shape, dtype, dev)
+    y, yr = _out_rows("out", out, x, shape, dtype, dev)
     gp, bp = _plain("gain", gain, dtype, (d,), dev), _plain("shift", shift, dtype, (d,), dev)
     stats = torch.empty((x.numel() // d, 2), dtype=torch.float32, device=dev) if with_stats else None
     _on(dev, B.ringada_norm_forward, desc, xr, rr, sr, gp, bp or None, yr, stats)
@@ -259,16 +265,24 @@ def norm_backward(dy, s, gain, stats, *, rms=False, dskip=None, dgain=None, dshi
     rows = s.numel() // d
     if stats is None:
         raise ValueError("the backward needs the forward's stats")
-    dx = _fresh(s) if out is None else out
+    dx, xr = _out_rows("out", out, s, shape, dtype, dev)
     dyr, sr = _ROWS.pack(*_rows("dy", dy, shape, dtype, dev)), _ROWS.pack(*_rows("s", s, shape, dtype, dev))
     kr = None if dskip is None else _ROWS.pack(*_rows("dskip", dskip, shape, dtype, dev))
-    xr = _ROWS.pack(*_rows("out", dx, shape, dtype, dev))
     gp, tp = _plain("gain", gain, dtype, (d,), dev), _plain("stats", stats, torch.float32, (rows, 2), dev)
     dgp, dbp = _plain("dgain", dgain, torch.float32, (d,), dev), _plain("dshift", dshift, torch.float32, (d,), dev)
     n = _norm_plan(desc) if dgp or dbp else 0
     ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
     _on(dev, B.ringada_norm_backward, desc, dyr, kr, sr, gp, tp, xr, dgp or None, dbp or None, ws, n)
     return dx
+
+
+def _out_view(name, t, like, shape, dtype, dev):
+    """As _out_rows, of [batch, rows, heads, d_head]."""
+    if t is None:
+        t = _fresh(like)
+        _, rows, h, dh = shape
+        return t, _VIEW.pack(t.data_ptr(), rows * h * dh, h * dh, dh)
+    return t, _VIEW.pack(*_view(name, t, shape, dtype, dev))
 
 
 def rotary_frequencies(sections, theta=10000.0, shared=False, device="cpu"):
@@ -303,12 +317,10 @@ def rotary(q, k=None, *, positions, freq, sections=None, inverse=False, out_q=No
         if kv == 0:
             raise ValueError("k: no heads")
         kr = _VIEW.pack(*_view("k", k, kshape, dtype, dev))
-        ok = _fresh(k) if out_k is None else out_k
-        okr = _VIEW.pack(*_view("out_k", ok, kshape, dtype, dev))
-    oq = _fresh(q) if out_q is None else out_q
+        ok, okr = _out_view("out_k", out_k, k, kshape, dtype, dev)
+    oq, oqr = _out_view("out_q", out_q, q, (b, rows, h, dh), dtype, dev)
     desc = _pack(_ROTARY, _DTYPES[dtype], b, rows, h, kv, dh, axes, *sections, *([0] * (4 - axes)), bool(inverse))
-    _on(dev, B.ringada_rotary, desc, _VIEW.pack(*_view("q", q, q.shape, dtype, dev)), kr, pp, fp,
-        _VIEW.pack(*_view("out_q", oq, q.shape, dtype, dev)), okr)
+    _on(dev, B.ringada_rotary, desc, _VIEW.pack(*_view("q", q, q.shape, dtype, dev)), kr, pp, fp, oqr, okr)
     return oq, (ok if k is not None else None)
 
 

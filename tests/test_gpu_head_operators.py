@@ -432,6 +432,18 @@ def test_vocab_in_pieces(dtype, n, V):
             R.check(name, g, *want[name])
 
 
+def test_vocab_long_sums_are_cut():
+    """dh over 300007 classes, with tiles enough for every CU."""
+    import torch
+    from paper_2502_19864_amd import operators as ops
+    h, w, labels, dloss = head("bf16", 3300, 2304, 300007, 1.0)
+    loss, lse, dh, _ = ops.vocab_ce_train(h, w, labels, dloss, frozen=True)
+    rows = slice(1000, 1200)
+    want = R.vocab(h[rows], w, labels[rows], dloss[rows])
+    for name, got in (("loss", loss), ("lse", lse), ("dh", dh)):
+        R.check(name, got[rows], *want[name])
+
+
 # ---------------------------------------------------------------- streams and graphs
 def calls(seed, n=70):
     """One call of each operator as a function of no arguments that returns its outputs."""

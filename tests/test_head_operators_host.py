@@ -194,7 +194,8 @@ def test_vocab_plan():
             copy = (n + 63) * (d + 63) * es + 32 * (n + 64) + 12 * 32 * 512
             held = es * max((1 << 31) // es, 256 * (V + 64)) * 5 // 4
             assert 0 < f <= copy + (1 << 28) and x <= copy + (1 << 28)
-            assert f <= t + (1 << 20) and t <= copy + held + 4 * V * d + (1 << 28)
+            cut = 4 * (min(n, held // V) + 255) * (d + 255) * (1 + (V >> 18))  # dh over more than 2^18 classes, in shares
+            assert f <= t + (1 << 20) and t <= copy + held + 4 * V * d + cut + (1 << 28)
 
 
 # ---------------------------------------------------------------- the Python front end
