@@ -610,7 +610,7 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   if (grads) {
     a.g_c = static_cast<float*>(take((size_t)a.n * 4));
     a.logits = take((size_t)a.R * a.Vp * es);
-    a.shares = static_cast<float*>(take(low ? vocab_share_bytes(a.n, a.d, a.V)
+    a.shares = static_cast<float*>(take(low ? vocab_share_bytes(a.n, a.R, a.d, a.V)
                                             : (size_t)F32_SLOTS * 4 * (f32_small(a.n, a.d) && f32_small(a.V, a.d) ? 1024 : 16384)));
     if (low && a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
     a.ld_acc = a.d;

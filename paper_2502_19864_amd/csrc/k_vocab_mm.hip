@@ -654,16 +654,16 @@ int vocab_mm_bn(int rows, int d, int V) { return logits_tile(rows, d, V) == Logi
 static bool wide_dh(int rows, int d) { return rows > 128 && tiles_of(rows, 256) * tiles_of(d, 256) >= 128; }
 static bool wide_dw(int rows, int d, int V) { return rows > 128 && tiles_of(V, 256) * tiles_of(d, 256) >= 128; }
 
-size_t vocab_share_bytes(int rows, int d, int V) {
+size_t vocab_share_bytes(int rows, int R, int d, int V) {
   auto bytes = [](int t, long tiles, int K) {
     // whichever rows count: shares times tiles are at most a round of workgroups, but for the chains
-    const long by_slots = tiles * k_shares(mm_slots(t), 1, K, MM_LEAST, MM_LONGEST), chains = tiles * ((K + (long)MM_LONGEST - 1) / MM_LONGEST);
-    const long most = by_slots < mm_slots(t) ? by_slots : mm_slots(t);
-    return (size_t)(most > chains ? most : chains) * t * t * 4;
+    const long by_slots = tiles * k_shares(mm_slots(t), 1, K, MM_LEAST, MM_LONGEST), chains = (K + (long)MM_LONGEST - 1) / MM_LONGEST;
+    const long most = by_slots < mm_slots(t) ? by_slots : mm_slots(t), cut = chains > 1 ? tiles * chains : 0;
+    return (size_t)(most > cut ? most : cut) * t * t * 4;
   };
   const int th = wide_dh(rows, d) ? 256 : 128, tw = wide_dw(rows, d, V) ? 256 : 128;
-  const size_t h = bytes(th, (long)tiles_of(rows, th) * tiles_of(d, th), V);
-  const size_t w = bytes(tw, (long)tiles_of(V, tw) * tiles_of(d, tw), rows);
+  const size_t h = bytes(th, (long)tiles_of(R, th) * tiles_of(d, th), V);
+  const size_t w = bytes(tw, (long)tiles_of(V, tw) * tiles_of(d, tw), R);
   return h > w ? h : w;
 }
 

@@ -274,7 +274,7 @@ struct VocabArgs {
 size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws);
 // the bf16 products (k_vocab_mm.hip): columns of a tile of logits, bytes of shares, the launches of one piece
 int vocab_mm_bn(int rows, int d, int V);
-size_t vocab_share_bytes(int rows, int d, int V);
+size_t vocab_share_bytes(int rows, int R, int d, int V);
 bool vocab_few(int rows, int d);         // whether rows are few enough to read w straight into registers
 int vocab_few_wgs(int rows, int d);
 void launch_vocab_few_bf16(const VocabArgs& a, hipStream_t s);
