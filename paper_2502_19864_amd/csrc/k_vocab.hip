@@ -371,7 +371,7 @@ __global__ __launch_bounds__(256, 2) void vocab_f32_k(VocabArgs a, F32Product p)
 // to registers, the four waves take every fourth eight of k and are added up in LDS in their order.  Lane l
 // holds row l % 32; half l / 32 feeds k0 + 4 (l / 32) + j to the j-th MFMA, the same in both operands.
 template <bool KA, bool KB, Prod E>
-__global__ __launch_bounds__(256) void vocab_f32_small_k(VocabArgs a, F32Product p) {
+__device__ __forceinline__ void f32_small(const VocabArgs& a, const F32Product& p, int wg) {
   constexpr int BT = 32, CP = BT + 4, PF = 4, LONG = 1024;
   __shared__ __attribute__((aligned(16))) float red[4][BT * CP];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
@@ -380,8 +380,8 @@ __global__ __launch_bounds__(256) void vocab_f32_small_k(VocabArgs a, F32Product
   const int tn = (N + BT - 1) / BT, tiles = (M + BT - 1) / BT * tn;
   const int Kall = E == Prod::Dw ? cnt : p.K;
   const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? k_shares(p.slots, tiles, Kall, F32_LEAST, F32_LONGEST) : 1;
-  if ((int)blockIdx.x >= tiles * splits) return;
-  const int split = blockIdx.x / tiles, tile = blockIdx.x - split * tiles;
+  if (wg >= tiles * splits) return;
+  const int split = wg / tiles, tile = wg - split * tiles;
   const int m0 = tile / tn * BT, n0 = tile % tn * BT;
   const int n8 = (Kall + 7) / 8;
   const int kb = (int)((long)n8 * split / splits) * 8, K = min(Kall, (int)((long)n8 * (split + 1) / splits) * 8);
@@ -435,6 +435,15 @@ __global__ __launch_bounds__(256) void vocab_f32_small_k(VocabArgs a, F32Product
   }
   __syncthreads();
   f32_epilogue<BT, CP, E>(a, p, red[0], M, N, m0, n0, tile, split, splits, tiles);
+}
+template <bool KA, bool KB, Prod E>
+__global__ __launch_bounds__(256) void vocab_f32_small_k(VocabArgs a, F32Product p) {
+  f32_small<KA, KB, E>(a, p, blockIdx.x);
+}
+// both gradients in one launch, dh by the first n_dh workgroups
+__global__ __launch_bounds__(256) void vocab_f32_small_grads_k(VocabArgs a, F32Product dh, F32Product dw, int n_dh) {
+  if ((int)blockIdx.x < n_dh) f32_small<true, false, Prod::Dh>(a, dh, blockIdx.x);
+  else f32_small<false, false, Prod::Dw>(a, dw, blockIdx.x - n_dh);
 }
 
 // dh or dw of a piece from its shares.  G threads take every G-th share of a column each, and are added up in their order.
@@ -573,7 +582,7 @@ __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
 static long up(long x, long m) { return (x + m - 1) / m * m; }
 
 // Whether the fp32 products take 32-wide tiles: where 128-wide ones leave most CUs idle
-static bool f32_small(long rows, long cols) { return up(rows, 128) / 128 * (up(cols, 128) / 128) < 128; }
+static bool small_tiles(long rows, long cols) { return up(rows, 128) / 128 * (up(cols, 128) / 128) < 128; }
 constexpr int F32_SLOTS = 512;
 
 // The workspace: sizes, and the pointers into it where there is one
@@ -582,7 +591,7 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   const long es = low ? 2 : 4, np = up(a.n, 64);
   a.Vp = (int)up(a.V, 64);
   a.dp = (int)up(a.d, 64);
-  a.bn = low ? vocab_mm_bn(a.n, a.d, a.V) : f32_small(a.n, a.V) ? 32 : 128;
+  a.bn = low ? vocab_mm_bn(a.n, a.d, a.V) : small_tiles(a.n, a.V) ? 32 : 128;
   a.few = low && !grads && vocab_few(a.n, a.d);
   a.tiles = a.few ? vocab_few_wgs(a.n, a.d) : (a.V + a.bn - 1) / a.bn;
   // rows at a time: 2 GiB of logits, 2^24 partial sums; whole tiles of rows
@@ -611,50 +620,61 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
     a.g_c = static_cast<float*>(take((size_t)a.n * 4));
     a.logits = take((size_t)a.R * a.Vp * es);
     a.shares = static_cast<float*>(take(low ? vocab_share_bytes(a.n, a.R, a.d, a.V)
-                                            : (size_t)F32_SLOTS * 4 * (f32_small(a.n, a.d) && f32_small(a.V, a.d) ? 1024 : 16384)));
+                                            : (size_t)F32_SLOTS * 4 * (small_tiles(a.n, a.d) && small_tiles(a.V, a.d) ? 1024 : 16384)));
     if (low && a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
     a.ld_acc = a.d;
   }
   return at;
 }
 
+static long f32_tiles(long rows, long cols, int bt) { return (up(rows, bt) / bt) * (up(cols, bt) / bt); }
+
+// sums of shares, where there may be any: dw's tiles are known here, dh's may be fewer
+template <Prod E>
+static void f32_shares(const VocabArgs& a, const F32Product& p, int bt, hipStream_t s) {
+  const long rows = E == Prod::Dw ? p.M : a.rows;
+  const int K = E == Prod::Dw ? a.rows : p.K;
+  if (k_shares(F32_SLOTS, E == Prod::Dw ? (int)f32_tiles(rows, p.N, bt) : 1, K, F32_LEAST, F32_LONGEST) == 1) return;
+  if (rows * p.N >= 262144) RG_LAUNCH((vocab_f32_shares_k<E, 1>), dim3((unsigned)rows, (p.N + 255) / 256), dim3(256), 0, s, a, p, bt);
+  else RG_LAUNCH((vocab_f32_shares_k<E, 8>), dim3((unsigned)rows, (p.N + 31) / 32), dim3(256), 0, s, a, p, bt);
+}
+
 template <bool KA, bool KB, Prod E>
-static void go_f32(const VocabArgs& a, F32Product p, bool small, hipStream_t s) {
+static void go_f32(const VocabArgs& a, const F32Product& p, bool small, hipStream_t s) {
   constexpr bool shared = E == Prod::Dh || E == Prod::Dw;
   const int bt = small ? 32 : 128;
-  const long rows = E == Prod::Dw ? p.M : a.rows, tiles = (up(rows, bt) / bt) * (up(p.N, bt) / bt);
-  const int K = E == Prod::Dw ? a.rows : p.K;
-  p.slots = F32_SLOTS;
+  const long tiles = f32_tiles(E == Prod::Dw ? p.M : a.rows, p.N, bt);
   const unsigned wgs = (unsigned)(shared && tiles < F32_SLOTS ? F32_SLOTS : tiles);
   if (small) RG_LAUNCH((vocab_f32_small_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, p);
   else if (E == Prod::Dw || (p.vb && a.d % 4 == 0)) RG_LAUNCH((vocab_f32_k<KA, KB, E, true>), dim3(wgs), dim3(256), 0, s, a, p);
   else if constexpr (E != Prod::Dw) RG_LAUNCH((vocab_f32_k<KA, KB, E, false>), dim3(wgs), dim3(256), 0, s, a, p);
-  // dw's tiles are known here, dh's may be fewer
-  if (shared && k_shares(F32_SLOTS, E == Prod::Dw ? (int)tiles : 1, K, F32_LEAST, F32_LONGEST) > 1)
-  {
-    constexpr Prod S = shared ? E : Prod::Dh;
-    if (rows * p.N >= 262144) RG_LAUNCH((vocab_f32_shares_k<S, 1>), dim3((unsigned)rows, (p.N + 255) / 256), dim3(256), 0, s, a, p, bt);
-    else RG_LAUNCH((vocab_f32_shares_k<S, 8>), dim3((unsigned)rows, (p.N + 31) / 32), dim3(256), 0, s, a, p, bt);
-  }
+  if constexpr (shared) f32_shares<E>(a, p, bt, s);
 }
 
-static void vocab_products_f32(const VocabArgs& a, int which, hipStream_t s) {
+static bool w_aligned(const VocabArgs& a) { return (reinterpret_cast<uintptr_t>(a.w) & 15u) == 0 && a.ldw % 4 == 0; }
+
+static void vocab_logits_f32(const VocabArgs& a, bool keep, hipStream_t s) {
   const float* H = static_cast<const float*>(a.hc) + (long)a.row0 * a.dp;
-  const float* W = static_cast<const float*>(a.w);
+  const F32Product p{H, a.dp, static_cast<const float*>(a.w), a.ldw, 0, a.V, a.d, w_aligned(a), F32_SLOTS};
+  if (keep) go_f32<true, true, Prod::Logits>(a, p, a.bn == 32, s);
+  else go_f32<true, true, Prod::Stats>(a, p, a.bn == 32, s);
+}
+
+static void vocab_grads_f32(const VocabArgs& a, hipStream_t s) {
+  const float* H = static_cast<const float*>(a.hc) + (long)a.row0 * a.dp;
   const float* P = static_cast<const float*>(a.logits);
-  const bool vw = (reinterpret_cast<uintptr_t>(W) & 15u) == 0 && a.ldw % 4 == 0;
-  F32Product p{};
-  if (which < 2) {
-    p = F32Product{H, a.dp, W, a.ldw, 0, a.V, a.d, vw, 0};
-    if (which) go_f32<true, true, Prod::Logits>(a, p, a.bn == 32, s);
-    else go_f32<true, true, Prod::Stats>(a, p, a.bn == 32, s);
-  } else if (which == 2) {
-    p = F32Product{P, a.Vp, W, a.ldw, 0, a.d, a.V, vw, 0};
-    go_f32<true, false, Prod::Dh>(a, p, f32_small(a.n, a.d), s);
-  } else {
-    p = F32Product{P, a.Vp, H, a.dp, a.V, a.d, 0, true, 0};
-    go_f32<false, false, Prod::Dw>(a, p, f32_small(a.V, a.d), s);
+  const F32Product h{P, a.Vp, static_cast<const float*>(a.w), a.ldw, 0, a.d, a.V, w_aligned(a), F32_SLOTS};
+  const F32Product w{P, a.Vp, H, a.dp, a.V, a.d, 0, true, F32_SLOTS};
+  const bool sh = small_tiles(a.n, a.d), sw = small_tiles(a.V, a.d);
+  // Small products are bound by their latency: both in one launch where neither has shares (128 x 512, d 128: 10.8 us, one after the other 7.2 and 4.9, and a launch less)
+  const long th = f32_tiles(a.rows, a.d, 32), tw = f32_tiles(a.V, a.d, 32);
+  if (a.dh && a.dw && sh && sw && k_shares(F32_SLOTS, 1, a.V, F32_LEAST, F32_LONGEST) == 1 &&
+      k_shares(F32_SLOTS, (int)tw, a.rows, F32_LEAST, F32_LONGEST) == 1) {
+    RG_LAUNCH(vocab_f32_small_grads_k, dim3((unsigned)(th + tw)), dim3(256), 0, s, a, h, w, (int)th);
+    return;
   }
+  if (a.dh) go_f32<true, false, Prod::Dh>(a, h, sh, s);
+  if (a.dw) go_f32<false, false, Prod::Dw>(a, w, sw, s);
 }
 
 template <typename T>
@@ -676,19 +696,17 @@ static hipError_t vocab_t(VocabArgs a, hipStream_t s) {
     a.first = a.row0 == 0;
     a.last = a.row0 + a.R >= a.n;
     if constexpr (low) launch_vocab_logits_bf16(a, grads, s);
-    else vocab_products_f32(a, grads, s);
+    else vocab_logits_f32(a, grads, s);
     if (!grads) {
       RG_LAUNCH(vocab_rows_k, dim3(a.rows), dim3(256), 0, s, a);
       continue;
     }
     RG_LAUNCH(vocab_p_k<T>, dim3((unsigned)up(a.rows, 64), (a.Vp + P_COLS - 1) / P_COLS), dim3(256), 0, s, a);
-    if (a.dh) {
-      if constexpr (low) launch_vocab_dh_bf16(a, s);
-      else vocab_products_f32(a, 2, s);
-    }
-    if (a.dw) {
-      if constexpr (low) launch_vocab_dw_bf16(a, s);
-      else vocab_products_f32(a, 3, s);
+    if constexpr (low) {
+      if (a.dh) launch_vocab_dh_bf16(a, s);
+      if (a.dw) launch_vocab_dw_bf16(a, s);
+    } else {
+      vocab_grads_f32(a, s);
     }
   }
   return hipGetLastError();
