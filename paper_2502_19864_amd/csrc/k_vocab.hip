@@ -50,6 +50,19 @@ __global__ __launch_bounds__(256) void vocab_count_k(VocabArgs a) {
   if (threadIdx.x == 0) a.block_count[blockIdx.x] = v;
 }
 
+// a row whose pieces are not aligned, zeros from d to dp: eight elements in flight per lane
+template <typename T>
+__device__ __forceinline__ void copy_row(T* dst, const T* src, int d, int dp, int lane) {
+  for (int k0 = lane; k0 < dp; k0 += 512) {
+    T x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = src[min(k0 + j * 64, d - 1)];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (k0 + j * 64 < dp) dst[k0 + j * 64] = k0 + j * 64 < d ? x[j] : T(0);
+  }
+}
+
 // A stable compaction: hc[i] is the i-th row that counts, zeros past d; without labels, every row.  A workgroup
 // takes PICK_ROWS rows of h and counts the labels before them.  The results of rows that do not count are written here.
 template <typename T>
@@ -111,7 +124,7 @@ __global__ __launch_bounds__(256) void vocab_pick_k(VocabArgs a, bool wide) {
         }
       }
     } else {
-      for (int k = lane; k < a.dp; k += 64) dst[k] = k < a.d ? src[k] : T(0);
+      copy_row(dst, src, a.d, a.dp, lane);
     }
   }
 }
@@ -126,9 +139,9 @@ struct F32Product {
   const float* A; long lda;
   const float* B; long ldb;
   int M, N, K;     // M of dw, k of the logits and of dh; the others are the rows that count
-  bool vb;         // B's rows are 16-byte aligned (A's always are)
   int slots;       // dh, dw: workgroups of one round
 };
+typedef f32x4 f32x4_a4 __attribute__((aligned(4)));  // w may lie anywhere: a load of four floats asks for 4 bytes
 constexpr int F32_LEAST = 512, F32_LONGEST = 1 << 30;  // of k to a share; chains are cut in the kernels
 
 template <Prod E>
@@ -193,30 +206,28 @@ __device__ __forceinline__ void f32_epilogue(const VocabArgs& a, const F32Produc
 // 128 x 128 tiles, 32 k at a time: registers -> LDS, four waves of 64 x 64, two workgroups per CU.  LDS keeps [k][row], rows of odd k
 // turned by 32 columns, so that the two k of an MFMA lie in different banks.  The loop has no branch: rows and k past the ends read
 // the last ones again.  Such rows are not stored, and such k meet zeros of A: hc and P are padded with them to whole tiles of
-// 64.  VB: B's rows are 16-byte aligned and a multiple of four long.
+// 64.  A piece of B that reaches past the end of its row is read from where it ends there, and moved (1189 x 2786, d 4070: 309
+// us of logits, 300 at d 4096; single loads 508).  d >= 4.
 // 4096 x 16000, d 2048: 132 TF (a tile of 16 k with guarded loads: 115; torch.mm 154).
-template <bool KM, bool V4>
+// PADDED: A, which has whole tiles of k
+template <bool KM, bool PADDED>
 struct F32Operand {
-  const char* base;  // uniform: the tile's first element
+  const char* base;  // uniform: three elements before the tile's first
   long step;         // bytes per 32 k
   uint32_t off[4];   // of this thread's four pieces of four
-  int more[4];       // elements behind each piece's first that are its own (not V4)
+  int past;          // how far a piece was moved back to end with its row (not KM)
   uint32_t ld4;
   __device__ __forceinline__ void init(const float* X, long ld, int r0, int rows, int k0) {
     const int tid = threadIdx.x;
     ld4 = (uint32_t)ld * 4;
-    base = reinterpret_cast<const char*>(KM ? X + (long)r0 * ld + k0 : X + (long)k0 * ld + r0);
+    base = reinterpret_cast<const char*>((KM ? X + (long)r0 * ld + k0 : X + (long)k0 * ld + r0) - 3);
     step = KM ? 128 : ld * 128;
+    const int c = min((tid & 31) * 4, rows - 4 - r0);  // -3 at least
+    past = KM || PADDED ? 0 : (tid & 31) * 4 - c;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if constexpr (KM) {
-        off[i] = (uint32_t)min(tid & 127, rows - 1 - r0) * ld4 + ((tid >> 7) * 16 + 4 * i) * 4;
-        more[i] = 3;
-      } else {
-        const int c = min((tid & 31) * 4, rows - (V4 ? 4 : 1) - r0);
-        off[i] = (uint32_t)((tid >> 5) + 8 * i) * ld4 + c * 4;
-        more[i] = min(3, rows - 1 - r0 - c);
-      }
+      if constexpr (KM) off[i] = (uint32_t)min(tid & 127, rows - 1 - r0) * ld4 + ((tid >> 7) * 16 + 4 * i + 3) * 4;
+      else off[i] = (uint32_t)((tid >> 5) + 8 * i) * ld4 + (c + 3) * 4;
     }
   }
   // tile t from k0 on; left: k of it that there are
@@ -226,23 +237,19 @@ struct F32Operand {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t o = off[i];
-      int m = more[i];
-      if (left < 32) {
+      int move = past;
+      if (!PADDED && left < 32) {
         if constexpr (KM) {
-          const int k = (tid >> 7) * 16 + 4 * i;
-          o -= max(0, k - (V4 ? left - 4 : left - 1)) * 4;
-          m = max(0, min(3, left - 1 - k));
+          move = max(0, (tid >> 7) * 16 + 4 * i - (left - 4));
+          o -= move * 4;
         } else {
           o -= max(0, (tid >> 5) + 8 * i - (left - 1)) * ld4;
         }
       }
-      if constexpr (V4) {
-        v[i] = *reinterpret_cast<const f32x4*>(b + o);
-      } else {
-        v[i].x = *reinterpret_cast<const float*>(b + o);
-        v[i].y = *reinterpret_cast<const float*>(b + o + min(1, m) * 4);
-        v[i].z = *reinterpret_cast<const float*>(b + o + min(2, m) * 4);
-        v[i].w = *reinterpret_cast<const float*>(b + o + m * 4);
+      v[i] = *reinterpret_cast<const f32x4_a4*>(b + o);
+      if (!PADDED && (!KM || left < 32)) {
+        if (move & 2) v[i].x = v[i].z, v[i].y = v[i].w;
+        if (move & 1) v[i].x = v[i].y, v[i].y = v[i].z, v[i].z = v[i].w;
       }
     }
   }
@@ -268,7 +275,7 @@ __device__ __forceinline__ void f32_put(float* s, const f32x4 (&v)[4]) {
   }
 }
 
-template <bool KA, bool KB, Prod E, bool VB>
+template <bool KA, bool KB, Prod E>
 __global__ __launch_bounds__(256, 2) void vocab_f32_k(VocabArgs a, F32Product p) {
   constexpr int BT = 128, BK = 32, CP = BT + 4, LONG = 1024, TILE = BK * BT;
   __shared__ __attribute__((aligned(16))) float smem[BT * CP];
@@ -308,7 +315,7 @@ __global__ __launch_bounds__(256, 2) void vocab_f32_k(VocabArgs a, F32Product p)
   };
   f32x4 ra[4], rb[4];
   F32Operand<KA, true> oa;
-  F32Operand<KB, VB> ob;
+  F32Operand<KB, false> ob;
   auto fetch = [&](int t) {
     t = min(t, t1 - 1);
     oa.fetch(t - t0, 32, ra);
@@ -388,12 +395,12 @@ __device__ __forceinline__ void f32_small(const VocabArgs& a, const F32Product& 
   f32x16 acc, sum;
 #pragma unroll
   for (int r = 0; r < 16; ++r) acc[r] = sum[r] = 0.f;
-  auto load = [&](auto KM, const float* X, long ld, int r0, int rows, bool wide, int k, float (&v)[4]) {
+  auto load = [&](auto KM, const float* X, long ld, int r0, int rows, int k, float (&v)[4]) {
     const int r = r0 + l32;
     if constexpr (decltype(KM)::value) {
       const float* q = X + (long)min(r, rows - 1) * ld + k;
-      if (wide && k + 4 <= K) {
-        *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(q);
+      if (k + 4 <= K) {
+        *reinterpret_cast<f32x4*>(v) = *reinterpret_cast<const f32x4_a4*>(q);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = k + i < K ? q[i] : 0.f;
@@ -408,8 +415,8 @@ __device__ __forceinline__ void f32_small(const VocabArgs& a, const F32Product& 
     float fa[PF][4], fb[PF][4];
 #pragma unroll
     for (int q = 0; q < PF; ++q) {  // past K: zeros
-      load(std::integral_constant<bool, KA>{}, p.A, p.lda, m0, M, true, k0 + q * 32 + half * 4, fa[q]);
-      load(std::integral_constant<bool, KB>{}, p.B, p.ldb, n0, N, p.vb, k0 + q * 32 + half * 4, fb[q]);
+      load(std::integral_constant<bool, KA>{}, p.A, p.lda, m0, M, k0 + q * 32 + half * 4, fa[q]);
+      load(std::integral_constant<bool, KB>{}, p.B, p.ldb, n0, N, k0 + q * 32 + half * 4, fb[q]);
     }
 #pragma unroll
     for (int q = 0; q < PF; ++q)
@@ -581,8 +588,8 @@ __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
 // ---------------------------------------------------------------- launches
 static long up(long x, long m) { return (x + m - 1) / m * m; }
 
-// Whether the fp32 products take 32-wide tiles: where 128-wide ones leave most CUs idle
-static bool small_tiles(long rows, long cols) { return up(rows, 128) / 128 * (up(cols, 128) / 128) < 128; }
+// Whether the fp32 products take 32-wide tiles: where 128-wide ones leave most CUs idle, or read a row of w too short for them
+static bool small_tiles(long rows, long cols, int d) { return d < 4 || up(rows, 128) / 128 * (up(cols, 128) / 128) < 128; }
 constexpr int F32_SLOTS = 512;
 
 // The workspace: sizes, and the pointers into it where there is one
@@ -591,7 +598,7 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   const long es = low ? 2 : 4, np = up(a.n, 64);
   a.Vp = (int)up(a.V, 64);
   a.dp = (int)up(a.d, 64);
-  a.bn = low ? vocab_mm_bn(a.n, a.d, a.V) : small_tiles(a.n, a.V) ? 32 : 128;
+  a.bn = low ? vocab_mm_bn(a.n, a.d, a.V) : small_tiles(a.n, a.V, a.d) ? 32 : 128;
   a.few = low && !grads && vocab_few(a.n, a.d);
   a.tiles = a.few ? vocab_few_wgs(a.n, a.d) : (a.V + a.bn - 1) / a.bn;
   // rows at a time: 2 GiB of logits, 2^24 partial sums; whole tiles of rows
@@ -620,7 +627,7 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
     a.g_c = static_cast<float*>(take((size_t)a.n * 4));
     a.logits = take((size_t)a.R * a.Vp * es);
     a.shares = static_cast<float*>(take(low ? vocab_share_bytes(a.n, a.R, a.d, a.V)
-                                            : (size_t)F32_SLOTS * 4 * (small_tiles(a.n, a.d) && small_tiles(a.V, a.d) ? 1024 : 16384)));
+                                            : (size_t)F32_SLOTS * 4 * (small_tiles(a.n, a.d, a.d) && small_tiles(a.V, a.d, a.d) ? 1024 : 16384)));
     if (low && a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
     a.ld_acc = a.d;
   }
@@ -646,16 +653,13 @@ static void go_f32(const VocabArgs& a, const F32Product& p, bool small, hipStrea
   const long tiles = f32_tiles(E == Prod::Dw ? p.M : a.rows, p.N, bt);
   const unsigned wgs = (unsigned)(shared && tiles < F32_SLOTS ? F32_SLOTS : tiles);
   if (small) RG_LAUNCH((vocab_f32_small_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, p);
-  else if (E == Prod::Dw || (p.vb && a.d % 4 == 0)) RG_LAUNCH((vocab_f32_k<KA, KB, E, true>), dim3(wgs), dim3(256), 0, s, a, p);
-  else if constexpr (E != Prod::Dw) RG_LAUNCH((vocab_f32_k<KA, KB, E, false>), dim3(wgs), dim3(256), 0, s, a, p);
+  else RG_LAUNCH((vocab_f32_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, p);
   if constexpr (shared) f32_shares<E>(a, p, bt, s);
 }
 
-static bool w_aligned(const VocabArgs& a) { return (reinterpret_cast<uintptr_t>(a.w) & 15u) == 0 && a.ldw % 4 == 0; }
-
 static void vocab_logits_f32(const VocabArgs& a, bool keep, hipStream_t s) {
   const float* H = static_cast<const float*>(a.hc) + (long)a.row0 * a.dp;
-  const F32Product p{H, a.dp, static_cast<const float*>(a.w), a.ldw, 0, a.V, a.d, w_aligned(a), F32_SLOTS};
+  const F32Product p{H, a.dp, static_cast<const float*>(a.w), a.ldw, 0, a.V, a.d, F32_SLOTS};
   if (keep) go_f32<true, true, Prod::Logits>(a, p, a.bn == 32, s);
   else go_f32<true, true, Prod::Stats>(a, p, a.bn == 32, s);
 }
@@ -663,9 +667,9 @@ static void vocab_logits_f32(const VocabArgs& a, bool keep, hipStream_t s) {
 static void vocab_grads_f32(const VocabArgs& a, hipStream_t s) {
   const float* H = static_cast<const float*>(a.hc) + (long)a.row0 * a.dp;
   const float* P = static_cast<const float*>(a.logits);
-  const F32Product h{P, a.Vp, static_cast<const float*>(a.w), a.ldw, 0, a.d, a.V, w_aligned(a), F32_SLOTS};
-  const F32Product w{P, a.Vp, H, a.dp, a.V, a.d, 0, true, F32_SLOTS};
-  const bool sh = small_tiles(a.n, a.d), sw = small_tiles(a.V, a.d);
+  const F32Product h{P, a.Vp, static_cast<const float*>(a.w), a.ldw, 0, a.d, a.V, F32_SLOTS};
+  const F32Product w{P, a.Vp, H, a.dp, a.V, a.d, 0, F32_SLOTS};
+  const bool sh = small_tiles(a.n, a.d, a.d), sw = small_tiles(a.V, a.d, a.d);
   // Small products are bound by their latency: both in one launch where neither has shares (128 x 512, d 128: 10.8 us, one after the other 7.2 and 4.9, and a launch less)
   const long th = f32_tiles(a.rows, a.d, 32), tw = f32_tiles(a.V, a.d, 32);
   if (a.dh && a.dw && sh && sw && k_shares(F32_SLOTS, 1, a.V, F32_LEAST, F32_LONGEST) == 1 &&

@@ -215,6 +215,8 @@ VOCAB = [  # dtype, rows, d, vocab, share of rows that count
     ("bf16", 32, 4096, 5000, 1.0), ("bf16", 32, 64, 20000, 0.7), ("bf16", 9, 1000, 100000, 1.0), ("bf16", 4500, 4096, 1000, 1.0),
     ("f32", 2100, 1000, 300, 1.0), ("f32", 1500, 1032, 1400, 1.0), ("f32", 1200, 1100, 2000, 1.0), ("bf16", 16, 2048, 17000, 1.0),
     ("bf16", 20, 2048, 17000, 0.9), ("bf16", 20, 512, 33000, 1.0), ("bf16", 20, 2048, 3000, 1.0), ("bf16", 1000, 72, 16000, 1.0), ("bf16", 2, 4096, 40000, 1.0), ("bf16", 1500, 520, 300, 0.8), ("bf16", 40, 16, 70000, 1.0),
+    ("f32", 1500, 1, 1600, 1.0), ("f32", 1500, 3, 1601, 0.9), ("f32", 1500, 4, 1602, 1.0), ("f32", 1501, 6, 1603, 1.0), ("f32", 17000, 3, 41, 1.0), ("f32", 17000, 7, 42, 0.8),
+    ("f32", 1400, 2051, 1411, 1.0), ("f32", 1300, 1022, 1999, 0.7), ("f32", 10, 1157, 2562, 1.0),
 ]
 
 
@@ -284,6 +286,20 @@ def test_vocab_next_takes_the_lowest_of_equals(dtype, n):
     zero = ops.vocab_next(torch.zeros_like(h), w)
     assert (zero[0] == 0).all()
     R.check("logprob", zero[1], torch.full((n,), -math.log(3000), device="cuda", dtype=torch.float64), torch.full((n,), 64 * R.E * 8, device="cuda", dtype=torch.float64))
+
+
+@pytest.mark.parametrize("n,d,V", [(1500, 133, 1502), (1500, 4, 1501), (40, 133, 300), (17000, 130, 40)])
+def test_f32_vocab_rows_from_any_address(n, d, V):
+    """Four floats at a time or not, the same products in the same order."""
+    import torch
+    from paper_2502_19864_amd import operators as ops
+    h, w, labels, dloss = head("f32", n, d, V, 0.9, seed=d)
+    want = ops.vocab_ce_train(h, w, labels, dloss)
+    for pad in (1, 2, 7):
+        wide = [torch.full((x.shape[0], d + pad + 1), math.nan, device="cuda") for x in (h, w)]
+        hs, ws = (x[:, pad:pad + d].copy_(y) for x, y in zip(wide, (h, w)))
+        assert all(torch.equal(a, b) for a, b in zip(ops.vocab_ce_train(hs, ws, labels, dloss), want))
+        assert all(torch.equal(a, b) for a, b in zip(ops.vocab_next(hs, ws), ops.vocab_next(h, w)))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
