@@ -84,8 +84,8 @@ __global__ __launch_bounds__(256) void rotary_k(RotaryArgs a, int rows_wg) {
   }
 }
 
-static bool wide_ok(const View& v, int es, int ve) {
-  return v.p == nullptr || ((reinterpret_cast<uintptr_t>(v.p) & 15u) == 0 && ((v.b | v.t | v.h) * es & 15) == 0 && ve);
+static bool wide_ok(const View& v, int es) {
+  return v.p == nullptr || ((reinterpret_cast<uintptr_t>(v.p) & 15u) == 0 && ((v.b | v.t | v.h) * es & 15) == 0);
 }
 
 template <typename T, int VE>
@@ -96,8 +96,8 @@ static hipError_t rotary_t(const RotaryArgs& a, hipStream_t s) {
   if (rows_wg < 1) rows_wg = 1;
   const long wgs = (rows + rows_wg - 1) / rows_wg;
   const int heads = a.H + a.Hkv, split = wgs >= 256 ? 1 : heads < 8 ? heads : 8;
-  const bool wide = VE > 1 && a.pairs % VE == 0 && a.dh % VE == 0 && wide_ok(a.q, sizeof(T), VE) && wide_ok(a.k, sizeof(T), VE) &&
-                    wide_ok(a.oq, sizeof(T), VE) && wide_ok(a.ok, sizeof(T), VE);
+  const bool wide = VE > 1 && a.pairs % VE == 0 && a.dh % VE == 0 && wide_ok(a.q, sizeof(T)) && wide_ok(a.k, sizeof(T)) &&
+                    wide_ok(a.oq, sizeof(T)) && wide_ok(a.ok, sizeof(T));
   if (wide) RG_LAUNCH((rotary_k<T, VE>), dim3((unsigned)wgs, split), dim3(256), 0, s, a, rows_wg);
   else RG_LAUNCH((rotary_k<T, 1>), dim3((unsigned)wgs, split), dim3(256), 0, s, a, rows_wg);
   return hipGetLastError();

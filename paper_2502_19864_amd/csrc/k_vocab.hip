@@ -139,10 +139,15 @@ struct F32Product {
   const float* A; long lda;
   const float* B; long ldb;
   int M, N, K;     // M of dw, k of the logits and of dh; the others are the rows that count
-  int slots;       // dh, dw: workgroups of one round
 };
 typedef f32x4 f32x4_a4 __attribute__((aligned(4)));  // w may lie anywhere: a load of four floats asks for 4 bytes
-constexpr int F32_LEAST = 512, F32_LONGEST = 1 << 30;  // of k to a share; chains are cut in the kernels
+// Shares of the k of bt x bt tiles of dh or dw, for 512 workgroups, two to a CU.  Wide tiles that come to little more than one
+// per CU take three each, as most CUs would wait for those with two (1189 x 4070 of 2786: 289 us and 11 more to add them up, 400 unshared).
+constexpr int F32_SLOTS = 512;
+__host__ __device__ inline int f32_splits(int bt, int tiles, int K) {
+  const int slots = bt == 128 && tiles > 256 && tiles * 3 <= 2 * F32_SLOTS ? 2 * F32_SLOTS : F32_SLOTS;
+  return k_shares(slots, tiles, K, 512, 1 << 30);  // chains are cut in the kernels
+}
 
 template <Prod E>
 __device__ __forceinline__ void f32_gradient(const VocabArgs& a, int m, int n, float v) {
@@ -285,7 +290,7 @@ __global__ __launch_bounds__(256, 2) void vocab_f32_k(VocabArgs a, F32Product p)
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
   const int tn = (N + BT - 1) / BT, tiles = (M + BT - 1) / BT * tn;
   const int Kall = E == Prod::Dw ? cnt : p.K;
-  const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? k_shares(p.slots, tiles, Kall, F32_LEAST, F32_LONGEST) : 1;
+  const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? f32_splits(BT, tiles, Kall) : 1;
   if ((int)blockIdx.x >= tiles * splits) return;
   const int split = blockIdx.x / tiles;
   int tm, tc;
@@ -386,7 +391,7 @@ __device__ __forceinline__ void f32_small(const VocabArgs& a, const F32Product& 
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
   const int tn = (N + BT - 1) / BT, tiles = (M + BT - 1) / BT * tn;
   const int Kall = E == Prod::Dw ? cnt : p.K;
-  const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? k_shares(p.slots, tiles, Kall, F32_LEAST, F32_LONGEST) : 1;
+  const int splits = (E == Prod::Dh || E == Prod::Dw) && tiles ? f32_splits(BT, tiles, Kall) : 1;
   if (wg >= tiles * splits) return;
   const int split = wg / tiles, tile = wg - split * tiles;
   const int m0 = tile / tn * BT, n0 = tile % tn * BT;
@@ -460,7 +465,7 @@ __global__ __launch_bounds__(256) void vocab_f32_shares_k(VocabArgs a, F32Produc
   const int cnt = piece_rows(a), M = E == Prod::Dw ? p.M : cnt, K = E == Prod::Dw ? cnt : p.K;
   const int m = blockIdx.x, lane = threadIdx.x % (256 / G), g = threadIdx.x / (256 / G), n = blockIdx.y * (256 / G) + lane;
   if (m >= M) return;
-  const int tn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * tn, splits = k_shares(p.slots, tiles, K, F32_LEAST, F32_LONGEST);
+  const int tn = (p.N + bt - 1) / bt, tiles = (M + bt - 1) / bt * tn, splits = f32_splits(bt, tiles, K);
   if (splits == 1) return;
   float v = 0.f;
   if (n < p.N) {
@@ -588,9 +593,31 @@ __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
 // ---------------------------------------------------------------- launches
 static long up(long x, long m) { return (x + m - 1) / m * m; }
 
-// Whether the fp32 products take 32-wide tiles: where 128-wide ones leave most CUs idle, or read a row of w too short for them
-static bool small_tiles(long rows, long cols, int d) { return d < 4 || up(rows, 128) / 128 * (up(cols, 128) / 128) < 128; }
-constexpr int F32_SLOTS = 512;
+static long f32_tiles(long rows, long cols, int bt) { return (up(rows, bt) / bt) * (up(cols, bt) / bt); }
+
+// Whether the fp32 products take 32-wide tiles: where 128-wide ones, with the shares of their k, leave most CUs idle (dh of 2048 x 768, 5000
+// classes: 321 us by 32, 159 + 6 by 128 in shares), where they would be half empty or less (32 x 30000, d 2048: logits 124 us and 163,
+// dh 78 and 152; 20 x 40000, d 256: logits 18 and 47), or where a row of w is too short for them
+static bool small_logits(const VocabArgs& a) { return a.d < 4 || a.n <= 64 || f32_tiles(a.n, a.V, 128) < 128; }
+static bool small_grad(long rows, int d, int K) {
+  const long tiles = f32_tiles(rows, d, 128);
+  return d <= 64 || rows <= 64 || tiles * (tiles < 128 ? f32_splits(128, (int)tiles, K) : 1) < 128;
+}
+static bool small_dh(const VocabArgs& a) { return small_grad(a.n, a.d, a.V); }
+static bool small_dw(const VocabArgs& a) { return small_grad(a.V, a.d, a.n); }
+// workgroups that dh or dw may have, whichever rows count
+static long f32_wgs(int bt, long tiles) {
+  const long slots = bt == 128 && tiles > 256 ? 2 * F32_SLOTS : F32_SLOTS;
+  return tiles > slots ? tiles : slots;
+}
+static size_t f32_share_bytes(const VocabArgs& a) {
+  auto bytes = [](bool small, long rows, int d) {
+    const int bt = small ? 32 : 128;
+    return (size_t)(bt == 128 && f32_tiles(rows, d, bt) > 256 ? 2 * F32_SLOTS : F32_SLOTS) * bt * bt * 4;
+  };
+  const size_t h = bytes(small_dh(a), a.n, a.d), w = bytes(small_dw(a), a.V, a.d);
+  return h > w ? h : w;
+}
 
 // The workspace: sizes, and the pointers into it where there is one
 size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
@@ -598,7 +625,7 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   const long es = low ? 2 : 4, np = up(a.n, 64);
   a.Vp = (int)up(a.V, 64);
   a.dp = (int)up(a.d, 64);
-  a.bn = low ? vocab_mm_bn(a.n, a.d, a.V) : small_tiles(a.n, a.V, a.d) ? 32 : 128;
+  a.bn = low ? vocab_mm_bn(a.n, a.d, a.V) : small_logits(a) ? 32 : 128;
   a.few = low && !grads && vocab_few(a.n, a.d);
   a.tiles = a.few ? vocab_few_wgs(a.n, a.d) : (a.V + a.bn - 1) / a.bn;
   // rows at a time: 2 GiB of logits, 2^24 partial sums; whole tiles of rows
@@ -626,22 +653,19 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   if (grads) {
     a.g_c = static_cast<float*>(take((size_t)a.n * 4));
     a.logits = take((size_t)a.R * a.Vp * es);
-    a.shares = static_cast<float*>(take(low ? vocab_share_bytes(a.n, a.R, a.d, a.V)
-                                            : (size_t)F32_SLOTS * 4 * (small_tiles(a.n, a.d, a.d) && small_tiles(a.V, a.d, a.d) ? 1024 : 16384)));
+    a.shares = static_cast<float*>(take(low ? vocab_share_bytes(a.n, a.R, a.d, a.V) : f32_share_bytes(a)));
     if (low && a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
     a.ld_acc = a.d;
   }
   return at;
 }
 
-static long f32_tiles(long rows, long cols, int bt) { return (up(rows, bt) / bt) * (up(cols, bt) / bt); }
-
 // sums of shares, where there may be any: dw's tiles are known here, dh's may be fewer
 template <Prod E>
 static void f32_shares(const VocabArgs& a, const F32Product& p, int bt, hipStream_t s) {
   const long rows = E == Prod::Dw ? p.M : a.rows;
   const int K = E == Prod::Dw ? a.rows : p.K;
-  if (k_shares(F32_SLOTS, E == Prod::Dw ? (int)f32_tiles(rows, p.N, bt) : 1, K, F32_LEAST, F32_LONGEST) == 1) return;
+  if (f32_splits(bt, E == Prod::Dw ? (int)f32_tiles(rows, p.N, bt) : 1, K) == 1) return;
   if (rows * p.N >= 262144) RG_LAUNCH((vocab_f32_shares_k<E, 1>), dim3((unsigned)rows, (p.N + 255) / 256), dim3(256), 0, s, a, p, bt);
   else RG_LAUNCH((vocab_f32_shares_k<E, 8>), dim3((unsigned)rows, (p.N + 31) / 32), dim3(256), 0, s, a, p, bt);
 }
@@ -651,7 +675,7 @@ static void go_f32(const VocabArgs& a, const F32Product& p, bool small, hipStrea
   constexpr bool shared = E == Prod::Dh || E == Prod::Dw;
   const int bt = small ? 32 : 128;
   const long tiles = f32_tiles(E == Prod::Dw ? p.M : a.rows, p.N, bt);
-  const unsigned wgs = (unsigned)(shared && tiles < F32_SLOTS ? F32_SLOTS : tiles);
+  const unsigned wgs = (unsigned)(shared ? f32_wgs(bt, tiles) : tiles);
   if (small) RG_LAUNCH((vocab_f32_small_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, p);
   else RG_LAUNCH((vocab_f32_k<KA, KB, E>), dim3(wgs), dim3(256), 0, s, a, p);
   if constexpr (shared) f32_shares<E>(a, p, bt, s);
@@ -659,7 +683,7 @@ static void go_f32(const VocabArgs& a, const F32Product& p, bool small, hipStrea
 
 static void vocab_logits_f32(const VocabArgs& a, bool keep, hipStream_t s) {
   const float* H = static_cast<const float*>(a.hc) + (long)a.row0 * a.dp;
-  const F32Product p{H, a.dp, static_cast<const float*>(a.w), a.ldw, 0, a.V, a.d, F32_SLOTS};
+  const F32Product p{H, a.dp, static_cast<const float*>(a.w), a.ldw, 0, a.V, a.d};
   if (keep) go_f32<true, true, Prod::Logits>(a, p, a.bn == 32, s);
   else go_f32<true, true, Prod::Stats>(a, p, a.bn == 32, s);
 }
@@ -667,13 +691,13 @@ static void vocab_logits_f32(const VocabArgs& a, bool keep, hipStream_t s) {
 static void vocab_grads_f32(const VocabArgs& a, hipStream_t s) {
   const float* H = static_cast<const float*>(a.hc) + (long)a.row0 * a.dp;
   const float* P = static_cast<const float*>(a.logits);
-  const F32Product h{P, a.Vp, static_cast<const float*>(a.w), a.ldw, 0, a.d, a.V, F32_SLOTS};
-  const F32Product w{P, a.Vp, H, a.dp, a.V, a.d, 0, F32_SLOTS};
-  const bool sh = small_tiles(a.n, a.d, a.d), sw = small_tiles(a.V, a.d, a.d);
+  const F32Product h{P, a.Vp, static_cast<const float*>(a.w), a.ldw, 0, a.d, a.V};
+  const F32Product w{P, a.Vp, H, a.dp, a.V, a.d, 0};
+  const bool sh = small_dh(a), sw = small_dw(a);
   // Small products are bound by their latency: both in one launch where neither has shares (128 x 512, d 128: 10.8 us, one after the other 7.2 and 4.9, and a launch less)
   const long th = f32_tiles(a.rows, a.d, 32), tw = f32_tiles(a.V, a.d, 32);
-  if (a.dh && a.dw && sh && sw && k_shares(F32_SLOTS, 1, a.V, F32_LEAST, F32_LONGEST) == 1 &&
-      k_shares(F32_SLOTS, (int)tw, a.rows, F32_LEAST, F32_LONGEST) == 1) {
+  if (a.dh && a.dw && sh && sw && f32_splits(32, 1, a.V) == 1 &&
+      f32_splits(32, (int)tw, a.rows) == 1) {
     RG_LAUNCH(vocab_f32_small_grads_k, dim3((unsigned)(th + tw)), dim3(256), 0, s, a, h, w, (int)th);
     return;
   }
