@@ -526,7 +526,7 @@ __global__ __launch_bounds__(256) void vocab_rows_k(VocabArgs a) {
   a.lse[row] = p.m + log_l;
 }
 
-// Loss and lse of a row, and its P in the place of the logits, rounded once to the storage type; zeros past V and in the rows
+// Loss and lse of a row, and its P in the place of the logits, rounded once to the storage type (few rows: in two parts); zeros past V and in the rows
 // up to a multiple of 64.  A workgroup takes 16384 columns of one row and joins the row's tiles by itself.
 // With bf16 tensors the logits come in fp16, as s - (the largest of their tile, which is in part): off by 2^-11 of that difference
 // at most, so P by 2^-11 (m - s) of itself.  What is large of P has s near m and keeps its digits; P a thousandth of its tile's
@@ -543,7 +543,15 @@ __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
   T* p = static_cast<T*>(a.logits) + at;
   auto store = [&](int v, const float (&x)[8]) {
     if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<bf16x8*>(p + v) = pack_frag(x);
+      const bf16x8 hi = pack_frag(x);
+      *reinterpret_cast<bf16x8*>(p + v) = hi;
+      if (two_parts(cnt)) {
+        float y[8];
+        unpack_frag(hi, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = x[e] - y[e];
+        *reinterpret_cast<bf16x8*>(p + (long)TWO_PARTS * a.Vp + v) = pack_frag(y);
+      }
     } else {
       St<T>::st4(p, v, x);
       St<T>::st4(p, v + 4, x + 4);
@@ -652,7 +660,7 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   }
   if (grads) {
     a.g_c = static_cast<float*>(take((size_t)a.n * 4));
-    a.logits = take((size_t)a.R * a.Vp * es);
+    a.logits = take((size_t)(low && a.R < 2 * TWO_PARTS ? 2 * TWO_PARTS : a.R) * a.Vp * es);
     a.shares = static_cast<float*>(take(low ? vocab_share_bytes(a.n, a.R, a.d, a.V) : f32_share_bytes(a)));
     if (low && a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
     a.ld_acc = a.d;

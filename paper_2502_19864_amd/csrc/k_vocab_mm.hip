@@ -152,9 +152,10 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
   const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int cnt = __builtin_amdgcn_readfirstlane(piece_rows(a));
   const int M = E == Prod::Dw ? p.M : cnt, N = p.N;
-  const int K = E == Prod::Dw ? cnt : p.K;
-  const int ntm = (M + BM - 1) / BM, ntn = (N + BN - 1) / BN, tiles = ntm * ntn;
   constexpr bool SHARED = E == Prod::Dh || E == Prod::Dw;
+  const bool two = SHARED && two_parts(cnt);
+  const int K = E == Prod::Dw ? (two ? 2 * TWO_PARTS : cnt) : p.K;
+  const int ntm = (M + BM - 1) / BM, ntn = (N + BN - 1) / BN, tiles = ntm * ntn;
   const int splits = SHARED && tiles ? __builtin_amdgcn_readfirstlane(k_shares(p.slots, tiles, K, MM_LEAST, MM_LONGEST)) : 1;
   const int nk_all = (K + BK - 1) / BK;
   int m0 = 0, n0 = 0, split = 0, kt0 = 0, nk = 0, tile = 0;
@@ -177,15 +178,16 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
   // part q of `of` of k-tile kt's DMA instructions.  A (hc in the logits, P) has zeros up to whole k-tiles; B has not.
   auto issue = [&](int kt, int slot, int q, int of) {
     const uint32_t l0 = lds_addr(smem) + slot * STAGE;
-    const int left = min(BK, K - (kt0 + kt) * BK);
+    const bool again = E == Prod::Dw && two;  // the second part meets the same rows of hc
+    const int kb = again ? 0 : kt0 + kt, left = again ? cnt : min(BK, K - kb * BK);
 #pragma unroll
     for (int i = LPT * q / of; i < LPT * (q + 1) / of; ++i) {
       if (i < OA::L) oa.dma(i, kt0 + kt, BK, l0, wave, wave_u, lane);
-      else ob.dma(i - OA::L, kt0 + kt, left, l0 + BM * BK * 2, wave, wave_u, lane);
+      else ob.dma(i - OA::L, kb, left, l0 + BM * BK * 2, wave, wave_u, lane);
     }
   };
   auto begin = [&] {
-    oa.init(p.A, p.lda, m0, M, wave, lane);
+    oa.init(p.A, p.lda, m0, E == Prod::Dh && two ? 2 * TWO_PARTS : M, wave, lane);
     ob.init(p.B, p.ldb, n0, N, wave, lane);
 #pragma unroll
     for (int t = 0; t < NS; ++t)
@@ -249,6 +251,32 @@ __global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabPro
     const bool more = locate(g);
     __builtin_amdgcn_s_waitcnt(0xF | (0x7 << 4) | (0x3 << 14));  // lgkmcnt == 0
     wg_barrier();  // every wave is done with the stages
+    if constexpr (E == Prod::Dh) {
+      static_assert(TM == TWO_PARTS && TWO_PARTS == BK && WN * TM * TN * 4 <= NS * STAGE, "a wave's rows are a part");
+      if (two) {  // the second part's sums to the first's
+        float* x = reinterpret_cast<float*>(smem) + wn * TM * TN + lane;
+        if (wm == 1) {
+#pragma unroll
+          for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) x[((i * FN + j) * 16 + r) * 64] = acc[i][j][r];
+        }
+        __builtin_amdgcn_s_waitcnt(0xF | (0x7 << 4) | (0x3 << 14));  // lgkmcnt == 0
+        wg_barrier();
+        if (wm == 0) {
+#pragma unroll
+          for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) acc[i][j][r] += x[((i * FN + j) * 16 + r) * 64];
+        }
+        __builtin_amdgcn_s_waitcnt(0xF | (0x7 << 4) | (0x3 << 14));
+        wg_barrier();
+      }
+    }
     if (more) begin();
 
     // Lane l holds of each 32x32 block row l % 32, columns 8 g + 4 (l / 32) + 0..3, g = 0..3.

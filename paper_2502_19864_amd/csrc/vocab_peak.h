@@ -42,6 +42,13 @@ __device__ __forceinline__ float dloss_unit(const VocabArgs& a) {
   return g >= 0x1p-40f && g <= 0x1p40f ? g : 1.f;
 }
 
+// With bf16 tensors P is rounded to bf16, and what is lost is a fair sum over many rows.  Over few it need not be: a row whose two likeliest
+// classes have nearly the same w leaves little of dh = P w but P's roundings (4 rows, one counts, 196 classes, d 8: 0.0057 off float64, the
+// rounding of dh itself 0.0017).  So where at most 64 rows of a piece count, P is kept in two parts, the second in the 64 rows
+// below, which the products' tiles have empty then: rows of A in dh, k in dw.
+constexpr int TWO_PARTS = 64;
+__device__ __forceinline__ bool two_parts(int cnt) { return cnt > 0 && cnt <= TWO_PARTS; }
+
 // Workgroups that share the k of a tile: where the tiles of the rows that count leave CUs idle, at least `least` of k to each, and
 // never more than `longest`, the chain of additions in the matrix unit that a sum's precision allows
 __host__ __device__ inline int k_shares(int slots, int tiles, int K, int least, int longest) {

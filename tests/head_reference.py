@@ -73,6 +73,7 @@ def vocab(h, w, labels, dloss=None):
     up = u if h.dtype is torch.bfloat16 else 0.0  # of P on its way into a product
     n, V, d = h.shape[0], w.shape[0], h.shape[1]
     at = ((labels >= 0) & (labels < V)).nonzero()[:, 0]
+    up = up * up if at.numel() <= 64 else up  # two parts
     H, W, lab = h[at].double(), w.double(), labels[at].long()[:, None]
     s, A = H @ W.T, H.abs() @ W.abs().T
     es = 8 * math.sqrt(d) * E * A
