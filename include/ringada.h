@@ -520,8 +520,12 @@ ringada_status ringada_vocab_plan(const ringada_vocab_desc* desc, size_t* forwar
 /* Softmax cross entropy of the logits s = h w^T, and its gradients in the same call:
  *   lse = log sum exp s,  loss = lse - s[label],  P = dloss (softmax(s) - onehot(label)),  dh = P w,  dw = P^T h.
  * A row that does not count has loss 0, lse 0 and a zero row in dh; its h and dloss are read into nothing, whatever they
- * hold.  Logits, softmax and sums are fp32.  With bf16 tensors the logits wait for their row's lse in fp16, as their distance
- * to the largest of 64 or 128 (off by 2^-11 of it), and P is rounded to bf16 on its way into the products (of at most 64 rows that count: to two bf16, 2^-16 of it), in units of the first counted row's |dloss| (where that is within 2^-40 and 2^40: entries of dloss may be up to 2^80 then).  An infinity or NaN in a row that counts gives NaN in it, and in dw.  No output may overlap
+ * hold.  Logits, softmax and sums are fp32.  With bf16 tensors:
+ *  - the logits wait for their row's lse in fp16, as their distance to the largest of 64 or 128 (off by 2^-11 of it);
+ *  - P is rounded to bf16 on its way into the products; of at most 64 rows that count, to two bf16, which leaves 2^-16 of it;
+ *  - P is in units of the first counted row's |dloss|, where that is within 2^-40 and 2^40: entries of dloss may be up to 2^80
+ *    then.
+ * An infinity or NaN in a row that counts gives NaN in it, and in dw.  No output may overlap
  * anything else.  Every sum has a fixed order: the same inputs give the same bits. */
 ringada_status ringada_vocab_ce(void* stream, const ringada_vocab_desc* desc, const ringada_vocab_tensors* t,
                                 void* workspace, size_t workspace_bytes);

@@ -9,6 +9,8 @@
 // 10^5 times, which leaves fp32 no digit of the angle's place in the turn.  The turns are counted in 64 bits,
 // the whole ones dropped, and only the rest rounded.  That costs a few 64-bit operations per row and pair, shared by all
 // heads: a workgroup forms its rows' (cos, sin) once, in LDS.
+//
+// Bound by memory: 2 x 4097 rows of 16 + 16 heads of 128 in bf16 take 26 us each way, 5.1 TB/s.
 #include "common.h"
 #include "kernels.h"
 
