@@ -372,6 +372,53 @@ def test_vocab_strides(dtype):
         assert all(torch.equal(a.reshape(b.shape), b) for a, b in zip(lead, base))
 
 
+@pytest.mark.parametrize("dtype,n,V", [("bf16", 5, 1100), ("bf16", 40, 1100), ("bf16", 300, 1100), ("f32", 20, 700), ("f32", 3000, 700)])
+def test_vocab_rows_far_apart(dtype, n, V):
+    """The largest row strides: w and dw span more than 2^32 bytes, their tiles almost as much."""
+    import torch
+    from paper_2502_19864_amd import operators as ops
+    d, ld = 264, 1 << 22
+    h, w, labels, dloss = head(dtype, n, d, V, 0.9)
+    far = lambda rows: torch.empty((rows - 1) * ld + d, dtype=h.dtype, device="cuda").as_strided((rows, d), (ld, 1))
+    w2, dw2 = far(V).copy_(w), far(V)
+    got, want = ops.vocab_ce_train(h, w2, labels, dloss, dw=dw2), ops.vocab_ce_train(h, w, labels, dloss)
+    assert got[3] is dw2 and all(torch.equal(a, b) for a, b in zip(got, want))
+    assert all(torch.equal(a, b) for a, b in zip(ops.vocab_ce_forward(h, w2, labels), ops.vocab_ce_forward(h, w, labels)))
+    assert all(torch.equal(a, b) for a, b in zip(ops.vocab_next(h, w2), ops.vocab_next(h, w)))
+    if n <= 300:
+        h2, dh2 = far(n).copy_(h), far(n)
+        got = ops.vocab_ce_train(h2, w, labels, dloss, dh=dh2)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype,n,d,V,counted", [c for c in VOCAB if c[1] * c[3] < 1 << 25][::2] + [("bf16", 700, 72, 900, 0.05), ("bf16", 90, 72, 900, 0.0)])
+def test_vocab_workspace_may_hold_anything(dtype, n, d, V, counted):
+    import torch
+    from paper_2502_19864_amd import binding as B
+    from paper_2502_19864_amd import operators as ops
+    h, w, labels, dloss = head(dtype, n, d, V, counted)
+    want, scored, nexts = ops.vocab_ce_train(h, w, labels, dloss), ops.vocab_ce_forward(h, w, labels), ops.vocab_next(h, w)
+    desc = B.VocabDesc(B.BF16 if dtype == "bf16" else B.F32, n, d, V)
+    sizes, stream = B.ringada_vocab_plan(desc), torch.cuda.current_stream().cuda_stream
+    hr, wr = B.Rows(h.data_ptr(), d), B.Rows(w.data_ptr(), d)
+    for fill in (255, 127):
+        loss, lse, dh, dw = (torch.full_like(t, 3) for t in want)
+        ws = torch.full((sizes[1],), fill, dtype=torch.uint8, device="cuda")
+        t = B.VocabTensors(hr, wr, labels.data_ptr(), loss.data_ptr(), lse.data_ptr(), dloss.data_ptr(), B.Rows(dh.data_ptr(), d),
+                           B.Rows(dw.data_ptr(), d))
+        B.ringada_vocab_ce(stream, desc, t, ws, sizes[1])
+        assert all(torch.equal(a, b) for a, b in zip((loss, lse, dh, dw), want))
+        loss, lse = (torch.full_like(t, 3) for t in scored)
+        ws = torch.full((sizes[0],), fill, dtype=torch.uint8, device="cuda")
+        t = B.VocabTensors(hr, wr, labels.data_ptr(), loss.data_ptr(), lse.data_ptr(), None, B.Rows(0, 0), B.Rows(0, 0))
+        B.ringada_vocab_ce(stream, desc, t, ws, sizes[0])
+        assert all(torch.equal(a, b) for a, b in zip((loss, lse), scored))
+        token, logprob = (torch.full_like(t, 3) for t in nexts)
+        ws = torch.full((sizes[2],), fill, dtype=torch.uint8, device="cuda")
+        B.ringada_vocab_next(stream, desc, hr, wr, token, logprob, ws, sizes[2])
+        assert torch.equal(token, nexts[0]) and torch.equal(logprob, nexts[1])
+
+
 def test_vocab_gradients_one_at_a_time():
     """dw without dh, through the C names; of rows with one dloss, several, and none in the first."""
     import torch
