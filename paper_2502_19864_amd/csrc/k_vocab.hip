@@ -738,12 +738,8 @@ static hipError_t vocab_t(VocabArgs a, hipStream_t s) {
       continue;
     }
     RG_LAUNCH(vocab_p_k<T>, dim3((unsigned)up(a.rows, 64), (a.Vp + P_COLS - 1) / P_COLS), dim3(256), 0, s, a);
-    if constexpr (low) {
-      if (a.dh) launch_vocab_dh_bf16(a, s);
-      if (a.dw) launch_vocab_dw_bf16(a, s);
-    } else {
-      vocab_grads_f32(a, s);
-    }
+    if constexpr (low) launch_vocab_grads_bf16(a, s);
+    else vocab_grads_f32(a, s);
   }
   return hipGetLastError();
 }

@@ -279,8 +279,7 @@ bool vocab_few(int rows, int d);         // whether rows are few enough to read 
 int vocab_few_wgs(int rows, int d);
 void launch_vocab_few_bf16(const VocabArgs& a, hipStream_t s);
 void launch_vocab_logits_bf16(const VocabArgs& a, bool keep, hipStream_t s);
-void launch_vocab_dh_bf16(const VocabArgs& a, hipStream_t s);
-void launch_vocab_dw_bf16(const VocabArgs& a, hipStream_t s);
+void launch_vocab_grads_bf16(const VocabArgs& a, hipStream_t s);
 hipError_t launch_vocab(int dtype, const VocabArgs& a, hipStream_t s);
 
 // ---------------------------------------------------------------- norms with their gradients (k_norm.hip)
