@@ -512,7 +512,7 @@ typedef struct {
 
 /* Host only.  Bytes of the workspaces of ringada_vocab_ce without and with gradients, and of ringada_vocab_next.
  * The logits are held for a piece of the rows at a time, at most 2 GiB of them (or 256 rows), beside a copy of h, 8 bytes for every
- * 32 logits, up to 64 MiB for sums that several workgroups share (over 2^18 classes or rows: one dh or dw in fp32 for each 2^18 of
+ * 32 logits and 4 for every 16384, up to 64 MiB for sums that several workgroups share (over 2^18 classes or rows: one dh or dw in fp32 for each 2^18 of
  * them), and, for rows of more than one piece in bf16, 4 vocab d bytes.  Any pointer may be NULL. */
 ringada_status ringada_vocab_plan(const ringada_vocab_desc* desc, size_t* forward_bytes, size_t* train_bytes,
                                   size_t* next_bytes);
@@ -522,7 +522,9 @@ ringada_status ringada_vocab_plan(const ringada_vocab_desc* desc, size_t* forwar
  * A row that does not count has loss 0, lse 0 and a zero row in dh; its h and dloss are read into nothing, whatever they
  * hold.  Logits, softmax and sums are fp32.  With bf16 tensors:
  *  - the logits wait for their row's lse in fp16, as their distance to the largest of 64 or 128 (off by 2^-11 of it);
- *  - P is rounded to bf16 on its way into the products; of at most 64 rows that count, to two bf16, which leaves 2^-16 of it;
+ *  - P is rounded to bf16 on its way into the products; of at most 64 rows that count, to two bf16, whose own error is 2^-16;
+ *  - what a row of the stored P falls short of its sum, zero, is added at w[label] in fp32: its errors reach dh as
+ *    their products with w - w[label], and what all classes have in common stays out;
  *  - P is in units of the first counted row's |dloss|, where that is within 2^-40 and 2^40: entries of dloss may be up to 2^80
  *    then.
  * An infinity or NaN in a row that counts gives NaN in it, and in dw.  No output may overlap

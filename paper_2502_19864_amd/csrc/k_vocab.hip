@@ -527,7 +527,7 @@ __global__ __launch_bounds__(256) void vocab_rows_k(VocabArgs a) {
 }
 
 // Loss and lse of a row, and its P in the place of the logits, rounded once to the storage type (few rows: in two parts); zeros past V and in the rows
-// up to a multiple of 64.  A workgroup takes 16384 columns of one row and joins the row's tiles by itself.
+// up to a multiple of 64; with bf16 tensors what the stored P falls short of a sum of zero (row_left).  A workgroup takes 16384 columns of one row and joins the row's tiles by itself.
 // With bf16 tensors the logits come in fp16, as s - (the largest of their tile, which is in part): off by 2^-11 of that difference
 // at most, so P by 2^-11 (m - s) of itself.  What is large of P has s near m and keeps its digits; P a thousandth of its tile's
 // largest is off by 2^-8.2 at most, its own rounding to bf16 by 2^-8; the label's entry comes from the loss, in fp32.  Half the bytes of fp32 logits:
@@ -536,21 +536,29 @@ constexpr int P_COLS = 16384;
 template <typename T>
 __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
   __shared__ Peak red[4];
+  __shared__ float short_of[4];
   const int m = blockIdx.x, cnt = piece_rows(a), tid = threadIdx.x, first = blockIdx.y * P_COLS + tid * 8;
   const int last = min((int)(blockIdx.y + 1) * P_COLS, a.Vp);
   if (m >= ((cnt + 63) & ~63)) return;
   const long at = (long)m * a.Vp;
   T* p = static_cast<T*>(a.logits) + at;
+  float left = 0.f;  // minus the sum of what is stored
   auto store = [&](int v, const float (&x)[8]) {
     if constexpr (sizeof(T) == 2) {
       const bf16x8 hi = pack_frag(x);
       *reinterpret_cast<bf16x8*>(p + v) = hi;
+      float y[8];
+      unpack_frag(hi, y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) left -= y[e];
       if (two_parts(cnt)) {
-        float y[8];
-        unpack_frag(hi, y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] = x[e] - y[e];
-        *reinterpret_cast<bf16x8*>(p + (long)TWO_PARTS * a.Vp + v) = pack_frag(y);
+        const bf16x8 lo = pack_frag(y);
+        *reinterpret_cast<bf16x8*>(p + (long)TWO_PARTS * a.Vp + v) = lo;
+        unpack_frag(lo, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) left -= y[e];
       }
     } else {
       St<T>::st4(p, v, x);
@@ -595,6 +603,12 @@ __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
       for (int e = 0; e < 8; ++e) x[e] = v0 + e == lab ? y : x[e];
     }
     store(v0, x);
+  }
+  if constexpr (sizeof(T) == 2) {
+    left = wave_sum(left);
+    if ((tid & 63) == 0) short_of[tid >> 6] = left;
+    __syncthreads();
+    if (tid == 0) a.left[(long)m * a.left_n + blockIdx.y] = (short_of[0] + short_of[1]) + (short_of[2] + short_of[3]);
   }
 }
 
@@ -661,6 +675,8 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   if (grads) {
     a.g_c = static_cast<float*>(take((size_t)a.n * 4));
     a.logits = take((size_t)(low && a.R < 2 * TWO_PARTS ? 2 * TWO_PARTS : a.R) * a.Vp * es);
+    a.left_n = (a.Vp + P_COLS - 1) / P_COLS;
+    a.left = low ? static_cast<float*>(take((size_t)a.R * a.left_n * 4)) : nullptr;
     a.shares = static_cast<float*>(take(low ? vocab_share_bytes(a.n, a.R, a.d, a.V) : f32_share_bytes(a)));
     if (low && a.n > a.R) a.dw_acc = static_cast<float*>(take((size_t)a.V * a.d * 4));
     a.ld_acc = a.d;
@@ -737,7 +753,7 @@ static hipError_t vocab_t(VocabArgs a, hipStream_t s) {
       RG_LAUNCH(vocab_rows_k, dim3(a.rows), dim3(256), 0, s, a);
       continue;
     }
-    RG_LAUNCH(vocab_p_k<T>, dim3((unsigned)up(a.rows, 64), (a.Vp + P_COLS - 1) / P_COLS), dim3(256), 0, s, a);
+    RG_LAUNCH(vocab_p_k<T>, dim3((unsigned)up(a.rows, 64), a.left_n), dim3(256), 0, s, a);
     if constexpr (low) launch_vocab_grads_bf16(a, s);
     else vocab_grads_f32(a, s);
   }

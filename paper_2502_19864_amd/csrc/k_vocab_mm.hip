@@ -195,6 +195,13 @@ __global__ __launch_bounds__(256) void vocab_shares_k(VocabArgs a, VocabProduct 
       for (int e = 0; e < 8; ++e) v[e] += red[threadIdx.x + o][e];
   }
   if (!in) return;
+  if constexpr (E == Prod::Dh) {
+    float c[8];
+    unpack_frag(*reinterpret_cast<const bf16x8*>(p.B + (long)a.lab_c[a.row0 + m] * p.ldb + n), c);
+    const float left = row_left(a, m);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += left * c[e];
+  }
   const float unit = dloss_unit(a);
   if (E == Prod::Dw && !(a.first && a.last)) {
     add_dw(a, m, n, unit, f32x4{v[0], v[1], v[2], v[3]});

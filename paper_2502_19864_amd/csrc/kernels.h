@@ -264,6 +264,7 @@ struct VocabArgs {
   int* n_counted; int* block_count;  // block_count: of every 1024 rows, or null where rows are few
   int* idx; int* lab_c; float* g_c; float* target;  // [n], by counted row: its place, label, gradient, label's logit
   void* logits;                 // [R][Vp]: fp32, or with bf16 tensors fp16, below their tile's maximum; P takes their place
+  float* left; int left_n;      // bf16: [R][left_n], what the stored P of a row's column runs fall short of zero
   float* shares;                // tiles of dh and of dw over shares of their k
   float* dw_acc; long ld_acc;   // bf16: dw between the pieces, [V][d]
   // a piece

@@ -212,16 +212,35 @@
       for (int i = 0; i < FM; ++i) {
         const int mb = em0 + i * 32;
         if (mb >= M) continue;  // wave-uniform
+        float left = 0.f;       // dh, not in shares: of this lane's row, for its label's row of w.  Asked for where it is needed: before the
+                                // wait above it took as long, and 256 x 256 tiles have no registers for it
+        const bf16* own = nullptr;
+        if constexpr (E == Prod::Dh)
+          if (packed) {
+            const int m = min(mb + l32, M - 1);
+            left = row_left(a, m);
+            own = p.B + (long)a.lab_c[a.row0 + m] * p.ldb;
+          }
         if (packed) {
 #pragma unroll
           for (int j = 0; j < FN; j += 2) {
             const int nb = en0 + j * 32;
             if (nb >= limit) continue;
+            uint2 c[8];
+            if constexpr (E == Prod::Dh)
+#pragma unroll
+              for (int q = 0; q < 8; ++q) c[q] = *reinterpret_cast<const uint2*>(own + min(nb + 8 * q + 4 * half, N - 4));
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
               float v[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) v[e] = acc[i][j + q / 4][q % 4 * 4 + e];
+              if constexpr (E == Prod::Dh) {
+                v[0] += left * __uint_as_float(c[q].x << 16);
+                v[1] += left * __uint_as_float(c[q].x & 0xffff0000u);
+                v[2] += left * __uint_as_float(c[q].y << 16);
+                v[3] += left * __uint_as_float(c[q].y & 0xffff0000u);
+              }
               uint2 w;
               if constexpr (E == Prod::Logits) {
                 const half4 h = {(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};

@@ -1,0 +1,77 @@
+"""What the vocabulary head and its gradients leave of quantities that the formulas let cancel, and what they make of
+infinities and of batches in pieces, against float64.  head_reference.py has the roundings' sizes."""
+import math
+
+import pytest
+
+import head_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+def gen(seed):
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return lambda *shape, std=1.0, dtype=torch.float32: (torch.randn(shape, generator=g, device="cuda") * std).to(dtype)
+
+
+def near_classes(n, d, V, apart, ahead, seed=0):
+    """bf16 classes that have most of their rows in common, and labels whose logits lead the others' mean by `ahead`."""
+    import torch
+    r = gen(n + 3 * d + V + seed)
+    w = (r(1, d, std=d ** -0.5) + apart * r(V, d, std=d ** -0.5)).bfloat16()
+    labels = torch.randint(0, V, (n,), generator=torch.Generator().manual_seed(n + seed)).cuda()
+    lead = w[labels].float() - w.float().mean(0)
+    h = (r(n, d) + lead * (ahead / lead.square().sum(1, keepdim=True))).bfloat16()
+    return h, w, labels.int(), r(n, std=1.0 / n)
+
+
+def dh_apart(h, w, labels, dloss, counted):
+    """(dh, bound): an entry of P that is off by e moves dh by e (w - w[label]), as the entries of a row sum to zero.  Of what all
+    classes have in common only the fp32 sums' roundings are left: of the products (8 sqrt(V) e), of the row of P (64 entries to a
+    thread, a tree of 8, runs of 16384 columns) and of the two roundings that put w[label] in."""
+    import torch
+    V, d = w.shape
+    u = R.half_step(torch.bfloat16)
+    up = u * u if counted <= 64 else u
+    H, W, lab = h.double(), w.double(), labels.long()[:, None]
+    s, A = H @ W.T, H.abs() @ W.abs().T
+    lse = torch.logsumexp(s, 1, keepdim=True)
+    logp = s - lse
+    p = logp.exp()
+    g = dloss.double()[:, None]
+    P = g * p.scatter(1, lab, torch.expm1(logp.gather(1, lab)))
+    es = 8 * math.sqrt(d) * R.E * A
+    elog = es + (p * es).sum(1, keepdim=True) + 4 * R.E * (1 + logp.abs())
+    # a logit waits in fp16 below its tile's maximum, which is at most lse: half a step of that distance
+    eP = g.abs() * p * (elog + 2.0 ** -11 * logp.abs() + 2.0 ** -24)
+    eP = (eP + up * (P.abs() + eP) * 1.01).scatter(1, lab, 0.0)
+    dh, size, apart = P @ W, P.abs() @ W.abs(), torch.empty_like(H)
+    for i in range(len(h)):
+        apart[i] = eP[i] @ (W - W[lab[i, 0]]).abs()
+    own = W[lab[:, 0]].abs() * P.abs().sum(1, keepdim=True)
+    e = apart + 8 * math.sqrt(V) * R.E * size + (64 + 8 + V / 16384 + 4) * R.E * own + 4 * R.E * size
+    return dh, 1.01 * e + u * (dh.abs() + e) * 1.01
+
+
+@pytest.mark.parametrize("ahead", [0.0, 3.0, 9.0])
+@pytest.mark.parametrize("n,d,V,apart", [
+    (1, 64, 40, 0.1), (64, 64, 40, 0.03), (65, 64, 40, 0.1), (65, 64, 40, 0.03), (1000, 64, 40, 0.03),  # dh without shares
+    (64, 128, 3000, 0.03), (65, 128, 3000, 0.03), (300, 72, 1100, 0.1), (70, 24, 40000, 0.03), (20, 24, 40000, 0.1),  # in shares; runs of columns
+    (4100, 2304, 520, 0.03)])  # 256 rows and columns to a tile
+def test_dh_of_classes_that_differ_little(n, d, V, apart, ahead):
+    import torch
+    from paper_2502_19864_amd import operators as ops
+    h, w, labels, dloss = near_classes(n, d, V, apart, ahead)
+    loss, lse, dh, dw = ops.vocab_ce_train(h, w, labels, dloss)
+    some = torch.arange(n, device="cuda")[:: max(1, n // 64)]
+    want, bound = dh_apart(h[some], w, labels[some], dloss[some], n)
+    R.check("dh", dh[some], want, bound)
+    # the same rows among others that do not count, and in a batch of another size
+    wide = torch.full((2 * n + 3, d), math.nan, dtype=h.dtype, device="cuda")
+    lab, g = torch.full((2 * n + 3,), -1, dtype=torch.int32, device="cuda"), torch.zeros(2 * n + 3, device="cuda")
+    wide[3::2], lab[3::2], g[3::2] = h, labels, dloss
+    among = ops.vocab_ce_train(wide, w, lab, g, frozen=True)[2]
+    assert not among[:3].any() and not among[4::2].any()
+    R.check("dh", among[3::2][some], want, bound)
