@@ -571,7 +571,7 @@ __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
     return;
   }
   const Peak q = join_row(a, m, red);
-  const float log_l = logf(q.l), lse = q.m + log_l;
+  const float log_l = logf(q.l), lse = q.m + log_l;  // P does not take lse, whose rounding would be in a whole row but its label
   const float loss = (q.m - a.target[a.row0 + m]) + log_l;  // not lse - s: of a row that is sure of its label little is left
   float g = a.g_c[a.row0 + m];
   if constexpr (sizeof(T) == 2) g /= dloss_unit(a);
@@ -586,14 +586,16 @@ __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {
     float x[8];
     if constexpr (sizeof(T) == 2) {
       const half8 h = *reinterpret_cast<const half8*>(static_cast<const _Float16*>(a.logits) + at + v0);
-      const float top = a.part[(long)m * a.tiles + min(v0, a.V - 1) / a.bn].x - lse;
+      const float top = a.part[(long)m * a.tiles + min(v0, a.V - 1) / a.bn].x - q.m - log_l;
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = (float)h[e] + top;
     } else {
       const float* s = static_cast<const float*>(a.logits) + at + v0;
       const float4 lo = *reinterpret_cast<const float4*>(s), hi = *reinterpret_cast<const float4*>(s + 4);
-      x[0] = lo.x - lse; x[1] = lo.y - lse; x[2] = lo.z - lse; x[3] = lo.w - lse;
-      x[4] = hi.x - lse; x[5] = hi.y - lse; x[6] = hi.z - lse; x[7] = hi.w - lse;
+      x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w;
+      x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = x[e] - q.m - log_l;
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = v0 + e < a.V ? g * exp_below(x[e]) : 0.f;

@@ -75,3 +75,26 @@ def test_dh_of_classes_that_differ_little(n, d, V, apart, ahead):
     among = ops.vocab_ce_train(wide, w, lab, g, frozen=True)[2]
     assert not among[:3].any() and not among[4::2].any()
     R.check("dh", among[3::2][some], want, bound)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("offset", [30.0, 300.0, 3000.0])
+@pytest.mark.parametrize("n,d,V", [(5, 40, 96), (70, 40, 96), (300, 136, 200)])
+def test_what_all_logits_share_reaches_no_gradient(n, d, V, offset, dtype):
+    """One column of w is 1 and one of h large: every logit has it, and the entries of a row of P sum to zero however
+    large it is, so that column of dh vanishes."""
+    import torch
+    from paper_2502_19864_amd import operators as ops
+    t, r = torch.bfloat16 if dtype == "bf16" else torch.float32, gen(n + V)
+    h, w = r(n, d, dtype=t), r(V, d, std=2 * d ** -0.5, dtype=t)
+    h[:, d - 1], w[:, d - 1] = offset, 1.0
+    labels = torch.randint(0, V, (n,), generator=torch.Generator().manual_seed(n)).cuda()
+    dloss = r(n)
+    dh = ops.vocab_ce_train(h, w, labels.int(), dloss)[2][:, d - 1]
+    logp = torch.log_softmax(h.double() @ w.double().T, 1)
+    p, mine = logp.exp(), logp.gather(1, labels[:, None])
+    # the entries: an argument's roundings and the function's two steps, whatever the logits' own; then a sum of V products, and
+    # in bf16 the row's sum and the product that take it off
+    entries = (p * 4 * R.E * (3 + logp.abs())).sum(1) + 8 * R.E * (1 - mine[:, 0])
+    sums = (8 * math.sqrt(V) + 80) * R.E * 2
+    R.check("dh", dh, torch.zeros(n, dtype=torch.float64, device="cuda"), dloss.double().abs() * (entries + sums))
