@@ -527,13 +527,14 @@ ringada_status ringada_vocab_plan(const ringada_vocab_desc* desc, size_t* forwar
  *    their products with w - w[label], and what all classes have in common stays out;
  *  - P is in units of the first counted row's |dloss|, where that is within 2^-40 and 2^40: entries of dloss may be up to 2^80
  *    then.
- * An infinity or NaN in a row that counts gives NaN in it, and in dw.  No output may overlap
+ * An infinity or NaN in a row that counts gives NaN in it, and in dw.  A class whose logit is -infinity by an infinity in w is left
+ * out; +infinity makes the row's loss and lse NaN; either leaves NaN or infinities in that column of dh.  No output may overlap
  * anything else.  Every sum has a fixed order: the same inputs give the same bits. */
 ringada_status ringada_vocab_ce(void* stream, const ringada_vocab_desc* desc, const ringada_vocab_tensors* t,
                                 void* workspace, size_t workspace_bytes);
 
 /* The class of the largest logit of every row of h (of equal ones the lowest; NaN logits are passed over, and a row of
- * nothing else gives some class in range) and its log-probability, s[token] - lse. */
+ * nothing else gives some class in range) and its log-probability, s[token] - lse, NaN where s[token] is infinite. */
 ringada_status ringada_vocab_next(void* stream, const ringada_vocab_desc* desc, const ringada_rows* h,
                                   const ringada_rows* w, int32_t* token, float* logprob, void* workspace,
                                   size_t workspace_bytes);

@@ -276,6 +276,11 @@ __device__ __forceinline__ void dma4_m0(const void* gbase, uint32_t voff, uint32
 __device__ __forceinline__ uint32_t lds_addr(const void* p) {
   return (uint32_t)(uintptr_t)(lds_ptr_t)p;
 }
+// 16 B of zeros at an LDS address, where a lane has nothing to load
+__device__ __forceinline__ void lds_zero16(uint32_t at) {
+  typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+  *(__attribute__((address_space(3))) u32x4_t*)at = u32x4_t{0, 0, 0, 0};
+}
 
 // ---------------------------------------------------------------- XCD-aware block order
 // Workgroups are dispatched round-robin over the 8 XCDs (linear workgroup id i

@@ -211,7 +211,7 @@ __device__ __forceinline__ void f32_epilogue(const VocabArgs& a, const F32Produc
 // 128 x 128 tiles, 32 k at a time: registers -> LDS, four waves of 64 x 64, two workgroups per CU.  LDS keeps [k][row], rows of odd k
 // turned by 32 columns, so that the two k of an MFMA lie in different banks.  The loop has no branch: rows and k past the ends read
 // the last ones again.  Such rows are not stored, and such k meet zeros of A: hc and P are padded with them to whole tiles of
-// 64.  A piece of B that reaches past the end of its row is read from where it ends there, and moved (1189 x 2786, d 4070: 309
+// 64.  In the logits they are zeros of w too, as an infinity read again would make a NaN.  A piece of B that reaches past the end of its row is read from where it ends there, and moved (1189 x 2786, d 4070: 309
 // us of logits, 300 at d 4096; single loads 508).  d >= 4.
 // 4096 x 16000, d 2048: 132 TF (a tile of 16 k with guarded loads: 115; torch.mm 154).
 // PADDED: A, which has whole tiles of k
@@ -255,6 +255,11 @@ struct F32Operand {
       if (!PADDED && (!KM || left < 32)) {
         if (move & 2) v[i].x = v[i].z, v[i].y = v[i].w;
         if (move & 1) v[i].x = v[i].y, v[i].y = v[i].z, v[i].z = v[i].w;
+        if constexpr (KM) {
+          const int k = (tid >> 7) * 16 + 4 * i;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[i][e] = k + e < left ? v[i][e] : 0.f;
+        }
       }
     }
   }

@@ -9,8 +9,9 @@
 //    touches hit all banks once;
 //  * [64][rows]: read by transposing loads, four k of 32 columns at a time; the 64-byte group of the columns
 //    at its number ^ k % 4, so those four rows lie in different banks.
-// Rows past the operands' ends are clamped (their results are not stored) and k past the end meets zeros
-// in the other operand: hc and P are padded with them.
+// Rows past the operands' ends are clamped (their results are not stored).  k past the end meets zeros in A: hc and P are
+// padded with them.  In w of the logits it is zeros too, as an infinity read again there would make a NaN; where B is [k][rows] it is its
+// last row again, whose infinities have made their columns NaN already.
 #include <type_traits>
 #include <utility>
 
@@ -65,13 +66,21 @@ struct Operand {
       else off[i] = (uint32_t)r * ld2 + min(pos ^ ((r & 3) << 2), (rows - first + 7) / 8 - 1) * 16;
     }
   }
-  // instruction i of k-tile kt; left: k of this tile that the operand has (BK: all).  Past them the last ones are read again.
+  // instruction i of k-tile kt; left: k of this tile that the operand has (BK: all), past them come zeros (KMAJOR) or the last one again.
+  // Zeros are there once the wave has waited for its LDS operations, as it does for the DMA.
   __device__ __forceinline__ void dma(int i, int kt, int left, uint32_t lds, int wave, int wave_u, int lane) const {
     uint32_t o = off[i];
     if (left < BK) {
-      const int r = (i * NW + wave) * RPI + lane / CPR;
-      if constexpr (KMAJOR) o -= max(0, (lane % CPR ^ (r / SWD % CPR)) - (left / 8 - 1)) * 16;
-      else o -= max(0, r - (left - 1)) * ld2;
+      if constexpr (KMAJOR) {
+        int at = lane;
+        asm volatile("" : "+v"(at));  // worked out here, not kept over the products
+        if ((at % CPR ^ (((i * NW + wave_u) * RPI + at / CPR) / SWD % CPR)) >= left / 8) {
+          lds_zero16(lds + (i * NW + wave_u) * 1024 + at * 16);
+          return;
+        }
+      } else {
+        o -= max(0, (i * NW + wave) * RPI + lane / CPR - (left - 1)) * ld2;
+      }
     }
     dma16_m0(base + (long)kt * step, o, lds + (i * NW + wave_u) * 1024);
   }
@@ -140,7 +149,7 @@ __device__ __forceinline__ void add_dw(const VocabArgs& a, int m, int n, float u
 template <int BM, int BN, int WM, int WN>
 constexpr int MM_LDS = 2 * (BM + BN) * 64 * 2 + WM * WN * 4096;
 template <int BM, int BN, int WM, int WN, bool KA, bool KB, Prod E>
-__global__ __launch_bounds__(64 * WM * WN) void vocab_mm_k(VocabArgs a, VocabProduct p) {
+__global__ __launch_bounds__(64 * WM * WN, 2) void vocab_mm_k(VocabArgs a, VocabProduct p) {
   __shared__ __attribute__((aligned(1024))) char smem[MM_LDS<BM, BN, WM, WN>];
   auto wg = [] { return blockIdx.x; };
   auto wgs = [] { return gridDim.x; };
@@ -244,7 +253,7 @@ __global__ __launch_bounds__(512, LDSB > 65536 ? 2 : 4) void vocab_few_k(VocabAr
     const bf16* row = w + (long)min(blk * 16 + l16, a.V - 1) * a.ldw;
     const int k0 = (ks + c * KS) * KC + g4 * 8;
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) {  // past d: the row's first elements, against zeros of h
+    for (int s = 0; s < STEPS; ++s) {  // past d: the row's first elements, which mul leaves out
       const int k = k0 + s * 32;
       y[s] = __builtin_nontemporal_load(reinterpret_cast<const bf16x8*>(row + (k < a.d ? k : 0)));
     }
@@ -291,10 +300,12 @@ __global__ __launch_bounds__(512, LDSB > 65536 ? 2 : 4) void vocab_few_k(VocabAr
   };
   auto mul = [&](const bf16x8 (&y)[STEPS], int kc) {
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s)
+    for (int s = 0; s < STEPS; ++s) {
+      const bf16x8 part = kc * KC + s * 32 + g4 * 8 < a.d ? y[s] : zero_frag();
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        acc[b] = mfma16(y[s], *reinterpret_cast<const bf16x8*>(hb[b] + kc * (KC * 2) + s * 64), acc[b]);
+        acc[b] = mfma16(part, *reinterpret_cast<const bf16x8*>(hb[b] + kc * (KC * 2) + s * 64), acc[b]);
+    }
   };
   const int steps = rounds * mine;
   int done = 0, at_blk = first;  // what is multiplied

@@ -98,3 +98,36 @@ def test_what_all_logits_share_reaches_no_gradient(n, d, V, offset, dtype):
     entries = (p * 4 * R.E * (3 + logp.abs())).sum(1) + 8 * R.E * (1 - mine[:, 0])
     sums = (8 * math.sqrt(V) + 80) * R.E * 2
     R.check("dh", dh, torch.zeros(n, dtype=torch.float64, device="cuda"), dloss.double().abs() * (entries + sums))
+
+
+@pytest.mark.parametrize("dtype,n,d,V", [
+    ("bf16", 3, 1000, 40000), ("bf16", 20, 2056, 40000), ("bf16", 3, 72, 700), ("bf16", 20, 264, 700), ("bf16", 9, 512, 3000),  # few rows
+    ("bf16", 70, 200, 900), ("bf16", 100, 8, 900), ("bf16", 190, 200, 60000), ("bf16", 512, 136, 30000), ("bf16", 128, 128, 500),  # tiles of 128, 192, 256 rows
+    ("f32", 5, 33, 300), ("f32", 70, 2, 90), ("f32", 70, 133, 16400), ("f32", 1500, 6, 1502), ("f32", 100, 64, 16400)])
+def test_infinite_weights(dtype, n, d, V):
+    """An infinity in w makes the logits of its class infinite or, against the other sign of h, leaves it out; it reaches no
+    other class, whatever of its row a kernel reads past d."""
+    import torch
+    from paper_2502_19864_amd import operators as ops
+    t, r = torch.bfloat16 if dtype == "bf16" else torch.float32, gen(n + d + V)
+    h, w = r(n, d, dtype=t), r(V, d, std=d ** -0.5, dtype=t)
+    labels = torch.randint(0, V - 8, (n,), generator=torch.Generator().manual_seed(n)).cuda().int()
+    for at in sorted({0, d // 2, d - 8 if d > 8 else d - 1, d - 1}):
+        h[:, at] = -1.0
+        for k, v in enumerate((V - 1, V - 7)):
+            out, far = w.clone(), w.clone()
+            out[v, at], far[v, at] = math.inf, 2.0 ** 100
+            loss, lse = ops.vocab_ce_forward(h, out, labels)
+            want = ops.vocab_ce_forward(h, far, labels)  # exp of -2^100 is 0 too
+            assert torch.equal(loss, want[0]) and torch.equal(lse, want[1]) and torch.isfinite(loss).all()
+            assert all(torch.equal(a, b) for a, b in zip(ops.vocab_next(h, out), ops.vocab_next(h, far)))
+            if k == 0:
+                dloss = torch.full((n,), 1.0 / n, device="cuda")
+                got, want = ops.vocab_ce_train(h, out, labels, dloss), ops.vocab_ce_train(h, far, labels, dloss)
+                rest = torch.arange(d, device="cuda") != at
+                assert all(torch.equal(a, b) for a, b in zip(got[:2], want[:2]))
+                assert torch.equal(got[2][:, rest], want[2][:, rest]) and torch.equal(got[3], want[3])
+            out[v, at] = -math.inf  # against h's -1: the largest logit there is
+            token, logprob = ops.vocab_next(h, out)
+            assert (token == v).all() and torch.isnan(logprob).all()
+            assert torch.isnan(ops.vocab_ce_forward(h, out, labels)[0]).all()
