@@ -454,10 +454,11 @@ static void go(const VocabArgs& a, VocabProduct p, hipStream_t s) {
 enum class LogitsTile { T256, T192, T128 };
 static LogitsTile logits_tile(int rows, int d, int V) {
   const int k = tiles_of(d, 64);
-  auto rounds = [](int tiles, int slots) { return (tiles + slots - 1) / slots; };
-  const float t256 = rounds(tiles_of(rows, 256) * tiles_of(V, 256), 256) * (8.f + 1.7f * k);
-  const float t192 = rounds(tiles_of(rows, 192) * tiles_of(V, 256), 256) * (8.f + 1.32f * k);
-  const float t128 = rounds(tiles_of(rows, 128) * tiles_of(V, 128), 512) * (7.f + 1.05f * k);
+  // up to 2^31 tiles
+  auto rounds = [=](int bm, int bn, int slots) { return ((long)tiles_of(rows, bm) * tiles_of(V, bn) + slots - 1) / slots; };
+  const float t256 = rounds(256, 256, 256) * (8.f + 1.7f * k);
+  const float t192 = rounds(192, 256, 256) * (8.f + 1.32f * k);
+  const float t128 = rounds(128, 128, 512) * (7.f + 1.05f * k);
   return t256 <= t192 && t256 <= t128 ? LogitsTile::T256 : t192 <= t128 ? LogitsTile::T192 : LogitsTile::T128;
 }
 int vocab_mm_bn(int rows, int d, int V) { return logits_tile(rows, d, V) == LogitsTile::T256 ? 128 : 64; }  // a wave's columns
