@@ -131,3 +131,48 @@ def test_infinite_weights(dtype, n, d, V):
             token, logprob = ops.vocab_next(h, out)
             assert (token == v).all() and torch.isnan(logprob).all()
             assert torch.isnan(ops.vocab_ce_forward(h, out, labels)[0]).all()
+
+
+PIECES = [  # dtype, d, vocab, rows that are held at a time, rows that count in the next piece
+    ("bf16", 8, 300007, 3328, 0), ("bf16", 8, 300007, 3328, 1), ("bf16", 8, 300007, 3328, 64), ("bf16", 8, 300007, 3328, 65),
+    ("bf16", 264, 300007, 3328, 200), ("bf16", 8, 4096, 262144, 37001), ("bf16", 136, 4096, 262144, 63),  # 256-wide dw; dw in shares
+    ("f32", 8, 300007, 1536, 1), ("f32", 264, 300007, 1536, 200), ("f32", 72, 4096, 131072, 8900)]  # 128-wide tiles, dw in shares
+
+
+@pytest.mark.parametrize("dtype,d,V,held,after", PIECES)
+def test_pieces_of_rows(dtype, d, V, held, after):
+    """More logits than are held at a time, `after` rows that count in the second piece: dw is carried from piece to piece, and few
+    rows there are in two parts."""
+    import torch
+    from paper_2502_19864_amd import binding as B
+    from paper_2502_19864_amd import operators as ops
+    t, code, es = (torch.bfloat16, B.BF16, 2) if dtype == "bf16" else (torch.float32, B.F32, 4)
+    counted, n = held + after, held + 260 + after
+    assert held == (1 << 31) // es // ((V + 63) // 64 * 64) // 256 * 256 < n <= 2 * held  # two pieces
+    plan = lambda rows: B.ringada_vocab_plan(B.VocabDesc(code, rows, d, V))[1]
+    if dtype == "bf16":
+        assert plan(n) - plan(held) >= 4 * V * d  # dw between them
+    h, w, labels, dloss = near_classes(n, d, V, 0.3, 3.0)
+    h, w = h.to(t), w.to(t)
+    off = torch.randperm(n, generator=torch.Generator().manual_seed(d))[:n - counted].cuda()
+    labels[off], h[off] = -1, math.nan
+    loss, lse, dh, dw = ops.vocab_ce_train(h, w, labels, dloss)
+    assert not any(x[off].any() for x in (loss, lse, dh))
+    at = (labels >= 0).nonzero()[:, 0]
+    step = 16384 if V < 10000 else 1024
+    want_dw = bound_dw = 0.0
+    for piece in (at[:held], at[held:])[:1 + (after > 0)]:
+        for rows in piece.split(step):
+            assert len(rows) > 64 or len(piece) <= 64  # two parts where the piece has them
+            want = R.vocab(h[rows], w, labels[rows], dloss[rows])
+            for name, got in (("loss", loss), ("lse", lse), ("dh", dh)):
+                R.check(name, got[rows], *want[name])
+            # the sums of these rows, each within its bound, are added in fp32: a few dozen additions in a row at most, of which
+            # the bound of a sum of m products, 8 sqrt(m) e, has its share
+            want_dw = want_dw + want["dw"][0]
+            bound_dw = bound_dw + want["dw"][1] * (1 + 8 / math.sqrt(len(rows)))
+    R.check("dw", dw, want_dw, bound_dw)
+    if dtype == "bf16":
+        for rows, m in ((at[:held:held // 5], held), (at[held::13], after)):
+            if len(rows):
+                R.check("dh", dh[rows], *dh_apart(h[rows], w, labels[rows], dloss[rows], m))
