@@ -176,3 +176,61 @@ def test_pieces_of_rows(dtype, d, V, held, after):
         for rows, m in ((at[:held:held // 5], held), (at[held::13], after)):
             if len(rows):
                 R.check("dh", dh[rows], *dh_apart(h[rows], w, labels[rows], dloss[rows], m))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_decoding_keeps_to_the_whole_sequence(dtype):
+    """Token by token against a cache and the whole sequence at once, within what their roundings leave; a step whose newest
+    key is missing is told apart by that.
+
+    Seven tensors lie between the embedding and the logits (norm, projection, rotary, attention, projection, sum, norm), so
+    two paths differ by up to 14 independent roundings, each of 0.0017 (bf16; fp32: 8 half steps, as a product's sum has more
+    of them) of an element in the mean square.  A logit takes them by its terms' root of squares; six times that is not
+    reached in some 10^5 logits."""
+    import torch
+    from test_gpu_head_operators import block_and_head, dt
+
+    from paper_2502_19864_amd import operators as ops
+    B, S, d, H, Hkv, dh, V = 3, 24, 128, 4, 2, 64, 900
+    p, ids = block_and_head(dtype, B, S, d, H, Hkv, dh, V, 5)
+    ids = ids.clamp(min=0)[:, :S]
+    w = gen(7)(V, d, std=0.5, dtype=dt(dtype))  # not the embedding, under which every input is its own next token, surely
+    freq = ops.rotary_frequencies((dh // 2,), device="cuda")
+    cache = torch.zeros(2, B, S, Hkv, dh, dtype=dt(dtype), device="cuda")
+    pos = torch.arange(S, dtype=torch.int32, device="cuda").expand(B, S).contiguous()
+    each = 0.0017 if dtype == "bf16" else 8 * R.E
+
+    def project(x, at, **out):
+        n, _, _ = ops.norm_forward(x, p["g1"], rms=True, with_stats=False)
+        qkv = (n.reshape(-1, d) @ p["wqkv"]).view(B, -1, H + 2 * Hkv, dh)
+        q, k = ops.rotary(qkv[:, :, :H], qkv[:, :, H:H + Hkv], positions=at, freq=freq, **out)
+        return q, k, qkv[:, :, H + Hkv:]
+
+    def finish(x, o):
+        a = (o.reshape(-1, H * dh) @ p["wo"]).view(x.shape)
+        return ops.norm_forward(a, p["g2"], rms=True, res=x, with_stats=False)[0]
+    q, k, v = project(p["emb"][ids], pos)
+    whole = finish(p["emb"][ids], ops.attention_forward(q, k, v, causal=True)[0])
+    token, logprob = ops.vocab_next(whole, w)
+    sure, off = 0, 0
+    for t in range(S):
+        x = p["emb"][ids[:, t:t + 1]]
+        q, _, v = project(x, pos[:, t:t + 1].contiguous(), out_k=cache[0][:, t:t + 1])
+        cache[1][:, t:t + 1] = v
+
+        def step(keys):
+            lens = torch.full((B,), keys, dtype=torch.int32, device="cuda")
+            return ops.vocab_next(finish(x, ops.attention_forward(q, cache[0], cache[1], causal=True, len_k=lens)[0])[:, 0], w)
+        terms = whole[:, t].double().square() @ w.double().square().T
+        tol = 6 * math.sqrt(14) * each * terms.amax(1).sqrt()
+        tok, lp = step(t + 1)
+        assert ((lp - logprob[:, t]).abs() <= tol).all()
+        best = (whole[:, t].double() @ w.double().T).topk(2, 1).values
+        clear = best[:, 0] - best[:, 1] > 2 * tol
+        assert torch.equal(tok[clear], token[:, t][clear])
+        sure += int(clear.sum())
+        if t:
+            tok, lp = step(t)
+            off += int(((lp - logprob[:, t]).abs() > tol).sum())
+    assert sure >= B * S // 2
+    assert off >= B * S // 4
