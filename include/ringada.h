@@ -511,9 +511,10 @@ typedef struct {
 } ringada_vocab_tensors;
 
 /* Host only.  Bytes of the workspaces of ringada_vocab_ce without and with gradients, and of ringada_vocab_next.
- * The logits are held for a piece of the rows at a time, at most 2 GiB of them (or 256 rows), beside a copy of h, 8 bytes for every
- * 32 logits and 4 for every 16384, up to 64 MiB for sums that several workgroups share (over 2^18 classes or rows: one dh or dw in fp32 for each 2^18 of
- * them), and, for rows of more than one piece in bf16, 4 vocab d bytes.  Any pointer may be NULL. */
+ * The logits are held for a piece of the rows at a time, at most 2 GiB of them (or 256 rows), beside a copy of h, 8 bytes (ringada_vocab_next: 12)
+ * for every 32 logits and 4 for every 16384, up to 64 MiB for sums that several workgroups share (over 2^18 classes or rows: one dh or dw in fp32 for each 2^18 of
+ * them), and, for rows of more than one piece in bf16, 4 vocab d bytes.  Up to 32 rows of bf16 without gradients whose h fits the LDS (15 at
+ * d 4096, 7 at 8192, 3 at 16384) take 4 KiB a row (ringada_vocab_next: 6) and no copy.  Any pointer may be NULL. */
 ringada_status ringada_vocab_plan(const ringada_vocab_desc* desc, size_t* forward_bytes, size_t* train_bytes,
                                   size_t* next_bytes);
 

@@ -10,8 +10,8 @@
 // position in seven) and whatever stands in the others reaches nothing.  The number is
 // known on the device only: grids are sized for all rows, and tiles past it end at once.
 //
-// The logits of a piece of the rows are held in fp32 while they are needed.  Pieces of the vocabulary would need
-// no more memory, but lse needs all columns before P has any: the product h w^T would run twice, 8 n V d
+// The logits of a piece of the rows are held while they are needed, in fp32 or, with bf16 tensors, in fp16 below their
+// tile's maximum.  Pieces of the vocabulary would need no more memory, but lse needs all columns before P has any: the product h w^T would run twice, 8 n V d
 // operations instead of 6.
 #include <type_traits>
 
@@ -661,6 +661,7 @@ size_t vocab_layout(int dtype, VocabArgs& a, bool grads, bool next, void* ws) {
   const long most = grads ? (low ? 1l << 30 : 1l << 29) / a.Vp : (1l << 24) / a.tiles;
   a.R = (int)(np <= most ? np : most / 256 * 256 > 256 ? most / 256 * 256 : 256);
   if (a.R > np) a.R = (int)np;
+  if (a.few) a.R = a.n;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     void* p = ws ? static_cast<char*>(ws) + at : nullptr;
