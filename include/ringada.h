@@ -482,7 +482,9 @@ typedef struct {
  * dimensions from 2 P on are copied.  Axis 0 has the first section[0] pairs, axis 1 the next, and so on.
  * positions: int32 [n_axes, batch, rows], any values; freq: double [P]; both device.  Angles are formed in 64 bits, the
  * rotation in fp32 with one rounding.  q_out may be q and k_out may be k (the same data and
- * strides); any other overlap of an output is refused.  k and k_out are NULL when n_kv_heads is 0. */
+ * strides); any other overlap of an output is refused.  k and k_out are NULL when n_kv_heads is 0.  Pairs and d_head that
+ * are multiples of 8 (f32: of 4), with 16-byte aligned data and strides, go 16 bytes at a time, others one element: six times
+ * slower and more. */
 ringada_status ringada_rotary(void* stream, const ringada_rotary_desc* desc, const ringada_view* q,
                               const ringada_view* k, const int32_t* positions, const double* freq,
                               const ringada_view* q_out, const ringada_view* k_out);
@@ -523,13 +525,13 @@ ringada_status ringada_vocab_plan(const ringada_vocab_desc* desc, size_t* forwar
  * A row that does not count has loss 0, lse 0 and a zero row in dh; its h and dloss are read into nothing, whatever they
  * hold.  Logits, softmax and sums are fp32.  With bf16 tensors:
  *  - the logits wait for their row's lse in fp16, as their distance to the largest of 64 or 128 (off by 2^-11 of it);
- *  - P is rounded to bf16 on its way into the products; of at most 64 rows that count, to two bf16, whose own error is 2^-16;
+ *  - P is rounded to bf16 on its way into the products; of at most 64 rows that count in a piece, to two bf16, whose own error is 2^-16;
  *  - what a row of the stored P falls short of its sum, zero, is added at w[label] in fp32: its errors reach dh as
  *    their products with w - w[label], and what all classes have in common stays out;
  *  - P is in units of the first counted row's |dloss|, where that is within 2^-40 and 2^40: entries of dloss may be up to 2^80
  *    then.
  * An infinity or NaN in a row that counts gives NaN in it, and in dw.  A class whose logit is -infinity by an infinity in w is left
- * out; +infinity makes the row's loss and lse NaN; either leaves NaN or infinities in that column of dh.  No output may overlap
+ * out; +infinity makes the row NaN, and dw; either leaves NaN or infinities in that column of dh.  No output may overlap
  * anything else.  Every sum has a fixed order: the same inputs give the same bits. */
 ringada_status ringada_vocab_ce(void* stream, const ringada_vocab_desc* desc, const ringada_vocab_tensors* t,
                                 void* workspace, size_t workspace_bytes);

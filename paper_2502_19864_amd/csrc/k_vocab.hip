@@ -211,8 +211,8 @@ __device__ __forceinline__ void f32_epilogue(const VocabArgs& a, const F32Produc
 // 128 x 128 tiles, 32 k at a time: registers -> LDS, four waves of 64 x 64, two workgroups per CU.  LDS keeps [k][row], rows of odd k
 // turned by 32 columns, so that the two k of an MFMA lie in different banks.  The loop has no branch: rows and k past the ends read
 // the last ones again.  Such rows are not stored, and such k meet zeros of A: hc and P are padded with them to whole tiles of
-// 64.  In the logits they are zeros of w too, as an infinity read again would make a NaN.  A piece of B that reaches past the end of its row is read from where it ends there, and moved (1189 x 2786, d 4070: 309
-// us of logits, 300 at d 4096; single loads 508).  d >= 4.
+// 64.  In the logits they are zeros of w too, as an infinity read again would make a NaN.  A piece of B that reaches past the end
+// of its row is read from where it ends there, and moved (1189 x 2786, d 4070: 309 us of logits, 300 at d 4096; single loads 508).  d >= 4.
 // 4096 x 16000, d 2048: 132 TF (a tile of 16 k with guarded loads: 115; torch.mm 154).
 // PADDED: A, which has whole tiles of k
 template <bool KM, bool PADDED>
@@ -536,7 +536,7 @@ __global__ __launch_bounds__(256) void vocab_rows_k(VocabArgs a) {
 // With bf16 tensors the logits come in fp16, as s - (the largest of their tile, which is in part): off by 2^-11 of that difference
 // at most, so P by 2^-11 (m - s) of itself.  What is large of P has s near m and keeps its digits; P a thousandth of its tile's
 // largest is off by 2^-8.2 at most, its own rounding to bf16 by 2^-8; the label's entry comes from the loss, in fp32.  Half the bytes of fp32 logits:
-// 2048 x 32000 take 50 to 54 us here instead of 78, and 16 less to store.
+// 2048 x 32000 took 50 to 54 us here instead of 78 (53 to 58 with the sums of what is stored), and 16 less to store.
 constexpr int P_COLS = 16384;
 template <typename T>
 __global__ __launch_bounds__(256) void vocab_p_k(VocabArgs a) {

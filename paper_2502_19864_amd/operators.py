@@ -88,7 +88,7 @@ def _pack(how, *values):
     try:
         return how.pack(*values)
     except struct.error as e:
-        raise ValueError(f"window, sinks and scale are numbers in range: {e}") from None
+        raise ValueError(f"window, sinks, scale, eps and sections are numbers in range: {e}") from None
 
 
 def _attn(q, k, v, o, lse, causal, window, sinks, scale, len_q, len_k, table, bucket):
