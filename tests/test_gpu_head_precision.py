@@ -55,7 +55,7 @@ def dh_apart(h, w, labels, dloss, counted):
     return dh, 1.01 * e + u * (dh.abs() + e) * 1.01
 
 
-@pytest.mark.parametrize("ahead", [0.0, 3.0, 9.0])
+@pytest.mark.parametrize("ahead", [0.0, 3.0, 9.0, 20.0])
 @pytest.mark.parametrize("n,d,V,apart", [
     (1, 64, 40, 0.1), (64, 64, 40, 0.03), (65, 64, 40, 0.1), (65, 64, 40, 0.03), (1000, 64, 40, 0.03),  # dh without shares
     (64, 128, 3000, 0.03), (65, 128, 3000, 0.03), (300, 72, 1100, 0.1), (70, 24, 40000, 0.03), (20, 24, 40000, 0.1),  # in shares; runs of columns
